@@ -260,6 +260,8 @@ def prepare(case, seed):
         if kind == "append":
             return st
         st["cache"].append(x["k"], x["v"], 0)
+        if kind == "track":
+            st["scores"] = torch.nn.functional.pad(x["scores"], (0, t_cap // BLOCK - nb))
         if kind == "evict":
             st["cache"].scores[:, :, :nb] = x["scores"]
             st["into"] = dq.Q8KVCache(B, H, Hq, -(-case["keep"] // 128) * 128, fmt, scores=True)
@@ -311,7 +313,8 @@ def run(state):
         return c.attend(state["q"], state["lens"], window=case["window"], sinks=case["sinks"])
     if kind == "track":
         scores = state["scores"].clone()          # this branch's own scores
-        return {"out": c.attend(state["q"], state["lens"], scores=scores), "scores": scores}
+        out = c.attend(state["q"], state["lens"], scores=scores)
+        return {"out": out, "scores": scores[:, :, :-(-T // BLOCK)]}
     to = state["into"]
     kept, lens = c.evict(state["lens"], case["keep"], case["sinks"], case["recent"], into=to)
     nb = -(-T // BLOCK)
