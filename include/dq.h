@@ -437,6 +437,154 @@ int dq_bf16_decode_attention_partial(const uint16_t* q, int32_t batch, int32_t q
                                      size_t workspace_bytes, void* stream);
 
 /*
+ * The 8-bit cache: between the records and the raw BF16 window, for layers or
+ * requests that want the shortest step at half the bytes of BF16.  A block is
+ * DQ_Q8_BLOCK = 32 consecutive tokens of one (sequence, KV head): the codes of
+ * its keys and of its values (head_dim 128) and one fp32 scale for each.
+ *   format: DQ_Q8_INT8 (codes -127..127, Q = 127) or DQ_Q8_E4M3 (OCP 8-bit
+ *           floating point, 4 exponent and 3 mantissa bits, Q = 448)
+ *   scale = fl32(max |x| / Q) over the block, code = x / scale rounded to the
+ *   type's nearest value (of the exact quotient, ties to even), x^ = scale code.
+ * A block whose largest magnitude is below 2^-96 is stored as zeros with scale
+ * 0.  Infinities and NaN are stored as zeros and set DQ_STATUS_RANGE.
+ *   k_data, v_data:   u8 [batch][kv_heads][t_cap / 32][4096], 16-byte aligned
+ *   k_scale, v_scale: fp32 [batch][kv_heads][t_cap / 32]
+ * The order of the 4096 codes within a block is the order in which the matrix
+ * cores take them; dq_q8_decode_kv reads tokens back.  In pool pages (the paged
+ * layout above) the same arrays are [num_pages][kv_heads][page_tokens / 32][..].
+ * t_cap is a positive multiple of 128; batch and kv_heads are at most 65535.
+ *
+ * dq_q8_encode_kv: appends tokens [t0, t0 + n_new) of bf16 keys and values
+ *   [batch][tokens][kv_heads][128] at element strides (channels contiguous), in
+ *   one launch.  t0 is a multiple of 32; a last block that n_new does not fill
+ *   is completed with zeros, so the next append starts at its first token (the
+ *   residual window holds the tokens of a block that is not full yet).
+ * dq_q8_decode_kv: the values of tokens [t0, t0 + n), t0 a multiple of 32, as
+ *   bf16 (scale code, rounded once to fp32 and once to bf16) to
+ *   [batch][n][kv_heads][128] at element strides.  Nothing else is written.
+ */
+#define DQ_Q8_BLOCK 32
+#define DQ_Q8_INT8 0
+#define DQ_Q8_E4M3 1
+int dq_q8_encode_kv(int32_t format, const uint16_t* k, int64_t k_stride_b, int64_t k_stride_t, int64_t k_stride_h,
+                    const uint16_t* v, int64_t v_stride_b, int64_t v_stride_t, int64_t v_stride_h, int32_t batch,
+                    int32_t kv_heads, int32_t t0, int32_t n_new, int32_t t_cap, uint8_t* k_data, float* k_scale,
+                    uint8_t* v_data, float* v_scale, uint32_t* status, void* stream);
+int dq_q8_encode_kv_paged(int32_t format, const uint16_t* k, int64_t k_stride_b, int64_t k_stride_t,
+                          int64_t k_stride_h, const uint16_t* v, int64_t v_stride_b, int64_t v_stride_t,
+                          int64_t v_stride_h, int32_t batch, int32_t kv_heads, int32_t t0, int32_t n_new,
+                          const int32_t* block_table, int32_t max_pages, int32_t page_tokens, int32_t num_pages,
+                          uint8_t* k_pool, float* k_scale_pool, uint8_t* v_pool, float* v_scale_pool,
+                          uint32_t* status, void* stream);
+int dq_q8_decode_kv(int32_t format, const uint8_t* k_data, const float* k_scale, const uint8_t* v_data,
+                    const float* v_scale, int32_t batch, int32_t kv_heads, int32_t t0, int32_t n, int32_t t_cap,
+                    uint16_t* k, int64_t k_stride_b, int64_t k_stride_t, int64_t k_stride_h, uint16_t* v,
+                    int64_t v_stride_b, int64_t v_stride_t, int64_t v_stride_h, void* stream);
+int dq_q8_decode_kv_paged(int32_t format, const uint8_t* k_pool, const float* k_scale_pool, const uint8_t* v_pool,
+                          const float* v_scale_pool, int32_t batch, int32_t kv_heads, int32_t t0, int32_t n,
+                          const int32_t* block_table, int32_t max_pages, int32_t page_tokens, int32_t num_pages,
+                          uint16_t* k, int64_t k_stride_b, int64_t k_stride_t, int64_t k_stride_h, uint16_t* v,
+                          int64_t v_stride_b, int64_t v_stride_t, int64_t v_stride_h, uint32_t* status,
+                          void* stream);
+
+/*
+ * One decode step of attention over the 8-bit cache: logits softmax_scale *
+ * q . k^, output sum a v^, as dq_decode_attention over records.
+ *   q:  bf16 [batch][q_heads][128];  out: fp32 [batch][q_heads][128]
+ *   seq_lens: device int32 [batch], tokens in the cache (each in [0, t_cap])
+ *   window, sinks: window = 0: every token is visible (sinks has to be 0).
+ *       window > 0: token t is visible if it is among the first `sinks` or
+ *       among the newest `window` of the sequence; only the blocks that hold
+ *       such tokens are read.
+ *   extra_lens: device int32 [batch] or NULL: tokens of each sequence that
+ *       follow the cached ones (a residual window's); the newest `window`
+ *       tokens are counted back from their end.  The residual window itself is
+ *       always attended to whole, so with it window should be at least r_cap.
+ *   block_lse: fp32 [batch][kv_heads][t_cap / 32][q_heads / kv_heads] or NULL:
+ *       receives the base-2 logarithm of each visible block's sum of
+ *       exponentials, for dq_q8_add_scores.  Other entries are left alone.
+ *   workspace: dq_decode_workspace_bytes(...) bytes
+ * A sequence with no visible token gives zeros; a query head with an infinity
+ * or NaN gives NaN.
+ * dq_q8_decode_attention_partial writes split-K partials into the workspace;
+ * finish it with dq_decode_attention_merge, with dq_decode_attention_residual
+ * and dq_decode_attention_merge, or with dq_decode_attention_merge_residual.
+ * dq_q8_decode_attention is the partial, the merge and, where scores is not
+ * NULL (block_lse is then required), dq_q8_add_scores in one call.
+ * Through a block table the step is the same; an entry outside the pool sets
+ * DQ_STATUS_PAGE and page 0 is read in its place.
+ * q_heads / kv_heads is at most 8.  Returns DQ_OK, DQ_ERR_INVALID_ARG,
+ * DQ_ERR_WORKSPACE or DQ_ERR_HIP.
+ *
+ * dq_q8_add_scores: scores[b][h][j] (fp32 [batch][kv_heads][t_cap / 32]) grows
+ * by the attention weight of block j in the step whose partials (of the cached
+ * tokens and, if dq_decode_attention_residual ran, of the raw ones) are in the
+ * workspace, summed over its tokens and the query heads of KV head h.  The
+ * arguments are those of the step.
+ */
+int dq_q8_decode_attention_partial(int32_t format, const uint16_t* q, int32_t batch, int32_t q_heads,
+                                   int32_t kv_heads, const uint8_t* k_data, const float* k_scale,
+                                   const uint8_t* v_data, const float* v_scale, const int32_t* seq_lens,
+                                   const int32_t* extra_lens, int32_t t_cap, int32_t window, int32_t sinks,
+                                   float softmax_scale, float* block_lse, void* workspace, size_t workspace_bytes,
+                                   void* stream);
+int dq_q8_decode_attention(int32_t format, const uint16_t* q, int32_t batch, int32_t q_heads, int32_t kv_heads,
+                           const uint8_t* k_data, const float* k_scale, const uint8_t* v_data, const float* v_scale,
+                           const int32_t* seq_lens, int32_t t_cap, int32_t window, int32_t sinks,
+                           float softmax_scale, float* out, float* block_lse, float* scores, void* workspace,
+                           size_t workspace_bytes, void* stream);
+int dq_q8_decode_attention_paged_partial(int32_t format, const uint16_t* q, int32_t batch, int32_t q_heads,
+                                         int32_t kv_heads, const uint8_t* k_pool, const float* k_scale_pool,
+                                         const uint8_t* v_pool, const float* v_scale_pool,
+                                         const int32_t* block_table, int32_t max_pages, int32_t page_tokens,
+                                         int32_t num_pages, const int32_t* seq_lens, const int32_t* extra_lens,
+                                         int32_t window, int32_t sinks, float softmax_scale, float* block_lse,
+                                         void* workspace, size_t workspace_bytes, uint32_t* status, void* stream);
+int dq_q8_decode_attention_paged(int32_t format, const uint16_t* q, int32_t batch, int32_t q_heads,
+                                 int32_t kv_heads, const uint8_t* k_pool, const float* k_scale_pool,
+                                 const uint8_t* v_pool, const float* v_scale_pool, const int32_t* block_table,
+                                 int32_t max_pages, int32_t page_tokens, int32_t num_pages,
+                                 const int32_t* seq_lens, int32_t window, int32_t sinks, float softmax_scale,
+                                 float* out, float* block_lse, float* scores, void* workspace,
+                                 size_t workspace_bytes, uint32_t* status, void* stream);
+int dq_q8_add_scores(int32_t batch, int32_t q_heads, int32_t kv_heads, const int32_t* seq_lens,
+                     const int32_t* extra_lens, int32_t t_cap, int32_t window, int32_t sinks,
+                     const float* block_lse, const void* workspace, size_t workspace_bytes, float* scores,
+                     void* stream);
+
+/*
+ * Eviction by accumulated attention weight.  Every (sequence, KV head) that
+ * holds more than keep / 32 blocks keeps its first `first` and its newest
+ * `last` tokens' blocks and, of the others, those with the largest scores (of
+ * equal ones the lower block; NaN counts as the smallest): keep / 32 blocks in
+ * all, in their order.  Codes, scales and scores move to their new places
+ * unchanged; shorter sequences keep everything.
+ *   keep, first, last: tokens, multiples of 32; first >= 0, last >= 32 (the
+ *       newest block may be partly filled and stays the newest), first + last
+ *       <= keep <= to_cap
+ *   kept: int32 [batch][kv_heads][keep / 32]: the old index of each kept block,
+ *       -1 behind the last
+ *   new_lens: device int32 [batch], may be seq_lens: the new lengths,
+ *       seq_lens[b] - 32 (blocks evicted)
+ *   to_*: the cache that receives the kept blocks: either the same arrays (in
+ *       place; to_cap = t_cap) or others, of to_cap tokens, that do not overlap
+ *       them.  Scores behind the kept ones, up to the old block count, become 0.
+ * In pool pages the eviction is in place; pages behind the new length are free
+ * for the caller.  An entry outside the pool sets DQ_STATUS_PAGE and nothing
+ * is written through it.
+ * Returns DQ_OK, DQ_ERR_INVALID_ARG or DQ_ERR_HIP.
+ */
+int dq_q8_evict(int32_t batch, int32_t kv_heads, const int32_t* seq_lens, int32_t* new_lens, int32_t t_cap,
+                int32_t to_cap, int32_t keep, int32_t first, int32_t last, uint8_t* k_data, float* k_scale,
+                uint8_t* v_data, float* v_scale, float* scores, uint8_t* to_k_data, float* to_k_scale,
+                uint8_t* to_v_data, float* to_v_scale, float* to_scores, int32_t* kept, void* stream);
+int dq_q8_evict_paged(int32_t batch, int32_t kv_heads, const int32_t* seq_lens, int32_t* new_lens, int32_t keep,
+                      int32_t first, int32_t last, const int32_t* block_table, int32_t max_pages,
+                      int32_t page_tokens, int32_t num_pages, uint8_t* k_pool, float* k_scale_pool,
+                      uint8_t* v_pool, float* v_scale_pool, float* scores, int32_t* kept, uint32_t* status,
+                      void* stream);
+
+/*
  * rANS-decodes records back to symbols (Alg. 2), for parity checks.
  *   records: u8 [n_streams][C]; sym: u8 [n_streams][head_dim];
  *   header:  u16 [n_streams][2] = (scale, offset) fp16 bits; may be NULL;

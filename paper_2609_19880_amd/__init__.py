@@ -13,7 +13,10 @@ Entry points (same names as the C ABI in ``include/dq.h``):
     dq_bf16_decode_attention_partial, dq_encode_kv_paged,
     dq_decode_attention_paged_partial, dq_token_record_stride, dq_encode_kv_token,
     dq_decode_attention_token_partial, dq_fixed_bits, dq_encode_kv_fixed,
-    dq_decode_attention_fixed_partial, dq_decode_symbols, dq_strerror, dq_last_error
+    dq_decode_attention_fixed_partial, dq_q8_encode_kv, dq_q8_encode_kv_paged, dq_q8_decode_kv,
+    dq_q8_decode_kv_paged, dq_q8_decode_attention, dq_q8_decode_attention_partial,
+    dq_q8_decode_attention_paged, dq_q8_decode_attention_paged_partial, dq_q8_add_scores, dq_q8_evict,
+    dq_q8_evict_paged, dq_decode_symbols, dq_strerror, dq_last_error
 """
 
 from ._lib import (  # noqa: F401
@@ -29,6 +32,10 @@ from ._lib import (  # noqa: F401
     dq_token_record_stride, token_records_shape, dq_encode_kv_token, dq_decode_attention_token_partial,
     token_pool_shape, dq_encode_kv_token_paged, dq_decode_attention_token_paged_partial,
     dq_fixed_bits, dq_encode_kv_fixed, dq_decode_attention_fixed_partial,
+    DQ_Q8_BLOCK, DQ_Q8_INT8, DQ_Q8_E4M3, dq_q8_encode_kv, dq_q8_encode_kv_paged, dq_q8_decode_kv,
+    dq_q8_decode_kv_paged, dq_q8_decode_attention, dq_q8_decode_attention_partial,
+    dq_q8_decode_attention_paged, dq_q8_decode_attention_paged_partial, dq_q8_add_scores, dq_q8_evict,
+    dq_q8_evict_paged,
     dq_decode_symbols, dq_strerror, dq_last_error, smallest_feasible_alpha,
 )
-from .cache import KVCache, StreamingKVCache, TokenKVCache  # noqa: F401
+from .cache import KVCache, Q8KVCache, StreamingKVCache, TokenKVCache  # noqa: F401

@@ -115,6 +115,24 @@ def _load():
     lib.dq_decode_attention_fixed_partial.restype = ctypes.c_int
     lib.dq_bf16_decode_attention_partial.argtypes = [P, I32, I32, I32, P, P, P, I32, ctypes.c_float, P, SZ, P]
     lib.dq_bf16_decode_attention_partial.restype = ctypes.c_int
+    F = ctypes.c_float
+    rows, span, pages = [P, I64, I64, I64], [I32, I32, I32, I32], [P, I32, I32, I32]
+    lib.dq_q8_encode_kv.argtypes = [I32, *rows, *rows, *span, I32, P, P, P, P, P, P]
+    lib.dq_q8_encode_kv_paged.argtypes = [I32, *rows, *rows, *span, *pages, P, P, P, P, P, P]
+    lib.dq_q8_decode_kv.argtypes = [I32, P, P, P, P, *span, I32, *rows, *rows, P]
+    lib.dq_q8_decode_kv_paged.argtypes = [I32, P, P, P, P, *span, *pages, *rows, *rows, P, P]
+    step = [I32, P, I32, I32, I32, P, P, P, P]
+    lib.dq_q8_decode_attention_partial.argtypes = [*step, P, P, I32, I32, I32, F, P, P, SZ, P]
+    lib.dq_q8_decode_attention.argtypes = [*step, P, I32, I32, I32, F, P, P, P, P, SZ, P]
+    lib.dq_q8_decode_attention_paged_partial.argtypes = [*step, *pages, P, P, I32, I32, F, P, P, SZ, P, P]
+    lib.dq_q8_decode_attention_paged.argtypes = [*step, *pages, P, I32, I32, F, P, P, P, P, SZ, P, P]
+    lib.dq_q8_add_scores.argtypes = [I32, I32, I32, P, P, I32, I32, I32, P, P, SZ, P, P]
+    lib.dq_q8_evict.argtypes = [I32, I32, P, P, I32, I32, I32, I32, I32, P, P, P, P, P, P, P, P, P, P, P, P]
+    lib.dq_q8_evict_paged.argtypes = [I32, I32, P, P, I32, I32, I32, *pages, P, P, P, P, P, P, P, P]
+    for name in ("encode_kv", "encode_kv_paged", "decode_kv", "decode_kv_paged", "decode_attention_partial",
+                 "decode_attention", "decode_attention_paged_partial", "decode_attention_paged", "add_scores",
+                 "evict", "evict_paged"):
+        getattr(lib, "dq_q8_" + name).restype = ctypes.c_int
     lib.dq_residual_append.argtypes = [P, P, I32, I32, I32, P, P, P, P, I32, P, P]
     lib.dq_residual_append.restype = ctypes.c_int
     lib.dq_residual_commit.argtypes = [P, P, I32, I32, P, P]
@@ -649,6 +667,318 @@ def dq_decode_attention(k_tables: Tables, v_tables: Tables, q, k_records, k_mean
                                   _ptr(seq_lens), t_cap, ctypes.c_float(scale), _ptr(out),
                                   _ptr(workspace), ws_bytes, _ptr(status), _stream(stream))
     _check(rc, "dq_decode_attention")
+
+
+# ------------------------------------------------------------- 8-bit cache
+
+DQ_Q8_BLOCK = 32
+DQ_Q8_INT8 = 0
+DQ_Q8_E4M3 = 1
+Q8_FORMATS = {"int8": DQ_Q8_INT8, "e4m3": DQ_Q8_E4M3}
+_Q8_BYTES = DQ_Q8_BLOCK * 128
+_INT_MAX = 0x7FFFFFFF
+
+
+def _q8_format(fmt) -> int:
+    f = Q8_FORMATS.get(fmt, fmt)
+    _need(f in (DQ_Q8_INT8, DQ_Q8_E4M3), "format must be 'int8' or 'e4m3'")
+    return f
+
+
+def _q8_here(t):
+    """The raw stream to enqueue on: the current one of the current device,
+    which has to be the tensors' own."""
+    dev = t.get_device()
+    _need(dev == torch.cuda.current_device(), "tensors must be on the current device")
+    return torch._C._cuda_getCurrentRawStream(dev)
+
+
+def _q8_stream(t, stream):
+    here = _q8_here(t)
+    return here if stream is None else int(stream.cuda_stream)
+
+
+def _q8_cache_args(k_data, k_scale, v_data, v_scale):
+    """Shape (rows, heads, blocks) of a cache's or pool's four arrays."""
+    shape = k_scale.shape
+    _need(k_data.dtype == torch.uint8 and k_data.is_contiguous() and k_data.dim() == 4
+          and k_data.shape[:3] == shape and k_data.shape[3] == _Q8_BYTES, "k_data must be uint8 [.., H, blocks, 4096]")
+    _need(v_data.dtype == torch.uint8 and v_data.is_contiguous() and v_data.shape == k_data.shape,
+          "v_data must match k_data")
+    _need(k_scale.dtype == torch.float32 and k_scale.is_contiguous() and v_scale.dtype == torch.float32
+          and v_scale.is_contiguous() and v_scale.shape == shape, "scales must be fp32 [.., H, blocks]")
+    dev = k_data.device
+    _need(dev.type == "cuda" and v_data.device == dev and k_scale.device == dev and v_scale.device == dev,
+          "the cache must be on one GPU")
+    return shape
+
+
+def _q8_rows_args(k, v, heads, dev):
+    for t, name in ((k, "k"), (v, "v")):
+        _need(t.dtype == torch.bfloat16 and t.dim() == 4 and t.shape[3] == 128 and t.stride(3) == 1
+              and t.shape[2] == heads and t.device == dev, name + " must be bf16 [B, T, H, 128] on the cache's GPU")
+    _need(v.shape[:2] == k.shape[:2], "k and v must have the same tokens")
+    return k.shape[0], k.shape[1]
+
+
+def _q8_status(status, dev):
+    _need(status is None or (status.device == dev and status.element_size() == 4), "status must be a device word")
+    return 0 if status is None else status.data_ptr()
+
+
+def _q8_table(block_table, batch, dev):
+    _need(block_table.dtype == torch.int32 and block_table.is_contiguous() and block_table.dim() == 2
+          and block_table.shape[0] == batch and block_table.device == dev,
+          "block_table must be int32 [batch, max_pages] on the cache's GPU")
+    return block_table.shape[1]
+
+
+def _q8_lens(t, batch, dev, name="seq_lens"):
+    _need(t.dtype == torch.int32 and t.is_contiguous() and t.numel() == batch and t.device == dev,
+          name + " must be int32 [batch] on the cache's GPU")
+    return t.data_ptr()
+
+
+def dq_q8_encode_kv(fmt, k, v, t0: int, k_data, k_scale, v_data, v_scale, status=None, stream=None):
+    """Append k, v (bf16 [B, T_new, H, 128], any strides but channels) at cache
+    position t0, a multiple of 32.  k_data, v_data uint8 [B, H, t_cap/32, 4096];
+    k_scale, v_scale fp32 [B, H, t_cap/32]."""
+    f = _q8_format(fmt)
+    B, H, nb = _q8_cache_args(k_data, k_scale, v_data, v_scale)
+    n, T = _q8_rows_args(k, v, H, k_data.device)
+    _need(n == B, "k and the cache must have the same batch")
+    _need(0 <= t0 <= _INT_MAX, "t0")
+    s = _q8_stream(k, stream)
+    rc = _lib.dq_q8_encode_kv(f, k.data_ptr(), k.stride(0), k.stride(1), k.stride(2), v.data_ptr(), v.stride(0),
+                              v.stride(1), v.stride(2), B, H, t0, T, nb * DQ_Q8_BLOCK, k_data.data_ptr(),
+                              k_scale.data_ptr(), v_data.data_ptr(), v_scale.data_ptr(),
+                              _q8_status(status, k_data.device), s)
+    _check(rc, "dq_q8_encode_kv")
+
+
+def dq_q8_encode_kv_paged(fmt, k, v, t0: int, block_table, k_pool, k_scale_pool, v_pool, v_scale_pool, status=None,
+                          stream=None):
+    """dq_q8_encode_kv into pool pages: pools uint8 [num_pages, H, page/32, 4096],
+    scales fp32 [num_pages, H, page/32]; block_table int32 [B, max_pages]."""
+    f = _q8_format(fmt)
+    num_pages, H, bpp = _q8_cache_args(k_pool, k_scale_pool, v_pool, v_scale_pool)
+    B, T = _q8_rows_args(k, v, H, k_pool.device)
+    _need(0 <= t0 <= _INT_MAX, "t0")
+    max_pages = _q8_table(block_table, B, k_pool.device)
+    s = _q8_stream(k, stream)
+    rc = _lib.dq_q8_encode_kv_paged(f, k.data_ptr(), k.stride(0), k.stride(1), k.stride(2), v.data_ptr(), v.stride(0),
+                                    v.stride(1), v.stride(2), B, H, t0, T, block_table.data_ptr(), max_pages,
+                                    bpp * DQ_Q8_BLOCK, num_pages, k_pool.data_ptr(), k_scale_pool.data_ptr(),
+                                    v_pool.data_ptr(), v_scale_pool.data_ptr(), _q8_status(status, k_pool.device), s)
+    _check(rc, "dq_q8_encode_kv_paged")
+
+
+def _q8_out_rows(k, v, batch, n, heads, dev):
+    if k is None:
+        k = torch.empty((batch, n, heads, 128), dtype=torch.bfloat16, device=dev)
+    if v is None:
+        v = torch.empty((batch, n, heads, 128), dtype=torch.bfloat16, device=dev)
+    _need(_q8_rows_args(k, v, heads, dev) == (batch, n), "k and v must be [B, n, H, 128]")
+    return k, v
+
+
+def dq_q8_decode_kv(fmt, k_data, k_scale, v_data, v_scale, t0: int, n: int, k=None, v=None, stream=None):
+    """The values of tokens [t0, t0 + n), t0 a multiple of 32, as bf16 [B, n, H, 128]."""
+    f = _q8_format(fmt)
+    B, H, nb = _q8_cache_args(k_data, k_scale, v_data, v_scale)
+    _need(0 <= t0 <= _INT_MAX and 0 <= n <= _INT_MAX, "t0 and n")
+    k, v = _q8_out_rows(k, v, B, n, H, k_data.device)
+    s = _q8_stream(k_data, stream)
+    if B and n:
+        rc = _lib.dq_q8_decode_kv(f, k_data.data_ptr(), k_scale.data_ptr(), v_data.data_ptr(), v_scale.data_ptr(), B, H,
+                                  t0, n, nb * DQ_Q8_BLOCK, k.data_ptr(), k.stride(0), k.stride(1), k.stride(2),
+                                  v.data_ptr(), v.stride(0), v.stride(1), v.stride(2), s)
+        _check(rc, "dq_q8_decode_kv")
+    return k, v
+
+
+def dq_q8_decode_kv_paged(fmt, k_pool, k_scale_pool, v_pool, v_scale_pool, block_table, t0: int, n: int, k=None,
+                          v=None, status=None, stream=None):
+    """dq_q8_decode_kv from pool pages."""
+    f = _q8_format(fmt)
+    num_pages, H, bpp = _q8_cache_args(k_pool, k_scale_pool, v_pool, v_scale_pool)
+    B = block_table.shape[0]
+    max_pages = _q8_table(block_table, B, k_pool.device)
+    _need(0 <= t0 <= _INT_MAX and 0 <= n <= _INT_MAX, "t0 and n")
+    k, v = _q8_out_rows(k, v, B, n, H, k_pool.device)
+    s = _q8_stream(k_pool, stream)
+    if B and n:
+        rc = _lib.dq_q8_decode_kv_paged(f, k_pool.data_ptr(), k_scale_pool.data_ptr(), v_pool.data_ptr(),
+                                        v_scale_pool.data_ptr(), B, H, t0, n, block_table.data_ptr(), max_pages,
+                                        bpp * DQ_Q8_BLOCK, num_pages, k.data_ptr(), k.stride(0), k.stride(1),
+                                        k.stride(2), v.data_ptr(), v.stride(0), v.stride(1), v.stride(2),
+                                        _q8_status(status, k_pool.device), s)
+        _check(rc, "dq_q8_decode_kv_paged")
+    return k, v
+
+
+def _q8_query(q, heads, dev):
+    _need(q.dtype == torch.bfloat16 and q.dim() == 3 and q.shape[2] == 128 and q.is_contiguous() and q.device == dev,
+          "q must be bf16 [B, Hq, 128], contiguous, on the cache's GPU")
+    return q.shape[0], q.shape[1]
+
+
+def _q8_out(out, q):
+    _need(out.dtype == torch.float32 and out.shape == q.shape and out.is_contiguous() and out.device == q.device,
+          "out must be fp32 of q's shape")
+    return out.data_ptr()
+
+
+def _q8_scores(scores, block_lse, batch, heads, blocks, group, dev):
+    """Pointers of the two score arrays (0 where absent)."""
+    for t, shape, name in ((scores, (batch, heads, blocks), "scores"),
+                           (block_lse, (batch, heads, blocks, group), "block_lse")):
+        _need(t is None or (t.dtype == torch.float32 and tuple(t.shape) == shape and t.is_contiguous()
+                            and t.device == dev), f"{name} must be fp32 {list(shape)} on the cache's GPU")
+    return 0 if scores is None else scores.data_ptr(), 0 if block_lse is None else block_lse.data_ptr()
+
+
+_RSQRT_D = 128 ** -0.5
+
+
+def _q8_workspace(workspace, dev):
+    """Pointer and size of the workspace."""
+    _need(workspace.device == dev and workspace.is_contiguous(), "workspace must be on the cache's GPU")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _q8_sees(window, sinks):
+    _need(0 <= window <= _INT_MAX and 0 <= sinks <= _INT_MAX, "window and sinks")
+    return window, sinks
+
+
+def dq_q8_decode_attention_partial(fmt, q, k_data, k_scale, v_data, v_scale, seq_lens, workspace, window: int = 0,
+                                   sinks: int = 0, extra_lens=None, softmax_scale=None, block_lse=None, stream=None):
+    """Split-K partials of one decode step over the 8-bit cache; finish with
+    dq_decode_attention_merge or dq_decode_attention_merge_residual."""
+    f = _q8_format(fmt)
+    B, H, nb = _q8_cache_args(k_data, k_scale, v_data, v_scale)
+    n, Hq = _q8_query(q, H, k_data.device)
+    _need(n == B, "q and the cache must have the same batch")
+    lens = _q8_lens(seq_lens, B, q.device)
+    extra = 0 if extra_lens is None else _q8_lens(extra_lens, B, q.device, "extra_lens")
+    _, lse = _q8_scores(None, block_lse, B, H, nb, Hq // H, q.device)
+    rc = _lib.dq_q8_decode_attention_partial(
+        f, q.data_ptr(), B, Hq, H, k_data.data_ptr(), k_scale.data_ptr(), v_data.data_ptr(), v_scale.data_ptr(), lens,
+        extra, nb * DQ_Q8_BLOCK, *_q8_sees(window, sinks), _RSQRT_D if softmax_scale is None else softmax_scale, lse,
+        *_q8_workspace(workspace, q.device), _q8_stream(q, stream))
+    _check(rc, "dq_q8_decode_attention_partial")
+
+
+def dq_q8_decode_attention(fmt, q, k_data, k_scale, v_data, v_scale, seq_lens, out, workspace, window: int = 0,
+                           sinks: int = 0, softmax_scale=None, block_lse=None, scores=None, stream=None):
+    """One decode step over the 8-bit cache: q bf16 [B, Hq, 128] -> out fp32.
+    window > 0: only the first `sinks` and the newest `window` tokens are
+    visible.  scores fp32 [B, H, t_cap/32] grow by the blocks' attention weight
+    (block_lse fp32 [B, H, t_cap/32, Hq/H] is its scratch)."""
+    f = _q8_format(fmt)
+    B, H, nb = _q8_cache_args(k_data, k_scale, v_data, v_scale)
+    n, Hq = _q8_query(q, H, k_data.device)
+    _need(n == B, "q and the cache must have the same batch")
+    sc, lse = _q8_scores(scores, block_lse, B, H, nb, Hq // H, q.device)
+    rc = _lib.dq_q8_decode_attention(
+        f, q.data_ptr(), B, Hq, H, k_data.data_ptr(), k_scale.data_ptr(), v_data.data_ptr(), v_scale.data_ptr(),
+        _q8_lens(seq_lens, B, q.device), nb * DQ_Q8_BLOCK, *_q8_sees(window, sinks),
+        _RSQRT_D if softmax_scale is None else softmax_scale, _q8_out(out, q), lse, sc,
+        *_q8_workspace(workspace, q.device), _q8_stream(q, stream))
+    _check(rc, "dq_q8_decode_attention")
+
+
+def dq_q8_decode_attention_paged_partial(fmt, q, k_pool, k_scale_pool, v_pool, v_scale_pool, block_table, seq_lens,
+                                         workspace, window: int = 0, sinks: int = 0, extra_lens=None,
+                                         softmax_scale=None, block_lse=None, status=None, stream=None):
+    """dq_q8_decode_attention_partial over pool pages; t_cap of the finishing
+    call is max_pages * page_tokens."""
+    f = _q8_format(fmt)
+    num_pages, H, bpp = _q8_cache_args(k_pool, k_scale_pool, v_pool, v_scale_pool)
+    B, Hq = _q8_query(q, H, k_pool.device)
+    max_pages = _q8_table(block_table, B, q.device)
+    lens = _q8_lens(seq_lens, B, q.device)
+    extra = 0 if extra_lens is None else _q8_lens(extra_lens, B, q.device, "extra_lens")
+    _, lse = _q8_scores(None, block_lse, B, H, max_pages * bpp, Hq // H, q.device)
+    rc = _lib.dq_q8_decode_attention_paged_partial(
+        f, q.data_ptr(), B, Hq, H, k_pool.data_ptr(), k_scale_pool.data_ptr(), v_pool.data_ptr(),
+        v_scale_pool.data_ptr(), block_table.data_ptr(), max_pages, bpp * DQ_Q8_BLOCK, num_pages, lens, extra,
+        *_q8_sees(window, sinks), _RSQRT_D if softmax_scale is None else softmax_scale, lse,
+        *_q8_workspace(workspace, q.device), _q8_status(status, q.device), _q8_stream(q, stream))
+    _check(rc, "dq_q8_decode_attention_paged_partial")
+
+
+def dq_q8_decode_attention_paged(fmt, q, k_pool, k_scale_pool, v_pool, v_scale_pool, block_table, seq_lens, out,
+                                 workspace, window: int = 0, sinks: int = 0, softmax_scale=None, block_lse=None,
+                                 scores=None, status=None, stream=None):
+    """dq_q8_decode_attention over pool pages (scores and block_lse have
+    max_pages * page/32 blocks per sequence)."""
+    f = _q8_format(fmt)
+    num_pages, H, bpp = _q8_cache_args(k_pool, k_scale_pool, v_pool, v_scale_pool)
+    B, Hq = _q8_query(q, H, k_pool.device)
+    max_pages = _q8_table(block_table, B, q.device)
+    sc, lse = _q8_scores(scores, block_lse, B, H, max_pages * bpp, Hq // H, q.device)
+    rc = _lib.dq_q8_decode_attention_paged(
+        f, q.data_ptr(), B, Hq, H, k_pool.data_ptr(), k_scale_pool.data_ptr(), v_pool.data_ptr(),
+        v_scale_pool.data_ptr(), block_table.data_ptr(), max_pages, bpp * DQ_Q8_BLOCK, num_pages,
+        _q8_lens(seq_lens, B, q.device), *_q8_sees(window, sinks), _RSQRT_D if softmax_scale is None else softmax_scale,
+        _q8_out(out, q), lse, sc, *_q8_workspace(workspace, q.device),
+        _q8_status(status, q.device), _q8_stream(q, stream))
+    _check(rc, "dq_q8_decode_attention_paged")
+
+
+def dq_q8_add_scores(q_heads: int, seq_lens, block_lse, workspace, scores, window: int = 0, sinks: int = 0,
+                     extra_lens=None, stream=None):
+    """scores fp32 [B, H, t_cap/32] grow by the attention weight of every block
+    in the step whose partials and block_lse are given (after
+    dq_decode_attention_residual, if the step has a residual window)."""
+    _need(scores.dim() == 3, "scores must be fp32 [B, H, t_cap/32]")
+    B, H, nb = scores.shape
+    sc, lse = _q8_scores(scores, block_lse, B, H, nb, q_heads // H, scores.device)
+    lens = _q8_lens(seq_lens, B, scores.device)
+    extra = 0 if extra_lens is None else _q8_lens(extra_lens, B, scores.device, "extra_lens")
+    rc = _lib.dq_q8_add_scores(B, q_heads, H, lens, extra, nb * DQ_Q8_BLOCK, *_q8_sees(window, sinks), lse,
+                               *_q8_workspace(workspace, scores.device), sc, _q8_stream(scores, stream))
+    _check(rc, "dq_q8_add_scores")
+
+
+def dq_q8_evict(seq_lens, new_lens, keep: int, first: int, last: int, source, to, kept, stream=None):
+    """Keep the blocks of the first `first` and newest `last` tokens and those of
+    the largest scores, keep tokens in all (multiples of 32).  source, to:
+    (k_data, k_scale, v_data, v_scale, scores), the same arrays for an eviction
+    in place; kept int32 [B, H, keep/32]; new_lens may be seq_lens."""
+    B, H, nb = _q8_cache_args(*source[:4])
+    tB, tH, tnb = _q8_cache_args(*to[:4])
+    dev = source[0].device
+    _need(max(keep, first, last) <= _INT_MAX and min(keep, first, last) >= 0, "keep, first and last")
+    _need((tB, tH) == (B, H) and to[0].device == dev, "both caches must have the same batch, heads and GPU")
+    _q8_scores(source[4], None, B, H, nb, 1, dev)
+    _q8_scores(to[4], None, B, H, tnb, 1, dev)
+    _need(kept.dtype == torch.int32 and tuple(kept.shape) == (B, H, keep // DQ_Q8_BLOCK) and kept.is_contiguous()
+          and kept.device == dev, "kept must be int32 [B, H, keep/32]")
+    rc = _lib.dq_q8_evict(B, H, _q8_lens(seq_lens, B, dev), _q8_lens(new_lens, B, dev, "new_lens"), nb * DQ_Q8_BLOCK,
+                          tnb * DQ_Q8_BLOCK, keep, first, last, *(t.data_ptr() for t in source),
+                          *(t.data_ptr() for t in to), kept.data_ptr(), _q8_stream(kept, stream))
+    _check(rc, "dq_q8_evict")
+
+
+def dq_q8_evict_paged(seq_lens, new_lens, keep: int, first: int, last: int, block_table, pools, scores, kept,
+                      status=None, stream=None):
+    """dq_q8_evict in place over pool pages: pools (k_pool, k_scale_pool, v_pool,
+    v_scale_pool), scores fp32 [B, H, max_pages * page/32]."""
+    num_pages, H, bpp = _q8_cache_args(*pools)
+    B, dev = block_table.shape[0], pools[0].device
+    _need(max(keep, first, last) <= _INT_MAX and min(keep, first, last) >= 0, "keep, first and last")
+    max_pages = _q8_table(block_table, B, dev)
+    _q8_scores(scores, None, B, H, max_pages * bpp, 1, dev)
+    _need(kept.dtype == torch.int32 and tuple(kept.shape) == (B, H, keep // DQ_Q8_BLOCK) and kept.is_contiguous()
+          and kept.device == dev, "kept must be int32 [B, H, keep/32]")
+    rc = _lib.dq_q8_evict_paged(B, H, _q8_lens(seq_lens, B, dev), _q8_lens(new_lens, B, dev, "new_lens"), keep, first,
+                                last, block_table.data_ptr(), max_pages, bpp * DQ_Q8_BLOCK, num_pages,
+                                *(t.data_ptr() for t in pools), scores.data_ptr(), kept.data_ptr(),
+                                _q8_status(status, dev), _q8_stream(kept, stream))
+    _check(rc, "dq_q8_evict_paged")
 
 
 DQ_NO_ALLOC_SCRATCH_BYTES = 8 << 20

@@ -109,6 +109,107 @@ class TokenKVCache:
         return out
 
 
+class Q8KVCache:
+    """Cache of 8-bit codes ("int8" or "e4m3") with one fp32 scale per block of
+    32 tokens, KV head and tensor (head_dim 128).
+
+    scores=True also keeps every block's accumulated attention weight
+    (``scores`` fp32 [B, H, t_cap/32]), which ``attend`` adds to and ``evict``
+    goes by."""
+
+    BLOCK = _lib.DQ_Q8_BLOCK
+
+    def __init__(self, batch: int, kv_heads: int, q_heads: int, t_cap: int, fmt: str = "int8", scores: bool = False,
+                 device="cuda"):
+        if t_cap <= 0 or t_cap % _lib.DQ_MEAN_WINDOW:
+            raise ValueError("t_cap must be a positive multiple of 128")
+        if fmt not in _lib.Q8_FORMATS:
+            raise ValueError("fmt must be 'int8' or 'e4m3'")
+        self.batch, self.kv_heads, self.q_heads, self.t_cap, self.head_dim = batch, kv_heads, q_heads, t_cap, 128
+        self.fmt = fmt
+        nb = t_cap // self.BLOCK
+        self.k_data = torch.zeros((batch, kv_heads, nb, self.BLOCK * 128), dtype=torch.uint8, device=device)
+        self.v_data = torch.zeros_like(self.k_data)
+        self.k_scales = torch.zeros((batch, kv_heads, nb), dtype=torch.float32, device=device)
+        self.v_scales = torch.zeros_like(self.k_scales)
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)
+        self.workspace = torch.empty(
+            _lib.dq_decode_workspace_bytes(batch, q_heads, kv_heads, t_cap), dtype=torch.uint8, device=device)
+        self.scores = torch.zeros_like(self.k_scales) if scores else None
+        self.block_lse = None
+        if scores:
+            self.block_lse = torch.empty((batch, kv_heads, nb, q_heads // kv_heads), dtype=torch.float32,
+                                         device=device)
+
+    @property
+    def arrays(self):
+        return self.k_data, self.k_scales, self.v_data, self.v_scales
+
+    def append(self, k, v, t0: int):
+        """Encode bf16 k, v [B, T_new, H, 128] as cache tokens [t0, t0 + T_new)
+        (t0 a multiple of 32; a last block that is not full is completed with
+        zeros)."""
+        _lib.dq_q8_encode_kv(self.fmt, k, v, t0, *self.arrays, status=self.status)
+
+    def read(self, t0: int, n: int):
+        """bf16 k, v [B, n, H, 128]: the values of tokens [t0, t0 + n)."""
+        return _lib.dq_q8_decode_kv(self.fmt, *self.arrays, t0, n)
+
+    def attend(self, q, seq_lens, out=None, softmax_scale=None, window: int = 0, sinks: int = 0, scores=None):
+        """q bf16 [B, Hq, 128] -> out fp32 over the first seq_lens[b] tokens or,
+        with a window, the first `sinks` and the newest `window` of them.  The
+        cache's own scores grow by the blocks' weights, or the given ones."""
+        if out is None:
+            out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
+        if scores is None:
+            scores = self.scores
+        elif self.block_lse is None:
+            raise ValueError("the cache was made without scores")
+        _lib.dq_q8_decode_attention(self.fmt, q, *self.arrays, seq_lens, out, self.workspace, window, sinks,
+                                    softmax_scale, self.block_lse, scores)
+        return out
+
+    def partial(self, q, seq_lens, softmax_scale=None, window: int = 0, sinks: int = 0, extra_lens=None):
+        """Split-K partials of one decode step into the workspace (finish with
+        merge; the scores' part of it with add_scores)."""
+        _lib.dq_q8_decode_attention_partial(self.fmt, q, *self.arrays, seq_lens, self.workspace, window, sinks,
+                                            extra_lens, softmax_scale, self.block_lse)
+
+    def merge(self, seq_lens, out):
+        _lib.dq_decode_attention_merge(self.batch, self.q_heads, self.kv_heads, seq_lens, self.t_cap,
+                                       self.workspace, out)
+
+    def add_scores(self, seq_lens, window: int = 0, sinks: int = 0, extra_lens=None):
+        _lib.dq_q8_add_scores(self.q_heads, seq_lens, self.block_lse, self.workspace, self.scores, window, sinks,
+                              extra_lens)
+
+    def evict(self, seq_lens, keep: int, sinks: int = 0, recent: int = 32, into=None, new_lens=None):
+        """Cut every sequence to at most `keep` tokens (a multiple of 32): the
+        blocks of its first `sinks` and newest `recent` tokens (rounded up to
+        32) and those of the largest scores, in their order; in place, or into
+        another Q8KVCache with scores.  Returns the kept blocks' old indexes
+        int32 [B, H, keep/32] (-1: none) and the new lengths (new_lens if
+        given, which may be seq_lens)."""
+        to = self if into is None else into
+        if self.scores is None or to.scores is None or to.fmt != self.fmt:
+            raise ValueError("eviction needs scores, and caches of one format")
+        if keep <= 0 or keep % self.BLOCK:
+            raise ValueError("keep must be a positive multiple of 32")
+        kept = torch.empty((self.batch, self.kv_heads, keep // self.BLOCK), dtype=torch.int32,
+                           device=self.k_data.device)
+        if new_lens is None:
+            new_lens = torch.empty_like(seq_lens)
+        up = -self.BLOCK
+        _lib.dq_q8_evict(seq_lens, new_lens, keep, sinks // up * up, max(recent // up * up, self.BLOCK),
+                         (*self.arrays, self.scores), (*to.arrays, to.scores), kept)
+        return kept, new_lens
+
+    def cache_bytes(self, tokens: int) -> int:
+        """Bytes of codes and scales that cover `tokens` tokens of every sequence."""
+        blocks = (tokens + self.BLOCK - 1) // self.BLOCK
+        return self.batch * self.kv_heads * blocks * 2 * (self.BLOCK * 128 + 4)
+
+
 class StreamingKVCache:
     """A compressed cache plus the BF16 residual window of the newest tokens.
 
@@ -121,23 +222,31 @@ class StreamingKVCache:
 
     streams="head" keeps one stream per (token, KV head) (a KVCache);
     streams="token" the paper's default grouping, one stream per token over
-    all KV heads (a TokenKVCache, tables built with head_dim 128 kv_heads).
+    all KV heads (a TokenKVCache, tables built with head_dim 128 kv_heads);
+    streams="int8" or "e4m3" 8-bit codes (a Q8KVCache, no tables), which also
+    give attention behind a window and, with scores=True, eviction.
     The ring, its append and commit, and the residual attention are the same
-    for both.
+    for all.
     """
 
     WINDOW = _lib.DQ_MEAN_WINDOW
 
     def __init__(self, batch: int, kv_heads: int, q_heads: int, t_cap: int, k_tables, v_tables,
-                 device="cuda", r_cap: int = 256, streams: str = "head"):
+                 device="cuda", r_cap: int = 256, streams: str = "head", scores: bool = False):
         if r_cap % self.WINDOW or not (2 * self.WINDOW <= r_cap <= 256):
             raise ValueError("r_cap must be 256 (two mean windows)")
         if streams == "head":
             self.cache = KVCache(batch, kv_heads, q_heads, t_cap, k_tables, v_tables, device=device)
         elif streams == "token":
             self.cache = TokenKVCache(batch, kv_heads, q_heads, t_cap, k_tables, v_tables, device=device)
+        elif streams in _lib.Q8_FORMATS:
+            if k_tables is not None or v_tables is not None:
+                raise ValueError("8-bit streams take no tables")
+            self.cache = Q8KVCache(batch, kv_heads, q_heads, t_cap, streams, scores=scores, device=device)
         else:
-            raise ValueError("streams must be 'head' or 'token'")
+            raise ValueError("streams must be 'head', 'token', 'int8' or 'e4m3'")
+        if scores and streams not in _lib.Q8_FORMATS:
+            raise ValueError("scores need 8-bit streams")
         self.streams = streams
         d = self.cache.head_dim
         self.r_cap = r_cap
@@ -190,12 +299,43 @@ class StreamingKVCache:
         self.n_comp += W
         self.n_res -= W
 
-    def attend(self, q, out=None, softmax_scale=None):
-        """q bf16 [B, Hq, d] -> out fp32 [B, Hq, d] over every token so far."""
+    def attend(self, q, out=None, softmax_scale=None, window: int = 0, sinks: int = 0):
+        """q bf16 [B, Hq, d] -> out fp32 [B, Hq, d] over every token so far, or
+        (8-bit streams; window >= r_cap) over the first `sinks` and the newest
+        `window` of them."""
         c = self.cache
         if out is None:
             out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
-        c.partial(q, self.seq_lens, softmax_scale)
+        if self.streams not in _lib.Q8_FORMATS:
+            if window or sinks:
+                raise ValueError("a window needs 8-bit streams")
+            c.partial(q, self.seq_lens, softmax_scale)
+        else:
+            if window and window < self.r_cap:
+                raise ValueError("window must be 0 or at least r_cap")
+            c.partial(q, self.seq_lens, softmax_scale, window, sinks, self.res_lens)
+            if c.scores is not None:
+                # the scores' weights need the raw tokens' partials in the workspace
+                _lib.dq_decode_attention_residual(q, self.res_k, self.res_v, self.seq_lens, self.res_lens, c.t_cap,
+                                                  c.workspace, softmax_scale=softmax_scale)
+                c.merge(self.seq_lens, out)
+                c.add_scores(self.seq_lens, window, sinks, self.res_lens)
+                return out
         _lib.dq_decode_attention_merge_residual(q, self.res_k, self.res_v, self.seq_lens, self.res_lens, c.t_cap,
                                                 c.workspace, out, softmax_scale=softmax_scale)
         return out
+
+    def evict(self, keep: int, sinks: int = 0, recent: int = 32):
+        """Cut the compressed side to `keep` tokens and up to r_cap - 1 more (the
+        ring's slots go by its length, so whole rings of tokens leave): of every
+        sequence and KV head the blocks with the least attention weight so far,
+        the first `sinks` and newest `recent` compressed tokens apart.  Returns
+        the kept blocks' old indexes, or None if nothing had to go."""
+        if self.streams not in _lib.Q8_FORMATS:
+            raise ValueError("eviction needs 8-bit streams")
+        gone = (self.n_comp - keep) // self.r_cap * self.r_cap
+        if gone <= 0:
+            return None
+        kept, _ = self.cache.evict(self.seq_lens, self.n_comp - gone, sinks, recent, new_lens=self.seq_lens)
+        self.n_comp -= gone
+        return kept

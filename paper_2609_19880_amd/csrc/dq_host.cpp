@@ -636,6 +636,217 @@ int dq_residual_commit(int32_t* seq_lens, int32_t* res_lens, int32_t B, int32_t 
     return dq::launch_residual_commit(seq_lens, res_lens, B, n, status, static_cast<hipStream_t>(stream));
 }
 
+// ------------------------------------------------------------- 8-bit cache
+
+static bool q8_cache_ok(const dq::Q8Cache& c) {
+    for (int i = 0; i < 2; ++i)
+        if (!c.data[i] || !c.scale[i] || (reinterpret_cast<uintptr_t>(c.data[i]) & 15)) return false;
+    return true;
+}
+
+static dq::Q8Cache q8_cache(const uint8_t* kd, const float* ks, const uint8_t* vd, const float* vs) {
+    return dq::Q8Cache{{const_cast<uint8_t*>(kd), const_cast<uint8_t*>(vd)},
+                       {const_cast<float*>(ks), const_cast<float*>(vs)}};
+}
+
+// Sizes, strides and (unless there is nothing to do) pointers of a span of
+// tokens [t0, t0 + n) of the cache.
+static int check_q8_rows(int32_t format, const dq::Q8Rows& k, const dq::Q8Rows& v, int32_t B, int32_t H, int32_t t0,
+                         int32_t n, int32_t t_cap, const dq::Q8Cache& c) {
+    if (format != DQ_Q8_INT8 && format != DQ_Q8_E4M3) return DQ_ERR_INVALID_ARG;
+    if (B < 0 || B > 65535 || H <= 0 || H > 65535 || t0 < 0 || n < 0 || t_cap <= 0) return DQ_ERR_INVALID_ARG;
+    if (t_cap % DQ_MEAN_WINDOW || t0 % DQ_Q8_BLOCK || (int64_t)t0 + n > t_cap) return DQ_ERR_INVALID_ARG;
+    if (k.sb < 0 || k.st < 0 || k.sh < 0 || v.sb < 0 || v.st < 0 || v.sh < 0) return DQ_ERR_INVALID_ARG;
+    if (B > 0 && n > 0 && (!k.p || !v.p || !q8_cache_ok(c))) return DQ_ERR_INVALID_ARG;
+    return DQ_OK;
+}
+
+static int q8_encode(int32_t format, const dq::Pages& pg, const dq::Q8Rows& k, const dq::Q8Rows& v, int32_t B,
+                     int32_t H, int32_t t0, int32_t n, int32_t t_cap, const dq::Q8Cache& c, uint32_t* status,
+                     void* stream) {
+    if (int rc = check_q8_rows(format, k, v, B, H, t0, n, t_cap, c)) return rc;
+    if (B == 0 || n == 0) return DQ_OK;
+    return dq::launch_q8_encode(format, pg, k, v, B, H, t0, n, t_cap, c, status, static_cast<hipStream_t>(stream));
+}
+
+static int q8_read(int32_t format, const dq::Pages& pg, const dq::Q8Cache& c, int32_t B, int32_t H, int32_t t0,
+                   int32_t n, int32_t t_cap, const dq::Q8Rows& k, const dq::Q8Rows& v, uint32_t* status,
+                   void* stream) {
+    if (int rc = check_q8_rows(format, k, v, B, H, t0, n, t_cap, c)) return rc;
+    if (B == 0 || n == 0) return DQ_OK;
+    return dq::launch_q8_read(format, pg, c, B, H, t0, n, t_cap, k, v, status, static_cast<hipStream_t>(stream));
+}
+
+int dq_q8_encode_kv(int32_t format, const uint16_t* k, int64_t ksb, int64_t kst, int64_t ksh, const uint16_t* v,
+                    int64_t vsb, int64_t vst, int64_t vsh, int32_t B, int32_t H, int32_t t0, int32_t n_new,
+                    int32_t t_cap, uint8_t* k_data, float* k_scale, uint8_t* v_data, float* v_scale,
+                    uint32_t* status, void* stream) {
+    return q8_encode(format, kContiguous, {k, ksb, kst, ksh}, {v, vsb, vst, vsh}, B, H, t0, n_new, t_cap,
+                     q8_cache(k_data, k_scale, v_data, v_scale), status, stream);
+}
+
+int dq_q8_encode_kv_paged(int32_t format, const uint16_t* k, int64_t ksb, int64_t kst, int64_t ksh,
+                          const uint16_t* v, int64_t vsb, int64_t vst, int64_t vsh, int32_t B, int32_t H, int32_t t0,
+                          int32_t n_new, const int32_t* block_table, int32_t max_pages, int32_t page_tokens,
+                          int32_t num_pages, uint8_t* k_pool, float* k_scale_pool, uint8_t* v_pool,
+                          float* v_scale_pool, uint32_t* status, void* stream) {
+    dq::Pages pg;
+    int32_t t_cap = 0;
+    if (int rc = paging(block_table, max_pages, page_tokens, num_pages, &pg, &t_cap)) return rc;
+    return q8_encode(format, pg, {k, ksb, kst, ksh}, {v, vsb, vst, vsh}, B, H, t0, n_new, t_cap,
+                     q8_cache(k_pool, k_scale_pool, v_pool, v_scale_pool), status, stream);
+}
+
+int dq_q8_decode_kv(int32_t format, const uint8_t* k_data, const float* k_scale, const uint8_t* v_data,
+                    const float* v_scale, int32_t B, int32_t H, int32_t t0, int32_t n, int32_t t_cap, uint16_t* k,
+                    int64_t ksb, int64_t kst, int64_t ksh, uint16_t* v, int64_t vsb, int64_t vst, int64_t vsh,
+                    void* stream) {
+    return q8_read(format, kContiguous, q8_cache(k_data, k_scale, v_data, v_scale), B, H, t0, n, t_cap,
+                   {k, ksb, kst, ksh}, {v, vsb, vst, vsh}, nullptr, stream);
+}
+
+int dq_q8_decode_kv_paged(int32_t format, const uint8_t* k_pool, const float* k_scale_pool, const uint8_t* v_pool,
+                          const float* v_scale_pool, int32_t B, int32_t H, int32_t t0, int32_t n,
+                          const int32_t* block_table, int32_t max_pages, int32_t page_tokens, int32_t num_pages,
+                          uint16_t* k, int64_t ksb, int64_t kst, int64_t ksh, uint16_t* v, int64_t vsb, int64_t vst,
+                          int64_t vsh, uint32_t* status, void* stream) {
+    dq::Pages pg;
+    int32_t t_cap = 0;
+    if (int rc = paging(block_table, max_pages, page_tokens, num_pages, &pg, &t_cap)) return rc;
+    return q8_read(format, pg, q8_cache(k_pool, k_scale_pool, v_pool, v_scale_pool), B, H, t0, n, t_cap,
+                   {k, ksb, kst, ksh}, {v, vsb, vst, vsh}, status, stream);
+}
+
+// Sizes every call of a step has in common.
+static int check_q8_step(int32_t B, int32_t Hq, int32_t Hkv, const int32_t* seq_lens, int32_t t_cap, int32_t window,
+                         int32_t sinks, const void* ws, size_t ws_bytes) {
+    if (B <= 0 || Hkv <= 0 || Hq <= 0 || Hq % Hkv || Hq / Hkv > 8 || B > 65535 || Hkv > 65535)
+        return DQ_ERR_INVALID_ARG;
+    if (t_cap <= 0 || t_cap % DQ_MEAN_WINDOW || !seq_lens) return DQ_ERR_INVALID_ARG;
+    if (window < 0 || sinks < 0 || (window == 0 && sinks)) return DQ_ERR_INVALID_ARG;
+    if (!ws || ws_bytes < dq::attention_workspace_bytes(B, Hq, Hkv, t_cap, 128)) return DQ_ERR_WORKSPACE;
+    return DQ_OK;
+}
+
+static int q8_partial(int32_t format, const dq::Pages& pg, const uint16_t* q, int32_t B, int32_t Hq, int32_t Hkv,
+                      const dq::Q8Cache& c, const int32_t* seq_lens, const int32_t* extra_lens, int32_t t_cap,
+                      int32_t window, int32_t sinks, float scale, float* lse, void* ws, size_t ws_bytes,
+                      uint32_t* status, void* stream) {
+    if (format != DQ_Q8_INT8 && format != DQ_Q8_E4M3) return DQ_ERR_INVALID_ARG;
+    if (!q || !q8_cache_ok(c) || !std::isfinite(scale)) return DQ_ERR_INVALID_ARG;
+    if (int rc = check_q8_step(B, Hq, Hkv, seq_lens, t_cap, window, sinks, ws, ws_bytes)) return rc;
+    return dq::launch_q8_partial(format, pg, q, B, Hq, Hkv, c, seq_lens, extra_lens, t_cap, window, sinks, scale, lse,
+                                 ws, status, static_cast<hipStream_t>(stream));
+}
+
+// Partial, merge and scores of one step.
+static int q8_attention(int32_t format, const dq::Pages& pg, const uint16_t* q, int32_t B, int32_t Hq, int32_t Hkv,
+                        const dq::Q8Cache& c, const int32_t* seq_lens, int32_t t_cap, int32_t window, int32_t sinks,
+                        float scale, float* out, float* lse, float* scores, void* ws, size_t ws_bytes,
+                        uint32_t* status, void* stream) {
+    if (!out || (scores && !lse)) return DQ_ERR_INVALID_ARG;
+    int rc = q8_partial(format, pg, q, B, Hq, Hkv, c, seq_lens, nullptr, t_cap, window, sinks, scale, lse, ws,
+                        ws_bytes, status, stream);
+    if (rc != DQ_OK) return rc;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    rc = dq::launch_attention_merge(B, Hq, Hkv, seq_lens, t_cap, ws, out, s);
+    if (rc != DQ_OK || !scores) return rc;
+    return dq::launch_q8_scores(B, Hq, Hkv, seq_lens, nullptr, t_cap, window, sinks, lse, ws, scores, s);
+}
+
+int dq_q8_decode_attention_partial(int32_t format, const uint16_t* q, int32_t B, int32_t Hq, int32_t Hkv,
+                                   const uint8_t* k_data, const float* k_scale, const uint8_t* v_data,
+                                   const float* v_scale, const int32_t* seq_lens, const int32_t* extra_lens,
+                                   int32_t t_cap, int32_t window, int32_t sinks, float scale, float* block_lse,
+                                   void* ws, size_t ws_bytes, void* stream) {
+    return q8_partial(format, kContiguous, q, B, Hq, Hkv, q8_cache(k_data, k_scale, v_data, v_scale), seq_lens,
+                      extra_lens, t_cap, window, sinks, scale, block_lse, ws, ws_bytes, nullptr, stream);
+}
+
+int dq_q8_decode_attention(int32_t format, const uint16_t* q, int32_t B, int32_t Hq, int32_t Hkv,
+                           const uint8_t* k_data, const float* k_scale, const uint8_t* v_data, const float* v_scale,
+                           const int32_t* seq_lens, int32_t t_cap, int32_t window, int32_t sinks, float scale,
+                           float* out, float* block_lse, float* scores, void* ws, size_t ws_bytes, void* stream) {
+    return q8_attention(format, kContiguous, q, B, Hq, Hkv, q8_cache(k_data, k_scale, v_data, v_scale), seq_lens,
+                        t_cap, window, sinks, scale, out, block_lse, scores, ws, ws_bytes, nullptr, stream);
+}
+
+int dq_q8_decode_attention_paged_partial(int32_t format, const uint16_t* q, int32_t B, int32_t Hq, int32_t Hkv,
+                                         const uint8_t* k_pool, const float* k_scale_pool, const uint8_t* v_pool,
+                                         const float* v_scale_pool, const int32_t* block_table, int32_t max_pages,
+                                         int32_t page_tokens, int32_t num_pages, const int32_t* seq_lens,
+                                         const int32_t* extra_lens, int32_t window, int32_t sinks, float scale,
+                                         float* block_lse, void* ws, size_t ws_bytes, uint32_t* status,
+                                         void* stream) {
+    dq::Pages pg;
+    int32_t t_cap = 0;
+    if (int rc = paging(block_table, max_pages, page_tokens, num_pages, &pg, &t_cap)) return rc;
+    return q8_partial(format, pg, q, B, Hq, Hkv, q8_cache(k_pool, k_scale_pool, v_pool, v_scale_pool), seq_lens,
+                      extra_lens, t_cap, window, sinks, scale, block_lse, ws, ws_bytes, status, stream);
+}
+
+int dq_q8_decode_attention_paged(int32_t format, const uint16_t* q, int32_t B, int32_t Hq, int32_t Hkv,
+                                 const uint8_t* k_pool, const float* k_scale_pool, const uint8_t* v_pool,
+                                 const float* v_scale_pool, const int32_t* block_table, int32_t max_pages,
+                                 int32_t page_tokens, int32_t num_pages, const int32_t* seq_lens, int32_t window,
+                                 int32_t sinks, float scale, float* out, float* block_lse, float* scores, void* ws,
+                                 size_t ws_bytes, uint32_t* status, void* stream) {
+    dq::Pages pg;
+    int32_t t_cap = 0;
+    if (int rc = paging(block_table, max_pages, page_tokens, num_pages, &pg, &t_cap)) return rc;
+    return q8_attention(format, pg, q, B, Hq, Hkv, q8_cache(k_pool, k_scale_pool, v_pool, v_scale_pool), seq_lens,
+                        t_cap, window, sinks, scale, out, block_lse, scores, ws, ws_bytes, status, stream);
+}
+
+int dq_q8_add_scores(int32_t B, int32_t Hq, int32_t Hkv, const int32_t* seq_lens, const int32_t* extra_lens,
+                     int32_t t_cap, int32_t window, int32_t sinks, const float* block_lse, const void* ws,
+                     size_t ws_bytes, float* scores, void* stream) {
+    if (!block_lse || !scores) return DQ_ERR_INVALID_ARG;
+    if (int rc = check_q8_step(B, Hq, Hkv, seq_lens, t_cap, window, sinks, ws, ws_bytes)) return rc;
+    return dq::launch_q8_scores(B, Hq, Hkv, seq_lens, extra_lens, t_cap, window, sinks, block_lse, ws, scores,
+                                static_cast<hipStream_t>(stream));
+}
+
+static int q8_evict(const dq::Pages& pg, int32_t B, int32_t H, const int32_t* seq_lens, int32_t* new_lens,
+                    int32_t t_cap, int32_t to_cap, int32_t keep, int32_t first, int32_t last, float* scores,
+                    float* to_scores, const dq::Q8Cache& from, const dq::Q8Cache& to, int32_t* kept,
+                    uint32_t* status, void* stream) {
+    if (B <= 0 || B > 65535 || H <= 0 || H > 65535 || t_cap <= 0 || t_cap % DQ_MEAN_WINDOW || to_cap <= 0 ||
+        to_cap % DQ_MEAN_WINDOW)
+        return DQ_ERR_INVALID_ARG;
+    if (!seq_lens || !new_lens || !scores || !to_scores || !kept || !q8_cache_ok(from) || !q8_cache_ok(to))
+        return DQ_ERR_INVALID_ARG;
+    if (keep % DQ_Q8_BLOCK || first % DQ_Q8_BLOCK || last % DQ_Q8_BLOCK) return DQ_ERR_INVALID_ARG;
+    if (first < 0 || last < DQ_Q8_BLOCK || (int64_t)first + last > keep || keep > to_cap) return DQ_ERR_INVALID_ARG;
+    // in place everything is, or nothing
+    const int same = (from.data[0] == to.data[0]) + (from.data[1] == to.data[1]) + (from.scale[0] == to.scale[0]) +
+                     (from.scale[1] == to.scale[1]) + (scores == to_scores);
+    if (same != 0 && (same != 5 || t_cap != to_cap)) return DQ_ERR_INVALID_ARG;
+    return dq::launch_q8_evict(pg, B, H, seq_lens, new_lens, t_cap, to_cap, keep, first, last, scores, to_scores,
+                               from, to, kept, status, static_cast<hipStream_t>(stream));
+}
+
+int dq_q8_evict(int32_t B, int32_t H, const int32_t* seq_lens, int32_t* new_lens, int32_t t_cap, int32_t to_cap,
+                int32_t keep, int32_t first, int32_t last, uint8_t* k_data, float* k_scale, uint8_t* v_data,
+                float* v_scale, float* scores, uint8_t* to_k_data, float* to_k_scale, uint8_t* to_v_data,
+                float* to_v_scale, float* to_scores, int32_t* kept, void* stream) {
+    return q8_evict(kContiguous, B, H, seq_lens, new_lens, t_cap, to_cap, keep, first, last, scores, to_scores,
+                    q8_cache(k_data, k_scale, v_data, v_scale),
+                    q8_cache(to_k_data, to_k_scale, to_v_data, to_v_scale), kept, nullptr, stream);
+}
+
+int dq_q8_evict_paged(int32_t B, int32_t H, const int32_t* seq_lens, int32_t* new_lens, int32_t keep, int32_t first,
+                      int32_t last, const int32_t* block_table, int32_t max_pages, int32_t page_tokens,
+                      int32_t num_pages, uint8_t* k_pool, float* k_scale_pool, uint8_t* v_pool, float* v_scale_pool,
+                      float* scores, int32_t* kept, uint32_t* status, void* stream) {
+    dq::Pages pg;
+    int32_t t_cap = 0;
+    if (int rc = paging(block_table, max_pages, page_tokens, num_pages, &pg, &t_cap)) return rc;
+    const dq::Q8Cache c = q8_cache(k_pool, k_scale_pool, v_pool, v_scale_pool);
+    return q8_evict(pg, B, H, seq_lens, new_lens, t_cap, t_cap, keep, first, last, scores, scores, c, c, kept, status,
+                    stream);
+}
+
 int dq_decode_symbols(const dq_tables* t, const uint8_t* records, int64_t n_streams, uint8_t* sym,
                       uint16_t* header, uint32_t* status, void* stream) {
     if (!table_args_ok(t) || n_streams < 0 || (n_streams > 0 && (!records || !sym)))

@@ -1,0 +1,1163 @@
+// The 8-bit cache: keys and values as int8 or e4m3 codes with one fp32 scale
+// for each block of 32 tokens of one (sequence, KV head) and tensor; its
+// encoder, the read-back, decode attention over it (all tokens, or the first
+// ones and the newest), the attention weight of every block, and the eviction
+// of the blocks with the least of it.
+//
+// Numbers.  s = fl32(max |x| / Q) over the block's 32 x 128 values, Q = 127 or
+// 448 (the type's largest); code = x / s rounded to the type's nearest value,
+// ties to even; x^ = s code.
+//
+// Layout.  A block is 4096 bytes in the order in which the matrix cores take
+// their operands, so that every read of the attention is 1024 contiguous bytes
+// per wavefront and no byte moves between lanes.  With t = 0..31 the token and
+// c = 0..127 the channel, lane = 16 grp + col:
+//   keys:   byte c % 16 of piece ((t / 16) 2 + c / 64) 64 + ((c / 16) % 4) 16 + t % 16
+//           (16-byte pieces; a lane's piece is 16 channels of one token: two
+//           8-channel slices of the A operand of a 16x16x32 product)
+//   values: byte ((c / 16) % 2) 8 + (t / 16) 4 + t % 4 of piece
+//           ((c / 32) 4 + (t / 4) % 4) 16 + c % 16
+//           (a lane's piece is two channels of the 8 tokens whose weights the
+//           first product leaves in that lane)
+#include <math.h>
+
+#include <algorithm>
+
+#include "dq_common.h"
+
+namespace dq {
+namespace {
+
+constexpr int kD = 128;
+constexpr int kBlk = DQ_Q8_BLOCK;            // tokens that share a scale
+constexpr int kBlkBytes = kBlk * kD;
+constexpr float kTiny = 0x1p-96f;            // a block below is stored as zeros
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+// Index of block `blk` of (b, h) in a cache of nb_cap blocks per sequence, or
+// in pool pages ([num_pages][H][page / 32]).
+__device__ __forceinline__ int64_t block_index(const Pages& pg, int H, int nb_cap, int b, int h, int blk, bool& bad) {
+    if (!pg.bt) return ((int64_t)b * H + h) * nb_cap + blk;
+    const int64_t p = physical_page(pg, b, blk * kBlk, bad);
+    const int bpp = 1 << (pg.page_shift - 5);
+    return (p * H + h) * bpp + (blk & (bpp - 1));
+}
+
+__device__ __forceinline__ int wave_index(int waves) {
+    return __builtin_amdgcn_readfirstlane((int)(blockIdx.x * waves + threadIdx.x / kWave));
+}
+
+// ------------------------------------------------------------------ encoder
+
+struct EncArgs {
+    const uint16_t* x[2];        // keys, values
+    int64_t sb[2], st[2], sh[2];
+    uint8_t* data[2];
+    float* scale[2];
+    uint32_t* status;
+    Pages pg;
+    int B, H, blk0, nblk, n_new, nb_cap;
+    int total;                   // wavefronts of one tensor: B nblk H
+    int aligned[2];              // rows are whole 16-byte pieces
+};
+
+// x / s with its last bit made odd where the quotient is not exact, so that a
+// later rounding to fewer bits is the rounding of the exact quotient.  t is
+// within an ulp of it; the sign of x - s t (exact: one rounding, of a nonzero
+// number far from underflow) says on which side.
+__device__ __forceinline__ float quotient_odd(float x, float s, float inv) {
+    float t = x * inv;
+    t = fmaf(fmaf(-s, t, x), inv, t);
+    const float r = fmaf(-s, t, x);
+    const uint32_t u = __float_as_uint(t);
+    const uint32_t away = (__float_as_uint(r) ^ u) >> 31;      // 0: |x / s| > |t|
+    const uint32_t v = (u & 1u) ? u : u + 1u - 2u * away;
+    return __uint_as_float(r == 0.f ? u : v);
+}
+
+// Four quotients to four code bytes.
+template <int FMT>
+__device__ __forceinline__ uint32_t codes4(const float (&t)[4]) {
+    if constexpr (FMT == DQ_Q8_E4M3) {
+        int w = __builtin_amdgcn_cvt_pk_fp8_f32(t[0], t[1], 0, false);
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(t[2], t[3], w, true);
+        return (uint32_t)w;
+    } else {
+        // t + 1.5 2^23 rounds t to an integer, ties to even, in the low bits
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(t[i] + 12582912.f);
+        const uint32_t lo = __builtin_amdgcn_perm(w[1], w[0], 0x0C0C0400u);
+        const uint32_t hi = __builtin_amdgcn_perm(w[3], w[2], 0x04000C0Cu);
+        return lo | hi;
+    }
+}
+
+__device__ __forceinline__ uint32_t pk_max(uint32_t a, uint32_t b) {
+    const u16x2 x = __builtin_bit_cast(u16x2, a), y = __builtin_bit_cast(u16x2, b);
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(x, y));
+}
+
+__device__ __forceinline__ uint32_t finite_pair(uint32_t w) {
+    if ((w & 0x7F80u) == 0x7F80u) w &= 0xFFFF0000u;
+    if ((w & 0x7F800000u) == 0x7F800000u) w &= 0x0000FFFFu;
+    return w;
+}
+
+__device__ __forceinline__ uint32_t quad_xor2(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, false);   // quad_perm [2, 3, 0, 1]
+}
+
+// One wavefront per block, heads fastest, so that the wavefronts of a
+// workgroup read neighbouring rows.  A lane holds 64 values: of keys, the
+// 16 channels of its four pieces; of values, 8 channels 8 (lane % 16) of the
+// tokens 16 h2 + 4 (lane / 16) + i, whose codes are byte-transposed in the
+// lane and swapped with lane ^ 2, which holds the pieces' other halves.
+template <int FMT>
+__global__ __launch_bounds__(256) void q8_encode_kernel(EncArgs a) {
+    const int lane = threadIdx.x & (kWave - 1);
+    int w = wave_index(4);
+    const int which = w >= a.total;
+    if (which) w -= a.total;
+    if (w >= a.total) return;
+    const int h = w % a.H, rest = w / a.H;
+    const int blk = rest % a.nblk, b = rest / a.nblk;
+    bool bad = false;
+    const int64_t bi = block_index(a.pg, a.H, a.nb_cap, b, h, a.blk0 + blk, bad);
+    if (bad) {
+        if (lane == 0 && a.status) atomicOr(a.status, DQ_STATUS_PAGE);
+        return;
+    }
+    const int rows = min(kBlk, a.n_new - blk * kBlk);
+    const uint16_t* src = a.x[which] + (int64_t)b * a.sb[which] + (int64_t)h * a.sh[which] +
+                          (int64_t)blk * kBlk * a.st[which];
+    const int64_t st = a.st[which];
+    const int col = lane & 15, grp = lane >> 4;
+    const bool keys = which == 0;
+    // load i: keys: token 16 (i / 4) + col, channels 64 ((i / 2) % 2) + 16 grp + 8 (i % 2);
+    //         values: token 16 (i / 4) + 4 grp + i % 4, channels 8 col
+    uint32_t x[8][4];
+    const int row0 = keys ? col : 4 * grp;
+    const int ch0 = keys ? 16 * grp : 8 * col;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int t = row0 + 16 * (i >> 2) + (keys ? 0 : i & 3);
+        const int c = ch0 + (keys ? 64 * ((i >> 1) & 1) + 8 * (i & 1) : 0);
+        uint4 v = uint4{0u, 0u, 0u, 0u};
+        if (t < rows) {
+            const uint16_t* p = src + t * st + c;
+            if (a.aligned[which]) {
+                v = *reinterpret_cast<const uint4*>(p);
+            } else {
+                v.x = (uint32_t)p[0] | ((uint32_t)p[1] << 16);
+                v.y = (uint32_t)p[2] | ((uint32_t)p[3] << 16);
+                v.z = (uint32_t)p[4] | ((uint32_t)p[5] << 16);
+                v.w = (uint32_t)p[6] | ((uint32_t)p[7] << 16);
+            }
+        }
+        x[i][0] = v.x;
+        x[i][1] = v.y;
+        x[i][2] = v.z;
+        x[i][3] = v.w;
+    }
+    // the largest magnitude: bf16 patterns without their signs order as integers
+    auto largest = [&]() {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) m = pk_max(m, x[i][j] & 0x7FFF7FFFu);
+        return wave_max((int)max(m & 0xFFFFu, m >> 16));
+    };
+    int top = largest();
+    if (top >= 0x7F80) {         // infinities and NaN count as zeros
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[i][j] = finite_pair(x[i][j]);
+        top = largest();
+        if (lane == 0 && a.status) atomicOr(a.status, DQ_STATUS_RANGE);
+    }
+    const float amax = __uint_as_float((uint32_t)top << 16);
+    const float s = amax < kTiny ? 0.f : amax / (FMT == DQ_Q8_E4M3 ? 448.f : 127.f);
+    if (lane == 0) a.scale[which][bi] = s;
+    uint32_t code[8][2];
+    if (s == 0.f) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) code[i][0] = code[i][1] = 0u;
+    } else {
+        // quotients of the block brought to magnitudes below 2 (exact powers of
+        // 2; what underflows is 2^-149 of the largest value and rounds to 0)
+        const int e = max(-126, min(126, 127 - (top >> 7)));
+        const float f = __uint_as_float((uint32_t)(e + 127) << 23);
+        const float ss = s * f, inv = 1.f / ss;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float t[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                t[2 * j] = quotient_odd(__uint_as_float(x[i][j] << 16) * f, ss, inv);
+                t[2 * j + 1] = quotient_odd(__uint_as_float(x[i][j] & 0xFFFF0000u) * f, ss, inv);
+            }
+            const float lo[4] = {t[0], t[1], t[2], t[3]}, hi[4] = {t[4], t[5], t[6], t[7]};
+            code[i][0] = codes4<FMT>(lo);
+            code[i][1] = codes4<FMT>(hi);
+        }
+    }
+    uint4* dst = reinterpret_cast<uint4*>(a.data[which] + bi * kBlkBytes);
+    if (keys) {
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+            dst[64 * p + lane] = uint4{code[2 * p][0], code[2 * p][1], code[2 * p + 1][0], code[2 * p + 1][1]};
+    } else {
+        // o[x][h2]: channel 8 col + x of tokens 16 h2 + 4 grp + 0..3
+        uint32_t o[8][2];
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const uint32_t c0 = code[4 * h2][q], c1 = code[4 * h2 + 1][q], c2 = code[4 * h2 + 2][q],
+                               c3 = code[4 * h2 + 3][q];
+                // bytes k of c0..c3 -> one word, for k = 0..3
+                const uint32_t a0 = __builtin_amdgcn_perm(c1, c0, 0x05010400u);   // c0.0 c1.0 c0.1 c1.1
+                const uint32_t a1 = __builtin_amdgcn_perm(c3, c2, 0x05010400u);
+                const uint32_t b0 = __builtin_amdgcn_perm(c1, c0, 0x07030602u);   // c0.2 c1.2 c0.3 c1.3
+                const uint32_t b1 = __builtin_amdgcn_perm(c3, c2, 0x07030602u);
+                o[4 * q + 0][h2] = __builtin_amdgcn_perm(a1, a0, 0x05040100u);
+                o[4 * q + 1][h2] = __builtin_amdgcn_perm(a1, a0, 0x07060302u);
+                o[4 * q + 2][h2] = __builtin_amdgcn_perm(b1, b0, 0x05040100u);
+                o[4 * q + 3][h2] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
+            }
+        // col = 4 np + 2 n2 + half: pieces of channels 32 np + 8 half + x, this
+        // lane's bytes 8 n2 ..; the lane with n2 = 0 writes x = 0..3, the other 4..7
+        const int n2 = (col >> 1) & 1;
+        uint4* to = dst + ((col >> 2) * 4 + grp) * 16 + 8 * (col & 1) + 4 * n2;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t give0 = n2 ? o[k][0] : o[k + 4][0], give1 = n2 ? o[k][1] : o[k + 4][1];
+            const uint32_t got0 = quad_xor2(give0), got1 = quad_xor2(give1);
+            const uint32_t mine0 = n2 ? o[k + 4][0] : o[k][0], mine1 = n2 ? o[k + 4][1] : o[k][1];
+            to[k] = n2 ? uint4{got0, got1, mine0, mine1} : uint4{mine0, mine1, got0, got1};
+        }
+    }
+}
+
+// ---------------------------------------------------------------- read-back
+
+struct ReadArgs {
+    const uint8_t* data[2];
+    const float* scale[2];
+    uint16_t* out[2];
+    int64_t sb[2], st[2], sh[2];
+    uint32_t* status;
+    Pages pg;
+    int B, H, blk0, nblk, n, nb_cap;
+    int total;
+    int aligned[2];
+};
+
+// Four code bytes to four floats.
+template <int FMT>
+__device__ __forceinline__ void floats4(uint32_t w, float (&f)[4]) {
+    if constexpr (FMT == DQ_Q8_E4M3) {
+        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false);
+        const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+        f[0] = lo[0];
+        f[1] = lo[1];
+        f[2] = hi[0];
+        f[3] = hi[1];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = (float)(int8_t)(w >> (8 * i));
+    }
+}
+
+// fp32 to bf16, ties to even (finite values)
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+    uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+    x += 0x7FFFu + ((x >> 16) & 1u);
+    y += 0x7FFFu + ((y >> 16) & 1u);
+    return __builtin_amdgcn_perm(y, x, 0x07060302u);
+}
+
+template <int FMT>
+__global__ __launch_bounds__(256) void q8_read_kernel(ReadArgs a) {
+    const int lane = threadIdx.x & (kWave - 1);
+    int w = wave_index(4);
+    const int which = w >= a.total;
+    if (which) w -= a.total;
+    if (w >= a.total) return;
+    const int h = w % a.H, rest = w / a.H;
+    const int blk = rest % a.nblk, b = rest / a.nblk;
+    bool bad = false;
+    const int64_t bi = block_index(a.pg, a.H, a.nb_cap, b, h, a.blk0 + blk, bad);
+    if (bad && lane == 0 && a.status) atomicOr(a.status, DQ_STATUS_PAGE);
+    const int rows = min(kBlk, a.n - blk * kBlk);
+    const float s = a.scale[which][bi];
+    const uint4* src = reinterpret_cast<const uint4*>(a.data[which] + bi * kBlkBytes);
+    const int64_t st = a.st[which];
+    uint16_t* dst = a.out[which] + (int64_t)b * a.sb[which] + (int64_t)h * a.sh[which] + (int64_t)blk * kBlk * st;
+    const int col = lane & 15, grp = lane >> 4;
+    const bool keys = which == 0;
+    uint32_t code[8][2];         // as in the encoder: 8 channels of one token per i
+    if (keys) {
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            const uint4 v = src[64 * p + lane];
+            code[2 * p][0] = v.x;
+            code[2 * p][1] = v.y;
+            code[2 * p + 1][0] = v.z;
+            code[2 * p + 1][1] = v.w;
+        }
+    } else {
+        const int n2 = (col >> 1) & 1;
+        const uint4* from = src + ((col >> 2) * 4 + grp) * 16 + 8 * (col & 1) + 4 * n2;
+        uint32_t o[8][2];
+        uint4 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = from[k];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t got0 = quad_xor2(n2 ? v[k].x : v[k].z), got1 = quad_xor2(n2 ? v[k].y : v[k].w);
+            const uint32_t mine0 = n2 ? v[k].z : v[k].x, mine1 = n2 ? v[k].w : v[k].y;
+            o[k][0] = n2 ? got0 : mine0;
+            o[k][1] = n2 ? got1 : mine1;
+            o[k + 4][0] = n2 ? mine0 : got0;
+            o[k + 4][1] = n2 ? mine1 : got1;
+        }
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const uint32_t c0 = o[4 * q][h2], c1 = o[4 * q + 1][h2], c2 = o[4 * q + 2][h2], c3 = o[4 * q + 3][h2];
+                const uint32_t a0 = __builtin_amdgcn_perm(c1, c0, 0x05010400u);
+                const uint32_t a1 = __builtin_amdgcn_perm(c3, c2, 0x05010400u);
+                const uint32_t b0 = __builtin_amdgcn_perm(c1, c0, 0x07030602u);
+                const uint32_t b1 = __builtin_amdgcn_perm(c3, c2, 0x07030602u);
+                code[4 * h2 + 0][q] = __builtin_amdgcn_perm(a1, a0, 0x05040100u);
+                code[4 * h2 + 1][q] = __builtin_amdgcn_perm(a1, a0, 0x07060302u);
+                code[4 * h2 + 2][q] = __builtin_amdgcn_perm(b1, b0, 0x05040100u);
+                code[4 * h2 + 3][q] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
+            }
+    }
+    const int row0 = keys ? col : 4 * grp;
+    const int ch0 = keys ? 16 * grp : 8 * col;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int t = row0 + 16 * (i >> 2) + (keys ? 0 : i & 3);
+        const int c = ch0 + (keys ? 64 * ((i >> 1) & 1) + 8 * (i & 1) : 0);
+        float f[4], g[4];
+        floats4<FMT>(code[i][0], f);
+        floats4<FMT>(code[i][1], g);
+        const uint4 v = {bf16_pair(f[0] * s, f[1] * s), bf16_pair(f[2] * s, f[3] * s),
+                         bf16_pair(g[0] * s, g[1] * s), bf16_pair(g[2] * s, g[3] * s)};
+        if (t < rows) {
+            uint16_t* p = dst + t * st + c;
+            if (a.aligned[which]) {
+                *reinterpret_cast<uint4*>(p) = v;
+            } else {
+                const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    p[2 * j] = (uint16_t)u[j];
+                    p[2 * j + 1] = (uint16_t)(u[j] >> 16);
+                }
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------- attention
+
+// Visible blocks of a sequence: the first `head` ones, then those from `from`
+// on; token t of them is visible if it is below the length and either below
+// `sinks` or at least `start`.
+struct Visible {
+    int T, sinks, start, head, from, count;
+};
+
+__device__ __forceinline__ Visible visible(int T, int extra, int window, int sinks) {
+    Visible v;
+    v.T = T;
+    const int nb = (T + kBlk - 1) / kBlk;
+    if (window <= 0) {
+        v.sinks = 0;
+        v.start = 0;
+        v.head = 0;
+        v.from = 0;
+    } else {
+        v.sinks = min(sinks, T);
+        const int64_t start = (int64_t)T + extra - window;
+        v.start = (int)max((int64_t)0, min(start, (int64_t)T));
+        v.head = (v.sinks + kBlk - 1) / kBlk;
+        // a block that the first tokens and the window share is listed once
+        v.from = max(v.head, v.start == T ? nb : v.start / kBlk);
+    }
+    v.count = v.head + max(0, nb - v.from);
+    return v;
+}
+
+struct Q8Args {
+    const uint16_t* q;
+    const uint8_t* k;
+    const float* ks;
+    const uint8_t* v;
+    const float* vs;
+    const int32_t* seq_lens;
+    const int32_t* extra_lens;   // tokens behind the cached ones, or NULL
+    Pages pg;
+    int Hq, Hkv, G, t_cap, chunk, nchunks, window, sinks;   // chunk in blocks
+    float scale_log2;
+    float* lse;                  // [B][Hkv][t_cap / 32][G], or NULL
+    uint32_t* status;
+    int32_t* ws_hdr;
+    float* ws_m;
+    float* ws_l;
+    float* ws_acc;
+};
+
+constexpr int kAWaves = 4;
+constexpr int kAThreads = kAWaves * kWave;
+constexpr int kGP = 8;                       // query-head slots
+constexpr float kBig = 3e38f;
+
+// Eight code bytes to eight fp16 values (exact for both types).
+template <int FMT>
+__device__ __forceinline__ f16x8 halves8(uint32_t lo, uint32_t hi) {
+    f16x2 h[4];
+    if constexpr (FMT == DQ_Q8_E4M3) {
+        h[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, 1.f, false);
+        h[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, 1.f, true);
+        h[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.f, false);
+        h[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.f, true);
+    } else {
+        // byte + 128 as the low bits of an fp16 in [1024, 2048), less 1152
+        const uint32_t magic = 0x64646464u;
+        const f16x2 off = {(_Float16)1152.f, (_Float16)1152.f};
+        lo ^= 0x80808080u;
+        hi ^= 0x80808080u;
+        h[0] = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(magic, lo, 0x04010400u)) - off;
+        h[1] = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(magic, lo, 0x04030402u)) - off;
+        h[2] = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(magic, hi, 0x04010400u)) - off;
+        h[3] = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(magic, hi, 0x04030402u)) - off;
+    }
+    f16x8 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        r[2 * i] = h[i][0];
+        r[2 * i + 1] = h[i][1];
+    }
+    return r;
+}
+
+__device__ __forceinline__ f32x4 mfma_f16(const f16x8& a, const f16x8& b, const f32x4& c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+__device__ __forceinline__ float clamp_big(float x) { return fminf(fmaxf(x, -kBig), kBig); }
+
+// One workgroup of four wavefronts per (chunk of visible blocks, KV head,
+// sequence); a wavefront takes every fourth block of the chunk and requests
+// the next one's 8 KB before it works on the one at hand.
+//   Scores: S^T (16 tokens x 16 columns) = K (16 x 128) Q^T on
+//   v_mfma_f32_16x16x32_f16.  Codes are exact in fp16, and so are the query's
+//   bf16 values once its largest is brought to 2^14 (its smaller ones down to
+//   2^-28 of it, the rest to 2^-39 of it).  Columns g and g + 8 both hold query
+//   head g.  Lane (grp, col) then has head col % 8 for tokens 16 h2 + 4 grp + i.
+//   Softmax online, in fp32 and base 2; the maximum is exchanged between the
+//   lanes of a head only when some lane exceeds it.
+//   Values: weights p 2^15 are split into two fp16 terms (22 bits, down to
+//   weights of 2^-18 of the largest), the first in the rows of heads 0..7, the
+//   second (times 2^11) in rows 8..15: one product of the 32 tokens gives both,
+//   its operand the weights as they lie.  The block's scale is applied to the
+//   product's fp32 result.
+template <int FMT, bool TRACK>
+__global__ __launch_bounds__(kAThreads) void q8_partial_kernel(Q8Args a) {
+    __shared__ float wm[kAWaves][kGP], wl[kAWaves][kGP];
+    __shared__ __align__(16) float wacc[kAWaves][kGP][kD];
+    const int c = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int G = a.G, NC = a.nchunks, nb_cap = a.t_cap / kBlk;
+    if ((c | h | b) == 0 && tid == 0) {
+        // a windowed step fills every chunk's slot, for whatever length: the
+        // merge takes min(chunks, ceil(T / 1)) of them, and chunk c >= T is empty
+        a.ws_hdr[0] = a.window > 0 ? 1 : a.chunk * kBlk;
+        a.ws_hdr[1] = NC;
+        a.ws_hdr[2] = 0;
+        a.ws_hdr[3] = 0;          // values are in the caller's basis
+    }
+    const int T = max(0, min(a.seq_lens[b], a.t_cap));
+    const int extra = a.extra_lens ? max(0, a.extra_lens[b]) : 0;
+    const Visible vis = visible(T, extra, a.window, a.sinks);
+    const int v0 = c * a.chunk, v1 = min(v0 + a.chunk, vis.count);
+    const int64_t slot0 = ((int64_t)b * a.Hq + h * G) * (NC + kResSlots) + c;
+    if (v0 >= v1) {
+        if (a.window > 0) {
+            for (int i = tid; i < G * kD; i += kAThreads) {
+                const int64_t slot = slot0 + (int64_t)(i / kD) * (NC + kResSlots);
+                a.ws_acc[slot * kD + i % kD] = 0.f;
+                if (i % kD == 0) {
+                    a.ws_m[slot] = -INFINITY;
+                    a.ws_l[slot] = 0.f;
+                }
+            }
+        }
+        return;                   // without a window the merge ignores the chunk
+    }
+    const int col = lane & 15, grp = lane >> 4, head = col & 7;
+
+    // ---- the query, scaled to fp16, in the columns of its head
+    f16x8 qb[4];                  // channels 64 (i / 2) + 16 grp + 8 (i % 2) ..
+    float c_head, bad_q;
+    {
+        uint16_t raw[4][8];
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                raw[i][e] = 0;
+                if (head < G)
+                    raw[i][e] = a.q[((int64_t)b * a.Hq + h * G + head) * kD + 64 * (i >> 1) + 16 * grp +
+                                    8 * (i & 1) + e];
+                top = max(top, (uint32_t)(raw[i][e] & 0x7FFF));
+            }
+        float m = __uint_as_float(top << 16);        // orders as the integer (NaN handled below)
+        const bool nonfinite = top >= 0x7F80;
+        bad_q = nonfinite ? 1.f : 0.f;
+        bad_q = fmaxf(bad_q, xor_lane<16>(bad_q, lane));
+        bad_q = fmaxf(bad_q, xor_lane<32>(bad_q, lane));
+        if (nonfinite) m = 0.f;
+        m = fmaxf(m, xor_lane<16>(m, lane));
+        m = fmaxf(m, xor_lane<32>(m, lane));
+        const int ex = bad_q > 0.f || m == 0.f ? 0 : ilogbf(m);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float f = ldexpf(bf16_to_f32(raw[i][e]), 14 - ex);
+                qb[i][e] = bad_q > 0.f ? (_Float16)0.f : (_Float16)f;
+            }
+        c_head = ldexpf(a.scale_log2, ex - 14);
+    }
+
+    float m_run = -3.4e38f, l_run = 0.f;
+    f32x4 acc[8];
+#pragma unroll
+    for (int n = 0; n < 8; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    bool bad = false;
+    auto block_of = [&](int v) { return v < vis.head ? v : vis.from + v - vis.head; };
+    uint4 kr[4], vr[4];
+    float ks, vs;
+    auto request = [&](int v) {
+        const int blk = block_of(v);
+        const int64_t bi = block_index(a.pg, a.Hkv, nb_cap, b, h, blk, bad);
+        const uint4* kp = reinterpret_cast<const uint4*>(a.k + bi * kBlkBytes) + lane;
+        const uint4* vp = reinterpret_cast<const uint4*>(a.v + bi * kBlkBytes) + lane;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) kr[i] = kp[64 * i];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) vr[i] = vp[64 * i];
+        ks = a.ks[bi];
+        vs = a.vs[bi];
+    };
+    int v = v0 + wave;
+    if (v < v1) request(v);
+    while (v < v1) {
+        uint4 kc[4], vc[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            kc[i] = kr[i];
+            vc[i] = vr[i];
+        }
+        const float ksc = ks, vsc = vs * 0x1p-15f;
+        const int blk = block_of(v), t0 = blk * kBlk;
+        const int vn = v + kAWaves;
+        if (vn < v1) request(vn);
+
+        // ---- scores in base 2
+        float x[8];
+        const float cf = clamp_big(ksc * c_head);
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2) {
+            f32x4 d = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const uint4 w = kc[2 * h2 + j];
+                d = mfma_f16(halves8<FMT>(w.x, w.y), qb[2 * j], d);
+                d = mfma_f16(halves8<FMT>(w.z, w.w), qb[2 * j + 1], d);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[4 * h2 + i] = clamp_big(d[i] * cf);
+        }
+        const bool whole = t0 + kBlk <= T && (t0 >= vis.start || t0 + kBlk <= vis.sinks);
+        if (!whole) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int t = t0 + 16 * (e >> 2) + 4 * grp + (e & 3);
+                if (!(t < T && (t >= vis.start || t < vis.sinks))) x[e] = -INFINITY;
+            }
+            // rows past the length may hold anything: no code stays
+            uint32_t keep[2] = {0u, 0u};
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (t0 + 16 * (e >> 2) + 4 * grp + (e & 3) < T) keep[e >> 2] |= 0xFFu << (8 * (e & 3));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                vc[i].x &= keep[0];
+                vc[i].y &= keep[1];
+                vc[i].z &= keep[0];
+                vc[i].w &= keep[1];
+            }
+        }
+
+        // ---- online softmax of head col % 8
+        float mt = x[0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) mt = fmaxf(mt, x[e]);
+        if (__builtin_amdgcn_ballot_w64(mt > m_run)) {
+            mt = fmaxf(mt, xor_lane<16>(mt, lane));
+            mt = fmaxf(mt, xor_lane<32>(mt, lane));
+            const float mn = fmaxf(m_run, mt);
+            const float corr = __builtin_amdgcn_exp2f(m_run - mn);
+            m_run = mn;
+            l_run *= corr;
+            float cr[4];          // of the accumulators' rows: head (4 grp + i) % 8
+#pragma unroll
+            for (int i = 0; i < 4; ++i) cr[i] = __shfl(corr, (4 * grp + i) & 7);
+#pragma unroll
+            for (int n = 0; n < 8; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[n][i] *= cr[i];
+        }
+        float ps = 0.f;
+        f16x8 w;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float p = __builtin_amdgcn_exp2f(x[e] - m_run);
+            ps += p;
+            const float f = p * 0x1p15f;
+            const _Float16 hi = (_Float16)f;
+            const _Float16 lo = (_Float16)((f - (float)hi) * 0x1p11f);
+            w[e] = col < 8 ? hi : lo;
+        }
+        l_run += ps;
+        if constexpr (TRACK) {
+            float bs = ps + xor_lane<16>(ps, lane);
+            bs += xor_lane<32>(bs, lane);
+            if (lane < G) a.lse[(((int64_t)b * a.Hkv + h) * nb_cap + blk) * G + lane] = log2f(bs) + m_run;
+        }
+
+        // ---- weighted values
+        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            const f32x4 d0 = mfma_f16(w, halves8<FMT>(vc[n].x, vc[n].y), zero);
+            const f32x4 d1 = mfma_f16(w, halves8<FMT>(vc[n].z, vc[n].w), zero);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                acc[2 * n][i] = fmaf(d0[i], vsc, acc[2 * n][i]);
+                acc[2 * n + 1][i] = fmaf(d1[i], vsc, acc[2 * n + 1][i]);
+            }
+        }
+        v = vn;
+    }
+    if (bad && lane == 0 && a.status) atomicOr(a.status, DQ_STATUS_PAGE);
+
+    // ---- the two terms of a weight, then the wavefronts
+    l_run += xor_lane<16>(l_run, lane);
+    l_run += xor_lane<32>(l_run, lane);
+#pragma unroll
+    for (int n = 0; n < 8; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float lo = xor_lane<32>(acc[n][i], lane);
+            if (grp < 2) wacc[wave][4 * grp + i][16 * n + col] = fmaf(lo, 0x1p-11f, acc[n][i]);
+        }
+    if (lane < kGP) {
+        wm[wave][lane] = m_run;
+        wl[wave][lane] = bad_q > 0.f ? NAN : l_run;
+    }
+    __syncthreads();
+    for (int i = tid; i < G * kD; i += kAThreads) {
+        const int g = i / kD, j = i % kD;
+        float M = wm[0][g];
+#pragma unroll
+        for (int u = 1; u < kAWaves; ++u) M = fmaxf(M, wm[u][g]);
+        float s = 0.f, l = 0.f;
+#pragma unroll
+        for (int u = 0; u < kAWaves; ++u) {
+            const float e = exp2f(wm[u][g] - M);
+            s = fmaf(wacc[u][g][j], e, s);
+            l = fmaf(wl[u][g], e, l);
+        }
+        const int64_t slot = slot0 + (int64_t)g * (NC + kResSlots);
+        a.ws_acc[slot * kD + j] = s;
+        if (j == 0) {
+            a.ws_m[slot] = l == 0.f ? -INFINITY : M;
+            a.ws_l[slot] = l;
+        }
+    }
+}
+
+// ------------------------------------------------------------------- scores
+
+struct ScoreArgs {
+    const int32_t* seq_lens;
+    const int32_t* extra_lens;
+    const float* lse;
+    const int32_t* ws_hdr;
+    const float* ws_m;
+    const float* ws_l;
+    float* scores;
+    int Hq, Hkv, G, t_cap, window, sinks, nc_max;
+};
+
+// scores[b][h][blk] += sum_g 2^(lse of the block - lse of all the step's
+// tokens).  The latter comes from the partials' maxima and sums, once per
+// workgroup; a thread takes one visible block.
+__global__ __launch_bounds__(256) void q8_scores_kernel(ScoreArgs a) {
+    __shared__ float total[kGP];
+    const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
+    const int lane = tid & (kWave - 1), wave = tid / kWave;
+    const int G = a.G;
+    const int chunk = max(a.ws_hdr[0], 1), NC = min(max(a.ws_hdr[1], 1), a.nc_max);
+    const int residual = min(max(a.ws_hdr[2], 0), kResSlots);
+    const int T = max(0, min(a.seq_lens[b], a.t_cap));
+    const int extra = a.extra_lens ? max(0, a.extra_lens[b]) : 0;
+    const Visible vis = visible(T, extra, a.window, a.sinks);
+    const int v = blockIdx.x * 256 + tid;
+    if ((int)blockIdx.x * 256 >= vis.count) return;
+    const int nc = (int)min((int64_t)NC, ((int64_t)T + chunk - 1) / chunk), np = nc + residual;
+    for (int g = wave; g < G; g += 4) {
+        const int64_t base = ((int64_t)b * a.Hq + h * G + g) * (NC + kResSlots);
+        float M = -INFINITY;
+        for (int i = lane; i < np; i += kWave) M = fmaxf(M, a.ws_m[base + (i < nc ? i : NC + i - nc)]);
+        M = wave_max(M);
+        float l = 0.f;
+        if (M != -INFINITY)
+            for (int i = lane; i < np; i += kWave) {
+                const int64_t s = base + (i < nc ? i : NC + i - nc);
+                l += a.ws_l[s] * exp2f(a.ws_m[s] - M);
+            }
+        l = wave_sum(l);
+        if (lane == 0) total[g] = M == -INFINITY ? INFINITY : M + log2f(l);
+    }
+    __syncthreads();
+    if (v >= vis.count) return;
+    const int blk = v < vis.head ? v : vis.from + v - vis.head;
+    const int64_t i = ((int64_t)b * a.Hkv + h) * (a.t_cap / kBlk) + blk;
+    float w = 0.f;
+    for (int g = 0; g < G; ++g) w += exp2f(a.lse[i * G + g] - total[g]);
+    a.scores[i] += w;
+}
+
+// ----------------------------------------------------------------- eviction
+
+struct EvictArgs {
+    const int32_t* seq_lens;
+    int32_t* new_lens;
+    int32_t* kept;               // [B][H][keep]
+    const float* scores;         // [B][H][nb_cap]
+    float* to_scores;            // [B][H][to_cap]
+    const uint8_t* data[2];
+    const float* scale[2];
+    uint8_t* to_data[2];
+    float* to_scale[2];
+    uint32_t* status;
+    Pages pg;
+    int H, t_cap, nb_cap, to_cap, keep, first, last;   // blocks
+    int parts;
+};
+
+constexpr int kSelThreads = 256;
+
+// Floats as unsigned integers of the same order (both zeros equal); NaN lowest.
+__device__ __forceinline__ uint32_t order_key(float x) {
+    if (x != x) return 0u;
+    const uint32_t u = __float_as_uint(x + 0.f);
+    return (u >> 31) ? ~u : u | 0x80000000u;
+}
+
+// One workgroup per (KV head, sequence) chooses the blocks: a radix selection
+// over the 32-bit keys of the blocks that are neither among the first nor the
+// newest finds the smallest kept key and how many of its ties are kept (the
+// lowest indexes), then one scan in block order writes the list and moves the
+// scores and the two scales, each to a place at or before its own.
+__global__ __launch_bounds__(kSelThreads) void q8_select_kernel(EvictArgs a) {
+    __shared__ uint32_t hist[256];
+    __shared__ uint32_t s_bin, s_rem;
+    __shared__ int s_tie[kSelThreads / kWave], s_kept[kSelThreads / kWave];
+    const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+    const int lane = tid & (kWave - 1), wave = tid / kWave;
+    const int T = max(0, min(a.seq_lens[b], a.t_cap));
+    const int nb = (T + kBlk - 1) / kBlk;
+    const int64_t row = (int64_t)b * a.H + h;
+    const float* sc = a.scores + row * a.nb_cap;
+    float* to = a.to_scores + row * a.to_cap;
+    int32_t* kept = a.kept + row * a.keep;
+    const bool cut = nb > a.keep;
+    const int lo = cut ? a.first : nb, hi = cut ? nb - a.last : nb;   // the blocks to choose from
+    uint32_t prefix = 0, rem = cut ? (uint32_t)(a.keep - a.first - a.last) : 0u;
+    if (cut && rem > 0) {
+        for (int shift = 24; shift >= 0; shift -= 8) {
+            hist[tid] = 0u;
+            __syncthreads();
+            for (int i = lo + tid; i < hi; i += kSelThreads) {
+                const uint32_t key = order_key(sc[i]);
+                if (shift == 24 || (key >> (shift + 8)) == prefix) atomicAdd(&hist[(key >> shift) & 255u], 1u);
+            }
+            __syncthreads();
+            if (wave == 0) {
+                // bins 4 (63 - lane) + 3 .. 4 (63 - lane), from the top
+                const int bin = 4 * (63 - lane);
+                uint32_t n[4], own = 0;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    n[k] = hist[bin + 3 - k];
+                    own += n[k];
+                }
+                uint32_t incl = own;
+                for (int d = 1; d < kWave; d <<= 1) {
+                    const uint32_t o = __shfl_up(incl, d);
+                    if (lane >= d) incl += o;
+                }
+                uint32_t before = incl - own;
+                if (before < rem && rem <= incl) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        if (before < rem && rem <= before + n[k]) {
+                            s_bin = (uint32_t)(bin + 3 - k);
+                            s_rem = rem - before;
+                        }
+                        before += n[k];
+                    }
+                }
+            }
+            __syncthreads();
+            prefix = (prefix << 8) | s_bin;
+            rem = s_rem;
+        }
+    }
+    // keys above `prefix` are kept, and the first `rem` equal to it
+    const bool choose = cut && a.keep > a.first + a.last;
+    int ties = 0, n = 0;                                  // of the blocks before this round
+    for (int i0 = 0; i0 < nb; i0 += kSelThreads) {
+        const int i = i0 + tid;
+        bool tie = false, keep = false;
+        float s = 0.f, x[2] = {0.f, 0.f};
+        bool bad = false;
+        if (i < nb) {
+            s = sc[i];
+            const int64_t bi = block_index(a.pg, a.H, a.nb_cap, b, h, i, bad);
+            x[0] = a.scale[0][bi];
+            x[1] = a.scale[1][bi];
+            keep = i < lo || i >= hi;
+            if (!keep && choose) {
+                const uint32_t key = order_key(s);
+                keep = key > prefix;
+                tie = key == prefix;
+            }
+        }
+        const uint64_t tb = __builtin_amdgcn_ballot_w64(tie);
+        const uint64_t below = (1ull << lane) - 1ull;
+        if (lane == 0) s_tie[wave] = __popcll(tb);
+        __syncthreads();
+        int t = ties + __popcll(tb & below);
+#pragma unroll
+        for (int u = 0; u < kSelThreads / kWave; ++u) {
+            if (u < wave) t += s_tie[u];
+            ties += s_tie[u];
+        }
+        if (tie && t < (int)rem) keep = true;
+        const uint64_t kb = __builtin_amdgcn_ballot_w64(keep);
+        if (lane == 0) s_kept[wave] = __popcll(kb);
+        __syncthreads();
+        int pos = n + __popcll(kb & below);
+#pragma unroll
+        for (int u = 0; u < kSelThreads / kWave; ++u) {
+            if (u < wave) pos += s_kept[u];
+            n += s_kept[u];
+        }
+        if (keep) {
+            kept[pos] = i;
+            to[pos] = s;
+            bool tbad = false;
+            const int64_t ti = block_index(a.pg, a.H, a.to_cap, b, h, pos, tbad);
+            if (!tbad) {
+                a.to_scale[0][ti] = x[0];
+                a.to_scale[1][ti] = x[1];
+            }
+            if ((bad || tbad) && a.status) atomicOr(a.status, DQ_STATUS_PAGE);
+        }
+        __syncthreads();
+    }
+    for (int i = n + tid; i < a.keep; i += kSelThreads) kept[i] = -1;
+    for (int i = n + tid; i < min(nb, a.to_cap); i += kSelThreads) to[i] = 0.f;
+}
+
+// The kept blocks' codes move to their places, which lie at or before their
+// old ones, in order.  A wavefront owns 256 bytes of every block of one (KV
+// head, sequence) and tensor and walks through the list: it reads 4 kMoveU
+// blocks' pieces, waits for all of them and writes them.  What it writes to has
+// been read by itself before, so no wavefront waits for another; into another
+// cache nothing overlaps and the list is cut into parts as well.
+constexpr int kMoveU = 8;
+
+__global__ __launch_bounds__(kWave) void q8_move_kernel(EvictArgs a) {
+    const int slice = blockIdx.x & 31, part = blockIdx.x >> 5, h = blockIdx.y, b = blockIdx.z;
+    const int lane = threadIdx.x;
+    if (blockIdx.x == 0 && h == 0 && lane == 0) {
+        const int T = max(0, min(a.seq_lens[b], a.t_cap));   // read by nobody else: it may be new_lens[b]
+        const int nb = (T + kBlk - 1) / kBlk;
+        a.new_lens[b] = T - max(0, nb - a.keep) * kBlk;
+    }
+    const int which = slice >> 4, off = (slice & 15) * 256 + (lane & 15) * 16;
+    const int32_t* kept = a.kept + ((int64_t)b * a.H + h) * a.keep;
+    const int per = (a.keep + a.parts - 1) / a.parts;
+    const int end = min(a.keep, (part + 1) * per);
+    for (int i0 = part * per; i0 < end; i0 += 4 * kMoveU) {
+        if (kept[i0] < 0) break;      // the list ends
+        uint4 x[kMoveU];
+        uint4* to[kMoveU];
+#pragma unroll
+        for (int u = 0; u < kMoveU; ++u) {
+            const int i = i0 + 4 * u + (lane >> 4);
+            to[u] = nullptr;
+            if (i < end) {
+                const int from = kept[i];
+                if (from >= 0) {
+                    bool bad = false;
+                    const int64_t si = block_index(a.pg, a.H, a.nb_cap, b, h, from, bad);
+                    const int64_t di = block_index(a.pg, a.H, a.to_cap, b, h, i, bad);
+                    const uint8_t* src = a.data[which] + si * kBlkBytes + off;
+                    uint8_t* dst = a.to_data[which] + di * kBlkBytes + off;
+                    if (!bad && src != dst) {
+                        x[u] = *reinterpret_cast<const uint4*>(src);
+                        to[u] = reinterpret_cast<uint4*>(dst);
+                    }
+                }
+            }
+        }
+        // every read of the round is back before the first write
+        __builtin_amdgcn_s_waitcnt(0);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int u = 0; u < kMoveU; ++u)
+            if (to[u]) *to[u] = x[u];
+    }
+}
+
+}  // namespace
+
+// ---------------------------------------------------------------- launchers
+
+static bool rows_aligned(const void* p, int64_t sb, int64_t st, int64_t sh) {
+    return ((reinterpret_cast<uintptr_t>(p) & 15) | ((sb | st | sh) & 7)) == 0;
+}
+
+int launch_q8_encode(int format, const Pages& pg, const Q8Rows& k, const Q8Rows& v, int32_t B, int32_t H, int32_t t0,
+                     int32_t n_new, int32_t t_cap, const Q8Cache& to, uint32_t* status, hipStream_t stream) {
+    EncArgs a;
+    const Q8Rows* rows[2] = {&k, &v};
+    for (int i = 0; i < 2; ++i) {
+        a.x[i] = rows[i]->p;
+        a.sb[i] = rows[i]->sb;
+        a.st[i] = rows[i]->st;
+        a.sh[i] = rows[i]->sh;
+        a.aligned[i] = rows_aligned(a.x[i], a.sb[i], a.st[i], a.sh[i]);
+        a.data[i] = to.data[i];
+        a.scale[i] = to.scale[i];
+    }
+    a.status = status;
+    a.pg = pg;
+    a.B = B;
+    a.H = H;
+    a.blk0 = t0 / kBlk;
+    a.nblk = (n_new + kBlk - 1) / kBlk;
+    a.n_new = n_new;
+    a.nb_cap = t_cap / kBlk;
+    const int64_t total = (int64_t)B * H * a.nblk;
+    if (total > (1 << 30)) return DQ_ERR_INVALID_ARG;
+    a.total = (int)total;
+    const dim3 grid((unsigned)((2 * total + 3) / 4));
+    if (format == DQ_Q8_E4M3)
+        q8_encode_kernel<DQ_Q8_E4M3><<<grid, 256, 0, stream>>>(a);
+    else
+        q8_encode_kernel<DQ_Q8_INT8><<<grid, 256, 0, stream>>>(a);
+    return hip_check("q8_encode launch", hipGetLastError());
+}
+
+int launch_q8_read(int format, const Pages& pg, const Q8Cache& from, int32_t B, int32_t H, int32_t t0, int32_t n,
+                   int32_t t_cap, const Q8Rows& k, const Q8Rows& v, uint32_t* status, hipStream_t stream) {
+    ReadArgs a;
+    const Q8Rows* rows[2] = {&k, &v};
+    for (int i = 0; i < 2; ++i) {
+        a.out[i] = const_cast<uint16_t*>(rows[i]->p);
+        a.sb[i] = rows[i]->sb;
+        a.st[i] = rows[i]->st;
+        a.sh[i] = rows[i]->sh;
+        a.aligned[i] = rows_aligned(a.out[i], a.sb[i], a.st[i], a.sh[i]);
+        a.data[i] = from.data[i];
+        a.scale[i] = from.scale[i];
+    }
+    a.status = status;
+    a.pg = pg;
+    a.B = B;
+    a.H = H;
+    a.blk0 = t0 / kBlk;
+    a.nblk = (n + kBlk - 1) / kBlk;
+    a.n = n;
+    a.nb_cap = t_cap / kBlk;
+    const int64_t total = (int64_t)B * H * a.nblk;
+    if (total > (1 << 30)) return DQ_ERR_INVALID_ARG;
+    a.total = (int)total;
+    const dim3 grid((unsigned)((2 * total + 3) / 4));
+    if (format == DQ_Q8_E4M3)
+        q8_read_kernel<DQ_Q8_E4M3><<<grid, 256, 0, stream>>>(a);
+    else
+        q8_read_kernel<DQ_Q8_INT8><<<grid, 256, 0, stream>>>(a);
+    return hip_check("q8_read launch", hipGetLastError());
+}
+
+namespace {
+
+// Chunks of visible blocks: about six workgroups per CU but at most 64 chunks
+// per sequence (the merge takes 64 partials in one pass, one per lane), at
+// least one block for every wavefront.
+struct Q8Plan {
+    int chunk, nchunks;          // blocks per chunk, chunks
+};
+
+Q8Plan q8_plan(int B, int Hkv, int t_cap, int window, int sinks) {
+    int64_t nb = t_cap / kBlk;
+    if (window > 0) {
+        // a window of w tokens meets at most w / 32 + 2 blocks
+        const int64_t seen = ((int64_t)sinks + kBlk - 1) / kBlk + (int64_t)window / kBlk + 2;
+        nb = std::min(nb, seen);
+    }
+    const int64_t pairs = (int64_t)B * Hkv;
+    const int64_t nc = std::max<int64_t>(1, std::min<int64_t>((6 * cu_count() + pairs - 1) / pairs, 64));
+    int64_t chunk = (nb + nc - 1) / nc;
+    chunk = std::max<int64_t>((chunk + kAWaves - 1) / kAWaves * kAWaves, kAWaves);
+    return Q8Plan{(int)chunk, (int)((nb + chunk - 1) / chunk)};
+}
+
+}  // namespace
+
+int launch_q8_partial(int format, const Pages& pg, const uint16_t* q, int32_t B, int32_t Hq, int32_t Hkv,
+                      const Q8Cache& c, const int32_t* seq_lens, const int32_t* extra_lens, int32_t t_cap,
+                      int32_t window, int32_t sinks, float scale, float* lse, void* ws, uint32_t* status,
+                      hipStream_t stream) {
+    const Q8Plan plan = q8_plan(B, Hkv, t_cap, window, sinks);
+    Q8Args a;
+    a.q = q;
+    a.k = c.data[0];
+    a.ks = c.scale[0];
+    a.v = c.data[1];
+    a.vs = c.scale[1];
+    a.seq_lens = seq_lens;
+    a.extra_lens = extra_lens;
+    a.pg = pg;
+    a.Hq = Hq;
+    a.Hkv = Hkv;
+    a.G = Hq / Hkv;
+    a.t_cap = t_cap;
+    a.chunk = plan.chunk;
+    a.nchunks = plan.nchunks;
+    a.window = window;
+    a.sinks = sinks;
+    a.scale_log2 = scale * 1.4426950408889634f;
+    a.lse = lse;
+    a.status = status;
+    const int64_t slots = ws_slots(B, Hq, t_cap);
+    a.ws_hdr = static_cast<int32_t*>(ws);
+    a.ws_acc = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + kWsHeader);
+    a.ws_m = a.ws_acc + slots * kD;
+    a.ws_l = a.ws_m + slots;
+    const dim3 grid(a.nchunks, Hkv, B);
+    if (format == DQ_Q8_E4M3) {
+        if (lse)
+            q8_partial_kernel<DQ_Q8_E4M3, true><<<grid, kAThreads, 0, stream>>>(a);
+        else
+            q8_partial_kernel<DQ_Q8_E4M3, false><<<grid, kAThreads, 0, stream>>>(a);
+    } else {
+        if (lse)
+            q8_partial_kernel<DQ_Q8_INT8, true><<<grid, kAThreads, 0, stream>>>(a);
+        else
+            q8_partial_kernel<DQ_Q8_INT8, false><<<grid, kAThreads, 0, stream>>>(a);
+    }
+    return hip_check("q8_partial launch", hipGetLastError());
+}
+
+int launch_q8_scores(int32_t B, int32_t Hq, int32_t Hkv, const int32_t* seq_lens, const int32_t* extra_lens,
+                     int32_t t_cap, int32_t window, int32_t sinks, const float* lse, const void* ws, float* scores,
+                     hipStream_t stream) {
+    const int64_t slots = ws_slots(B, Hq, t_cap);
+    ScoreArgs a;
+    a.seq_lens = seq_lens;
+    a.extra_lens = extra_lens;
+    a.lse = lse;
+    a.ws_hdr = static_cast<const int32_t*>(ws);
+    a.ws_m = reinterpret_cast<const float*>(static_cast<const uint8_t*>(ws) + kWsHeader) + slots * kD;
+    a.ws_l = a.ws_m + slots;
+    a.scores = scores;
+    a.Hq = Hq;
+    a.Hkv = Hkv;
+    a.G = Hq / Hkv;
+    a.t_cap = t_cap;
+    a.window = window;
+    a.sinks = sinks;
+    a.nc_max = (int)(slots / ((int64_t)B * Hq)) - kResSlots;
+    const Q8Plan plan = q8_plan(B, Hkv, t_cap, window, sinks);
+    const int64_t blocks = (int64_t)plan.chunk * plan.nchunks;   // at least the visible ones
+    q8_scores_kernel<<<dim3((unsigned)((blocks + 255) / 256), Hkv, B), 256, 0, stream>>>(a);
+    return hip_check("q8_scores launch", hipGetLastError());
+}
+
+int launch_q8_evict(const Pages& pg, int32_t B, int32_t H, const int32_t* seq_lens, int32_t* new_lens, int32_t t_cap,
+                    int32_t to_cap, int32_t keep, int32_t first, int32_t last, const float* scores,
+                    float* to_scores, const Q8Cache& from, const Q8Cache& to, int32_t* kept, uint32_t* status,
+                    hipStream_t stream) {
+    EvictArgs a;
+    a.seq_lens = seq_lens;
+    a.new_lens = new_lens;
+    a.kept = kept;
+    a.scores = scores;
+    a.to_scores = to_scores;
+    for (int i = 0; i < 2; ++i) {
+        a.data[i] = from.data[i];
+        a.scale[i] = from.scale[i];
+        a.to_data[i] = to.data[i];
+        a.to_scale[i] = to.scale[i];
+    }
+    a.status = status;
+    a.pg = pg;
+    a.H = H;
+    a.t_cap = t_cap;
+    a.nb_cap = t_cap / kBlk;
+    a.to_cap = to_cap / kBlk;
+    a.keep = keep / kBlk;
+    a.first = first / kBlk;
+    a.last = last / kBlk;
+    q8_select_kernel<<<dim3(H, B), kSelThreads, 0, stream>>>(a);
+    if (int rc = hip_check("q8_select launch", hipGetLastError())) return rc;
+    // into another cache: parts of at least one round of a wavefront, up to
+    // about 16 wavefronts per CU
+    a.parts = 1;
+    if (a.data[0] != a.to_data[0]) {
+        const int64_t waves = 32LL * B * H;
+        a.parts = (int)std::max<int64_t>(
+            1, std::min<int64_t>((16 * cu_count() + waves - 1) / waves, (a.keep + 4 * kMoveU - 1) / (4 * kMoveU)));
+    }
+    q8_move_kernel<<<dim3(32 * a.parts, H, B), kWave, 0, stream>>>(a);
+    return hip_check("q8_move launch", hipGetLastError());
+}
+
+}  // namespace dq
