@@ -490,7 +490,8 @@ int dq_q8_decode_kv_paged(int32_t format, const uint8_t* k_pool, const float* k_
 /*
  * One decode step of attention over the 8-bit cache: logits softmax_scale *
  * q . k^, output sum a v^, as dq_decode_attention over records.
- *   q:  bf16 [batch][q_heads][128];  out: fp32 [batch][q_heads][128]
+ *   q:  bf16 [batch][q_heads][128], 16-byte aligned
+ *   out: fp32 [batch][q_heads][128], 8-byte aligned
  *   seq_lens: device int32 [batch], tokens in the cache (each in [0, t_cap])
  *   window, sinks: window = 0: every token is visible (sinks has to be 0).
  *       window > 0: token t is visible if it is among the first `sinks` or

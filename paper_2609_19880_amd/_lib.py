@@ -685,21 +685,16 @@ def _q8_format(fmt) -> int:
     return f
 
 
-def _q8_here(t):
-    """The raw stream to enqueue on: the current one of the current device,
-    which has to be the tensors' own."""
-    dev = t.get_device()
-    _need(dev == torch.cuda.current_device(), "tensors must be on the current device")
-    return torch._C._cuda_getCurrentRawStream(dev)
-
-
 def _q8_stream(t, stream):
-    here = _q8_here(t)
-    return here if stream is None else int(stream.cuda_stream)
+    """The raw stream to enqueue on; the tensors have to be on the current device."""
+    dev = t.get_device()
+    _need(dev == torch._C._cuda_getDevice(), "tensors must be on the current device")
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else int(stream.cuda_stream)
 
 
 def _q8_cache_args(k_data, k_scale, v_data, v_scale):
-    """Shape (rows, heads, blocks) of a cache's or pool's four arrays."""
+    """Shape (rows, heads, blocks) of a cache's or pool's four arrays, their GPU
+    and their addresses."""
     shape = k_scale.shape
     _need(k_data.dtype == torch.uint8 and k_data.is_contiguous() and k_data.dim() == 4
           and k_data.shape[:3] == shape and k_data.shape[3] == _Q8_BYTES, "k_data must be uint8 [.., H, blocks, 4096]")
@@ -710,7 +705,7 @@ def _q8_cache_args(k_data, k_scale, v_data, v_scale):
     dev = k_data.device
     _need(dev.type == "cuda" and v_data.device == dev and k_scale.device == dev and v_scale.device == dev,
           "the cache must be on one GPU")
-    return shape
+    return (*shape, dev, (k_data.data_ptr(), k_scale.data_ptr(), v_data.data_ptr(), v_scale.data_ptr()))
 
 
 def _q8_rows_args(k, v, heads, dev):
@@ -739,21 +734,21 @@ def _q8_lens(t, batch, dev, name="seq_lens"):
     return t.data_ptr()
 
 
+def _q8_encode(fmt: int, cache, k, v, t0, status, stream):
+    B, H, nb, dev, at = cache
+    n, T = _q8_rows_args(k, v, H, dev)
+    _need(n == B, "k and the cache must have the same batch")
+    _need(0 <= t0 <= _INT_MAX, "t0")
+    rc = _lib.dq_q8_encode_kv(fmt, k.data_ptr(), *k.stride()[:3], v.data_ptr(), *v.stride()[:3], B, H, t0, T,
+                              nb * DQ_Q8_BLOCK, *at, _q8_status(status, dev), _q8_stream(k, stream))
+    _check(rc, "dq_q8_encode_kv")
+
+
 def dq_q8_encode_kv(fmt, k, v, t0: int, k_data, k_scale, v_data, v_scale, status=None, stream=None):
     """Append k, v (bf16 [B, T_new, H, 128], any strides but channels) at cache
     position t0, a multiple of 32.  k_data, v_data uint8 [B, H, t_cap/32, 4096];
     k_scale, v_scale fp32 [B, H, t_cap/32]."""
-    f = _q8_format(fmt)
-    B, H, nb = _q8_cache_args(k_data, k_scale, v_data, v_scale)
-    n, T = _q8_rows_args(k, v, H, k_data.device)
-    _need(n == B, "k and the cache must have the same batch")
-    _need(0 <= t0 <= _INT_MAX, "t0")
-    s = _q8_stream(k, stream)
-    rc = _lib.dq_q8_encode_kv(f, k.data_ptr(), k.stride(0), k.stride(1), k.stride(2), v.data_ptr(), v.stride(0),
-                              v.stride(1), v.stride(2), B, H, t0, T, nb * DQ_Q8_BLOCK, k_data.data_ptr(),
-                              k_scale.data_ptr(), v_data.data_ptr(), v_scale.data_ptr(),
-                              _q8_status(status, k_data.device), s)
-    _check(rc, "dq_q8_encode_kv")
+    _q8_encode(_q8_format(fmt), _q8_cache_args(k_data, k_scale, v_data, v_scale), k, v, t0, status, stream)
 
 
 def dq_q8_encode_kv_paged(fmt, k, v, t0: int, block_table, k_pool, k_scale_pool, v_pool, v_scale_pool, status=None,
@@ -761,59 +756,52 @@ def dq_q8_encode_kv_paged(fmt, k, v, t0: int, block_table, k_pool, k_scale_pool,
     """dq_q8_encode_kv into pool pages: pools uint8 [num_pages, H, page/32, 4096],
     scales fp32 [num_pages, H, page/32]; block_table int32 [B, max_pages]."""
     f = _q8_format(fmt)
-    num_pages, H, bpp = _q8_cache_args(k_pool, k_scale_pool, v_pool, v_scale_pool)
-    B, T = _q8_rows_args(k, v, H, k_pool.device)
+    num_pages, H, bpp, dev, at = _q8_cache_args(k_pool, k_scale_pool, v_pool, v_scale_pool)
+    B, T = _q8_rows_args(k, v, H, dev)
     _need(0 <= t0 <= _INT_MAX, "t0")
-    max_pages = _q8_table(block_table, B, k_pool.device)
-    s = _q8_stream(k, stream)
-    rc = _lib.dq_q8_encode_kv_paged(f, k.data_ptr(), k.stride(0), k.stride(1), k.stride(2), v.data_ptr(), v.stride(0),
-                                    v.stride(1), v.stride(2), B, H, t0, T, block_table.data_ptr(), max_pages,
-                                    bpp * DQ_Q8_BLOCK, num_pages, k_pool.data_ptr(), k_scale_pool.data_ptr(),
-                                    v_pool.data_ptr(), v_scale_pool.data_ptr(), _q8_status(status, k_pool.device), s)
+    max_pages = _q8_table(block_table, B, dev)
+    rc = _lib.dq_q8_encode_kv_paged(f, k.data_ptr(), *k.stride()[:3], v.data_ptr(), *v.stride()[:3], B, H, t0, T,
+                                    block_table.data_ptr(), max_pages, bpp * DQ_Q8_BLOCK, num_pages, *at,
+                                    _q8_status(status, dev), _q8_stream(k, stream))
     _check(rc, "dq_q8_encode_kv_paged")
 
 
 def _q8_out_rows(k, v, batch, n, heads, dev):
-    if k is None:
-        k = torch.empty((batch, n, heads, 128), dtype=torch.bfloat16, device=dev)
-    if v is None:
-        v = torch.empty((batch, n, heads, 128), dtype=torch.bfloat16, device=dev)
-    _need(_q8_rows_args(k, v, heads, dev) == (batch, n), "k and v must be [B, n, H, 128]")
+    if k is None and v is None:
+        return torch.empty((2, batch, n, heads, 128), dtype=torch.bfloat16, device=dev).unbind()
+    _need(k is not None and v is not None and _q8_rows_args(k, v, heads, dev) == (batch, n),
+          "k and v must be [B, n, H, 128], both or neither")
+    return k, v
+
+
+def _q8_read(fmt: int, cache, t0, n, k, v, stream):
+    B, H, nb, dev, at = cache
+    _need(0 <= t0 <= _INT_MAX and 0 <= n <= _INT_MAX, "t0 and n")
+    k, v = _q8_out_rows(k, v, B, n, H, dev)
+    rc = _lib.dq_q8_decode_kv(fmt, *at, B, H, t0, n, nb * DQ_Q8_BLOCK, k.data_ptr(), *k.stride()[:3], v.data_ptr(),
+                              *v.stride()[:3], _q8_stream(k, stream))
+    _check(rc, "dq_q8_decode_kv")
     return k, v
 
 
 def dq_q8_decode_kv(fmt, k_data, k_scale, v_data, v_scale, t0: int, n: int, k=None, v=None, stream=None):
     """The values of tokens [t0, t0 + n), t0 a multiple of 32, as bf16 [B, n, H, 128]."""
-    f = _q8_format(fmt)
-    B, H, nb = _q8_cache_args(k_data, k_scale, v_data, v_scale)
-    _need(0 <= t0 <= _INT_MAX and 0 <= n <= _INT_MAX, "t0 and n")
-    k, v = _q8_out_rows(k, v, B, n, H, k_data.device)
-    s = _q8_stream(k_data, stream)
-    if B and n:
-        rc = _lib.dq_q8_decode_kv(f, k_data.data_ptr(), k_scale.data_ptr(), v_data.data_ptr(), v_scale.data_ptr(), B, H,
-                                  t0, n, nb * DQ_Q8_BLOCK, k.data_ptr(), k.stride(0), k.stride(1), k.stride(2),
-                                  v.data_ptr(), v.stride(0), v.stride(1), v.stride(2), s)
-        _check(rc, "dq_q8_decode_kv")
-    return k, v
+    return _q8_read(_q8_format(fmt), _q8_cache_args(k_data, k_scale, v_data, v_scale), t0, n, k, v, stream)
 
 
 def dq_q8_decode_kv_paged(fmt, k_pool, k_scale_pool, v_pool, v_scale_pool, block_table, t0: int, n: int, k=None,
                           v=None, status=None, stream=None):
     """dq_q8_decode_kv from pool pages."""
     f = _q8_format(fmt)
-    num_pages, H, bpp = _q8_cache_args(k_pool, k_scale_pool, v_pool, v_scale_pool)
+    num_pages, H, bpp, dev, at = _q8_cache_args(k_pool, k_scale_pool, v_pool, v_scale_pool)
     B = block_table.shape[0]
-    max_pages = _q8_table(block_table, B, k_pool.device)
+    max_pages = _q8_table(block_table, B, dev)
     _need(0 <= t0 <= _INT_MAX and 0 <= n <= _INT_MAX, "t0 and n")
-    k, v = _q8_out_rows(k, v, B, n, H, k_pool.device)
-    s = _q8_stream(k_pool, stream)
-    if B and n:
-        rc = _lib.dq_q8_decode_kv_paged(f, k_pool.data_ptr(), k_scale_pool.data_ptr(), v_pool.data_ptr(),
-                                        v_scale_pool.data_ptr(), B, H, t0, n, block_table.data_ptr(), max_pages,
-                                        bpp * DQ_Q8_BLOCK, num_pages, k.data_ptr(), k.stride(0), k.stride(1),
-                                        k.stride(2), v.data_ptr(), v.stride(0), v.stride(1), v.stride(2),
-                                        _q8_status(status, k_pool.device), s)
-        _check(rc, "dq_q8_decode_kv_paged")
+    k, v = _q8_out_rows(k, v, B, n, H, dev)
+    rc = _lib.dq_q8_decode_kv_paged(f, *at, B, H, t0, n, block_table.data_ptr(), max_pages, bpp * DQ_Q8_BLOCK,
+                                    num_pages, k.data_ptr(), *k.stride()[:3], v.data_ptr(), *v.stride()[:3],
+                                    _q8_status(status, dev), _q8_stream(k, stream))
+    _check(rc, "dq_q8_decode_kv_paged")
     return k, v
 
 
@@ -852,22 +840,43 @@ def _q8_sees(window, sinks):
     return window, sinks
 
 
+def _q8_partial(fmt: int, cache, q, seq_lens, workspace, window, sinks, extra_lens, softmax_scale, block_lse, stream):
+    B, H, nb, dev, at = cache
+    n, Hq = _q8_query(q, H, dev)
+    _need(n == B, "q and the cache must have the same batch")
+    extra = 0 if extra_lens is None else _q8_lens(extra_lens, B, dev, "extra_lens")
+    _, lse = _q8_scores(None, block_lse, B, H, nb, Hq // H, dev)
+    rc = _lib.dq_q8_decode_attention_partial(
+        fmt, q.data_ptr(), B, Hq, H, *at, _q8_lens(seq_lens, B, dev), extra, nb * DQ_Q8_BLOCK,
+        *_q8_sees(window, sinks), _RSQRT_D if softmax_scale is None else softmax_scale, lse,
+        *_q8_workspace(workspace, dev), _q8_stream(q, stream))
+    _check(rc, "dq_q8_decode_attention_partial")
+
+
 def dq_q8_decode_attention_partial(fmt, q, k_data, k_scale, v_data, v_scale, seq_lens, workspace, window: int = 0,
                                    sinks: int = 0, extra_lens=None, softmax_scale=None, block_lse=None, stream=None):
     """Split-K partials of one decode step over the 8-bit cache; finish with
     dq_decode_attention_merge or dq_decode_attention_merge_residual."""
-    f = _q8_format(fmt)
-    B, H, nb = _q8_cache_args(k_data, k_scale, v_data, v_scale)
-    n, Hq = _q8_query(q, H, k_data.device)
+    _q8_partial(_q8_format(fmt), _q8_cache_args(k_data, k_scale, v_data, v_scale), q, seq_lens, workspace, window,
+                sinks, extra_lens, softmax_scale, block_lse, stream)
+
+
+def _q8_attention(fmt: int, cache, q, seq_lens, out, workspace, window, sinks, softmax_scale, block_lse, scores,
+                  stream):
+    B, H, nb, dev, at = cache
+    n, Hq = _q8_query(q, H, dev)
     _need(n == B, "q and the cache must have the same batch")
-    lens = _q8_lens(seq_lens, B, q.device)
-    extra = 0 if extra_lens is None else _q8_lens(extra_lens, B, q.device, "extra_lens")
-    _, lse = _q8_scores(None, block_lse, B, H, nb, Hq // H, q.device)
-    rc = _lib.dq_q8_decode_attention_partial(
-        f, q.data_ptr(), B, Hq, H, k_data.data_ptr(), k_scale.data_ptr(), v_data.data_ptr(), v_scale.data_ptr(), lens,
-        extra, nb * DQ_Q8_BLOCK, *_q8_sees(window, sinks), _RSQRT_D if softmax_scale is None else softmax_scale, lse,
-        *_q8_workspace(workspace, q.device), _q8_stream(q, stream))
-    _check(rc, "dq_q8_decode_attention_partial")
+    if out is None:
+        out = torch.empty_like(q, dtype=torch.float32)
+    sc = lse = 0
+    if scores is not None or block_lse is not None:
+        sc, lse = _q8_scores(scores, block_lse, B, H, nb, Hq // H, dev)
+    rc = _lib.dq_q8_decode_attention(
+        fmt, q.data_ptr(), B, Hq, H, *at, _q8_lens(seq_lens, B, dev), nb * DQ_Q8_BLOCK, *_q8_sees(window, sinks),
+        _RSQRT_D if softmax_scale is None else softmax_scale, _q8_out(out, q), lse, sc,
+        *_q8_workspace(workspace, dev), _q8_stream(q, stream))
+    _check(rc, "dq_q8_decode_attention")
+    return out
 
 
 def dq_q8_decode_attention(fmt, q, k_data, k_scale, v_data, v_scale, seq_lens, out, workspace, window: int = 0,
@@ -876,17 +885,8 @@ def dq_q8_decode_attention(fmt, q, k_data, k_scale, v_data, v_scale, seq_lens, o
     window > 0: only the first `sinks` and the newest `window` tokens are
     visible.  scores fp32 [B, H, t_cap/32] grow by the blocks' attention weight
     (block_lse fp32 [B, H, t_cap/32, Hq/H] is its scratch)."""
-    f = _q8_format(fmt)
-    B, H, nb = _q8_cache_args(k_data, k_scale, v_data, v_scale)
-    n, Hq = _q8_query(q, H, k_data.device)
-    _need(n == B, "q and the cache must have the same batch")
-    sc, lse = _q8_scores(scores, block_lse, B, H, nb, Hq // H, q.device)
-    rc = _lib.dq_q8_decode_attention(
-        f, q.data_ptr(), B, Hq, H, k_data.data_ptr(), k_scale.data_ptr(), v_data.data_ptr(), v_scale.data_ptr(),
-        _q8_lens(seq_lens, B, q.device), nb * DQ_Q8_BLOCK, *_q8_sees(window, sinks),
-        _RSQRT_D if softmax_scale is None else softmax_scale, _q8_out(out, q), lse, sc,
-        *_q8_workspace(workspace, q.device), _q8_stream(q, stream))
-    _check(rc, "dq_q8_decode_attention")
+    _q8_attention(_q8_format(fmt), _q8_cache_args(k_data, k_scale, v_data, v_scale), q, seq_lens, out, workspace,
+                  window, sinks, softmax_scale, block_lse, scores, stream)
 
 
 def dq_q8_decode_attention_paged_partial(fmt, q, k_pool, k_scale_pool, v_pool, v_scale_pool, block_table, seq_lens,
@@ -895,17 +895,16 @@ def dq_q8_decode_attention_paged_partial(fmt, q, k_pool, k_scale_pool, v_pool, v
     """dq_q8_decode_attention_partial over pool pages; t_cap of the finishing
     call is max_pages * page_tokens."""
     f = _q8_format(fmt)
-    num_pages, H, bpp = _q8_cache_args(k_pool, k_scale_pool, v_pool, v_scale_pool)
-    B, Hq = _q8_query(q, H, k_pool.device)
-    max_pages = _q8_table(block_table, B, q.device)
-    lens = _q8_lens(seq_lens, B, q.device)
-    extra = 0 if extra_lens is None else _q8_lens(extra_lens, B, q.device, "extra_lens")
-    _, lse = _q8_scores(None, block_lse, B, H, max_pages * bpp, Hq // H, q.device)
+    num_pages, H, bpp, dev, at = _q8_cache_args(k_pool, k_scale_pool, v_pool, v_scale_pool)
+    B, Hq = _q8_query(q, H, dev)
+    max_pages = _q8_table(block_table, B, dev)
+    extra = 0 if extra_lens is None else _q8_lens(extra_lens, B, dev, "extra_lens")
+    _, lse = _q8_scores(None, block_lse, B, H, max_pages * bpp, Hq // H, dev)
     rc = _lib.dq_q8_decode_attention_paged_partial(
-        f, q.data_ptr(), B, Hq, H, k_pool.data_ptr(), k_scale_pool.data_ptr(), v_pool.data_ptr(),
-        v_scale_pool.data_ptr(), block_table.data_ptr(), max_pages, bpp * DQ_Q8_BLOCK, num_pages, lens, extra,
-        *_q8_sees(window, sinks), _RSQRT_D if softmax_scale is None else softmax_scale, lse,
-        *_q8_workspace(workspace, q.device), _q8_status(status, q.device), _q8_stream(q, stream))
+        f, q.data_ptr(), B, Hq, H, *at, block_table.data_ptr(), max_pages, bpp * DQ_Q8_BLOCK, num_pages,
+        _q8_lens(seq_lens, B, dev), extra, *_q8_sees(window, sinks),
+        _RSQRT_D if softmax_scale is None else softmax_scale, lse, *_q8_workspace(workspace, dev),
+        _q8_status(status, dev), _q8_stream(q, stream))
     _check(rc, "dq_q8_decode_attention_paged_partial")
 
 
@@ -915,16 +914,14 @@ def dq_q8_decode_attention_paged(fmt, q, k_pool, k_scale_pool, v_pool, v_scale_p
     """dq_q8_decode_attention over pool pages (scores and block_lse have
     max_pages * page/32 blocks per sequence)."""
     f = _q8_format(fmt)
-    num_pages, H, bpp = _q8_cache_args(k_pool, k_scale_pool, v_pool, v_scale_pool)
-    B, Hq = _q8_query(q, H, k_pool.device)
-    max_pages = _q8_table(block_table, B, q.device)
-    sc, lse = _q8_scores(scores, block_lse, B, H, max_pages * bpp, Hq // H, q.device)
+    num_pages, H, bpp, dev, at = _q8_cache_args(k_pool, k_scale_pool, v_pool, v_scale_pool)
+    B, Hq = _q8_query(q, H, dev)
+    max_pages = _q8_table(block_table, B, dev)
+    sc, lse = _q8_scores(scores, block_lse, B, H, max_pages * bpp, Hq // H, dev)
     rc = _lib.dq_q8_decode_attention_paged(
-        f, q.data_ptr(), B, Hq, H, k_pool.data_ptr(), k_scale_pool.data_ptr(), v_pool.data_ptr(),
-        v_scale_pool.data_ptr(), block_table.data_ptr(), max_pages, bpp * DQ_Q8_BLOCK, num_pages,
-        _q8_lens(seq_lens, B, q.device), *_q8_sees(window, sinks), _RSQRT_D if softmax_scale is None else softmax_scale,
-        _q8_out(out, q), lse, sc, *_q8_workspace(workspace, q.device),
-        _q8_status(status, q.device), _q8_stream(q, stream))
+        f, q.data_ptr(), B, Hq, H, *at, block_table.data_ptr(), max_pages, bpp * DQ_Q8_BLOCK, num_pages,
+        _q8_lens(seq_lens, B, dev), *_q8_sees(window, sinks), _RSQRT_D if softmax_scale is None else softmax_scale,
+        _q8_out(out, q), lse, sc, *_q8_workspace(workspace, dev), _q8_status(status, dev), _q8_stream(q, stream))
     _check(rc, "dq_q8_decode_attention_paged")
 
 
@@ -943,41 +940,46 @@ def dq_q8_add_scores(q_heads: int, seq_lens, block_lse, workspace, scores, windo
     _check(rc, "dq_q8_add_scores")
 
 
+def _q8_kept(kept, keep, first, last, batch, heads, dev):
+    _need(0 <= first <= _INT_MAX and 0 <= last <= _INT_MAX and 0 <= keep <= _INT_MAX, "keep, first and last")
+    _need(kept.dtype == torch.int32 and kept.shape == (batch, heads, keep // DQ_Q8_BLOCK) and kept.is_contiguous()
+          and kept.device == dev, "kept must be int32 [B, H, keep/32]")
+    return kept.data_ptr()
+
+
+def _q8_evict(seq_lens, new_lens, keep, first, last, source, scores, to, to_scores, kept, stream):
+    B, H, nb, dev, at = source
+    tB, tH, tnb, tdev, to_at = to
+    _need(tB == B and tH == H and tdev == dev, "both caches must have the same batch, heads and GPU")
+    sc, _ = _q8_scores(scores, None, B, H, nb, 1, dev)
+    tsc, _ = _q8_scores(to_scores, None, B, H, tnb, 1, dev)
+    rc = _lib.dq_q8_evict(B, H, _q8_lens(seq_lens, B, dev), _q8_lens(new_lens, B, dev, "new_lens"), nb * DQ_Q8_BLOCK,
+                          tnb * DQ_Q8_BLOCK, keep, first, last, *at, sc, *to_at, tsc,
+                          _q8_kept(kept, keep, first, last, B, H, dev), _q8_stream(kept, stream))
+    _check(rc, "dq_q8_evict")
+
+
 def dq_q8_evict(seq_lens, new_lens, keep: int, first: int, last: int, source, to, kept, stream=None):
     """Keep the blocks of the first `first` and newest `last` tokens and those of
     the largest scores, keep tokens in all (multiples of 32).  source, to:
     (k_data, k_scale, v_data, v_scale, scores), the same arrays for an eviction
     in place; kept int32 [B, H, keep/32]; new_lens may be seq_lens."""
-    B, H, nb = _q8_cache_args(*source[:4])
-    tB, tH, tnb = _q8_cache_args(*to[:4])
-    dev = source[0].device
-    _need(max(keep, first, last) <= _INT_MAX and min(keep, first, last) >= 0, "keep, first and last")
-    _need((tB, tH) == (B, H) and to[0].device == dev, "both caches must have the same batch, heads and GPU")
-    _q8_scores(source[4], None, B, H, nb, 1, dev)
-    _q8_scores(to[4], None, B, H, tnb, 1, dev)
-    _need(kept.dtype == torch.int32 and tuple(kept.shape) == (B, H, keep // DQ_Q8_BLOCK) and kept.is_contiguous()
-          and kept.device == dev, "kept must be int32 [B, H, keep/32]")
-    rc = _lib.dq_q8_evict(B, H, _q8_lens(seq_lens, B, dev), _q8_lens(new_lens, B, dev, "new_lens"), nb * DQ_Q8_BLOCK,
-                          tnb * DQ_Q8_BLOCK, keep, first, last, *(t.data_ptr() for t in source),
-                          *(t.data_ptr() for t in to), kept.data_ptr(), _q8_stream(kept, stream))
-    _check(rc, "dq_q8_evict")
+    _q8_evict(seq_lens, new_lens, keep, first, last, _q8_cache_args(*source[:4]), source[4], _q8_cache_args(*to[:4]),
+              to[4], kept, stream)
 
 
 def dq_q8_evict_paged(seq_lens, new_lens, keep: int, first: int, last: int, block_table, pools, scores, kept,
                       status=None, stream=None):
     """dq_q8_evict in place over pool pages: pools (k_pool, k_scale_pool, v_pool,
     v_scale_pool), scores fp32 [B, H, max_pages * page/32]."""
-    num_pages, H, bpp = _q8_cache_args(*pools)
-    B, dev = block_table.shape[0], pools[0].device
-    _need(max(keep, first, last) <= _INT_MAX and min(keep, first, last) >= 0, "keep, first and last")
+    num_pages, H, bpp, dev, at = _q8_cache_args(*pools)
+    B = block_table.shape[0]
     max_pages = _q8_table(block_table, B, dev)
-    _q8_scores(scores, None, B, H, max_pages * bpp, 1, dev)
-    _need(kept.dtype == torch.int32 and tuple(kept.shape) == (B, H, keep // DQ_Q8_BLOCK) and kept.is_contiguous()
-          and kept.device == dev, "kept must be int32 [B, H, keep/32]")
+    sc, _ = _q8_scores(scores, None, B, H, max_pages * bpp, 1, dev)
     rc = _lib.dq_q8_evict_paged(B, H, _q8_lens(seq_lens, B, dev), _q8_lens(new_lens, B, dev, "new_lens"), keep, first,
-                                last, block_table.data_ptr(), max_pages, bpp * DQ_Q8_BLOCK, num_pages,
-                                *(t.data_ptr() for t in pools), scores.data_ptr(), kept.data_ptr(),
-                                _q8_status(status, dev), _q8_stream(kept, stream))
+                                last, block_table.data_ptr(), max_pages, bpp * DQ_Q8_BLOCK, num_pages, *at, sc,
+                                _q8_kept(kept, keep, first, last, B, H, dev), _q8_status(status, dev),
+                                _q8_stream(kept, stream))
     _check(rc, "dq_q8_evict_paged")
 
 

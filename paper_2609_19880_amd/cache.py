@@ -127,11 +127,10 @@ class Q8KVCache:
             raise ValueError("fmt must be 'int8' or 'e4m3'")
         self.batch, self.kv_heads, self.q_heads, self.t_cap, self.head_dim = batch, kv_heads, q_heads, t_cap, 128
         self.fmt = fmt
+        self._format = _lib.Q8_FORMATS[fmt]
         nb = t_cap // self.BLOCK
-        self.k_data = torch.zeros((batch, kv_heads, nb, self.BLOCK * 128), dtype=torch.uint8, device=device)
-        self.v_data = torch.zeros_like(self.k_data)
-        self.k_scales = torch.zeros((batch, kv_heads, nb), dtype=torch.float32, device=device)
-        self.v_scales = torch.zeros_like(self.k_scales)
+        self._arrays = tuple(torch.zeros((batch, kv_heads, nb, *rest), dtype=dtype, device=device)
+                             for rest, dtype in 2 * [((self.BLOCK * 128,), torch.uint8), ((), torch.float32)])
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
         self.workspace = torch.empty(
             _lib.dq_decode_workspace_bytes(batch, q_heads, kv_heads, t_cap), dtype=torch.uint8, device=device)
@@ -140,40 +139,56 @@ class Q8KVCache:
         if scores:
             self.block_lse = torch.empty((batch, kv_heads, nb, q_heads // kv_heads), dtype=torch.float32,
                                          device=device)
+        # sizes and addresses of the cache's own arrays, checked once
+        self._at = _lib._q8_cache_args(*self._arrays) if self.status.is_cuda else None
 
     @property
     def arrays(self):
-        return self.k_data, self.k_scales, self.v_data, self.v_scales
+        """(k_data, k_scales, v_data, v_scales)"""
+        return self._arrays
+
+    @property
+    def k_data(self):
+        return self._arrays[0]
+
+    @property
+    def k_scales(self):
+        return self._arrays[1]
+
+    @property
+    def v_data(self):
+        return self._arrays[2]
+
+    @property
+    def v_scales(self):
+        return self._arrays[3]
 
     def append(self, k, v, t0: int):
         """Encode bf16 k, v [B, T_new, H, 128] as cache tokens [t0, t0 + T_new)
         (t0 a multiple of 32; a last block that is not full is completed with
         zeros)."""
-        _lib.dq_q8_encode_kv(self.fmt, k, v, t0, *self.arrays, status=self.status)
+        _lib._q8_encode(self._format, self._at, k, v, t0, self.status, None)
 
     def read(self, t0: int, n: int):
         """bf16 k, v [B, n, H, 128]: the values of tokens [t0, t0 + n)."""
-        return _lib.dq_q8_decode_kv(self.fmt, *self.arrays, t0, n)
+        return _lib._q8_read(self._format, self._at, t0, n, None, None, None)
 
     def attend(self, q, seq_lens, out=None, softmax_scale=None, window: int = 0, sinks: int = 0, scores=None):
         """q bf16 [B, Hq, 128] -> out fp32 over the first seq_lens[b] tokens or,
         with a window, the first `sinks` and the newest `window` of them.  The
         cache's own scores grow by the blocks' weights, or the given ones."""
-        if out is None:
-            out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
         if scores is None:
             scores = self.scores
         elif self.block_lse is None:
             raise ValueError("the cache was made without scores")
-        _lib.dq_q8_decode_attention(self.fmt, q, *self.arrays, seq_lens, out, self.workspace, window, sinks,
-                                    softmax_scale, self.block_lse, scores)
-        return out
+        return _lib._q8_attention(self._format, self._at, q, seq_lens, out, self.workspace, window, sinks,
+                                  softmax_scale, self.block_lse, scores, None)
 
     def partial(self, q, seq_lens, softmax_scale=None, window: int = 0, sinks: int = 0, extra_lens=None):
         """Split-K partials of one decode step into the workspace (finish with
         merge; the scores' part of it with add_scores)."""
-        _lib.dq_q8_decode_attention_partial(self.fmt, q, *self.arrays, seq_lens, self.workspace, window, sinks,
-                                            extra_lens, softmax_scale, self.block_lse)
+        _lib._q8_partial(self._format, self._at, q, seq_lens, self.workspace, window, sinks, extra_lens,
+                         softmax_scale, self.block_lse, None)
 
     def merge(self, seq_lens, out):
         _lib.dq_decode_attention_merge(self.batch, self.q_heads, self.kv_heads, seq_lens, self.t_cap,
@@ -195,13 +210,12 @@ class Q8KVCache:
             raise ValueError("eviction needs scores, and caches of one format")
         if keep <= 0 or keep % self.BLOCK:
             raise ValueError("keep must be a positive multiple of 32")
-        kept = torch.empty((self.batch, self.kv_heads, keep // self.BLOCK), dtype=torch.int32,
-                           device=self.k_data.device)
+        kept = self.status.new_empty((self.batch, self.kv_heads, keep // self.BLOCK))
         if new_lens is None:
             new_lens = torch.empty_like(seq_lens)
         up = -self.BLOCK
-        _lib.dq_q8_evict(seq_lens, new_lens, keep, sinks // up * up, max(recent // up * up, self.BLOCK),
-                         (*self.arrays, self.scores), (*to.arrays, to.scores), kept)
+        _lib._q8_evict(seq_lens, new_lens, keep, sinks // up * up, max(recent // up * up, self.BLOCK), self._at,
+                       self.scores, to._at, to.scores, kept, None)
         return kept, new_lens
 
     def cache_bytes(self, tokens: int) -> int:

@@ -728,30 +728,38 @@ static int check_q8_step(int32_t B, int32_t Hq, int32_t Hkv, const int32_t* seq_
     return DQ_OK;
 }
 
+static int check_q8_query(int32_t format, const uint16_t* q, const dq::Q8Cache& c, float scale) {
+    if (format != DQ_Q8_INT8 && format != DQ_Q8_E4M3) return DQ_ERR_INVALID_ARG;
+    if (!q || (reinterpret_cast<uintptr_t>(q) & 15) || !q8_cache_ok(c) || !std::isfinite(scale))
+        return DQ_ERR_INVALID_ARG;
+    return DQ_OK;
+}
+
 static int q8_partial(int32_t format, const dq::Pages& pg, const uint16_t* q, int32_t B, int32_t Hq, int32_t Hkv,
                       const dq::Q8Cache& c, const int32_t* seq_lens, const int32_t* extra_lens, int32_t t_cap,
                       int32_t window, int32_t sinks, float scale, float* lse, void* ws, size_t ws_bytes,
                       uint32_t* status, void* stream) {
-    if (format != DQ_Q8_INT8 && format != DQ_Q8_E4M3) return DQ_ERR_INVALID_ARG;
-    if (!q || !q8_cache_ok(c) || !std::isfinite(scale)) return DQ_ERR_INVALID_ARG;
+    if (int rc = check_q8_query(format, q, c, scale)) return rc;
     if (int rc = check_q8_step(B, Hq, Hkv, seq_lens, t_cap, window, sinks, ws, ws_bytes)) return rc;
     return dq::launch_q8_partial(format, pg, q, B, Hq, Hkv, c, seq_lens, extra_lens, t_cap, window, sinks, scale, lse,
-                                 ws, status, static_cast<hipStream_t>(stream));
+                                 nullptr, nullptr, ws, status, static_cast<hipStream_t>(stream), nullptr);
 }
 
-// Partial, merge and scores of one step.
+// Partial, merge and scores of one step: one launch where one chunk holds
+// every sequence, else two.
 static int q8_attention(int32_t format, const dq::Pages& pg, const uint16_t* q, int32_t B, int32_t Hq, int32_t Hkv,
                         const dq::Q8Cache& c, const int32_t* seq_lens, int32_t t_cap, int32_t window, int32_t sinks,
                         float scale, float* out, float* lse, float* scores, void* ws, size_t ws_bytes,
                         uint32_t* status, void* stream) {
-    if (!out || (scores && !lse)) return DQ_ERR_INVALID_ARG;
-    int rc = q8_partial(format, pg, q, B, Hq, Hkv, c, seq_lens, nullptr, t_cap, window, sinks, scale, lse, ws,
-                        ws_bytes, status, stream);
-    if (rc != DQ_OK) return rc;
+    if (!out || (reinterpret_cast<uintptr_t>(out) & 7) || (scores && !lse)) return DQ_ERR_INVALID_ARG;
+    if (int rc = check_q8_query(format, q, c, scale)) return rc;
+    if (int rc = check_q8_step(B, Hq, Hkv, seq_lens, t_cap, window, sinks, ws, ws_bytes)) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    rc = dq::launch_attention_merge(B, Hq, Hkv, seq_lens, t_cap, ws, out, s);
-    if (rc != DQ_OK || !scores) return rc;
-    return dq::launch_q8_scores(B, Hq, Hkv, seq_lens, nullptr, t_cap, window, sinks, lse, ws, scores, s);
+    bool done = false;
+    const int rc = dq::launch_q8_partial(format, pg, q, B, Hq, Hkv, c, seq_lens, nullptr, t_cap, window, sinks, scale,
+                                         lse, out, scores, ws, status, s, &done);
+    if (rc != DQ_OK || done) return rc;
+    return dq::launch_q8_finish(B, Hq, Hkv, seq_lens, nullptr, t_cap, window, sinks, lse, ws, out, scores, s);
 }
 
 int dq_q8_decode_attention_partial(int32_t format, const uint16_t* q, int32_t B, int32_t Hq, int32_t Hkv,
@@ -803,7 +811,7 @@ int dq_q8_add_scores(int32_t B, int32_t Hq, int32_t Hkv, const int32_t* seq_lens
                      size_t ws_bytes, float* scores, void* stream) {
     if (!block_lse || !scores) return DQ_ERR_INVALID_ARG;
     if (int rc = check_q8_step(B, Hq, Hkv, seq_lens, t_cap, window, sinks, ws, ws_bytes)) return rc;
-    return dq::launch_q8_scores(B, Hq, Hkv, seq_lens, extra_lens, t_cap, window, sinks, block_lse, ws, scores,
+    return dq::launch_q8_finish(B, Hq, Hkv, seq_lens, extra_lens, t_cap, window, sinks, block_lse, ws, nullptr, scores,
                                 static_cast<hipStream_t>(stream));
 }
 

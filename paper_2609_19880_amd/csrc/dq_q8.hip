@@ -22,6 +22,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "dq_common.h"
 
@@ -35,6 +36,7 @@ constexpr float kTiny = 0x1p-96f;            // a block below is stored as zeros
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
@@ -410,9 +412,14 @@ struct Q8Args {
     const int32_t* seq_lens;
     const int32_t* extra_lens;   // tokens behind the cached ones, or NULL
     Pages pg;
-    int Hq, Hkv, G, t_cap, chunk, nchunks, window, sinks;   // chunk in blocks
+    int Hq, Hkv, G, t_cap, window, sinks;
+    int chunk, nchunks;          // blocks per chunk, chunk slots per sequence
+    int B, target;               // target > 0: the chunk length follows the lengths
     float scale_log2;
     float* lse;                  // [B][Hkv][t_cap / 32][G], or NULL
+    float* out;                  // one chunk: the step's result goes here, or NULL
+    float* scores;               // with out
+    int early;                   // blocks are requested before the length is known
     uint32_t* status;
     int32_t* ws_hdr;
     float* ws_m;
@@ -420,10 +427,18 @@ struct Q8Args {
     float* ws_acc;
 };
 
-constexpr int kAWaves = 4;
+constexpr int kAWaves = 8;
 constexpr int kAThreads = kAWaves * kWave;
 constexpr int kGP = 8;                       // query-head slots
 constexpr float kBig = 3e38f;
+
+typedef const __attribute__((address_space(1))) uint8_t* GlobalBytes;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ uint4 load16(GlobalBytes p) {
+    const u32x4 v = *reinterpret_cast<const __attribute__((address_space(1))) u32x4*>(p);
+    return uint4{v[0], v[1], v[2], v[3]};
+}
 
 // Eight code bytes to eight fp16 values (exact for both types).
 template <int FMT>
@@ -458,10 +473,86 @@ __device__ __forceinline__ f32x4 mfma_f16(const f16x8& a, const f16x8& b, const 
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
-__device__ __forceinline__ float clamp_big(float x) { return fminf(fmaxf(x, -kBig), kBig); }
+__device__ __forceinline__ float clamp_big(float x) { return __builtin_amdgcn_fmed3f(x, -kBig, kBig); }
 
-// One workgroup of four wavefronts per (chunk of visible blocks, KV head,
-// sequence); a wavefront takes every fourth block of the chunk and requests
+// A uniform address of memory that this kernel does not write, through the
+// scalar unit: what arrives there keeps out of the vector loads' order, so no
+// wait for it waits for a prefetched block.
+template <typename T>
+__device__ __forceinline__ T scalar_load(const T* p) {
+    return *reinterpret_cast<const __attribute__((address_space(4))) T*>(reinterpret_cast<uintptr_t>(p));
+}
+
+// What workgroup `id` works on, where the chunk length follows the sequences'
+// lengths: all blocks there are, cut into about `target` equal chunks (at most
+// `nchunks` in the longest sequence), sequence after sequence, head after head.
+// A batch of unlike lengths then ends much as one of like lengths does, and a
+// buffer's unused capacity costs nothing (chunks cut from the capacity alone:
+// 4096 tokens in a buffer of 131072 28.7 us against 9.9; 16 sequences, one of
+// 131072 and fifteen of 2000 tokens, 134 against 62).
+struct Share {
+    int b, h, c, chunk;          // c = -1: nothing
+};
+
+__device__ __forceinline__ int wave_scan(int v) {      // inclusive sums over the lanes
+    v += dpp0<0x111, 0xF>(v);    // row_shr:1
+    v += dpp0<0x112, 0xF>(v);    // row_shr:2
+    v += dpp0<0x114, 0xF>(v);    // row_shr:4
+    v += dpp0<0x118, 0xF>(v);    // row_shr:8
+    v += dpp0<0x142, 0xA>(v);    // row_bcast:15 into rows 1 and 3
+    v += dpp0<0x143, 0xC>(v);    // row_bcast:31 into rows 2 and 3
+    return v;
+}
+
+__device__ __forceinline__ Share share_of(const Q8Args& a, int id, int lane) {
+    auto blocks = [&](int T) { return (max(0, min(T, a.t_cap)) + kBlk - 1) / kBlk; };
+    auto length = [&](int total, int longest) {
+        int c = (total + a.target - 1) / a.target;
+        // unlike lengths leave many last chunks that are not full: cut finer, but
+        // not below two blocks per wavefront
+        if (total < longest * a.B / 4 * 3) c = max(min(c, 2 * kAWaves), (c + 2) / 3);
+        c = max(c, (longest + a.nchunks - 1) / a.nchunks);
+        return max((c + 3) & ~3, total > 2 * a.target ? 8 : 4);
+    };
+    if (a.B == 1) {
+        const int n = blocks(scalar_load(a.seq_lens)), chunk = length(n, n), used = (n + chunk - 1) / chunk;
+        if (id >= used * a.Hkv) return Share{0, 0, -1, chunk};
+        return Share{0, id / used, id % used, chunk};
+    }
+    int total = 0, longest = 0;
+    int mine = 0;                // blocks of sequence `lane` of the group at hand
+    auto read = [&](int b0) { mine = b0 + lane < a.B ? blocks(a.seq_lens[b0 + lane]) : 0; };
+    for (int b0 = 0; b0 < a.B; b0 += kWave) {
+        read(b0);
+        total += wave_sum(mine);
+        longest = max(longest, wave_max(mine));
+    }
+    const int chunk = length(total, longest);
+    // the full chunks, then the sequences' last ones that are not: short work
+    // comes last and evens out the end
+    for (int pass = 0; pass < 2; ++pass) {
+        int before = 0;          // chunks of one head of the sequences before the group
+        for (int b0 = 0; b0 < a.B; b0 += kWave) {
+            if (a.B > kWave) read(b0);
+            const int full = mine / chunk, own = pass == 0 ? full : (int)(mine > full * chunk);
+            const int upto = before + wave_scan(own);
+            const int all = __builtin_amdgcn_readlane(upto, 63);
+            if (id < all * a.Hkv) {
+                // the first sequence whose chunks, of all heads, reach past id
+                const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto * a.Hkv > id));
+                const int r = id - __builtin_amdgcn_readlane(upto - own, l) * a.Hkv;
+                const int n = __builtin_amdgcn_readlane(own, l);
+                return Share{b0 + l, r / n, pass == 0 ? r % n : __builtin_amdgcn_readlane(full, l), chunk};
+            }
+            before = all;
+        }
+        id -= before * a.Hkv;
+    }
+    return Share{0, 0, -1, chunk};
+}
+
+// One workgroup of eight wavefronts per (chunk of visible blocks, KV head,
+// sequence); a wavefront takes every eighth block of the chunk and requests
 // the next one's 8 KB before it works on the one at hand.
 //   Scores: S^T (16 tokens x 16 columns) = K (16 x 128) Q^T on
 //   v_mfma_f32_16x16x32_f16.  Codes are exact in fp16, and so are the query's
@@ -472,32 +563,106 @@ __device__ __forceinline__ float clamp_big(float x) { return fminf(fmaxf(x, -kBi
 //   lanes of a head only when some lane exceeds it.
 //   Values: weights p 2^15 are split into two fp16 terms (22 bits, down to
 //   weights of 2^-18 of the largest), the first in the rows of heads 0..7, the
-//   second (times 2^11) in rows 8..15: one product of the 32 tokens gives both,
-//   its operand the weights as they lie.  The block's scale is applied to the
+//   second in rows 8..15: one product of the 32 tokens gives both, its operand
+//   the weights as they lie.  The block's scale is applied to the
 //   product's fp32 result.
 template <int FMT, bool TRACK>
-__global__ __launch_bounds__(kAThreads) void q8_partial_kernel(Q8Args a) {
+__global__ __launch_bounds__(kAThreads, 4) void q8_partial_kernel(Q8Args a) {
     __shared__ float wm[kAWaves][kGP], wl[kAWaves][kGP];
     __shared__ __align__(16) float wacc[kAWaves][kGP][kD];
-    const int c = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+    int c = blockIdx.x, h = blockIdx.y, b = blockIdx.z, chunk = a.chunk;
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int G = a.G, NC = a.nchunks, nb_cap = a.t_cap / kBlk;
-    if ((c | h | b) == 0 && tid == 0) {
+    const int col = lane & 15, grp = lane >> 4, head = col & 7;
+    const bool first = (blockIdx.x | blockIdx.y | blockIdx.z) == 0 && tid == 0;
+    if (a.target > 0) {
+        const Share w = share_of(a, (int)blockIdx.x, lane);
+        h = w.h;
+        c = w.c;
+        b = w.b;
+        chunk = w.chunk;
+        if (first) a.ws_hdr[0] = chunk * kBlk;
+    } else if (first) {
         // a windowed step fills every chunk's slot, for whatever length: the
         // merge takes min(chunks, ceil(T / 1)) of them, and chunk c >= T is empty
-        a.ws_hdr[0] = a.window > 0 ? 1 : a.chunk * kBlk;
+        a.ws_hdr[0] = a.window > 0 ? 1 : chunk * kBlk;
+    }
+    if (first) {
         a.ws_hdr[1] = NC;
         a.ws_hdr[2] = 0;
         a.ws_hdr[3] = 0;          // values are in the caller's basis
     }
-    const int T = max(0, min(a.seq_lens[b], a.t_cap));
-    const int extra = a.extra_lens ? max(0, a.extra_lens[b]) : 0;
+    // (uniform, which the compiler does not see)
+    c = __builtin_amdgcn_readfirstlane(c);
+    h = __builtin_amdgcn_readfirstlane(h);
+    b = __builtin_amdgcn_readfirstlane(b);
+    chunk = __builtin_amdgcn_readfirstlane(chunk);
+    if (c < 0) return;            // more workgroups than chunks
+    const int v0 = c * chunk;
+
+    bool bad = false;
+    uint4 kr[4], vr[4];
+    float ks_next = 0.f, vs_next = 0.f;
+    // where block `blk` lies: its pool page is looked up an iteration before it
+    // is needed
+    int page = 0;
+    int64_t bi = 0;
+    auto look_up = [&](int blk) {
+        if (a.pg.bt) page = scalar_load(a.pg.bt + (int64_t)b * a.pg.max_pages + ((blk * kBlk) >> a.pg.page_shift));
+    };
+    auto locate = [&](int blk) {
+        if (!a.pg.bt) {
+            bi = ((int64_t)b * a.Hkv + h) * nb_cap + blk;
+            return;
+        }
+        if (page < 0 || page >= a.pg.num_pages) {
+            bad = true;
+            page = 0;
+        }
+        const int bpp = 1 << (a.pg.page_shift - 5);
+        bi = ((int64_t)page * a.Hkv + h) * bpp + (blk & (bpp - 1));
+    };
+    // (the empty statement keeps the block's address in scalar registers: one
+    // vector register, the lane's offset, then serves every load)
+    auto request_k = [&]() {
+        GlobalBytes p = reinterpret_cast<GlobalBytes>(reinterpret_cast<uintptr_t>(a.k + bi * kBlkBytes));
+        asm("" : "+s"(p));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) kr[i] = load16(p + 16u * lane + 1024u * i);
+        ks_next = scalar_load(a.ks + bi);
+        vs_next = scalar_load(a.vs + bi);
+    };
+    auto request_v = [&]() {
+        GlobalBytes p = reinterpret_cast<GlobalBytes>(reinterpret_cast<uintptr_t>(a.v + bi * kBlkBytes));
+        asm("" : "+s"(p));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) vr[i] = load16(p + 16u * lane + 1024u * i);
+    };
+    const int T_raw = scalar_load(a.seq_lens + b);
+    const int extra = a.extra_lens ? max(0, scalar_load(a.extra_lens + b)) : 0;
+    // the query: channels 64 (i / 2) + 16 grp + 8 (i % 2) .. of the lane's head
+    uint4 raw[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        raw[i] = uint4{0u, 0u, 0u, 0u};
+        if (head < G)
+            raw[i] = *reinterpret_cast<const uint4*>(a.q + ((int64_t)b * a.Hq + h * G + head) * kD + 64 * (i >> 1) +
+                                                     16 * grp + 8 * (i & 1));
+    }
+    if (a.early) {
+        locate(min(v0 + wave, nb_cap - 1));
+        request_k();
+        request_v();
+    }
+    const int T = max(0, min(T_raw, a.t_cap));
     const Visible vis = visible(T, extra, a.window, a.sinks);
-    const int v0 = c * a.chunk, v1 = min(v0 + a.chunk, vis.count);
+    const int v1 = min(v0 + chunk, vis.count);
     const int64_t slot0 = ((int64_t)b * a.Hq + h * G) * (NC + kResSlots) + c;
     if (v0 >= v1) {
-        if (a.window > 0) {
+        if (a.out) {
+            for (int i = tid; i < G * kD; i += kAThreads) a.out[((int64_t)b * a.Hq + h * G) * kD + i] = 0.f;
+        } else if (a.window > 0) {
             for (int i = tid; i < G * kD; i += kAThreads) {
                 const int64_t slot = slot0 + (int64_t)(i / kD) * (NC + kResSlots);
                 a.ws_acc[slot * kD + i % kD] = 0.f;
@@ -509,41 +674,34 @@ __global__ __launch_bounds__(kAThreads) void q8_partial_kernel(Q8Args a) {
         }
         return;                   // without a window the merge ignores the chunk
     }
-    const int col = lane & 15, grp = lane >> 4, head = col & 7;
 
     // ---- the query, scaled to fp16, in the columns of its head
-    f16x8 qb[4];                  // channels 64 (i / 2) + 16 grp + 8 (i % 2) ..
-    float c_head, bad_q;
+    f16x8 qb[4];
+    float c_head;
+    bool bad_q;
     {
-        uint16_t raw[4][8];
         uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                raw[i][e] = 0;
-                if (head < G)
-                    raw[i][e] = a.q[((int64_t)b * a.Hq + h * G + head) * kD + 64 * (i >> 1) + 16 * grp +
-                                    8 * (i & 1) + e];
-                top = max(top, (uint32_t)(raw[i][e] & 0x7FFF));
-            }
-        float m = __uint_as_float(top << 16);        // orders as the integer (NaN handled below)
-        const bool nonfinite = top >= 0x7F80;
-        bad_q = nonfinite ? 1.f : 0.f;
-        bad_q = fmaxf(bad_q, xor_lane<16>(bad_q, lane));
-        bad_q = fmaxf(bad_q, xor_lane<32>(bad_q, lane));
-        if (nonfinite) m = 0.f;
+            top = pk_max(top, pk_max(pk_max(raw[i].x & 0x7FFF7FFFu, raw[i].y & 0x7FFF7FFFu),
+                                     pk_max(raw[i].z & 0x7FFF7FFFu, raw[i].w & 0x7FFF7FFFu)));
+        // patterns without their signs order as integers, and as small floats
+        float m = (float)max(top & 0xFFFFu, top >> 16);
         m = fmaxf(m, xor_lane<16>(m, lane));
         m = fmaxf(m, xor_lane<32>(m, lane));
-        const int ex = bad_q > 0.f || m == 0.f ? 0 : ilogbf(m);
+        bad_q = m >= 32640.f;     // 0x7F80: an infinity or NaN
+        const int up = bad_q ? 0 : 14 - (max((int)m >> 7, 1) - 127);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float f = ldexpf(bf16_to_f32(raw[i][e]), 14 - ex);
-                qb[i][e] = bad_q > 0.f ? (_Float16)0.f : (_Float16)f;
+            for (int e = 0; e < 4; ++e) {
+                const float lo = __uint_as_float(w[e] << 16), hi = __uint_as_float(w[e] & 0xFFFF0000u);
+                qb[i][2 * e] = bad_q ? (_Float16)0.f : (_Float16)__builtin_ldexpf(lo, up);
+                qb[i][2 * e + 1] = bad_q ? (_Float16)0.f : (_Float16)__builtin_ldexpf(hi, up);
             }
-        c_head = ldexpf(a.scale_log2, ex - 14);
+        }
+        c_head = __builtin_ldexpf(a.scale_log2, -up);
     }
 
     float m_run = -3.4e38f, l_run = 0.f;
@@ -551,50 +709,44 @@ __global__ __launch_bounds__(kAThreads) void q8_partial_kernel(Q8Args a) {
 #pragma unroll
     for (int n = 0; n < 8; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    bool bad = false;
     auto block_of = [&](int v) { return v < vis.head ? v : vis.from + v - vis.head; };
-    uint4 kr[4], vr[4];
-    float ks, vs;
-    auto request = [&](int v) {
-        const int blk = block_of(v);
-        const int64_t bi = block_index(a.pg, a.Hkv, nb_cap, b, h, blk, bad);
-        const uint4* kp = reinterpret_cast<const uint4*>(a.k + bi * kBlkBytes) + lane;
-        const uint4* vp = reinterpret_cast<const uint4*>(a.v + bi * kBlkBytes) + lane;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) kr[i] = kp[64 * i];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) vr[i] = vp[64 * i];
-        ks = a.ks[bi];
-        vs = a.vs[bi];
-    };
     int v = v0 + wave;
-    if (v < v1) request(v);
-    while (v < v1) {
-        uint4 kc[4], vc[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            kc[i] = kr[i];
-            vc[i] = vr[i];
+    if (v < v1) {
+        if (!a.early) {
+            look_up(block_of(v));
+            locate(block_of(v));
+            request_k();
+            request_v();
         }
-        const float ksc = ks, vsc = vs * 0x1p-15f;
+        if (v + kAWaves < v1) look_up(block_of(v + kAWaves));
+    }
+    // One block; the next one is requested on the way (its keys once these have
+    // become scores, its values once these are added) or there is none.  Two
+    // copies: a request under a branch would make every wait one for all loads.
+    auto step = [&](auto more) {
         const int blk = block_of(v), t0 = blk * kBlk;
         const int vn = v + kAWaves;
-        if (vn < v1) request(vn);
+        const float ks = ks_next, vs = vs_next;
 
         // ---- scores in base 2
         float x[8];
-        const float cf = clamp_big(ksc * c_head);
+        const float cf = clamp_big(ks * c_head);
 #pragma unroll
         for (int h2 = 0; h2 < 2; ++h2) {
             f32x4 d = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const uint4 w = kc[2 * h2 + j];
+                const uint4 w = kr[2 * h2 + j];
                 d = mfma_f16(halves8<FMT>(w.x, w.y), qb[2 * j], d);
                 d = mfma_f16(halves8<FMT>(w.z, w.w), qb[2 * j + 1], d);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) x[4 * h2 + i] = clamp_big(d[i] * cf);
+        }
+        if constexpr (decltype(more)::value) {
+            locate(block_of(vn));
+            request_k();
+            if (vn + kAWaves < v1) look_up(block_of(vn + kAWaves));
         }
         const bool whole = t0 + kBlk <= T && (t0 >= vis.start || t0 + kBlk <= vis.sinks);
         if (!whole) {
@@ -610,10 +762,10 @@ __global__ __launch_bounds__(kAThreads) void q8_partial_kernel(Q8Args a) {
                 if (t0 + 16 * (e >> 2) + 4 * grp + (e & 3) < T) keep[e >> 2] |= 0xFFu << (8 * (e & 3));
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                vc[i].x &= keep[0];
-                vc[i].y &= keep[1];
-                vc[i].z &= keep[0];
-                vc[i].w &= keep[1];
+                vr[i].x &= keep[0];
+                vr[i].y &= keep[1];
+                vr[i].z &= keep[0];
+                vr[i].w &= keep[1];
             }
         }
 
@@ -636,37 +788,49 @@ __global__ __launch_bounds__(kAThreads) void q8_partial_kernel(Q8Args a) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[n][i] *= cr[i];
         }
+        // weights times 2^15 (sums as well); the second term of a weight below
+        // 2^-18 of the largest is a subnormal fp16, 2^-40 of the largest off at most
         float ps = 0.f;
-        f16x8 w;
+        uint32_t w2[4];
+        const float m15 = m_run - 15.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float p = __builtin_amdgcn_exp2f(x[e] - m_run);
-            ps += p;
-            const float f = p * 0x1p15f;
-            const _Float16 hi = (_Float16)f;
-            const _Float16 lo = (_Float16)((f - (float)hi) * 0x1p11f);
-            w[e] = col < 8 ? hi : lo;
+        for (int e = 0; e < 8; e += 2) {
+            const f32x2 f = {__builtin_amdgcn_exp2f(x[e] - m15), __builtin_amdgcn_exp2f(x[e + 1] - m15)};
+            ps += f[0];
+            ps += f[1];
+            const f16x2 hi = __builtin_convertvector(f, f16x2);
+            const f32x2 r = {f[0] - (float)hi[0], f[1] - (float)hi[1]};
+            const f16x2 lo = __builtin_convertvector(r, f16x2);
+            w2[e / 2] = __builtin_bit_cast(uint32_t, col < 8 ? hi : lo);
         }
+        const f16x8 w = __builtin_bit_cast(f16x8, uint4{w2[0], w2[1], w2[2], w2[3]});
         l_run += ps;
         if constexpr (TRACK) {
             float bs = ps + xor_lane<16>(ps, lane);
             bs += xor_lane<32>(bs, lane);
-            if (lane < G) a.lse[(((int64_t)b * a.Hkv + h) * nb_cap + blk) * G + lane] = log2f(bs) + m_run;
+            if (lane < G) a.lse[(((int64_t)b * a.Hkv + h) * nb_cap + blk) * G + lane] = log2f(bs) + m15;
         }
 
         // ---- weighted values
         const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+        const float vsc = vs * 0x1p-15f;
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
-            const f32x4 d0 = mfma_f16(w, halves8<FMT>(vc[n].x, vc[n].y), zero);
-            const f32x4 d1 = mfma_f16(w, halves8<FMT>(vc[n].z, vc[n].w), zero);
+            const f32x4 d0 = mfma_f16(w, halves8<FMT>(vr[n].x, vr[n].y), zero);
+            const f32x4 d1 = mfma_f16(w, halves8<FMT>(vr[n].z, vr[n].w), zero);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 acc[2 * n][i] = fmaf(d0[i], vsc, acc[2 * n][i]);
                 acc[2 * n + 1][i] = fmaf(d1[i], vsc, acc[2 * n + 1][i]);
             }
+            // here, not behind the next request: few products' results at a time
+            asm("" : "+v"(acc[2 * n]), "+v"(acc[2 * n + 1]));
         }
-        v = vn;
+        if constexpr (decltype(more)::value) request_v();
+    };
+    if (v < v1) {
+        for (; v + kAWaves < v1; v += kAWaves) step(std::true_type{});
+        step(std::false_type{});
     }
     if (bad && lane == 0 && a.status) atomicOr(a.status, DQ_STATUS_PAGE);
 
@@ -678,11 +842,11 @@ __global__ __launch_bounds__(kAThreads) void q8_partial_kernel(Q8Args a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float lo = xor_lane<32>(acc[n][i], lane);
-            if (grp < 2) wacc[wave][4 * grp + i][16 * n + col] = fmaf(lo, 0x1p-11f, acc[n][i]);
+            if (grp < 2) wacc[wave][4 * grp + i][16 * n + col] = acc[n][i] + lo;
         }
     if (lane < kGP) {
         wm[wave][lane] = m_run;
-        wl[wave][lane] = bad_q > 0.f ? NAN : l_run;
+        wl[wave][lane] = bad_q ? NAN : l_run * 0x1p-15f;
     }
     __syncthreads();
     for (int i = tid; i < G * kD; i += kAThreads) {
@@ -697,6 +861,10 @@ __global__ __launch_bounds__(kAThreads) void q8_partial_kernel(Q8Args a) {
             s = fmaf(wacc[u][g][j], e, s);
             l = fmaf(wl[u][g], e, l);
         }
+        if (a.out) {
+            a.out[((int64_t)b * a.Hq + h * G + g) * kD + j] = l == 0.f ? 0.f : s / l;
+            continue;
+        }
         const int64_t slot = slot0 + (int64_t)g * (NC + kResSlots);
         a.ws_acc[slot * kD + j] = s;
         if (j == 0) {
@@ -704,58 +872,158 @@ __global__ __launch_bounds__(kAThreads) void q8_partial_kernel(Q8Args a) {
             a.ws_l[slot] = l;
         }
     }
+    if constexpr (TRACK) {
+        if (!a.scores) return;
+        // the whole step is here: every block's weight (the barrier above orders
+        // the wavefronts' writes of lse)
+        float total[kGP];
+#pragma unroll
+        for (int g = 0; g < kGP; ++g) {
+            float M = wm[0][g], l = 0.f;
+#pragma unroll
+            for (int u = 1; u < kAWaves; ++u) M = fmaxf(M, wm[u][g]);
+#pragma unroll
+            for (int u = 0; u < kAWaves; ++u) l = fmaf(wl[u][g], exp2f(wm[u][g] - M), l);
+            total[g] = l == 0.f ? INFINITY : M + log2f(l);
+        }
+        for (int u = tid; u < vis.count; u += kAThreads) {
+            const int64_t i = ((int64_t)b * a.Hkv + h) * nb_cap + block_of(u);
+            float w = 0.f;
+#pragma unroll
+            for (int g = 0; g < kGP; ++g)
+                if (g < G) w += exp2f(a.lse[i * G + g] - total[g]);
+            a.scores[i] += w;
+        }
+    }
 }
 
-// ------------------------------------------------------------------- scores
+// ----------------------------------------------------- merge and the scores
 
-struct ScoreArgs {
+struct FinishArgs {
     const int32_t* seq_lens;
     const int32_t* extra_lens;
     const float* lse;
     const int32_t* ws_hdr;
     const float* ws_m;
     const float* ws_l;
-    float* scores;
+    const float* ws_acc;
+    float* out;                  // [B][Hq][128], or NULL
+    float* scores;               // [B][Hkv][t_cap / 32], or NULL
     int Hq, Hkv, G, t_cap, window, sinks, nc_max;
+    int nc;                      // chunk slots per sequence, 0: as the workspace says
+    int heads;                   // workgroups per KV head that merge: G or 0
 };
 
-// scores[b][h][blk] += sum_g 2^(lse of the block - lse of all the step's
-// tokens).  The latter comes from the partials' maxima and sums, once per
-// workgroup; a thread takes one visible block.
-__global__ __launch_bounds__(256) void q8_scores_kernel(ScoreArgs a) {
-    __shared__ float total[kGP];
-    const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
-    const int lane = tid & (kWave - 1), wave = tid / kWave;
-    const int G = a.G;
-    const int chunk = max(a.ws_hdr[0], 1), NC = min(max(a.ws_hdr[1], 1), a.nc_max);
-    const int residual = min(max(a.ws_hdr[2], 0), kResSlots);
-    const int T = max(0, min(a.seq_lens[b], a.t_cap));
-    const int extra = a.extra_lens ? max(0, a.extra_lens[b]) : 0;
-    const Visible vis = visible(T, extra, a.window, a.sinks);
-    const int v = blockIdx.x * 256 + tid;
-    if ((int)blockIdx.x * 256 >= vis.count) return;
-    const int nc = (int)min((int64_t)NC, ((int64_t)T + chunk - 1) / chunk), np = nc + residual;
-    for (int g = wave; g < G; g += 4) {
-        const int64_t base = ((int64_t)b * a.Hq + h * G + g) * (NC + kResSlots);
-        float M = -INFINITY;
-        for (int i = lane; i < np; i += kWave) M = fmaxf(M, a.ws_m[base + (i < nc ? i : NC + i - nc)]);
-        M = wave_max(M);
-        float l = 0.f;
-        if (M != -INFINITY)
-            for (int i = lane; i < np; i += kWave) {
-                const int64_t s = base + (i < nc ? i : NC + i - nc);
-                l += a.ws_l[s] * exp2f(a.ws_m[s] - M);
-            }
-        l = wave_sum(l);
-        if (lane == 0) total[g] = M == -INFINITY ? INFINITY : M + log2f(l);
+constexpr int kScoreBlocks = 128;            // blocks per workgroup of the scores
+constexpr int kFinishFirst = 8;              // partials requested at once
+constexpr int kFinishBatch = 16;             // partials per further memory round trip
+
+// One wavefront per workgroup.  The first G of a (KV head, sequence) merge one
+// query head each, lane l holding channels 2 l and 2 l + 1; the others add
+// block weights to the scores: sum_g 2^(lse of the block - lse of the step),
+// the latter from the partials' maxima and sums (as many partials as lanes or
+// fewer, in general).
+__global__ __launch_bounds__(kWave) void q8_finish_kernel(FinishArgs a) {
+    const int h = blockIdx.y, b = blockIdx.z, lane = threadIdx.x, G = a.G;
+    // (the stores of this kernel are to other memory than these loads)
+    const int NC = a.nc ? a.nc : min(max(scalar_load(a.ws_hdr + 1), 1), a.nc_max);
+    const int64_t base = ((int64_t)b * a.Hq + h * G) * (NC + kResSlots);
+    // a merging wavefront requests its first partials before it knows how many there are
+    float2 x[kFinishBatch];
+    float m_lane = 0.f, l_lane = 0.f;
+    const bool merge = (int)blockIdx.x < a.heads;
+    if (merge) {
+        const int64_t s0 = base + (int64_t)blockIdx.x * (NC + kResSlots);
+        const int64_t s1 = s0 + min(lane, NC + kResSlots - 1);
+        m_lane = a.ws_m[s1];
+        l_lane = a.ws_l[s1];
+#pragma unroll
+        for (int u = 0; u < kFinishFirst; ++u)
+            x[u] = *(reinterpret_cast<const float2*>(a.ws_acc + (s0 + min(u, NC - 1)) * kD) + lane);
     }
-    __syncthreads();
-    if (v >= vis.count) return;
-    const int blk = v < vis.head ? v : vis.from + v - vis.head;
-    const int64_t i = ((int64_t)b * a.Hkv + h) * (a.t_cap / kBlk) + blk;
-    float w = 0.f;
-    for (int g = 0; g < G; ++g) w += exp2f(a.lse[i * G + g] - total[g]);
-    a.scores[i] += w;
+    const int chunk = max(scalar_load(a.ws_hdr), 1);
+    const int residual = a.nc ? 0 : min(max(scalar_load(a.ws_hdr + 2), 0), kResSlots);
+    const int T = max(0, min(scalar_load(a.seq_lens + b), a.t_cap));
+    const int nc = (int)min((int64_t)NC, ((int64_t)T + chunk - 1) / chunk), np = nc + residual;
+    auto slot_of = [&](int g, int i) { return base + (int64_t)g * (NC + kResSlots) + (i < nc ? i : NC + i - nc); };
+    if (merge) {
+        // the merge runs where no residual window does: partials 0 .. nc - 1
+        const int g = blockIdx.x;
+        float2* dst = reinterpret_cast<float2*>(a.out + ((int64_t)b * a.Hq + h * G + g) * kD) + lane;
+        if (lane >= nc) m_lane = -INFINITY;
+        float M = m_lane;
+        for (int i = lane + kWave; i < nc; i += kWave) M = fmaxf(M, a.ws_m[slot_of(g, i)]);
+        M = wave_max(M);
+        if (M == -INFINITY) {
+            *dst = float2{0.f, 0.f};
+            return;
+        }
+        const float e_lane = lane < nc ? exp2f(m_lane - M) : 0.f;
+        float l = wave_sum(lane < nc ? l_lane * e_lane : 0.f);
+        float2 acc = {0.f, 0.f};
+        auto add = [&](int i0, int n) {
+#pragma unroll
+            for (int u = 0; u < kFinishBatch; ++u) {
+                const int i = i0 + u;
+                if (u < n && i < nc) {
+                    float e;
+                    if (i < kWave) {
+                        e = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(e_lane), i));
+                    } else {
+                        e = exp2f(a.ws_m[slot_of(g, i)] - M);
+                        l += a.ws_l[slot_of(g, i)] * e;
+                    }
+                    acc.x = fmaf(x[u].x, e, acc.x);
+                    acc.y = fmaf(x[u].y, e, acc.y);
+                }
+            }
+        };
+        add(0, kFinishFirst);
+        for (int i0 = kFinishFirst; i0 < nc; i0 += kFinishBatch) {
+#pragma unroll
+            for (int u = 0; u < kFinishBatch; ++u)
+                x[u] = *(reinterpret_cast<const float2*>(a.ws_acc + slot_of(g, min(i0 + u, nc - 1)) * kD) + lane);
+            add(i0, kFinishBatch);
+        }
+        *dst = float2{acc.x / l, acc.y / l};
+        return;
+    }
+    const int extra = a.extra_lens ? max(0, scalar_load(a.extra_lens + b)) : 0;
+    const Visible vis = visible(T, extra, a.window, a.sinks);
+    const int first = ((int)blockIdx.x - a.heads) * kScoreBlocks;
+    if (first >= vis.count) return;
+    float m[kGP], l[kGP], total[kGP];
+#pragma unroll
+    for (int g = 0; g < kGP; ++g) {
+        const bool in = g < G && lane < np;
+        const int64_t s = slot_of(min(g, G - 1), min(lane, max(np - 1, 0)));
+        m[g] = in ? a.ws_m[s] : -INFINITY;
+        l[g] = in ? a.ws_l[s] : 0.f;
+    }
+#pragma unroll
+    for (int g = 0; g < kGP; ++g) {
+        total[g] = INFINITY;
+        if (g < G) {
+            float M = m[g];
+            for (int i = lane + kWave; i < np; i += kWave) M = fmaxf(M, a.ws_m[slot_of(g, i)]);
+            M = wave_max(M);
+            if (M != -INFINITY) {
+                float sum = l[g] * exp2f(m[g] - M);
+                for (int i = lane + kWave; i < np; i += kWave)
+                    sum += a.ws_l[slot_of(g, i)] * exp2f(a.ws_m[slot_of(g, i)] - M);
+                total[g] = M + log2f(wave_sum(sum));
+            }
+        }
+    }
+    for (int v = first + lane; v < min(first + kScoreBlocks, vis.count); v += kWave) {
+        const int blk = v < vis.head ? v : vis.from + v - vis.head;
+        const int64_t i = ((int64_t)b * a.Hkv + h) * (a.t_cap / kBlk) + blk;
+        float w = 0.f;
+#pragma unroll
+        for (int g = 0; g < kGP; ++g)
+            if (g < G) w += exp2f(a.lse[i * G + g] - total[g]);
+        a.scores[i] += w;
+    }
 }
 
 // ----------------------------------------------------------------- eviction
@@ -772,11 +1040,13 @@ struct EvictArgs {
     float* to_scale[2];
     uint32_t* status;
     Pages pg;
-    int H, t_cap, nb_cap, to_cap, keep, first, last;   // blocks
-    int parts;
+    int H, t_cap, nb_cap, to_cap, keep, first, last;   // blocks, but t_cap
 };
 
-constexpr int kSelThreads = 256;
+constexpr int kSelThreads = 1024;
+constexpr int kSelWaves = kSelThreads / kWave;
+constexpr int kSelKeys = 8;                  // blocks per thread and round
+constexpr int kDigits = 2048;                // 11 bits of a key per pass
 
 // Floats as unsigned integers of the same order (both zeros equal); NaN lowest.
 __device__ __forceinline__ uint32_t order_key(float x) {
@@ -786,14 +1056,17 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 }
 
 // One workgroup per (KV head, sequence) chooses the blocks: a radix selection
-// over the 32-bit keys of the blocks that are neither among the first nor the
-// newest finds the smallest kept key and how many of its ties are kept (the
-// lowest indexes), then one scan in block order writes the list and moves the
-// scores and the two scales, each to a place at or before its own.
+// (11, 11 and 10 bits) over the keys of the blocks that are neither among the
+// first nor the newest finds the smallest kept key and how many of its ties are
+// kept (the lowest indexes), then one scan in block order writes the list and
+// moves the scores and the two scales, each to a place at or before its own.
+// Up to 8192 blocks (262144 tokens) are read once and stay in registers; longer
+// sequences are read again in each pass and scanned in rounds of 8192.
 __global__ __launch_bounds__(kSelThreads) void q8_select_kernel(EvictArgs a) {
-    __shared__ uint32_t hist[256];
+    __shared__ uint32_t hist[kDigits];
+    __shared__ uint32_t part[kSelWaves];
     __shared__ uint32_t s_bin, s_rem;
-    __shared__ int s_tie[kSelThreads / kWave], s_kept[kSelThreads / kWave];
+    __shared__ int s_tie[kSelKeys][kSelWaves], s_kept[kSelKeys][kSelWaves];
     const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
     const int lane = tid & (kWave - 1), wave = tid / kWave;
     const int T = max(0, min(a.seq_lens[b], a.t_cap));
@@ -804,125 +1077,152 @@ __global__ __launch_bounds__(kSelThreads) void q8_select_kernel(EvictArgs a) {
     int32_t* kept = a.kept + row * a.keep;
     const bool cut = nb > a.keep;
     const int lo = cut ? a.first : nb, hi = cut ? nb - a.last : nb;   // the blocks to choose from
+    constexpr int kRound = kSelKeys * kSelThreads;
+    float s[kSelKeys], x[kSelKeys][2];
+    bool bad = false;
+    auto read = [&](int i0) {
+#pragma unroll
+        for (int r = 0; r < kSelKeys; ++r) {
+            const int i = i0 + r * kSelThreads + tid;
+            s[r] = x[r][0] = x[r][1] = 0.f;
+            if (i < nb) {
+                s[r] = sc[i];
+                const int64_t bi = block_index(a.pg, a.H, a.nb_cap, b, h, i, bad);
+                x[r][0] = a.scale[0][bi];
+                x[r][1] = a.scale[1][bi];
+            }
+        }
+    };
+    read(0);
     uint32_t prefix = 0, rem = cut ? (uint32_t)(a.keep - a.first - a.last) : 0u;
-    if (cut && rem > 0) {
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            hist[tid] = 0u;
+    const bool choose = rem > 0;
+    if (choose) {
+        for (int pass = 0; pass < 3; ++pass) {
+            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+            const uint32_t digits = pass == 2 ? 1024u : 2048u;
+            auto count = [&](float score, int i) {
+                const uint32_t key = order_key(score);
+                if (i >= lo && i < hi && (pass == 0 || (key >> (shift + (pass == 2 ? 10 : 11))) == prefix))
+                    atomicAdd(&hist[(key >> shift) & (digits - 1)], 1u);
+            };
+            hist[tid] = hist[tid + kSelThreads] = 0u;
             __syncthreads();
-            for (int i = lo + tid; i < hi; i += kSelThreads) {
-                const uint32_t key = order_key(sc[i]);
-                if (shift == 24 || (key >> (shift + 8)) == prefix) atomicAdd(&hist[(key >> shift) & 255u], 1u);
+#pragma unroll
+            for (int r = 0; r < kSelKeys; ++r) {
+                const int i = r * kSelThreads + tid;
+                if (i < nb) count(s[r], i);
+            }
+            for (int i = kRound + tid; i < nb; i += kSelThreads) count(sc[i], i);
+            __syncthreads();
+            // thread t: the digits 2047 - 2 t and 2046 - 2 t, counted from the top
+            const int d = kDigits - 1 - 2 * tid;
+            const uint32_t n0 = hist[d], n1 = hist[d - 1];
+            uint32_t incl = n0 + n1;
+#pragma unroll
+            for (int k = 1; k < kWave; k <<= 1) {
+                const uint32_t o = __shfl_up(incl, k);
+                if (lane >= k) incl += o;
+            }
+            if (lane == kWave - 1) part[wave] = incl;
+            __syncthreads();
+            uint32_t above = incl - n0 - n1;
+            for (int w = 0; w < wave; ++w) above += part[w];
+            if (above < rem && rem <= above + n0) {
+                s_bin = (uint32_t)d;
+                s_rem = rem - above;
+            } else if (above + n0 < rem && rem <= above + n0 + n1) {
+                s_bin = (uint32_t)(d - 1);
+                s_rem = rem - above - n0;
             }
             __syncthreads();
-            if (wave == 0) {
-                // bins 4 (63 - lane) + 3 .. 4 (63 - lane), from the top
-                const int bin = 4 * (63 - lane);
-                uint32_t n[4], own = 0;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    n[k] = hist[bin + 3 - k];
-                    own += n[k];
-                }
-                uint32_t incl = own;
-                for (int d = 1; d < kWave; d <<= 1) {
-                    const uint32_t o = __shfl_up(incl, d);
-                    if (lane >= d) incl += o;
-                }
-                uint32_t before = incl - own;
-                if (before < rem && rem <= incl) {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        if (before < rem && rem <= before + n[k]) {
-                            s_bin = (uint32_t)(bin + 3 - k);
-                            s_rem = rem - before;
-                        }
-                        before += n[k];
-                    }
-                }
-            }
-            __syncthreads();
-            prefix = (prefix << 8) | s_bin;
+            prefix = (prefix << (pass == 2 ? 10 : 11)) | s_bin;
             rem = s_rem;
         }
     }
     // keys above `prefix` are kept, and the first `rem` equal to it
-    const bool choose = cut && a.keep > a.first + a.last;
     int ties = 0, n = 0;                                  // of the blocks before this round
-    for (int i0 = 0; i0 < nb; i0 += kSelThreads) {
-        const int i = i0 + tid;
-        bool tie = false, keep = false;
-        float s = 0.f, x[2] = {0.f, 0.f};
-        bool bad = false;
-        if (i < nb) {
-            s = sc[i];
-            const int64_t bi = block_index(a.pg, a.H, a.nb_cap, b, h, i, bad);
-            x[0] = a.scale[0][bi];
-            x[1] = a.scale[1][bi];
-            keep = i < lo || i >= hi;
-            if (!keep && choose) {
-                const uint32_t key = order_key(s);
-                keep = key > prefix;
-                tie = key == prefix;
-            }
-        }
-        const uint64_t tb = __builtin_amdgcn_ballot_w64(tie);
-        const uint64_t below = (1ull << lane) - 1ull;
-        if (lane == 0) s_tie[wave] = __popcll(tb);
-        __syncthreads();
-        int t = ties + __popcll(tb & below);
+    const uint64_t below = (1ull << lane) - 1ull;
+    for (int i0 = 0; i0 < nb; i0 += kRound) {
+        if (i0) read(i0);
+        uint32_t keep = 0, tie = 0;                       // bit r: block i0 + 1024 r + tid
+        int t[kSelKeys], pos[kSelKeys];
 #pragma unroll
-        for (int u = 0; u < kSelThreads / kWave; ++u) {
-            if (u < wave) t += s_tie[u];
-            ties += s_tie[u];
-        }
-        if (tie && t < (int)rem) keep = true;
-        const uint64_t kb = __builtin_amdgcn_ballot_w64(keep);
-        if (lane == 0) s_kept[wave] = __popcll(kb);
-        __syncthreads();
-        int pos = n + __popcll(kb & below);
-#pragma unroll
-        for (int u = 0; u < kSelThreads / kWave; ++u) {
-            if (u < wave) pos += s_kept[u];
-            n += s_kept[u];
-        }
-        if (keep) {
-            kept[pos] = i;
-            to[pos] = s;
-            bool tbad = false;
-            const int64_t ti = block_index(a.pg, a.H, a.to_cap, b, h, pos, tbad);
-            if (!tbad) {
-                a.to_scale[0][ti] = x[0];
-                a.to_scale[1][ti] = x[1];
+        for (int r = 0; r < kSelKeys; ++r) {
+            const int i = i0 + r * kSelThreads + tid;
+            if (i < nb) {
+                bool k = i < lo || i >= hi;
+                if (!k && choose) {
+                    const uint32_t key = order_key(s[r]);
+                    k = key > prefix;
+                    tie |= (key == prefix ? 1u : 0u) << r;
+                }
+                keep |= (k ? 1u : 0u) << r;
             }
-            if ((bad || tbad) && a.status) atomicOr(a.status, DQ_STATUS_PAGE);
+            const uint64_t tb = __builtin_amdgcn_ballot_w64((tie >> r) & 1u);
+            t[r] = __popcll(tb & below);
+            if (lane == 0) s_tie[r][wave] = __popcll(tb);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kSelKeys; ++r) {
+            int before = ties;
+            for (int w = 0; w < kSelWaves; ++w) {
+                if (w == wave) before = ties;
+                ties += s_tie[r][w];
+            }
+            if (((tie >> r) & 1u) && before + t[r] < (int)rem) keep |= 1u << r;
+            const uint64_t kb = __builtin_amdgcn_ballot_w64((keep >> r) & 1u);
+            pos[r] = __popcll(kb & below);
+            if (lane == 0) s_kept[r][wave] = __popcll(kb);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kSelKeys; ++r) {
+            int before = n;
+            for (int w = 0; w < kSelWaves; ++w) {
+                if (w == wave) before = n;
+                n += s_kept[r][w];
+            }
+            if ((keep >> r) & 1u) {
+                const int p = before + pos[r];
+                kept[p] = i0 + r * kSelThreads + tid;
+                to[p] = s[r];
+                bool tbad = false;
+                const int64_t ti = block_index(a.pg, a.H, a.to_cap, b, h, p, tbad);
+                if (!tbad) {
+                    a.to_scale[0][ti] = x[r][0];
+                    a.to_scale[1][ti] = x[r][1];
+                }
+                bad |= tbad;
+            }
         }
         __syncthreads();
     }
+    if (bad && a.status) atomicOr(a.status, DQ_STATUS_PAGE);
     for (int i = n + tid; i < a.keep; i += kSelThreads) kept[i] = -1;
     for (int i = n + tid; i < min(nb, a.to_cap); i += kSelThreads) to[i] = 0.f;
 }
 
-// The kept blocks' codes move to their places, which lie at or before their
-// old ones, in order.  A wavefront owns 256 bytes of every block of one (KV
-// head, sequence) and tensor and walks through the list: it reads 4 kMoveU
-// blocks' pieces, waits for all of them and writes them.  What it writes to has
-// been read by itself before, so no wavefront waits for another; into another
-// cache nothing overlaps and the list is cut into parts as well.
+__device__ __forceinline__ void new_length(const EvictArgs& a, int b) {
+    const int T = max(0, min(a.seq_lens[b], a.t_cap));   // read by nobody else in this launch: it may be new_lens[b]
+    const int nb = (T + kBlk - 1) / kBlk;
+    a.new_lens[b] = T - max(0, nb - a.keep) * kBlk;
+}
+
+// In place the kept blocks' codes move to places at or before their old ones,
+// in order.  A wavefront owns 256 bytes of every block of one (KV head,
+// sequence) and tensor and walks through the list: it reads 4 kMoveU blocks'
+// pieces, waits for all of them and writes them.  What it writes to has been
+// read by itself before, so no wavefront waits for another.
 constexpr int kMoveU = 8;
 
 __global__ __launch_bounds__(kWave) void q8_move_kernel(EvictArgs a) {
-    const int slice = blockIdx.x & 31, part = blockIdx.x >> 5, h = blockIdx.y, b = blockIdx.z;
+    const int slice = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
     const int lane = threadIdx.x;
-    if (blockIdx.x == 0 && h == 0 && lane == 0) {
-        const int T = max(0, min(a.seq_lens[b], a.t_cap));   // read by nobody else: it may be new_lens[b]
-        const int nb = (T + kBlk - 1) / kBlk;
-        a.new_lens[b] = T - max(0, nb - a.keep) * kBlk;
-    }
+    if (slice == 0 && h == 0 && lane == 0) new_length(a, b);
     const int which = slice >> 4, off = (slice & 15) * 256 + (lane & 15) * 16;
     const int32_t* kept = a.kept + ((int64_t)b * a.H + h) * a.keep;
-    const int per = (a.keep + a.parts - 1) / a.parts;
-    const int end = min(a.keep, (part + 1) * per);
-    for (int i0 = part * per; i0 < end; i0 += 4 * kMoveU) {
+    for (int i0 = 0; i0 < a.keep; i0 += 4 * kMoveU) {
         if (kept[i0] < 0) break;      // the list ends
         uint4 x[kMoveU];
         uint4* to[kMoveU];
@@ -930,17 +1230,15 @@ __global__ __launch_bounds__(kWave) void q8_move_kernel(EvictArgs a) {
         for (int u = 0; u < kMoveU; ++u) {
             const int i = i0 + 4 * u + (lane >> 4);
             to[u] = nullptr;
-            if (i < end) {
+            if (i < a.keep) {
                 const int from = kept[i];
-                if (from >= 0) {
+                if (from > i) {
                     bool bad = false;
                     const int64_t si = block_index(a.pg, a.H, a.nb_cap, b, h, from, bad);
                     const int64_t di = block_index(a.pg, a.H, a.to_cap, b, h, i, bad);
-                    const uint8_t* src = a.data[which] + si * kBlkBytes + off;
-                    uint8_t* dst = a.to_data[which] + di * kBlkBytes + off;
-                    if (!bad && src != dst) {
-                        x[u] = *reinterpret_cast<const uint4*>(src);
-                        to[u] = reinterpret_cast<uint4*>(dst);
+                    if (!bad) {
+                        x[u] = *reinterpret_cast<const uint4*>(a.data[which] + si * kBlkBytes + off);
+                        to[u] = reinterpret_cast<uint4*>(a.to_data[which] + di * kBlkBytes + off);
                     }
                 }
             }
@@ -952,6 +1250,24 @@ __global__ __launch_bounds__(kWave) void q8_move_kernel(EvictArgs a) {
         for (int u = 0; u < kMoveU; ++u)
             if (to[u]) *to[u] = x[u];
     }
+}
+
+// Into another cache nothing overlaps: a wavefront per kept block and tensor.
+__global__ __launch_bounds__(256) void q8_copy_kernel(EvictArgs a) {
+    const int h = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & (kWave - 1);
+    if (blockIdx.x == 0 && h == 0 && threadIdx.x == 0) new_length(a, b);
+    const int w = wave_index(4), i = w >> 1, which = w & 1;
+    if (i >= a.keep) return;
+    const int64_t row = (int64_t)b * a.H + h;
+    const int from = a.kept[row * a.keep + i];
+    if (from < 0) return;
+    const uint4* src = reinterpret_cast<const uint4*>(a.data[which] + (row * a.nb_cap + from) * kBlkBytes) + lane;
+    uint4* dst = reinterpret_cast<uint4*>(a.to_data[which] + (row * a.to_cap + i) * kBlkBytes) + lane;
+    uint4 x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = src[64 * k];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) dst[64 * k] = x[k];
 }
 
 }  // namespace
@@ -1028,34 +1344,72 @@ int launch_q8_read(int format, const Pages& pg, const Q8Cache& from, int32_t B, 
 
 namespace {
 
-// Chunks of visible blocks: about six workgroups per CU but at most 64 chunks
-// per sequence (the merge takes 64 partials in one pass, one per lane), at
-// least one block for every wavefront.
+// Blocks of one sequence that a step can see.
+int64_t seen_blocks(int t_cap, int window, int sinks) {
+    const int64_t nb = t_cap / kBlk;
+    // a window of w tokens meets at most w / 32 + 2 blocks
+    return window > 0 ? std::min(nb, ((int64_t)sinks + kBlk - 1) / kBlk + (int64_t)window / kBlk + 2) : nb;
+}
+
+// How a step is cut.
 struct Q8Plan {
-    int chunk, nchunks;          // blocks per chunk, chunks
+    int chunk, nchunks;          // blocks per chunk, chunk slots per sequence
+    int target, items;           // > 0: chunks over all sequences, workgroups per KV head
+    bool whole;                  // one chunk per sequence, nothing to merge
 };
 
-Q8Plan q8_plan(int B, int Hkv, int t_cap, int window, int sinks) {
-    int64_t nb = t_cap / kBlk;
-    if (window > 0) {
-        // a window of w tokens meets at most w / 32 + 2 blocks
-        const int64_t seen = ((int64_t)sinks + kBlk - 1) / kBlk + (int64_t)window / kBlk + 2;
-        nb = std::min(nb, seen);
+// One chunk per sequence where it is short (up to 16 blocks: 8 KV heads of one
+// sequence of 512 tokens take 7.5 us in one launch, 8.0 in two) or where the
+// (sequence, KV head) pairs fill the CUs by themselves (half of them: up to 64
+// blocks, 16 sequences of 2048 tokens 17.1 against 18.5 us; twice: up to 128,
+// 64 of 4096 93 against 99 us; beyond, unlike lengths would leave CUs idle).
+// Else about two workgroups per CU, which is what fits: at 16 x 32768 tokens
+// one takes 189 us, two 185, three 188.  At most 32 chunks per sequence (one
+// sequence of 32768 tokens: 19.5 us against 21.8 with 64) unless that leaves
+// CUs without work, of four blocks at least (eight wavefronts, then, have half
+// a block each), eight once the blocks are more than four per CU.
+Q8Plan q8_plan(int B, int Hkv, int t_cap, int window, int sinks, bool whole) {
+    const int64_t nb = seen_blocks(t_cap, window, sinks);
+    const int64_t pairs = (int64_t)B * Hkv, cus = cu_count();
+    Q8Plan p{};
+    if (whole && (nb <= 16 || (2 * pairs >= cus && nb <= 64) || (pairs >= 2 * cus && nb <= 128))) {
+        p.chunk = (int)nb;
+        p.nchunks = 1;
+        p.whole = true;
+        return p;
     }
-    const int64_t pairs = (int64_t)B * Hkv;
-    const int64_t nc = std::max<int64_t>(1, std::min<int64_t>((6 * cu_count() + pairs - 1) / pairs, 64));
+    const int64_t most = std::min((nb + 3) / 4, std::max<int64_t>(32, (cus + pairs - 1) / pairs));
+    if (window == 0 && B <= 256 && B * nb < (1 << 30)) {
+        p.nchunks = (int)most;
+        p.target = (int)std::max<int64_t>(1, 2 * cus / Hkv);
+        p.items = (int)std::min<int64_t>(3 * p.target + B, B * most);
+        return p;
+    }
+    const int64_t nc = std::min((2 * cus + pairs - 1) / pairs, most);
     int64_t chunk = (nb + nc - 1) / nc;
-    chunk = std::max<int64_t>((chunk + kAWaves - 1) / kAWaves * kAWaves, kAWaves);
-    return Q8Plan{(int)chunk, (int)((nb + chunk - 1) / chunk)};
+    chunk = std::max<int64_t>((chunk + 3) / 4 * 4, nb * pairs > 4 * cus ? 8 : 4);
+    p.chunk = (int)chunk;
+    p.nchunks = (int)((nb + chunk - 1) / chunk);
+    return p;
+}
+
+template <int FMT>
+void launch_q8_format(const Q8Args& a, dim3 grid, hipStream_t stream) {
+    if (a.lse)
+        q8_partial_kernel<FMT, true><<<grid, kAThreads, 0, stream>>>(a);
+    else
+        q8_partial_kernel<FMT, false><<<grid, kAThreads, 0, stream>>>(a);
 }
 
 }  // namespace
 
 int launch_q8_partial(int format, const Pages& pg, const uint16_t* q, int32_t B, int32_t Hq, int32_t Hkv,
                       const Q8Cache& c, const int32_t* seq_lens, const int32_t* extra_lens, int32_t t_cap,
-                      int32_t window, int32_t sinks, float scale, float* lse, void* ws, uint32_t* status,
-                      hipStream_t stream) {
-    const Q8Plan plan = q8_plan(B, Hkv, t_cap, window, sinks);
+                      int32_t window, int32_t sinks, float scale, float* lse, float* out, float* scores, void* ws,
+                      uint32_t* status, hipStream_t stream, bool* done) {
+    const Q8Plan plan = q8_plan(B, Hkv, t_cap, window, sinks, out != nullptr);
+    const bool whole = plan.whole;
+    if (done) *done = whole;
     Q8Args a;
     a.q = q;
     a.k = c.data[0];
@@ -1075,38 +1429,38 @@ int launch_q8_partial(int format, const Pages& pg, const uint16_t* q, int32_t B,
     a.sinks = sinks;
     a.scale_log2 = scale * 1.4426950408889634f;
     a.lse = lse;
+    a.out = whole ? out : nullptr;
+    a.scores = whole ? scores : nullptr;
+    a.B = B;
+    a.target = plan.target;
+    a.early = whole && window == 0 && !pg.bt && (int64_t)Hkv * B <= cu_count();
     a.status = status;
     const int64_t slots = ws_slots(B, Hq, t_cap);
     a.ws_hdr = static_cast<int32_t*>(ws);
     a.ws_acc = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + kWsHeader);
     a.ws_m = a.ws_acc + slots * kD;
     a.ws_l = a.ws_m + slots;
-    const dim3 grid(a.nchunks, Hkv, B);
-    if (format == DQ_Q8_E4M3) {
-        if (lse)
-            q8_partial_kernel<DQ_Q8_E4M3, true><<<grid, kAThreads, 0, stream>>>(a);
-        else
-            q8_partial_kernel<DQ_Q8_E4M3, false><<<grid, kAThreads, 0, stream>>>(a);
-    } else {
-        if (lse)
-            q8_partial_kernel<DQ_Q8_INT8, true><<<grid, kAThreads, 0, stream>>>(a);
-        else
-            q8_partial_kernel<DQ_Q8_INT8, false><<<grid, kAThreads, 0, stream>>>(a);
-    }
+    const dim3 grid = plan.target ? dim3((unsigned)plan.items * Hkv) : dim3(plan.nchunks, Hkv, B);
+    if (format == DQ_Q8_E4M3)
+        launch_q8_format<DQ_Q8_E4M3>(a, grid, stream);
+    else
+        launch_q8_format<DQ_Q8_INT8>(a, grid, stream);
     return hip_check("q8_partial launch", hipGetLastError());
 }
 
-int launch_q8_scores(int32_t B, int32_t Hq, int32_t Hkv, const int32_t* seq_lens, const int32_t* extra_lens,
-                     int32_t t_cap, int32_t window, int32_t sinks, const float* lse, const void* ws, float* scores,
-                     hipStream_t stream) {
+int launch_q8_finish(int32_t B, int32_t Hq, int32_t Hkv, const int32_t* seq_lens, const int32_t* extra_lens,
+                     int32_t t_cap, int32_t window, int32_t sinks, const float* lse, const void* ws, float* out,
+                     float* scores, hipStream_t stream) {
     const int64_t slots = ws_slots(B, Hq, t_cap);
-    ScoreArgs a;
+    FinishArgs a;
     a.seq_lens = seq_lens;
     a.extra_lens = extra_lens;
     a.lse = lse;
     a.ws_hdr = static_cast<const int32_t*>(ws);
-    a.ws_m = reinterpret_cast<const float*>(static_cast<const uint8_t*>(ws) + kWsHeader) + slots * kD;
+    a.ws_acc = reinterpret_cast<const float*>(static_cast<const uint8_t*>(ws) + kWsHeader);
+    a.ws_m = a.ws_acc + slots * kD;
     a.ws_l = a.ws_m + slots;
+    a.out = out;
     a.scores = scores;
     a.Hq = Hq;
     a.Hkv = Hkv;
@@ -1115,10 +1469,12 @@ int launch_q8_scores(int32_t B, int32_t Hq, int32_t Hkv, const int32_t* seq_lens
     a.window = window;
     a.sinks = sinks;
     a.nc_max = (int)(slots / ((int64_t)B * Hq)) - kResSlots;
-    const Q8Plan plan = q8_plan(B, Hkv, t_cap, window, sinks);
-    const int64_t blocks = (int64_t)plan.chunk * plan.nchunks;   // at least the visible ones
-    q8_scores_kernel<<<dim3((unsigned)((blocks + 255) / 256), Hkv, B), 256, 0, stream>>>(a);
-    return hip_check("q8_scores launch", hipGetLastError());
+    // (the partials of the one-call form: the plan is known here)
+    a.nc = out ? q8_plan(B, Hkv, t_cap, window, sinks, true).nchunks : 0;
+    a.heads = out ? a.G : 0;
+    const int64_t parts = scores ? (seen_blocks(t_cap, window, sinks) + kScoreBlocks - 1) / kScoreBlocks : 0;
+    q8_finish_kernel<<<dim3((unsigned)(a.heads + parts), Hkv, B), kWave, 0, stream>>>(a);
+    return hip_check("q8_finish launch", hipGetLastError());
 }
 
 int launch_q8_evict(const Pages& pg, int32_t B, int32_t H, const int32_t* seq_lens, int32_t* new_lens, int32_t t_cap,
@@ -1148,15 +1504,10 @@ int launch_q8_evict(const Pages& pg, int32_t B, int32_t H, const int32_t* seq_le
     a.last = last / kBlk;
     q8_select_kernel<<<dim3(H, B), kSelThreads, 0, stream>>>(a);
     if (int rc = hip_check("q8_select launch", hipGetLastError())) return rc;
-    // into another cache: parts of at least one round of a wavefront, up to
-    // about 16 wavefronts per CU
-    a.parts = 1;
-    if (a.data[0] != a.to_data[0]) {
-        const int64_t waves = 32LL * B * H;
-        a.parts = (int)std::max<int64_t>(
-            1, std::min<int64_t>((16 * cu_count() + waves - 1) / waves, (a.keep + 4 * kMoveU - 1) / (4 * kMoveU)));
-    }
-    q8_move_kernel<<<dim3(32 * a.parts, H, B), kWave, 0, stream>>>(a);
+    if (a.data[0] == a.to_data[0])
+        q8_move_kernel<<<dim3(32, H, B), kWave, 0, stream>>>(a);
+    else
+        q8_copy_kernel<<<dim3((unsigned)((2 * (int64_t)a.keep + 3) / 4), H, B), 256, 0, stream>>>(a);
     return hip_check("q8_move launch", hipGetLastError());
 }
 

@@ -343,7 +343,10 @@ def test_paged(dq, fmt, page):
         assert torch.equal(out, want) and torch.equal(scores, ref.scores)
         dq.dq_q8_decode_attention_paged_partial(fmt, q, *pools, cut, seq, ref.workspace, window, sinks, status=status)
         dq.dq_decode_attention_merge(B, H * G, H, seq, t_cap, ref.workspace, out)
-        assert torch.equal(out, want)
+        # the one-call form cuts the tokens otherwise: the same scores, weights of
+        # 22 bits against other maxima (2 x 2^-22), sums over 32 blocks and their
+        # parts with a rounding of 2^-24 each (2 x 40 x 2^-24): below 2^-17
+        assert ((out - want).norm(dim=2) <= want.norm(dim=2) * 2.0 ** -17).all()
     assert int(status.item()) == 0
     bad = bt.clone()
     bad[0, 0], bad[1, 0] = pools[0].shape[0], -5
