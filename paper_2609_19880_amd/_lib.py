@@ -832,7 +832,7 @@ _RSQRT_D = 128 ** -0.5
 def _q8_workspace(workspace, dev):
     """Pointer and size of the workspace."""
     _need(workspace.device == dev and workspace.is_contiguous(), "workspace must be on the cache's GPU")
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    return workspace.data_ptr(), workspace.nbytes
 
 
 def _q8_sees(window, sinks):
@@ -864,18 +864,30 @@ def dq_q8_decode_attention_partial(fmt, q, k_data, k_scale, v_data, v_scale, seq
 def _q8_attention(fmt: int, cache, q, seq_lens, out, workspace, window, sinks, softmax_scale, block_lse, scores,
                   stream):
     B, H, nb, dev, at = cache
-    n, Hq = _q8_query(q, H, dev)
-    _need(n == B, "q and the cache must have the same batch")
+    if not (q.dtype == torch.bfloat16 and q.dim() == 3 and q.is_contiguous() and q.device == dev
+            and seq_lens.dtype == torch.int32 and seq_lens.is_contiguous() and seq_lens.numel() == B
+            and seq_lens.device == dev and workspace.device == dev and workspace.is_contiguous()):
+        # what is wrong, by name
+        _q8_query(q, H, dev)
+        _q8_lens(seq_lens, B, dev)
+        _q8_workspace(workspace, dev)
+    n, Hq, d = q.shape
+    _need(n == B and d == 128 and 0 <= window <= _INT_MAX and 0 <= sinks <= _INT_MAX,
+          "q must be [batch of the cache, Hq, 128]; window and sinks")
     if out is None:
         out = torch.empty_like(q, dtype=torch.float32)
+    else:
+        _need(out.dtype == torch.float32 and out.shape == q.shape and out.is_contiguous() and out.device == dev,
+              "out must be fp32 of q's shape")
     sc = lse = 0
     if scores is not None or block_lse is not None:
         sc, lse = _q8_scores(scores, block_lse, B, H, nb, Hq // H, dev)
     rc = _lib.dq_q8_decode_attention(
-        fmt, q.data_ptr(), B, Hq, H, *at, _q8_lens(seq_lens, B, dev), nb * DQ_Q8_BLOCK, *_q8_sees(window, sinks),
-        _RSQRT_D if softmax_scale is None else softmax_scale, _q8_out(out, q), lse, sc,
-        *_q8_workspace(workspace, dev), _q8_stream(q, stream))
-    _check(rc, "dq_q8_decode_attention")
+        fmt, q.data_ptr(), B, Hq, H, *at, seq_lens.data_ptr(), nb * DQ_Q8_BLOCK, window, sinks,
+        _RSQRT_D if softmax_scale is None else softmax_scale, out.data_ptr(), lse, sc, workspace.data_ptr(),
+        workspace.nbytes, _q8_stream(q, stream))
+    if rc:
+        _check(rc, "dq_q8_decode_attention")
     return out
 
 

@@ -99,6 +99,31 @@ __device__ __forceinline__ uint32_t codes4(const float (&t)[4]) {
     }
 }
 
+// Whether a quotient within 2^-22 of t, relative, might lie on another side of
+// a border between two codes than t does (or on it).
+//   int8: the border is half an integer away from the nearest one.
+//   e4m3: three bits behind the leading one stay, so borders have the 20 bits
+//   below them at 0x80000; below 2^-6 the steps stay those of 2^-6, which
+//   adding it shows.
+template <int FMT>
+__device__ __forceinline__ bool near_border(const float (&t)[8]) {
+    if constexpr (FMT == DQ_Q8_E4M3) {
+        uint32_t least = ~0u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float m = fabsf(t[i]);
+            const uint32_t u = __float_as_uint(m < 0x1p-6f ? m + 0x1p-6f : m);
+            least = min(least, (u + 0x80008u) & 0xFFFFFu);
+        }
+        return least <= 16u;
+    } else {
+        float most = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(t[i] - ((t[i] + 12582912.f) - 12582912.f)));
+        return most > 0.5f - 0x1p-14f;
+    }
+}
+
 __device__ __forceinline__ uint32_t pk_max(uint32_t a, uint32_t b) {
     const u16x2 x = __builtin_bit_cast(u16x2, a), y = __builtin_bit_cast(u16x2, b);
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(x, y));
@@ -145,26 +170,27 @@ __global__ __launch_bounds__(256) void q8_encode_kernel(EncArgs a) {
     uint32_t x[8][4];
     const int row0 = keys ? col : 4 * grp;
     const int ch0 = keys ? 16 * grp : 8 * col;
+    auto token = [&](int i) { return row0 + 16 * (i >> 2) + (keys ? 0 : i & 3); };
+    auto channel = [&](int i) { return ch0 + (keys ? 64 * ((i >> 1) & 1) + 8 * (i & 1) : 0); };
+    if (rows >= kBlk && a.aligned[which]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int t = row0 + 16 * (i >> 2) + (keys ? 0 : i & 3);
-        const int c = ch0 + (keys ? 64 * ((i >> 1) & 1) + 8 * (i & 1) : 0);
-        uint4 v = uint4{0u, 0u, 0u, 0u};
-        if (t < rows) {
-            const uint16_t* p = src + t * st + c;
-            if (a.aligned[which]) {
-                v = *reinterpret_cast<const uint4*>(p);
-            } else {
-                v.x = (uint32_t)p[0] | ((uint32_t)p[1] << 16);
-                v.y = (uint32_t)p[2] | ((uint32_t)p[3] << 16);
-                v.z = (uint32_t)p[4] | ((uint32_t)p[5] << 16);
-                v.w = (uint32_t)p[6] | ((uint32_t)p[7] << 16);
+        for (int i = 0; i < 8; ++i) {
+            const uint4 v = *reinterpret_cast<const uint4*>(src + token(i) * st + channel(i));
+            x[i][0] = v.x;
+            x[i][1] = v.y;
+            x[i][2] = v.z;
+            x[i][3] = v.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[i][0] = x[i][1] = x[i][2] = x[i][3] = 0u;
+            if (token(i) < rows) {
+                const uint16_t* p = src + token(i) * st + channel(i);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[i][j] = (uint32_t)p[2 * j] | ((uint32_t)p[2 * j + 1] << 16);
             }
         }
-        x[i][0] = v.x;
-        x[i][1] = v.y;
-        x[i][2] = v.z;
-        x[i][3] = v.w;
     }
     // the largest magnitude: bf16 patterns without their signs order as integers
     auto largest = [&]() {
@@ -192,18 +218,29 @@ __global__ __launch_bounds__(256) void q8_encode_kernel(EncArgs a) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) code[i][0] = code[i][1] = 0u;
     } else {
+        // x times the rounded reciprocal is within 2^-22 of the quotient: its code
+        // is the quotient's unless a border is that near, which of the 512 values
+        // at hand one is in 1 of 100 (e4m3) to 1 of 16 cases (int8).  Then
         // quotients of the block brought to magnitudes below 2 (exact powers of
         // 2; what underflows is 2^-149 of the largest value and rounds to 0)
-        const int e = max(-126, min(126, 127 - (top >> 7)));
-        const float f = __uint_as_float((uint32_t)(e + 127) << 23);
-        const float ss = s * f, inv = 1.f / ss;
+        const float inv = 1.f / s;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             float t[8];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                t[2 * j] = quotient_odd(__uint_as_float(x[i][j] << 16) * f, ss, inv);
-                t[2 * j + 1] = quotient_odd(__uint_as_float(x[i][j] & 0xFFFF0000u) * f, ss, inv);
+                t[2 * j] = __uint_as_float(x[i][j] << 16) * inv;
+                t[2 * j + 1] = __uint_as_float(x[i][j] & 0xFFFF0000u) * inv;
+            }
+            if (__builtin_amdgcn_ballot_w64(near_border<FMT>(t))) {
+                const int e = max(-126, min(126, 127 - (top >> 7)));
+                const float f = __uint_as_float((uint32_t)(e + 127) << 23);
+                const float ss = s * f, exact_inv = 1.f / ss;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    t[2 * j] = quotient_odd(__uint_as_float(x[i][j] << 16) * f, ss, exact_inv);
+                    t[2 * j + 1] = quotient_odd(__uint_as_float(x[i][j] & 0xFFFF0000u) * f, ss, exact_inv);
+                }
             }
             const float lo[4] = {t[0], t[1], t[2], t[3]}, hi[4] = {t[4], t[5], t[6], t[7]};
             code[i][0] = codes4<FMT>(lo);
@@ -1043,9 +1080,6 @@ struct EvictArgs {
     int H, t_cap, nb_cap, to_cap, keep, first, last;   // blocks, but t_cap
 };
 
-constexpr int kSelThreads = 1024;
-constexpr int kSelWaves = kSelThreads / kWave;
-constexpr int kSelKeys = 8;                  // blocks per thread and round
 constexpr int kDigits = 2048;                // 11 bits of a key per pass
 
 // Floats as unsigned integers of the same order (both zeros equal); NaN lowest.
@@ -1055,37 +1089,39 @@ __device__ __forceinline__ uint32_t order_key(float x) {
     return (u >> 31) ? ~u : u | 0x80000000u;
 }
 
-// One workgroup per (KV head, sequence) chooses the blocks: a radix selection
-// (11, 11 and 10 bits) over the keys of the blocks that are neither among the
-// first nor the newest finds the smallest kept key and how many of its ties are
-// kept (the lowest indexes), then one scan in block order writes the list and
-// moves the scores and the two scales, each to a place at or before its own.
-// Up to 8192 blocks (262144 tokens) are read once and stay in registers; longer
-// sequences are read again in each pass and scanned in rounds of 8192.
-__global__ __launch_bounds__(kSelThreads) void q8_select_kernel(EvictArgs a) {
-    __shared__ uint32_t hist[kDigits];
+// One workgroup per (KV head, sequence) chooses the blocks, then one scan in
+// block order writes the list and moves the scores and the two scales, each to
+// a place at or before its own.  The choice, among the blocks that are neither
+// the first nor the newest ones:
+//   KEYS = 1 (up to one block per thread): a block's rank, the number of blocks
+//   before it in the order of (score, lower index), counted against all others
+//   (LDS broadcasts, two instructions per pair);
+//   else a radix selection (11, 11 and 10 bits of a key) finds the smallest
+//   kept key and how many of its ties are kept (the lowest indexes).  KEYS
+//   THREADS blocks are read once and stay in registers; longer sequences are
+//   read again in each pass and scanned in rounds of so many.
+template <int THREADS, int KEYS>
+__global__ __launch_bounds__(THREADS) void q8_select_kernel(EvictArgs a) {
+    constexpr int kSelThreads = THREADS, kSelWaves = THREADS / kWave, kSelKeys = KEYS;
+    __shared__ __align__(16) uint32_t hist[KEYS == 1 ? THREADS : kDigits];
     __shared__ uint32_t part[kSelWaves];
     __shared__ uint32_t s_bin, s_rem;
     __shared__ int s_tie[kSelKeys][kSelWaves], s_kept[kSelKeys][kSelWaves];
     const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
     const int lane = tid & (kWave - 1), wave = tid / kWave;
-    const int T = max(0, min(a.seq_lens[b], a.t_cap));
-    const int nb = (T + kBlk - 1) / kBlk;
     const int64_t row = (int64_t)b * a.H + h;
     const float* sc = a.scores + row * a.nb_cap;
     float* to = a.to_scores + row * a.to_cap;
     int32_t* kept = a.kept + row * a.keep;
-    const bool cut = nb > a.keep;
-    const int lo = cut ? a.first : nb, hi = cut ? nb - a.last : nb;   // the blocks to choose from
     constexpr int kRound = kSelKeys * kSelThreads;
     float s[kSelKeys], x[kSelKeys][2];
     bool bad = false;
-    auto read = [&](int i0) {
+    auto read = [&](int i0, int n) {
 #pragma unroll
         for (int r = 0; r < kSelKeys; ++r) {
             const int i = i0 + r * kSelThreads + tid;
             s[r] = x[r][0] = x[r][1] = 0.f;
-            if (i < nb) {
+            if (i < n) {
                 s[r] = sc[i];
                 const int64_t bi = block_index(a.pg, a.H, a.nb_cap, b, h, i, bad);
                 x[r][0] = a.scale[0][bi];
@@ -1093,10 +1129,48 @@ __global__ __launch_bounds__(kSelThreads) void q8_select_kernel(EvictArgs a) {
             }
         }
     };
-    read(0);
+    // the first round is requested before the length is known, but in pages,
+    // whose table may name none behind it
+    if (!a.pg.bt) read(0, a.nb_cap);
+    const int T = max(0, min(a.seq_lens[b], a.t_cap));
+    const int nb = (T + kBlk - 1) / kBlk;
+    if (a.pg.bt) read(0, nb);
+    const bool cut = nb > a.keep;
+    const int lo = cut ? a.first : nb, hi = cut ? nb - a.last : nb;   // the blocks to choose from
     uint32_t prefix = 0, rem = cut ? (uint32_t)(a.keep - a.first - a.last) : 0u;
     const bool choose = rem > 0;
-    if (choose) {
+    bool among = false;                                   // KEYS = 1: this thread's block is kept
+    if constexpr (KEYS == 1) {
+        if (choose) {
+            const uint32_t key = order_key(s[0]);
+            const int m = hi - lo, me = tid - lo;
+            if (me >= 0 && me < m) hist[me] = key;
+            if (tid >= m && tid < ((m + 3) & ~3)) hist[tid] = 0u;   // (nothing is below 0)
+            __syncthreads();
+            // below the wavefront's own blocks ties count, above them they do not
+            const int w0 = min(max(wave * kWave - lo, 0), m) & ~3;
+            const int w1 = min((max((wave + 1) * kWave - lo, 0) + 3) & ~3, (m + 3) & ~3);
+            const uint4* keys = reinterpret_cast<const uint4*>(hist);
+            int rank = 0;
+#pragma unroll 8
+            for (int j = 0; j < w0; j += 4) {
+                const uint4 k = keys[j / 4];
+                rank += (k.x >= key) + (k.y >= key) + (k.z >= key) + (k.w >= key);
+            }
+#pragma unroll 4
+            for (int j = w0; j < w1; j += 4) {
+                const uint4 k = keys[j / 4];
+                rank += (k.x > key || (k.x == key && j < me)) + (k.y > key || (k.y == key && j + 1 < me)) +
+                        (k.z > key || (k.z == key && j + 2 < me)) + (k.w > key || (k.w == key && j + 3 < me));
+            }
+#pragma unroll 8
+            for (int j = w1; j < m; j += 4) {
+                const uint4 k = keys[j / 4];
+                rank += (k.x > key) + (k.y > key) + (k.z > key) + (k.w > key);
+            }
+            among = rank < (int)rem;
+        }
+    } else if (choose) {
         for (int pass = 0; pass < 3; ++pass) {
             const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
             const uint32_t digits = pass == 2 ? 1024u : 2048u;
@@ -1105,7 +1179,7 @@ __global__ __launch_bounds__(kSelThreads) void q8_select_kernel(EvictArgs a) {
                 if (i >= lo && i < hi && (pass == 0 || (key >> (shift + (pass == 2 ? 10 : 11))) == prefix))
                     atomicAdd(&hist[(key >> shift) & (digits - 1)], 1u);
             };
-            hist[tid] = hist[tid + kSelThreads] = 0u;
+            for (int d = tid; d < kDigits; d += kSelThreads) hist[d] = 0u;
             __syncthreads();
 #pragma unroll
             for (int r = 0; r < kSelKeys; ++r) {
@@ -1143,7 +1217,7 @@ __global__ __launch_bounds__(kSelThreads) void q8_select_kernel(EvictArgs a) {
     int ties = 0, n = 0;                                  // of the blocks before this round
     const uint64_t below = (1ull << lane) - 1ull;
     for (int i0 = 0; i0 < nb; i0 += kRound) {
-        if (i0) read(i0);
+        if (i0) read(i0, nb);
         uint32_t keep = 0, tie = 0;                       // bit r: block i0 + 1024 r + tid
         int t[kSelKeys], pos[kSelKeys];
 #pragma unroll
@@ -1151,7 +1225,9 @@ __global__ __launch_bounds__(kSelThreads) void q8_select_kernel(EvictArgs a) {
             const int i = i0 + r * kSelThreads + tid;
             if (i < nb) {
                 bool k = i < lo || i >= hi;
-                if (!k && choose) {
+                if (KEYS == 1) {
+                    k = k || among;
+                } else if (!k && choose) {
                     const uint32_t key = order_key(s[r]);
                     k = key > prefix;
                     tie |= (key == prefix ? 1u : 0u) << r;
@@ -1502,7 +1578,14 @@ int launch_q8_evict(const Pages& pg, int32_t B, int32_t H, const int32_t* seq_le
     a.keep = keep / kBlk;
     a.first = first / kBlk;
     a.last = last / kBlk;
-    q8_select_kernel<<<dim3(H, B), kSelThreads, 0, stream>>>(a);
+    if (a.nb_cap <= 256)
+        q8_select_kernel<256, 1><<<dim3(H, B), 256, 0, stream>>>(a);
+    else if (a.nb_cap <= 512)
+        q8_select_kernel<512, 1><<<dim3(H, B), 512, 0, stream>>>(a);
+    else if (a.nb_cap <= 4096)
+        q8_select_kernel<1024, 4><<<dim3(H, B), 1024, 0, stream>>>(a);
+    else
+        q8_select_kernel<1024, 8><<<dim3(H, B), 1024, 0, stream>>>(a);
     if (int rc = hip_check("q8_select launch", hipGetLastError())) return rc;
     if (a.data[0] == a.to_data[0])
         q8_move_kernel<<<dim3(32, H, B), kWave, 0, stream>>>(a);
