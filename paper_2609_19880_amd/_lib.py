@@ -709,11 +709,16 @@ def _q8_cache_args(k_data, k_scale, v_data, v_scale):
 
 
 def _q8_rows_args(k, v, heads, dev):
+    """Batch and tokens of the rows k and v."""
+    shape = k.shape
+    if (k.dtype == torch.bfloat16 and v.dtype == torch.bfloat16 and len(shape) == 4 and v.shape == shape
+            and shape[3] == 128 and shape[2] == heads and k.stride(3) == 1 and v.stride(3) == 1 and k.device == dev
+            and v.device == dev):
+        return shape[0], shape[1]
     for t, name in ((k, "k"), (v, "v")):
         _need(t.dtype == torch.bfloat16 and t.dim() == 4 and t.shape[3] == 128 and t.stride(3) == 1
               and t.shape[2] == heads and t.device == dev, name + " must be bf16 [B, T, H, 128] on the cache's GPU")
-    _need(v.shape[:2] == k.shape[:2], "k and v must have the same tokens")
-    return k.shape[0], k.shape[1]
+    raise ValueError("k and v must have the same tokens")
 
 
 def _q8_status(status, dev):
@@ -767,20 +772,24 @@ def dq_q8_encode_kv_paged(fmt, k, v, t0: int, block_table, k_pool, k_scale_pool,
 
 
 def _q8_out_rows(k, v, batch, n, heads, dev):
-    if k is None and v is None:
-        return torch.empty((2, batch, n, heads, 128), dtype=torch.bfloat16, device=dev).unbind()
     _need(k is not None and v is not None and _q8_rows_args(k, v, heads, dev) == (batch, n),
           "k and v must be [B, n, H, 128], both or neither")
-    return k, v
 
 
 def _q8_read(fmt: int, cache, t0, n, k, v, stream):
     B, H, nb, dev, at = cache
     _need(0 <= t0 <= _INT_MAX and 0 <= n <= _INT_MAX, "t0 and n")
-    k, v = _q8_out_rows(k, v, B, n, H, dev)
-    rc = _lib.dq_q8_decode_kv(fmt, *at, B, H, t0, n, nb * DQ_Q8_BLOCK, k.data_ptr(), *k.stride()[:3], v.data_ptr(),
-                              *v.stride()[:3], _q8_stream(k, stream))
-    _check(rc, "dq_q8_decode_kv")
+    if k is None and v is None:
+        k, v = torch.empty((2, B, n, H, 128), dtype=torch.bfloat16, device=dev).unbind()
+        sb, st = n * H * 128, H * 128
+        ks = vs = (sb, st, 128)
+    else:
+        _q8_out_rows(k, v, B, n, H, dev)
+        ks, vs = k.stride()[:3], v.stride()[:3]
+    rc = _lib.dq_q8_decode_kv(fmt, *at, B, H, t0, n, nb * DQ_Q8_BLOCK, k.data_ptr(), *ks, v.data_ptr(), *vs,
+                              _q8_stream(k, stream))
+    if rc:
+        _check(rc, "dq_q8_decode_kv")
     return k, v
 
 
@@ -797,7 +806,9 @@ def dq_q8_decode_kv_paged(fmt, k_pool, k_scale_pool, v_pool, v_scale_pool, block
     B = block_table.shape[0]
     max_pages = _q8_table(block_table, B, dev)
     _need(0 <= t0 <= _INT_MAX and 0 <= n <= _INT_MAX, "t0 and n")
-    k, v = _q8_out_rows(k, v, B, n, H, dev)
+    if k is None and v is None:
+        k, v = torch.empty((2, B, n, H, 128), dtype=torch.bfloat16, device=dev).unbind()
+    _q8_out_rows(k, v, B, n, H, dev)
     rc = _lib.dq_q8_decode_kv_paged(f, *at, B, H, t0, n, block_table.data_ptr(), max_pages, bpp * DQ_Q8_BLOCK,
                                     num_pages, k.data_ptr(), *k.stride()[:3], v.data_ptr(), *v.stride()[:3],
                                     _q8_status(status, dev), _q8_stream(k, stream))
@@ -819,10 +830,12 @@ def _q8_out(out, q):
 
 def _q8_scores(scores, block_lse, batch, heads, blocks, group, dev):
     """Pointers of the two score arrays (0 where absent)."""
-    for t, shape, name in ((scores, (batch, heads, blocks), "scores"),
-                           (block_lse, (batch, heads, blocks, group), "block_lse")):
-        _need(t is None or (t.dtype == torch.float32 and tuple(t.shape) == shape and t.is_contiguous()
-                            and t.device == dev), f"{name} must be fp32 {list(shape)} on the cache's GPU")
+    _need(scores is None or (scores.dtype == torch.float32 and scores.shape == (batch, heads, blocks)
+                             and scores.is_contiguous() and scores.device == dev),
+          "scores must be fp32 [B, H, blocks] on the cache's GPU")
+    _need(block_lse is None or (block_lse.dtype == torch.float32 and block_lse.shape == (batch, heads, blocks, group)
+                                and block_lse.is_contiguous() and block_lse.device == dev),
+          "block_lse must be fp32 [B, H, blocks, Hq / H] on the cache's GPU")
     return 0 if scores is None else scores.data_ptr(), 0 if block_lse is None else block_lse.data_ptr()
 
 
