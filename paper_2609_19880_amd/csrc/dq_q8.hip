@@ -38,6 +38,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 // Index of block `blk` of (b, h) in a cache of nb_cap blocks per sequence, or
@@ -135,6 +136,11 @@ __device__ __forceinline__ uint32_t finite_pair(uint32_t w) {
     return w;
 }
 
+// A wavefront's LDS copy of a block of values, between the lanes' order of work
+// (four neighbouring pieces each) and the order of memory (whole lines per
+// access); pieces swap places so that neither order meets a bank twice.
+__device__ __forceinline__ int staged(int piece) { return piece ^ ((piece >> 2) & 3); }
+
 __device__ __forceinline__ uint32_t quad_xor2(uint32_t v) {
     return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, false);   // quad_perm [2, 3, 0, 1]
 }
@@ -146,6 +152,7 @@ __device__ __forceinline__ uint32_t quad_xor2(uint32_t v) {
 // lane and swapped with lane ^ 2, which holds the pieces' other halves.
 template <int FMT>
 __global__ __launch_bounds__(256) void q8_encode_kernel(EncArgs a) {
+    __shared__ __align__(16) uint4 stage[4][256];
     const int lane = threadIdx.x & (kWave - 1);
     int w = wave_index(4);
     const int which = w >= a.total;
@@ -175,11 +182,11 @@ __global__ __launch_bounds__(256) void q8_encode_kernel(EncArgs a) {
     if (rows >= kBlk && a.aligned[which]) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const uint4 v = *reinterpret_cast<const uint4*>(src + token(i) * st + channel(i));
-            x[i][0] = v.x;
-            x[i][1] = v.y;
-            x[i][2] = v.z;
-            x[i][3] = v.w;
+            const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + token(i) * st + channel(i)));
+            x[i][0] = v[0];
+            x[i][1] = v[1];
+            x[i][2] = v[2];
+            x[i][3] = v[3];
         }
     } else {
 #pragma unroll
@@ -274,14 +281,18 @@ __global__ __launch_bounds__(256) void q8_encode_kernel(EncArgs a) {
         // col = 4 np + 2 n2 + half: pieces of channels 32 np + 8 half + x, this
         // lane's bytes 8 n2 ..; the lane with n2 = 0 writes x = 0..3, the other 4..7
         const int n2 = (col >> 1) & 1;
-        uint4* to = dst + ((col >> 2) * 4 + grp) * 16 + 8 * (col & 1) + 4 * n2;
+        uint4* to = stage[threadIdx.x / kWave];
+        const int p0 = ((col >> 2) * 4 + grp) * 16 + 8 * (col & 1) + 4 * n2;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const uint32_t give0 = n2 ? o[k][0] : o[k + 4][0], give1 = n2 ? o[k][1] : o[k + 4][1];
             const uint32_t got0 = quad_xor2(give0), got1 = quad_xor2(give1);
             const uint32_t mine0 = n2 ? o[k + 4][0] : o[k][0], mine1 = n2 ? o[k + 4][1] : o[k][1];
-            to[k] = n2 ? uint4{got0, got1, mine0, mine1} : uint4{mine0, mine1, got0, got1};
+            to[staged(p0 + k)] = n2 ? uint4{got0, got1, mine0, mine1} : uint4{mine0, mine1, got0, got1};
         }
+        wave_sync();
+#pragma unroll
+        for (int p = 0; p < 4; ++p) dst[64 * p + lane] = to[staged(64 * p + lane)];
     }
 }
 
@@ -325,6 +336,7 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
 
 template <int FMT>
 __global__ __launch_bounds__(256) void q8_read_kernel(ReadArgs a) {
+    __shared__ __align__(16) uint4 stage[4][256];
     const int lane = threadIdx.x & (kWave - 1);
     int w = wave_index(4);
     const int which = w >= a.total;
@@ -343,22 +355,30 @@ __global__ __launch_bounds__(256) void q8_read_kernel(ReadArgs a) {
     const int col = lane & 15, grp = lane >> 4;
     const bool keys = which == 0;
     uint32_t code[8][2];         // as in the encoder: 8 channels of one token per i
+    u32x4 piece[4];
+#pragma unroll
+    for (int p = 0; p < 4; ++p)
+        piece[p] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src) + 64 * p + lane);
     if (keys) {
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-            const uint4 v = src[64 * p + lane];
-            code[2 * p][0] = v.x;
-            code[2 * p][1] = v.y;
-            code[2 * p + 1][0] = v.z;
-            code[2 * p + 1][1] = v.w;
+            code[2 * p][0] = piece[p][0];
+            code[2 * p][1] = piece[p][1];
+            code[2 * p + 1][0] = piece[p][2];
+            code[2 * p + 1][1] = piece[p][3];
         }
     } else {
         const int n2 = (col >> 1) & 1;
-        const uint4* from = src + ((col >> 2) * 4 + grp) * 16 + 8 * (col & 1) + 4 * n2;
+        uint4* from = stage[threadIdx.x / kWave];
+        const int p0 = ((col >> 2) * 4 + grp) * 16 + 8 * (col & 1) + 4 * n2;
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+            from[staged(64 * p + lane)] = uint4{piece[p][0], piece[p][1], piece[p][2], piece[p][3]};
+        wave_sync();
         uint32_t o[8][2];
         uint4 v[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = from[k];
+        for (int k = 0; k < 4; ++k) v[k] = from[staged(p0 + k)];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const uint32_t got0 = quad_xor2(n2 ? v[k].x : v[k].z), got1 = quad_xor2(n2 ? v[k].y : v[k].w);
@@ -452,6 +472,8 @@ struct Q8Args {
     int Hq, Hkv, G, t_cap, window, sinks;
     int chunk, nchunks;          // blocks per chunk, chunk slots per sequence
     int B, target;               // target > 0: the chunk length follows the lengths
+    int items;                   // most chunks per KV head
+    float per_cu;                // just below 1 / CUs
     float scale_log2;
     float* lse;                  // [B][Hkv][t_cap / 32][G], or NULL
     float* out;                  // one chunk: the step's result goes here, or NULL
@@ -467,13 +489,16 @@ struct Q8Args {
 constexpr int kAWaves = 8;
 constexpr int kAThreads = kAWaves * kWave;
 constexpr int kGP = 8;                       // query-head slots
+constexpr int kChunkCost = 8;                // what a chunk costs besides its blocks, in blocks
 constexpr float kBig = 3e38f;
 
 typedef const __attribute__((address_space(1))) uint8_t* GlobalBytes;
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
+// Nontemporal: a step reads every block once, and lines that do not settle in
+// L2 stream at 6.7 TB/s where they reached 5.8 (16 x 32768 tokens: 159 us
+// against 184; one sequence of 4096, which would fit: no difference).
 __device__ __forceinline__ uint4 load16(GlobalBytes p) {
-    const u32x4 v = *reinterpret_cast<const __attribute__((address_space(1))) u32x4*>(p);
+    const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const __attribute__((address_space(1))) u32x4*>(p));
     return uint4{v[0], v[1], v[2], v[3]};
 }
 
@@ -525,8 +550,8 @@ __device__ __forceinline__ T scalar_load(const T* p) {
 // `nchunks` in the longest sequence), sequence after sequence, head after head.
 // A batch of unlike lengths then ends much as one of like lengths does, and a
 // buffer's unused capacity costs nothing (chunks cut from the capacity alone:
-// 4096 tokens in a buffer of 131072 28.7 us against 9.9; 16 sequences, one of
-// 131072 and fifteen of 2000 tokens, 134 against 62).
+// 4096 tokens in a buffer of 131072 28.7 us against 10.3; 16 sequences, one of
+// 131072 and fifteen of 2000 tokens, 134 against 60).
 struct Share {
     int b, h, c, chunk;          // c = -1: nothing
 };
@@ -544,12 +569,25 @@ __device__ __forceinline__ int wave_scan(int v) {      // inclusive sums over th
 __device__ __forceinline__ Share share_of(const Q8Args& a, int id, int lane) {
     auto blocks = [&](int T) { return (max(0, min(T, a.t_cap)) + kBlk - 1) / kBlk; };
     auto length = [&](int total, int longest) {
-        int c = (total + a.target - 1) / a.target;
-        // unlike lengths leave many last chunks that are not full: cut finer, but
-        // not below two blocks per wavefront
-        if (total < longest * a.B / 4 * 3) c = max(min(c, 2 * kAWaves), (c + 2) / 3);
-        c = max(c, (longest + a.nchunks - 1) / a.nchunks);
-        return max((c + 3) & ~3, total > 2 * a.target ? 8 : 4);
+        if (total < longest * a.B / 4 * 3) {
+            // unlike lengths leave many last chunks that are not full: six per CU,
+            // but of two blocks per wavefront or more where one per CU has them
+            const int c = (total + a.target - 1) / a.target;
+            const int fine = max(max(min(c, 2 * kAWaves), (c + 5) / 6), (longest + a.nchunks - 1) / a.nchunks);
+            return max((fine + 3) & ~3, 4);
+        }
+        // lane l tries (l + 1) step chunks per sequence: the blocks that the
+        // busiest CU then takes
+        const int step = (a.nchunks + 63) / 64, cuts = (lane + 1) * step;
+        const int c = max(((uint32_t)(longest + cuts - 1) / (uint32_t)cuts + 3) & ~3u, 4u);
+        const int n = (uint32_t)(longest + c - 1) / (uint32_t)c;
+        // (items Hkv is at most 6 CUs + B Hkv)
+        float cost = 3e8f;
+        if (cuts <= a.nchunks && n * a.B <= a.items)
+            cost = ceilf((float)(n * a.B * a.Hkv) * a.per_cu) * (float)(c + kChunkCost);
+        const float least = wave_min(cost);
+        const int best = __builtin_ctzll(__builtin_amdgcn_ballot_w64(cost == least));
+        return __builtin_amdgcn_readlane(c, best);
     };
     if (a.B == 1) {
         const int n = blocks(scalar_load(a.seq_lens)), chunk = length(n, n), used = (n + chunk - 1) / chunk;
@@ -1329,6 +1367,9 @@ __global__ __launch_bounds__(kWave) void q8_move_kernel(EvictArgs a) {
 }
 
 // Into another cache nothing overlaps: a wavefront per kept block and tensor.
+// The old blocks are read past the caches, the new ones stay in them for
+// whoever reads them next (131072 tokens to half and read back: 143 us against
+// 158 without, 150 with both past the caches).
 __global__ __launch_bounds__(256) void q8_copy_kernel(EvictArgs a) {
     const int h = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & (kWave - 1);
     if (blockIdx.x == 0 && h == 0 && threadIdx.x == 0) new_length(a, b);
@@ -1337,11 +1378,11 @@ __global__ __launch_bounds__(256) void q8_copy_kernel(EvictArgs a) {
     const int64_t row = (int64_t)b * a.H + h;
     const int from = a.kept[row * a.keep + i];
     if (from < 0) return;
-    const uint4* src = reinterpret_cast<const uint4*>(a.data[which] + (row * a.nb_cap + from) * kBlkBytes) + lane;
-    uint4* dst = reinterpret_cast<uint4*>(a.to_data[which] + (row * a.to_cap + i) * kBlkBytes) + lane;
-    uint4 x[4];
+    const u32x4* src = reinterpret_cast<const u32x4*>(a.data[which] + (row * a.nb_cap + from) * kBlkBytes) + lane;
+    u32x4* dst = reinterpret_cast<u32x4*>(a.to_data[which] + (row * a.to_cap + i) * kBlkBytes) + lane;
+    u32x4 x[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) x[k] = src[64 * k];
+    for (int k = 0; k < 4; ++k) x[k] = __builtin_nontemporal_load(src + 64 * k);
 #pragma unroll
     for (int k = 0; k < 4; ++k) dst[64 * k] = x[k];
 }
@@ -1435,15 +1476,15 @@ struct Q8Plan {
 };
 
 // One chunk per sequence where it is short (up to 16 blocks: 8 KV heads of one
-// sequence of 512 tokens take 7.5 us in one launch, 8.0 in two) or where the
+// sequence of 512 tokens take 7.5 us in one launch, 7.9 in two) or where the
 // (sequence, KV head) pairs fill the CUs by themselves (half of them: up to 64
-// blocks, 16 sequences of 2048 tokens 17.1 against 18.5 us; twice: up to 128,
-// 64 of 4096 93 against 99 us; beyond, unlike lengths would leave CUs idle).
-// Else about two workgroups per CU, which is what fits: at 16 x 32768 tokens
-// one takes 189 us, two 185, three 188.  At most 32 chunks per sequence (one
-// sequence of 32768 tokens: 19.5 us against 21.8 with 64) unless that leaves
-// CUs without work, of four blocks at least (eight wavefronts, then, have half
-// a block each), eight once the blocks are more than four per CU.
+// blocks, 32 sequences of 2048 tokens 22 against 28 us; twice: up to 128, 128
+// of 4096 158 against 173 us; beyond, unlike lengths would leave CUs idle).
+// Else the kernel or, behind a window, the loop below picks the chunk length
+// for which the busiest CU has the least to do (3 sequences of 32768 tokens:
+// 36 us; two workgroups per CU at any length 40, one 46).  At most 32 chunks
+// per sequence (one of 32768 tokens: 19.5 us against 21.8 with 64, before the
+// loads became nontemporal) unless that leaves CUs without work.
 Q8Plan q8_plan(int B, int Hkv, int t_cap, int window, int sinks, bool whole) {
     const int64_t nb = seen_blocks(t_cap, window, sinks);
     const int64_t pairs = (int64_t)B * Hkv, cus = cu_count();
@@ -1457,13 +1498,19 @@ Q8Plan q8_plan(int B, int Hkv, int t_cap, int window, int sinks, bool whole) {
     const int64_t most = std::min((nb + 3) / 4, std::max<int64_t>(32, (cus + pairs - 1) / pairs));
     if (window == 0 && B <= 256 && B * nb < (1 << 30)) {
         p.nchunks = (int)most;
-        p.target = (int)std::max<int64_t>(1, 2 * cus / Hkv);
-        p.items = (int)std::min<int64_t>(3 * p.target + B, B * most);
+        p.target = (int)std::max<int64_t>(1, cus / Hkv);
+        p.items = (int)std::min<int64_t>(6 * p.target + B, B * most);
         return p;
     }
-    const int64_t nc = std::min((2 * cus + pairs - 1) / pairs, most);
-    int64_t chunk = (nb + nc - 1) / nc;
-    chunk = std::max<int64_t>((chunk + 3) / 4 * 4, nb * pairs > 4 * cus ? 8 : 4);
+    int64_t chunk = nb, best = INT64_MAX;
+    for (int64_t n = 1; n <= std::min<int64_t>(most, 64); ++n) {
+        const int64_t c = ((nb + n - 1) / n + 3) / 4 * 4;
+        const int64_t cost = ((nb + c - 1) / c * pairs + cus - 1) / cus * (c + kChunkCost);
+        if (cost < best) {
+            best = cost;
+            chunk = c;
+        }
+    }
     p.chunk = (int)chunk;
     p.nchunks = (int)((nb + chunk - 1) / chunk);
     return p;
@@ -1509,6 +1556,8 @@ int launch_q8_partial(int format, const Pages& pg, const uint16_t* q, int32_t B,
     a.scores = whole ? scores : nullptr;
     a.B = B;
     a.target = plan.target;
+    a.items = plan.items;
+    a.per_cu = 0.99999f / (float)cu_count();
     a.early = whole && window == 0 && !pg.bt && (int64_t)Hkv * B <= cu_count();
     a.status = status;
     const int64_t slots = ws_slots(B, Hq, t_cap);
