@@ -863,16 +863,16 @@ __global__ __launch_bounds__(kAThreads, 4) void q8_partial_kernel(Q8Args a) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[n][i] *= cr[i];
         }
-        // weights times 2^15 (sums as well); the second term of a weight below
-        // 2^-18 of the largest is a subnormal fp16, 2^-40 of the largest off at most
+        // the second term of a weight below 2^-18 of the largest is a subnormal
+        // fp16, 2^-40 of the largest off at most
         float ps = 0.f;
         uint32_t w2[4];
-        const float m15 = m_run - 15.f;
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
-            const f32x2 f = {__builtin_amdgcn_exp2f(x[e] - m15), __builtin_amdgcn_exp2f(x[e + 1] - m15)};
-            ps += f[0];
-            ps += f[1];
+            const f32x2 p = {__builtin_amdgcn_exp2f(x[e] - m_run), __builtin_amdgcn_exp2f(x[e + 1] - m_run)};
+            ps += p[0];
+            ps += p[1];
+            const f32x2 f = {p[0] * 0x1p15f, p[1] * 0x1p15f};
             const f16x2 hi = __builtin_convertvector(f, f16x2);
             const f32x2 r = {f[0] - (float)hi[0], f[1] - (float)hi[1]};
             const f16x2 lo = __builtin_convertvector(r, f16x2);
@@ -883,7 +883,7 @@ __global__ __launch_bounds__(kAThreads, 4) void q8_partial_kernel(Q8Args a) {
         if constexpr (TRACK) {
             float bs = ps + xor_lane<16>(ps, lane);
             bs += xor_lane<32>(bs, lane);
-            if (lane < G) a.lse[(((int64_t)b * a.Hkv + h) * nb_cap + blk) * G + lane] = log2f(bs) + m15;
+            if (lane < G) a.lse[(((int64_t)b * a.Hkv + h) * nb_cap + blk) * G + lane] = log2f(bs) + m_run;
         }
 
         // ---- weighted values
@@ -921,7 +921,7 @@ __global__ __launch_bounds__(kAThreads, 4) void q8_partial_kernel(Q8Args a) {
         }
     if (lane < kGP) {
         wm[wave][lane] = m_run;
-        wl[wave][lane] = bad_q ? NAN : l_run * 0x1p-15f;
+        wl[wave][lane] = bad_q ? NAN : l_run;
     }
     __syncthreads();
     for (int i = tid; i < G * kD; i += kAThreads) {

@@ -248,6 +248,30 @@ def test_attention_sizes_of_scores(dq, fmt, spread):
 
 
 @pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("bits", range(10, 40, 3))
+def test_attention_any_size_of_the_largest_score(dq, fmt, bits):
+    """Scores about 2^bits whose largest grows from block to block, also where
+    fp32 holds no differences of a few units any more."""
+    T = 256
+    k, v = _kv(19, 1, T, 1)
+    k = (k.sign() * (1 + torch.arange(T).view(1, T, 1, 1) / T)).to(torch.bfloat16)
+    k[..., 1:] = 0
+    q = torch.zeros((1, 2, 128), dtype=torch.bfloat16)
+    q[0, 0, 0], q[0, 1, 0] = 2.0 ** bits, -(2.0 ** bits)
+    cache = dq.Q8KVCache(1, 1, 2, T, fmt)
+    cache.append(k.to(DEV), v.to(DEV), 0)
+    out = cache.attend(q.to(DEV), torch.tensor([T], dtype=torch.int32, device=DEV), softmax_scale=1.0)
+    kf, vf = _held(k, fmt), _held(v, fmt)
+    ref, _ = q8.attention(q.double().numpy(), kf, vf, [T], 2, 1.0)
+    # one product and four roundings: a score of at most 2^(bits + 1.6) in base 2
+    # is off by 2^(bits - 20), and so is a weight; from 2^16 on the keys with the
+    # largest code (equal scores, exactly) share all the weight, since the next
+    # code's score lies 2^(bits - 6) below
+    tol = (2.0 ** (bits - 19) if bits < 16 else 0.0) + 1e-5
+    assert np.max(np.abs(out[0].double().cpu().numpy() - ref[0])) <= tol * np.abs(vf).max()
+
+
+@pytest.mark.parametrize("fmt", FMTS)
 def test_rows_behind_the_length_do_not_matter(dq, fmt):
     """Codes of no number, infinite and NaN scales behind the length; bit for bit."""
     for window, sinks in ((0, 0), (70, 40)):
