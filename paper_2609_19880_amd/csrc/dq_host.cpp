@@ -15,6 +15,7 @@
 #include <vector>
 
 #include "dq_internal.h"
+#include "dq_q8.h"
 
 namespace {
 

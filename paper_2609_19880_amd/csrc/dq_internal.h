@@ -214,36 +214,6 @@ int launch_residual_commit(int32_t* seq_lens, int32_t* res_lens, int32_t B, int3
 int launch_bf16_partial(const uint16_t* q, int32_t B, int32_t Hq, int32_t Hkv, const uint16_t* k,
                         const uint16_t* v, const int32_t* seq_lens, int32_t t_cap, float scale, void* ws,
                         hipStream_t stream);
-
-// The 8-bit cache: keys [0] and values [1].
-struct Q8Cache {
-    uint8_t* data[2];
-    float* scale[2];
-};
-// bf16 rows [B][T][H][128] at element strides.
-struct Q8Rows {
-    const uint16_t* p;
-    int64_t sb, st, sh;
-};
-int launch_q8_encode(int format, const Pages& pg, const Q8Rows& k, const Q8Rows& v, int32_t B, int32_t H, int32_t t0,
-                     int32_t n_new, int32_t t_cap, const Q8Cache& to, uint32_t* status, hipStream_t stream);
-int launch_q8_read(int format, const Pages& pg, const Q8Cache& from, int32_t B, int32_t H, int32_t t0, int32_t n,
-                   int32_t t_cap, const Q8Rows& k, const Q8Rows& v, uint32_t* status, hipStream_t stream);
-// out: the step's result where one chunk holds the whole of every sequence
-// (*done then, scores included); else the partials alone are written.
-int launch_q8_partial(int format, const Pages& pg, const uint16_t* q, int32_t B, int32_t Hq, int32_t Hkv,
-                      const Q8Cache& c, const int32_t* seq_lens, const int32_t* extra_lens, int32_t t_cap,
-                      int32_t window, int32_t sinks, float scale, float* lse, float* out, float* scores, void* ws,
-                      uint32_t* status, hipStream_t stream, bool* done);
-// The merge (out, may be NULL) and the blocks' weights (scores, may be NULL).
-int launch_q8_finish(int32_t B, int32_t Hq, int32_t Hkv, const int32_t* seq_lens, const int32_t* extra_lens,
-                     int32_t t_cap, int32_t window, int32_t sinks, const float* lse, const void* ws, float* out,
-                     float* scores, hipStream_t stream);
-// keep, first and last in tokens, multiples of 32
-int launch_q8_evict(const Pages& pg, int32_t B, int32_t H, const int32_t* seq_lens, int32_t* new_lens, int32_t t_cap,
-                    int32_t to_cap, int32_t keep, int32_t first, int32_t last, const float* scores,
-                    float* to_scores, const Q8Cache& from, const Q8Cache& to, int32_t* kept, uint32_t* status,
-                    hipStream_t stream);
 int launch_attention_merge(int32_t B, int32_t Hq, int32_t Hkv, const int32_t* seq_lens,
                            int32_t t_cap, const void* ws, float* out, hipStream_t stream,
                            int64_t ws_slots_used = 0);

@@ -25,6 +25,7 @@
 #include <type_traits>
 
 #include "dq_common.h"
+#include "dq_q8.h"
 
 namespace dq {
 namespace {
