@@ -504,9 +504,9 @@ int dq_q8_decode_kv_paged(int32_t format, const uint8_t* k_pool, const float* k_
  *   block_lse: fp32 [batch][kv_heads][t_cap / 32][q_heads / kv_heads] or NULL:
  *       receives the base-2 logarithm of each visible block's sum of
  *       exponentials, for dq_q8_add_scores.  Other entries are left alone.
- *   workspace: dq_decode_workspace_bytes(...) bytes
+ *   workspace: dq_decode_workspace_bytes(...) bytes, 16-byte aligned
  * A sequence with no visible token gives zeros; a query head with an infinity
- * or NaN gives NaN.
+ * or NaN gives NaN, in its KV head's scores too.
  * dq_q8_decode_attention_partial writes split-K partials into the workspace;
  * finish it with dq_decode_attention_merge, with dq_decode_attention_residual
  * and dq_decode_attention_merge, or with dq_decode_attention_merge_residual.
@@ -521,7 +521,9 @@ int dq_q8_decode_kv_paged(int32_t format, const uint8_t* k_pool, const float* k_
  * by the attention weight of block j in the step whose partials (of the cached
  * tokens and, if dq_decode_attention_residual ran, of the raw ones) are in the
  * workspace, summed over its tokens and the query heads of KV head h.  The
- * arguments are those of the step.
+ * arguments are those of the step.  The step has to be one of the _partial
+ * calls: dq_q8_decode_attention, which may finish without the workspace, adds
+ * to the scores by itself.
  */
 int dq_q8_decode_attention_partial(int32_t format, const uint16_t* q, int32_t batch, int32_t q_heads,
                                    int32_t kv_heads, const uint8_t* k_data, const float* k_scale,
@@ -570,9 +572,9 @@ int dq_q8_add_scores(int32_t batch, int32_t q_heads, int32_t kv_heads, const int
  *   to_*: the cache that receives the kept blocks: either the same arrays (in
  *       place; to_cap = t_cap) or others, of to_cap tokens, that do not overlap
  *       them.  Scores behind the kept ones, up to the old block count, become 0.
- * In pool pages the eviction is in place; pages behind the new length are free
- * for the caller.  An entry outside the pool sets DQ_STATUS_PAGE and nothing
- * is written through it.
+ * In pool pages the eviction is in place, so none of the pages may belong to
+ * two sequences; pages behind the new length are free for the caller.  An entry
+ * outside the pool sets DQ_STATUS_PAGE and nothing is written through it.
  * Returns DQ_OK, DQ_ERR_INVALID_ARG or DQ_ERR_HIP.
  */
 int dq_q8_evict(int32_t batch, int32_t kv_heads, const int32_t* seq_lens, int32_t* new_lens, int32_t t_cap,

@@ -740,6 +740,7 @@ def _q8_lens(t, batch, dev, name="seq_lens"):
 
 
 def _q8_encode(fmt: int, cache, k, v, t0, status, stream):
+    _need(cache is not None, "the cache must be on one GPU")
     B, H, nb, dev, at = cache
     n, T = _q8_rows_args(k, v, H, dev)
     _need(n == B, "k and the cache must have the same batch")
@@ -776,11 +777,20 @@ def _q8_out_rows(k, v, batch, n, heads, dev):
           "k and v must be [B, n, H, 128], both or neither")
 
 
+def _q8_new_rows(batch, n, heads, dev, stream):
+    # (memory of the stream that fills it)
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return _q8_new_rows(batch, n, heads, dev, None)
+    return torch.empty((2, batch, n, heads, 128), dtype=torch.bfloat16, device=dev).unbind()
+
+
 def _q8_read(fmt: int, cache, t0, n, k, v, stream):
+    _need(cache is not None, "the cache must be on one GPU")
     B, H, nb, dev, at = cache
     _need(0 <= t0 <= _INT_MAX and 0 <= n <= _INT_MAX, "t0 and n")
     if k is None and v is None:
-        k, v = torch.empty((2, B, n, H, 128), dtype=torch.bfloat16, device=dev).unbind()
+        k, v = _q8_new_rows(B, n, H, dev, stream)
         sb, st = n * H * 128, H * 128
         ks = vs = (sb, st, 128)
     else:
@@ -807,7 +817,7 @@ def dq_q8_decode_kv_paged(fmt, k_pool, k_scale_pool, v_pool, v_scale_pool, block
     max_pages = _q8_table(block_table, B, dev)
     _need(0 <= t0 <= _INT_MAX and 0 <= n <= _INT_MAX, "t0 and n")
     if k is None and v is None:
-        k, v = torch.empty((2, B, n, H, 128), dtype=torch.bfloat16, device=dev).unbind()
+        k, v = _q8_new_rows(B, n, H, dev, stream)
     _q8_out_rows(k, v, B, n, H, dev)
     rc = _lib.dq_q8_decode_kv_paged(f, *at, B, H, t0, n, block_table.data_ptr(), max_pages, bpp * DQ_Q8_BLOCK,
                                     num_pages, k.data_ptr(), *k.stride()[:3], v.data_ptr(), *v.stride()[:3],
@@ -854,6 +864,7 @@ def _q8_sees(window, sinks):
 
 
 def _q8_partial(fmt: int, cache, q, seq_lens, workspace, window, sinks, extra_lens, softmax_scale, block_lse, stream):
+    _need(cache is not None, "the cache must be on one GPU")
     B, H, nb, dev, at = cache
     n, Hq = _q8_query(q, H, dev)
     _need(n == B, "q and the cache must have the same batch")
@@ -876,6 +887,7 @@ def dq_q8_decode_attention_partial(fmt, q, k_data, k_scale, v_data, v_scale, seq
 
 def _q8_attention(fmt: int, cache, q, seq_lens, out, workspace, window, sinks, softmax_scale, block_lse, scores,
                   stream):
+    _need(cache is not None, "the cache must be on one GPU")
     B, H, nb, dev, at = cache
     if not (q.dtype == torch.bfloat16 and q.dim() == 3 and q.is_contiguous() and q.device == dev
             and seq_lens.dtype == torch.int32 and seq_lens.is_contiguous() and seq_lens.numel() == B
@@ -973,6 +985,7 @@ def _q8_kept(kept, keep, first, last, batch, heads, dev):
 
 
 def _q8_evict(seq_lens, new_lens, keep, first, last, source, scores, to, to_scores, kept, stream):
+    _need(source is not None and to is not None, "the cache must be on one GPU")
     B, H, nb, dev, at = source
     tB, tH, tnb, tdev, to_at = to
     _need(tB == B and tH == H and tdev == dev, "both caches must have the same batch, heads and GPU")

@@ -726,6 +726,7 @@ static int check_q8_step(int32_t B, int32_t Hq, int32_t Hkv, const int32_t* seq_
     if (t_cap <= 0 || t_cap % DQ_MEAN_WINDOW || !seq_lens) return DQ_ERR_INVALID_ARG;
     if (window < 0 || sinks < 0 || (window == 0 && sinks)) return DQ_ERR_INVALID_ARG;
     if (!ws || ws_bytes < dq::attention_workspace_bytes(B, Hq, Hkv, t_cap, 128)) return DQ_ERR_WORKSPACE;
+    if (reinterpret_cast<uintptr_t>(ws) & 15) return DQ_ERR_INVALID_ARG;   // scalar and float2 accesses
     return DQ_OK;
 }
 

@@ -1504,10 +1504,12 @@ Q8Plan q8_plan(int B, int Hkv, int t_cap, int window, int sinks, bool whole) {
         return p;
     }
     const int64_t most = std::min((nb + 3) / 4, std::max<int64_t>(32, (cus + pairs - 1) / pairs));
-    if (window == 0 && B <= 256 && B * nb < (1 << 30)) {
+    const int64_t target = std::max<int64_t>(1, cus / Hkv), items = std::min(6 * target + B, B * most);
+    // (a workgroup reads all lengths; a grid has under 2^32 work-items along x)
+    if (window == 0 && B <= 256 && B * nb < (1 << 30) && items * Hkv < (1 << 23)) {
         p.nchunks = (int)most;
-        p.target = (int)std::max<int64_t>(1, cus / Hkv);
-        p.items = (int)std::min<int64_t>(6 * p.target + B, B * most);
+        p.target = (int)target;
+        p.items = (int)items;
         return p;
     }
     int64_t chunk = nb, best = INT64_MAX;

@@ -230,6 +230,33 @@ def test_attention_long_split(dq, fmt):
 
 
 @pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("B,t_cap", [(70, 2048), (130, 1024), (300, 640)])
+def test_attention_many_sequences(dq, fmt, B, t_cap):
+    """More sequences than a wavefront has lanes, of unlike and of like lengths
+    (zero and one among them), in one call and as partials."""
+    H, G = 1, 2
+    k, v = _kv(19, 2, t_cap, H)
+    of = torch.arange(B) % 2
+    g = torch.Generator().manual_seed(B)
+    q = torch.randn((B, H * G, 128), generator=g).to(torch.bfloat16)
+    cache = dq.Q8KVCache(B, H, H * G, t_cap, fmt)
+    cache.append(k[of].to(DEV), v[of].to(DEV), 0)
+    qf, kf, vf = q.double().numpy(), _held(k, fmt)[of.numpy()], _held(v, fmt)[of.numpy()]
+    unlike = torch.where(torch.rand(B, generator=g) < 0.8, torch.randint(0, 90, (B,), generator=g), t_cap - 3)
+    unlike[:3] = torch.tensor([0, 1, t_cap])
+    for lens in (unlike.tolist(), [t_cap - b % 5 for b in range(B)], [0] * B):
+        seq = torch.tensor(lens, dtype=torch.int32, device=DEV)
+        ref, _ = q8.attention(qf, kf, vf, lens, G, 128 ** -0.5, 0, 0)
+        out = torch.full((B, H * G, 128), math.nan, device=DEV)
+        cache.attend(q.to(DEV), seq, out=out)
+        _check_out(out, ref, qf, kf, lens, G, 128 ** -0.5)
+        out.fill_(math.nan)
+        cache.partial(q.to(DEV), seq)
+        cache.merge(seq, out)
+        _check_out(out, ref, qf, kf, lens, G, 128 ** -0.5)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("spread", [1e-20, 1e15])
 def test_attention_sizes_of_scores(dq, fmt, spread):
     """Keys and values of any size: finite, and (where the scores are small) right."""
@@ -425,6 +452,21 @@ def test_scores(dq, fmt, G, window, sinks):
     assert torch.equal(cache.scores, first + first)
 
 
+@pytest.mark.parametrize("window,sinks", [(0, 0), (7000, 64)])
+def test_scores_of_partials(dq, window, sinks):
+    """More partials than a wavefront has lanes; the weights of a step's partials
+    by a call of their own."""
+    cache, seq, q, _, weight = _attend_case(dq, "int8", [16300], 4, H=1, t_cap=16384, window=window, sinks=sinks,
+                                            scores=True)
+    # as in test_scores
+    assert np.max(np.abs(cache.scores.double().cpu().numpy() - weight)) <= 4 * 3e-5
+    cache.scores.zero_()
+    cache.partial(q, seq, window=window, sinks=sinks)
+    cache.add_scores(seq, window, sinks)
+    assert np.max(np.abs(cache.scores.double().cpu().numpy() - weight)) <= 4 * 3e-5
+    assert np.isclose(float(cache.scores.sum(dtype=torch.float64)), 4, rtol=3e-5)
+
+
 def _fill(dq, fmt, B, H, t_cap, lens, seed, levels=None):
     k, v = _kv(seed, B, t_cap, H)
     cache = dq.Q8KVCache(B, H, 4 * H, t_cap, fmt, scores=True)
@@ -489,6 +531,26 @@ def test_evict_nan_scores_and_many_blocks(dq):
         want = q8.evict(old_scores[b, h].cpu().numpy(), 2048, 1875, 1, 2)
         assert kept[b, h].tolist() == want
         assert torch.equal(cache.k_data[b, h, :1875], old[0][b, h][torch.tensor(want, device=DEV)])
+
+
+@pytest.mark.parametrize("into", [False, True])
+@pytest.mark.parametrize("blocks", [260, 500, 4100, 9400, 17000])
+def test_evict_numbers_of_blocks(dq, blocks, into):
+    """Every kind of selection, up to several rounds; ties among them; bytes as they are."""
+    B, H, t_cap = 2, 1, blocks * 32
+    g = torch.Generator().manual_seed(blocks)
+    cache = dq.Q8KVCache(B, H, H, t_cap, scores=True)
+    for x in cache.arrays:
+        x.copy_(torch.randint(0, 255, x.shape, generator=g, dtype=torch.int32))
+    cache.scores.copy_((torch.rand(cache.scores.shape, generator=g) * 50).floor() / 50 - 0.5)
+    lens = [t_cap, t_cap - 65]
+    seq = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    keep = blocks * 2 // 3 // 4 * 128
+    to = dq.Q8KVCache(B, H, H, keep, scores=True) if into else cache
+    old, old_scores = [x.clone() for x in cache.arrays], cache.scores.clone()
+    kept, new_lens = cache.evict(seq, keep, 70, 130, into=to if into else None)
+    torch.cuda.synchronize()
+    _check_evict(old, old_scores, lens, to, kept, new_lens, keep, 96, 160)
 
 
 @pytest.mark.parametrize("page", [128, 512])
@@ -670,3 +732,40 @@ def test_two_streams(dq):
         torch.cuda.synchronize()
         for (_, _, _, out, _), got in zip(cases, outs):
             assert all(torch.equal(x, out) for x in got)
+
+
+def test_graph_of_an_eviction_in_place(dq):
+    """A captured eviction in place, lengths included, replayed on new contents."""
+    cache, seq = _fill(dq, "e4m3", 2, 2, 1024, [1024, 300], 71)
+    arrays = [x.clone() for x in cache.arrays]
+    kept = torch.empty((2, 2, 8), dtype=torch.int32, device=DEV)
+
+    def cut():
+        own = (*cache.arrays, cache.scores)
+        dq.dq_q8_evict(seq, seq, 256, 64, 32, own, own, kept)
+
+    cut()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        cut()
+    for i in range(3):
+        for x, y in zip(arrays, cache.arrays):
+            y.copy_(x)
+        cache.scores.copy_(torch.rand(cache.scores.shape, generator=torch.Generator().manual_seed(80 + i)))
+        lens = [[1024, 0], [999, 256], [257, 1000]][i]
+        seq.copy_(torch.tensor(lens, dtype=torch.int32))
+        before = cache.scores.clone()
+        g.replay()
+        torch.cuda.synchronize()
+        _check_evict(arrays, before, lens, cache, kept, seq, 256, 64, 32)
+
+
+def test_read_on_another_stream(dq):
+    cache, _ = _fill(dq, "int8", 1, 2, 1024, [1024], 73)
+    want = cache.read(32, 900)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = dq.dq_q8_decode_kv("int8", *cache.arrays, 32, 900, stream=side)
+    side.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(got, want))

@@ -149,3 +149,19 @@ def test_cache_on_the_host_keeps_shapes():
     with pytest.raises(ValueError):
         dq.Q8KVCache(2, 2, 8, 256, device="cpu").evict(lens, 128)
     assert ctypes.sizeof(ctypes.c_float) == 4
+
+
+def test_workspace_alignment():
+    assert C.dq_q8_decode_attention_partial(*_swap(STEP, dict(ws=P + 8))) == INVALID
+    assert C.dq_q8_add_scores(2, 32, 8, P, None, 256, 0, 0, P, P + 4, 1 << 40, P, None) == INVALID
+
+
+def test_cache_off_the_gpu_is_refused():
+    c = dq.Q8KVCache(1, 2, 4, 256, scores=True, device="cpu")
+    lens = torch.zeros(1, dtype=torch.int32)
+    rows = torch.zeros((1, 32, 2, 128), dtype=torch.bfloat16)
+    q = torch.zeros((1, 4, 128), dtype=torch.bfloat16)
+    for call in (lambda: c.append(rows, rows, 0), lambda: c.read(0, 32), lambda: c.attend(q, lens),
+                 lambda: c.partial(q, lens), lambda: c.evict(lens, 128)):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
