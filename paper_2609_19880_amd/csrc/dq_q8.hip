@@ -508,7 +508,8 @@ typedef const __attribute__((address_space(1))) uint8_t* GlobalBytes;
 
 // Nontemporal: a step reads every block once, and lines that do not settle in
 // L2 stream at 6.7 TB/s where they reached 5.8 (16 x 32768 tokens: 159 us
-// against 184; one sequence of 4096, which would fit: no difference).
+// against 189; one sequence of 32768 16.7 against 19.8, one of 4096, which
+// would fit: no difference).
 __device__ __forceinline__ uint4 load16(GlobalBytes p) {
     const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const __attribute__((address_space(1))) u32x4*>(p));
     return uint4{v[0], v[1], v[2], v[3]};
@@ -1484,15 +1485,16 @@ struct Q8Plan {
 };
 
 // One chunk per sequence where it is short (up to 16 blocks: 8 KV heads of one
-// sequence of 512 tokens take 7.5 us in one launch, 7.9 in two) or where the
+// sequence of 512 tokens take 7.6 us in one launch, 7.9 in two) or where the
 // (sequence, KV head) pairs fill the CUs by themselves (half of them: up to 64
-// blocks, 32 sequences of 2048 tokens 22 against 28 us; twice: up to 128, 128
-// of 4096 158 against 173 us; beyond, unlike lengths would leave CUs idle).
+// blocks, 32 sequences of 2048 tokens 22 against 27 us; twice: up to 128, 128
+// of 4096 159 against 170 us; beyond, unlike lengths would leave CUs idle).
 // Else the kernel or, behind a window, the loop below picks the chunk length
 // for which the busiest CU has the least to do (3 sequences of 32768 tokens:
-// 36 us; two workgroups per CU at any length 40, one 46).  At most 32 chunks
-// per sequence (one of 32768 tokens: 19.5 us against 21.8 with 64, before the
-// loads became nontemporal) unless that leaves CUs without work.
+// 35 us; two workgroups per CU at any length 40, one 46).  At most 32 chunks
+// per sequence (64 make no difference to one of 32768 tokens, 16.7 us, and cost
+// a long one among fifteen short ones 2 of 60) unless that leaves CUs without
+// work.
 Q8Plan q8_plan(int B, int Hkv, int t_cap, int window, int sinks, bool whole) {
     const int64_t nb = seen_blocks(t_cap, window, sinks);
     const int64_t pairs = (int64_t)B * Hkv, cus = cu_count();
