@@ -757,11 +757,11 @@ static int q8_attention(int32_t format, const dq::Pages& pg, const uint16_t* q, 
     if (int rc = check_q8_query(format, q, c, scale)) return rc;
     if (int rc = check_q8_step(B, Hq, Hkv, seq_lens, t_cap, window, sinks, ws, ws_bytes)) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    bool done = false;
+    int slots = 0;
     const int rc = dq::launch_q8_partial(format, pg, q, B, Hq, Hkv, c, seq_lens, nullptr, t_cap, window, sinks, scale,
-                                         lse, out, scores, ws, status, s, &done);
-    if (rc != DQ_OK || done) return rc;
-    return dq::launch_q8_finish(B, Hq, Hkv, seq_lens, nullptr, t_cap, window, sinks, lse, ws, out, scores, s);
+                                         lse, out, scores, ws, status, s, &slots);
+    if (rc != DQ_OK || slots == 0) return rc;
+    return dq::launch_q8_finish(B, Hq, Hkv, seq_lens, nullptr, t_cap, window, sinks, lse, ws, out, scores, slots, s);
 }
 
 int dq_q8_decode_attention_partial(int32_t format, const uint16_t* q, int32_t B, int32_t Hq, int32_t Hkv,
@@ -813,7 +813,7 @@ int dq_q8_add_scores(int32_t B, int32_t Hq, int32_t Hkv, const int32_t* seq_lens
                      size_t ws_bytes, float* scores, void* stream) {
     if (!block_lse || !scores) return DQ_ERR_INVALID_ARG;
     if (int rc = check_q8_step(B, Hq, Hkv, seq_lens, t_cap, window, sinks, ws, ws_bytes)) return rc;
-    return dq::launch_q8_finish(B, Hq, Hkv, seq_lens, extra_lens, t_cap, window, sinks, block_lse, ws, nullptr, scores,
+    return dq::launch_q8_finish(B, Hq, Hkv, seq_lens, extra_lens, t_cap, window, sinks, block_lse, ws, nullptr, scores, 0,
                                 static_cast<hipStream_t>(stream));
 }
 

@@ -1080,6 +1080,17 @@ __global__ __launch_bounds__(kWave) void q8_finish_kernel(FinishArgs a) {
     const Visible vis = visible(T, extra, a.window, a.sinks);
     const int first = ((int)blockIdx.x - a.heads) * kScoreBlocks;
     if (first >= vis.count) return;
+    // the blocks' terms are requested beside the partials' maxima and sums
+    float term[kScoreBlocks / kWave][kGP], score[kScoreBlocks / kWave];
+    int64_t at[kScoreBlocks / kWave];
+#pragma unroll
+    for (int r = 0; r < kScoreBlocks / kWave; ++r) {
+        const int v = min(first + r * kWave + lane, vis.count - 1);
+        at[r] = ((int64_t)b * a.Hkv + h) * (a.t_cap / kBlk) + (v < vis.head ? v : vis.from + v - vis.head);
+        score[r] = a.scores[at[r]];
+#pragma unroll
+        for (int g = 0; g < kGP; ++g) term[r][g] = a.lse[at[r] * G + min(g, G - 1)];
+    }
     float m[kGP], l[kGP], total[kGP];
 #pragma unroll
     for (int g = 0; g < kGP; ++g) {
@@ -1103,14 +1114,13 @@ __global__ __launch_bounds__(kWave) void q8_finish_kernel(FinishArgs a) {
             }
         }
     }
-    for (int v = first + lane; v < min(first + kScoreBlocks, vis.count); v += kWave) {
-        const int blk = v < vis.head ? v : vis.from + v - vis.head;
-        const int64_t i = ((int64_t)b * a.Hkv + h) * (a.t_cap / kBlk) + blk;
+#pragma unroll
+    for (int r = 0; r < kScoreBlocks / kWave; ++r) {
         float w = 0.f;
 #pragma unroll
         for (int g = 0; g < kGP; ++g)
-            if (g < G) w += exp2f(a.lse[i * G + g] - total[g]);
-        a.scores[i] += w;
+            if (g < G) w += exp2f(term[r][g] - total[g]);
+        if (first + r * kWave + lane < vis.count) a.scores[at[r]] = score[r] + w;
     }
 }
 
@@ -1495,9 +1505,9 @@ struct Q8Plan {
 // per sequence (64 make no difference to one of 32768 tokens, 16.7 us, and cost
 // a long one among fifteen short ones 2 of 60) unless that leaves CUs without
 // work.
-Q8Plan q8_plan(int B, int Hkv, int t_cap, int window, int sinks, bool whole) {
+Q8Plan q8_plan(int64_t cus, int B, int Hkv, int t_cap, int window, int sinks, bool whole) {
     const int64_t nb = seen_blocks(t_cap, window, sinks);
-    const int64_t pairs = (int64_t)B * Hkv, cus = cu_count();
+    const int64_t pairs = (int64_t)B * Hkv;
     Q8Plan p{};
     if (whole && (nb <= 16 || (2 * pairs >= cus && nb <= 64) || (pairs >= 2 * cus && nb <= 128))) {
         p.chunk = (int)nb;
@@ -1514,10 +1524,13 @@ Q8Plan q8_plan(int B, int Hkv, int t_cap, int window, int sinks, bool whole) {
         p.items = (int)items;
         return p;
     }
-    int64_t chunk = nb, best = INT64_MAX;
-    for (int64_t n = 1; n <= std::min<int64_t>(most, 64); ++n) {
-        const int64_t c = ((nb + n - 1) / n + 3) / 4 * 4;
-        const int64_t cost = ((nb + c - 1) / c * pairs + cus - 1) / cus * (c + kChunkCost);
+    // (every call of a windowed step comes here: no 64-bit divisions)
+    const uint32_t blocks = (uint32_t)nb;
+    uint32_t chunk = blocks;
+    double best = INFINITY;
+    for (uint32_t n = 1; n <= (uint32_t)std::min<int64_t>(most, 64); ++n) {
+        const uint32_t c = ((blocks + n - 1) / n + 3) & ~3u, used = (blocks + c - 1) / c;
+        const double cost = std::ceil((double)(used * pairs) / (double)cus) * (double)(c + kChunkCost);
         if (cost < best) {
             best = cost;
             chunk = c;
@@ -1541,10 +1554,11 @@ void launch_q8_format(const Q8Args& a, dim3 grid, hipStream_t stream) {
 int launch_q8_partial(int format, const Pages& pg, const uint16_t* q, int32_t B, int32_t Hq, int32_t Hkv,
                       const Q8Cache& c, const int32_t* seq_lens, const int32_t* extra_lens, int32_t t_cap,
                       int32_t window, int32_t sinks, float scale, float* lse, float* out, float* scores, void* ws,
-                      uint32_t* status, hipStream_t stream, bool* done) {
-    const Q8Plan plan = q8_plan(B, Hkv, t_cap, window, sinks, out != nullptr);
+                      uint32_t* status, hipStream_t stream, int* slots) {
+    const int cus = cu_count();
+    const Q8Plan plan = q8_plan(cus, B, Hkv, t_cap, window, sinks, out != nullptr);
     const bool whole = plan.whole;
-    if (done) *done = whole;
+    if (slots) *slots = whole ? 0 : plan.nchunks;
     Q8Args a;
     a.q = q;
     a.k = c.data[0];
@@ -1569,14 +1583,14 @@ int launch_q8_partial(int format, const Pages& pg, const uint16_t* q, int32_t B,
     a.B = B;
     a.target = plan.target;
     a.items = plan.items;
-    a.per_cu = 0.99999f / (float)cu_count();
-    a.early = whole && window == 0 && !pg.bt && (int64_t)Hkv * B <= cu_count();
+    a.per_cu = 0.99999f / (float)cus;
+    a.early = whole && window == 0 && !pg.bt && (int64_t)Hkv * B <= cus;
     a.status = status;
-    const int64_t slots = ws_slots(B, Hq, t_cap);
+    const int64_t held = ws_slots(B, Hq, t_cap);
     a.ws_hdr = static_cast<int32_t*>(ws);
     a.ws_acc = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + kWsHeader);
-    a.ws_m = a.ws_acc + slots * kD;
-    a.ws_l = a.ws_m + slots;
+    a.ws_m = a.ws_acc + held * kD;
+    a.ws_l = a.ws_m + held;
     const dim3 grid = plan.target ? dim3((unsigned)plan.items * Hkv) : dim3(plan.nchunks, Hkv, B);
     if (format == DQ_Q8_E4M3)
         launch_q8_format<DQ_Q8_E4M3>(a, grid, stream);
@@ -1587,16 +1601,16 @@ int launch_q8_partial(int format, const Pages& pg, const uint16_t* q, int32_t B,
 
 int launch_q8_finish(int32_t B, int32_t Hq, int32_t Hkv, const int32_t* seq_lens, const int32_t* extra_lens,
                      int32_t t_cap, int32_t window, int32_t sinks, const float* lse, const void* ws, float* out,
-                     float* scores, hipStream_t stream) {
-    const int64_t slots = ws_slots(B, Hq, t_cap);
+                     float* scores, int slots, hipStream_t stream) {
+    const int64_t held = ws_slots(B, Hq, t_cap);
     FinishArgs a;
     a.seq_lens = seq_lens;
     a.extra_lens = extra_lens;
     a.lse = lse;
     a.ws_hdr = static_cast<const int32_t*>(ws);
     a.ws_acc = reinterpret_cast<const float*>(static_cast<const uint8_t*>(ws) + kWsHeader);
-    a.ws_m = a.ws_acc + slots * kD;
-    a.ws_l = a.ws_m + slots;
+    a.ws_m = a.ws_acc + held * kD;
+    a.ws_l = a.ws_m + held;
     a.out = out;
     a.scores = scores;
     a.Hq = Hq;
@@ -1605,9 +1619,8 @@ int launch_q8_finish(int32_t B, int32_t Hq, int32_t Hkv, const int32_t* seq_lens
     a.t_cap = t_cap;
     a.window = window;
     a.sinks = sinks;
-    a.nc_max = (int)(slots / ((int64_t)B * Hq)) - kResSlots;
-    // (the partials of the one-call form: the plan is known here)
-    a.nc = out ? q8_plan(B, Hkv, t_cap, window, sinks, true).nchunks : 0;
+    a.nc_max = (int)max_chunks(t_cap);
+    a.nc = slots;
     a.heads = out ? a.G : 0;
     const int64_t parts = scores ? (seen_blocks(t_cap, window, sinks) + kScoreBlocks - 1) / kScoreBlocks : 0;
     q8_finish_kernel<<<dim3((unsigned)(a.heads + parts), Hkv, B), kWave, 0, stream>>>(a);
