@@ -1002,17 +1002,29 @@ struct FinishArgs {
     int heads;                   // workgroups per KV head that merge: G or 0
 };
 
-constexpr int kScoreBlocks = 128;            // blocks per workgroup of the scores
-constexpr int kFinishFirst = 8;              // partials requested at once
+constexpr int kScoreBlocks = 128;            // blocks per wavefront of the scores
+constexpr int kFinishFirst = 8;              // partials per wavefront requested at once
 constexpr int kFinishBatch = 16;             // partials per further memory round trip
+// Up to so many merges have four wavefronts each, others one (four: 8 KV heads of
+// one sequence of 4096 tokens 9.0 us the step against 10.7, one KV head of 120000
+// tokens, whose partials are over two hundred, 16 against 39; one: 32 heads of 48
+// sequences of up to 8192 tokens 94 against 99 us, most of whose requests find no
+// partial).
+constexpr int kFewMerges = 128;
+constexpr int kMostChunks = 4 * kWave;       // (one wavefront has at most 32: many pairs)
 
-// One wavefront per workgroup.  The first G of a (KV head, sequence) merge one
-// query head each, lane l holding channels 2 l and 2 l + 1; the others add
-// block weights to the scores: sum_g 2^(lse of the block - lse of the step),
-// the latter from the partials' maxima and sums (as many partials as lanes or
-// fewer, in general).
-__global__ __launch_bounds__(kWave) void q8_finish_kernel(FinishArgs a) {
-    const int h = blockIdx.y, b = blockIdx.z, lane = threadIdx.x, G = a.G;
+// The first G workgroups of a (KV head, sequence) merge one query head each:
+// wavefront w of W takes the partials w, w + W, ..., lane l the maximum and sum
+// of the l-th of them and of all the channels 2 l and 2 l + 1; the wavefronts'
+// results meet in LDS.  The others' wavefronts add block weights to the
+// scores: sum_g 2^(lse of the block - lse of the step), the latter from the
+// partials' maxima and sums (as many partials as lanes or fewer, in general).
+template <int WAVES>
+__global__ __launch_bounds__(WAVES* kWave) void q8_finish_kernel(FinishArgs a) {
+    __shared__ float wm[WAVES], wl[WAVES];
+    __shared__ float2 wacc[WAVES][kWave];
+    const int h = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & (kWave - 1), G = a.G;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
     // (the stores of this kernel are to other memory than these loads)
     const int NC = a.nc ? a.nc : min(max(scalar_load(a.ws_hdr + 1), 1), a.nc_max);
     const int64_t base = ((int64_t)b * a.Hq + h * G) * (NC + kResSlots);
@@ -1020,65 +1032,78 @@ __global__ __launch_bounds__(kWave) void q8_finish_kernel(FinishArgs a) {
     float2 x[kFinishBatch];
     float m_lane = 0.f, l_lane = 0.f;
     const bool merge = (int)blockIdx.x < a.heads;
+    const int64_t s0 = base + (int64_t)blockIdx.x * (NC + kResSlots);
+    auto partial = [&](int u, int last) {
+        const int64_t slot = s0 + min(wave + WAVES * u, last);
+        return *(reinterpret_cast<const float2*>(a.ws_acc + slot * kD) + lane);
+    };
     if (merge) {
-        const int64_t s0 = base + (int64_t)blockIdx.x * (NC + kResSlots);
-        const int64_t s1 = s0 + min(lane, NC + kResSlots - 1);
+        const int64_t s1 = s0 + min(wave + WAVES * lane, NC - 1);
         m_lane = a.ws_m[s1];
         l_lane = a.ws_l[s1];
 #pragma unroll
-        for (int u = 0; u < kFinishFirst; ++u)
-            x[u] = *(reinterpret_cast<const float2*>(a.ws_acc + (s0 + min(u, NC - 1)) * kD) + lane);
+        for (int u = 0; u < kFinishFirst; ++u) x[u] = partial(u, NC - 1);
     }
     const int chunk = max(scalar_load(a.ws_hdr), 1);
     const int residual = a.nc ? 0 : min(max(scalar_load(a.ws_hdr + 2), 0), kResSlots);
     const int T = max(0, min(scalar_load(a.seq_lens + b), a.t_cap));
     const int nc = (int)min((int64_t)NC, ((int64_t)T + chunk - 1) / chunk), np = nc + residual;
-    auto slot_of = [&](int g, int i) { return base + (int64_t)g * (NC + kResSlots) + (i < nc ? i : NC + i - nc); };
     if (merge) {
-        // the merge runs where no residual window does: partials 0 .. nc - 1
-        const int g = blockIdx.x;
-        float2* dst = reinterpret_cast<float2*>(a.out + ((int64_t)b * a.Hq + h * G + g) * kD) + lane;
-        if (lane >= nc) m_lane = -INFINITY;
-        float M = m_lane;
-        for (int i = lane + kWave; i < nc; i += kWave) M = fmaxf(M, a.ws_m[slot_of(g, i)]);
-        M = wave_max(M);
-        if (M == -INFINITY) {
-            *dst = float2{0.f, 0.f};
-            return;
-        }
-        const float e_lane = lane < nc ? exp2f(m_lane - M) : 0.f;
-        float l = wave_sum(lane < nc ? l_lane * e_lane : 0.f);
+        // the merge runs where no residual window does: partials 0 .. nc - 1,
+        // at most kMostChunks
+        const int n = max(0, nc - wave + WAVES - 1) / WAVES;
+        if (lane >= n) m_lane = -INFINITY;
+        const float M = wave_max(m_lane);
+        // (a partial without weight, or none: 0, whatever its slot holds)
+        const float e_lane = m_lane == -INFINITY ? 0.f : exp2f(m_lane - M);
+        const float l = wave_sum(m_lane == -INFINITY ? 0.f : l_lane * e_lane);
         float2 acc = {0.f, 0.f};
-        auto add = [&](int i0, int n) {
+        auto add = [&](int u0, int most) {
 #pragma unroll
             for (int u = 0; u < kFinishBatch; ++u) {
-                const int i = i0 + u;
-                if (u < n && i < nc) {
-                    float e;
-                    if (i < kWave) {
-                        e = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(e_lane), i));
-                    } else {
-                        e = exp2f(a.ws_m[slot_of(g, i)] - M);
-                        l += a.ws_l[slot_of(g, i)] * e;
-                    }
+                if (u < most && u0 + u < n) {
+                    const float e = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(e_lane), u0 + u));
                     acc.x = fmaf(x[u].x, e, acc.x);
                     acc.y = fmaf(x[u].y, e, acc.y);
                 }
             }
         };
         add(0, kFinishFirst);
-        for (int i0 = kFinishFirst; i0 < nc; i0 += kFinishBatch) {
+        for (int u0 = kFinishFirst; u0 < n; u0 += kFinishBatch) {
 #pragma unroll
-            for (int u = 0; u < kFinishBatch; ++u)
-                x[u] = *(reinterpret_cast<const float2*>(a.ws_acc + slot_of(g, min(i0 + u, nc - 1)) * kD) + lane);
-            add(i0, kFinishBatch);
+            for (int u = 0; u < kFinishBatch; ++u) x[u] = partial(u0 + u, nc - 1);
+            add(u0, kFinishBatch);
         }
-        *dst = float2{acc.x / l, acc.y / l};
+        wacc[wave][lane] = acc;
+        if (lane == 0) {
+            wm[wave] = M;
+            wl[wave] = l;
+        }
+        __syncthreads();
+        if (wave > 0) return;
+        float top = wm[0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) top = fmaxf(top, wm[w]);
+        float2 out = {0.f, 0.f};
+        if (top != -INFINITY) {
+            float sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                const float e = exp2f(wm[w] - top);
+                sum = fmaf(wl[w], e, sum);
+                out.x = fmaf(wacc[w][lane].x, e, out.x);
+                out.y = fmaf(wacc[w][lane].y, e, out.y);
+            }
+            out.x /= sum;
+            out.y /= sum;
+        }
+        *(reinterpret_cast<float2*>(a.out + ((int64_t)b * a.Hq + h * G + (int)blockIdx.x) * kD) + lane) = out;
         return;
     }
+    auto slot_of = [&](int g, int i) { return base + (int64_t)g * (NC + kResSlots) + (i < nc ? i : NC + i - nc); };
     const int extra = a.extra_lens ? max(0, scalar_load(a.extra_lens + b)) : 0;
     const Visible vis = visible(T, extra, a.window, a.sinks);
-    const int first = ((int)blockIdx.x - a.heads) * kScoreBlocks;
+    const int first = (((int)blockIdx.x - a.heads) * WAVES + wave) * kScoreBlocks;
     if (first >= vis.count) return;
     // the blocks' terms are requested beside the partials' maxima and sums
     float term[kScoreBlocks / kWave][kGP], score[kScoreBlocks / kWave];
@@ -1515,7 +1540,8 @@ Q8Plan q8_plan(int64_t cus, int B, int Hkv, int t_cap, int window, int sinks, bo
         p.whole = true;
         return p;
     }
-    const int64_t most = std::min((nb + 3) / 4, std::max<int64_t>(32, (cus + pairs - 1) / pairs));
+    const int64_t most =
+        std::min({(nb + 3) / 4, std::max<int64_t>(32, (cus + pairs - 1) / pairs), (int64_t)kMostChunks});
     const int64_t target = std::max<int64_t>(1, cus / Hkv), items = std::min(6 * target + B, B * most);
     // (a workgroup reads all lengths; a grid has under 2^32 work-items along x)
     if (window == 0 && B <= 256 && B * nb < (1 << 30) && items * Hkv < (1 << 23)) {
@@ -1622,8 +1648,14 @@ int launch_q8_finish(int32_t B, int32_t Hq, int32_t Hkv, const int32_t* seq_lens
     a.nc_max = (int)max_chunks(t_cap);
     a.nc = slots;
     a.heads = out ? a.G : 0;
-    const int64_t parts = scores ? (seen_blocks(t_cap, window, sinks) + kScoreBlocks - 1) / kScoreBlocks : 0;
-    q8_finish_kernel<<<dim3((unsigned)(a.heads + parts), Hkv, B), kWave, 0, stream>>>(a);
+    const bool four = (int64_t)B * Hq <= kFewMerges;
+    const int each = kScoreBlocks * (four ? 4 : 1);
+    const int64_t parts = scores ? (seen_blocks(t_cap, window, sinks) + each - 1) / each : 0;
+    const dim3 grid((unsigned)(a.heads + parts), Hkv, B);
+    if (four)
+        q8_finish_kernel<4><<<grid, 4 * kWave, 0, stream>>>(a);
+    else
+        q8_finish_kernel<1><<<grid, kWave, 0, stream>>>(a);
     return hip_check("q8_finish launch", hipGetLastError());
 }
 
