@@ -1529,19 +1529,21 @@ struct Q8Plan {
 // 35 us; two workgroups per CU at any length 40, one 46).  At most 32 chunks
 // per sequence (64 make no difference to one of 32768 tokens, 16.7 us, and cost
 // a long one among fifteen short ones 2 of 60) unless that leaves CUs without
-// work.
-Q8Plan q8_plan(int64_t cus, int B, int Hkv, int t_cap, int window, int sinks, bool whole) {
+// work; at most 64 for the merges outside this file, which take as many in one
+// pass (one KV head of 120000 tokens, partials and merge: 21 us against 42 with
+// 235 chunks).
+Q8Plan q8_plan(int64_t cus, int B, int Hkv, int t_cap, int window, int sinks, bool one_call) {
     const int64_t nb = seen_blocks(t_cap, window, sinks);
     const int64_t pairs = (int64_t)B * Hkv;
     Q8Plan p{};
-    if (whole && (nb <= 16 || (2 * pairs >= cus && nb <= 64) || (pairs >= 2 * cus && nb <= 128))) {
+    if (one_call && (nb <= 16 || (2 * pairs >= cus && nb <= 64) || (pairs >= 2 * cus && nb <= 128))) {
         p.chunk = (int)nb;
         p.nchunks = 1;
         p.whole = true;
         return p;
     }
     const int64_t most =
-        std::min({(nb + 3) / 4, std::max<int64_t>(32, (cus + pairs - 1) / pairs), (int64_t)kMostChunks});
+        std::min({(nb + 3) / 4, std::max<int64_t>(32, (cus + pairs - 1) / pairs), (int64_t)(one_call ? kMostChunks : kWave)});
     const int64_t target = std::max<int64_t>(1, cus / Hkv), items = std::min(6 * target + B, B * most);
     // (a workgroup reads all lengths; a grid has under 2^32 work-items along x)
     if (window == 0 && B <= 256 && B * nb < (1 << 30) && items * Hkv < (1 << 23)) {
