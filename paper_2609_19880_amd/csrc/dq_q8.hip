@@ -1372,45 +1372,60 @@ __device__ __forceinline__ void new_length(const EvictArgs& a, int b) {
 }
 
 // In place the kept blocks' codes move to places at or before their old ones,
-// in order.  A wavefront owns 256 bytes of every block of one (KV head,
-// sequence) and tensor and walks through the list: it reads 4 kMoveU blocks'
-// pieces, waits for all of them and writes them.  What it writes to has been
-// read by itself before, so no wavefront waits for another.
-constexpr int kMoveU = 8;
+// in order.  A workgroup owns 256 bytes of every block of one (KV head,
+// sequence) and tensor and walks through the list, 32 blocks per wavefront and
+// round: all of a round's pieces are read before any is written, and what a later
+// round reads lies behind all that was written, so no workgroup waits for
+// another.  The list is read a round ahead, the blocks past L2 (131072 tokens to
+// half, selection included: 59 us; 102 with reads that settle in L2, 378 with one
+// wavefront per workgroup; into another cache 53).  512 bytes or whole rows per
+// workgroup leave CUs idle (one KV head 94 and 174 against 55 us).
+constexpr int kMoveU = 8;                    // pieces of 16 bytes per lane and round
+constexpr int kMoveBlocks = 4 * kMoveU;      // blocks per wavefront and round
 
-__global__ __launch_bounds__(kWave) void q8_move_kernel(EvictArgs a) {
+__global__ __launch_bounds__(1024) void q8_move_kernel(EvictArgs a) {
     const int slice = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
-    const int lane = threadIdx.x;
-    if (slice == 0 && h == 0 && lane == 0) new_length(a, b);
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    if (slice == 0 && h == 0 && threadIdx.x == 0) new_length(a, b);
     const int which = slice >> 4, off = (slice & 15) * 256 + (lane & 15) * 16;
     const int32_t* kept = a.kept + ((int64_t)b * a.H + h) * a.keep;
-    for (int i0 = 0; i0 < a.keep; i0 += 4 * kMoveU) {
+    const int round = (int)blockDim.x / kWave * kMoveBlocks;
+    const int mine = wave * kMoveBlocks + (lane >> 4);
+    int from[kMoveU];
+    auto list = [&](int i0) {
+#pragma unroll
+        for (int u = 0; u < kMoveU; ++u) from[u] = kept[min(i0 + mine + 4 * u, a.keep - 1)];
+    };
+    list(0);
+    for (int i0 = 0; i0 < a.keep; i0 += round) {
         if (kept[i0] < 0) break;      // the list ends
-        uint4 x[kMoveU];
-        uint4* to[kMoveU];
+        u32x4 x[kMoveU];
+        int64_t to[kMoveU];           // the piece's block, -1: nothing moves
+        int64_t at[kMoveU];
 #pragma unroll
         for (int u = 0; u < kMoveU; ++u) {
-            const int i = i0 + 4 * u + (lane >> 4);
-            to[u] = nullptr;
-            if (i < a.keep) {
-                const int from = kept[i];
-                if (from > i) {
-                    bool bad = false;
-                    const int64_t si = block_index(a.pg, a.H, a.nb_cap, b, h, from, bad);
-                    const int64_t di = block_index(a.pg, a.H, a.to_cap, b, h, i, bad);
-                    if (!bad) {
-                        x[u] = *reinterpret_cast<const uint4*>(a.data[which] + si * kBlkBytes + off);
-                        to[u] = reinterpret_cast<uint4*>(a.to_data[which] + di * kBlkBytes + off);
-                    }
-                }
+            const int i = i0 + mine + 4 * u;
+            to[u] = -1;
+            if (i < a.keep && from[u] > i) {
+                bool bad = false;
+                at[u] = block_index(a.pg, a.H, a.nb_cap, b, h, from[u], bad);
+                to[u] = block_index(a.pg, a.H, a.to_cap, b, h, i, bad);
+                if (bad) to[u] = -1;
             }
         }
+#pragma unroll
+        for (int u = 0; u < kMoveU; ++u)
+            if (to[u] >= 0)
+                x[u] = __builtin_nontemporal_load(
+                    reinterpret_cast<const u32x4*>(a.data[which] + at[u] * kBlkBytes + off));
+        if (i0 + round < a.keep) list(i0 + round);
         // every read of the round is back before the first write
         __builtin_amdgcn_s_waitcnt(0);
         __builtin_amdgcn_sched_barrier(0);
+        __syncthreads();
 #pragma unroll
         for (int u = 0; u < kMoveU; ++u)
-            if (to[u]) *to[u] = x[u];
+            if (to[u] >= 0) *reinterpret_cast<u32x4*>(a.to_data[which] + to[u] * kBlkBytes + off) = x[u];
     }
 }
 
@@ -1696,7 +1711,7 @@ int launch_q8_evict(const Pages& pg, int32_t B, int32_t H, const int32_t* seq_le
         q8_select_kernel<1024, 8><<<dim3(H, B), 1024, 0, stream>>>(a);
     if (int rc = hip_check("q8_select launch", hipGetLastError())) return rc;
     if (a.data[0] == a.to_data[0])
-        q8_move_kernel<<<dim3(32, H, B), kWave, 0, stream>>>(a);
+        q8_move_kernel<<<dim3(32, H, B), kWave * std::min((a.keep + kMoveBlocks - 1) / kMoveBlocks, 16), 0, stream>>>(a);
     else
         q8_copy_kernel<<<dim3((unsigned)((2 * (int64_t)a.keep + 3) / 4), H, B), 256, 0, stream>>>(a);
     return hip_check("q8_move launch", hipGetLastError());
