@@ -498,8 +498,7 @@ struct Q8Args {
     float* ws_acc;
 };
 
-constexpr int kAWaves = 8;
-constexpr int kAThreads = kAWaves * kWave;
+constexpr int kAWaves = 8;                   // wavefronts per workgroup (4 for short sequences)
 constexpr int kGP = 8;                       // query-head slots
 constexpr int kChunkCost = 8;                // what a chunk costs besides its blocks, in blocks
 constexpr float kBig = 3e38f;
@@ -639,8 +638,8 @@ __device__ __forceinline__ Share share_of(const Q8Args& a, int id, int lane) {
     return Share{0, 0, -1, chunk};
 }
 
-// One workgroup of eight wavefronts per (chunk of visible blocks, KV head,
-// sequence); a wavefront takes every eighth block of the chunk and requests
+// One workgroup of eight (or four) wavefronts per (chunk of visible blocks, KV
+// head, sequence); a wavefront takes every eighth block of the chunk and requests
 // the next one's 8 KB before it works on the one at hand.
 //   Scores: S^T (16 tokens x 16 columns) = K (16 x 128) Q^T on
 //   v_mfma_f32_16x16x32_f16.  Codes are exact in fp16, and so are the query's
@@ -654,10 +653,10 @@ __device__ __forceinline__ Share share_of(const Q8Args& a, int id, int lane) {
 //   second in rows 8..15: one product of the 32 tokens gives both, its operand
 //   the weights as they lie.  The block's scale is applied to the
 //   product's fp32 result.
-template <int FMT, bool TRACK>
-__global__ __launch_bounds__(kAThreads, 4) void q8_partial_kernel(Q8Args a) {
-    __shared__ float wm[kAWaves][kGP], wl[kAWaves][kGP];
-    __shared__ __align__(16) float wacc[kAWaves][kGP][kD];
+template <int FMT, bool TRACK, int WAVES>
+__global__ __launch_bounds__(WAVES* kWave, 4) void q8_partial_kernel(Q8Args a) {
+    __shared__ float wm[WAVES][kGP], wl[WAVES][kGP];
+    __shared__ __align__(16) float wacc[WAVES][kGP][kD];
     int c = blockIdx.x, h = blockIdx.y, b = blockIdx.z, chunk = a.chunk;
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -749,9 +748,9 @@ __global__ __launch_bounds__(kAThreads, 4) void q8_partial_kernel(Q8Args a) {
     const int64_t slot0 = ((int64_t)b * a.Hq + h * G) * (NC + kResSlots) + c;
     if (v0 >= v1) {
         if (a.out) {
-            for (int i = tid; i < G * kD; i += kAThreads) a.out[((int64_t)b * a.Hq + h * G) * kD + i] = 0.f;
+            for (int i = tid; i < G * kD; i += WAVES * kWave) a.out[((int64_t)b * a.Hq + h * G) * kD + i] = 0.f;
         } else if (a.window > 0) {
-            for (int i = tid; i < G * kD; i += kAThreads) {
+            for (int i = tid; i < G * kD; i += WAVES * kWave) {
                 const int64_t slot = slot0 + (int64_t)(i / kD) * (NC + kResSlots);
                 a.ws_acc[slot * kD + i % kD] = 0.f;
                 if (i % kD == 0) {
@@ -806,14 +805,14 @@ __global__ __launch_bounds__(kAThreads, 4) void q8_partial_kernel(Q8Args a) {
             request_k();
             request_v();
         }
-        if (v + kAWaves < v1) look_up(block_of(v + kAWaves));
+        if (v + WAVES < v1) look_up(block_of(v + WAVES));
     }
     // One block; the next one is requested on the way (its keys once these have
     // become scores, its values once these are added) or there is none.  Two
     // copies: a request under a branch would make every wait one for all loads.
     auto step = [&](auto more) {
         const int blk = block_of(v), t0 = blk * kBlk;
-        const int vn = v + kAWaves;
+        const int vn = v + WAVES;
         const float ks = ks_next, vs = vs_next;
 
         // ---- scores in base 2
@@ -834,7 +833,7 @@ __global__ __launch_bounds__(kAThreads, 4) void q8_partial_kernel(Q8Args a) {
         if constexpr (decltype(more)::value) {
             locate(block_of(vn));
             request_k();
-            if (vn + kAWaves < v1) look_up(block_of(vn + kAWaves));
+            if (vn + WAVES < v1) look_up(block_of(vn + WAVES));
         }
         const bool whole = t0 + kBlk <= T && (t0 >= vis.start || t0 + kBlk <= vis.sinks);
         if (!whole) {
@@ -917,7 +916,7 @@ __global__ __launch_bounds__(kAThreads, 4) void q8_partial_kernel(Q8Args a) {
         if constexpr (decltype(more)::value) request_v();
     };
     if (v < v1) {
-        for (; v + kAWaves < v1; v += kAWaves) step(std::true_type{});
+        for (; v + WAVES < v1; v += WAVES) step(std::true_type{});
         step(std::false_type{});
     }
     if (bad && lane == 0 && a.status) atomicOr(a.status, DQ_STATUS_PAGE);
@@ -937,14 +936,14 @@ __global__ __launch_bounds__(kAThreads, 4) void q8_partial_kernel(Q8Args a) {
         wl[wave][lane] = bad_q ? NAN : l_run;
     }
     __syncthreads();
-    for (int i = tid; i < G * kD; i += kAThreads) {
+    for (int i = tid; i < G * kD; i += WAVES * kWave) {
         const int g = i / kD, j = i % kD;
         float M = wm[0][g];
 #pragma unroll
-        for (int u = 1; u < kAWaves; ++u) M = fmaxf(M, wm[u][g]);
+        for (int u = 1; u < WAVES; ++u) M = fmaxf(M, wm[u][g]);
         float s = 0.f, l = 0.f;
 #pragma unroll
-        for (int u = 0; u < kAWaves; ++u) {
+        for (int u = 0; u < WAVES; ++u) {
             const float e = exp2f(wm[u][g] - M);
             s = fmaf(wacc[u][g][j], e, s);
             l = fmaf(wl[u][g], e, l);
@@ -969,12 +968,12 @@ __global__ __launch_bounds__(kAThreads, 4) void q8_partial_kernel(Q8Args a) {
         for (int g = 0; g < kGP; ++g) {
             float M = wm[0][g], l = 0.f;
 #pragma unroll
-            for (int u = 1; u < kAWaves; ++u) M = fmaxf(M, wm[u][g]);
+            for (int u = 1; u < WAVES; ++u) M = fmaxf(M, wm[u][g]);
 #pragma unroll
-            for (int u = 0; u < kAWaves; ++u) l = fmaf(wl[u][g], exp2f(wm[u][g] - M), l);
+            for (int u = 0; u < WAVES; ++u) l = fmaf(wl[u][g], exp2f(wm[u][g] - M), l);
             total[g] = l == 0.f ? INFINITY : M + log2f(l);
         }
-        for (int u = tid; u < vis.count; u += kAThreads) {
+        for (int u = tid; u < vis.count; u += WAVES * kWave) {
             const int64_t i = ((int64_t)b * a.Hkv + h) * nb_cap + block_of(u);
             float w = 0.f;
 #pragma unroll
@@ -1584,12 +1583,12 @@ Q8Plan q8_plan(int64_t cus, int B, int Hkv, int t_cap, int window, int sinks, bo
     return p;
 }
 
-template <int FMT>
+template <int FMT, int WAVES>
 void launch_q8_format(const Q8Args& a, dim3 grid, hipStream_t stream) {
     if (a.lse)
-        q8_partial_kernel<FMT, true><<<grid, kAThreads, 0, stream>>>(a);
+        q8_partial_kernel<FMT, true, WAVES><<<grid, WAVES * kWave, 0, stream>>>(a);
     else
-        q8_partial_kernel<FMT, false><<<grid, kAThreads, 0, stream>>>(a);
+        q8_partial_kernel<FMT, false, WAVES><<<grid, WAVES * kWave, 0, stream>>>(a);
 }
 
 }  // namespace
@@ -1635,10 +1634,16 @@ int launch_q8_partial(int format, const Pages& pg, const uint16_t* q, int32_t B,
     a.ws_m = a.ws_acc + held * kD;
     a.ws_l = a.ws_m + held;
     const dim3 grid = plan.target ? dim3((unsigned)plan.items * Hkv) : dim3(plan.nchunks, Hkv, B);
+    // Four wavefronts where a sequence has few blocks (up to 8: 8 KV heads of one of
+    // 37 tokens 5.4 us against 5.7) or the pairs fill the CUs twice and more (up to
+    // 32: more workgroups start at a time; 300 sequences of 200 tokens 26 against 34
+    // us, of 400 46 against 51, of 1000 104 both; beyond, unlike lengths lose: 128 of
+    // up to 2000 51 against 47).
+    const bool small = whole && (plan.chunk <= 8 || (plan.chunk <= 32 && (int64_t)B * Hkv >= 2 * cus));
     if (format == DQ_Q8_E4M3)
-        launch_q8_format<DQ_Q8_E4M3>(a, grid, stream);
+        small ? launch_q8_format<DQ_Q8_E4M3, 4>(a, grid, stream) : launch_q8_format<DQ_Q8_E4M3, 8>(a, grid, stream);
     else
-        launch_q8_format<DQ_Q8_INT8>(a, grid, stream);
+        small ? launch_q8_format<DQ_Q8_INT8, 4>(a, grid, stream) : launch_q8_format<DQ_Q8_INT8, 8>(a, grid, stream);
     return hip_check("q8_partial launch", hipGetLastError());
 }
 

@@ -223,6 +223,16 @@ def test_attention_windows(dq, fmt, window, sinks):
 
 
 @pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("window,sinks", [(0, 0), (70, 33)])
+def test_attention_short_sequences(dq, fmt, window, sinks):
+    """One launch each: a few short sequences, and many of a few blocks, with their weights."""
+    for lens, t_cap in (([1, 256, 37, 0, 129], 256), ([(37 * b) % 385 for b in range(260)], 384)):
+        cache, _, _, _, weight = _attend_case(dq, fmt, lens, 3, t_cap=t_cap, window=window, sinks=sinks, scores=True)
+        # as in test_scores
+        assert np.max(np.abs(cache.scores.double().cpu().numpy() - weight)) <= 3 * 3e-5
+
+
+@pytest.mark.parametrize("fmt", FMTS)
 def test_attention_long_split(dq, fmt):
     """Chunks of many blocks, and the longest split (64 chunks)."""
     _attend_case(dq, fmt, [16384, 9999], 4, H=1, t_cap=16384)
