@@ -571,7 +571,8 @@ int dq_q8_add_scores(int32_t batch, int32_t q_heads, int32_t kv_heads, const int
  *       seq_lens[b] - 32 (blocks evicted)
  *   to_*: the cache that receives the kept blocks: either the same arrays (in
  *       place; to_cap = t_cap) or others, of to_cap tokens, that do not overlap
- *       them.  Scores behind the kept ones, up to the old block count, become 0.
+ *       them.  Scores behind the kept ones become 0, in place up to the old block
+ *       count.
  * In pool pages the eviction is in place, so none of the pages may belong to
  * two sequences; pages behind the new length are free for the caller.  An entry
  * outside the pool sets DQ_STATUS_PAGE and nothing is written through it.

@@ -166,8 +166,10 @@ class Q8KVCache:
     def append(self, k, v, t0: int):
         """Encode bf16 k, v [B, T_new, H, 128] as cache tokens [t0, t0 + T_new)
         (t0 a multiple of 32; a last block that is not full is completed with
-        zeros)."""
+        zeros).  The blocks' scores begin at 0."""
         _lib._q8_encode(self._format, self._at, k, v, t0, self.status, None)
+        if self.scores is not None:
+            self.scores[:, :, t0 // self.BLOCK:(t0 + k.shape[1] + self.BLOCK - 1) // self.BLOCK].zero_()
 
     def read(self, t0: int, n: int):
         """bf16 k, v [B, n, H, 128]: the values of tokens [t0, t0 + n)."""

@@ -1361,7 +1361,8 @@ __global__ __launch_bounds__(THREADS) void q8_select_kernel(EvictArgs a) {
     }
     if (bad && a.status) atomicOr(a.status, DQ_STATUS_PAGE);
     for (int i = n + tid; i < a.keep; i += kSelThreads) kept[i] = -1;
-    for (int i = n + tid; i < min(nb, a.to_cap); i += kSelThreads) to[i] = 0.f;
+    const int end = a.scores == a.to_scores ? min(nb, a.to_cap) : a.to_cap;
+    for (int i = n + tid; i < end; i += kSelThreads) to[i] = 0.f;
 }
 
 __device__ __forceinline__ void new_length(const EvictArgs& a, int b) {

@@ -530,6 +530,19 @@ def test_evict(dq, fmt, levels, keep, first, last):
             assert [int(x) for x in new_lens] == [T - 32 * max(0, (T + 31) // 32 - keep // 32) for T in lens]
 
 
+def test_scores_begin_at_zero(dq):
+    """Of appended blocks, and behind the kept ones of a cache that held more before."""
+    cache, seq = _fill(dq, "int8", 2, 2, 512, [512, 100], 27)
+    before = cache.scores.clone()
+    k, v = _kv(28, 2, 40, 2)
+    cache.append(k.to(DEV), v.to(DEV), 64)
+    before[:, :, 2:4] = 0
+    assert torch.equal(cache.scores, before)
+    to, _ = _fill(dq, "int8", 2, 2, 1024, [1024, 1024], 29)
+    cache.evict(seq, 256, 32, 64, into=to)
+    assert not to.scores[0, :, 8:].any() and not to.scores[1, :, 4:].any()
+
+
 def test_evict_nan_scores_and_many_blocks(dq):
     cache, seq = _fill(dq, "int8", 1, 2, 65536, [65536], 23)
     cache.scores[0, 0, 5::7] = math.nan
