@@ -524,6 +524,8 @@ int dq_q8_decode_kv_paged(int32_t format, const uint8_t* k_pool, const float* k_
  * arguments are those of the step.  The step has to be one of the _partial
  * calls: dq_q8_decode_attention, which may finish without the workspace, adds
  * to the scores by itself.
+ * dq_q8_merge_scores: dq_decode_attention_merge and dq_q8_add_scores of such a
+ * step in one launch.
  */
 int dq_q8_decode_attention_partial(int32_t format, const uint16_t* q, int32_t batch, int32_t q_heads,
                                    int32_t kv_heads, const uint8_t* k_data, const float* k_scale,
@@ -554,6 +556,10 @@ int dq_q8_add_scores(int32_t batch, int32_t q_heads, int32_t kv_heads, const int
                      const int32_t* extra_lens, int32_t t_cap, int32_t window, int32_t sinks,
                      const float* block_lse, const void* workspace, size_t workspace_bytes, float* scores,
                      void* stream);
+int dq_q8_merge_scores(int32_t batch, int32_t q_heads, int32_t kv_heads, const int32_t* seq_lens,
+                       const int32_t* extra_lens, int32_t t_cap, int32_t window, int32_t sinks,
+                       const float* block_lse, const void* workspace, size_t workspace_bytes, float* out,
+                       float* scores, void* stream);
 
 /*
  * Eviction by accumulated attention weight.  Every (sequence, KV head) that

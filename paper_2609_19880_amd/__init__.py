@@ -15,7 +15,8 @@ Entry points (same names as the C ABI in ``include/dq.h``):
     dq_decode_attention_token_partial, dq_fixed_bits, dq_encode_kv_fixed,
     dq_decode_attention_fixed_partial, dq_q8_encode_kv, dq_q8_encode_kv_paged, dq_q8_decode_kv,
     dq_q8_decode_kv_paged, dq_q8_decode_attention, dq_q8_decode_attention_partial,
-    dq_q8_decode_attention_paged, dq_q8_decode_attention_paged_partial, dq_q8_add_scores, dq_q8_evict,
+    dq_q8_decode_attention_paged, dq_q8_decode_attention_paged_partial, dq_q8_add_scores,
+    dq_q8_merge_scores, dq_q8_evict,
     dq_q8_evict_paged, dq_decode_symbols, dq_strerror, dq_last_error
 """
 
@@ -34,7 +35,8 @@ from ._lib import (  # noqa: F401
     dq_fixed_bits, dq_encode_kv_fixed, dq_decode_attention_fixed_partial,
     DQ_Q8_BLOCK, DQ_Q8_INT8, DQ_Q8_E4M3, dq_q8_encode_kv, dq_q8_encode_kv_paged, dq_q8_decode_kv,
     dq_q8_decode_kv_paged, dq_q8_decode_attention, dq_q8_decode_attention_partial,
-    dq_q8_decode_attention_paged, dq_q8_decode_attention_paged_partial, dq_q8_add_scores, dq_q8_evict,
+    dq_q8_decode_attention_paged, dq_q8_decode_attention_paged_partial, dq_q8_add_scores,
+    dq_q8_merge_scores, dq_q8_evict,
     dq_q8_evict_paged,
     dq_decode_symbols, dq_strerror, dq_last_error, smallest_feasible_alpha,
 )

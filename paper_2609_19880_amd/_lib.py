@@ -127,11 +127,12 @@ def _load():
     lib.dq_q8_decode_attention_paged_partial.argtypes = [*step, *pages, P, P, I32, I32, F, P, P, SZ, P, P]
     lib.dq_q8_decode_attention_paged.argtypes = [*step, *pages, P, I32, I32, F, P, P, P, P, SZ, P, P]
     lib.dq_q8_add_scores.argtypes = [I32, I32, I32, P, P, I32, I32, I32, P, P, SZ, P, P]
+    lib.dq_q8_merge_scores.argtypes = [I32, I32, I32, P, P, I32, I32, I32, P, P, SZ, P, P, P]
     lib.dq_q8_evict.argtypes = [I32, I32, P, P, I32, I32, I32, I32, I32, P, P, P, P, P, P, P, P, P, P, P, P]
     lib.dq_q8_evict_paged.argtypes = [I32, I32, P, P, I32, I32, I32, *pages, P, P, P, P, P, P, P, P]
     for name in ("encode_kv", "encode_kv_paged", "decode_kv", "decode_kv_paged", "decode_attention_partial",
                  "decode_attention", "decode_attention_paged_partial", "decode_attention_paged", "add_scores",
-                 "evict", "evict_paged"):
+                 "merge_scores", "evict", "evict_paged"):
         getattr(lib, "dq_q8_" + name).restype = ctypes.c_int
     lib.dq_residual_append.argtypes = [P, P, I32, I32, I32, P, P, P, P, I32, P, P]
     lib.dq_residual_append.restype = ctypes.c_int
@@ -975,6 +976,23 @@ def dq_q8_add_scores(q_heads: int, seq_lens, block_lse, workspace, scores, windo
     rc = _lib.dq_q8_add_scores(B, q_heads, H, lens, extra, nb * DQ_Q8_BLOCK, *_q8_sees(window, sinks), lse,
                                *_q8_workspace(workspace, scores.device), sc, _q8_stream(scores, stream))
     _check(rc, "dq_q8_add_scores")
+
+
+def dq_q8_merge_scores(q_heads: int, seq_lens, block_lse, workspace, out, scores, window: int = 0, sinks: int = 0,
+                       extra_lens=None, stream=None):
+    """dq_decode_attention_merge (out fp32 [B, Hq, 128]) and dq_q8_add_scores in
+    one launch."""
+    _need(scores.dim() == 3, "scores must be fp32 [B, H, t_cap/32]")
+    B, H, nb = scores.shape
+    dev = scores.device
+    sc, lse = _q8_scores(scores, block_lse, B, H, nb, q_heads // H, dev)
+    _need(out.dtype == torch.float32 and out.shape == (B, q_heads, 128) and out.is_contiguous() and out.device == dev,
+          "out must be fp32 [B, Hq, 128]")
+    extra = 0 if extra_lens is None else _q8_lens(extra_lens, B, dev, "extra_lens")
+    rc = _lib.dq_q8_merge_scores(B, q_heads, H, _q8_lens(seq_lens, B, dev), extra, nb * DQ_Q8_BLOCK,
+                                 *_q8_sees(window, sinks), lse, *_q8_workspace(workspace, dev), out.data_ptr(), sc,
+                                 _q8_stream(scores, stream))
+    _check(rc, "dq_q8_merge_scores")
 
 
 def _q8_kept(kept, keep, first, last, batch, heads, dev):

@@ -200,6 +200,11 @@ class Q8KVCache:
         _lib.dq_q8_add_scores(self.q_heads, seq_lens, self.block_lse, self.workspace, self.scores, window, sinks,
                               extra_lens)
 
+    def merge_scores(self, seq_lens, out, window: int = 0, sinks: int = 0, extra_lens=None):
+        """merge and add_scores in one launch."""
+        _lib.dq_q8_merge_scores(self.q_heads, seq_lens, self.block_lse, self.workspace, out, self.scores, window,
+                                sinks, extra_lens)
+
     def evict(self, seq_lens, keep: int, sinks: int = 0, recent: int = 32, into=None, new_lens=None):
         """Cut every sequence to at most `keep` tokens (a multiple of 32): the
         blocks of its first `sinks` and newest `recent` tokens (rounded up to
@@ -334,8 +339,7 @@ class StreamingKVCache:
                 # the scores' weights need the raw tokens' partials in the workspace
                 _lib.dq_decode_attention_residual(q, self.res_k, self.res_v, self.seq_lens, self.res_lens, c.t_cap,
                                                   c.workspace, softmax_scale=softmax_scale)
-                c.merge(self.seq_lens, out)
-                c.add_scores(self.seq_lens, window, sinks, self.res_lens)
+                c.merge_scores(self.seq_lens, out, window, sinks, self.res_lens)
                 return out
         _lib.dq_decode_attention_merge_residual(q, self.res_k, self.res_v, self.seq_lens, self.res_lens, c.t_cap,
                                                 c.workspace, out, softmax_scale=softmax_scale)

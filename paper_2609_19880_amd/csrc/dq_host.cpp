@@ -817,6 +817,15 @@ int dq_q8_add_scores(int32_t B, int32_t Hq, int32_t Hkv, const int32_t* seq_lens
                                 static_cast<hipStream_t>(stream));
 }
 
+int dq_q8_merge_scores(int32_t B, int32_t Hq, int32_t Hkv, const int32_t* seq_lens, const int32_t* extra_lens,
+                       int32_t t_cap, int32_t window, int32_t sinks, const float* block_lse, const void* ws,
+                       size_t ws_bytes, float* out, float* scores, void* stream) {
+    if (!block_lse || !scores || !out || (reinterpret_cast<uintptr_t>(out) & 7)) return DQ_ERR_INVALID_ARG;
+    if (int rc = check_q8_step(B, Hq, Hkv, seq_lens, t_cap, window, sinks, ws, ws_bytes)) return rc;
+    return dq::launch_q8_finish(B, Hq, Hkv, seq_lens, extra_lens, t_cap, window, sinks, block_lse, ws, out, scores, 0,
+                                static_cast<hipStream_t>(stream));
+}
+
 static int q8_evict(const dq::Pages& pg, int32_t B, int32_t H, const int32_t* seq_lens, int32_t* new_lens,
                     int32_t t_cap, int32_t to_cap, int32_t keep, int32_t first, int32_t last, float* scores,
                     float* to_scores, const dq::Q8Cache& from, const dq::Q8Cache& to, int32_t* kept,

@@ -1036,27 +1036,53 @@ __global__ __launch_bounds__(WAVES* kWave) void q8_finish_kernel(FinishArgs a) {
         const int64_t slot = s0 + min(wave + WAVES * u, last);
         return *(reinterpret_cast<const float2*>(a.ws_acc + slot * kD) + lane);
     };
+    // a residual window's partials, these many per wavefront
+    constexpr int kRes = kResSlots / WAVES;
+    float rm[kRes], rl[kRes];
+    float2 rx[kRes];
     if (merge) {
         const int64_t s1 = s0 + min(wave + WAVES * lane, NC - 1);
         m_lane = a.ws_m[s1];
         l_lane = a.ws_l[s1];
 #pragma unroll
         for (int u = 0; u < kFinishFirst; ++u) x[u] = partial(u, NC - 1);
+        if (a.nc == 0) {
+#pragma unroll
+            for (int r = 0; r < kRes; ++r) {
+                const int64_t slot = s0 + NC + wave * kRes + r;
+                rm[r] = a.ws_m[slot];
+                rl[r] = a.ws_l[slot];
+                rx[r] = *(reinterpret_cast<const float2*>(a.ws_acc + slot * kD) + lane);
+            }
+        }
     }
     const int chunk = max(scalar_load(a.ws_hdr), 1);
     const int residual = a.nc ? 0 : min(max(scalar_load(a.ws_hdr + 2), 0), kResSlots);
     const int T = max(0, min(scalar_load(a.seq_lens + b), a.t_cap));
     const int nc = (int)min((int64_t)NC, ((int64_t)T + chunk - 1) / chunk), np = nc + residual;
     if (merge) {
-        // the merge runs where no residual window does: partials 0 .. nc - 1,
-        // at most kMostChunks
+        // partials 0 .. nc - 1, at most kMostChunks, and the residual window's
         const int n = max(0, nc - wave + WAVES - 1) / WAVES;
         if (lane >= n) m_lane = -INFINITY;
-        const float M = wave_max(m_lane);
+        float M = wave_max(m_lane);
+#pragma unroll
+        for (int r = 0; r < kRes; ++r) {
+            if (wave * kRes + r >= residual) rm[r] = -INFINITY;
+            M = fmaxf(M, rm[r]);
+        }
         // (a partial without weight, or none: 0, whatever its slot holds)
         const float e_lane = m_lane == -INFINITY ? 0.f : exp2f(m_lane - M);
-        const float l = wave_sum(m_lane == -INFINITY ? 0.f : l_lane * e_lane);
+        float l = wave_sum(m_lane == -INFINITY ? 0.f : l_lane * e_lane);
         float2 acc = {0.f, 0.f};
+#pragma unroll
+        for (int r = 0; r < kRes; ++r) {
+            if (rm[r] != -INFINITY) {
+                const float e = exp2f(rm[r] - M);
+                l = fmaf(rl[r], e, l);
+                acc.x = fmaf(rx[r].x, e, acc.x);
+                acc.y = fmaf(rx[r].y, e, acc.y);
+            }
+        }
         auto add = [&](int u0, int most) {
 #pragma unroll
             for (int u = 0; u < kFinishBatch; ++u) {

@@ -477,6 +477,34 @@ def test_scores_of_partials(dq, window, sinks):
     assert np.isclose(float(cache.scores.sum(dtype=torch.float64)), 4, rtol=3e-5)
 
 
+@pytest.mark.parametrize("lens,G,t_cap", [([1000, 0, 33, 500], 4, 1024), ([16300], 2, 16384), ([300, 1] * 40, 2, 384)])
+@pytest.mark.parametrize("raw", [False, True])
+def test_merge_scores_is_merge_and_scores(dq, lens, G, t_cap, raw):
+    """In one launch what the two give, with and without a residual window (of 0 to 200 tokens)."""
+    cache, seq, q, _, _ = _attend_case(dq, "e4m3", lens, G, H=2, t_cap=t_cap, scores=True)
+    B = len(lens)
+    rk, rv = (x.to(DEV).permute(0, 2, 1, 3).contiguous() for x in _kv(33, B, 256, 2))
+    extra = torch.tensor([(200, 0, 7)[b % 3] for b in range(B)], dtype=torch.int32, device=DEV) if raw else None
+    both = []
+    for one in (False, True):
+        out = torch.full((B, 2 * G, 128), math.nan, device=DEV)
+        cache.scores.zero_()
+        cache.partial(q, seq, extra_lens=extra)
+        if raw:
+            dq.dq_decode_attention_residual(q, rk, rv, seq, extra, t_cap, cache.workspace)
+        if one:
+            cache.merge_scores(seq, out, extra_lens=extra)
+        else:
+            cache.merge(seq, out)
+            cache.add_scores(seq, extra_lens=extra)
+        both.append((out, cache.scores.clone()))
+    (a, sa), (b, sb) = both
+    assert torch.equal(sa, sb)
+    # the same partials in another order: at most 70 of them, a rounding of 2^-24 for
+    # each product and each sum of the output and of its denominator
+    assert ((a - b).norm(dim=2) <= a.norm(dim=2) * 4 * 70 * 2.0 ** -24).all()
+
+
 def _fill(dq, fmt, B, H, t_cap, lens, seed, levels=None):
     k, v = _kv(seed, B, t_cap, H)
     cache = dq.Q8KVCache(B, H, 4 * H, t_cap, fmt, scores=True)

@@ -165,3 +165,13 @@ def test_cache_off_the_gpu_is_refused():
                  lambda: c.partial(q, lens), lambda: c.evict(lens, 128)):
         with pytest.raises(ValueError, match="GPU"):
             call()
+
+
+@pytest.mark.parametrize("bad,code", [
+    (dict(B=0), INVALID), (dict(Hq=12), INVALID), (dict(H=0), INVALID), (dict(lens=None), INVALID),
+    (dict(cap=160), INVALID), (dict(s=3), INVALID), (dict(lse=None), INVALID), (dict(ws=None), WORKSPACE),
+    (dict(ws=P + 8), INVALID), (dict(n=1000), WORKSPACE), (dict(out=None), INVALID), (dict(out=P + 4), INVALID),
+    (dict(sc=None), INVALID)])
+def test_merge_scores_refusals(bad, code):
+    a = dict(B=2, Hq=32, H=8, lens=P, extra=None, cap=256, w=0, s=0, lse=P, ws=P, n=1 << 40, out=P, sc=P, stream=None)
+    assert C.dq_q8_merge_scores(*_swap(a, bad)) == code
