@@ -886,8 +886,7 @@ def dq_q8_decode_attention_partial(fmt, q, k_data, k_scale, v_data, v_scale, seq
                 sinks, extra_lens, softmax_scale, block_lse, stream)
 
 
-def _q8_attention(fmt: int, cache, q, seq_lens, out, workspace, window, sinks, softmax_scale, block_lse, scores,
-                  stream):
+def _q8_attention(fmt: int, cache, q, seq_lens, out, workspace, window, sinks, softmax_scale, lse, sc, stream):
     _need(cache is not None, "the cache must be on one GPU")
     B, H, nb, dev, at = cache
     if not (q.dtype == torch.bfloat16 and q.dim() == 3 and q.is_contiguous() and q.device == dev
@@ -905,9 +904,6 @@ def _q8_attention(fmt: int, cache, q, seq_lens, out, workspace, window, sinks, s
     else:
         _need(out.dtype == torch.float32 and out.shape == q.shape and out.is_contiguous() and out.device == dev,
               "out must be fp32 of q's shape")
-    sc = lse = 0
-    if scores is not None or block_lse is not None:
-        sc, lse = _q8_scores(scores, block_lse, B, H, nb, Hq // H, dev)
     rc = _lib.dq_q8_decode_attention(
         fmt, q.data_ptr(), B, Hq, H, *at, seq_lens.data_ptr(), nb * DQ_Q8_BLOCK, window, sinks,
         _RSQRT_D if softmax_scale is None else softmax_scale, out.data_ptr(), lse, sc, workspace.data_ptr(),
@@ -923,8 +919,10 @@ def dq_q8_decode_attention(fmt, q, k_data, k_scale, v_data, v_scale, seq_lens, o
     window > 0: only the first `sinks` and the newest `window` tokens are
     visible.  scores fp32 [B, H, t_cap/32] grow by the blocks' attention weight
     (block_lse fp32 [B, H, t_cap/32, Hq/H] is its scratch)."""
-    _q8_attention(_q8_format(fmt), _q8_cache_args(k_data, k_scale, v_data, v_scale), q, seq_lens, out, workspace,
-                  window, sinks, softmax_scale, block_lse, scores, stream)
+    cache = _q8_cache_args(k_data, k_scale, v_data, v_scale)
+    B, H, nb, dev, _ = cache
+    sc, lse = _q8_scores(scores, block_lse, B, H, nb, q.shape[1] // H, dev)
+    _q8_attention(_q8_format(fmt), cache, q, seq_lens, out, workspace, window, sinks, softmax_scale, lse, sc, stream)
 
 
 def dq_q8_decode_attention_paged_partial(fmt, q, k_pool, k_scale_pool, v_pool, v_scale_pool, block_table, seq_lens,
@@ -1002,13 +1000,11 @@ def _q8_kept(kept, keep, first, last, batch, heads, dev):
     return kept.data_ptr()
 
 
-def _q8_evict(seq_lens, new_lens, keep, first, last, source, scores, to, to_scores, kept, stream):
+def _q8_evict(seq_lens, new_lens, keep, first, last, source, sc, to, tsc, kept, stream):
     _need(source is not None and to is not None, "the cache must be on one GPU")
     B, H, nb, dev, at = source
     tB, tH, tnb, tdev, to_at = to
     _need(tB == B and tH == H and tdev == dev, "both caches must have the same batch, heads and GPU")
-    sc, _ = _q8_scores(scores, None, B, H, nb, 1, dev)
-    tsc, _ = _q8_scores(to_scores, None, B, H, tnb, 1, dev)
     rc = _lib.dq_q8_evict(B, H, _q8_lens(seq_lens, B, dev), _q8_lens(new_lens, B, dev, "new_lens"), nb * DQ_Q8_BLOCK,
                           tnb * DQ_Q8_BLOCK, keep, first, last, *at, sc, *to_at, tsc,
                           _q8_kept(kept, keep, first, last, B, H, dev), _q8_stream(kept, stream))
@@ -1020,8 +1016,10 @@ def dq_q8_evict(seq_lens, new_lens, keep: int, first: int, last: int, source, to
     the largest scores, keep tokens in all (multiples of 32).  source, to:
     (k_data, k_scale, v_data, v_scale, scores), the same arrays for an eviction
     in place; kept int32 [B, H, keep/32]; new_lens may be seq_lens."""
-    _q8_evict(seq_lens, new_lens, keep, first, last, _q8_cache_args(*source[:4]), source[4], _q8_cache_args(*to[:4]),
-              to[4], kept, stream)
+    src, dst = _q8_cache_args(*source[:4]), _q8_cache_args(*to[:4])
+    sc, _ = _q8_scores(source[4], None, *src[:3], 1, src[3])
+    tsc, _ = _q8_scores(to[4], None, *dst[:3], 1, dst[3])
+    _q8_evict(seq_lens, new_lens, keep, first, last, src, sc, dst, tsc, kept, stream)
 
 
 def dq_q8_evict_paged(seq_lens, new_lens, keep: int, first: int, last: int, block_table, pools, scores, kept,

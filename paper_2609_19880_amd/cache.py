@@ -134,13 +134,21 @@ class Q8KVCache:
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
         self.workspace = torch.empty(
             _lib.dq_decode_workspace_bytes(batch, q_heads, kv_heads, t_cap), dtype=torch.uint8, device=device)
-        self.scores = torch.zeros_like(self.k_scales) if scores else None
-        self.block_lse = None
+        self._scores = self._block_lse = None
         if scores:
-            self.block_lse = torch.empty((batch, kv_heads, nb, q_heads // kv_heads), dtype=torch.float32,
-                                         device=device)
+            self._scores = torch.zeros_like(self.k_scales)
+            self._block_lse = torch.empty((batch, kv_heads, nb, q_heads // kv_heads), dtype=torch.float32,
+                                          device=device)
+        self._locate()
+
+    def _locate(self):
         # sizes and addresses of the cache's own arrays, checked once
         self._at = _lib._q8_cache_args(*self._arrays) if self.status.is_cuda else None
+        self._score_at, self._lse_at = (0 if x is None else x.data_ptr() for x in (self._scores, self._block_lse))
+
+    def __setstate__(self, state):
+        self.__dict__.update(state)
+        self._locate()               # a deep copy has arrays of its own
 
     @property
     def arrays(self):
@@ -163,6 +171,16 @@ class Q8KVCache:
     def v_scales(self):
         return self._arrays[3]
 
+    @property
+    def scores(self):
+        """fp32 [B, H, t_cap/32], or None"""
+        return self._scores
+
+    @property
+    def block_lse(self):
+        """the steps' scratch for the scores, fp32 [B, H, t_cap/32, Hq/H], or None"""
+        return self._block_lse
+
     def append(self, k, v, t0: int):
         """Encode bf16 k, v [B, T_new, H, 128] as cache tokens [t0, t0 + T_new)
         (t0 a multiple of 32; a last block that is not full is completed with
@@ -179,12 +197,15 @@ class Q8KVCache:
         """q bf16 [B, Hq, 128] -> out fp32 over the first seq_lens[b] tokens or,
         with a window, the first `sinks` and the newest `window` of them.  The
         cache's own scores grow by the blocks' weights, or the given ones."""
-        if scores is None:
-            scores = self.scores
-        elif self.block_lse is None:
-            raise ValueError("the cache was made without scores")
+        at = self._score_at
+        if at and (q.dim() != 3 or q.shape[1] != self.q_heads):
+            raise ValueError("q must be [B, q_heads, 128]")
+        if scores is not None:
+            if self._scores is None:
+                raise ValueError("the cache was made without scores")
+            at, _ = _lib._q8_scores(scores, None, *self._at[:3], 1, self._at[3])
         return _lib._q8_attention(self._format, self._at, q, seq_lens, out, self.workspace, window, sinks,
-                                  softmax_scale, self.block_lse, scores, None)
+                                  softmax_scale, self._lse_at, at, None)
 
     def partial(self, q, seq_lens, softmax_scale=None, window: int = 0, sinks: int = 0, extra_lens=None):
         """Split-K partials of one decode step into the workspace (finish with
@@ -222,7 +243,7 @@ class Q8KVCache:
             new_lens = torch.empty_like(seq_lens)
         up = -self.BLOCK
         _lib._q8_evict(seq_lens, new_lens, keep, sinks // up * up, max(recent // up * up, self.BLOCK), self._at,
-                       self.scores, to._at, to.scores, kept, None)
+                       self._score_at, to._at, to._score_at, kept, None)
         return kept, new_lens
 
     def cache_bytes(self, tokens: int) -> int:

@@ -11,6 +11,7 @@ ln 2 times that, doubled by the softmax's denominator.  Weights carry 22 bits
 (2^-22) and the sums of the values a few roundings more (2^-21 covers them
 up to the lengths used here).  `_tol` is that bound."""
 
+import copy
 import math
 
 import numpy as np
@@ -820,3 +821,27 @@ def test_read_on_another_stream(dq):
     got = dq.dq_q8_decode_kv("int8", *cache.arrays, 32, 900, stream=side)
     side.synchronize()
     assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+def test_deep_copy_is_a_cache_of_its_own(dq):
+    cache, seq, q, out, _ = _attend_case(dq, "int8", [300, 45], 2, t_cap=384, scores=True)
+    other = copy.deepcopy(cache)
+    before, scores = [x.clone() for x in cache.arrays], cache.scores.clone()
+    assert torch.equal(other.attend(q, seq), out) and torch.equal(other.scores, 2 * scores)
+    k, v = _kv(91, 2, 384, 2)
+    other.append(k.to(DEV), v.to(DEV), 0)
+    other.evict(seq, 128, 32, 32)
+    torch.cuda.synchronize()
+    assert torch.equal(cache.scores, scores) and all(torch.equal(x, y) for x, y in zip(cache.arrays, before))
+    assert torch.equal(cache.attend(q, seq), out)
+
+
+def test_query_heads_other_than_the_cache_s(dq):
+    """The scores' scratch is made for the cache's heads."""
+    cache = dq.Q8KVCache(1, 2, 4, 128, scores=True)
+    lens = torch.full((1,), 64, dtype=torch.int32, device=DEV)
+    q = torch.zeros((1, 16, 128), dtype=torch.bfloat16, device=DEV)
+    for call in (lambda: cache.attend(q, lens), lambda: cache.attend(q, lens, scores=cache.scores),
+                 lambda: cache.partial(q, lens)):
+        with pytest.raises((ValueError, dq.DqError)):
+            call()
