@@ -1200,27 +1200,51 @@ __device__ __forceinline__ uint32_t order_key(float x) {
     return (u >> 31) ? ~u : u | 0x80000000u;
 }
 
+__device__ __forceinline__ void new_length(const EvictArgs& a, int b) {
+    const int T = max(0, min(a.seq_lens[b], a.t_cap));
+    const int nb = (T + kBlk - 1) / kBlk;
+    a.new_lens[b] = T - max(0, nb - a.keep) * kBlk;
+}
+
+// Where nothing overlaps: one wavefront, one block of a tensor.  The old blocks
+// are read past the caches, the new ones stay in them for whoever reads them next
+// (131072 tokens to half and read back: 143 us against 158 without, 150 with both
+// past the caches).
+__device__ __forceinline__ void copy_block(const EvictArgs& a, int64_t row, int which, int from, int i, int lane) {
+    const u32x4* src = reinterpret_cast<const u32x4*>(a.data[which] + (row * a.nb_cap + from) * kBlkBytes) + lane;
+    u32x4* dst = reinterpret_cast<u32x4*>(a.to_data[which] + (row * a.to_cap + i) * kBlkBytes) + lane;
+    u32x4 x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = __builtin_nontemporal_load(src + 64 * k);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) dst[64 * k] = x[k];
+}
+
 // One workgroup per (KV head, sequence) chooses the blocks, then one scan in
 // block order writes the list and moves the scores and the two scales, each to
 // a place at or before its own.  The choice, among the blocks that are neither
 // the first nor the newest ones:
 //   KEYS = 1 (up to one block per thread): a block's rank, the number of blocks
 //   before it in the order of (score, lower index), counted against all others
-//   (LDS broadcasts, two instructions per pair);
+//   (LDS broadcasts, two instructions per pair).  COPY: several workgroups choose the
+//   same and then copy the kept blocks, one of them writes what else there is;
 //   else a radix selection (11, 11 and 10 bits of a key) finds the smallest
 //   kept key and how many of its ties are kept (the lowest indexes).  KEYS
 //   THREADS blocks are read once and stay in registers; longer sequences are
 //   read again in each pass and scanned in rounds of so many.
-template <int THREADS, int KEYS>
+template <int THREADS, int KEYS, bool COPY = false>
 __global__ __launch_bounds__(THREADS) void q8_select_kernel(EvictArgs a) {
+    static_assert(KEYS == 1 || !COPY, "the list of kept blocks is in LDS");
     constexpr int kSelThreads = THREADS, kSelWaves = THREADS / kWave, kSelKeys = KEYS;
     __shared__ __align__(16) uint32_t hist[KEYS == 1 ? THREADS : kDigits];
     __shared__ uint32_t part[kSelWaves];
+    __shared__ int list[COPY ? THREADS : 1];
     __shared__ uint32_t s_bin, s_rem;
     __shared__ int s_tie[kSelKeys][kSelWaves], s_kept[kSelKeys][kSelWaves];
     const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
     const int lane = tid & (kWave - 1), wave = tid / kWave;
     const int64_t row = (int64_t)b * a.H + h;
+    const bool writes = !COPY || blockIdx.z == 0;         // the list, the scores and the scales
     const float* sc = a.scores + row * a.nb_cap;
     float* to = a.to_scores + row * a.to_cap;
     int32_t* kept = a.kept + row * a.keep;
@@ -1234,9 +1258,11 @@ __global__ __launch_bounds__(THREADS) void q8_select_kernel(EvictArgs a) {
             s[r] = x[r][0] = x[r][1] = 0.f;
             if (i < n) {
                 s[r] = sc[i];
-                const int64_t bi = block_index(a.pg, a.H, a.nb_cap, b, h, i, bad);
-                x[r][0] = a.scale[0][bi];
-                x[r][1] = a.scale[1][bi];
+                if (writes) {
+                    const int64_t bi = block_index(a.pg, a.H, a.nb_cap, b, h, i, bad);
+                    x[r][0] = a.scale[0][bi];
+                    x[r][1] = a.scale[1][bi];
+                }
             }
         }
     };
@@ -1372,29 +1398,34 @@ __global__ __launch_bounds__(THREADS) void q8_select_kernel(EvictArgs a) {
             }
             if ((keep >> r) & 1u) {
                 const int p = before + pos[r];
-                kept[p] = i0 + r * kSelThreads + tid;
-                to[p] = s[r];
-                bool tbad = false;
-                const int64_t ti = block_index(a.pg, a.H, a.to_cap, b, h, p, tbad);
-                if (!tbad) {
-                    a.to_scale[0][ti] = x[r][0];
-                    a.to_scale[1][ti] = x[r][1];
+                if (COPY) list[p] = tid;
+                if (writes) {
+                    kept[p] = i0 + r * kSelThreads + tid;
+                    to[p] = s[r];
+                    bool tbad = false;
+                    const int64_t ti = block_index(a.pg, a.H, a.to_cap, b, h, p, tbad);
+                    if (!tbad) {
+                        a.to_scale[0][ti] = x[r][0];
+                        a.to_scale[1][ti] = x[r][1];
+                    }
+                    bad |= tbad;
                 }
-                bad |= tbad;
             }
         }
         __syncthreads();
     }
     if (bad && a.status) atomicOr(a.status, DQ_STATUS_PAGE);
-    for (int i = n + tid; i < a.keep; i += kSelThreads) kept[i] = -1;
-    const int end = a.scores == a.to_scores ? min(nb, a.to_cap) : a.to_cap;
-    for (int i = n + tid; i < end; i += kSelThreads) to[i] = 0.f;
-}
-
-__device__ __forceinline__ void new_length(const EvictArgs& a, int b) {
-    const int T = max(0, min(a.seq_lens[b], a.t_cap));   // read by nobody else in this launch: it may be new_lens[b]
-    const int nb = (T + kBlk - 1) / kBlk;
-    a.new_lens[b] = T - max(0, nb - a.keep) * kBlk;
+    if (writes) {
+        for (int i = n + tid; i < a.keep; i += kSelThreads) kept[i] = -1;
+        const int end = a.scores == a.to_scores ? min(nb, a.to_cap) : a.to_cap;
+        for (int i = n + tid; i < end; i += kSelThreads) to[i] = 0.f;
+    }
+    if constexpr (COPY) {
+        if (writes && h == 0 && tid == 0) new_length(a, b);
+        // (the round's last barrier is behind the list)
+        for (int w = (int)blockIdx.z * kSelWaves + wave; w < 2 * n; w += (int)gridDim.z * kSelWaves)
+            copy_block(a, row, w & 1, list[w >> 1], w >> 1, lane);
+    }
 }
 
 // In place the kept blocks' codes move to places at or before their old ones,
@@ -1455,25 +1486,15 @@ __global__ __launch_bounds__(1024) void q8_move_kernel(EvictArgs a) {
     }
 }
 
-// Into another cache nothing overlaps: a wavefront per kept block and tensor.
-// The old blocks are read past the caches, the new ones stay in them for
-// whoever reads them next (131072 tokens to half and read back: 143 us against
-// 158 without, 150 with both past the caches).
+// Into another cache: a wavefront per kept block and tensor.
 __global__ __launch_bounds__(256) void q8_copy_kernel(EvictArgs a) {
     const int h = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & (kWave - 1);
     if (blockIdx.x == 0 && h == 0 && threadIdx.x == 0) new_length(a, b);
-    const int w = wave_index(4), i = w >> 1, which = w & 1;
+    const int w = wave_index(4), i = w >> 1;
     if (i >= a.keep) return;
     const int64_t row = (int64_t)b * a.H + h;
     const int from = a.kept[row * a.keep + i];
-    if (from < 0) return;
-    const u32x4* src = reinterpret_cast<const u32x4*>(a.data[which] + (row * a.nb_cap + from) * kBlkBytes) + lane;
-    u32x4* dst = reinterpret_cast<u32x4*>(a.to_data[which] + (row * a.to_cap + i) * kBlkBytes) + lane;
-    u32x4 x[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) x[k] = __builtin_nontemporal_load(src + 64 * k);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) dst[64 * k] = x[k];
+    if (from >= 0) copy_block(a, row, w & 1, from, i, lane);
 }
 
 }  // namespace
@@ -1733,6 +1754,18 @@ int launch_q8_evict(const Pages& pg, int32_t B, int32_t H, const int32_t* seq_le
     a.keep = keep / kBlk;
     a.first = first / kBlk;
     a.last = last / kBlk;
+    // Into another cache a short sequence's choice is quick enough for every
+    // workgroup that copies to make it again: one launch, two workgroups per CU (8 KV
+    // heads of one sequence of 2048 tokens 5.2 us against 6.9 in two, 16 of 4096 tokens
+    // 27 against 30; over 256 blocks no gain, one of 16384 17.8 against 17.5).  Not
+    // where the new lengths replace the old ones, which all of them read.
+    const bool apart = a.data[0] != a.to_data[0] && (new_lens + B <= seq_lens || seq_lens + B <= new_lens);
+    if (apart && a.nb_cap <= 256) {
+        const int64_t some = std::max<int64_t>(2 * cu_count() / ((int64_t)B * H), 1);
+        const dim3 grid(H, B, (unsigned)std::min<int64_t>(some, (2 * a.keep + 3) / 4));
+        q8_select_kernel<256, 1, true><<<grid, 256, 0, stream>>>(a);
+        return hip_check("q8_select launch", hipGetLastError());
+    }
     if (a.nb_cap <= 256)
         q8_select_kernel<256, 1><<<dim3(H, B), 256, 0, stream>>>(a);
     else if (a.nb_cap <= 512)

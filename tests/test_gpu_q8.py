@@ -605,6 +605,18 @@ def test_evict_numbers_of_blocks(dq, blocks, into):
     _check_evict(old, old_scores, lens, to, kept, new_lens, keep, 96, 160)
 
 
+def test_evict_into_another_cache_over_the_old_lengths(dq):
+    """The new lengths in the old ones' place, a short and a long cache."""
+    for t_cap in (1024, 16384):
+        lens = [t_cap, 700, 0, 33]
+        cache, seq = _fill(dq, "int8", 4, 2, t_cap, lens, 35)
+        to = dq.Q8KVCache(4, 2, 8, 512, scores=True)
+        kept, new_lens = cache.evict(seq, 512, 32, 64, into=to, new_lens=seq)
+        torch.cuda.synchronize()
+        assert new_lens is seq
+        _check_evict(cache.arrays, cache.scores, lens, to, kept, seq, 512, 32, 64)
+
+
 @pytest.mark.parametrize("page", [128, 512])
 def test_evict_paged(dq, page):
     B, H, t_cap, keep = 3, 2, 2048, 640
