@@ -887,18 +887,20 @@ def dq_q8_decode_attention_partial(fmt, q, k_data, k_scale, v_data, v_scale, seq
 
 
 def _q8_attention(fmt: int, cache, q, seq_lens, out, workspace, window, sinks, softmax_scale, lse, sc, stream):
-    _need(cache is not None, "the cache must be on one GPU")
+    if cache is None:
+        raise ValueError("the cache must be on one GPU")
     B, H, nb, dev, at = cache
-    if not (q.dtype == torch.bfloat16 and q.dim() == 3 and q.is_contiguous() and q.device == dev
-            and seq_lens.dtype == torch.int32 and seq_lens.is_contiguous() and seq_lens.numel() == B
-            and seq_lens.device == dev and workspace.device == dev and workspace.is_contiguous()):
+    on = q.get_device()          # (-1 off the GPU)
+    if not (q.dtype is torch.bfloat16 and q.dim() == 3 and q.is_contiguous() and on == dev.index
+            and seq_lens.dtype is torch.int32 and seq_lens.is_contiguous() and seq_lens.numel() == B
+            and seq_lens.get_device() == on and workspace.get_device() == on and workspace.is_contiguous()):
         # what is wrong, by name
         _q8_query(q, H, dev)
         _q8_lens(seq_lens, B, dev)
         _q8_workspace(workspace, dev)
     n, Hq, d = q.shape
-    _need(n == B and d == 128 and 0 <= window <= _INT_MAX and 0 <= sinks <= _INT_MAX,
-          "q must be [batch of the cache, Hq, 128]; window and sinks")
+    if not (n == B and d == 128 and 0 <= window <= _INT_MAX and 0 <= sinks <= _INT_MAX):
+        raise ValueError("q must be [batch of the cache, Hq, 128]; window and sinks")
     if out is None:
         out = torch.empty_like(q, dtype=torch.float32)
     else:
@@ -921,7 +923,9 @@ def dq_q8_decode_attention(fmt, q, k_data, k_scale, v_data, v_scale, seq_lens, o
     (block_lse fp32 [B, H, t_cap/32, Hq/H] is its scratch)."""
     cache = _q8_cache_args(k_data, k_scale, v_data, v_scale)
     B, H, nb, dev, _ = cache
-    sc, lse = _q8_scores(scores, block_lse, B, H, nb, q.shape[1] // H, dev)
+    sc = lse = 0
+    if scores is not None or block_lse is not None:
+        sc, lse = _q8_scores(scores, block_lse, B, H, nb, _q8_query(q, H, dev)[1] // H, dev)
     _q8_attention(_q8_format(fmt), cache, q, seq_lens, out, workspace, window, sinks, softmax_scale, lse, sc, stream)
 
 

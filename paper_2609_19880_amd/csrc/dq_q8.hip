@@ -1604,8 +1604,8 @@ Q8Plan q8_plan(int64_t cus, int B, int Hkv, int t_cap, int window, int sinks, bo
         p.whole = true;
         return p;
     }
-    const int64_t most =
-        std::min({(nb + 3) / 4, std::max<int64_t>(32, (cus + pairs - 1) / pairs), (int64_t)(one_call ? kMostChunks : kWave)});
+    const int64_t most = std::min({(nb + 3) / 4, std::max<int64_t>(32, (cus + pairs - 1) / pairs),
+                                   (int64_t)(one_call ? kMostChunks : kWave)});
     const int64_t target = std::max<int64_t>(1, cus / Hkv), items = std::min(6 * target + B, B * most);
     // (a workgroup reads all lengths; a grid has under 2^32 work-items along x)
     if (window == 0 && B <= 256 && B * nb < (1 << 30) && items * Hkv < (1 << 23)) {
@@ -1775,8 +1775,9 @@ int launch_q8_evict(const Pages& pg, int32_t B, int32_t H, const int32_t* seq_le
     else
         q8_select_kernel<1024, 8><<<dim3(H, B), 1024, 0, stream>>>(a);
     if (int rc = hip_check("q8_select launch", hipGetLastError())) return rc;
+    const int waves = std::min((a.keep + kMoveBlocks - 1) / kMoveBlocks, 16);
     if (a.data[0] == a.to_data[0])
-        q8_move_kernel<<<dim3(32, H, B), kWave * std::min((a.keep + kMoveBlocks - 1) / kMoveBlocks, 16), 0, stream>>>(a);
+        q8_move_kernel<<<dim3(32, H, B), waves * kWave, 0, stream>>>(a);
     else
         q8_copy_kernel<<<dim3((unsigned)((2 * (int64_t)a.keep + 3) / 4), H, B), 256, 0, stream>>>(a);
     return hip_check("q8_move launch", hipGetLastError());
