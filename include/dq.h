@@ -563,14 +563,16 @@ int dq_q8_merge_scores(int32_t batch, int32_t q_heads, int32_t kv_heads, const i
 
 /*
  * Eviction by accumulated attention weight.  Every (sequence, KV head) that
- * holds more than keep / 32 blocks keeps its first `first` and its newest
- * `last` tokens' blocks and, of the others, those with the largest scores (of
+ * holds more than keep / 32 blocks keeps its first `first` / 32 and its newest
+ * `last` / 32 blocks and, of the others, those with the largest scores (of
  * equal ones the lower block; NaN counts as the smallest): keep / 32 blocks in
  * all, in their order.  Codes, scales and scores move to their new places
  * unchanged; shorter sequences keep everything.
- *   keep, first, last: tokens, multiples of 32; first >= 0, last >= 32 (the
- *       newest block may be partly filled and stays the newest), first + last
- *       <= keep <= to_cap
+ *   keep, first, last: whole blocks, counted as 32 tokens each; first >= 0,
+ *       last >= 32, first + last <= keep <= to_cap.  The newest block counts as
+ *       one of the last / 32 however few tokens it holds, so between last - 31
+ *       and last of a sequence's newest tokens stay for certain.  last = n + 31,
+ *       rounded up to a multiple of 32, keeps the newest n at every length.
  *   kept: int32 [batch][kv_heads][keep / 32]: the old index of each kept block,
  *       -1 behind the last
  *   new_lens: device int32 [batch], may be seq_lens: the new lengths,

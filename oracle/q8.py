@@ -18,7 +18,9 @@ Definition
   t >= T + e - w.
 * Scores: a block's weight in a step is the sum of a over its tokens and the
   query heads of its KV head.
-* Eviction: blocks ranked by score, ties to the lower index, NaN lowest.
+* Eviction: whole blocks, the partly filled newest one counted as one; the first
+  and the newest ones stay, the others are ranked by score, ties to the lower
+  index, NaN lowest.
 """
 
 from __future__ import annotations

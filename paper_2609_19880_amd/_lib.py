@@ -1016,8 +1016,9 @@ def _q8_evict(seq_lens, new_lens, keep, first, last, source, sc, to, tsc, kept, 
 
 
 def dq_q8_evict(seq_lens, new_lens, keep: int, first: int, last: int, source, to, kept, stream=None):
-    """Keep the blocks of the first `first` and newest `last` tokens and those of
-    the largest scores, keep tokens in all (multiples of 32).  source, to:
+    """Keep the first `first` / 32 and newest `last` / 32 blocks (the newest one
+    may be partly filled) and those of the largest scores, keep / 32 in all
+    (multiples of 32).  source, to:
     (k_data, k_scale, v_data, v_scale, scores), the same arrays for an eviction
     in place; kept int32 [B, H, keep/32]; new_lens may be seq_lens."""
     src, dst = _q8_cache_args(*source[:4]), _q8_cache_args(*to[:4])

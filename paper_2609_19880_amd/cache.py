@@ -227,12 +227,14 @@ class Q8KVCache:
                                 sinks, extra_lens)
 
     def evict(self, seq_lens, keep: int, sinks: int = 0, recent: int = 32, into=None, new_lens=None):
-        """Cut every sequence to at most `keep` tokens (a multiple of 32): the
-        blocks of its first `sinks` and newest `recent` tokens (rounded up to
-        32) and those of the largest scores, in their order; in place, or into
-        another Q8KVCache with scores.  Returns the kept blocks' old indexes
-        int32 [B, H, keep/32] (-1: none) and the new lengths (new_lens if
-        given, which may be seq_lens)."""
+        """Cut every sequence to at most `keep` / 32 blocks (`keep` a multiple of
+        32): its first `sinks` / 32 and newest `recent` / 32 blocks (both rounded
+        up, and one at least of the newest) and those of the largest scores, in
+        their order; in place, or into another Q8KVCache with scores.  The newest
+        block counts as one however few tokens it holds: recent = n + 31 keeps
+        the newest n tokens at every length.  Returns the kept blocks' old
+        indexes int32 [B, H, keep/32] (-1: none) and the new lengths (new_lens
+        if given, which may be seq_lens)."""
         to = self if into is None else into
         if self.scores is None or to.scores is None or to.fmt != self.fmt:
             raise ValueError("eviction needs scores, and caches of one format")

@@ -1,0 +1,56 @@
+"""The 8-bit cache object on the GPU: what its documents promise of the tokens
+that an eviction keeps, of swapped arrays and of query heads, with expectations
+from token positions and memory, not from the library's block rules."""
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+
+
+@pytest.fixture(scope="module")
+def dq():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2609_19880_amd as mod
+    return mod
+
+
+def _kept_tokens(kept, T):
+    """Old positions of the tokens that are left, from the list of kept blocks."""
+    return {t for blk in kept.tolist() if blk >= 0 for t in range(32 * blk, min(32 * blk + 32, T))}
+
+
+@pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 64, 65])
+def test_evict_keeps_the_newest_tokens_of_every_length(dq, n):
+    """recent = n + 31 keeps the newest n tokens, and recent = n, a multiple of
+    32, all but 31 of them at least, however full the newest block is; scores
+    that fall towards the newest tokens, the first ones' lowest."""
+    lens = list(range(257, 257 + 64))
+    B, t_cap, keep = len(lens), 384, 192
+    cache = dq.Q8KVCache(B, 1, 1, t_cap, scores=True)
+    falling = torch.arange(t_cap // 32, 0, -1, dtype=torch.float32, device=DEV)
+    falling[:2] = -1.0
+    seq = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    for recent, promised in ((n + 31, n), (n, n - 31)):
+        cache.scores.copy_(falling.expand(B, 1, -1))
+        into = dq.Q8KVCache(B, 1, 1, 256, scores=True)
+        kept, new_lens = cache.evict(seq, keep, 40, recent, into=into)
+        for b, T in enumerate(lens):
+            left = _kept_tokens(kept[b, 0], T)
+            assert left >= set(range(40)) and left >= set(range(T - max(1, promised), T)), (T, recent)
+            assert int(new_lens[b]) == len(left) <= keep
+
+
+def test_evict_of_a_barely_started_block(dq):
+    """Four blocks, the newest of one token, the newest but one with the least
+    weight: recent = 32 is that one token's block, recent = 63 the 32 newest tokens."""
+    cache = dq.Q8KVCache(1, 1, 1, 128, scores=True)
+    seq = torch.tensor([97], dtype=torch.int32, device=DEV)
+    for recent, want in ((32, [0, 3]), (63, [2, 3])):
+        cache.scores.copy_(torch.tensor([5.0, 1.0, 0.0, 9.0]).view(1, 1, 4))
+        into = dq.Q8KVCache(1, 1, 1, 128, scores=True)
+        kept, new_lens = cache.evict(seq, 64, 0, recent, into=into)
+        assert kept.tolist() == [[want]] and int(new_lens[0]) == 33
