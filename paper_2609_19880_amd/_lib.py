@@ -741,7 +741,6 @@ def _q8_lens(t, batch, dev, name="seq_lens"):
 
 
 def _q8_encode(fmt: int, cache, k, v, t0, status, stream):
-    _need(cache is not None, "the cache must be on one GPU")
     B, H, nb, dev, at = cache
     n, T = _q8_rows_args(k, v, H, dev)
     _need(n == B, "k and the cache must have the same batch")
@@ -787,7 +786,6 @@ def _q8_new_rows(batch, n, heads, dev, stream):
 
 
 def _q8_read(fmt: int, cache, t0, n, k, v, stream):
-    _need(cache is not None, "the cache must be on one GPU")
     B, H, nb, dev, at = cache
     _need(0 <= t0 <= _INT_MAX and 0 <= n <= _INT_MAX, "t0 and n")
     if k is None and v is None:
@@ -865,7 +863,6 @@ def _q8_sees(window, sinks):
 
 
 def _q8_partial(fmt: int, cache, q, seq_lens, workspace, window, sinks, extra_lens, softmax_scale, block_lse, stream):
-    _need(cache is not None, "the cache must be on one GPU")
     B, H, nb, dev, at = cache
     n, Hq = _q8_query(q, H, dev)
     _need(n == B, "q and the cache must have the same batch")
@@ -887,8 +884,6 @@ def dq_q8_decode_attention_partial(fmt, q, k_data, k_scale, v_data, v_scale, seq
 
 
 def _q8_attention(fmt: int, cache, q, seq_lens, out, workspace, window, sinks, softmax_scale, lse, sc, stream):
-    if cache is None:
-        raise ValueError("the cache must be on one GPU")
     B, H, nb, dev, at = cache
     on = q.get_device()          # (-1 off the GPU)
     if not (q.dtype is torch.bfloat16 and q.dim() == 3 and q.is_contiguous() and on == dev.index
@@ -1005,7 +1000,6 @@ def _q8_kept(kept, keep, first, last, batch, heads, dev):
 
 
 def _q8_evict(seq_lens, new_lens, keep, first, last, source, sc, to, tsc, kept, stream):
-    _need(source is not None and to is not None, "the cache must be on one GPU")
     B, H, nb, dev, at = source
     tB, tH, tnb, tdev, to_at = to
     _need(tB == B and tH == H and tdev == dev, "both caches must have the same batch, heads and GPU")

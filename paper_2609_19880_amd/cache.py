@@ -139,16 +139,29 @@ class Q8KVCache:
             self._scores = torch.zeros_like(self.k_scales)
             self._block_lse = torch.empty((batch, kv_heads, nb, q_heads // kv_heads), dtype=torch.float32,
                                           device=device)
-        self._locate()
+        self._checked = None
 
-    def _locate(self):
-        # sizes and addresses of the cache's own arrays, checked once
-        self._at = _lib._q8_cache_args(*self._arrays) if self.status.is_cuda else None
-        self._score_at, self._lse_at = (0 if x is None else x.data_ptr() for x in (self._scores, self._block_lse))
+    def __getstate__(self):
+        return {**self.__dict__, "_checked": None}      # a copy's arrays lie elsewhere
 
-    def __setstate__(self, state):
-        self.__dict__.update(state)
-        self._locate()               # a deep copy has arrays of its own
+    def _where(self):
+        """Sizes, GPU and addresses of the arrays as _lib._q8_cache_args gives
+        them, and the addresses of the two score arrays (0: none).  A tensor can
+        be given other memory (set_, .data), so every call asks where they lie
+        and how long they are; what has moved is checked anew."""
+        k, ks, v, vs = self._arrays
+        now = (k.data_ptr(), ks.data_ptr(), v.data_ptr(), vs.data_ptr(), k.nbytes, ks.nbytes, v.nbytes, vs.nbytes)
+        if self._scores is not None:
+            s, lse = self._scores, self._block_lse
+            now += (s.data_ptr(), lse.data_ptr(), s.nbytes, lse.nbytes)
+        if self._checked is None or self._checked[0] != now:
+            at = _lib._q8_cache_args(*self._arrays)
+            if at[:3] != (self.batch, self.kv_heads, self.t_cap // self.BLOCK):
+                raise ValueError("the cache's arrays must keep their shapes")
+            score_at, lse_at = _lib._q8_scores(self._scores, self._block_lse, *at[:3],
+                                               self.q_heads // self.kv_heads, at[3])
+            self._checked = now, at, score_at, lse_at
+        return self._checked[1:]
 
     @property
     def arrays(self):
@@ -185,32 +198,32 @@ class Q8KVCache:
         """Encode bf16 k, v [B, T_new, H, 128] as cache tokens [t0, t0 + T_new)
         (t0 a multiple of 32; a last block that is not full is completed with
         zeros).  The blocks' scores begin at 0."""
-        _lib._q8_encode(self._format, self._at, k, v, t0, self.status, None)
+        _lib._q8_encode(self._format, self._where()[0], k, v, t0, self.status, None)
         if self.scores is not None:
             self.scores[:, :, t0 // self.BLOCK:(t0 + k.shape[1] + self.BLOCK - 1) // self.BLOCK].zero_()
 
     def read(self, t0: int, n: int):
         """bf16 k, v [B, n, H, 128]: the values of tokens [t0, t0 + n)."""
-        return _lib._q8_read(self._format, self._at, t0, n, None, None, None)
+        return _lib._q8_read(self._format, self._where()[0], t0, n, None, None, None)
 
     def attend(self, q, seq_lens, out=None, softmax_scale=None, window: int = 0, sinks: int = 0, scores=None):
         """q bf16 [B, Hq, 128] -> out fp32 over the first seq_lens[b] tokens or,
         with a window, the first `sinks` and the newest `window` of them.  The
         cache's own scores grow by the blocks' weights, or the given ones."""
-        at = self._score_at
-        if at and (q.dim() != 3 or q.shape[1] != self.q_heads):
+        at, score_at, lse_at = self._where()
+        if score_at and (q.dim() != 3 or q.shape[1] != self.q_heads):
             raise ValueError("q must be [B, q_heads, 128]")
         if scores is not None:
             if self._scores is None:
                 raise ValueError("the cache was made without scores")
-            at, _ = _lib._q8_scores(scores, None, *self._at[:3], 1, self._at[3])
-        return _lib._q8_attention(self._format, self._at, q, seq_lens, out, self.workspace, window, sinks,
-                                  softmax_scale, self._lse_at, at, None)
+            score_at, _ = _lib._q8_scores(scores, None, *at[:3], 1, at[3])
+        return _lib._q8_attention(self._format, at, q, seq_lens, out, self.workspace, window, sinks, softmax_scale,
+                                  lse_at, score_at, None)
 
     def partial(self, q, seq_lens, softmax_scale=None, window: int = 0, sinks: int = 0, extra_lens=None):
         """Split-K partials of one decode step into the workspace (finish with
         merge; the scores' part of it with add_scores)."""
-        _lib._q8_partial(self._format, self._at, q, seq_lens, self.workspace, window, sinks, extra_lens,
+        _lib._q8_partial(self._format, self._where()[0], q, seq_lens, self.workspace, window, sinks, extra_lens,
                          softmax_scale, self.block_lse, None)
 
     def merge(self, seq_lens, out):
@@ -244,8 +257,10 @@ class Q8KVCache:
         if new_lens is None:
             new_lens = torch.empty_like(seq_lens)
         up = -self.BLOCK
-        _lib._q8_evict(seq_lens, new_lens, keep, sinks // up * up, max(recent // up * up, self.BLOCK), self._at,
-                       self._score_at, to._at, to._score_at, kept, None)
+        at, score_at, _ = self._where()
+        to_at, to_score_at, _ = to._where()
+        _lib._q8_evict(seq_lens, new_lens, keep, sinks // up * up, max(recent // up * up, self.BLOCK), at, score_at,
+                       to_at, to_score_at, kept, None)
         return kept, new_lens
 
     def cache_bytes(self, tokens: int) -> int:

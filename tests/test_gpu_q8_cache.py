@@ -54,3 +54,50 @@ def test_evict_of_a_barely_started_block(dq):
         into = dq.Q8KVCache(1, 1, 1, 128, scores=True)
         kept, new_lens = cache.evict(seq, 64, 0, recent, into=into)
         assert kept.tolist() == [[want]] and int(new_lens[0]) == 33
+
+
+def _random_cache(dq, seed, t_cap=384, heads=2, group=2):
+    g = torch.Generator().manual_seed(seed)
+    cache = dq.Q8KVCache(1, heads, heads * group, t_cap, scores=True)
+    k, v = (torch.randn((1, t_cap, heads, 128), generator=g).to(torch.bfloat16).to(DEV) for _ in range(2))
+    cache.append(k, v, 0)
+    q = torch.randn((1, heads * group, 128), generator=g).to(torch.bfloat16).to(DEV)
+    return cache, q
+
+
+def test_arrays_with_other_memory(dq):
+    """A cache whose arrays were given other memory works on that memory and
+    leaves the old one alone (which this test keeps, so no access can go astray)."""
+    a, q = _random_cache(dq, 1)
+    b, _ = _random_cache(dq, 2)
+    lens = torch.tensor([384], dtype=torch.int32, device=DEV)
+    want, want_rows = b.attend(q, lens), b.read(0, 100)
+    want_scores = b.scores.clone()
+    held = [x.data for x in (*a.arrays, a.scores, a.block_lse)]
+    before = [x.clone() for x in held]
+    for x, y in zip(a.arrays, b.arrays):
+        x.data = y.clone()
+    a.scores.data = torch.zeros_like(a.scores)
+    a.block_lse.data = torch.empty_like(a.block_lse)
+    assert torch.equal(a.attend(q, lens), want) and torch.equal(a.scores, want_scores)
+    assert all(torch.equal(x, y) for x, y in zip(a.read(0, 100), want_rows))
+    kept, _ = a.evict(lens, 128, 32, 32)
+    at = kept[0, 0].long()
+    assert torch.equal(a.k_data[0, 0, :4], b.k_data[0, 0][at])
+    assert all(torch.equal(x, y) for x, y in zip(held, before))
+
+
+def test_arrays_that_do_not_fit_are_refused(dq):
+    lens = torch.tensor([384], dtype=torch.int32, device=DEV)
+    for change in (lambda c: setattr(c.k_data, "data", c.k_data[:, :, :4].contiguous()),
+                   lambda c: setattr(c.v_scales, "data", c.v_scales.cpu()),
+                   lambda c: c.k_scales.set_(),
+                   lambda c: [setattr(x, "data", x[:, :, :8].contiguous()) for x in c.arrays],
+                   lambda c: setattr(c.scores, "data", c.scores[:, :1].contiguous())):
+        cache, q = _random_cache(dq, 3)
+        cache.attend(q, lens)
+        change(cache)
+        for call in (lambda: cache.attend(q, lens), lambda: cache.partial(q, lens), lambda: cache.read(0, 32),
+                     lambda: cache.evict(lens, 128)):
+            with pytest.raises(ValueError):
+                call()
