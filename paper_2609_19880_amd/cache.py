@@ -221,8 +221,14 @@ class Q8KVCache:
                                   lse_at, score_at, None)
 
     def partial(self, q, seq_lens, softmax_scale=None, window: int = 0, sinks: int = 0, extra_lens=None):
-        """Split-K partials of one decode step into the workspace (finish with
-        merge; the scores' part of it with add_scores)."""
+        """Split-K partials of one decode step over q bf16 [B, q_heads, 128] into
+        the workspace (finish with merge; the scores' part of it with
+        add_scores)."""
+        if q.dim() != 3 or q.shape[1] != self.q_heads:
+            raise ValueError("q must be [B, q_heads, 128]")      # merge takes the cache's head count
+        self._partial(q, seq_lens, softmax_scale, window, sinks, extra_lens)
+
+    def _partial(self, q, seq_lens, softmax_scale, window, sinks, extra_lens):
         _lib._q8_partial(self._format, self._where()[0], q, seq_lens, self.workspace, window, sinks, extra_lens,
                          softmax_scale, self.block_lse, None)
 
@@ -372,7 +378,7 @@ class StreamingKVCache:
         else:
             if window and window < self.r_cap:
                 raise ValueError("window must be 0 or at least r_cap")
-            c.partial(q, self.seq_lens, softmax_scale, window, sinks, self.res_lens)
+            c._partial(q, self.seq_lens, softmax_scale, window, sinks, self.res_lens)
             if c.scores is not None:
                 # the scores' weights need the raw tokens' partials in the workspace
                 _lib.dq_decode_attention_residual(q, self.res_k, self.res_v, self.seq_lens, self.res_lens, c.t_cap,

@@ -101,3 +101,29 @@ def test_arrays_that_do_not_fit_are_refused(dq):
                      lambda: cache.evict(lens, 128)):
             with pytest.raises(ValueError):
                 call()
+
+
+@pytest.mark.parametrize("scores", [False, True])
+def test_partials_of_other_query_heads_are_refused(dq, scores):
+    """merge reads the workspace by the cache's own head count."""
+    cache = dq.Q8KVCache(1, 2, 8, 256, scores=scores)
+    lens = torch.full((1,), 200, dtype=torch.int32, device=DEV)
+    for heads in (2, 4, 6, 16):
+        with pytest.raises(ValueError):
+            cache.partial(torch.zeros((1, heads, 128), dtype=torch.bfloat16, device=DEV), lens)
+    with pytest.raises(ValueError):
+        cache.partial(torch.zeros((8, 128), dtype=torch.bfloat16, device=DEV), lens)
+
+
+def test_a_streaming_step_of_fewer_query_heads(dq):
+    """Its merge goes by the query's own heads: the first heads of a wider step."""
+    g = torch.Generator().manual_seed(5)
+    c = dq.StreamingKVCache(1, 2, 8, 512, None, None, streams="int8")
+    k, v = (torch.randn((1, 400, 2, 128), generator=g).to(torch.bfloat16).to(DEV) for _ in range(2))
+    c.prefill(k, v)
+    q = torch.randn((1, 8, 128), generator=g).to(torch.bfloat16).to(DEV)
+    some = q.view(1, 2, 4, 128)[:, :, :2].reshape(1, 4, 128).contiguous()
+    want = c.attend(q).view(1, 2, 4, 128)[:, :, :2].reshape(1, 4, 128)
+    # other head counts cut the tokens otherwise: weights of 22 bits against other
+    # maxima (2 x 2^-22), sums of up to 13 blocks and 256 raw tokens: below 2^-15
+    assert ((c.attend(some) - want).norm(dim=2) <= want.norm(dim=2) * 2.0 ** -15).all()

@@ -1,0 +1,15 @@
+"""The 8-bit cache object's argument checks that need no GPU."""
+
+import pytest
+import torch
+
+dq = pytest.importorskip("paper_2609_19880_amd")
+
+
+@pytest.mark.parametrize("scores", [False, True])
+def test_partials_of_other_query_heads_are_refused(scores):
+    c = dq.Q8KVCache(1, 2, 8, 256, scores=scores, device="cpu")
+    lens = torch.zeros(1, dtype=torch.int32)
+    for shape in ((1, 4, 128), (1, 16, 128), (8, 128)):
+        with pytest.raises(ValueError, match="q_heads"):
+            c.partial(torch.zeros(shape, dtype=torch.bfloat16), lens)
