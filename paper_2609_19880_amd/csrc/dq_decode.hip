@@ -1478,7 +1478,7 @@ int launch_decode_symbols(const dq_tables* tab, const uint8_t* records, int64_t 
 size_t attention_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t t_cap, int32_t d) {
     (void)Hkv;
     const int64_t slots = ws_slots(B, Hq, t_cap);
-    return (size_t)kWsHeader + (size_t)(slots * d + 2 * slots) * sizeof(float);
+    return (size_t)kWsHeader + (size_t)(slots * d + 2 * slots + ws_blocks(B, Hq, t_cap)) * sizeof(float);
 }
 
 bool attention_supports(const dq_tables* tk, const dq_tables* tv) {

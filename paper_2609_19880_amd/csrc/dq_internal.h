@@ -20,12 +20,14 @@ constexpr int kBracketUnits = 40 * kLambdaSteps;  // hi - lo = 40 octaves
 // (per-token streams; the per-head and BF16 kernels take chunks of at least
 // kMinChunkHead).  Slots NC .. NC + kResSlots - 1 of each (sequence, query
 // head) hold the residual window's partials, one per workgroup of its split.
+// Behind them, for the 8-bit cache's block weights, fp32 [B][Hkv][t_cap / 32][Hq / Hkv].
 constexpr int kWsHeader = 256;
 constexpr int kMinChunk = 128;
 constexpr int kMinChunkHead = 256;
 constexpr int kResSlots = 4;
 inline int64_t max_chunks(int t_cap) { return (t_cap + kMinChunk - 1) / kMinChunk; }
 inline int64_t ws_slots(int B, int Hq, int t_cap) { return (int64_t)B * Hq * (max_chunks(t_cap) + kResSlots); }
+inline int64_t ws_blocks(int B, int Hq, int t_cap) { return (int64_t)B * Hq * (t_cap / DQ_Q8_BLOCK); }
 int cu_count();   // CUs of the current device
 
 // Where the records and key means of (sequence b, KV head h, token t) live.

@@ -488,6 +488,7 @@ struct Q8Args {
     float per_cu;                // just below 1 / CUs
     float scale_log2;
     float* lse;                  // [B][Hkv][t_cap / 32][G], or NULL
+    float* top;                  // with lse, of the same shape: what lse is relative to
     float* out;                  // one chunk: the step's result goes here, or NULL
     float* scores;               // with out
     int early;                   // blocks are requested before the length is known
@@ -895,7 +896,12 @@ __global__ __launch_bounds__(WAVES* kWave, 4) void q8_partial_kernel(Q8Args a) {
         if constexpr (TRACK) {
             float bs = ps + xor_lane<16>(ps, lane);
             bs += xor_lane<32>(bs, lane);
-            if (lane < G) a.lse[(((int64_t)b * a.Hkv + h) * nb_cap + blk) * G + lane] = log2f(bs) + m_run;
+            // (apart: their sum would lose the block's weight to a large maximum's last bit)
+            if (lane < G) {
+                const int64_t i = (((int64_t)b * a.Hkv + h) * nb_cap + blk) * G + lane;
+                a.lse[i] = log2f(bs);
+                a.top[i] = m_run;
+            }
         }
 
         // ---- weighted values
@@ -962,8 +968,8 @@ __global__ __launch_bounds__(WAVES* kWave, 4) void q8_partial_kernel(Q8Args a) {
     if constexpr (TRACK) {
         if (!a.scores) return;
         // the whole step is here: every block's weight (the barrier above orders
-        // the wavefronts' writes of lse)
-        float total[kGP];
+        // the wavefronts' writes of lse and top)
+        float top[kGP], total[kGP];
 #pragma unroll
         for (int g = 0; g < kGP; ++g) {
             float M = wm[0][g], l = 0.f;
@@ -971,14 +977,15 @@ __global__ __launch_bounds__(WAVES* kWave, 4) void q8_partial_kernel(Q8Args a) {
             for (int u = 1; u < WAVES; ++u) M = fmaxf(M, wm[u][g]);
 #pragma unroll
             for (int u = 0; u < WAVES; ++u) l = fmaf(wl[u][g], exp2f(wm[u][g] - M), l);
-            total[g] = l == 0.f ? INFINITY : M + log2f(l);
+            top[g] = l == 0.f ? INFINITY : M;
+            total[g] = log2f(l == 0.f ? 1.f : l);
         }
         for (int u = tid; u < vis.count; u += WAVES * kWave) {
             const int64_t i = ((int64_t)b * a.Hkv + h) * nb_cap + block_of(u);
             float w = 0.f;
 #pragma unroll
             for (int g = 0; g < kGP; ++g)
-                if (g < G) w += exp2f(a.lse[i * G + g] - total[g]);
+                if (g < G) w += exp2f((a.top[i * G + g] - top[g]) + (a.lse[i * G + g] - total[g]));
             a.scores[i] += w;
         }
     }
@@ -990,6 +997,7 @@ struct FinishArgs {
     const int32_t* seq_lens;
     const int32_t* extra_lens;
     const float* lse;
+    const float* top;
     const int32_t* ws_hdr;
     const float* ws_m;
     const float* ws_l;
@@ -1018,6 +1026,8 @@ constexpr int kMostChunks = 4 * kWave;       // (one wavefront has at most 32: m
 // results meet in LDS.  The others' wavefronts add block weights to the
 // scores: sum_g 2^(lse of the block - lse of the step), the latter from the
 // partials' maxima and sums (as many partials as lanes or fewer, in general).
+// Both logarithms come as a maximum and what is relative to it, and the maxima
+// are subtracted first: exact where a weight counts, however large the scores.
 template <int WAVES>
 __global__ __launch_bounds__(WAVES* kWave) void q8_finish_kernel(FinishArgs a) {
     __shared__ float wm[WAVES], wl[WAVES];
@@ -1131,7 +1141,7 @@ __global__ __launch_bounds__(WAVES* kWave) void q8_finish_kernel(FinishArgs a) {
     const int first = (((int)blockIdx.x - a.heads) * WAVES + wave) * kScoreBlocks;
     if (first >= vis.count) return;
     // the blocks' terms are requested beside the partials' maxima and sums
-    float term[kScoreBlocks / kWave][kGP], score[kScoreBlocks / kWave];
+    float term[kScoreBlocks / kWave][kGP], at_top[kScoreBlocks / kWave][kGP], score[kScoreBlocks / kWave];
     int64_t at[kScoreBlocks / kWave];
 #pragma unroll
     for (int r = 0; r < kScoreBlocks / kWave; ++r) {
@@ -1139,9 +1149,12 @@ __global__ __launch_bounds__(WAVES* kWave) void q8_finish_kernel(FinishArgs a) {
         at[r] = ((int64_t)b * a.Hkv + h) * (a.t_cap / kBlk) + (v < vis.head ? v : vis.from + v - vis.head);
         score[r] = a.scores[at[r]];
 #pragma unroll
-        for (int g = 0; g < kGP; ++g) term[r][g] = a.lse[at[r] * G + min(g, G - 1)];
+        for (int g = 0; g < kGP; ++g) {
+            term[r][g] = a.lse[at[r] * G + min(g, G - 1)];
+            at_top[r][g] = a.top[at[r] * G + min(g, G - 1)];
+        }
     }
-    float m[kGP], l[kGP], total[kGP];
+    float m[kGP], l[kGP], top[kGP], total[kGP];
 #pragma unroll
     for (int g = 0; g < kGP; ++g) {
         const bool in = g < G && lane < np;
@@ -1151,7 +1164,8 @@ __global__ __launch_bounds__(WAVES* kWave) void q8_finish_kernel(FinishArgs a) {
     }
 #pragma unroll
     for (int g = 0; g < kGP; ++g) {
-        total[g] = INFINITY;
+        top[g] = INFINITY;
+        total[g] = 0.f;
         if (g < G) {
             float M = m[g];
             for (int i = lane + kWave; i < np; i += kWave) M = fmaxf(M, a.ws_m[slot_of(g, i)]);
@@ -1160,7 +1174,8 @@ __global__ __launch_bounds__(WAVES* kWave) void q8_finish_kernel(FinishArgs a) {
                 float sum = l[g] * exp2f(m[g] - M);
                 for (int i = lane + kWave; i < np; i += kWave)
                     sum += a.ws_l[slot_of(g, i)] * exp2f(a.ws_m[slot_of(g, i)] - M);
-                total[g] = M + log2f(wave_sum(sum));
+                top[g] = M;
+                total[g] = log2f(wave_sum(sum));
             }
         }
     }
@@ -1169,7 +1184,7 @@ __global__ __launch_bounds__(WAVES* kWave) void q8_finish_kernel(FinishArgs a) {
         float w = 0.f;
 #pragma unroll
         for (int g = 0; g < kGP; ++g)
-            if (g < G) w += exp2f(term[r][g] - total[g]);
+            if (g < G) w += exp2f((at_top[r][g] - top[g]) + (term[r][g] - total[g]));
         if (first + r * kWave + lane < vis.count) a.scores[at[r]] = score[r] + w;
     }
 }
@@ -1681,6 +1696,7 @@ int launch_q8_partial(int format, const Pages& pg, const uint16_t* q, int32_t B,
     a.ws_acc = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + kWsHeader);
     a.ws_m = a.ws_acc + held * kD;
     a.ws_l = a.ws_m + held;
+    a.top = a.ws_l + held;
     const dim3 grid = plan.target ? dim3((unsigned)plan.items * Hkv) : dim3(plan.nchunks, Hkv, B);
     // Four wavefronts where a sequence has few blocks (up to 8: 8 KV heads of one of
     // 37 tokens 5.4 us against 5.7) or the pairs fill the CUs twice and more (up to
@@ -1707,6 +1723,7 @@ int launch_q8_finish(int32_t B, int32_t Hq, int32_t Hkv, const int32_t* seq_lens
     a.ws_acc = reinterpret_cast<const float*>(static_cast<const uint8_t*>(ws) + kWsHeader);
     a.ws_m = a.ws_acc + held * kD;
     a.ws_l = a.ws_m + held;
+    a.top = a.ws_l + held;
     a.out = out;
     a.scores = scores;
     a.Hq = Hq;

@@ -1,0 +1,118 @@
+"""Block weights of the 8-bit cache for scores of any size, from counts of tokens."""
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+
+
+@pytest.fixture(scope="module")
+def dq():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2609_19880_amd as mod
+    return mod
+
+
+# Two heads, q = +-2^bits in channel 0; keys 1 or 2 there and nothing else.  In a
+# block with both, codes are the same as in every other such block, so each of the
+# two scores is one number everywhere, and the lower one lies 2^(bits - 1) and more
+# below: no weight from bits = 9 on (2^-256).  The first head's weight is spread
+# evenly over the tokens with 2, the second's over those with 1: a block's is their
+# count over the count of all.
+# Rounded: log2 of the two counts (below 2^5 and 2^15, two units of 2^-20 each at
+# most), their difference (2^-21), 2^x (two units in the last place), the sums:
+# ln 2 (4 + 1/2) 2^-20 + 4 2^-24 < 2^-17, relative to each head's term.
+REL = 2.0 ** -17
+
+
+def _counts(blocks):
+    return 1 + (7 * np.arange(blocks)) % 31          # tokens with 1, 1..31 of 32
+
+
+def _cache(dq, fmt, blocks, t_cap, lens):
+    n = _counts(blocks)
+    one = np.arange(32)[None, :] < n[:, None]
+    k = torch.zeros((1, 32 * blocks, 1, 128), dtype=torch.bfloat16)
+    k[0, :, 0, 0] = torch.from_numpy(np.where(one, 1.0, 2.0).reshape(-1)).to(torch.bfloat16)
+    cache = dq.Q8KVCache(len(lens), 1, 2, t_cap, fmt, scores=True)
+    k = k.to(DEV).expand(len(lens), -1, -1, -1)
+    cache.append(k, k, 0)
+    return cache, torch.tensor(lens, dtype=torch.int32, device=DEV)
+
+
+def _weights(T, blocks):
+    """[blocks, 2]"""
+    n = _counts(blocks)
+    one = np.arange(32)[None, :] < n[:, None]
+    seen = np.arange(32 * blocks).reshape(blocks, 32) < T
+    c = np.stack([(~one & seen).sum(1), (one & seen).sum(1)], axis=1).astype(np.float64)
+    return c / c.sum(axis=0)
+
+
+def _check(scores, lens, blocks):
+    got = scores.double().cpu().numpy()[:, 0]
+    for b, T in enumerate(lens):
+        want = _weights(T, blocks).sum(axis=1)
+        assert np.max(np.abs(got[b, :blocks] - want) / np.maximum(want, 1e-30)) <= REL, (b, got[b, :4], want[:4])
+        assert abs(got[b].sum() - 2) <= 2 * REL and not got[b, blocks:].any()
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("bits", [9, 12, 16, 20, 23, 24, 30, 37, 60, 120])
+@pytest.mark.parametrize("blocks,t_cap,lens", [(16, 512, [512]), (16, 512, [512, 500]), (48, 2048, [1536, 1535]),
+                                               (256, 8192, [8192]), (50, 1664, [1600, 1597, 1599] * 30)])
+def test_weights_of_any_size_of_scores(dq, fmt, bits, blocks, t_cap, lens):
+    """The one-call step in one launch and in two, few sequences and many; its
+    partials with the scores alone, and with the merge."""
+    cache, seq = _cache(dq, fmt, blocks, t_cap, lens)
+    q = torch.zeros((len(lens), 2, 128), dtype=torch.bfloat16, device=DEV)
+    q[:, 0, 0], q[:, 1, 0] = 2.0 ** bits, -(2.0 ** bits)
+    out = cache.attend(q, seq, softmax_scale=1.0)
+    _check(cache.scores, lens, blocks)
+    cache.scores.zero_()
+    cache.partial(q, seq, softmax_scale=1.0)
+    cache.add_scores(seq)
+    _check(cache.scores, lens, blocks)
+    cache.scores.zero_()
+    both = torch.empty_like(out)
+    cache.merge_scores(seq, both)
+    _check(cache.scores, lens, blocks)
+    # the values are the keys: 2 and 1 (its code's value) in channel 0
+    assert torch.allclose(out[:, 0, 0], torch.full((len(lens),), 2.0, device=DEV), rtol=2.0 ** -20, atol=0)
+    assert torch.allclose(both, out, rtol=2.0 ** -20, atol=0)
+
+
+@pytest.mark.parametrize("bits", [9, 23, 37])
+def test_weights_of_any_size_beside_raw_tokens(dq, bits):
+    """A residual window with as large scores takes its share of the weight."""
+    blocks, r = 40, 100
+    cache, seq = _cache(dq, "e4m3", blocks, 1280, [1280])
+    q = torch.zeros((1, 2, 128), dtype=torch.bfloat16, device=DEV)
+    q[0, 0, 0], q[0, 1, 0] = 2.0 ** bits, -(2.0 ** bits)
+    ring = torch.zeros((1, 1, 256, 128), dtype=torch.bfloat16, device=DEV)
+    ring[..., 0] = 2.0
+    extra = torch.tensor([r], dtype=torch.int32, device=DEV)
+    cache.partial(q, seq, softmax_scale=1.0, extra_lens=extra)
+    dq.dq_decode_attention_residual(q, ring, ring, seq, extra, 1280, cache.workspace, softmax_scale=1.0)
+    cache.add_scores(seq, extra_lens=extra)
+    # The raw keys are 2 exactly, the cached ones 448 fl32(2 / 448), and either side's
+    # score, 2^(bits + 1) log2(e) in base 2, meets up to four factors of 1 + 2^-24 (the
+    # scale, its logarithm's, their product, the score): they lie up to
+    # 8 x 2^-24 x 2^(bits + 1.6) apart, a factor on the first head's share of the cached
+    # tokens (5e-4 at bits = 9) or, from 2^20 on, all or nothing.  How the blocks
+    # divide that share among them is as exact as without raw tokens.
+    share = _weights(1280, blocks)
+    twos = (32 - _counts(blocks)).sum()
+    got = cache.scores.double().cpu().numpy()[0, 0]
+    cached = got.sum() - 1.0
+    if bits < 20:
+        apart = 8 * 2.0 ** -24 * 2.0 ** (bits + 1.6) * np.log(2)
+        assert abs(cached * (twos + r) / twos - 1) <= apart + 2 * REL
+    else:
+        assert -2 * REL <= cached <= 1 + 2 * REL
+    want = share[:, 0] * cached + share[:, 1]
+    assert np.max(np.abs(got - want) / want) <= 3 * REL
