@@ -259,6 +259,8 @@ class Q8KVCache:
             raise ValueError("eviction needs scores, and caches of one format")
         if keep <= 0 or keep % self.BLOCK:
             raise ValueError("keep must be a positive multiple of 32")
+        if sinks < 0 or recent < 0:
+            raise ValueError("sinks and recent must not be negative")
         kept = self.status.new_empty((self.batch, self.kv_heads, keep // self.BLOCK))
         if new_lens is None:
             new_lens = torch.empty_like(seq_lens)
