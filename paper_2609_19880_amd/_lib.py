@@ -686,11 +686,14 @@ def _q8_format(fmt) -> int:
     return f
 
 
+_current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
+
 def _q8_stream(t, stream):
     """The raw stream to enqueue on; the tensors have to be on the current device."""
     dev = t.get_device()
-    _need(dev == torch._C._cuda_getDevice(), "tensors must be on the current device")
-    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else int(stream.cuda_stream)
+    _need(dev == _current_device(), "tensors must be on the current device")
+    return _current_stream(dev) if stream is None else int(stream.cuda_stream)
 
 
 def _q8_cache_args(k_data, k_scale, v_data, v_scale):
@@ -901,10 +904,15 @@ def _q8_attention(fmt: int, cache, q, seq_lens, out, workspace, window, sinks, s
     else:
         _need(out.dtype == torch.float32 and out.shape == q.shape and out.is_contiguous() and out.device == dev,
               "out must be fp32 of q's shape")
+    # (_q8_stream, but for the calls it takes)
+    if stream is None and on == _current_device():
+        raw = _current_stream(on)
+    else:
+        raw = _q8_stream(q, stream)
     rc = _lib.dq_q8_decode_attention(
         fmt, q.data_ptr(), B, Hq, H, *at, seq_lens.data_ptr(), nb * DQ_Q8_BLOCK, window, sinks,
         _RSQRT_D if softmax_scale is None else softmax_scale, out.data_ptr(), lse, sc, workspace.data_ptr(),
-        workspace.nbytes, _q8_stream(q, stream))
+        workspace.nbytes, raw)
     if rc:
         _check(rc, "dq_q8_decode_attention")
     return out

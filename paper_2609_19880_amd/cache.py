@@ -154,14 +154,15 @@ class Q8KVCache:
         if self._scores is not None:
             s, lse = self._scores, self._block_lse
             now += (s.data_ptr(), lse.data_ptr(), s.nbytes, lse.nbytes)
-        if self._checked is None or self._checked[0] != now:
+        checked = self._checked
+        if checked is None or checked[0] != now:
             at = _lib._q8_cache_args(*self._arrays)
             if at[:3] != (self.batch, self.kv_heads, self.t_cap // self.BLOCK):
                 raise ValueError("the cache's arrays must keep their shapes")
             score_at, lse_at = _lib._q8_scores(self._scores, self._block_lse, *at[:3],
                                                self.q_heads // self.kv_heads, at[3])
-            self._checked = now, at, score_at, lse_at
-        return self._checked[1:]
+            self._checked = checked = now, (at, score_at, lse_at)
+        return checked[1]
 
     @property
     def arrays(self):
