@@ -689,11 +689,11 @@ def _q8_format(fmt) -> int:
 _current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
 
-def _q8_stream(t, stream):
-    """The raw stream to enqueue on; the tensors have to be on the current device."""
-    dev = t.get_device()
-    _need(dev == _current_device(), "tensors must be on the current device")
-    return _current_stream(dev) if stream is None else int(stream.cuda_stream)
+def _q8_stream(index, stream):
+    """The raw stream to enqueue on; the tensors' device has to be the current one."""
+    if index != _current_device():
+        raise ValueError("tensors must be on the current device")
+    return _current_stream(index) if stream is None else int(stream.cuda_stream)
 
 
 def _q8_cache_args(k_data, k_scale, v_data, v_scale):
@@ -746,11 +746,12 @@ def _q8_lens(t, batch, dev, name="seq_lens"):
 def _q8_encode(fmt: int, cache, k, v, t0, status, stream):
     B, H, nb, dev, at = cache
     n, T = _q8_rows_args(k, v, H, dev)
-    _need(n == B, "k and the cache must have the same batch")
-    _need(0 <= t0 <= _INT_MAX, "t0")
+    if n != B or not 0 <= t0 <= _INT_MAX:
+        raise ValueError("k and the cache must have the same batch; t0")
     rc = _lib.dq_q8_encode_kv(fmt, k.data_ptr(), *k.stride()[:3], v.data_ptr(), *v.stride()[:3], B, H, t0, T,
-                              nb * DQ_Q8_BLOCK, *at, _q8_status(status, dev), _q8_stream(k, stream))
-    _check(rc, "dq_q8_encode_kv")
+                              nb * DQ_Q8_BLOCK, *at, _q8_status(status, dev), _q8_stream(dev.index, stream))
+    if rc:
+        _check(rc, "dq_q8_encode_kv")
 
 
 def dq_q8_encode_kv(fmt, k, v, t0: int, k_data, k_scale, v_data, v_scale, status=None, stream=None):
@@ -771,7 +772,7 @@ def dq_q8_encode_kv_paged(fmt, k, v, t0: int, block_table, k_pool, k_scale_pool,
     max_pages = _q8_table(block_table, B, dev)
     rc = _lib.dq_q8_encode_kv_paged(f, k.data_ptr(), *k.stride()[:3], v.data_ptr(), *v.stride()[:3], B, H, t0, T,
                                     block_table.data_ptr(), max_pages, bpp * DQ_Q8_BLOCK, num_pages, *at,
-                                    _q8_status(status, dev), _q8_stream(k, stream))
+                                    _q8_status(status, dev), _q8_stream(dev.index, stream))
     _check(rc, "dq_q8_encode_kv_paged")
 
 
@@ -790,7 +791,8 @@ def _q8_new_rows(batch, n, heads, dev, stream):
 
 def _q8_read(fmt: int, cache, t0, n, k, v, stream):
     B, H, nb, dev, at = cache
-    _need(0 <= t0 <= _INT_MAX and 0 <= n <= _INT_MAX, "t0 and n")
+    if not (0 <= t0 <= _INT_MAX and 0 <= n <= _INT_MAX):
+        raise ValueError("t0 and n")
     if k is None and v is None:
         k, v = _q8_new_rows(B, n, H, dev, stream)
         sb, st = n * H * 128, H * 128
@@ -799,7 +801,7 @@ def _q8_read(fmt: int, cache, t0, n, k, v, stream):
         _q8_out_rows(k, v, B, n, H, dev)
         ks, vs = k.stride()[:3], v.stride()[:3]
     rc = _lib.dq_q8_decode_kv(fmt, *at, B, H, t0, n, nb * DQ_Q8_BLOCK, k.data_ptr(), *ks, v.data_ptr(), *vs,
-                              _q8_stream(k, stream))
+                              _q8_stream(dev.index, stream))
     if rc:
         _check(rc, "dq_q8_decode_kv")
     return k, v
@@ -823,7 +825,7 @@ def dq_q8_decode_kv_paged(fmt, k_pool, k_scale_pool, v_pool, v_scale_pool, block
     _q8_out_rows(k, v, B, n, H, dev)
     rc = _lib.dq_q8_decode_kv_paged(f, *at, B, H, t0, n, block_table.data_ptr(), max_pages, bpp * DQ_Q8_BLOCK,
                                     num_pages, k.data_ptr(), *k.stride()[:3], v.data_ptr(), *v.stride()[:3],
-                                    _q8_status(status, dev), _q8_stream(k, stream))
+                                    _q8_status(status, dev), _q8_stream(dev.index, stream))
     _check(rc, "dq_q8_decode_kv_paged")
     return k, v
 
@@ -874,7 +876,7 @@ def _q8_partial(fmt: int, cache, q, seq_lens, workspace, window, sinks, extra_le
     rc = _lib.dq_q8_decode_attention_partial(
         fmt, q.data_ptr(), B, Hq, H, *at, _q8_lens(seq_lens, B, dev), extra, nb * DQ_Q8_BLOCK,
         *_q8_sees(window, sinks), _RSQRT_D if softmax_scale is None else softmax_scale, lse,
-        *_q8_workspace(workspace, dev), _q8_stream(q, stream))
+        *_q8_workspace(workspace, dev), _q8_stream(dev.index, stream))
     _check(rc, "dq_q8_decode_attention_partial")
 
 
@@ -904,15 +906,10 @@ def _q8_attention(fmt: int, cache, q, seq_lens, out, workspace, window, sinks, s
     else:
         _need(out.dtype == torch.float32 and out.shape == q.shape and out.is_contiguous() and out.device == dev,
               "out must be fp32 of q's shape")
-    # (_q8_stream, but for the calls it takes)
-    if stream is None and on == _current_device():
-        raw = _current_stream(on)
-    else:
-        raw = _q8_stream(q, stream)
     rc = _lib.dq_q8_decode_attention(
         fmt, q.data_ptr(), B, Hq, H, *at, seq_lens.data_ptr(), nb * DQ_Q8_BLOCK, window, sinks,
         _RSQRT_D if softmax_scale is None else softmax_scale, out.data_ptr(), lse, sc, workspace.data_ptr(),
-        workspace.nbytes, raw)
+        workspace.nbytes, _q8_stream(on, stream))
     if rc:
         _check(rc, "dq_q8_decode_attention")
     return out
@@ -947,7 +944,7 @@ def dq_q8_decode_attention_paged_partial(fmt, q, k_pool, k_scale_pool, v_pool, v
         f, q.data_ptr(), B, Hq, H, *at, block_table.data_ptr(), max_pages, bpp * DQ_Q8_BLOCK, num_pages,
         _q8_lens(seq_lens, B, dev), extra, *_q8_sees(window, sinks),
         _RSQRT_D if softmax_scale is None else softmax_scale, lse, *_q8_workspace(workspace, dev),
-        _q8_status(status, dev), _q8_stream(q, stream))
+        _q8_status(status, dev), _q8_stream(dev.index, stream))
     _check(rc, "dq_q8_decode_attention_paged_partial")
 
 
@@ -964,7 +961,8 @@ def dq_q8_decode_attention_paged(fmt, q, k_pool, k_scale_pool, v_pool, v_scale_p
     rc = _lib.dq_q8_decode_attention_paged(
         f, q.data_ptr(), B, Hq, H, *at, block_table.data_ptr(), max_pages, bpp * DQ_Q8_BLOCK, num_pages,
         _q8_lens(seq_lens, B, dev), *_q8_sees(window, sinks), _RSQRT_D if softmax_scale is None else softmax_scale,
-        _q8_out(out, q), lse, sc, *_q8_workspace(workspace, dev), _q8_status(status, dev), _q8_stream(q, stream))
+        _q8_out(out, q), lse, sc, *_q8_workspace(workspace, dev), _q8_status(status, dev),
+        _q8_stream(dev.index, stream))
     _check(rc, "dq_q8_decode_attention_paged")
 
 
@@ -979,7 +977,7 @@ def dq_q8_add_scores(q_heads: int, seq_lens, block_lse, workspace, scores, windo
     lens = _q8_lens(seq_lens, B, scores.device)
     extra = 0 if extra_lens is None else _q8_lens(extra_lens, B, scores.device, "extra_lens")
     rc = _lib.dq_q8_add_scores(B, q_heads, H, lens, extra, nb * DQ_Q8_BLOCK, *_q8_sees(window, sinks), lse,
-                               *_q8_workspace(workspace, scores.device), sc, _q8_stream(scores, stream))
+                               *_q8_workspace(workspace, scores.device), sc, _q8_stream(scores.device.index, stream))
     _check(rc, "dq_q8_add_scores")
 
 
@@ -996,7 +994,7 @@ def dq_q8_merge_scores(q_heads: int, seq_lens, block_lse, workspace, out, scores
     extra = 0 if extra_lens is None else _q8_lens(extra_lens, B, dev, "extra_lens")
     rc = _lib.dq_q8_merge_scores(B, q_heads, H, _q8_lens(seq_lens, B, dev), extra, nb * DQ_Q8_BLOCK,
                                  *_q8_sees(window, sinks), lse, *_q8_workspace(workspace, dev), out.data_ptr(), sc,
-                                 _q8_stream(scores, stream))
+                                 _q8_stream(scores.device.index, stream))
     _check(rc, "dq_q8_merge_scores")
 
 
@@ -1013,7 +1011,7 @@ def _q8_evict(seq_lens, new_lens, keep, first, last, source, sc, to, tsc, kept, 
     _need(tB == B and tH == H and tdev == dev, "both caches must have the same batch, heads and GPU")
     rc = _lib.dq_q8_evict(B, H, _q8_lens(seq_lens, B, dev), _q8_lens(new_lens, B, dev, "new_lens"), nb * DQ_Q8_BLOCK,
                           tnb * DQ_Q8_BLOCK, keep, first, last, *at, sc, *to_at, tsc,
-                          _q8_kept(kept, keep, first, last, B, H, dev), _q8_stream(kept, stream))
+                          _q8_kept(kept, keep, first, last, B, H, dev), _q8_stream(dev.index, stream))
     _check(rc, "dq_q8_evict")
 
 
@@ -1040,7 +1038,7 @@ def dq_q8_evict_paged(seq_lens, new_lens, keep: int, first: int, last: int, bloc
     rc = _lib.dq_q8_evict_paged(B, H, _q8_lens(seq_lens, B, dev), _q8_lens(new_lens, B, dev, "new_lens"), keep, first,
                                 last, block_table.data_ptr(), max_pages, bpp * DQ_Q8_BLOCK, num_pages, *at, sc,
                                 _q8_kept(kept, keep, first, last, B, H, dev), _q8_status(status, dev),
-                                _q8_stream(kept, stream))
+                                _q8_stream(dev.index, stream))
     _check(rc, "dq_q8_evict_paged")
 
 
