@@ -507,7 +507,9 @@ int dq_q8_decode_kv_paged(int32_t format, const uint8_t* k_pool, const float* k_
  *       holds.  Other entries are left alone.
  *   workspace: dq_decode_workspace_bytes(...) bytes, 16-byte aligned
  * A sequence with no visible token gives zeros; a query head with an infinity
- * or NaN gives NaN, in its KV head's scores too.
+ * or NaN gives NaN, in its KV head's scores too.  Weighted values are summed in
+ * fp32 before they are divided by the sum of the weights, so values larger than
+ * 2^127 over the number of visible tokens can give infinities.
  * dq_q8_decode_attention_partial writes split-K partials into the workspace;
  * finish it with dq_decode_attention_merge, with dq_decode_attention_residual
  * and dq_decode_attention_merge, or with dq_decode_attention_merge_residual.
@@ -524,7 +526,9 @@ int dq_q8_decode_kv_paged(int32_t format, const uint8_t* k_pool, const float* k_
  * workspace, summed over its tokens and the query heads of KV head h.  The
  * arguments are those of the step.  The step has to be one of the _partial
  * calls: dq_q8_decode_attention, which may finish without the workspace, adds
- * to the scores by itself.
+ * to the scores by itself.  A score holds the weight of the steps that added to
+ * it: none of the attention of a prompt, and none of the steps in which the
+ * block's tokens were still raw ones of a residual window.
  * dq_q8_merge_scores: dq_decode_attention_merge and dq_q8_add_scores of such a
  * step in one launch.
  */
@@ -566,9 +570,10 @@ int dq_q8_merge_scores(int32_t batch, int32_t q_heads, int32_t kv_heads, const i
  * Eviction by accumulated attention weight.  Every (sequence, KV head) that
  * holds more than keep / 32 blocks keeps its first `first` / 32 and its newest
  * `last` / 32 blocks and, of the others, those with the largest scores (of
- * equal ones the lower block; NaN counts as the smallest): keep / 32 blocks in
- * all, in their order.  Codes, scales and scores move to their new places
- * unchanged; shorter sequences keep everything.
+ * equal ones the lower block, so that before the first step with scores the
+ * oldest stay; NaN counts as the smallest): keep / 32 blocks in all, in their
+ * order.  Codes, scales and scores move to their new places unchanged; shorter
+ * sequences keep everything.
  *   keep, first, last: whole blocks, counted as 32 tokens each; first >= 0,
  *       last >= 32, first + last <= keep <= to_cap.  The newest block counts as
  *       one of the last / 32 however few tokens it holds, so between last - 31

@@ -115,7 +115,9 @@ class Q8KVCache:
 
     scores=True also keeps every block's accumulated attention weight
     (``scores`` fp32 [B, H, t_cap/32]), which ``attend`` adds to and ``evict``
-    goes by."""
+    goes by.  It is the weight since the block was encoded: a prompt's attention
+    and the steps in which its tokens were raw do not count, and before the
+    first step all scores are 0, of which ``evict`` keeps the oldest."""
 
     BLOCK = _lib.DQ_Q8_BLOCK
 
@@ -395,9 +397,10 @@ class StreamingKVCache:
     def evict(self, keep: int, sinks: int = 0, recent: int = 32):
         """Cut the compressed side to `keep` tokens and up to r_cap - 1 more (the
         ring's slots go by its length, so whole rings of tokens leave): of every
-        sequence and KV head the blocks with the least attention weight so far,
-        the first `sinks` and newest `recent` compressed tokens apart.  Returns
-        the kept blocks' old indexes, or None if nothing had to go."""
+        sequence and KV head the blocks with the least attention weight since
+        they left the ring, the first `sinks` and newest `recent` compressed
+        tokens apart.  Returns the kept blocks' old indexes, or None if nothing
+        had to go."""
         if self.streams not in _lib.Q8_FORMATS:
             raise ValueError("eviction needs 8-bit streams")
         gone = (self.n_comp - keep) // self.r_cap * self.r_cap

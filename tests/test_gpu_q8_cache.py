@@ -127,3 +127,26 @@ def test_a_streaming_step_of_fewer_query_heads(dq):
     # other head counts cut the tokens otherwise: weights of 22 bits against other
     # maxima (2 x 2^-22), sums of up to 13 blocks and 256 raw tokens: below 2^-15
     assert ((c.attend(some) - want).norm(dim=2) <= want.norm(dim=2) * 2.0 ** -15).all()
+
+
+def test_what_a_streaming_cache_s_scores_count(dq):
+    """Nothing of a prompt, nothing of a block's steps in the ring, all of its
+    steps since; without a step an eviction keeps the oldest blocks."""
+    g = torch.Generator().manual_seed(6)
+    c = dq.StreamingKVCache(1, 2, 4, 1024, None, None, streams="int8", scores=True)
+    k, v = (torch.randn((1, 1024, 2, 128), generator=g).to(torch.bfloat16).to(DEV) for _ in range(2))
+    q = torch.randn((1, 4, 128), generator=g).to(torch.bfloat16).to(DEV)
+    c.prefill(k[:, :768], v[:, :768])                       # 640 encoded, 128 raw
+    assert c.n_comp == 640 and not c.cache.scores.any()
+    c.attend(q)
+    first = c.cache.scores.clone()
+    assert (first[:, :, :20] > 0).all() and not first[:, :, 20:].any()
+    for t in range(768, 896):
+        c.append(k[:, t].contiguous(), v[:, t].contiguous())
+    assert c.n_comp == 768 and torch.equal(c.cache.scores, first)      # tokens 640..767: in the ring until now
+    c.attend(q)
+    assert (c.cache.scores[:, :, 20:24] > 0).all()
+    fresh = dq.StreamingKVCache(1, 2, 4, 1024, None, None, streams="int8", scores=True)
+    fresh.prefill(k[:, :768], v[:, :768])
+    kept = fresh.evict(384, 32, 64)
+    assert kept.tolist() == [[[*range(10), 18, 19]] * 2]
