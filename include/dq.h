@@ -502,9 +502,9 @@ int dq_q8_decode_kv_paged(int32_t format, const uint8_t* k_pool, const float* k_
  *       tokens are counted back from their end.  The residual window itself is
  *       always attended to whole, so with it window should be at least r_cap.
  *   block_lse: fp32 [batch][kv_heads][t_cap / 32][q_heads / kv_heads] or NULL:
- *       receives, for dq_q8_add_scores, the base-2 logarithm of each visible
- *       block's sum of exponentials, relative to a maximum that the workspace
- *       holds.  Other entries are left alone.
+ *       receives the base-2 logarithm of each visible block's sum of
+ *       exponentials, for dq_q8_add_scores (what its rounding to fp32 leaves is
+ *       kept in the workspace).  Other entries are left alone.
  *   workspace: dq_decode_workspace_bytes(...) bytes, 16-byte aligned
  * A sequence with no visible token gives zeros; a query head with an infinity
  * or NaN gives NaN, in its KV head's scores too.  Weighted values are summed in

@@ -488,7 +488,7 @@ struct Q8Args {
     float per_cu;                // just below 1 / CUs
     float scale_log2;
     float* lse;                  // [B][Hkv][t_cap / 32][G], or NULL
-    float* top;                  // with lse, of the same shape: what lse is relative to
+    float* lse_rest;             // with lse, of the same shape: what its rounding left
     float* out;                  // one chunk: the step's result goes here, or NULL
     float* scores;               // with out
     int early;                   // blocks are requested before the length is known
@@ -896,11 +896,13 @@ __global__ __launch_bounds__(WAVES* kWave, 4) void q8_partial_kernel(Q8Args a) {
         if constexpr (TRACK) {
             float bs = ps + xor_lane<16>(ps, lane);
             bs += xor_lane<32>(bs, lane);
-            // (apart: their sum would lose the block's weight to a large maximum's last bit)
+            // the maximum and the logarithm as a rounded sum and what the rounding left,
+            // which is the block's weight where the maximum is large (Knuth's two-sum)
             if (lane < G) {
                 const int64_t i = (((int64_t)b * a.Hkv + h) * nb_cap + blk) * G + lane;
-                a.lse[i] = log2f(bs);
-                a.top[i] = m_run;
+                const float lg = log2f(bs), sum = m_run + lg, of_lg = sum - m_run;
+                a.lse[i] = sum;
+                a.lse_rest[i] = bs == 0.f ? 0.f : (m_run - (sum - of_lg)) + (lg - of_lg);
             }
         }
 
@@ -968,7 +970,7 @@ __global__ __launch_bounds__(WAVES* kWave, 4) void q8_partial_kernel(Q8Args a) {
     if constexpr (TRACK) {
         if (!a.scores) return;
         // the whole step is here: every block's weight (the barrier above orders
-        // the wavefronts' writes of lse and top)
+        // the wavefronts' writes of lse and lse_rest)
         float top[kGP], total[kGP];
 #pragma unroll
         for (int g = 0; g < kGP; ++g) {
@@ -985,7 +987,7 @@ __global__ __launch_bounds__(WAVES* kWave, 4) void q8_partial_kernel(Q8Args a) {
             float w = 0.f;
 #pragma unroll
             for (int g = 0; g < kGP; ++g)
-                if (g < G) w += exp2f((a.top[i * G + g] - top[g]) + (a.lse[i * G + g] - total[g]));
+                if (g < G) w += exp2f((a.lse[i * G + g] - top[g]) + (a.lse_rest[i * G + g] - total[g]));
             a.scores[i] += w;
         }
     }
@@ -997,7 +999,7 @@ struct FinishArgs {
     const int32_t* seq_lens;
     const int32_t* extra_lens;
     const float* lse;
-    const float* top;
+    const float* lse_rest;
     const int32_t* ws_hdr;
     const float* ws_m;
     const float* ws_l;
@@ -1026,8 +1028,8 @@ constexpr int kMostChunks = 4 * kWave;       // (one wavefront has at most 32: m
 // results meet in LDS.  The others' wavefronts add block weights to the
 // scores: sum_g 2^(lse of the block - lse of the step), the latter from the
 // partials' maxima and sums (as many partials as lanes or fewer, in general).
-// Both logarithms come as a maximum and what is relative to it, and the maxima
-// are subtracted first: exact where a weight counts, however large the scores.
+// Both logarithms come in two parts, a large and a small one, and the large
+// ones are subtracted first: exact where a weight counts, however large the scores.
 template <int WAVES>
 __global__ __launch_bounds__(WAVES* kWave) void q8_finish_kernel(FinishArgs a) {
     __shared__ float wm[WAVES], wl[WAVES];
@@ -1141,7 +1143,7 @@ __global__ __launch_bounds__(WAVES* kWave) void q8_finish_kernel(FinishArgs a) {
     const int first = (((int)blockIdx.x - a.heads) * WAVES + wave) * kScoreBlocks;
     if (first >= vis.count) return;
     // the blocks' terms are requested beside the partials' maxima and sums
-    float term[kScoreBlocks / kWave][kGP], at_top[kScoreBlocks / kWave][kGP], score[kScoreBlocks / kWave];
+    float term[kScoreBlocks / kWave][kGP], rest[kScoreBlocks / kWave][kGP], score[kScoreBlocks / kWave];
     int64_t at[kScoreBlocks / kWave];
 #pragma unroll
     for (int r = 0; r < kScoreBlocks / kWave; ++r) {
@@ -1151,7 +1153,7 @@ __global__ __launch_bounds__(WAVES* kWave) void q8_finish_kernel(FinishArgs a) {
 #pragma unroll
         for (int g = 0; g < kGP; ++g) {
             term[r][g] = a.lse[at[r] * G + min(g, G - 1)];
-            at_top[r][g] = a.top[at[r] * G + min(g, G - 1)];
+            rest[r][g] = a.lse_rest[at[r] * G + min(g, G - 1)];
         }
     }
     float m[kGP], l[kGP], top[kGP], total[kGP];
@@ -1184,7 +1186,7 @@ __global__ __launch_bounds__(WAVES* kWave) void q8_finish_kernel(FinishArgs a) {
         float w = 0.f;
 #pragma unroll
         for (int g = 0; g < kGP; ++g)
-            if (g < G) w += exp2f((at_top[r][g] - top[g]) + (term[r][g] - total[g]));
+            if (g < G) w += exp2f((term[r][g] - top[g]) + (rest[r][g] - total[g]));
         if (first + r * kWave + lane < vis.count) a.scores[at[r]] = score[r] + w;
     }
 }
@@ -1696,7 +1698,7 @@ int launch_q8_partial(int format, const Pages& pg, const uint16_t* q, int32_t B,
     a.ws_acc = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + kWsHeader);
     a.ws_m = a.ws_acc + held * kD;
     a.ws_l = a.ws_m + held;
-    a.top = a.ws_l + held;
+    a.lse_rest = a.ws_l + held;
     const dim3 grid = plan.target ? dim3((unsigned)plan.items * Hkv) : dim3(plan.nchunks, Hkv, B);
     // Four wavefronts where a sequence has few blocks (up to 8: 8 KV heads of one of
     // 37 tokens 5.4 us against 5.7) or the pairs fill the CUs twice and more (up to
@@ -1723,7 +1725,7 @@ int launch_q8_finish(int32_t B, int32_t Hq, int32_t Hkv, const int32_t* seq_lens
     a.ws_acc = reinterpret_cast<const float*>(static_cast<const uint8_t*>(ws) + kWsHeader);
     a.ws_m = a.ws_acc + held * kD;
     a.ws_l = a.ws_m + held;
-    a.top = a.ws_l + held;
+    a.lse_rest = a.ws_l + held;
     a.out = out;
     a.scores = scores;
     a.Hq = Hq;

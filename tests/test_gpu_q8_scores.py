@@ -116,3 +116,23 @@ def test_weights_of_any_size_beside_raw_tokens(dq, bits):
         assert -2 * REL <= cached <= 1 + 2 * REL
     want = share[:, 0] * cached + share[:, 1]
     assert np.max(np.abs(got - want) / want) <= 3 * REL
+
+
+@pytest.mark.parametrize("bits", [2, 12, 30, 120])
+def test_block_lse_is_the_blocks_log_sum_exp(dq, bits):
+    """Rounded to fp32: the two heads' tokens of a block (5 or 27 and the like) at
+    2^(bits + 1) and -2^bits (times log2 e), the others 2^bits below."""
+    cache, seq = _cache(dq, "e4m3", 16, 512, [512])
+    q = torch.zeros((1, 2, 128), dtype=torch.bfloat16, device=DEV)
+    q[0, 0, 0], q[0, 1, 0] = 2.0 ** bits, -(2.0 ** bits)
+    cache.attend(q, seq, softmax_scale=1.0)
+    got = cache.block_lse[0, 0].double().cpu().numpy()
+    n = _counts(16)
+    two, one = 448 * float(np.float32(2 / 448)), 224 * float(np.float32(2 / 448))
+    for j in range(16):
+        for i, (top, low, many, few) in enumerate(((two, one, 32 - n[j], n[j]), (-one, -two, n[j], 32 - n[j]))):
+            want = top * 2.0 ** bits * np.log2(np.e) + np.log2(many + few * np.exp((low - top) * 2.0 ** bits))
+            # a score's four factors and its sum are rounded; the exponentials, their
+            # sum and its logarithm meet two units each of numbers below 2^5; the result
+            most = max(abs(top), abs(low)) * 2.0 ** (bits + 0.53)
+            assert abs(got[j, i] - want) <= 5 * 2.0 ** -24 * most + 6 * 2.0 ** -19 + abs(want) * 2.0 ** -24
