@@ -971,7 +971,7 @@ def dq_q8_add_scores(q_heads: int, seq_lens, block_lse, workspace, scores, windo
     """scores fp32 [B, H, t_cap/32] grow by the attention weight of every block
     in the step whose partials and block_lse are given (after
     dq_decode_attention_residual, if the step has a residual window)."""
-    _need(scores.dim() == 3, "scores must be fp32 [B, H, t_cap/32]")
+    _need(scores is not None and scores.dim() == 3, "scores must be fp32 [B, H, t_cap/32]")
     B, H, nb = scores.shape
     sc, lse = _q8_scores(scores, block_lse, B, H, nb, q_heads // H, scores.device)
     lens = _q8_lens(seq_lens, B, scores.device)
@@ -985,7 +985,7 @@ def dq_q8_merge_scores(q_heads: int, seq_lens, block_lse, workspace, out, scores
                        extra_lens=None, stream=None):
     """dq_decode_attention_merge (out fp32 [B, Hq, 128]) and dq_q8_add_scores in
     one launch."""
-    _need(scores.dim() == 3, "scores must be fp32 [B, H, t_cap/32]")
+    _need(scores is not None and scores.dim() == 3, "scores must be fp32 [B, H, t_cap/32]")
     B, H, nb = scores.shape
     dev = scores.device
     sc, lse = _q8_scores(scores, block_lse, B, H, nb, q_heads // H, dev)
