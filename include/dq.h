@@ -603,6 +603,138 @@ int dq_q8_evict_paged(int32_t batch, int32_t kv_heads, const int32_t* seq_lens, 
                       void* stream);
 
 /*
+ * Rotary positions.  Pair i of a head's first `rotary_dim` channels, (a, b), at
+ * position p becomes
+ *   (a cos x - b sin x, a sin x + b cos x) magnitude,   x = p freq[i],
+ * where the pairs are (i, i + rotary_dim / 2) (DQ_ROPE_HALF) or (2 i, 2 i + 1)
+ * (DQ_ROPE_INTERLEAVED); the channels from rotary_dim on stay as they are.  Keys
+ * are rotated before they are appended to a cache, queries before they attend.
+ * transposed = 1 changes the sign of x: the transposed map, which gives the
+ * gradient of the inputs from that of the outputs and, with magnitude 1, turns
+ * rotated vectors back.
+ *
+ * dq_rope_frequencies: host only.  freq fp64 [rotary_dim / 2] receives the angles
+ *   per token, *magnitude the factor of the rotated values.  With
+ *   f_i = base^(-2 i / rotary_dim):
+ *   DQ_ROPE_NONE    f_i
+ *   DQ_ROPE_LINEAR  f_i / factor
+ *   DQ_ROPE_NTK     the same with base factor^(rotary_dim / (rotary_dim - 2)) in
+ *                   base's place (rotary_dim > 2)
+ *   DQ_ROPE_BANDS   w f_i + (1 - w) f_i / factor, w rising evenly from 0 at
+ *                   turns_low to 1 at turns_high turns of the pair over
+ *                   `original` tokens (turns_low < turns_high)
+ *   DQ_ROPE_YARN    the same mixture, w falling evenly over the index i from 1 at
+ *                   floor(j(turns_high)) to 0 at ceil(j(turns_low)), j(n) =
+ *                   rotary_dim ln(original / (2 pi n)) / (2 ln base) (the ends
+ *                   kept within 0 and rotary_dim - 1, and at least 0.001 apart);
+ *                   the magnitude is 0.1 ln factor + 1 where factor > 1
+ *   The magnitude is 1 otherwise.  base > 0 (YARN: other than 1), factor >= 1,
+ *   turns and original > 0 where they count; all finite.
+ * dq_rope: rotates the queries and the keys of a chunk in one launch.
+ *   freq: device fp64 [rotary_dim / 2]; any frequencies, dq_rope_frequencies'
+ *       or the caller's
+ *   q, k: bf16 [batch][tokens][heads][head_dim] at element strides, channels
+ *       contiguous; either may be absent (NULL, 0 heads).  q_out, k_out: where
+ *       the results go, at strides of their own: the same tensor (same address
+ *       and strides), or one that overlaps neither input, in which no two
+ *       elements share an address.
+ *   positions: device int32, position of token t of sequence b at
+ *       positions[b pos_stride_b + t pos_stride_t], of any sign; or NULL:
+ *       positions are t0 + t, plus starts[b] where starts (device int32 [batch])
+ *       is not NULL, as the lengths of a cache are.  With positions, starts is
+ *       NULL and t0 is 0.
+ * Angles are computed in fp64 and reduced to a part of a turn before they are
+ * rounded; results are computed in fp32 and rounded to bf16 once.
+ * rotary_dim is even, 2 <= rotary_dim <= head_dim <= 1024; heads at most 65535;
+ * batch tokens at most 2^26; strides not negative.  Return DQ_OK (nothing is
+ * launched when batch or tokens is 0), DQ_ERR_INVALID_ARG or DQ_ERR_HIP.
+ */
+#define DQ_ROPE_HALF 0
+#define DQ_ROPE_INTERLEAVED 1
+#define DQ_ROPE_NONE 0
+#define DQ_ROPE_LINEAR 1
+#define DQ_ROPE_NTK 2
+#define DQ_ROPE_BANDS 3
+#define DQ_ROPE_YARN 4
+int dq_rope_frequencies(int32_t scaling, int32_t rotary_dim, double base, double factor, double original,
+                        double turns_low, double turns_high, double* freq, double* magnitude);
+int dq_rope(int32_t layout, int32_t transposed, const double* freq, float magnitude, int32_t rotary_dim,
+            int32_t head_dim, int32_t batch, int32_t tokens, const uint16_t* q, int64_t q_stride_b,
+            int64_t q_stride_t, int64_t q_stride_h, int32_t q_heads, uint16_t* q_out, int64_t qo_stride_b,
+            int64_t qo_stride_t, int64_t qo_stride_h, const uint16_t* k, int64_t k_stride_b, int64_t k_stride_t,
+            int64_t k_stride_h, int32_t kv_heads, uint16_t* k_out, int64_t ko_stride_b, int64_t ko_stride_t,
+            int64_t ko_stride_h, const int32_t* positions, int64_t pos_stride_b, int64_t pos_stride_t,
+            const int32_t* starts, int32_t t0, void* stream);
+
+/*
+ * Attention of a chunk of tokens over the 8-bit cache: n_q queries of every
+ * sequence at once, logits softmax_scale * q . k^, output sum a v^.
+ *   q:   bf16 [batch][n_q][q_heads][128] at element strides, channels contiguous;
+ *        query head i reads KV head i / (q_heads / kv_heads)
+ *   out: bf16 [batch][n_q][q_heads][128] likewise, no two elements at one address
+ *   q_lens: device int32 [batch] or NULL: the first q_lens[b] of the n_q queries
+ *        count (each in [0, n_q]); NULL: all.  Output rows behind them are left
+ *        as they are.
+ *   seq_lens: device int32 [batch], tokens in the cache (each in [0, t_cap])
+ *   causal = 1: the queries are those of the sequence's newest tokens, which the
+ *        cache holds already: query i of q_len has position p = seq_len - q_len
+ *        + i and sees the tokens t <= p.  window > 0: of those, t < sinks or
+ *        t > p - window, as the decode step of that token would; only blocks that
+ *        hold such tokens are read.  window = 0: all of them (sinks is 0 then).
+ *   causal = 0: every query sees all seq_len tokens, as a decoder's queries do
+ *        of an encoder's states that the cache holds (window and sinks are 0).
+ *   workspace: dq_chunk_workspace_bytes(...) bytes, 16-byte aligned (NULL where
+ *        that is 0); calls that may overlap in time need one each
+ * A query that sees no token gives zeros; one with an infinity or NaN that sees
+ * some gives NaN.  Scores and sums are held in fp32; the weights are rounded to
+ * fp16 for the product with the values, which are exact, and the output to bf16.
+ * Through a block table the call is the same; an entry outside the pool sets
+ * DQ_STATUS_PAGE and page 0 is read in its place.
+ * batch and kv_heads at most 65535, n_q q_heads at most 2^26, batch kv_heads
+ * ceil(n_q (q_heads / kv_heads) / 128) at most 2^22.  Returns DQ_OK (nothing is
+ * launched when batch or n_q is 0), DQ_ERR_INVALID_ARG, DQ_ERR_WORKSPACE or
+ * DQ_ERR_HIP.
+ *
+ * dq_cross_attention: the same, not causal, over an encoder's states in BF16.
+ *   k, v: bf16 [batch][n_kv][kv_heads][128] at element strides (0 where sequences
+ *        share states), channels contiguous
+ *   kv_lens: device int32 [batch] or NULL: states of each sequence (each in
+ *        [0, n_kv]); NULL: n_kv
+ *   mask: device u8 [batch][n_kv], rows mask_stride_b apart, or NULL: states with
+ *        0 are hidden (their keys and values may hold anything)
+ * A query whose sequence has no visible state gives zeros.  Infinities and NaN
+ * in a query or a visible state give what the formula gives.  Weights are rounded to
+ * bf16 for the product with the values.  n_kv is at most 2^30.
+ *
+ * dq_chunk_workspace_bytes: for both; t_cap is the cache's capacity (max_pages *
+ * page_tokens) or n_kv.  0 for sizes that the calls refuse.
+ */
+size_t dq_chunk_workspace_bytes(int32_t batch, int32_t n_q, int32_t q_heads, int32_t kv_heads, int32_t t_cap);
+int dq_q8_chunk_attention(int32_t format, const uint16_t* q, int64_t q_stride_b, int64_t q_stride_t,
+                          int64_t q_stride_h, int32_t batch, int32_t n_q, int32_t q_heads, int32_t kv_heads,
+                          const uint8_t* k_data, const float* k_scale, const uint8_t* v_data, const float* v_scale,
+                          const int32_t* q_lens, const int32_t* seq_lens, int32_t t_cap, int32_t causal,
+                          int32_t window, int32_t sinks, float softmax_scale, uint16_t* out, int64_t o_stride_b,
+                          int64_t o_stride_t, int64_t o_stride_h, void* workspace, size_t workspace_bytes,
+                          void* stream);
+int dq_q8_chunk_attention_paged(int32_t format, const uint16_t* q, int64_t q_stride_b, int64_t q_stride_t,
+                                int64_t q_stride_h, int32_t batch, int32_t n_q, int32_t q_heads, int32_t kv_heads,
+                                const uint8_t* k_pool, const float* k_scale_pool, const uint8_t* v_pool,
+                                const float* v_scale_pool, const int32_t* block_table, int32_t max_pages,
+                                int32_t page_tokens, int32_t num_pages, const int32_t* q_lens,
+                                const int32_t* seq_lens, int32_t causal, int32_t window, int32_t sinks,
+                                float softmax_scale, uint16_t* out, int64_t o_stride_b, int64_t o_stride_t,
+                                int64_t o_stride_h, void* workspace, size_t workspace_bytes, uint32_t* status,
+                                void* stream);
+int dq_cross_attention(const uint16_t* q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h, int32_t batch,
+                       int32_t n_q, int32_t q_heads, int32_t kv_heads, const uint16_t* k, int64_t k_stride_b,
+                       int64_t k_stride_t, int64_t k_stride_h, const uint16_t* v, int64_t v_stride_b,
+                       int64_t v_stride_t, int64_t v_stride_h, int32_t n_kv, const int32_t* q_lens,
+                       const int32_t* kv_lens, const uint8_t* mask, int64_t mask_stride_b, float softmax_scale,
+                       uint16_t* out, int64_t o_stride_b, int64_t o_stride_t, int64_t o_stride_h, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/*
  * rANS-decodes records back to symbols (Alg. 2), for parity checks.
  *   records: u8 [n_streams][C]; sym: u8 [n_streams][head_dim];
  *   header:  u16 [n_streams][2] = (scale, offset) fp16 bits; may be NULL;

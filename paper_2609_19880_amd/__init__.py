@@ -17,7 +17,8 @@ Entry points (same names as the C ABI in ``include/dq.h``):
     dq_q8_decode_kv_paged, dq_q8_decode_attention, dq_q8_decode_attention_partial,
     dq_q8_decode_attention_paged, dq_q8_decode_attention_paged_partial, dq_q8_add_scores,
     dq_q8_merge_scores, dq_q8_evict,
-    dq_q8_evict_paged, dq_decode_symbols, dq_strerror, dq_last_error
+    dq_q8_evict_paged, dq_rope_frequencies, dq_rope, dq_chunk_workspace_bytes, dq_q8_chunk_attention,
+    dq_q8_chunk_attention_paged, dq_cross_attention, dq_decode_symbols, dq_strerror, dq_last_error
 """
 
 from ._lib import (  # noqa: F401
@@ -38,6 +39,10 @@ from ._lib import (  # noqa: F401
     dq_q8_decode_attention_paged, dq_q8_decode_attention_paged_partial, dq_q8_add_scores,
     dq_q8_merge_scores, dq_q8_evict,
     dq_q8_evict_paged,
+    DQ_ROPE_HALF, DQ_ROPE_INTERLEAVED, DQ_ROPE_NONE, DQ_ROPE_LINEAR, DQ_ROPE_NTK, DQ_ROPE_BANDS, DQ_ROPE_YARN,
+    dq_rope_frequencies, dq_rope, dq_chunk_workspace_bytes, dq_q8_chunk_attention, dq_q8_chunk_attention_paged,
+    dq_cross_attention,
     dq_decode_symbols, dq_strerror, dq_last_error, smallest_feasible_alpha,
 )
 from .cache import KVCache, Q8KVCache, StreamingKVCache, TokenKVCache  # noqa: F401
+from .positions import RotaryPositions  # noqa: F401

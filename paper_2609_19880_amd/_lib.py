@@ -134,6 +134,21 @@ def _load():
                  "decode_attention", "decode_attention_paged_partial", "decode_attention_paged", "add_scores",
                  "merge_scores", "evict", "evict_paged"):
         getattr(lib, "dq_q8_" + name).restype = ctypes.c_int
+    D = ctypes.c_double
+    lib.dq_rope_frequencies.argtypes = [I32, I32, D, D, D, D, D, P, P]
+    lib.dq_rope_frequencies.restype = ctypes.c_int
+    lib.dq_rope.argtypes = [I32, I32, P, F, I32, I32, I32, I32, *rows, I32, *rows, *rows, I32, *rows, P, I64, I64, P,
+                            I32, P]
+    lib.dq_rope.restype = ctypes.c_int
+    lib.dq_chunk_workspace_bytes.argtypes = [I32, I32, I32, I32, I32]
+    lib.dq_chunk_workspace_bytes.restype = SZ
+    chunk = [I32, *rows, I32, I32, I32, I32, P, P, P, P]
+    lib.dq_q8_chunk_attention.argtypes = [*chunk, P, P, I32, I32, I32, I32, F, *rows, P, SZ, P]
+    lib.dq_q8_chunk_attention.restype = ctypes.c_int
+    lib.dq_q8_chunk_attention_paged.argtypes = [*chunk, *pages, P, P, I32, I32, I32, F, *rows, P, SZ, P, P]
+    lib.dq_q8_chunk_attention_paged.restype = ctypes.c_int
+    lib.dq_cross_attention.argtypes = [*rows, I32, I32, I32, I32, *rows, *rows, I32, P, P, P, I64, F, *rows, P, SZ, P]
+    lib.dq_cross_attention.restype = ctypes.c_int
     lib.dq_residual_append.argtypes = [P, P, I32, I32, I32, P, P, P, P, I32, P, P]
     lib.dq_residual_append.restype = ctypes.c_int
     lib.dq_residual_commit.argtypes = [P, P, I32, I32, P, P]
@@ -1040,6 +1055,217 @@ def dq_q8_evict_paged(seq_lens, new_lens, keep: int, first: int, last: int, bloc
                                 _q8_kept(kept, keep, first, last, B, H, dev), _q8_status(status, dev),
                                 _q8_stream(dev.index, stream))
     _check(rc, "dq_q8_evict_paged")
+
+
+# ------------------------- rotary positions, attention of many queries at once
+
+DQ_ROPE_HALF = 0
+DQ_ROPE_INTERLEAVED = 1
+DQ_ROPE_NONE = 0
+DQ_ROPE_LINEAR = 1
+DQ_ROPE_NTK = 2
+DQ_ROPE_BANDS = 3
+DQ_ROPE_YARN = 4
+ROPE_LAYOUTS = {"half": DQ_ROPE_HALF, "interleaved": DQ_ROPE_INTERLEAVED}
+ROPE_SCALINGS = {"none": DQ_ROPE_NONE, "linear": DQ_ROPE_LINEAR, "ntk": DQ_ROPE_NTK, "bands": DQ_ROPE_BANDS,
+                 "yarn": DQ_ROPE_YARN}
+
+
+def dq_rope_frequencies(rotary_dim: int, base: float = 10000.0, scaling="none", factor: float = 1.0,
+                        original: float = 0.0, turns=(1.0, 4.0)):
+    """Angles per token (fp64 numpy [rotary_dim / 2]) and the factor of the
+    rotated values (host only); scaling "none", "linear", "ntk", "bands" or
+    "yarn", turns = (turns_low, turns_high)."""
+    kind = ROPE_SCALINGS.get(scaling, scaling)
+    _need(kind in ROPE_SCALINGS.values(), "scaling must be 'none', 'linear', 'ntk', 'bands' or 'yarn'")
+    _need(0 < rotary_dim <= 1024, "rotary_dim")
+    freq = np.zeros(max(1, rotary_dim // 2), np.float64)
+    magnitude = ctypes.c_double()
+    rc = _lib.dq_rope_frequencies(kind, rotary_dim, base, factor, original, turns[0], turns[1], freq.ctypes.data,
+                                  ctypes.byref(magnitude))
+    _check(rc, "dq_rope_frequencies")
+    return freq, magnitude.value
+
+
+def _rope_rows(x, out, name, dev, stream):
+    """Rows [B, T, H, d] bf16 and where they go (a new tensor unless given)."""
+    _need(x.dtype is torch.bfloat16 and x.dim() == 4 and x.stride(3) == 1 and x.device == dev,
+          name + " must be bf16 [B, T, H, d], channels contiguous, on the frequencies' GPU")
+    if out is None:
+        if stream is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=dev)
+        else:                        # memory of the stream that fills it
+            with torch.cuda.stream(stream):
+                out = torch.empty(x.shape, dtype=x.dtype, device=dev)
+    else:
+        _need(out.dtype is torch.bfloat16 and out.shape == x.shape and out.stride(3) == 1 and out.device == dev,
+              name + "_out must be bf16 of " + name + "'s shape on the same GPU")
+    return out, (x.data_ptr(), *x.stride()[:3]), (out.data_ptr(), *out.stride()[:3])
+
+
+_NO_ROWS = (0, 0, 0, 0)
+
+
+def dq_rope(freq, q=None, k=None, positions=None, starts=None, t0: int = 0, layout="half", transposed: bool = False,
+            magnitude: float = 1.0, q_out=None, k_out=None, stream=None):
+    """Rotates bf16 q [B, T, Hq, d] and k [B, T, Hkv, d] (either may be None) by
+    their positions: int32 positions [B, T], or t0 + t plus int32 starts [B].
+    freq: fp64 [rotary_dim / 2] on the GPU.  Returns (q_out, k_out), new tensors
+    unless given (the inputs themselves rotate in place)."""
+    lay = ROPE_LAYOUTS.get(layout, layout)
+    _need(lay in (DQ_ROPE_HALF, DQ_ROPE_INTERLEAVED), "layout must be 'half' or 'interleaved'")
+    dev = freq.device
+    _need(freq.dtype is torch.float64 and freq.dim() == 1 and freq.is_contiguous() and dev.type == "cuda",
+          "freq must be fp64 [rotary_dim / 2] on a GPU")
+    x = k if q is None else q
+    _need(x is not None, "q or k")
+    _need(x.dim() == 4, "q and k must be bf16 [B, T, H, d]")
+    B, T, _, d = x.shape
+    qr = qo = kr = ko = _NO_ROWS
+    Hq = Hkv = 0
+    if q is not None:
+        q_out, qr, qo = _rope_rows(q, q_out, "q", dev, stream)
+        Hq = q.shape[2]
+    if k is not None:
+        _need(k.dim() == 4 and k.shape[0] == B and k.shape[1] == T and k.shape[3] == d,
+              "q and k must have the same sequences, tokens and channels")
+        k_out, kr, ko = _rope_rows(k, k_out, "k", dev, stream)
+        Hkv = k.shape[2]
+    at = psb = pst = start = 0
+    if positions is not None:
+        _need(positions.dtype is torch.int32 and positions.shape == (B, T) and positions.device == dev,
+              "positions must be int32 [B, T] on the same GPU")
+        at, psb, pst = positions.data_ptr(), *positions.stride()
+        _need(starts is None and t0 == 0, "positions, or starts and t0")
+    elif starts is not None:
+        start = _q8_lens(starts, B, dev, "starts")
+    _need(-_INT_MAX <= t0 <= _INT_MAX, "t0")
+    rc = _lib.dq_rope(lay, int(bool(transposed)), freq.data_ptr(), magnitude, 2 * freq.shape[0], d, B, T, *qr, Hq, *qo,
+                      *kr, Hkv, *ko, at, psb, pst, start, t0, _q8_stream(dev.index, stream))
+    if rc:
+        _check(rc, "dq_rope")
+    return q_out, k_out
+
+
+def dq_chunk_workspace_bytes(batch: int, n_q: int, q_heads: int, kv_heads: int, t_cap: int) -> int:
+    """Workspace of dq_q8_chunk_attention and dq_cross_attention (t_cap: the
+    cache's capacity, or the encoder states of a sequence); may be 0."""
+    return int(_lib.dq_chunk_workspace_bytes(batch, n_q, q_heads, kv_heads, t_cap))
+
+
+def _chunk_rows(q, out, batch, heads, dev, stream):
+    """Queries [B, n, Hq, 128] and where the results go."""
+    _need(q.dtype is torch.bfloat16 and q.dim() == 4 and q.shape[0] == batch and q.shape[3] == 128
+          and q.stride(3) == 1 and q.device == dev and q.shape[2] % heads == 0,
+          "q must be bf16 [B, n, Hq, 128], channels contiguous, on the cache's GPU, Hq a multiple of the KV heads")
+    if out is None:
+        if stream is None:
+            out = torch.empty(q.shape, dtype=torch.bfloat16, device=dev)
+        else:                        # memory of the stream that fills it
+            with torch.cuda.stream(stream):
+                out = torch.empty(q.shape, dtype=torch.bfloat16, device=dev)
+    else:
+        _need(out.dtype is torch.bfloat16 and out.shape == q.shape and out.stride(3) == 1 and out.device == dev,
+              "out must be bf16 of q's shape")
+    return out
+
+
+def _chunk_workspace(workspace, B, n, Hq, H, t_cap, dev, stream):
+    if workspace is None:
+        need = _lib.dq_chunk_workspace_bytes(B, n, Hq, H, t_cap)
+        if need == 0:
+            return None, 0, 0
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        else:
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    return (workspace, *_q8_workspace(workspace, dev))
+
+
+def _q8_chunk(fmt: int, cache, q, seq_lens, q_lens, causal, window, sinks, out, softmax_scale, workspace, stream,
+              paged=None):
+    rows, H, nb, dev, at = cache
+    B = rows if paged is None else paged[0].shape[0]
+    out = _chunk_rows(q, out, B, H, dev, stream)
+    n, Hq = q.shape[1], q.shape[2]
+    lens = _q8_lens(seq_lens, B, dev)
+    new = 0 if q_lens is None else _q8_lens(q_lens, B, dev, "q_lens")
+    _q8_sees(window, sinks)
+    scale = _RSQRT_D if softmax_scale is None else softmax_scale
+    if paged is None:
+        t_cap = nb * DQ_Q8_BLOCK
+        held, ws, ws_bytes = _chunk_workspace(workspace, B, n, Hq, H, t_cap, dev, stream)
+        rc = _lib.dq_q8_chunk_attention(
+            fmt, q.data_ptr(), *q.stride()[:3], B, n, Hq, H, *at, new, lens, t_cap, int(bool(causal)), window, sinks,
+            scale, out.data_ptr(), *out.stride()[:3], ws, ws_bytes, _q8_stream(dev.index, stream))
+        if rc:
+            _check(rc, "dq_q8_chunk_attention")
+        return out
+    block_table, status = paged
+    max_pages, page = _q8_table(block_table, B, dev), nb * DQ_Q8_BLOCK
+    held, ws, ws_bytes = _chunk_workspace(workspace, B, n, Hq, H, min(max_pages * page, _INT_MAX), dev, stream)
+    rc = _lib.dq_q8_chunk_attention_paged(
+        fmt, q.data_ptr(), *q.stride()[:3], B, n, Hq, H, *at, block_table.data_ptr(), max_pages, page, rows, new, lens,
+        int(bool(causal)), window, sinks, scale, out.data_ptr(), *out.stride()[:3], ws, ws_bytes,
+        _q8_status(status, dev), _q8_stream(dev.index, stream))
+    if rc:
+        _check(rc, "dq_q8_chunk_attention_paged")
+    return out
+
+
+def dq_q8_chunk_attention(fmt, q, k_data, k_scale, v_data, v_scale, seq_lens, q_lens=None, causal: bool = True,
+                          window: int = 0, sinks: int = 0, out=None, softmax_scale=None, workspace=None, stream=None):
+    """Attention of n queries per sequence over the 8-bit cache: q bf16 [B, n,
+    Hq, 128] -> out bf16 (new unless given).  causal: the queries are those of
+    the newest q_lens[b] (or n) of the seq_lens[b] cached tokens and see the
+    tokens up to their own, with a window the first `sinks` and the newest
+    `window` of them; else every query sees all seq_lens[b].  Output rows from
+    q_lens[b] on are left as they are."""
+    return _q8_chunk(_q8_format(fmt), _q8_cache_args(k_data, k_scale, v_data, v_scale), q, seq_lens, q_lens, causal,
+                     window, sinks, out, softmax_scale, workspace, stream)
+
+
+def dq_q8_chunk_attention_paged(fmt, q, k_pool, k_scale_pool, v_pool, v_scale_pool, block_table, seq_lens, q_lens=None,
+                                causal: bool = True, window: int = 0, sinks: int = 0, out=None, softmax_scale=None,
+                                workspace=None, status=None, stream=None):
+    """dq_q8_chunk_attention over pool pages."""
+    return _q8_chunk(_q8_format(fmt), _q8_cache_args(k_pool, k_scale_pool, v_pool, v_scale_pool), q, seq_lens, q_lens,
+                     causal, window, sinks, out, softmax_scale, workspace, stream, (block_table, status))
+
+
+def dq_cross_attention(q, k, v, kv_lens=None, mask=None, q_lens=None, out=None, softmax_scale=None, workspace=None,
+                       stream=None):
+    """Cross attention: q bf16 [B, n, Hq, 128] over an encoder's states k, v bf16
+    [B, T, H, 128] (any strides but channels) -> out bf16 (new unless given).
+    kv_lens int32 [B]: states of each sequence; mask bool or uint8 [B, T]: those
+    with 0 are hidden; q_lens int32 [B]: queries of each sequence, rows behind
+    them are left as they are."""
+    dev = k.device
+    _need(dev.type == "cuda", "k must be on a GPU")
+    for t, name in ((k, "k"), (v, "v")):
+        _need(t.dtype is torch.bfloat16 and t.dim() == 4 and t.shape == k.shape and t.shape[3] == 128
+              and t.stride(3) == 1 and t.device == dev,
+              name + " must be bf16 [B, T, H, 128], channels contiguous, both of one shape and GPU")
+    B, T, H, _ = k.shape
+    _need(H > 0, "k and v must have heads")
+    out = _chunk_rows(q, out, B, H, dev, stream)
+    n, Hq = q.shape[1], q.shape[2]
+    lens = 0 if kv_lens is None else _q8_lens(kv_lens, B, dev, "kv_lens")
+    new = 0 if q_lens is None else _q8_lens(q_lens, B, dev, "q_lens")
+    hide = hide_sb = 0
+    if mask is not None:
+        _need(mask.dtype in (torch.bool, torch.uint8) and mask.shape == (B, T) and mask.device == dev
+              and (mask.stride(1) == 1 or T <= 1), "mask must be bool or uint8 [B, T], rows contiguous, on k's GPU")
+        hide, hide_sb = mask.data_ptr(), mask.stride(0)
+    held, ws, ws_bytes = _chunk_workspace(workspace, B, n, Hq, H, T, dev, stream)
+    rc = _lib.dq_cross_attention(
+        q.data_ptr(), *q.stride()[:3], B, n, Hq, H, k.data_ptr(), *k.stride()[:3], v.data_ptr(), *v.stride()[:3], T,
+        new, lens, hide, hide_sb, _RSQRT_D if softmax_scale is None else softmax_scale, out.data_ptr(),
+        *out.stride()[:3], ws, ws_bytes, _q8_stream(dev.index, stream))
+    if rc:
+        _check(rc, "dq_cross_attention")
+    return out
 
 
 DQ_NO_ALLOC_SCRATCH_BYTES = 8 << 20

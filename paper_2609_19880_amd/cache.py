@@ -223,6 +223,17 @@ class Q8KVCache:
         return _lib._q8_attention(self._format, at, q, seq_lens, out, self.workspace, window, sinks, softmax_scale,
                                   lse_at, score_at, None)
 
+    def attend_chunk(self, q, seq_lens, q_lens=None, out=None, softmax_scale=None, causal: bool = True,
+                     window: int = 0, sinks: int = 0, workspace=None):
+        """q bf16 [B, n, Hq, 128] -> out bf16: the attention of a chunk whose
+        tokens the cache holds already (seq_lens counts them): query i of the
+        sequence's newest n, or q_lens[b], tokens sees those up to its own or,
+        with a window, the first `sinks` and the newest `window` of them.  Not
+        causal: every query sees all seq_lens[b] tokens, as of an encoder's
+        states.  Scores stay as they are."""
+        return _lib._q8_chunk(self._format, self._where()[0], q, seq_lens, q_lens, causal, window, sinks, out,
+                              softmax_scale, workspace, None)
+
     def partial(self, q, seq_lens, softmax_scale=None, window: int = 0, sinks: int = 0, extra_lens=None):
         """Split-K partials of one decode step over q bf16 [B, q_heads, 128] into
         the workspace (finish with merge; the scores' part of it with

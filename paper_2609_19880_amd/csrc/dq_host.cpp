@@ -12,8 +12,10 @@
 #include <cstdlib>
 #include <cstring>
 #include <new>
+#include <utility>
 #include <vector>
 
+#include "dq_chunk.h"
 #include "dq_internal.h"
 #include "dq_q8.h"
 
@@ -864,6 +866,175 @@ int dq_q8_evict_paged(int32_t B, int32_t H, const int32_t* seq_lens, int32_t* ne
     const dq::Q8Cache c = q8_cache(k_pool, k_scale_pool, v_pool, v_scale_pool);
     return q8_evict(pg, B, H, seq_lens, new_lens, t_cap, t_cap, keep, first, last, scores, scores, c, c, kept, status,
                     stream);
+}
+
+// -------------------------------------------------------- rotary positions
+
+int dq_rope_frequencies(int32_t scaling, int32_t r, double base, double factor, double original, double turns_low,
+                        double turns_high, double* freq, double* magnitude) {
+    if (!freq || !magnitude || r < 2 || r > 1024 || r % 2) return DQ_ERR_INVALID_ARG;
+    if (scaling < DQ_ROPE_NONE || scaling > DQ_ROPE_YARN) return DQ_ERR_INVALID_ARG;
+    if (!std::isfinite(base) || base <= 0) return DQ_ERR_INVALID_ARG;
+    const bool mixed = scaling == DQ_ROPE_BANDS || scaling == DQ_ROPE_YARN;
+    if (scaling != DQ_ROPE_NONE && !(std::isfinite(factor) && factor >= 1)) return DQ_ERR_INVALID_ARG;
+    if (scaling == DQ_ROPE_NTK && r == 2) return DQ_ERR_INVALID_ARG;
+    if (mixed && !(std::isfinite(original) && original > 0 && std::isfinite(turns_high) && turns_low > 0 &&
+                   turns_low < turns_high))
+        return DQ_ERR_INVALID_ARG;
+    if (scaling == DQ_ROPE_YARN && base == 1) return DQ_ERR_INVALID_ARG;
+    const double two_pi = 6.283185307179586477;
+    if (scaling == DQ_ROPE_NTK) base *= std::pow(factor, (double)r / (r - 2));
+    *magnitude = scaling == DQ_ROPE_YARN && factor > 1 ? 0.1 * std::log(factor) + 1 : 1;
+    double first = 0, last = 0;
+    if (scaling == DQ_ROPE_YARN) {
+        auto index = [&](double n) { return r * std::log(original / (two_pi * n)) / (2 * std::log(base)); };
+        first = std::max(std::floor(index(turns_high)), 0.0);
+        last = std::max(std::min(std::ceil(index(turns_low)), r - 1.0), first + 0.001);
+    }
+    for (int i = 0; i < r / 2; ++i) {
+        const double f = std::pow(base, -2.0 * i / r);
+        double w = 1;            // how much of f is kept; the rest is scaled
+        if (scaling == DQ_ROPE_LINEAR) w = 0;
+        if (scaling == DQ_ROPE_BANDS) w = (original * f / two_pi - turns_low) / (turns_high - turns_low);
+        if (scaling == DQ_ROPE_YARN) w = 1 - (i - first) / (last - first);
+        w = std::min(std::max(w, 0.0), 1.0);
+        freq[i] = w == 1 ? f : w == 0 ? f / factor : w * f + (1 - w) * (f / factor);
+    }
+    return DQ_OK;
+}
+
+// No two elements of [B][T][H][d] at these strides share an address: of the
+// axes that have more than one entry, each step is longer than all that lies
+// within it.
+static bool separate(const dq::Q8Rows& r, int64_t B, int64_t T, int64_t H, int64_t d) {
+    std::pair<int64_t, int64_t> axes[3] = {{r.sb, B}, {r.st, T}, {r.sh, H}};
+    std::sort(axes, axes + 3);
+    int64_t held = d;            // elements from the first to behind the last one so far
+    for (const auto& x : axes) {
+        if (x.second <= 1) continue;
+        if (x.first < held) return false;
+        if (x.first > INT64_MAX / 4 / x.second) return false;
+        held += x.first * (x.second - 1);
+    }
+    return true;
+}
+
+static int check_rope_rows(const dq::RopeRows& r, int32_t B, int32_t T, int32_t d) {
+    if (r.heads < 0 || r.heads > 65535) return DQ_ERR_INVALID_ARG;
+    if (r.heads == 0) return r.in.p || r.out.p ? DQ_ERR_INVALID_ARG : DQ_OK;
+    if (!r.in.p || !r.out.p) return DQ_ERR_INVALID_ARG;
+    if (r.in.sb < 0 || r.in.st < 0 || r.in.sh < 0 || r.out.sb < 0 || r.out.st < 0 || r.out.sh < 0)
+        return DQ_ERR_INVALID_ARG;
+    if (!separate(r.out, B, T, r.heads, d)) return DQ_ERR_INVALID_ARG;
+    if (r.in.p == r.out.p && ((B > 1 && r.in.sb != r.out.sb) || (T > 1 && r.in.st != r.out.st) ||
+                              (r.heads > 1 && r.in.sh != r.out.sh)))
+        return DQ_ERR_INVALID_ARG;
+    return DQ_OK;
+}
+
+int dq_rope(int32_t layout, int32_t transposed, const double* freq, float magnitude, int32_t rotary_dim,
+            int32_t head_dim, int32_t B, int32_t T, const uint16_t* q, int64_t qsb, int64_t qst, int64_t qsh,
+            int32_t Hq, uint16_t* qo, int64_t qosb, int64_t qost, int64_t qosh, const uint16_t* k, int64_t ksb,
+            int64_t kst, int64_t ksh, int32_t Hkv, uint16_t* ko, int64_t kosb, int64_t kost, int64_t kosh,
+            const int32_t* positions, int64_t psb, int64_t pst, const int32_t* starts, int32_t t0, void* stream) {
+    if (layout != DQ_ROPE_HALF && layout != DQ_ROPE_INTERLEAVED) return DQ_ERR_INVALID_ARG;
+    if ((transposed != 0 && transposed != 1) || !std::isfinite(magnitude)) return DQ_ERR_INVALID_ARG;
+    if (rotary_dim < 2 || rotary_dim % 2 || head_dim < rotary_dim || head_dim > 1024) return DQ_ERR_INVALID_ARG;
+    if (B < 0 || T < 0 || (int64_t)B * T > (1 << 26) || psb < 0 || pst < 0) return DQ_ERR_INVALID_ARG;
+    if (positions && (starts || t0)) return DQ_ERR_INVALID_ARG;
+    const dq::RopeRows rq{{q, qsb, qst, qsh}, {qo, qosb, qost, qosh}, Hq};
+    const dq::RopeRows rk{{k, ksb, kst, ksh}, {ko, kosb, kost, kosh}, Hkv};
+    if (B == 0 || T == 0) return DQ_OK;
+    if (int rc = check_rope_rows(rq, B, T, head_dim)) return rc;
+    if (int rc = check_rope_rows(rk, B, T, head_dim)) return rc;
+    if (!freq || Hq + Hkv == 0) return DQ_ERR_INVALID_ARG;
+    return dq::launch_rope(layout, transposed, freq, magnitude, rotary_dim, rq, rk, B, T, head_dim, positions, psb,
+                           pst, starts, t0, static_cast<hipStream_t>(stream));
+}
+
+// ----------------------------------------------- attention of many queries
+
+static bool chunk_sizes_ok(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t t_cap) {
+    if (B < 0 || B > 65535 || n_q < 0 || Hkv <= 0 || Hkv > 65535 || Hq <= 0 || Hq % Hkv || t_cap < 0) return false;
+    if ((int64_t)n_q * Hq > (1 << 26)) return false;
+    return (int64_t)B * Hkv * (((int64_t)n_q * (Hq / Hkv) + 127) / 128) <= (1 << 22);
+}
+
+size_t dq_chunk_workspace_bytes(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t t_cap) {
+    if (!chunk_sizes_ok(B, n_q, Hq, Hkv, t_cap) || B == 0 || n_q == 0) return 0;
+    return dq::chunk_workspace_bytes(B, n_q, Hq, Hkv, t_cap);
+}
+
+static int chunk_attention(const dq::ChunkSource& src, const dq::ChunkCall& c, void* ws, size_t ws_bytes,
+                           uint32_t* status, void* stream) {
+    if (!chunk_sizes_ok(c.B, c.n_q, c.Hq, c.Hkv, c.t_cap) || !std::isfinite(c.scale)) return DQ_ERR_INVALID_ARG;
+    if (c.q.sb < 0 || c.q.st < 0 || c.q.sh < 0 || c.out.sb < 0 || c.out.st < 0 || c.out.sh < 0)
+        return DQ_ERR_INVALID_ARG;
+    if (c.B == 0 || c.n_q == 0) return DQ_OK;
+    if (!c.q.p || !c.out.p || !separate(c.out, c.B, c.n_q, c.Hq, 128)) return DQ_ERR_INVALID_ARG;
+    const size_t need = dq::chunk_workspace_bytes(c.B, c.n_q, c.Hq, c.Hkv, c.t_cap);
+    if (need && (!ws || ws_bytes < need)) return DQ_ERR_WORKSPACE;
+    if (need && (reinterpret_cast<uintptr_t>(ws) & 15)) return DQ_ERR_INVALID_ARG;
+    return dq::launch_chunk(src, c, ws, status, static_cast<hipStream_t>(stream));
+}
+
+static int q8_chunk(int32_t format, const dq::Pages& pg, const dq::Q8Cache& cache, const dq::ChunkCall& c, void* ws,
+                    size_t ws_bytes, uint32_t* status, void* stream) {
+    if (format != DQ_Q8_INT8 && format != DQ_Q8_E4M3) return DQ_ERR_INVALID_ARG;
+    if (c.t_cap <= 0 || c.t_cap % DQ_MEAN_WINDOW) return DQ_ERR_INVALID_ARG;
+    if (c.causal != 0 && c.causal != 1) return DQ_ERR_INVALID_ARG;
+    if (c.window < 0 || c.sinks < 0 || (c.window == 0 && c.sinks) || (c.window && !c.causal)) return DQ_ERR_INVALID_ARG;
+    if (c.B > 0 && c.n_q > 0 && (!q8_cache_ok(cache) || !c.seq_lens)) return DQ_ERR_INVALID_ARG;
+    dq::ChunkSource src{};
+    src.format = format;
+    src.pg = pg;
+    src.cache = cache;
+    return chunk_attention(src, c, ws, ws_bytes, status, stream);
+}
+
+int dq_q8_chunk_attention(int32_t format, const uint16_t* q, int64_t qsb, int64_t qst, int64_t qsh, int32_t B,
+                          int32_t n_q, int32_t Hq, int32_t Hkv, const uint8_t* k_data, const float* k_scale,
+                          const uint8_t* v_data, const float* v_scale, const int32_t* q_lens,
+                          const int32_t* seq_lens, int32_t t_cap, int32_t causal, int32_t window, int32_t sinks,
+                          float scale, uint16_t* out, int64_t osb, int64_t ost, int64_t osh, void* ws,
+                          size_t ws_bytes, void* stream) {
+    const dq::ChunkCall c{{q, qsb, qst, qsh}, {out, osb, ost, osh}, B, n_q, Hq, Hkv, t_cap, q_lens, seq_lens, causal,
+                          window, sinks, scale};
+    return q8_chunk(format, kContiguous, q8_cache(k_data, k_scale, v_data, v_scale), c, ws, ws_bytes, nullptr, stream);
+}
+
+int dq_q8_chunk_attention_paged(int32_t format, const uint16_t* q, int64_t qsb, int64_t qst, int64_t qsh, int32_t B,
+                                int32_t n_q, int32_t Hq, int32_t Hkv, const uint8_t* k_pool,
+                                const float* k_scale_pool, const uint8_t* v_pool, const float* v_scale_pool,
+                                const int32_t* block_table, int32_t max_pages, int32_t page_tokens,
+                                int32_t num_pages, const int32_t* q_lens, const int32_t* seq_lens, int32_t causal,
+                                int32_t window, int32_t sinks, float scale, uint16_t* out, int64_t osb, int64_t ost,
+                                int64_t osh, void* ws, size_t ws_bytes, uint32_t* status, void* stream) {
+    dq::Pages pg;
+    int32_t t_cap = 0;
+    if (int rc = paging(block_table, max_pages, page_tokens, num_pages, &pg, &t_cap)) return rc;
+    const dq::ChunkCall c{{q, qsb, qst, qsh}, {out, osb, ost, osh}, B, n_q, Hq, Hkv, t_cap, q_lens, seq_lens, causal,
+                          window, sinks, scale};
+    return q8_chunk(format, pg, q8_cache(k_pool, k_scale_pool, v_pool, v_scale_pool), c, ws, ws_bytes, status, stream);
+}
+
+int dq_cross_attention(const uint16_t* q, int64_t qsb, int64_t qst, int64_t qsh, int32_t B, int32_t n_q, int32_t Hq,
+                       int32_t Hkv, const uint16_t* k, int64_t ksb, int64_t kst, int64_t ksh, const uint16_t* v,
+                       int64_t vsb, int64_t vst, int64_t vsh, int32_t n_kv, const int32_t* q_lens,
+                       const int32_t* kv_lens, const uint8_t* mask, int64_t mask_sb, float scale, uint16_t* out,
+                       int64_t osb, int64_t ost, int64_t osh, void* ws, size_t ws_bytes, void* stream) {
+    if (n_kv < 0 || n_kv > (1 << 30) || mask_sb < 0) return DQ_ERR_INVALID_ARG;
+    if (ksb < 0 || kst < 0 || ksh < 0 || vsb < 0 || vst < 0 || vsh < 0) return DQ_ERR_INVALID_ARG;
+    if (B > 0 && n_q > 0 && n_kv > 0 && (!k || !v)) return DQ_ERR_INVALID_ARG;
+    const dq::ChunkCall c{{q, qsb, qst, qsh}, {out, osb, ost, osh}, B, n_q, Hq, Hkv, n_kv, q_lens, kv_lens, 0, 0, 0,
+                          scale};
+    dq::ChunkSource src{};
+    src.format = dq::kChunkBf16;
+    src.k = {k, ksb, kst, ksh};
+    src.v = {v, vsb, vst, vsh};
+    src.mask = mask;
+    src.mask_sb = mask_sb;
+    return chunk_attention(src, c, ws, ws_bytes, nullptr, stream);
 }
 
 int dq_decode_symbols(const dq_tables* t, const uint8_t* records, int64_t n_streams, uint8_t* sym,

@@ -1,0 +1,190 @@
+"""Rotary positions on the GPU against the formula in 64 bits.
+
+Tolerance of an element: the result is rounded to bf16 once, 2^-8 of it, and
+computed in fp32 from a cosine and a sine whose errors are the angle's rounding
+to fp32 (2^-26 of a turn, 2^-23.3), the function's (2 ulp, 2^-22) and the two of
+the products: 2^-20 of (|a| + |b|) magnitude covers them."""
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+
+
+@pytest.fixture(scope="module")
+def dq():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2609_19880_amd as mod
+    return mod
+
+
+def _x(seed, *shape):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed)).to(torch.bfloat16)
+
+
+def _ref(x, freq, magnitude, at, layout, transposed):
+    """fp64 result and the bound of its error, numpy; at [B, T] integers."""
+    x = x.double().cpu().numpy()
+    r = 2 * len(freq)
+    turn = at.astype(np.float64)[..., None] * freq
+    turn = (-turn if transposed else turn)[:, :, None]
+    c, s = np.cos(turn) * magnitude, np.sin(turn) * magnitude
+    ia, ib = (np.arange(r // 2), np.arange(r // 2) + r // 2) if layout == "half" else (np.arange(0, r, 2), np.arange(1, r, 2))
+    a, b = x[..., ia], x[..., ib]
+    y, tol = x.copy(), np.zeros_like(x)
+    y[..., ia], y[..., ib] = a * c - b * s, a * s + b * c
+    tol[..., ia] = tol[..., ib] = 2.0 ** -20 * (np.abs(a) + np.abs(b)) * abs(magnitude)
+    tol[..., :r] += 2.0 ** -8 * np.abs(y[..., :r])
+    return y, tol
+
+
+def _check(got, x, freq, magnitude, at, layout, transposed):
+    y, tol = _ref(x, freq, magnitude, at, layout, transposed)
+    err = np.abs(got.double().cpu().numpy() - y)
+    assert (err <= tol).all(), float((err - tol).max())
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("B,T,Hq,Hkv,d,r", [
+    (1, 1, 1, 1, 128, 128), (1, 1, 32, 8, 128, 128), (2, 33, 3, 1, 128, 64), (3, 7, 8, 2, 64, 64), (1, 5000, 2, 1, 128, 128),
+    (2, 17, 2, 2, 96, 96), (1, 9, 5, 1, 80, 32), (2, 11, 1, 1, 7, 6), (1, 3, 2, 1, 130, 2), (1, 600, 4, 4, 256, 250),
+    (1, 2, 3, 3, 1024, 1024), (600, 1, 2, 1, 128, 96)])
+def test_sizes(dq, layout, transposed, B, T, Hq, Hkv, d, r):
+    q, k = _x(T, B, T, Hq, d), _x(T + 1, B, T, Hkv, d)
+    rope = dq.RotaryPositions(r, base=10000.0, layout=layout, magnitude=1.25)
+    freq = rope.freq.cpu().numpy()
+    starts = np.random.default_rng(T).integers(0, 100000, B).astype(np.int32)
+    at = starts[:, None] + np.arange(T)
+    qo, ko = rope.apply(q.to(DEV), k.to(DEV), starts=torch.from_numpy(starts).to(DEV), transposed=transposed)
+    _check(qo, q, freq, 1.25, at, layout, transposed)
+    _check(ko, k, freq, 1.25, at, layout, transposed)
+    # given positions are the same, and so are either tensor alone and t0
+    pos = torch.from_numpy(at.astype(np.int32)).to(DEV)
+    q1, k1 = rope.apply(q.to(DEV), None, positions=pos, transposed=transposed)
+    assert k1 is None and torch.equal(q1, qo)
+    q2, k2 = rope.apply(None, k.to(DEV), positions=pos, transposed=transposed)
+    assert q2 is None and torch.equal(k2, ko)
+    q3, _ = rope.apply(q[:1].to(DEV), t0=int(starts[0]), transposed=transposed)
+    assert torch.equal(q3, qo[:1])
+
+
+@pytest.mark.parametrize("scaling,args", [("none", {}), ("linear", dict(factor=8.0)), ("ntk", dict(factor=4.0)),
+                                          ("bands", dict(factor=8.0, original=8192.0)),
+                                          ("yarn", dict(factor=16.0, original=4096.0))])
+def test_far_positions(dq, scaling, args):
+    """Up to the ends of 32 bits, of both signs: the angle's fraction is kept."""
+    rope = dq.RotaryPositions(128, base=500000.0, scaling=scaling, **args)
+    freq = rope.freq.cpu().numpy()
+    at = np.array([[0, 1, -1, 131071, 1 << 20, -(1 << 24) + 1, (1 << 31) - 1, -(1 << 31), 1234567890]], np.int64)
+    q = _x(1, 1, at.shape[1], 2, 128)
+    qo, _ = rope.apply(q.to(DEV), positions=torch.from_numpy(at.astype(np.int32)).to(DEV))
+    # (the product itself has a rounding of 2^-53 of up to 2^31 radians, here and in the reference)
+    _check(qo, q, freq, rope.magnitude, at, "half", False)
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("r", [128, 64])
+def test_in_place_strides_and_alignment(dq, layout, r):
+    B, T, H = 2, 37, 3
+    x = _x(5, B, T, H, 128).to(DEV)
+    rope = dq.RotaryPositions(r, layout=layout)
+    pos = torch.randint(0, 5000, (B, T), dtype=torch.int32, device=DEV)
+    want, _ = rope.apply(x, positions=pos)
+    same = x.clone()
+    got, _ = rope.apply(same, positions=pos, q_out=same)
+    assert got is same and torch.equal(same, want)
+    # one tensor that holds queries, keys and values, rotated in place
+    fused = torch.cat([x, x, x], dim=2)
+    rope.apply(fused[:, :, :H], fused[:, :, H:2 * H], positions=pos, q_out=fused[:, :, :H], k_out=fused[:, :, H:2 * H])
+    assert torch.equal(fused[:, :, :H], want) and torch.equal(fused[:, :, H:2 * H], want)
+    assert torch.equal(fused[:, :, 2 * H:], x)
+    heads_first = x.permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3)
+    odd = torch.full((B, T, H, 133), 9.0, dtype=torch.bfloat16, device=DEV)
+    odd[..., 1:129] = x
+    for src in (heads_first, odd[..., 1:129]):
+        out = torch.full((B, T, H, 131), 9.0, dtype=torch.bfloat16, device=DEV)
+        got, _ = rope.apply(src, positions=pos, q_out=out[..., 2:130])
+        assert torch.equal(got, want) and bool((out[..., :2] == 9).all()) and bool((out[..., 130:] == 9).all())
+        got, _ = rope.apply(src, positions=pos)
+        assert torch.equal(got, want)
+    # an input that sequences and heads share, and positions that sequences share
+    one = x[:1, :, :1]
+    got, _ = rope.apply(one.expand(B, T, H, 128), positions=pos[:1].expand(B, T))
+    first, _ = rope.apply(one, positions=pos[:1])
+    assert torch.equal(got, first.expand(B, T, H, 128))
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_transposed_is_the_gradient(dq, layout):
+    """<R x, w> = <x, R' w> within the roundings, the gradient of a sum of
+    weighted outputs against differences, and back again at magnitude 1."""
+    B, T, H, d, r = 2, 50, 2, 128, 96
+    x, w = _x(1, B, T, H, d).to(DEV), _x(2, B, T, H, d).to(DEV)
+    pos = torch.randint(0, 9000, (B, T), dtype=torch.int32, device=DEV)
+    rope = dq.RotaryPositions(r, layout=layout, magnitude=1.5)
+    y, _ = rope.apply(x, positions=pos)
+    grad, _ = rope.apply(w, positions=pos, transposed=True)
+    _check(grad, w, rope.freq.cpu().numpy(), 1.5, pos.cpu().numpy().astype(np.int64), layout, True)
+    a = (y.double() * w.double()).sum(dim=3)
+    b = (x.double() * grad.double()).sum(dim=3)
+    # every output and every gradient is off by at most 2^-8 of it, and a little
+    bound = (2.0 ** -8 + 2.0 ** -18) * ((y.double() * w.double()).abs() + (x.double() * grad.double()).abs()).sum(dim=3)
+    assert bool(((a - b).abs() <= bound).all())
+    # differences: the map is linear, so a step of any size will do; 2^10 of one channel
+    for c in (0, 5, 95, 96, 127):
+        step = x.clone()
+        step[..., c] = x[..., c] + 1024.0
+        took = (step[..., c].double() - x[..., c].double())
+        ys, _ = rope.apply(step, positions=pos)
+        slope = ((ys.double() - y.double()) * w.double()).sum(dim=3) / took
+        tol = (2.0 ** -8 + 2.0 ** -18) * (((ys.double().abs() + y.double().abs()) * w.double().abs()).sum(dim=3) / took.abs()
+                                          + grad[..., c].double().abs())
+        assert bool(((slope - grad[..., c].double()).abs() <= tol).all()), c
+    turn = dq.RotaryPositions(r, layout=layout)
+    back, _ = turn.apply(turn.apply(x, positions=pos)[0], positions=pos, transposed=True)
+    # (two roundings of a vector whose pairs keep their length)
+    assert float((back.double() - x.double()).norm() / x.double().norm()) < 2 * 2.0 ** -8
+
+
+def test_graph_and_stream(dq):
+    rope = dq.RotaryPositions(128)
+    q, k = _x(1, 3, 2, 8, 128).to(DEV), _x(2, 3, 2, 2, 128).to(DEV)
+    lens = torch.tensor([5, 0, 4000], dtype=torch.int32, device=DEV)
+    qo, ko = torch.zeros_like(q), torch.zeros_like(k)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        rope.apply(q, k, starts=lens, q_out=qo, k_out=ko)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        rope.apply(q, k, starts=lens, q_out=qo, k_out=ko)
+    for i in range(4):
+        q.copy_(_x(10 + i, 3, 2, 8, 128))
+        lens += 7 * i
+        qo.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        wq, wk = rope.apply(q, k, starts=lens)
+        assert torch.equal(qo, wq) and torch.equal(ko, wk)
+    torch.cuda.synchronize()
+    sq, sk = rope.apply(q, k, starts=lens, stream=side)
+    side.synchronize()
+    assert torch.equal(sq, wq) and torch.equal(sk, wk)
+
+
+def test_not_finite(dq):
+    """NaN and infinities stay in their pair."""
+    x = _x(1, 1, 4, 1, 128)
+    x[0, 1, 0, 3], x[0, 2, 0, 70] = math.nan, math.inf
+    y, _ = dq.RotaryPositions(128).apply(x.to(DEV), t0=9)
+    bad = ~torch.isfinite(y[0, :, 0].float())
+    want = torch.zeros((4, 128), dtype=torch.bool)
+    want[1, [3, 67]] = want[2, [6, 70]] = True
+    assert torch.equal(bad.cpu(), want)
