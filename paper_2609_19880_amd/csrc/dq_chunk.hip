@@ -31,7 +31,6 @@ namespace {
 constexpr int kD = 128;
 constexpr int kBlk = DQ_Q8_BLOCK;
 constexpr int kBlkBytes = kBlk * kD;
-constexpr int kTile = 2;                     // blocks of 32 tokens per step
 constexpr float kBig = 3e38f;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kRowsOf = 32;                  // rows per wavefront
@@ -260,76 +259,86 @@ __device__ __forceinline__ uint32_t bf16_two(float x, float y) {
     return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x, (__bf16)y});
 }
 
+// A uniform address of memory that this kernel does not write, through the
+// scalar unit, beside the vector loads' order.
+template <typename T>
+__device__ __forceinline__ T scalar_load(const T* p) {
+    return *reinterpret_cast<const __attribute__((address_space(4))) T*>(reinterpret_cast<uintptr_t>(p));
+}
+
 __device__ __forceinline__ float clamped(float x) {    // NaN stays
     x = x > kBig ? kBig : x;
     return x < -kBig ? -kBig : x;
 }
 
-// -------------------------------------------------------------- the kernel
+// Two rounded weights' sum added to x, in fp32.
+template <int SRC>
+__device__ __forceinline__ float plus_weights(uint32_t w, float x) {
+    if constexpr (SRC == kChunkBf16)
+        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), bf16x2{(__bf16)1.f, (__bf16)1.f}, x, false);
+    else
+        return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, w), f16x2{(_Float16)1.f, (_Float16)1.f}, x, false);
+}
 
-// One workgroup of NW wavefronts per item: 32 NW rows, 32 per wavefront.
-// Steps of 64 tokens: codes are read, converted to fp16 once for the workgroup
-// and laid into LDS as the products take them (values transposed by the order
-// of the codes, or, in BF16, by the LDS read).  The next step's codes are on
-// their way meanwhile.
-template <int SRC, int NW>
-__global__ __launch_bounds__(NW* kWave, 2) void chunk_kernel(ChunkArgs a) {
-    constexpr int R = NW * kRowsOf, NT = NW * kWave;
-    constexpr bool q8 = SRC != kChunkBf16;
-    constexpr int kPieces = q8 ? 1024 / NT : 2048 / NT;   // 16-byte pieces per thread and step
-    __shared__ u32x4 lk[2][kTile][8][64];
-    __shared__ u32x4 lv[2][kTile][8][64];
-    __shared__ float2 lscale[2][kTile][2];       // keys: scale; values: log2 of it
+// ------------------------------------------------------- rows of a wavefront
 
-    const int tid = threadIdx.x, lane = tid & (kWave - 1);
-    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-    const int col = lane & 31, half = lane >> 5;
-    const Item it = find_item<R>(a, (int)blockIdx.x, lane);
-    if (it.tile < 0) return;
-    const int b = __builtin_amdgcn_readfirstlane(it.b), h = __builtin_amdgcn_readfirstlane(it.h);
-    const int tile = __builtin_amdgcn_readfirstlane(it.tile), piece = __builtin_amdgcn_readfirstlane(it.c);
-    const int chunk = __builtin_amdgcn_readfirstlane(it.chunk);
-    const Seq seq = seq_of<R>(a, b);
-    const int rows = seq.n * a.G;                // of the whole sequence
-    const int r0 = tile * R, r1 = min(r0 + R, rows);
-    const Sees see = sees(a, seq, r0, r1);
-    const int u0 = min((int64_t)piece * chunk, (int64_t)0x7FFFFFFF);
-    const bool whole = pieces(see.count, chunk) == 1;
-    if (u0 >= see.count && piece > 0) return;    // the merge does not ask for it
-    const int u1 = (int)min((int64_t)u0 + chunk, (int64_t)see.count);
+// What 32 rows (one wavefront's) hold: queries as the first product's operand,
+// sums, and the softmax state.  The lanes l and l ^ 32 share row l % 32; each
+// has the scores of 16 of a block's 32 tokens, 8 (i / 4) + 4 (l / 32) + i % 4.
+//
+// The state's maximum m is not the running maximum but one that the sums keep
+// until a block's weights, relative to it, add up to more than 2^15: weights of
+// m itself are 2^7, so fp16 holds what lies 2^8 above and, exactly, 2^21 below.
+// Most blocks so need no maximum and scale nothing: their weights are computed
+// with the m at hand and only checked.  A row's bits do not depend on the rows
+// beside it.
+template <int SRC>
+struct Rows {
+    static constexpr bool q8 = SRC != kChunkBf16;
+    static constexpr float kUp = q8 ? 2.f : 0.f;
+    static constexpr float kMost = q8 ? 0x1p15f : 0x1p60f;
 
-    // ------------------------------------------------ this lane's row
-    const int wr0 = r0 + wave * kRowsOf, r = wr0 + col;
-    const bool live = wr0 < rows, valid = r < rows;
-    const int row = min(r, rows - 1);
-    const int token = row / a.G, head = h * a.G + row % a.G;
-    // what the row sees: t < limit and (t < sinks or t >= start)
-    const int limit = a.causal ? max(0, min(see.T, see.off + token + 1)) : see.T;
-    const int start = a.window > 0 ? (int)max((int64_t)0, (int64_t)see.off + token + 1 - a.window) : 0;
-    const int sinks = a.sinks;
-    const int lim_lo = __builtin_amdgcn_readfirstlane(limit);                    // rows are in order
-    const int lim_hi = __builtin_amdgcn_readlane(limit, 31);
-    const int start_hi = __builtin_amdgcn_readlane(start, 31);
+    u32x4 q[8];
+    f32x16 o[4];
+    float m, l, vref, qc;        // vref: log2 of the scale that the values are relative to
+    int limit, start, sinks;     // the row sees t < limit, of those t < sinks or t >= start
+    int lim_lo, lim_hi, start_hi;
+    bool live, careful;   // careful: a row has no maximum yet, or one of 2^11 or more
 
-    u32x4 qf[8];
-    float qc = a.scale_log2, l = 0.f;
-    {
+    __device__ __forceinline__ void load(const ChunkArgs& a, const Sees& see, int b, int h, int r0, int rows, int lane) {
+        const int half = lane >> 5, r = r0 + (lane & 31);
+        const bool valid = r < rows;
+        const int row = min(r, rows - 1), token = row / a.G, head = h * a.G + (row - token * a.G);
+        live = r0 < rows;
+        limit = a.causal ? max(0, min(see.T, see.off + token + 1)) : see.T;
+        start = a.window > 0 ? (int)max((int64_t)0, (int64_t)see.off + token + 1 - a.window) : 0;
+        sinks = a.sinks;
+        lim_lo = __builtin_amdgcn_readfirstlane(limit);                          // rows are in order
+        lim_hi = __builtin_amdgcn_readlane(limit, 31);
+        start_hi = __builtin_amdgcn_readlane(start, 31);
+        m = -INFINITY;
+        l = 0.f;
+        vref = kNoScale;
+        qc = a.scale_log2;
+        careful = true;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = f32x16{};
         const uint16_t* p = a.q + (int64_t)b * a.q_sb + (int64_t)token * a.q_st + (int64_t)head * a.q_sh;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             // channels of operand j: as the keys' pieces hold them, or in order
             const int ch = q8 ? 16 * (2 * (j >> 1) + half) + 8 * (j & 1) : 16 * j + 8 * half;
-            qf[j] = u32x4{0u, 0u, 0u, 0u};
+            q[j] = u32x4{0u, 0u, 0u, 0u};
             if (valid) {
                 if (a.q_aligned) {
-                    qf[j] = *reinterpret_cast<const u32x4*>(p + ch);
+                    q[j] = *reinterpret_cast<const u32x4*>(p + ch);
                 } else {
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        qf[j][i] = (uint32_t)p[ch + 2 * i] | ((uint32_t)p[ch + 2 * i + 1] << 16);
+                        q[j][i] = (uint32_t)p[ch + 2 * i] | ((uint32_t)p[ch + 2 * i + 1] << 16);
                 }
             }
-            if (a.negative) qf[j] ^= 0x80008000u;
+            if (a.negative) q[j] ^= 0x80008000u;
         }
         if constexpr (q8) {
             int top = 0;
@@ -337,65 +346,277 @@ __global__ __launch_bounds__(NW* kWave, 2) void chunk_kernel(ChunkArgs a) {
             for (int j = 0; j < 8; ++j)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    top = max(top, max((int)(qf[j][i] & 0x7FFFu), (int)((qf[j][i] >> 16) & 0x7FFFu)));
+                    top = max(top, max((int)(q[j][i] & 0x7FFFu), (int)((q[j][i] >> 16) & 0x7FFFu)));
             top = max(top, __float_as_int(xor_lane<32>(__int_as_float(top), lane)));
             const bool nan = top >= 0x7F80;      // infinities and NaN make the row NaN
             if (nan && limit > 0) l = NAN;
-            const int e = top >= 0x80 ? (top >> 7) - 127 : -126;
-            const int up = 13 - e;
+            const int up = 13 - (top >= 0x80 ? (top >> 7) - 127 : -126);
             qc = ldexpf(qc, -up);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float x = ldexpf(__uint_as_float(qf[j][i] << 16), up);
-                    const float y = ldexpf(__uint_as_float(qf[j][i] & 0xFFFF0000u), up);
-                    qf[j][i] = nan ? 0u : weights2<SRC>(x, y);
+                    const float x = ldexpf(__uint_as_float(q[j][i] << 16), up);
+                    const float y = ldexpf(__uint_as_float(q[j][i] & 0xFFFF0000u), up);
+                    q[j][i] = nan ? 0u : weights2<SRC>(x, y);
                 }
         }
     }
+
+    // Operands 4 part .. of the keys.
+    __device__ __forceinline__ void scores(f32x16& s, int part, const u32x4 (&kf)[4]) const {
+        if (part == 0) s = f32x16{};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s = mma<SRC>(kf[j], q[4 * part + j], s);
+    }
+
+    // The weights exp2(s c + e) and their sum, of the rounded ones.
+    __device__ __forceinline__ float weigh(const f32x16& s, float c, float e, u32x4 (&p)[2]) const {
+        float sum = 0.f;
+#pragma unroll
+        for (int st = 0; st < 2; ++st)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int at = 4 * st + 8 * (i >> 1) + 2 * (i & 1);
+                const float x = __builtin_amdgcn_exp2f(fmaf(s[at], c, e));
+                const float y = __builtin_amdgcn_exp2f(fmaf(s[at + 1], c, e));
+                p[st][i] = weights2<SRC>(x, y);
+                sum = plus_weights<SRC>(p[st][i], sum);
+            }
+        return sum;
+    }
+
+    __device__ __forceinline__ float mu() const { return m == -INFINITY ? 0.f : m; }
+
+    // The softmax of a block whose scores are s, times c: p are its weights.
+    // t0: the block's first token; shown: bit t of it is clear where token t is
+    // hidden; vl: log2 of the values' scale, kNoScale for a block of zeros (any
+    // weight will do).
+    __device__ __forceinline__ void block(f32x16& s, float c, float vl, int t0, uint32_t shown, int lane,
+                                          u32x4 (&p)[2]) {
+        const bool masked = shown != ~0u || t0 + kBlk > lim_lo || (start_hi > 0 && t0 < start_hi && t0 + kBlk > sinks);
+        float d = 0.f;
+        if constexpr (q8) d = vl <= kNoScale ? 0.f : fmaxf(vl - vref, -60.f);
+        float sum = weigh(s, c, kUp + d - mu(), p);
+        bool again = masked || careful;
+        // (weights that fp16 would lose need their sum in fp32)
+        if constexpr (q8) again = again || !(d >= -2.f && d <= 0.f);
+        if (again || __builtin_amdgcn_ballot_w64(sum > kMost) != 0) sum = anew(s, c, sum, vl, d, t0, shown, masked, lane, p);
+        l += q8 ? sum * __builtin_amdgcn_exp2f(-d) : sum;
+    }
+
+    // The same with masks, a new maximum or a new scale; d becomes the block's.
+    // sum: of the weights without them.
+    __device__ __forceinline__ float anew(f32x16& s, float c, float sum, float vl, float& d, int t0, uint32_t shown,
+                                          bool masked, int lane, u32x4 (&p)[2]) {
+        // (the empty statement keeps what masks need in here: outside the loop it
+        // would take registers that every block is short of)
+        int half = lane >> 5;
+        asm volatile("" : "+v"(half));
+        float top = s[0];                        // (NaN where every score is)
+#pragma unroll
+        for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
+        top *= c;
+        // scores so large that a fused product would differ from the maximum by
+        // more than a rounding of it
+        const bool exact = masked || __builtin_amdgcn_ballot_w64(fmaxf(fabsf(mu()), fabsf(top)) >= 0x1p11f) != 0;
+        if (exact) {
+            top = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int in = 8 * (e >> 2) + 4 * half + (e & 3), t = t0 + in;
+                const bool on = (t < limit) & ((t >= start) | (t < sinks)) & (((shown >> in) & 1) != 0);
+                s[e] = on ? clamped(s[e] * c) : -INFINITY;
+                top = fmaxf(top, s[e]);
+            }
+            c = 1.f;
+        }
+        top = fmaxf(top, xor_lane<32>(top, lane));
+        sum = fmaxf(sum, xor_lane<32>(sum, lane));
+        const bool higher = (m == -INFINITY || (exact ? top > m + 4.f : sum > kMost)) && top > m;
+        float f = higher ? __builtin_amdgcn_exp2f(m - top) : 1.f;
+        m = higher ? top : m;
+        l *= f;
+        if constexpr (q8) {
+            if (d > 0.f) {
+                // room for scales of twice the size
+                f *= __builtin_amdgcn_exp2f(vref - (vl + 1.f));
+                vref = vl + 1.f;
+                d = -1.f;
+            }
+        }
+        // (whole vectors: element by element the compiler holds the sums twice)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] *= f;
+        careful = __builtin_amdgcn_ballot_w64(!(fabsf(m) < 0x1p11f)) != 0;
+        float e0 = kUp + d;
+        if (exact) {
+            // (large scores: the difference first, which is exact where it counts)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] -= mu();
+        } else {
+            e0 -= mu();
+        }
+        const float rounded = weigh(s, c, e0, p);
+        if (!q8 || d >= -2.f) return rounded;
+        float all = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) all += __builtin_amdgcn_exp2f(fmaf(s[e], c, e0));
+        return all;
+    }
+
+    // The values of half of a block's tokens.
+    __device__ __forceinline__ void values(const u32x4 (&vf)[4], const u32x4& p) {
+#pragma unroll
+        for (int np = 0; np < 4; ++np) o[np] = mma<SRC>(vf[np], p, o[np]);
+    }
+};
+
+// -------------------------------------------------------------- the kernel
+
+constexpr int kWaves = 4;
+constexpr int kThreads = kWaves * kWave;
+constexpr int kR = kWaves * kRowsOf;         // rows of a tile
+
+// A step's keys and values (64 tokens) in LDS.  Keys: operand j of a block at
+// kKeyOp j, a lane's 16 bytes at half (kKeyOp / 2) + 16 (token % 32).  Codes
+// become fp16; values of codes lie as their operands do (2 np + st, 1 KB each),
+// BF16 values as rows that the LDS reads transposed.  Where rows of BF16 are
+// written a piece of 8 channels at a time, 16 (keys) and 64 bytes (values) of
+// padding keep the 16 pieces of a row in different banks.
+template <int SRC>
+struct Lds {
+    static constexpr bool q8 = SRC != kChunkBf16;
+    static constexpr int kKeyOp = q8 ? 1024 : 1056;
+    static constexpr int kKeys = 8 * kKeyOp;
+    static constexpr int kValRow = 320;
+    static constexpr int kStage = kKeys + (q8 ? 8192 : kBlk * kValRow);
+};
+
+typedef const __attribute__((address_space(1))) uint8_t* GlobalBytes;
+typedef const __attribute__((address_space(1))) float* GlobalFloats;
+typedef const __attribute__((address_space(1))) u32x4* GlobalPieces;
+
+template <int SRC>
+__device__ __forceinline__ void read_keys(const char* at, int part, int lane, u32x4 (&kf)[4]) {
+    const char* p = at + (lane >> 5) * (Lds<SRC>::kKeyOp / 2) + (lane & 31) * 16;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) kf[j] = *reinterpret_cast<const u32x4*>(p + (4 * part + j) * Lds<SRC>::kKeyOp);
+}
+
+template <int SRC>
+__device__ __forceinline__ void read_values(const char* at, int st, int lane, u32x4 (&vf)[4]) {
+    if constexpr (Lds<SRC>::q8) {
+#pragma unroll
+        for (int np = 0; np < 4; ++np) vf[np] = *reinterpret_cast<const u32x4*>(at + (2 * np + st) * 1024 + lane * 16);
+    } else {
+        // four rows of 16 channels, transposed: tokens 8 st + 4 half + 0..3, then 16 further on
+        const char* p = at + (4 * (lane >> 5) + ((lane >> 2) & 3)) * Lds<SRC>::kValRow + ((lane >> 4) & 1) * 32 +
+                        (lane & 3) * 8 + 8 * st * Lds<SRC>::kValRow;
+        typedef __attribute__((address_space(3))) i16x4* LdsRows;
+#pragma unroll
+        for (int np = 0; np < 4; ++np) {
+            const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsRows)(p + 64 * np));
+            const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsRows)(p + 64 * np + 16 * Lds<SRC>::kValRow));
+            const u32x2 l2 = __builtin_bit_cast(u32x2, lo), h2 = __builtin_bit_cast(u32x2, hi);
+            vf[np] = u32x4{l2[0], l2[1], h2[0], h2[1]};
+        }
+    }
+}
+
+__device__ __forceinline__ void store_row(const ChunkArgs& a, int b, int token, int head, int ch, uint32_t w0,
+                                          uint32_t w1) {
+    uint16_t* x = a.out + (int64_t)b * a.o_sb + (int64_t)token * a.o_st + (int64_t)head * a.o_sh + ch;
+    if (a.out_aligned) {
+        *reinterpret_cast<u32x2*>(x) = u32x2{w0, w1};
+    } else {
+        x[0] = (uint16_t)w0;
+        x[1] = (uint16_t)(w0 >> 16);
+        x[2] = (uint16_t)w1;
+        x[3] = (uint16_t)(w1 >> 16);
+    }
+}
+
+// One workgroup of four wavefronts per item: 128 rows, 32 per wavefront, three
+// workgroups per CU.  A step is a block of 32 tokens: its codes are read,
+// converted to fp16 once for the workgroup and laid into LDS as the products
+// take them, while the step before it is worked on: one barrier per step.
+template <int SRC>
+__global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
+    typedef Lds<SRC> L;
+    constexpr bool q8 = L::q8;
+    constexpr int kPieces = q8 ? 2 : 4;          // 16-byte pieces per thread and step: keys, then values
+    __shared__ __attribute__((aligned(16))) char lds[2 * L::kStage];
+    __shared__ float lscale[2][2];               // the keys' scale, log2 of the values'
+
+    const int tid = threadIdx.x, lane = tid & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const Item it = find_item<kR>(a, (int)blockIdx.x, lane);
+    if (it.tile < 0) return;
+    const int b = __builtin_amdgcn_readfirstlane(it.b), h = __builtin_amdgcn_readfirstlane(it.h);
+    const int tile = __builtin_amdgcn_readfirstlane(it.tile), piece = __builtin_amdgcn_readfirstlane(it.c);
+    const int chunk = __builtin_amdgcn_readfirstlane(it.chunk);
+    const Seq seq = seq_of<kR>(a, b);
+    const int rows = seq.n * a.G;                // of the whole sequence
+    const int r0 = tile * kR;
+    const Sees see = sees(a, seq, r0, min(r0 + kR, rows));
+    const bool whole = pieces(see.count, chunk) == 1;
+    const int u0 = (int)min((int64_t)piece * chunk, (int64_t)0x7FFFFF00);
+    if (u0 >= see.count && piece > 0) return;    // the merge does not ask for it
+    const int u1 = (int)min((int64_t)u0 + chunk, (int64_t)see.count);
+
+    Rows<SRC> me;
+    me.load(a, see, b, h, r0 + wave * kRowsOf, rows, lane);
 
     // ------------------------------------------------ loads
     bool bad = false;
     auto block_of = [&](int u) { return u < see.head ? u : see.from + (u - see.head); };
     u32x4 reg[kPieces];
-    float sreg[kPieces];
-    // requests the step of blocks u, u + 1
+    // Codes: pages are looked up a step before they are needed, and scales are
+    // read by lanes 0 and 1 of wavefront 0 (keys, values): nothing here waits for
+    // memory.  Block `at` lies at page (H per_page) + h per_page + at % per_page;
+    // without a table the sequence is the page.
+    float sreg = 0.f;
+    int page = b;
+    const int per_page = a.pg.bt ? 1 << (a.pg.page_shift - 5) : a.t_cap / kBlk;
+    const int in_page = a.pg.bt ? per_page - 1 : 0x7FFFFFFF, pages = a.pg.bt ? a.pg.num_pages : a.B;
+    const uint32_t page_blocks = (uint32_t)(a.H * per_page);
+    const int64_t head_blocks = (int64_t)h * per_page;
+    const int32_t* table = a.pg.bt ? a.pg.bt + (int64_t)b * a.pg.max_pages : nullptr;
+    GlobalBytes k_codes = (GlobalBytes)(uintptr_t)a.k, v_codes = (GlobalBytes)(uintptr_t)a.v;
+    GlobalFloats scale_of = (GlobalFloats)(uintptr_t)(lane & 1 ? a.vs : a.ks);
+    // BF16: this thread's piece of rows 16 i + tid / 16
+    const uint16_t* k_row = nullptr;
+    const uint16_t* v_row = nullptr;
+    int64_t k_st = 0, v_st = 0;
+    if constexpr (!q8) {
+        k_st = a.k_st;
+        v_st = a.v_st;
+        k_row = reinterpret_cast<const uint16_t*>(a.k) + b * a.k_sb + h * a.k_sh + (tid >> 4) * k_st + 8 * (tid & 15);
+        v_row = reinterpret_cast<const uint16_t*>(a.v) + b * a.v_sb + h * a.v_sh + (tid >> 4) * v_st + 8 * (tid & 15);
+    }
+    auto look_up = [&](int u) {
+        if (q8 && table && u < u1) page = scalar_load(table + ((block_of(u) * kBlk) >> a.pg.page_shift));
+    };
+    // requests block u
     auto request = [&](int u) {
-        if constexpr (q8) {
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
-                const int p = tid + i * NT;      // block, keys or values, piece
-                const int blk = __builtin_amdgcn_readfirstlane(p >> 9), kind = __builtin_amdgcn_readfirstlane((p >> 8) & 1);
-                reg[i] = u32x4{0u, 0u, 0u, 0u};
-                sreg[i] = 0.f;
-                if (u + blk < u1) {
-                    const int at = block_of(u + blk);
-                    int64_t bi;
-                    if (a.pg.bt) {
-                        const int64_t pp = physical_page(a.pg, b, at * kBlk, bad);
-                        const int bpp = 1 << (a.pg.page_shift - 5);
-                        bi = (pp * a.H + h) * bpp + (at & (bpp - 1));
-                    } else {
-                        bi = ((int64_t)b * a.H + h) * (a.t_cap / kBlk) + at;
-                    }
-                    reg[i] = reinterpret_cast<const u32x4*>((kind ? a.v : a.k) + bi * kBlkBytes)[p & 255];
-                    if ((p & 255) == 0) sreg[i] = (kind ? a.vs : a.ks)[bi];
-                }
-            }
+        for (int i = 0; i < kPieces; ++i) reg[i] = u32x4{0u, 0u, 0u, 0u};
+        if (u >= u1) return;
+        if constexpr (q8) {
+            const bool in = (uint32_t)page < (uint32_t)pages;
+            bad = bad || !in;
+            const int64_t bi = (int64_t)((uint64_t)(uint32_t)(in ? page : 0) * page_blocks) + head_blocks +
+                               (block_of(u) & in_page);
+            reg[0] = *reinterpret_cast<GlobalPieces>(k_codes + bi * kBlkBytes + 16 * tid);
+            reg[1] = *reinterpret_cast<GlobalPieces>(v_codes + bi * kBlkBytes + 16 * tid);
+            if (tid < 2) sreg = scale_of[bi];
         } else {
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) {
-                const int p = tid + i * NT;      // keys or values, token, piece
-                const int kind = __builtin_amdgcn_readfirstlane(p >> 10), t = block_of(u) * kBlk + ((p >> 4) & 63), ch = 8 * (p & 15);
-                reg[i] = u32x4{0u, 0u, 0u, 0u};
-                bool in = t < see.T;
-                // a hidden token's value must not reach the sum, whatever it is
-                if (kind && a.mask && in) in = a.mask[(int64_t)b * a.mask_sb + t] != 0;
-                if (in) {
-                    const uint16_t* x = reinterpret_cast<const uint16_t*>(kind ? a.v : a.k) +
-                                        (int64_t)b * (kind ? a.v_sb : a.k_sb) + (int64_t)h * (kind ? a.v_sh : a.k_sh) +
-                                        (int64_t)t * (kind ? a.v_st : a.k_st) + ch;
+                const int t0 = u * kBlk + 16 * (i & 1);
+                if (t0 + (tid >> 4) < see.T) {
+                    const uint16_t* x = i >> 1 ? v_row + t0 * v_st : k_row + t0 * k_st;
                     if (a.kv_aligned) {
                         reg[i] = *reinterpret_cast<const u32x4*>(x);
                     } else {
@@ -407,242 +628,143 @@ __global__ __launch_bounds__(NW* kWave, 2) void chunk_kernel(ChunkArgs a) {
             }
         }
     };
-    auto lay = [&](int buf) {
+    // BF16: the mask's byte of token lane % 32 of a block, and the tokens it shows
+    uint32_t mreg = 0;
+    const uint8_t* mask = !q8 && a.mask ? a.mask + b * a.mask_sb : nullptr;
+    auto request_mask = [&](int u) {
+        if (mask) {
+            const int t = u * kBlk + (lane & 31);
+            mreg = u < u1 && t < see.T ? mask[t] : 0;
+        }
+    };
+    auto shown_now = [&]() -> uint32_t { return mask ? (uint32_t)__builtin_amdgcn_ballot_w64(mreg != 0) : ~0u; };
+    auto keys_at = [&](int step) { return lds + (step & 1) * L::kStage; };
+    auto values_at = [&](int step) { return lds + (step & 1) * L::kStage + L::kKeys; };
+    // where this thread's pieces of stage 0 go
+    int k_to, v_to;
+    if constexpr (q8) {
+        // piece ((t / 16) 2 + c / 64) 64 + ((c / 16) % 4) 16 + t % 16
+        const int t = ((tid >> 7) << 4) | (tid & 15), slice = ((tid >> 6) & 1) * 4 + ((tid >> 4) & 3);
+        k_to = (slice >> 1) * 2048 + (slice & 1) * 512 + t * 16;
+        // piece ((c / 32) 4 + (t / 4) % 4) 16 + c % 16
+        const int np = tid >> 6, grp = (tid >> 4) & 3;
+        v_to = L::kKeys + (np * 2 + (grp >> 1)) * 1024 + (grp & 1) * 512 + (tid & 15) * 16;
+    } else {
+        k_to = (tid & 15) * (L::kKeyOp / 2) + (tid >> 4) * 16;
+        v_to = L::kKeys + (tid >> 4) * L::kValRow + (tid & 15) * 16;
+    }
+    // lays what was requested into step `step`; of the values, those that `shown` shows
+    auto lay = [&](int step, uint32_t shown) {
+        char* to = lds + (step & 1) * L::kStage;
+        if constexpr (q8) {
+            if (tid < 2) {
+                float x = sreg;
+                if (tid) x = x > 0.f ? __builtin_amdgcn_logf(x) : kNoScale;
+                lscale[step & 1][tid] = x;
+            }
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const int p = tid + i * NT;
-            if constexpr (q8) {
-                const int blk = p >> 9, kind = (p >> 8) & 1, at = p & 255;
+            for (int i = 0; i < 2; ++i) {
                 const u32x2 w0 = halves4<SRC>(reg[i][0]), w1 = halves4<SRC>(reg[i][1]);
                 const u32x2 w2 = halves4<SRC>(reg[i][2]), w3 = halves4<SRC>(reg[i][3]);
-                const u32x4 lo = {w0[0], w0[1], w1[0], w1[1]}, hi = {w2[0], w2[1], w3[0], w3[1]};
-                if (kind == 0) {
-                    // piece ((t / 16) 2 + c / 64) 64 + ((c / 16) % 4) 16 + t % 16
-                    const int t = ((at >> 7) << 4) | (at & 15), slice = ((at >> 6) & 1) * 4 + ((at >> 4) & 3);
-                    u32x4* to = &lk[buf][blk][(slice >> 1) * 2][(slice & 1) * 32 + t];
-                    to[0] = lo;
-                    to[64] = hi;
-                } else {
-                    // piece ((c / 32) 4 + (t / 4) % 4) 16 + c % 16
-                    const int np = at >> 6, grp = (at >> 4) & 3;
-                    u32x4* to = &lv[buf][blk][np * 2 + (grp >> 1)][(grp & 1) * 32 + (at & 15)];
-                    to[0] = lo;
-                    to[16] = hi;
-                }
-                if (at == 0) {
-                    if (kind == 0)
-                        lscale[buf][blk][0].x = sreg[i];
-                    else
-                        lscale[buf][blk][0].y = sreg[i] > 0.f ? __builtin_amdgcn_logf(sreg[i]) : kNoScale;
-                }
-            } else {
-                const int kind = p >> 10, t = (p >> 4) & 63, g = p & 15;
-                if (kind == 0)
-                    lk[buf][t >> 5][g >> 1][(g & 1) * 32 + ((t & 31) ^ g)] = reg[i];
-                else
-                    (&lv[buf][0][0][0])[t * 16 + (g ^ ((t & 3) << 2))] = reg[i];
+                *reinterpret_cast<u32x4*>(to + (i ? v_to : k_to)) = u32x4{w0[0], w0[1], w1[0], w1[1]};
+                *reinterpret_cast<u32x4*>(to + (i ? v_to + 256 : k_to + 1024)) = u32x4{w2[0], w2[1], w3[0], w3[1]};
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                *reinterpret_cast<u32x4*>(to + k_to + 256 * i) = reg[i];
+                // (a hidden token's value must not reach the sum, whatever it is)
+                if (mask && !((shown >> (16 * i + (tid >> 4))) & 1)) reg[2 + i] = u32x4{0u, 0u, 0u, 0u};
+                *reinterpret_cast<u32x4*>(to + v_to + 16 * i * L::kValRow) = reg[2 + i];
             }
         }
     };
 
-    f32x16 o[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
-    float m = -INFINITY, vref = kNoScale;
-    constexpr float kUp = q8 ? 7.f : 0.f;        // weights of the maximum are 2^7
-
     if (u0 < u1) {
+        look_up(u0);
+        request_mask(u0);
         request(u0);
-        lay(0);
-    }
-    __syncthreads();
-    int buf = 0;
-    for (int u = u0; u < u1; u += kTile, buf ^= 1) {
-        if (u + kTile < u1) request(u + kTile);
-        int t0[kTile];
-#pragma unroll
-        for (int i = 0; i < kTile; ++i) t0[i] = u + i < u1 ? block_of(u + i) * kBlk : 0x7FFFFF00;
-        uint64_t shown = ~0ull;
-        if (!q8 && a.mask) {
-            const int t = t0[0] + lane;
-            const bool on = t < see.T && a.mask[(int64_t)b * a.mask_sb + t] != 0;
-            shown = __builtin_amdgcn_ballot_w64(on);
-        }
-        // (a wavefront whose rows see none of the step's tokens has nothing to do)
-        if (live && t0[0] < lim_hi && shown != 0) {
-            f32x16 s[kTile];
-            float c[kTile], d[kTile], vl[kTile];
-#pragma unroll
-            for (int i = 0; i < kTile; ++i) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[i][e] = 0.f;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const u32x4 kf = lk[buf][i][j][q8 ? lane : half * 32 + (col ^ (2 * j + half))];
-                    s[i] = mma<SRC>(kf, qf[j], s[i]);
-                }
-                c[i] = qc;
-                d[i] = 0.f;
-                vl[i] = kNoScale;
+        look_up(u0 + 1);
+        uint32_t shown = shown_now();
+        lay(0, shown);
+        request_mask(u0 + 1);
+        request(u0 + 1);
+        look_up(u0 + 2);
+        __syncthreads();
+        int step = 0;
+        for (int u = u0; u < u1; ++u, ++step) {
+            const uint32_t shown_next = shown_now();
+            lay(step + 1, shown_next);
+            request_mask(u + 2);
+            request(u + 2);
+            look_up(u + 3);
+            __builtin_amdgcn_sched_barrier(0);
+            const int t0 = block_of(u) * kBlk;
+            // (a wavefront whose rows see none of the block has nothing to do)
+            if (me.live && t0 < me.lim_hi && shown != 0) {
+                f32x16 s;
+                u32x4 p[2];
+                float c = me.qc, vl = kNoScale;
                 if constexpr (q8) {
-                    c[i] = qc * lscale[buf][i][0].x;
-                    vl[i] = lscale[buf][i][0].y;
-                }
-            }
-            bool plain = shown == ~0ull;
-#pragma unroll
-            for (int i = 0; i < kTile; ++i) {
-                plain = plain && t0[i] + kBlk <= lim_lo;
-                if (a.window > 0) plain = plain && (t0[i] >= start_hi || t0[i] + kBlk <= sinks);
-            }
-            float top = NAN;                     // (stays where every score is NaN)
-#pragma unroll
-            for (int i = 0; i < kTile; ++i) {
-                float x = s[i][0];
-#pragma unroll
-                for (int e = 1; e < 16; ++e) x = fmaxf(x, s[i][e]);
-                top = fmaxf(top, x * c[i]);
-            }
-            if (!plain || __builtin_amdgcn_ballot_w64(fabsf(top) >= 0x1p11f) != 0) {
-                // masks, and scores so large that a fused product would differ
-                // from the maximum by more than a rounding of it
-                plain = false;
-                top = -INFINITY;
-#pragma unroll
-                for (int i = 0; i < kTile; ++i)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int in = 8 * (e >> 2) + 4 * half + (e & 3), t = t0[i] + in;
-                        bool on = t < limit;
-                        if (a.window > 0) on = on && (t < sinks || t >= start);
-                        if (!q8) on = on && ((shown >> (i * kBlk + in)) & 1);
-                        const float x = on ? clamped(s[i][e] * c[i]) : -INFINITY;
-                        s[i][e] = x;
-                        top = fmaxf(top, x);
-                    }
-            }
-            top = fmaxf(top, xor_lane<32>(top, lane));
-            // The sums keep the maximum they began with until a score exceeds it
-            // by 8 (weights up to 2^15 then): most steps scale nothing.
-            const float vtop = fmaxf(vl[0], vl[1]);
-            const bool wide = q8 && vtop > vref;
-            if (wide || __builtin_amdgcn_ballot_w64(top > m + 8.f) != 0) {
-                // (row by row: a row's bits do not depend on its neighbours)
-                const float mn = top > m + 8.f ? top : m;
-                float f = m == mn ? 1.f : __builtin_amdgcn_exp2f(m - mn);
-                m = mn;
-                l *= f;
-                if (wide) {
-                    f *= __builtin_amdgcn_exp2f(vref - (vtop + 1.f));
-                    vref = vtop + 1.f;
+                    c *= lscale[step & 1][0];
+                    vl = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(lscale[step & 1][1])));
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) o[i][e] *= f;
-            }
-            const float mu = m == -INFINITY ? 0.f : m;
-            float e0[kTile];
-#pragma unroll
-            for (int i = 0; i < kTile; ++i) {
-                // a block of zeros: any weight will do; below 2^-60 of the largest
-                // scale fp16 weights are 0 in any case
-                if constexpr (q8) d[i] = vl[i] <= kNoScale ? 0.f : fmaxf(vl[i] - vref, -60.f);
-                e0[i] = kUp + d[i] - mu;
-            }
-            if (!plain) {
-#pragma unroll
-                for (int i = 0; i < kTile; ++i) {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) s[i][e] -= mu;
-                    c[i] = 1.f;
-                    e0[i] = kUp + d[i];
+                for (int part = 0; part < 2; ++part) {
+                    u32x4 kf[4];
+                    read_keys<SRC>(keys_at(step), part, lane, kf);
+                    me.scores(s, part, kf);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-            }
-#pragma unroll
-            for (int i = 0; i < kTile; ++i) {
-                float sum = 0.f;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    s[i][e] = __builtin_amdgcn_exp2f(fmaf(s[i][e], c[i], e0[i]));
-                    sum += s[i][e];
-                }
-                l += q8 ? sum * __builtin_amdgcn_exp2f(-d[i]) : sum;
-            }
-#pragma unroll
-            for (int i = 0; i < kTile; ++i)
+                me.block(s, c, vl, t0, shown, lane, p);
 #pragma unroll
                 for (int st = 0; st < 2; ++st) {
-                    const u32x4 pf = {weights2<SRC>(s[i][4 * st], s[i][4 * st + 1]),
-                                      weights2<SRC>(s[i][4 * st + 2], s[i][4 * st + 3]),
-                                      weights2<SRC>(s[i][8 + 4 * st], s[i][9 + 4 * st]),
-                                      weights2<SRC>(s[i][10 + 4 * st], s[i][11 + 4 * st])};
-#pragma unroll
-                    for (int np = 0; np < 4; ++np) {
-                        u32x4 vf;
-                        if constexpr (q8) {
-                            vf = lv[buf][i][np * 2 + st][lane];
-                        } else {
-                            // four rows of 16 channels, transposed: tokens .. + 0..3, then 16 further on
-                            const int rr = (lane >> 2) & 3, x = (lane >> 4) & 1, q4 = lane & 3;
-                            const int t = i * kBlk + 8 * st + 4 * half + rr;
-                            const char* at = reinterpret_cast<const char*>(&lv[buf][0][0][0]) + t * 256 +
-                                             ((4 * np + 2 * x + (q4 >> 1)) ^ (rr << 2)) * 16 + 8 * (q4 & 1);
-                            typedef __attribute__((address_space(3))) i16x4* LdsRows;
-                            const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsRows)(at));
-                            const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsRows)(at + 16 * 256));
-                            const u32x2 l2 = __builtin_bit_cast(u32x2, lo), h2 = __builtin_bit_cast(u32x2, hi);
-                            vf = u32x4{l2[0], l2[1], h2[0], h2[1]};
-                        }
-                        o[np] = mma<SRC>(vf, pf, o[np]);
-                    }
+                    u32x4 vf[4];
+                    __builtin_amdgcn_sched_barrier(0);
+                    read_values<SRC>(values_at(step), st, lane, vf);
+                    me.values(vf, p[st]);
                 }
+            }
+            shown = shown_next;
+            __syncthreads();
         }
-        if (u + kTile < u1) lay(buf ^ 1);
-        __syncthreads();
     }
     if (bad && a.status) atomicOr(a.status, DQ_STATUS_PAGE);
 
+    // (whole vectors up to here: or the loop copies the sums' elements at every turn)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(me.o[i]));
+
     // ------------------------------------------------ results
-    l += xor_lane<32>(l, lane);
-    const float up = q8 ? __builtin_amdgcn_exp2f(vref) : 1.f;
+    const float l = me.l + xor_lane<32>(me.l, lane);
+    const float up = q8 ? __builtin_amdgcn_exp2f(me.vref) : 1.f;
+    const int half = lane >> 5;
     if (whole) {
-        if (!valid) return;
-        // rows that see nothing: zeros
-        const float f = l == 0.f ? 0.f : up / l;
-        uint16_t* p = a.out + (int64_t)b * a.o_sb + (int64_t)token * a.o_st + (int64_t)head * a.o_sh + 4 * half;
+        const int r = r0 + wave * kRowsOf + (lane & 31), token = r / a.G, head = h * a.G + r - token * a.G;
+        if (r >= rows) return;
+        const float f = l == 0.f ? 0.f : up / l; // rows that see nothing: zeros
 #pragma unroll
         for (int np = 0; np < 4; ++np)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t w0 = bf16_two(o[np][4 * i] * f, o[np][4 * i + 1] * f);
-                const uint32_t w1 = bf16_two(o[np][4 * i + 2] * f, o[np][4 * i + 3] * f);
-                uint16_t* x = p + 32 * np + 8 * i;
-                if (a.out_aligned) {
-                    *reinterpret_cast<u32x2*>(x) = u32x2{w0, w1};
-                } else {
-                    x[0] = (uint16_t)w0;
-                    x[1] = (uint16_t)(w0 >> 16);
-                    x[2] = (uint16_t)w1;
-                    x[3] = (uint16_t)(w1 >> 16);
-                }
-            }
+            for (int i = 0; i < 4; ++i)
+                store_row(a, b, token, head, 32 * np + 8 * i + 4 * half,
+                          bf16_two(me.o[np][4 * i] * f, me.o[np][4 * i + 1] * f),
+                          bf16_two(me.o[np][4 * i + 2] * f, me.o[np][4 * i + 3] * f));
         return;
     }
     const int64_t slot = it.slot;
-    float* acc = a.ws_acc + (slot * R + wave * kRowsOf + col) * kD + 4 * half;
+    float* acc = a.ws_acc + (slot * kR + wave * kRowsOf + (lane & 31)) * kD + 4 * half;
 #pragma unroll
     for (int np = 0; np < 4; ++np)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             *reinterpret_cast<f32x4*>(acc + 32 * np + 8 * i) =
-                f32x4{o[np][4 * i] * up, o[np][4 * i + 1] * up, o[np][4 * i + 2] * up, o[np][4 * i + 3] * up};
+                f32x4{me.o[np][4 * i] * up, me.o[np][4 * i + 1] * up, me.o[np][4 * i + 2] * up,
+                      me.o[np][4 * i + 3] * up};
     if (half == 0) {
-        float* ml = a.ws_ml + slot * 2 * R + wave * kRowsOf + col;
-        ml[0] = m;
-        ml[R] = l;
+        float* ml = a.ws_ml + slot * 2 * kR + wave * kRowsOf + (lane & 31);
+        ml[0] = me.m;
+        ml[kR] = l;
     }
 }
 
@@ -700,7 +822,7 @@ struct HostPlan {
 HostPlan host_plan(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t t_cap) {
     HostPlan p;
     const int64_t rows = (int64_t)n_q * (Hq / Hkv);
-    p.rows = rows > 128 ? 256 : 128;
+    p.rows = kR;
     p.segs = (int64_t)B * Hkv * ((rows + p.rows - 1) / p.rows);
     p.pieces = std::max<int64_t>(1, ((int64_t)t_cap / kBlk + kLeast) / kLeast);
     // (a plan that cuts has fewer than kTarget segments, each cut has at most one
@@ -712,10 +834,7 @@ HostPlan host_plan(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t t_ca
 
 template <int SRC>
 void launch_source(const ChunkArgs& a, const HostPlan& p, hipStream_t stream) {
-    if (p.rows == 256)
-        chunk_kernel<SRC, 8><<<dim3((unsigned)p.grid), 512, 0, stream>>>(a);
-    else
-        chunk_kernel<SRC, 4><<<dim3((unsigned)p.grid), 256, 0, stream>>>(a);
+    chunk_kernel<SRC><<<dim3((unsigned)p.grid), kThreads, 0, stream>>>(a);
 }
 
 bool aligned16(const Q8Rows& r) {
@@ -788,10 +907,7 @@ int launch_chunk(const ChunkSource& src, const ChunkCall& c, void* ws, uint32_t*
     // it knows whether the plan cuts)
     if (!c.q_lens && p.segs >= kTarget) return DQ_OK;
     const dim3 grid((unsigned)(((int64_t)c.n_q * c.Hq + 3) / 4), c.B);
-    if (p.rows == 256)
-        chunk_merge_kernel<256><<<grid, 256, 0, stream>>>(a);
-    else
-        chunk_merge_kernel<128><<<grid, 256, 0, stream>>>(a);
+    chunk_merge_kernel<kR><<<grid, 256, 0, stream>>>(a);
     return hip_check("chunk_merge launch", hipGetLastError());
 }
 
