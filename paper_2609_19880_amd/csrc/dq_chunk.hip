@@ -83,12 +83,23 @@ struct Seq {
     int T, n, tiles, units;      // tokens, new tokens, row tiles, most blocks that a row tile sees
 };
 
-template <int R>
+// Sequences of few rows and of many have a kernel each (tiles: 0 for the other's).
+struct Few {
+    static constexpr int kRows = 64;             // of a tile
+    static constexpr bool kFew = true;
+};
+struct Many {
+    static constexpr int kRows = 128;
+    static constexpr bool kFew = false;
+};
+
+template <typename K>
 __device__ __forceinline__ Seq seq_of(const ChunkArgs& a, int b) {
+    constexpr int R = K::kRows;
     Seq s;
     s.T = a.seq_lens ? max(0, min(a.seq_lens[b], a.t_cap)) : a.t_cap;
     s.n = a.q_lens ? max(0, min(a.q_lens[b], a.n_q)) : a.n_q;
-    s.tiles = (s.n * a.G + R - 1) / R;
+    s.tiles = (s.n * a.G <= Few::kRows) == K::kFew ? (s.n * a.G + R - 1) / R : 0;
     const int all = (int)(((int64_t)s.T + kBlk - 1) / kBlk);
     s.units = all;
     if (a.window > 0) {
@@ -105,29 +116,30 @@ struct Item {
 };
 
 // The blocks of one piece, and where item `id` lies.  All lanes agree.
-template <int R>
+template <typename K>
 __device__ __forceinline__ int plan_chunk(const ChunkArgs& a, int lane) {
-    double total = 0, segs = 0;
+    // (sums in fp32: the same bits wherever they are taken; a chunk a millionth too
+    // short adds an item, which the workspace has room for)
+    float total = 0, segs = 0;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
-        double t = 0, s = 0;
+        float t = 0, s = 0;
         if (b0 + lane < a.B) {
-            const Seq q = seq_of<R>(a, b0 + lane);
-            s = q.tiles;
-            t = (double)q.tiles * q.units;
+            const Seq q = seq_of<K>(a, b0 + lane);
+            s = (float)q.tiles;
+            t = s * (float)q.units;
         }
-        total += wave_reduce(t, [](double x, double y) { return x + y; });
-        segs += wave_reduce(s, [](double x, double y) { return x + y; });
+        total += wave_sum(t);
+        segs += wave_sum(s);
     }
-    total *= a.H;
-    segs *= a.H;
-    if (segs >= a.target) return 0x7FFFFFFE;
-    const int c = (int)ceil(total / a.target);
-    return max((c + 1) & ~1, a.least);
+    total *= (float)a.H;
+    segs *= (float)a.H;
+    if (segs >= (float)a.target) return 0x7FFFFFFE;
+    return max((int)ceilf(total / (float)a.target), a.least);
 }
 
 __device__ __forceinline__ int pieces(int units, int chunk) { return max(1, (units - 1) / chunk + 1); }
 
-template <int R>
+template <typename K>
 __device__ __forceinline__ int items_of(const ChunkArgs& a, const Seq& s, int chunk) {
     return s.tiles * pieces(s.units, chunk) * a.H;
 }
@@ -144,12 +156,12 @@ __device__ __forceinline__ int scan64(int v) {         // inclusive sums over th
 
 // Item number `id` of the plan: sequence after sequence, KV head after KV head,
 // the last row tiles (which see most) first, their pieces in order.
-template <int R>
+template <typename K>
 __device__ __forceinline__ Item find_item(const ChunkArgs& a, int id, int lane) {
-    Item it{0, 0, -1, 0, plan_chunk<R>(a, lane), 0};
+    Item it{0, 0, -1, 0, plan_chunk<K>(a, lane), 0};
     int all = 0;
     for (int b0 = 0; b0 < a.B; b0 += kWave)
-        all += wave_sum(b0 + lane < a.B ? items_of<R>(a, seq_of<R>(a, b0 + lane), it.chunk) : 0);
+        all += wave_sum(b0 + lane < a.B ? items_of<K>(a, seq_of<K>(a, b0 + lane), it.chunk) : 0);
     // workgroups go to the 8 XCDs in turn: an XCD takes items that follow each
     // other, which share keys and values in its L2
     const int per = (all + 7) / 8;
@@ -160,8 +172,8 @@ __device__ __forceinline__ Item find_item(const ChunkArgs& a, int id, int lane) 
         Seq s{0, 0, 0, 0};
         int own = 0;
         if (b0 + lane < a.B) {
-            s = seq_of<R>(a, b0 + lane);
-            own = items_of<R>(a, s, it.chunk);
+            s = seq_of<K>(a, b0 + lane);
+            own = items_of<K>(a, s, it.chunk);
         }
         const int upto = before + scan64(own);
         const int last = __builtin_amdgcn_readlane(upto, 63);
@@ -183,12 +195,12 @@ __device__ __forceinline__ Item find_item(const ChunkArgs& a, int id, int lane) 
 }
 
 // The slot of piece 0 of (b, h, tile).
-template <int R>
+template <typename K>
 __device__ __forceinline__ int first_slot(const ChunkArgs& a, int b, int h, int tile, int chunk, int lane) {
     int before = 0;
     for (int b0 = 0; b0 < b; b0 += kWave)
-        before += wave_sum(b0 + lane < b ? items_of<R>(a, seq_of<R>(a, b0 + lane), chunk) : 0);
-    const Seq s = seq_of<R>(a, b);
+        before += wave_sum(b0 + lane < b ? items_of<K>(a, seq_of<K>(a, b0 + lane), chunk) : 0);
+    const Seq s = seq_of<K>(a, b);
     return before + (h * s.tiles + (s.tiles - 1 - tile)) * pieces(s.units, chunk);
 }
 
@@ -477,6 +489,7 @@ struct Rows {
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kR = kWaves * kRowsOf;         // rows of a tile
+static_assert(kR == Many::kRows, "the plan's tiles");
 
 // A step's keys and values (64 tokens) in LDS.  Keys: operand j of a block at
 // kKeyOp j, a lane's 16 bytes at half (kKeyOp / 2) + 16 (token % 32).  Codes
@@ -551,12 +564,12 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
 
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-    const Item it = find_item<kR>(a, (int)blockIdx.x, lane);
+    const Item it = find_item<Many>(a, (int)blockIdx.x, lane);
     if (it.tile < 0) return;
     const int b = __builtin_amdgcn_readfirstlane(it.b), h = __builtin_amdgcn_readfirstlane(it.h);
     const int tile = __builtin_amdgcn_readfirstlane(it.tile), piece = __builtin_amdgcn_readfirstlane(it.c);
     const int chunk = __builtin_amdgcn_readfirstlane(it.chunk);
-    const Seq seq = seq_of<kR>(a, b);
+    const Seq seq = seq_of<Many>(a, b);
     const int rows = seq.n * a.G;                // of the whole sequence
     const int r0 = tile * kR;
     const Sees see = sees(a, seq, r0, min(r0 + kR, rows));
@@ -768,27 +781,266 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
     }
 }
 
+// ------------------------------------------------------ few rows, one sequence
+//
+// Up to 64 rows of a (sequence, KV head): a wavefront takes every eighth block
+// (or every fourth, of one half of the rows) straight from memory and converts
+// it for itself; the wavefronts' sums are joined in LDS at the end.  Bound by
+// memory: a block's codes are requested as soon as the registers of the last
+// one's are free, keys while the weights are computed, values while the next
+// scores are.
+//
+// Values of codes: a lane reads whole 16-byte pieces (two channels 16 apart of 8
+// tokens), so that operand 2 m + e has channels 64 m + 32 (row / 16) + 16 e +
+// row % 16 in its rows.  BF16 rows go through an LDS area of the wavefront's own.
+
+constexpr int kFewWaves = 8;
+constexpr int kFewThreads = kFewWaves * kWave;
+constexpr int kJoinRow = 68;                     // floats: 64 channels, and 4 to keep rows in different banks
+
+template <int SRC>
+__global__ __launch_bounds__(kFewThreads, 2) void few_kernel(ChunkArgs a) {
+    typedef Lds<SRC> L;
+    constexpr bool q8 = L::q8;
+    constexpr int kJoin = kFewWaves * kRowsOf * kJoinRow * 4, kOwn = q8 ? 0 : L::kStage;
+    __shared__ __attribute__((aligned(16))) char lds[kJoin > kFewWaves * kOwn ? kJoin : kFewWaves * kOwn];
+    __shared__ float wm[kFewWaves][kRowsOf], wl[kFewWaves][kRowsOf];
+
+    const int tid = threadIdx.x, lane = tid & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const Item it = find_item<Few>(a, (int)blockIdx.x, lane);
+    if (it.tile < 0) return;
+    const int b = __builtin_amdgcn_readfirstlane(it.b), h = __builtin_amdgcn_readfirstlane(it.h);
+    const int piece = __builtin_amdgcn_readfirstlane(it.c), chunk = __builtin_amdgcn_readfirstlane(it.chunk);
+    const Seq seq = seq_of<Few>(a, b);
+    const int rows = seq.n * a.G;
+    const Sees see = sees(a, seq, 0, rows);
+    const bool whole = pieces(see.count, chunk) == 1;
+    const int u0 = (int)min((int64_t)piece * chunk, (int64_t)0x7FFFFF00);
+    if (u0 >= see.count && piece > 0) return;
+    const int u1 = (int)min((int64_t)u0 + chunk, (int64_t)see.count);
+    const int parts = rows > kRowsOf ? 2 : 1;    // of the rows
+    const int part = wave & (parts - 1), first = wave >> (parts - 1), every = kFewWaves / parts;
+
+    bool bad = false;
+    auto block_of = [&](int u) { return u < see.head ? u : see.from + (u - see.head); };
+    constexpr int kRaw = q8 ? 4 : 8;
+    u32x4 kraw[kRaw], vraw[kRaw];
+    float ks = 0.f, vs = 0.f, ks_next = 0.f, vs_next = 0.f;
+    uint32_t mreg = 0;
+    // codes: as in chunk_kernel; pages a block ahead
+    int page = b;
+    const int per_page = a.pg.bt ? 1 << (a.pg.page_shift - 5) : a.t_cap / kBlk;
+    const int in_page = a.pg.bt ? per_page - 1 : 0x7FFFFFFF, pages = a.pg.bt ? a.pg.num_pages : a.B;
+    const uint32_t page_blocks = (uint32_t)(a.H * per_page);
+    const int64_t head_blocks = (int64_t)h * per_page;
+    const int32_t* table = a.pg.bt ? a.pg.bt + (int64_t)b * a.pg.max_pages : nullptr;
+    const int k_lane = ((lane >> 4) & 1) * 2048 + (lane & 15) * 16 + (lane >> 5) * 256;
+    const int v_lane = ((lane >> 4) & 1) * 1024 + (lane & 15) * 16 + (lane >> 5) * 256;
+    int64_t bi = 0;
+    auto look_up = [&](int u) {
+        if (q8 && table && u < u1) page = scalar_load(table + ((block_of(u) * kBlk) >> a.pg.page_shift));
+    };
+    auto locate = [&](int u) {
+        if constexpr (q8) {
+            if (u >= u1) return;
+            const bool in = (uint32_t)page < (uint32_t)pages;
+            bad = bad || !in;
+            bi = (int64_t)((uint64_t)(uint32_t)(in ? page : 0) * page_blocks) + head_blocks + (block_of(u) & in_page);
+            ks_next = scalar_load(a.ks + bi);
+            vs_next = scalar_load(a.vs + bi);
+        }
+    };
+    auto request = [&](u32x4 (&raw)[kRaw], int u, bool values) {
+        if (u >= u1) return;
+        if constexpr (q8) {
+            GlobalBytes p = (GlobalBytes)(uintptr_t)((values ? a.v : a.k) + bi * kBlkBytes) + (values ? v_lane : k_lane);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                raw[i] = __builtin_nontemporal_load(
+                    reinterpret_cast<GlobalPieces>(p + (values ? (i >> 1) * 2048 + (i & 1) * 512 : i * 512)));
+        } else {
+            const int64_t st = values ? a.v_st : a.k_st;
+            const uint16_t* base = reinterpret_cast<const uint16_t*>(values ? a.v : a.k) +
+                                   b * (values ? a.v_sb : a.k_sb) + h * (values ? a.v_sh : a.k_sh) + 8 * (lane & 15);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int t = u * kBlk + 4 * i + (lane >> 4);
+                raw[i] = u32x4{0u, 0u, 0u, 0u};
+                if (t < see.T) {
+                    const uint16_t* x = base + t * st;
+                    if (a.kv_aligned) {
+                        raw[i] = *reinterpret_cast<const u32x4*>(x);
+                    } else {
+#pragma unroll
+                        for (int w = 0; w < 4; ++w)
+                            raw[i][w] = (uint32_t)x[2 * w] | ((uint32_t)x[2 * w + 1] << 16);
+                    }
+                }
+            }
+        }
+    };
+    const uint8_t* mask = !q8 && a.mask ? a.mask + b * a.mask_sb : nullptr;
+    auto request_mask = [&](int u) {
+        if (mask) {
+            const int t = u * kBlk + (lane & 31);
+            mreg = u < u1 && t < see.T ? mask[t] : 0;
+        }
+    };
+    char* own = lds + wave * kOwn;
+
+    int u = u0 + first;
+    look_up(u);
+    locate(u);
+    request_mask(u);
+    request(kraw, u, false);
+    request(vraw, u, true);
+    look_up(u + every);
+    Rows<SRC> me;
+    me.load(a, see, b, h, part * kRowsOf, rows, lane);
+    for (; u < u1; u += every) {
+        const int t0 = block_of(u) * kBlk;
+        const uint32_t shown = mask ? (uint32_t)__builtin_amdgcn_ballot_w64(mreg != 0) : ~0u;
+        const bool on = t0 < me.lim_hi && shown != 0;
+        f32x16 s = f32x16{};
+        u32x4 p[2];
+        float c = me.qc, vl = kNoScale;
+        if constexpr (q8) {
+            ks = ks_next;
+            vs = vs_next;
+            c *= ks;
+            vl = vs > 0.f ? __builtin_amdgcn_logf(vs) : kNoScale;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const u32x2 w0 = halves4<SRC>(kraw[i][0]), w1 = halves4<SRC>(kraw[i][1]);
+                const u32x2 w2 = halves4<SRC>(kraw[i][2]), w3 = halves4<SRC>(kraw[i][3]);
+                s = mma<SRC>(u32x4{w0[0], w0[1], w1[0], w1[1]}, me.q[2 * i], s);
+                s = mma<SRC>(u32x4{w2[0], w2[1], w3[0], w3[1]}, me.q[2 * i + 1], s);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                *reinterpret_cast<u32x4*>(own + (lane & 15) * (L::kKeyOp / 2) + (4 * i + (lane >> 4)) * 16) = kraw[i];
+            wave_sync();
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                u32x4 kf[4];
+                read_keys<SRC>(own, j, lane, kf);
+                me.scores(s, j, kf);
+            }
+        }
+        request_mask(u + every);
+        locate(u + every);
+        request(kraw, u + every, false);
+        look_up(u + 2 * every);
+        if (on) {
+            me.block(s, c, vl, t0, shown, lane, p);
+            if constexpr (q8) {
+#pragma unroll
+                for (int st = 0; st < 2; ++st)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const u32x4& w = vraw[2 * i + st];
+                        const u32x2 w0 = halves4<SRC>(w[0]), w1 = halves4<SRC>(w[1]);
+                        const u32x2 w2 = halves4<SRC>(w[2]), w3 = halves4<SRC>(w[3]);
+                        me.o[2 * i] = mma<SRC>(u32x4{w0[0], w0[1], w1[0], w1[1]}, p[st], me.o[2 * i]);
+                        me.o[2 * i + 1] = mma<SRC>(u32x4{w2[0], w2[1], w3[0], w3[1]}, p[st], me.o[2 * i + 1]);
+                    }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int t = 4 * i + (lane >> 4);
+                    // (a hidden token's value must not reach the sum, whatever it is)
+                    if (mask && !((shown >> t) & 1)) vraw[i] = u32x4{0u, 0u, 0u, 0u};
+                    *reinterpret_cast<u32x4*>(own + L::kKeys + t * L::kValRow + (lane & 15) * 16) = vraw[i];
+                }
+                wave_sync();
+#pragma unroll
+                for (int st = 0; st < 2; ++st) {
+                    u32x4 vf[4];
+                    read_values<SRC>(own + L::kKeys, st, lane, vf);
+                    me.values(vf, p[st]);
+                }
+            }
+        }
+        wave_sync();
+        request(vraw, u + every, true);
+    }
+    if (bad && a.status) atomicOr(a.status, DQ_STATUS_PAGE);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(me.o[i]));
+
+    // ------------------------------------------------ the wavefronts' sums
+    const int half = lane >> 5, col = lane & 31;
+    const float l = me.l + xor_lane<32>(me.l, lane), up = q8 ? __builtin_amdgcn_exp2f(me.vref) : 1.f;
+    if (half == 0) {
+        wm[wave][col] = me.m;
+        wl[wave][col] = l;
+    }
+    float* join = reinterpret_cast<float*>(lds);
+#pragma unroll
+    for (int m2 = 0; m2 < 2; ++m2) {             // channels 64 m2 ..
+        __syncthreads();                         // (the area may still be read)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int ch = q8 ? 32 * (i >> 1) + 16 * e + 8 * (i & 1) + 4 * half : 32 * e + 8 * i + 4 * half;
+                const f32x16& o = me.o[2 * m2 + e];
+                *reinterpret_cast<f32x4*>(join + (wave * kRowsOf + col) * kJoinRow + ch) =
+                    f32x4{o[4 * i] * up, o[4 * i + 1] * up, o[4 * i + 2] * up, o[4 * i + 3] * up};
+            }
+        __syncthreads();
+        for (int i = tid; i < parts * kRowsOf * 16; i += kFewThreads) {
+            const int r = i >> 4, ch = (i & 15) * 4;
+            if (r >= rows) continue;
+            float top = -INFINITY;
+            for (int w = r >> 5; w < kFewWaves; w += parts) top = fmaxf(top, wm[w][r & 31]);
+            float sum = 0.f;
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+            for (int w = r >> 5; w < kFewWaves; w += parts) {
+                const float mw = wm[w][r & 31], f = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - top);
+                sum = fmaf(wl[w][r & 31], f, sum);
+                acc += *reinterpret_cast<const f32x4*>(join + (w * kRowsOf + (r & 31)) * kJoinRow + ch) * f;
+            }
+            if (whole) {
+                const float f = sum == 0.f ? 0.f : 1.f / sum;    // rows that see nothing: zeros
+                const int token = r / a.G, head = h * a.G + r - token * a.G;
+                store_row(a, b, token, head, 64 * m2 + ch, bf16_two(acc[0] * f, acc[1] * f),
+                          bf16_two(acc[2] * f, acc[3] * f));
+            } else {
+                const int64_t slot = it.slot;
+                *reinterpret_cast<f32x4*>(a.ws_acc + (slot * Few::kRows + r) * kD + 64 * m2 + ch) = acc;
+                if (m2 == 0 && ch == 0) {
+                    a.ws_ml[slot * 2 * Few::kRows + r] = top;
+                    a.ws_ml[slot * 2 * Few::kRows + Few::kRows + r] = sum;
+                }
+            }
+        }
+    }
+}
+
 // The pieces of a row joined: one wavefront per row, two channels a lane.
-template <int R>
-__global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a) {
-    const int lane = threadIdx.x & (kWave - 1);
-    const int b = blockIdx.y;
-    const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
-    const Seq seq = seq_of<R>(a, b);
+template <typename K>
+__device__ __forceinline__ void merge_row(const ChunkArgs& a, int64_t id, int b, int lane) {
+    constexpr int R = K::kRows;
+    const Seq seq = seq_of<K>(a, b);
+    if (seq.tiles == 0) return;
     const int rows = seq.n * a.G;
     if (id >= (int64_t)rows * a.H) return;
     const int h = (int)(id / rows), r = (int)(id % rows), tile = r / R;
-    const int chunk = plan_chunk<R>(a, lane);
+    const int chunk = plan_chunk<K>(a, lane);
     const Sees see = sees(a, seq, tile * R, min(tile * R + R, rows));
     const int nc = pieces(see.count, chunk);
     if (nc == 1) return;
-    const int64_t slot = first_slot<R>(a, b, h, tile, chunk, lane);
+    const int64_t slot = first_slot<K>(a, b, h, tile, chunk, lane);
     const float* ml = a.ws_ml + slot * 2 * R + r % R;
     float top = -INFINITY;
     for (int c = lane; c < nc; c += kWave) top = fmaxf(top, ml[(int64_t)c * 2 * R]);
     top = wave_max(top);
     float l = 0.f, x = 0.f, y = 0.f;
     const float* acc = a.ws_acc + (slot * R + r % R) * kD + 2 * lane;
+#pragma unroll 4
     for (int c = 0; c < nc; ++c) {
         const float mc = ml[(int64_t)c * 2 * R];
         const float w = mc == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - top);
@@ -809,32 +1061,49 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a) {
     }
 }
 
+__global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs few, ChunkArgs many) {
+    const int lane = threadIdx.x & (kWave - 1);
+    const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
+    if (few.target) merge_row<Few>(few, id, blockIdx.y, lane);
+    if (many.target) merge_row<Many>(many, id, blockIdx.y, lane);
+}
+
 // ------------------------------------------------------------------- host
 
 constexpr int kTarget = 512;                 // work items wanted: two per CU
 constexpr int kLeast = 8;                    // blocks of one piece, at least
 
+// A kernel's part of the work, as far as the host knows it.
 struct HostPlan {
+    bool runs;
     int rows;                    // per tile
-    int64_t segs, pieces, slots, grid;
+    int64_t segs, slots, grid;
+
+    int64_t floats() const { return slots * rows * (kD + 2); }
 };
 
-HostPlan host_plan(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t t_cap) {
+template <typename K>
+HostPlan host_plan(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t t_cap, bool lens) {
     HostPlan p;
     const int64_t rows = (int64_t)n_q * (Hq / Hkv);
-    p.rows = kR;
-    p.segs = (int64_t)B * Hkv * ((rows + p.rows - 1) / p.rows);
-    p.pieces = std::max<int64_t>(1, ((int64_t)t_cap / kBlk + kLeast) / kLeast);
+    // chunks of unlike lengths may be of either kind
+    p.runs = K::kFew ? rows <= Few::kRows || lens : rows > Few::kRows;
+    p.rows = K::kRows;
+    p.segs = (int64_t)B * Hkv * (K::kFew ? 1 : (rows + p.rows - 1) / p.rows);
+    const int64_t pieces = std::max<int64_t>(1, ((int64_t)t_cap / kBlk + kLeast) / kLeast);
     // (a plan that cuts has fewer than kTarget segments, each cut has at most one
     // piece more than an even share of the items wanted)
-    p.slots = p.pieces == 1 ? 0 : std::min<int64_t>(2 * kTarget, p.segs * p.pieces);
+    p.slots = pieces == 1 || !p.runs ? 0 : std::min<int64_t>(2 * kTarget + 8, p.segs * pieces);
     p.grid = (std::max(p.segs, p.slots) + 7) / 8 * 8;
     return p;
 }
 
 template <int SRC>
-void launch_source(const ChunkArgs& a, const HostPlan& p, hipStream_t stream) {
-    chunk_kernel<SRC><<<dim3((unsigned)p.grid), kThreads, 0, stream>>>(a);
+int launch_source(const ChunkArgs& few, const HostPlan& pf, const ChunkArgs& many, const HostPlan& pm,
+                  hipStream_t stream) {
+    if (pf.runs) few_kernel<SRC><<<dim3((unsigned)pf.grid), kFewThreads, 0, stream>>>(few);
+    if (pm.runs) chunk_kernel<SRC><<<dim3((unsigned)pm.grid), kThreads, 0, stream>>>(many);
+    return hip_check("chunk launch", hipGetLastError());
 }
 
 bool aligned16(const Q8Rows& r) {
@@ -844,12 +1113,14 @@ bool aligned16(const Q8Rows& r) {
 }  // namespace
 
 size_t chunk_workspace_bytes(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t t_cap) {
-    const HostPlan p = host_plan(B, n_q, Hq, Hkv, t_cap);
-    return (size_t)p.slots * p.rows * (kD + 2) * sizeof(float);
+    // (with or without lengths of the chunks: the larger)
+    return (size_t)(host_plan<Few>(B, n_q, Hq, Hkv, t_cap, true).floats() +
+                    host_plan<Many>(B, n_q, Hq, Hkv, t_cap, true).floats()) * sizeof(float);
 }
 
 int launch_chunk(const ChunkSource& src, const ChunkCall& c, void* ws, uint32_t* status, hipStream_t stream) {
-    const HostPlan p = host_plan(c.B, c.n_q, c.Hq, c.Hkv, c.t_cap);
+    const HostPlan pf = host_plan<Few>(c.B, c.n_q, c.Hq, c.Hkv, c.t_cap, c.q_lens != nullptr);
+    const HostPlan pm = host_plan<Many>(c.B, c.n_q, c.Hq, c.Hkv, c.t_cap, c.q_lens != nullptr);
     ChunkArgs a;
     a.q = c.q.p;
     a.q_sb = c.q.sb;
@@ -893,21 +1164,28 @@ int launch_chunk(const ChunkSource& src, const ChunkCall& c, void* ws, uint32_t*
     a.target = kTarget;
     a.least = kLeast;
     a.status = status;
-    a.ws_acc = static_cast<float*>(ws);
-    a.ws_ml = a.ws_acc + p.slots * p.rows * kD;
+    ChunkArgs few = a, many = a;
+    few.ws_acc = static_cast<float*>(ws);
+    few.ws_ml = few.ws_acc + pf.slots * pf.rows * kD;
+    many.ws_acc = few.ws_acc + pf.floats();
+    many.ws_ml = many.ws_acc + pm.slots * pm.rows * kD;
+    int rc;
     if (src.format == DQ_Q8_E4M3)
-        launch_source<DQ_Q8_E4M3>(a, p, stream);
+        rc = launch_source<DQ_Q8_E4M3>(few, pf, many, pm, stream);
     else if (src.format == DQ_Q8_INT8)
-        launch_source<DQ_Q8_INT8>(a, p, stream);
+        rc = launch_source<DQ_Q8_INT8>(few, pf, many, pm, stream);
     else
-        launch_source<kChunkBf16>(a, p, stream);
-    if (int rc = hip_check("chunk launch", hipGetLastError())) return rc;
-    if (p.slots == 0) return DQ_OK;
-    // (segments are as many as the host counts where all chunks are full: then
-    // it knows whether the plan cuts)
-    if (!c.q_lens && p.segs >= kTarget) return DQ_OK;
+        rc = launch_source<kChunkBf16>(few, pf, many, pm, stream);
+    if (rc != DQ_OK) return rc;
+    // nothing to join where nothing can be cut (segments are as many as the host
+    // counts where all chunks are full)
+    const bool fm = pf.slots > 0 && (c.q_lens || pf.segs < kTarget);
+    const bool mm = pm.slots > 0 && (c.q_lens || pm.segs < kTarget);
+    if (!fm && !mm) return DQ_OK;
+    if (!fm) few.target = 0;
+    if (!mm) many.target = 0;
     const dim3 grid((unsigned)(((int64_t)c.n_q * c.Hq + 3) / 4), c.B);
-    chunk_merge_kernel<kR><<<grid, 256, 0, stream>>>(a);
+    chunk_merge_kernel<<<grid, 256, 0, stream>>>(few, many);
     return hip_check("chunk_merge launch", hipGetLastError());
 }
 
