@@ -65,7 +65,7 @@ struct ChunkArgs {
     int q_aligned, kv_aligned, out_aligned;
     float scale_log2;            // |softmax scale| log2 e
     int negative;                // the softmax scale is
-    int target, least;           // work items wanted, fewest blocks of one
+    int cuts;                    // pieces may be cut (0: every segment is one item)
     uint32_t* status;
     float* ws_acc;               // [slot][rows][128]
     float* ws_ml;                // [slot][2][rows]
@@ -74,10 +74,10 @@ struct ChunkArgs {
 // ------------------------------------------------------------------- shares
 //
 // A segment is a tile of rows of one (sequence, KV head).  Where there are
-// fewer segments than the GPU takes at a time, their tokens are cut into
-// pieces of `chunk` blocks, so that there are about `target` work items; the
-// pieces of a row are joined by the merge kernel.  Lengths are known on the
-// device only, so every workgroup derives the same plan from them.
+// fewer segments than would fill the GPU twice, their tokens are cut into
+// pieces of `chunk` blocks; the pieces of a row are joined by the merge kernel.
+// Lengths are known on the device only, so every workgroup derives the same
+// plan from them.
 
 struct Seq {
     int T, n, tiles, units;      // tokens, new tokens, row tiles, most blocks that a row tile sees
@@ -87,11 +87,16 @@ struct Seq {
 struct Few {
     static constexpr int kRows = 64;             // of a tile
     static constexpr bool kFew = true;
+    static constexpr int kAtOnce = 256;          // workgroups that the GPU takes at a time
+    static constexpr int kCost = 16;             // what an item costs besides its blocks, in blocks
 };
 struct Many {
     static constexpr int kRows = 128;
     static constexpr bool kFew = false;
+    static constexpr int kAtOnce = 768;
+    static constexpr int kCost = 8;
 };
+constexpr int kLeast = 8;                        // blocks of one piece, at least
 
 template <typename K>
 __device__ __forceinline__ Seq seq_of(const ChunkArgs& a, int b) {
@@ -115,26 +120,42 @@ struct Item {
     int chunk, slot;
 };
 
-// The blocks of one piece, and where item `id` lies.  All lanes agree.
+// The blocks of one piece.  All lanes agree.
 template <typename K>
 __device__ __forceinline__ int plan_chunk(const ChunkArgs& a, int lane) {
+    if (!a.cuts) return 0x7FFFFFFE;
     // (sums in fp32: the same bits wherever they are taken; a chunk a millionth too
     // short adds an item, which the workspace has room for)
     float total = 0, segs = 0;
+    int longest = 0;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
         float t = 0, s = 0;
+        int n = 0;
         if (b0 + lane < a.B) {
             const Seq q = seq_of<K>(a, b0 + lane);
             s = (float)q.tiles;
             t = s * (float)q.units;
+            n = q.tiles ? q.units : 0;
         }
         total += wave_sum(t);
         segs += wave_sum(s);
+        longest = max(longest, wave_max(n));
     }
     total *= (float)a.H;
     segs *= (float)a.H;
-    if (segs >= (float)a.target) return 0x7FFFFFFE;
-    return max((int)ceilf(total / (float)a.target), a.least);
+    constexpr float kMost = 2 * K::kAtOnce;
+    if (segs >= kMost) return 0x7FFFFFFE;
+    if (total < 0.75f * segs * (float)longest) {
+        // unlike lengths leave pieces that are not full: small ones even out the end
+        return max((int)ceilf(total / kMost), kLeast);
+    }
+    // lane l tries l + 1 pieces per segment: rounds, and what one takes
+    const int c = max((int)((uint32_t)(longest + lane) / (uint32_t)(lane + 1)), kLeast);
+    const float items = segs * (float)((uint32_t)(longest + c - 1) / (uint32_t)c);
+    float cost = ceilf(items / K::kAtOnce) * (float)(c + K::kCost);
+    if (items > kMost && lane > 0) cost = 3e38f;
+    const float least = wave_min(cost);
+    return max(1, __builtin_amdgcn_readlane(c, __builtin_ctzll(__builtin_amdgcn_ballot_w64(cost == least))));
 }
 
 __device__ __forceinline__ int pieces(int units, int chunk) { return max(1, (units - 1) / chunk + 1); }
@@ -155,53 +176,45 @@ __device__ __forceinline__ int scan64(int v) {         // inclusive sums over th
 }
 
 // Item number `id` of the plan: sequence after sequence, KV head after KV head,
-// the last row tiles (which see most) first, their pieces in order.
-template <typename K>
+// the last row tiles (which see most) first, their pieces in order.  Or segment
+// number `id` (SEGMENT), with its first piece.
+template <typename K, bool SEGMENT>
 __device__ __forceinline__ Item find_item(const ChunkArgs& a, int id, int lane) {
     Item it{0, 0, -1, 0, plan_chunk<K>(a, lane), 0};
-    int all = 0;
-    for (int b0 = 0; b0 < a.B; b0 += kWave)
-        all += wave_sum(b0 + lane < a.B ? items_of<K>(a, seq_of<K>(a, b0 + lane), it.chunk) : 0);
-    // workgroups go to the 8 XCDs in turn: an XCD takes items that follow each
-    // other, which share keys and values in its L2
-    const int per = (all + 7) / 8;
-    const int x = (id & 7) * per + (id >> 3);
-    if ((id >> 3) >= per || x >= all) return it;
-    int before = 0;
+    auto at = [&](int b0) { return b0 + lane < a.B ? seq_of<K>(a, b0 + lane) : Seq{0, 0, 0, 0}; };
+    int x = id;
+    if (!SEGMENT) {
+        int all = 0;
+        for (int b0 = 0; b0 < a.B; b0 += kWave) all += wave_sum(items_of<K>(a, at(b0), it.chunk));
+        // workgroups go to the 8 XCDs in turn: an XCD takes items that follow each
+        // other, which share keys and values in its L2
+        const int per = (all + 7) / 8;
+        x = (id & 7) * per + (id >> 3);
+        if ((id >> 3) >= per || x >= all) return it;
+    }
+    int before = 0, slots = 0;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
-        Seq s{0, 0, 0, 0};
-        int own = 0;
-        if (b0 + lane < a.B) {
-            s = seq_of<K>(a, b0 + lane);
-            own = items_of<K>(a, s, it.chunk);
-        }
+        const Seq s = at(b0);
+        const int own_items = items_of<K>(a, s, it.chunk), own = SEGMENT ? s.tiles * a.H : own_items;
         const int upto = before + scan64(own);
         const int last = __builtin_amdgcn_readlane(upto, 63);
+        const int held = SEGMENT ? slots + scan64(own_items) : upto;
         if (x < last) {
             const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > x));
             const int r = x - __builtin_amdgcn_readlane(upto - own, l);
             const int nc = pieces(__builtin_amdgcn_readlane(s.units, l), it.chunk);
-            const int tiles = __builtin_amdgcn_readlane(s.tiles, l);
+            const int tiles = __builtin_amdgcn_readlane(s.tiles, l), each = SEGMENT ? 1 : nc;
             it.b = b0 + l;
-            it.h = r / (tiles * nc);
-            it.tile = tiles - 1 - (r / nc) % tiles;
-            it.c = r % nc;
-            it.slot = x;
+            it.h = r / (tiles * each);
+            it.tile = tiles - 1 - (r / each) % tiles;
+            it.c = r % each;
+            it.slot = SEGMENT ? __builtin_amdgcn_readlane(held - own_items, l) + r * nc : x;
             return it;
         }
         before = last;
+        slots = SEGMENT ? __builtin_amdgcn_readlane(held, 63) : 0;
     }
     return it;
-}
-
-// The slot of piece 0 of (b, h, tile).
-template <typename K>
-__device__ __forceinline__ int first_slot(const ChunkArgs& a, int b, int h, int tile, int chunk, int lane) {
-    int before = 0;
-    for (int b0 = 0; b0 < b; b0 += kWave)
-        before += wave_sum(b0 + lane < b ? items_of<K>(a, seq_of<K>(a, b0 + lane), chunk) : 0);
-    const Seq s = seq_of<K>(a, b);
-    return before + (h * s.tiles + (s.tiles - 1 - tile)) * pieces(s.units, chunk);
 }
 
 // Blocks that rows [r0, r1) of a sequence see: the first `head`, then those
@@ -313,7 +326,8 @@ struct Rows {
     u32x4 q[8];
     f32x16 o[4];
     float m, l, vref, qc;        // vref: log2 of the scale that the values are relative to
-    int limit, start, sinks;     // the row sees t < limit, of those t < sinks or t >= start
+    int end;                     // the row sees t < end, of those t < sinks or t >= end - window
+    int T, window, sinks;
     int lim_lo, lim_hi, start_hi;
     bool live, careful;   // careful: a row has no maximum yet, or one of 2^11 or more
 
@@ -322,12 +336,14 @@ struct Rows {
         const bool valid = r < rows;
         const int row = min(r, rows - 1), token = row / a.G, head = h * a.G + (row - token * a.G);
         live = r0 < rows;
-        limit = a.causal ? max(0, min(see.T, see.off + token + 1)) : see.T;
-        start = a.window > 0 ? (int)max((int64_t)0, (int64_t)see.off + token + 1 - a.window) : 0;
+        T = see.T;
+        window = a.window > 0 ? a.window : 0x7FFFFFFF;
         sinks = a.sinks;
-        lim_lo = __builtin_amdgcn_readfirstlane(limit);                          // rows are in order
-        lim_hi = __builtin_amdgcn_readlane(limit, 31);
-        start_hi = __builtin_amdgcn_readlane(start, 31);
+        end = a.causal ? see.off + token + 1 : T;                                // (may be negative)
+        auto start = [&](int e) { return e <= window ? 0 : e - window; };
+        lim_lo = max(0, min(T, __builtin_amdgcn_readfirstlane(end)));            // rows are in order
+        lim_hi = max(0, min(T, __builtin_amdgcn_readlane(end, 31)));
+        start_hi = start(__builtin_amdgcn_readlane(end, 31));
         m = -INFINITY;
         l = 0.f;
         vref = kNoScale;
@@ -361,7 +377,7 @@ struct Rows {
                     top = max(top, max((int)(q[j][i] & 0x7FFFu), (int)((q[j][i] >> 16) & 0x7FFFu)));
             top = max(top, __float_as_int(xor_lane<32>(__int_as_float(top), lane)));
             const bool nan = top >= 0x7F80;      // infinities and NaN make the row NaN
-            if (nan && limit > 0) l = NAN;
+            if (nan && end > 0 && T > 0) l = NAN;
             const int up = 13 - (top >= 0x80 ? (top >> 7) - 127 : -126);
             qc = ldexpf(qc, -up);
 #pragma unroll
@@ -406,43 +422,39 @@ struct Rows {
     // weight will do).
     __device__ __forceinline__ void block(f32x16& s, float c, float vl, int t0, uint32_t shown, int lane,
                                           u32x4 (&p)[2]) {
-        const bool masked = shown != ~0u || t0 + kBlk > lim_lo || (start_hi > 0 && t0 < start_hi && t0 + kBlk > sinks);
+        c = fmaxf(c, 0x1p-120f);                 // (a factor of 0, which hidden scores could not bear)
+        if (shown != ~0u || t0 + kBlk > lim_lo || (start_hi > 0 && t0 < start_hi && t0 + kBlk > sinks)) {
+            auto below = [&](int t) { return t <= t0 ? 0u : t - t0 >= kBlk ? ~0u : (1u << (t - t0)) - 1u; };
+            const uint32_t past = end <= window ? 0u : below(end - window);
+            const uint32_t vis = (shown & below(min(end, T)) & (~past | below(sinks))) >> (4 * (lane >> 5));
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = (vis >> (8 * (e >> 2) + (e & 3))) & 1 ? s[e] : -INFINITY;
+        }
         float d = 0.f;
         if constexpr (q8) d = vl <= kNoScale ? 0.f : fmaxf(vl - vref, -60.f);
         float sum = weigh(s, c, kUp + d - mu(), p);
-        bool again = masked || careful;
+        bool again = careful;
         // (weights that fp16 would lose need their sum in fp32)
         if constexpr (q8) again = again || !(d >= -2.f && d <= 0.f);
-        if (again || __builtin_amdgcn_ballot_w64(sum > kMost) != 0) sum = anew(s, c, sum, vl, d, t0, shown, masked, lane, p);
+        if (again || __builtin_amdgcn_ballot_w64(sum > kMost) != 0) sum = anew(s, c, sum, vl, d, lane, p);
         l += q8 ? sum * __builtin_amdgcn_exp2f(-d) : sum;
     }
 
-    // The same with masks, a new maximum or a new scale; d becomes the block's.
-    // sum: of the weights without them.
-    __device__ __forceinline__ float anew(f32x16& s, float c, float sum, float vl, float& d, int t0, uint32_t shown,
-                                          bool masked, int lane, u32x4 (&p)[2]) {
-        // (the empty statement keeps what masks need in here: outside the loop it
-        // would take registers that every block is short of)
-        int half = lane >> 5;
-        asm volatile("" : "+v"(half));
+    // The same with a new maximum or a new scale; d becomes the block's.  sum: of
+    // the weights without them.  (Selections rather than branches, and one place
+    // that scales the sums: with branches the compiler keeps both results.)
+    __device__ __forceinline__ float anew(f32x16& s, float c, float sum, float vl, float& d, int lane, u32x4 (&p)[2]) {
         float top = s[0];                        // (NaN where every score is)
 #pragma unroll
         for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
         top *= c;
         // scores so large that a fused product would differ from the maximum by
         // more than a rounding of it
-        const bool exact = masked || __builtin_amdgcn_ballot_w64(fmaxf(fabsf(mu()), fabsf(top)) >= 0x1p11f) != 0;
-        if (exact) {
-            top = -INFINITY;
+        const float high = top == -INFINITY ? 0.f : fabsf(top);
+        const bool exact = __builtin_amdgcn_ballot_w64(fmaxf(fabsf(mu()), high) >= 0x1p11f) != 0;
+        top = top == -INFINITY ? top : clamped(top);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int in = 8 * (e >> 2) + 4 * half + (e & 3), t = t0 + in;
-                const bool on = (t < limit) & ((t >= start) | (t < sinks)) & (((shown >> in) & 1) != 0);
-                s[e] = on ? clamped(s[e] * c) : -INFINITY;
-                top = fmaxf(top, s[e]);
-            }
-            c = 1.f;
-        }
+        for (int e = 0; e < 16; ++e) s[e] = exact && s[e] != -INFINITY ? clamped(s[e] * c) : s[e];
         top = fmaxf(top, xor_lane<32>(top, lane));
         sum = fmaxf(sum, xor_lane<32>(sum, lane));
         const bool higher = (m == -INFINITY || (exact ? top > m + 4.f : sum > kMost)) && top > m;
@@ -461,14 +473,11 @@ struct Rows {
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] *= f;
         careful = __builtin_amdgcn_ballot_w64(!(fabsf(m) < 0x1p11f)) != 0;
-        float e0 = kUp + d;
-        if (exact) {
-            // (large scores: the difference first, which is exact where it counts)
+        // (large scores: the difference first, which is exact where it counts)
+        const float less = exact ? mu() : 0.f, e0 = exact ? kUp + d : kUp + d - mu();
+        c = exact ? 1.f : c;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] -= mu();
-        } else {
-            e0 -= mu();
-        }
+        for (int e = 0; e < 16; ++e) s[e] -= less;
         const float rounded = weigh(s, c, e0, p);
         if (!q8 || d >= -2.f) return rounded;
         float all = 0.f;
@@ -486,10 +495,6 @@ struct Rows {
 
 // -------------------------------------------------------------- the kernel
 
-constexpr int kWaves = 4;
-constexpr int kThreads = kWaves * kWave;
-constexpr int kR = kWaves * kRowsOf;         // rows of a tile
-static_assert(kR == Many::kRows, "the plan's tiles");
 
 // A step's keys and values (64 tokens) in LDS.  Keys: operand j of a block at
 // kKeyOp j, a lane's 16 bytes at half (kKeyOp / 2) + 16 (token % 32).  Codes
@@ -508,6 +513,7 @@ struct Lds {
 
 typedef const __attribute__((address_space(1))) uint8_t* GlobalBytes;
 typedef const __attribute__((address_space(1))) float* GlobalFloats;
+typedef const __attribute__((address_space(1))) int32_t* GlobalInts;
 typedef const __attribute__((address_space(1))) u32x4* GlobalPieces;
 
 template <int SRC>
@@ -550,29 +556,88 @@ __device__ __forceinline__ void store_row(const ChunkArgs& a, int b, int token, 
     }
 }
 
-// One workgroup of four wavefronts per item: 128 rows, 32 per wavefront, three
-// workgroups per CU.  A step is a block of 32 tokens: its codes are read,
-// converted to fp16 once for the workgroup and laid into LDS as the products
-// take them, while the step before it is worked on: one barrier per step.
+constexpr int kThreads = 4 * kWave;
+
+// The sums of a workgroup's wavefronts joined in LDS and written: wavefront w has
+// rows 32 (w % parts) .. of the tokens that it has seen.  PAIRED: operand 2 m + e
+// has channels 64 m + 32 (row / 16) + 16 e + row % 16, else 32 (2 m + e) + row.
+constexpr int kJoinRow = 68;                     // floats: 64 channels, and 4 to keep rows in different banks
+
+template <typename K, int WAVES, bool PAIRED>
+__device__ __forceinline__ void join_rows(const ChunkArgs& a, const f32x16 (&o)[4], float m, float l, float up,
+                                          float* join, float (&wm)[WAVES][kRowsOf], float (&wl)[WAVES][kRowsOf],
+                                          int parts, int rows, int r0, int b, int h, bool whole, int64_t slot) {
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, half = lane >> 5, col = lane & 31;
+    if (half == 0) {
+        wm[wave][col] = m;
+        wl[wave][col] = l;
+    }
+#pragma unroll
+    for (int m2 = 0; m2 < 2; ++m2) {             // channels 64 m2 ..
+        __syncthreads();                         // (the area may still be read)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int ch = PAIRED ? 32 * (i >> 1) + 16 * e + 8 * (i & 1) + 4 * half : 32 * e + 8 * i + 4 * half;
+                const f32x16& x = o[2 * m2 + e];
+                *reinterpret_cast<f32x4*>(join + (wave * kRowsOf + col) * kJoinRow + ch) =
+                    f32x4{x[4 * i] * up, x[4 * i + 1] * up, x[4 * i + 2] * up, x[4 * i + 3] * up};
+            }
+        __syncthreads();
+        for (int i = tid; i < parts * kRowsOf * 16; i += WAVES * kWave) {
+            const int in = i >> 4, ch = (i & 15) * 4, r = r0 + in;
+            if (r >= rows) break;
+            float top = -INFINITY;
+            for (int w = in >> 5; w < WAVES; w += parts) top = fmaxf(top, wm[w][in & 31]);
+            float sum = 0.f;
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+            for (int w = in >> 5; w < WAVES; w += parts) {
+                const float mw = wm[w][in & 31], f = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - top);
+                sum = fmaf(wl[w][in & 31], f, sum);
+                acc += *reinterpret_cast<const f32x4*>(join + (w * kRowsOf + (in & 31)) * kJoinRow + ch) * f;
+            }
+            if (whole) {
+                const float f = sum == 0.f ? 0.f : 1.f / sum;    // rows that see nothing: zeros
+                const int token = r / a.G, head = h * a.G + r - token * a.G;
+                store_row(a, b, token, head, 64 * m2 + ch, bf16_two(acc[0] * f, acc[1] * f),
+                          bf16_two(acc[2] * f, acc[3] * f));
+            } else {
+                *reinterpret_cast<f32x4*>(a.ws_acc + (slot * K::kRows + in) * kD + 64 * m2 + ch) = acc;
+                if (m2 == 0 && ch == 0) {
+                    a.ws_ml[slot * 2 * K::kRows + in] = top;
+                    a.ws_ml[slot * 2 * K::kRows + K::kRows + in] = sum;
+                }
+            }
+        }
+    }
+}
+
+// One workgroup of four wavefronts per item: 128 rows, 32 per wavefront.  A
+// block's codes are read, converted to fp16 once for the workgroup and laid into
+// LDS as the products take them while the block before is worked on: one barrier
+// per block.  Three wavefronts per SIMD, of three workgroups, hide one another's
+// waits; more would leave too few registers for the sums (64), the queries (32)
+// and a block's scores.
 template <int SRC>
 __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
     typedef Lds<SRC> L;
     constexpr bool q8 = L::q8;
-    constexpr int kPieces = q8 ? 2 : 4;          // 16-byte pieces per thread and step: keys, then values
+    constexpr int kPieces = q8 ? 2 : 4;          // 16-byte pieces per thread and block: keys, then values
     __shared__ __attribute__((aligned(16))) char lds[2 * L::kStage];
-    __shared__ float lscale[2][2];               // the keys' scale, log2 of the values'
+    __shared__ float2 lscale[2];                 // the keys' scale, log2 of the values'
 
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-    const Item it = find_item<Many>(a, (int)blockIdx.x, lane);
+    const Item it = find_item<Many, false>(a, (int)blockIdx.x, lane);
     if (it.tile < 0) return;
     const int b = __builtin_amdgcn_readfirstlane(it.b), h = __builtin_amdgcn_readfirstlane(it.h);
     const int tile = __builtin_amdgcn_readfirstlane(it.tile), piece = __builtin_amdgcn_readfirstlane(it.c);
     const int chunk = __builtin_amdgcn_readfirstlane(it.chunk);
     const Seq seq = seq_of<Many>(a, b);
     const int rows = seq.n * a.G;                // of the whole sequence
-    const int r0 = tile * kR;
-    const Sees see = sees(a, seq, r0, min(r0 + kR, rows));
+    const int r0 = tile * Many::kRows;
+    const Sees see = sees(a, seq, r0, min(r0 + Many::kRows, rows));
     const bool whole = pieces(see.count, chunk) == 1;
     const int u0 = (int)min((int64_t)piece * chunk, (int64_t)0x7FFFFF00);
     if (u0 >= see.count && piece > 0) return;    // the merge does not ask for it
@@ -585,19 +650,22 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
     bool bad = false;
     auto block_of = [&](int u) { return u < see.head ? u : see.from + (u - see.head); };
     u32x4 reg[kPieces];
-    // Codes: pages are looked up a step before they are needed, and scales are
-    // read by lanes 0 and 1 of wavefront 0 (keys, values): nothing here waits for
-    // memory.  Block `at` lies at page (H per_page) + h per_page + at % per_page;
-    // without a table the sequence is the page.
-    float sreg = 0.f;
+    // Codes: pages are looked up a block before they are needed, in the vector
+    // loads' order, and the scales come with the codes: nothing here waits for
+    // memory, as a scalar load would make every wait for LDS do.  Block `at` lies
+    // at page (H per_page) + h per_page + at % per_page; without a table the
+    // sequence is the page.
+    float ks = 0.f, vs = 0.f;
     int page = b;
     const int per_page = a.pg.bt ? 1 << (a.pg.page_shift - 5) : a.t_cap / kBlk;
     const int in_page = a.pg.bt ? per_page - 1 : 0x7FFFFFFF, pages = a.pg.bt ? a.pg.num_pages : a.B;
     const uint32_t page_blocks = (uint32_t)(a.H * per_page);
     const int64_t head_blocks = (int64_t)h * per_page;
-    const int32_t* table = a.pg.bt ? a.pg.bt + (int64_t)b * a.pg.max_pages : nullptr;
+    GlobalInts table = (GlobalInts)(uintptr_t)(a.pg.bt + (a.pg.bt ? (int64_t)b * a.pg.max_pages : 0));
     GlobalBytes k_codes = (GlobalBytes)(uintptr_t)a.k, v_codes = (GlobalBytes)(uintptr_t)a.v;
-    GlobalFloats scale_of = (GlobalFloats)(uintptr_t)(lane & 1 ? a.vs : a.ks);
+    GlobalFloats k_scales = (GlobalFloats)(uintptr_t)a.ks, v_scales = (GlobalFloats)(uintptr_t)a.vs;
+    uint32_t none = 0;                           // an offset that the compiler takes for a lane's
+    asm("" : "+v"(none));
     // BF16: this thread's piece of rows 16 i + tid / 16
     const uint16_t* k_row = nullptr;
     const uint16_t* v_row = nullptr;
@@ -609,7 +677,7 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
         v_row = reinterpret_cast<const uint16_t*>(a.v) + b * a.v_sb + h * a.v_sh + (tid >> 4) * v_st + 8 * (tid & 15);
     }
     auto look_up = [&](int u) {
-        if (q8 && table && u < u1) page = scalar_load(table + ((block_of(u) * kBlk) >> a.pg.page_shift));
+        if (q8 && a.pg.bt && u < u1) page = table[((block_of(u) * kBlk) >> a.pg.page_shift) + none];
     };
     // requests block u
     auto request = [&](int u) {
@@ -617,13 +685,20 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
         for (int i = 0; i < kPieces; ++i) reg[i] = u32x4{0u, 0u, 0u, 0u};
         if (u >= u1) return;
         if constexpr (q8) {
-            const bool in = (uint32_t)page < (uint32_t)pages;
+            const int at = __builtin_amdgcn_readfirstlane(page);
+            const bool in = (uint32_t)at < (uint32_t)pages;
             bad = bad || !in;
-            const int64_t bi = (int64_t)((uint64_t)(uint32_t)(in ? page : 0) * page_blocks) + head_blocks +
+            const int64_t bi = (int64_t)((uint64_t)(uint32_t)(in ? at : 0) * page_blocks) + head_blocks +
                                (block_of(u) & in_page);
-            reg[0] = *reinterpret_cast<GlobalPieces>(k_codes + bi * kBlkBytes + 16 * tid);
-            reg[1] = *reinterpret_cast<GlobalPieces>(v_codes + bi * kBlkBytes + 16 * tid);
-            if (tid < 2) sreg = scale_of[bi];
+            // (the empty statement keeps the block's address in scalar registers)
+            GlobalBytes kp = k_codes + bi * kBlkBytes, vp = v_codes + bi * kBlkBytes;
+            asm("" : "+s"(kp), "+s"(vp));
+            reg[0] = *reinterpret_cast<GlobalPieces>(kp + 16u * (uint32_t)tid);
+            reg[1] = *reinterpret_cast<GlobalPieces>(vp + 16u * (uint32_t)tid);
+            if (wave == 0) {
+                ks = (k_scales + bi)[none];
+                vs = (v_scales + bi)[none];
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) {
@@ -670,11 +745,7 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
     auto lay = [&](int step, uint32_t shown) {
         char* to = lds + (step & 1) * L::kStage;
         if constexpr (q8) {
-            if (tid < 2) {
-                float x = sreg;
-                if (tid) x = x > 0.f ? __builtin_amdgcn_logf(x) : kNoScale;
-                lscale[step & 1][tid] = x;
-            }
+            if (tid == 0) lscale[step & 1] = float2{ks, vs > 0.f ? __builtin_amdgcn_logf(vs) : kNoScale};
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const u32x2 w0 = halves4<SRC>(reg[i][0]), w1 = halves4<SRC>(reg[i][1]);
@@ -719,8 +790,9 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
                 u32x4 p[2];
                 float c = me.qc, vl = kNoScale;
                 if constexpr (q8) {
-                    c *= lscale[step & 1][0];
-                    vl = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(lscale[step & 1][1])));
+                    const float2 scales = lscale[step & 1];
+                    c *= scales.x;
+                    vl = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(scales.y)));
                 }
 #pragma unroll
                 for (int part = 0; part < 2; ++part) {
@@ -743,7 +815,6 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
         }
     }
     if (bad && a.status) atomicOr(a.status, DQ_STATUS_PAGE);
-
     // (whole vectors up to here: or the loop copies the sums' elements at every turn)
 #pragma unroll
     for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(me.o[i]));
@@ -752,6 +823,7 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
     const float l = me.l + xor_lane<32>(me.l, lane);
     const float up = q8 ? __builtin_amdgcn_exp2f(me.vref) : 1.f;
     const int half = lane >> 5;
+    const int64_t slot = it.slot;
     if (whole) {
         const int r = r0 + wave * kRowsOf + (lane & 31), token = r / a.G, head = h * a.G + r - token * a.G;
         if (r >= rows) return;
@@ -765,8 +837,7 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
                           bf16_two(me.o[np][4 * i + 2] * f, me.o[np][4 * i + 3] * f));
         return;
     }
-    const int64_t slot = it.slot;
-    float* acc = a.ws_acc + (slot * kR + wave * kRowsOf + (lane & 31)) * kD + 4 * half;
+    float* acc = a.ws_acc + (slot * Many::kRows + wave * kRowsOf + (lane & 31)) * kD + 4 * half;
 #pragma unroll
     for (int np = 0; np < 4; ++np)
 #pragma unroll
@@ -775,9 +846,9 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
                 f32x4{me.o[np][4 * i] * up, me.o[np][4 * i + 1] * up, me.o[np][4 * i + 2] * up,
                       me.o[np][4 * i + 3] * up};
     if (half == 0) {
-        float* ml = a.ws_ml + slot * 2 * kR + wave * kRowsOf + (lane & 31);
+        float* ml = a.ws_ml + slot * 2 * Many::kRows + wave * kRowsOf + (lane & 31);
         ml[0] = me.m;
-        ml[kR] = l;
+        ml[Many::kRows] = l;
     }
 }
 
@@ -796,8 +867,6 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
 
 constexpr int kFewWaves = 8;
 constexpr int kFewThreads = kFewWaves * kWave;
-constexpr int kJoinRow = 68;                     // floats: 64 channels, and 4 to keep rows in different banks
-
 template <int SRC>
 __global__ __launch_bounds__(kFewThreads, 2) void few_kernel(ChunkArgs a) {
     typedef Lds<SRC> L;
@@ -808,7 +877,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_kernel(ChunkArgs a) {
 
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-    const Item it = find_item<Few>(a, (int)blockIdx.x, lane);
+    const Item it = find_item<Few, false>(a, (int)blockIdx.x, lane);
     if (it.tile < 0) return;
     const int b = __builtin_amdgcn_readfirstlane(it.b), h = __builtin_amdgcn_readfirstlane(it.h);
     const int piece = __builtin_amdgcn_readfirstlane(it.c), chunk = __builtin_amdgcn_readfirstlane(it.chunk);
@@ -970,114 +1039,95 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_kernel(ChunkArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(me.o[i]));
 
-    // ------------------------------------------------ the wavefronts' sums
-    const int half = lane >> 5, col = lane & 31;
-    const float l = me.l + xor_lane<32>(me.l, lane), up = q8 ? __builtin_amdgcn_exp2f(me.vref) : 1.f;
-    if (half == 0) {
-        wm[wave][col] = me.m;
-        wl[wave][col] = l;
-    }
-    float* join = reinterpret_cast<float*>(lds);
-#pragma unroll
-    for (int m2 = 0; m2 < 2; ++m2) {             // channels 64 m2 ..
-        __syncthreads();                         // (the area may still be read)
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int ch = q8 ? 32 * (i >> 1) + 16 * e + 8 * (i & 1) + 4 * half : 32 * e + 8 * i + 4 * half;
-                const f32x16& o = me.o[2 * m2 + e];
-                *reinterpret_cast<f32x4*>(join + (wave * kRowsOf + col) * kJoinRow + ch) =
-                    f32x4{o[4 * i] * up, o[4 * i + 1] * up, o[4 * i + 2] * up, o[4 * i + 3] * up};
+    join_rows<Few, kFewWaves, q8>(a, me.o, me.m, me.l + xor_lane<32>(me.l, lane),
+                                  q8 ? __builtin_amdgcn_exp2f(me.vref) : 1.f, reinterpret_cast<float*>(lds), wm, wl,
+                                  parts, rows, 0, b, h, whole, it.slot);
+}
+
+// The pieces of a segment's rows joined: a workgroup has 16 rows, half a
+// wavefront each at a time, four channels a lane.
+constexpr int kMergeRows = 16;
+
+// Over the 32 lanes of half a wavefront; every lane gets the result.
+template <typename Op>
+__device__ __forceinline__ float half_reduce(float v, int lane, Op op) {
+    v = op(v, xor_lane<1>(v, lane));
+    v = op(v, xor_lane<2>(v, lane));
+    v = op(v, xor_lane<4>(v, lane));
+    v = op(v, xor_lane<8>(v, lane));
+    return op(v, xor_lane<16>(v, lane));
+}
+
+template <typename K>
+__device__ __forceinline__ void merge_rows(const ChunkArgs& a, int id, int lane) {
+    constexpr int R = K::kRows, kParts = R / kMergeRows;
+    const Item it = find_item<K, true>(a, id / kParts, lane);
+    if (it.tile < 0) return;
+    const int b = __builtin_amdgcn_readfirstlane(it.b), h = __builtin_amdgcn_readfirstlane(it.h);
+    const int tile = __builtin_amdgcn_readfirstlane(it.tile);
+    const Seq seq = seq_of<K>(a, b);
+    const int rows = seq.n * a.G, r0 = tile * R;
+    const Sees see = sees(a, seq, r0, min(r0 + R, rows));
+    const int nc = __builtin_amdgcn_readfirstlane(pieces(see.count, it.chunk));
+    if (nc == 1) return;
+    const int64_t slot = __builtin_amdgcn_readfirstlane(it.slot);
+    const int ch = 4 * (lane & 31);
+    for (int i = (int)threadIdx.x >> 5; i < kMergeRows; i += 8) {
+        const int in = (id % kParts) * kMergeRows + i, r = r0 + in;
+        if (r >= rows) break;
+        const float* ml = a.ws_ml + slot * 2 * R + in;
+        const float* acc = a.ws_acc + (slot * R + in) * kD + ch;
+        // 32 pieces at a time: lane c % 32 has piece c's maximum and sum
+        const int mine = lane & 31;
+        float top = -INFINITY;
+        for (int c = mine; c < nc; c += 32) top = fmaxf(top, ml[(int64_t)c * 2 * R]);
+        top = half_reduce(top, lane, [](float p, float q) { return fmaxf(p, q); });
+        float l = 0.f;
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        for (int c0 = 0; c0 < nc; c0 += 32) {
+            float w = 0.f;
+            if (c0 + mine < nc) {
+                const float mc = ml[(int64_t)(c0 + mine) * 2 * R];
+                w = mc == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - top);
+                l = fmaf(ml[(int64_t)(c0 + mine) * 2 * R + R], w, l);
             }
-        __syncthreads();
-        for (int i = tid; i < parts * kRowsOf * 16; i += kFewThreads) {
-            const int r = i >> 4, ch = (i & 15) * 4;
-            if (r >= rows) continue;
-            float top = -INFINITY;
-            for (int w = r >> 5; w < kFewWaves; w += parts) top = fmaxf(top, wm[w][r & 31]);
-            float sum = 0.f;
-            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-            for (int w = r >> 5; w < kFewWaves; w += parts) {
-                const float mw = wm[w][r & 31], f = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - top);
-                sum = fmaf(wl[w][r & 31], f, sum);
-                acc += *reinterpret_cast<const f32x4*>(join + (w * kRowsOf + (r & 31)) * kJoinRow + ch) * f;
-            }
-            if (whole) {
-                const float f = sum == 0.f ? 0.f : 1.f / sum;    // rows that see nothing: zeros
-                const int token = r / a.G, head = h * a.G + r - token * a.G;
-                store_row(a, b, token, head, 64 * m2 + ch, bf16_two(acc[0] * f, acc[1] * f),
-                          bf16_two(acc[2] * f, acc[3] * f));
-            } else {
-                const int64_t slot = it.slot;
-                *reinterpret_cast<f32x4*>(a.ws_acc + (slot * Few::kRows + r) * kD + 64 * m2 + ch) = acc;
-                if (m2 == 0 && ch == 0) {
-                    a.ws_ml[slot * 2 * Few::kRows + r] = top;
-                    a.ws_ml[slot * 2 * Few::kRows + Few::kRows + r] = sum;
+            const int n = min(32, nc - c0);
+            for (int c1 = 0; c1 < n; c1 += 8) {
+                f32x4 v[8];                      // (eight loads on their way at a time)
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                    v[c] = *reinterpret_cast<const f32x4*>(acc + (int64_t)(c0 + min(c1 + c, n - 1)) * R * kD);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    const float wc = __shfl(w, min(c1 + c, 31), 32);
+                    if (c1 + c < n) x += v[c] * wc;
                 }
             }
         }
+        l = half_reduce(l, lane, [](float p, float q) { return p + q; });
+        const float f = l == 0.f ? 0.f : 1.f / l;
+        const int token = r / a.G, head = h * a.G + r - token * a.G;
+        store_row(a, b, token, head, ch, bf16_two(x[0] * f, x[1] * f), bf16_two(x[2] * f, x[3] * f));
     }
 }
 
-// The pieces of a row joined: one wavefront per row, two channels a lane.
-template <typename K>
-__device__ __forceinline__ void merge_row(const ChunkArgs& a, int64_t id, int b, int lane) {
-    constexpr int R = K::kRows;
-    const Seq seq = seq_of<K>(a, b);
-    if (seq.tiles == 0) return;
-    const int rows = seq.n * a.G;
-    if (id >= (int64_t)rows * a.H) return;
-    const int h = (int)(id / rows), r = (int)(id % rows), tile = r / R;
-    const int chunk = plan_chunk<K>(a, lane);
-    const Sees see = sees(a, seq, tile * R, min(tile * R + R, rows));
-    const int nc = pieces(see.count, chunk);
-    if (nc == 1) return;
-    const int64_t slot = first_slot<K>(a, b, h, tile, chunk, lane);
-    const float* ml = a.ws_ml + slot * 2 * R + r % R;
-    float top = -INFINITY;
-    for (int c = lane; c < nc; c += kWave) top = fmaxf(top, ml[(int64_t)c * 2 * R]);
-    top = wave_max(top);
-    float l = 0.f, x = 0.f, y = 0.f;
-    const float* acc = a.ws_acc + (slot * R + r % R) * kD + 2 * lane;
-#pragma unroll 4
-    for (int c = 0; c < nc; ++c) {
-        const float mc = ml[(int64_t)c * 2 * R];
-        const float w = mc == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - top);
-        const float2 v = *reinterpret_cast<const float2*>(acc + (int64_t)c * R * kD);
-        l = fmaf(ml[(int64_t)c * 2 * R + R], w, l);
-        x = fmaf(v.x, w, x);
-        y = fmaf(v.y, w, y);
-    }
-    const float f = l == 0.f ? 0.f : 1.f / l;
-    const int token = r / a.G, head = h * a.G + r % a.G;
-    uint16_t* p = a.out + (int64_t)b * a.o_sb + (int64_t)token * a.o_st + (int64_t)head * a.o_sh + 2 * lane;
-    const uint32_t w = bf16_two(x * f, y * f);
-    if (a.out_aligned) {
-        *reinterpret_cast<uint32_t*>(p) = w;
-    } else {
-        p[0] = (uint16_t)w;
-        p[1] = (uint16_t)(w >> 16);
-    }
-}
-
-__global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs few, ChunkArgs many) {
+__global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs few, ChunkArgs many, int few_groups) {
     const int lane = threadIdx.x & (kWave - 1);
-    const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
-    if (few.target) merge_row<Few>(few, id, blockIdx.y, lane);
-    if (many.target) merge_row<Many>(many, id, blockIdx.y, lane);
+    if ((int)blockIdx.x < few_groups)
+        merge_rows<Few>(few, blockIdx.x, lane);
+    else
+        merge_rows<Many>(many, (int)blockIdx.x - few_groups, lane);
 }
 
 // ------------------------------------------------------------------- host
-
-constexpr int kTarget = 512;                 // work items wanted: two per CU
-constexpr int kLeast = 8;                    // blocks of one piece, at least
 
 // A kernel's part of the work, as far as the host knows it.
 struct HostPlan {
     bool runs;
     int rows;                    // per tile
     int64_t segs, slots, grid;
+    int64_t merges;              // workgroups of the merge
 
     int64_t floats() const { return slots * rows * (kD + 2); }
 };
@@ -1091,10 +1141,13 @@ HostPlan host_plan(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t t_ca
     p.rows = K::kRows;
     p.segs = (int64_t)B * Hkv * (K::kFew ? 1 : (rows + p.rows - 1) / p.rows);
     const int64_t pieces = std::max<int64_t>(1, ((int64_t)t_cap / kBlk + kLeast) / kLeast);
-    // (a plan that cuts has fewer than kTarget segments, each cut has at most one
-    // piece more than an even share of the items wanted)
-    p.slots = pieces == 1 || !p.runs ? 0 : std::min<int64_t>(2 * kTarget + 8, p.segs * pieces);
+    // A plan that cuts has fewer segments than would fill the GPU twice and, all
+    // in all, fewer than twice as many items.  Segments are as many as are counted
+    // here where all chunks are full.
+    const bool cuts = p.runs && pieces > 1 && (lens || p.segs < 2 * K::kAtOnce);
+    p.slots = cuts ? std::min<int64_t>(4 * K::kAtOnce + 8, p.segs * pieces) : 0;
     p.grid = (std::max(p.segs, p.slots) + 7) / 8 * 8;
+    p.merges = cuts ? std::min<int64_t>(2 * K::kAtOnce, p.segs) * (K::kRows / kMergeRows) : 0;
     return p;
 }
 
@@ -1161,10 +1214,10 @@ int launch_chunk(const ChunkSource& src, const ChunkCall& c, void* ws, uint32_t*
                       (uintptr_t)(c.out.sh * 2)) & 7) == 0;
     a.scale_log2 = fabsf(c.scale) * kLog2e;
     a.negative = c.scale < 0.f;
-    a.target = kTarget;
-    a.least = kLeast;
     a.status = status;
     ChunkArgs few = a, many = a;
+    few.cuts = pf.slots > 0;
+    many.cuts = pm.slots > 0;
     few.ws_acc = static_cast<float*>(ws);
     few.ws_ml = few.ws_acc + pf.slots * pf.rows * kD;
     many.ws_acc = few.ws_acc + pf.floats();
@@ -1177,15 +1230,8 @@ int launch_chunk(const ChunkSource& src, const ChunkCall& c, void* ws, uint32_t*
     else
         rc = launch_source<kChunkBf16>(few, pf, many, pm, stream);
     if (rc != DQ_OK) return rc;
-    // nothing to join where nothing can be cut (segments are as many as the host
-    // counts where all chunks are full)
-    const bool fm = pf.slots > 0 && (c.q_lens || pf.segs < kTarget);
-    const bool mm = pm.slots > 0 && (c.q_lens || pm.segs < kTarget);
-    if (!fm && !mm) return DQ_OK;
-    if (!fm) few.target = 0;
-    if (!mm) many.target = 0;
-    const dim3 grid((unsigned)(((int64_t)c.n_q * c.Hq + 3) / 4), c.B);
-    chunk_merge_kernel<<<grid, 256, 0, stream>>>(few, many);
+    if (pf.merges + pm.merges == 0) return DQ_OK;
+    chunk_merge_kernel<<<dim3((unsigned)(pf.merges + pm.merges)), 256, 0, stream>>>(few, many, (int)pf.merges);
     return hip_check("chunk_merge launch", hipGetLastError());
 }
 
