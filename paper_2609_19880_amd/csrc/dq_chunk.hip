@@ -96,6 +96,7 @@ struct Many {
     static constexpr int kAtOnce = 768;
     static constexpr int kCost = 8;
 };
+constexpr float kFine = 2.f;
 constexpr int kLeast = 8;                        // blocks of one piece, at least
 
 template <typename K>
@@ -128,7 +129,13 @@ __device__ __forceinline__ int plan_chunk(const ChunkArgs& a, int lane) {
     // short adds an item, which the workspace has room for)
     float total = 0, segs = 0;
     int longest = 0;
-    for (int b0 = 0; b0 < a.B; b0 += kWave) {
+    if (a.B == 1) {
+        const Seq q = seq_of<K>(a, 0);
+        segs = (float)q.tiles;
+        total = segs * (float)q.units;
+        longest = q.units;
+    }
+    for (int b0 = 0; b0 < a.B && a.B > 1; b0 += kWave) {
         float t = 0, s = 0;
         int n = 0;
         if (b0 + lane < a.B) {
@@ -147,7 +154,7 @@ __device__ __forceinline__ int plan_chunk(const ChunkArgs& a, int lane) {
     if (segs >= kMost) return 0x7FFFFFFE;
     if (total < 0.75f * segs * (float)longest) {
         // unlike lengths leave pieces that are not full: small ones even out the end
-        return max((int)ceilf(total / kMost), kLeast);
+        return max((int)ceilf(total / (K::kAtOnce * kFine)), kLeast);
     }
     // lane l tries l + 1 pieces per segment: rounds, and what one takes
     const int c = max((int)((uint32_t)(longest + lane) / (uint32_t)(lane + 1)), kLeast);
@@ -160,11 +167,6 @@ __device__ __forceinline__ int plan_chunk(const ChunkArgs& a, int lane) {
 
 __device__ __forceinline__ int pieces(int units, int chunk) { return max(1, (units - 1) / chunk + 1); }
 
-template <typename K>
-__device__ __forceinline__ int items_of(const ChunkArgs& a, const Seq& s, int chunk) {
-    return s.tiles * pieces(s.units, chunk) * a.H;
-}
-
 __device__ __forceinline__ int scan64(int v) {         // inclusive sums over the lanes
     v += dpp0<0x111, 0xF>(v);
     v += dpp0<0x112, 0xF>(v);
@@ -175,44 +177,58 @@ __device__ __forceinline__ int scan64(int v) {         // inclusive sums over th
     return v;
 }
 
-// Item number `id` of the plan: sequence after sequence, KV head after KV head,
-// the last row tiles (which see most) first, their pieces in order.  Or segment
-// number `id` (SEGMENT), with its first piece.
+// Work item `id`, or segment `id` (SEGMENT), with the slot of its (first) piece.
+// Slots go sequence after sequence, KV head after KV head, the last row tiles
+// (which see most) first, their pieces in order.  Workgroups go to the 8 XCDs in
+// turn; what shares keys and values should meet in one L2, and all XCDs should
+// have sequences of every length: each takes its heads of all sequences where
+// there are a multiple of 8, else an eighth of the slots.
 template <typename K, bool SEGMENT>
 __device__ __forceinline__ Item find_item(const ChunkArgs& a, int id, int lane) {
     Item it{0, 0, -1, 0, plan_chunk<K>(a, lane), 0};
     auto at = [&](int b0) { return b0 + lane < a.B ? seq_of<K>(a, b0 + lane) : Seq{0, 0, 0, 0}; };
-    int x = id;
-    if (!SEGMENT) {
-        int all = 0;
-        for (int b0 = 0; b0 < a.B; b0 += kWave) all += wave_sum(items_of<K>(a, at(b0), it.chunk));
-        // workgroups go to the 8 XCDs in turn: an XCD takes items that follow each
-        // other, which share keys and values in its L2
+    const bool by_head = !SEGMENT && a.H % 8 == 0;
+    const int heads = by_head ? a.H / 8 : a.H;   // of those that x counts
+    int x = by_head ? id >> 3 : id;
+    // what a sequence has of what x counts
+    auto count = [&](const Seq& s) { return s.tiles * heads * (SEGMENT ? 1 : pieces(s.units, it.chunk)); };
+    if (!SEGMENT && !by_head) {
+        int all = a.B == 1 ? count(seq_of<K>(a, 0)) : 0;
+        for (int b0 = 0; b0 < a.B && a.B > 1; b0 += kWave) all += wave_sum(count(at(b0)));
         const int per = (all + 7) / 8;
+        if ((id >> 3) >= per) return it;
         x = (id & 7) * per + (id >> 3);
-        if ((id >> 3) >= per || x >= all) return it;
+    }
+    // of sequence b, whose first slot is `slot`: entry r
+    auto entry = [&](int b, int tiles, int nc, int slot, int r) {
+        const uint32_t each = SEGMENT ? 1u : (uint32_t)nc, t = (uint32_t)r / each, h = t / (uint32_t)tiles;
+        const int late = (int)(t - h * (uint32_t)tiles);
+        it.b = b;
+        it.h = by_head ? 8 * (int)h + (id & 7) : (int)h;
+        it.tile = tiles - 1 - late;
+        it.c = r - (int)(t * each);
+        it.slot = slot + (it.h * tiles + late) * nc + it.c;
+    };
+    if (a.B == 1) {
+        // (uniform arithmetic, no sums over the lanes)
+        const Seq s = seq_of<K>(a, 0);
+        if (x < count(s)) entry(0, s.tiles, pieces(s.units, it.chunk), 0, x);
+        return it;
     }
     int before = 0, slots = 0;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
         const Seq s = at(b0);
-        const int own_items = items_of<K>(a, s, it.chunk), own = SEGMENT ? s.tiles * a.H : own_items;
-        const int upto = before + scan64(own);
+        const int own = count(s), held = s.tiles * a.H * pieces(s.units, it.chunk);
+        const int upto = before + scan64(own), held_upto = slots + scan64(held);
         const int last = __builtin_amdgcn_readlane(upto, 63);
-        const int held = SEGMENT ? slots + scan64(own_items) : upto;
         if (x < last) {
             const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > x));
-            const int r = x - __builtin_amdgcn_readlane(upto - own, l);
-            const int nc = pieces(__builtin_amdgcn_readlane(s.units, l), it.chunk);
-            const int tiles = __builtin_amdgcn_readlane(s.tiles, l), each = SEGMENT ? 1 : nc;
-            it.b = b0 + l;
-            it.h = r / (tiles * each);
-            it.tile = tiles - 1 - (r / each) % tiles;
-            it.c = r % each;
-            it.slot = SEGMENT ? __builtin_amdgcn_readlane(held - own_items, l) + r * nc : x;
+            entry(b0 + l, __builtin_amdgcn_readlane(s.tiles, l), pieces(__builtin_amdgcn_readlane(s.units, l), it.chunk),
+                  __builtin_amdgcn_readlane(held_upto - held, l), x - __builtin_amdgcn_readlane(upto - own, l));
             return it;
         }
         before = last;
-        slots = SEGMENT ? __builtin_amdgcn_readlane(held, 63) : 0;
+        slots = __builtin_amdgcn_readlane(held_upto, 63);
     }
     return it;
 }
