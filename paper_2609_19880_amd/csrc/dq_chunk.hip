@@ -96,7 +96,6 @@ struct Many {
     static constexpr int kAtOnce = 768;
     static constexpr int kCost = 8;
 };
-constexpr float kFine = 2.f;
 constexpr int kLeast = 8;                        // blocks of one piece, at least
 
 template <typename K>
@@ -154,7 +153,7 @@ __device__ __forceinline__ int plan_chunk(const ChunkArgs& a, int lane) {
     if (segs >= kMost) return 0x7FFFFFFE;
     if (total < 0.75f * segs * (float)longest) {
         // unlike lengths leave pieces that are not full: small ones even out the end
-        return max((int)ceilf(total / (K::kAtOnce * kFine)), kLeast);
+        return max((int)ceilf(total / K::kAtOnce), kLeast);
     }
     // lane l tries l + 1 pieces per segment: rounds, and what one takes
     const int c = max((int)((uint32_t)(longest + lane) / (uint32_t)(lane + 1)), kLeast);
@@ -179,10 +178,13 @@ __device__ __forceinline__ int scan64(int v) {         // inclusive sums over th
 
 // Work item `id`, or segment `id` (SEGMENT), with the slot of its (first) piece.
 // Slots go sequence after sequence, KV head after KV head, the last row tiles
-// (which see most) first, their pieces in order.  Workgroups go to the 8 XCDs in
-// turn; what shares keys and values should meet in one L2, and all XCDs should
-// have sequences of every length: each takes its heads of all sequences where
-// there are a multiple of 8, else an eighth of the slots.
+// (which see most) first, their pieces in order.
+//
+// Workgroups go to the 8 XCDs in turn; what shares keys and values should meet in
+// one L2, and all XCDs should have sequences of every length: each takes its
+// heads of all sequences where there are a multiple of 8, else an eighth of the
+// items.  Items come in three passes, the whole pieces, the last ones of more
+// than half a piece and the rest: short work evens out the end.
 template <typename K, bool SEGMENT>
 __device__ __forceinline__ Item find_item(const ChunkArgs& a, int id, int lane) {
     Item it{0, 0, -1, 0, plan_chunk<K>(a, lane), 0};
@@ -190,45 +192,65 @@ __device__ __forceinline__ Item find_item(const ChunkArgs& a, int id, int lane) 
     const bool by_head = !SEGMENT && a.H % 8 == 0;
     const int heads = by_head ? a.H / 8 : a.H;   // of those that x counts
     int x = by_head ? id >> 3 : id;
-    // what a sequence has of what x counts
-    auto count = [&](const Seq& s) { return s.tiles * heads * (SEGMENT ? 1 : pieces(s.units, it.chunk)); };
+    // pieces of a sequence's segment in a pass
+    auto full = [&](int units) { return (int)((uint32_t)units / (uint32_t)it.chunk); };
+    auto in_pass = [&](int units, int pass) {
+        if (SEGMENT) return 1;
+        const int n = full(units);
+        if (pass == 0) return n;
+        const int rest = units - n * it.chunk;
+        return (int)(rest > it.chunk / 2 ? pass == 1 : (rest > 0 || n == 0) && pass == 2);
+    };
     if (!SEGMENT && !by_head) {
-        int all = a.B == 1 ? count(seq_of<K>(a, 0)) : 0;
-        for (int b0 = 0; b0 < a.B && a.B > 1; b0 += kWave) all += wave_sum(count(at(b0)));
+        int all = 0;
+        for (int b0 = 0; b0 < a.B; b0 += kWave) {
+            const Seq s = at(b0);
+            all += wave_sum(s.tiles * heads * pieces(s.units, it.chunk));
+        }
         const int per = (all + 7) / 8;
         if ((id >> 3) >= per) return it;
         x = (id & 7) * per + (id >> 3);
     }
-    // of sequence b, whose first slot is `slot`: entry r
-    auto entry = [&](int b, int tiles, int nc, int slot, int r) {
-        const uint32_t each = SEGMENT ? 1u : (uint32_t)nc, t = (uint32_t)r / each, h = t / (uint32_t)tiles;
+    // of sequence b, whose first slot is `slot`: entry r of a pass
+    auto entry = [&](int b, int tiles, int units, int slot, int pass, int r) {
+        const uint32_t each = (uint32_t)in_pass(units, pass), t = (uint32_t)r / each, h = t / (uint32_t)tiles;
         const int late = (int)(t - h * (uint32_t)tiles);
         it.b = b;
         it.h = by_head ? 8 * (int)h + (id & 7) : (int)h;
         it.tile = tiles - 1 - late;
-        it.c = r - (int)(t * each);
-        it.slot = slot + (it.h * tiles + late) * nc + it.c;
+        it.c = SEGMENT ? 0 : pass == 0 ? r - (int)(t * each) : full(units);
+        it.slot = slot + (it.h * tiles + late) * pieces(units, it.chunk) + it.c;
     };
-    if (a.B == 1) {
-        // (uniform arithmetic, no sums over the lanes)
-        const Seq s = seq_of<K>(a, 0);
-        if (x < count(s)) entry(0, s.tiles, pieces(s.units, it.chunk), 0, x);
-        return it;
-    }
-    int before = 0, slots = 0;
-    for (int b0 = 0; b0 < a.B; b0 += kWave) {
-        const Seq s = at(b0);
-        const int own = count(s), held = s.tiles * a.H * pieces(s.units, it.chunk);
-        const int upto = before + scan64(own), held_upto = slots + scan64(held);
-        const int last = __builtin_amdgcn_readlane(upto, 63);
-        if (x < last) {
-            const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > x));
-            entry(b0 + l, __builtin_amdgcn_readlane(s.tiles, l), pieces(__builtin_amdgcn_readlane(s.units, l), it.chunk),
-                  __builtin_amdgcn_readlane(held_upto - held, l), x - __builtin_amdgcn_readlane(upto - own, l));
-            return it;
+    for (int pass = 0; pass < (SEGMENT ? 1 : 3); ++pass) {
+        if (a.B == 1) {
+            // (uniform arithmetic, no sums over the lanes)
+            const Seq s = seq_of<K>(a, 0);
+            const int own = s.tiles * heads * in_pass(s.units, pass);
+            if (x < own) {
+                entry(0, s.tiles, s.units, 0, pass, x);
+                return it;
+            }
+            x -= own;
+            continue;
         }
-        before = last;
-        slots = __builtin_amdgcn_readlane(held_upto, 63);
+        int before = 0, slots = 0;
+        for (int b0 = 0; b0 < a.B; b0 += kWave) {
+            const Seq s = at(b0);
+            const int own = s.tiles * heads * in_pass(s.units, pass), held = s.tiles * a.H * pieces(s.units, it.chunk);
+            const int upto = before + scan64(own);
+            const int last = __builtin_amdgcn_readlane(upto, 63);
+            const int held_upto = slots + scan64(held);
+            if (x < last) {
+                const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > x));
+                entry(b0 + l, __builtin_amdgcn_readlane(s.tiles, l), __builtin_amdgcn_readlane(s.units, l),
+                      __builtin_amdgcn_readlane(held_upto - held, l), pass,
+                      x - __builtin_amdgcn_readlane(upto - own, l));
+                return it;
+            }
+            before = last;
+            slots = __builtin_amdgcn_readlane(held_upto, 63);
+        }
+        x -= before;
     }
     return it;
 }
@@ -671,7 +693,7 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
     // memory, as a scalar load would make every wait for LDS do.  Block `at` lies
     // at page (H per_page) + h per_page + at % per_page; without a table the
     // sequence is the page.
-    float ks = 0.f, vs = 0.f;
+    float sreg = 0.f;
     int page = b;
     const int per_page = a.pg.bt ? 1 << (a.pg.page_shift - 5) : a.t_cap / kBlk;
     const int in_page = a.pg.bt ? per_page - 1 : 0x7FFFFFFF, pages = a.pg.bt ? a.pg.num_pages : a.B;
@@ -679,7 +701,7 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
     const int64_t head_blocks = (int64_t)h * per_page;
     GlobalInts table = (GlobalInts)(uintptr_t)(a.pg.bt + (a.pg.bt ? (int64_t)b * a.pg.max_pages : 0));
     GlobalBytes k_codes = (GlobalBytes)(uintptr_t)a.k, v_codes = (GlobalBytes)(uintptr_t)a.v;
-    GlobalFloats k_scales = (GlobalFloats)(uintptr_t)a.ks, v_scales = (GlobalFloats)(uintptr_t)a.vs;
+    GlobalFloats scales = (GlobalFloats)(uintptr_t)(wave ? a.vs : a.ks);         // (wavefronts 0 and 1)
     uint32_t none = 0;                           // an offset that the compiler takes for a lane's
     asm("" : "+v"(none));
     // BF16: this thread's piece of rows 16 i + tid / 16
@@ -711,10 +733,7 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
             asm("" : "+s"(kp), "+s"(vp));
             reg[0] = *reinterpret_cast<GlobalPieces>(kp + 16u * (uint32_t)tid);
             reg[1] = *reinterpret_cast<GlobalPieces>(vp + 16u * (uint32_t)tid);
-            if (wave == 0) {
-                ks = (k_scales + bi)[none];
-                vs = (v_scales + bi)[none];
-            }
+            if (wave < 2) sreg = (scales + bi)[none];
         } else {
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) {
@@ -761,7 +780,8 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
     auto lay = [&](int step, uint32_t shown) {
         char* to = lds + (step & 1) * L::kStage;
         if constexpr (q8) {
-            if (tid == 0) lscale[step & 1] = float2{ks, vs > 0.f ? __builtin_amdgcn_logf(vs) : kNoScale};
+            if (tid == 0) lscale[step & 1].x = sreg;
+            if (tid == kWave) lscale[step & 1].y = sreg > 0.f ? __builtin_amdgcn_logf(sreg) : kNoScale;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const u32x2 w0 = halves4<SRC>(reg[i][0]), w1 = halves4<SRC>(reg[i][1]);
@@ -806,9 +826,9 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
                 u32x4 p[2];
                 float c = me.qc, vl = kNoScale;
                 if constexpr (q8) {
-                    const float2 scales = lscale[step & 1];
-                    c *= scales.x;
-                    vl = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(scales.y)));
+                    const float2 both = lscale[step & 1];
+                    c *= both.x;
+                    vl = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(both.y)));
                 }
 #pragma unroll
                 for (int part = 0; part < 2; ++part) {
