@@ -1087,16 +1087,20 @@ def dq_rope_frequencies(rotary_dim: int, base: float = 10000.0, scaling="none", 
     return freq, magnitude.value
 
 
+def _like(x, stream):
+    """A new tensor of x's shape and type, contiguous, in memory of the stream that fills it."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return _like(x, None)
+    return torch.empty_like(x) if x.is_contiguous() else torch.empty_like(x, memory_format=torch.contiguous_format)
+
+
 def _rope_rows(x, out, name, dev, stream):
     """Rows [B, T, H, d] bf16 and where they go (a new tensor unless given)."""
     _need(x.dtype is torch.bfloat16 and x.dim() == 4 and x.stride(3) == 1 and x.device == dev,
           name + " must be bf16 [B, T, H, d], channels contiguous, on the frequencies' GPU")
     if out is None:
-        if stream is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=dev)
-        else:                        # memory of the stream that fills it
-            with torch.cuda.stream(stream):
-                out = torch.empty(x.shape, dtype=x.dtype, device=dev)
+        out = _like(x, stream)
     else:
         _need(out.dtype is torch.bfloat16 and out.shape == x.shape and out.stride(3) == 1 and out.device == dev,
               name + "_out must be bf16 of " + name + "'s shape on the same GPU")
@@ -1159,27 +1163,26 @@ def _chunk_rows(q, out, batch, heads, dev, stream):
           and q.stride(3) == 1 and q.device == dev and q.shape[2] % heads == 0,
           "q must be bf16 [B, n, Hq, 128], channels contiguous, on the cache's GPU, Hq a multiple of the KV heads")
     if out is None:
-        if stream is None:
-            out = torch.empty(q.shape, dtype=torch.bfloat16, device=dev)
-        else:                        # memory of the stream that fills it
-            with torch.cuda.stream(stream):
-                out = torch.empty(q.shape, dtype=torch.bfloat16, device=dev)
+        out = _like(q, stream)
     else:
         _need(out.dtype is torch.bfloat16 and out.shape == q.shape and out.stride(3) == 1 and out.device == dev,
               "out must be bf16 of q's shape")
     return out
 
 
-def _chunk_workspace(workspace, B, n, Hq, H, t_cap, dev, stream):
+def _chunk_workspace(workspace, q, H, t_cap, dev, stream):
+    """The workspace (a new one unless given), its pointer and size."""
     if workspace is None:
+        B, n, Hq, _ = q.shape
         need = _lib.dq_chunk_workspace_bytes(B, n, Hq, H, t_cap)
         if need == 0:
             return None, 0, 0
         if stream is not None:
             with torch.cuda.stream(stream):
-                workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+                workspace = q.new_empty(need // 2)
         else:
-            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+            workspace = q.new_empty(need // 2)       # (bf16 elements)
+        return workspace, workspace.data_ptr(), need
     return (workspace, *_q8_workspace(workspace, dev))
 
 
@@ -1195,7 +1198,7 @@ def _q8_chunk(fmt: int, cache, q, seq_lens, q_lens, causal, window, sinks, out, 
     scale = _RSQRT_D if softmax_scale is None else softmax_scale
     if paged is None:
         t_cap = nb * DQ_Q8_BLOCK
-        held, ws, ws_bytes = _chunk_workspace(workspace, B, n, Hq, H, t_cap, dev, stream)
+        held, ws, ws_bytes = _chunk_workspace(workspace, q, H, t_cap, dev, stream)
         rc = _lib.dq_q8_chunk_attention(
             fmt, q.data_ptr(), *q.stride()[:3], B, n, Hq, H, *at, new, lens, t_cap, int(bool(causal)), window, sinks,
             scale, out.data_ptr(), *out.stride()[:3], ws, ws_bytes, _q8_stream(dev.index, stream))
@@ -1204,7 +1207,7 @@ def _q8_chunk(fmt: int, cache, q, seq_lens, q_lens, causal, window, sinks, out, 
         return out
     block_table, status = paged
     max_pages, page = _q8_table(block_table, B, dev), nb * DQ_Q8_BLOCK
-    held, ws, ws_bytes = _chunk_workspace(workspace, B, n, Hq, H, min(max_pages * page, _INT_MAX), dev, stream)
+    held, ws, ws_bytes = _chunk_workspace(workspace, q, H, min(max_pages * page, _INT_MAX), dev, stream)
     rc = _lib.dq_q8_chunk_attention_paged(
         fmt, q.data_ptr(), *q.stride()[:3], B, n, Hq, H, *at, block_table.data_ptr(), max_pages, page, rows, new, lens,
         int(bool(causal)), window, sinks, scale, out.data_ptr(), *out.stride()[:3], ws, ws_bytes,
@@ -1258,7 +1261,7 @@ def dq_cross_attention(q, k, v, kv_lens=None, mask=None, q_lens=None, out=None, 
         _need(mask.dtype in (torch.bool, torch.uint8) and mask.shape == (B, T) and mask.device == dev
               and (mask.stride(1) == 1 or T <= 1), "mask must be bool or uint8 [B, T], rows contiguous, on k's GPU")
         hide, hide_sb = mask.data_ptr(), mask.stride(0)
-    held, ws, ws_bytes = _chunk_workspace(workspace, B, n, Hq, H, T, dev, stream)
+    held, ws, ws_bytes = _chunk_workspace(workspace, q, H, T, dev, stream)
     rc = _lib.dq_cross_attention(
         q.data_ptr(), *q.stride()[:3], B, n, Hq, H, k.data_ptr(), *k.stride()[:3], v.data_ptr(), *v.stride()[:3], T,
         new, lens, hide, hide_sb, _RSQRT_D if softmax_scale is None else softmax_scale, out.data_ptr(),
