@@ -120,10 +120,11 @@ struct Item {
     int chunk, slot;
 };
 
+constexpr int kWhole = 0x7FFFFFFE;               // no piece is cut
+
 // The blocks of one piece.  All lanes agree.
 template <typename K>
 __device__ __forceinline__ int plan_chunk(const ChunkArgs& a, int lane) {
-    if (!a.cuts) return 0x7FFFFFFE;
     // (sums in fp32: the same bits wherever they are taken; a chunk a millionth too
     // short adds an item, which the workspace has room for)
     float total = 0, segs = 0;
@@ -150,7 +151,7 @@ __device__ __forceinline__ int plan_chunk(const ChunkArgs& a, int lane) {
     total *= (float)a.H;
     segs *= (float)a.H;
     constexpr float kMost = 2 * K::kAtOnce;
-    if (segs >= kMost) return 0x7FFFFFFE;
+    if (segs >= kMost) return kWhole;
     if (total < 0.75f * segs * (float)longest) {
         // unlike lengths leave pieces that are not full: small ones even out the end
         return max((int)ceilf(total / K::kAtOnce), kLeast);
@@ -187,7 +188,28 @@ __device__ __forceinline__ int scan64(int v) {         // inclusive sums over th
 // than half a piece and the rest: short work evens out the end.
 template <typename K, bool SEGMENT>
 __device__ __forceinline__ Item find_item(const ChunkArgs& a, int id, int lane) {
-    Item it{0, 0, -1, 0, plan_chunk<K>(a, lane), 0};
+    Item it{0, 0, -1, 0, kWhole, 0};
+    if (!a.cuts) {
+        // every segment whole, as many as full chunks have: no lengths needed to find it
+        const uint32_t tiles = K::kFew ? 1u : ((uint32_t)a.n_q * (uint32_t)a.G + K::kRows - 1) / K::kRows;
+        const bool heads8 = a.H % 8 == 0;
+        const uint32_t heads = heads8 ? (uint32_t)a.H / 8 : (uint32_t)a.H, all = (uint32_t)a.B * heads * tiles;
+        uint32_t x = (uint32_t)id >> 3;
+        if (!heads8) {
+            const uint32_t per = (all + 7) / 8;
+            if (x >= per) return it;
+            x += (uint32_t)(id & 7) * per;
+        }
+        if (x >= all) return it;
+        const uint32_t r = x / tiles;
+        it.b = (int)(r / heads);
+        it.h = (int)(r % heads);
+        if (heads8) it.h = 8 * it.h + (id & 7);
+        it.tile = (int)(tiles - 1 - x % tiles);
+        if (it.tile >= seq_of<K>(a, it.b).tiles) it.tile = -1;
+        return it;
+    }
+    it.chunk = plan_chunk<K>(a, lane);
     auto at = [&](int b0) { return b0 + lane < a.B ? seq_of<K>(a, b0 + lane) : Seq{0, 0, 0, 0}; };
     const bool by_head = !SEGMENT && a.H % 8 == 0;
     const int heads = by_head ? a.H / 8 : a.H;   // of those that x counts
@@ -221,7 +243,7 @@ __device__ __forceinline__ Item find_item(const ChunkArgs& a, int id, int lane) 
         it.c = SEGMENT ? 0 : pass == 0 ? r - (int)(t * each) : full(units);
         it.slot = slot + (it.h * tiles + late) * pieces(units, it.chunk) + it.c;
     };
-    for (int pass = 0; pass < (SEGMENT ? 1 : 3); ++pass) {
+    for (int pass = SEGMENT || it.chunk != kWhole ? 0 : 2; pass < (SEGMENT ? 1 : 3); ++pass) {
         if (a.B == 1) {
             // (uniform arithmetic, no sums over the lanes)
             const Seq s = seq_of<K>(a, 0);
@@ -351,10 +373,10 @@ __device__ __forceinline__ float plus_weights(uint32_t w, float x) {
 //
 // The state's maximum m is not the running maximum but one that the sums keep
 // until a block's weights, relative to it, add up to more than 2^15: weights of
-// m itself are 2^7, so fp16 holds what lies 2^8 above and, exactly, 2^21 below.
-// Most blocks so need no maximum and scale nothing: their weights are computed
-// with the m at hand and only checked.  A row's bits do not depend on the rows
-// beside it.
+// m itself are 2^2, so fp16 holds what lies 2^13 above and, to its 11 bits, 2^16
+// below (to 2^-25 beyond).  Most blocks so need no maximum and scale nothing:
+// their weights are computed with the m at hand and only checked.  A row's bits
+// do not depend on the rows beside it, but where their scores pass 2^11.
 template <int SRC>
 struct Rows {
     static constexpr bool q8 = SRC != kChunkBf16;
@@ -1180,7 +1202,9 @@ HostPlan host_plan(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t t_ca
     // A plan that cuts has fewer segments than would fill the GPU twice and, all
     // in all, fewer than twice as many items.  Segments are as many as are counted
     // here where all chunks are full.
-    const bool cuts = p.runs && pieces > 1 && (lens || p.segs < 2 * K::kAtOnce);
+    // Every workgroup reads all lengths then: not of more than 128 sequences,
+    // which fill the GPU by themselves.
+    const bool cuts = p.runs && pieces > 1 && B <= 128 && (lens || p.segs < 2 * K::kAtOnce);
     p.slots = cuts ? std::min<int64_t>(4 * K::kAtOnce + 8, p.segs * pieces) : 0;
     p.grid = (std::max(p.segs, p.slots) + 7) / 8 * 8;
     p.merges = cuts ? std::min<int64_t>(2 * K::kAtOnce, p.segs) * (K::kRows / kMergeRows) : 0;

@@ -138,7 +138,9 @@ def test_chunk_sizes(dq, fmt, B, T, n, H, G, causal):
 
 @pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("B,T,n,H,G,cap", [(6, 500, 40, 2, 4, 512), (70, 130, 12, 1, 3, 256), (130, 90, 5, 1, 1, 128),
-                                           (4, 3000, 200, 2, 2, 16384)])
+                                           (4, 3000, 200, 2, 2, 16384), (150, 700, 40, 1, 4, 768),
+                                           (140, 300, 70, 8, 1, 384), (9, 2000, 33, 8, 4, 2048),
+                                           (70, 1500, 90, 3, 2, 1536)])
 def test_ragged(dq, fmt, B, T, n, H, G, cap):
     """Lengths from none up, chunks from none up, chunks longer than their
     sequence (their first rows see nothing); rows behind a chunk stay."""
