@@ -122,6 +122,20 @@ struct Item {
 
 constexpr int kWhole = 0x7FFFFFFE;               // no piece is cut
 
+// What pieces of c blocks take, `segs` segments' of `longest` blocks at most:
+// rounds of as many as the GPU takes at a time, each its blocks and a piece's own cost.
+template <typename K>
+__host__ __device__ inline float plan_cost(float segs, int longest, int c) {
+    const float items = segs * (float)((uint32_t)(longest + c - 1) / (uint32_t)c);
+    if (items > 2 * K::kAtOnce && c < longest) return 3e38f;
+    return ceilf(items / K::kAtOnce) * (float)(c + K::kCost);
+}
+// Blocks of a piece where a segment has n + 1 of them.
+__host__ __device__ inline int plan_try(int longest, int n) {
+    const int c = (int)((uint32_t)(longest + n) / (uint32_t)(n + 1));
+    return c > kLeast ? c : kLeast;
+}
+
 // The blocks of one piece.  All lanes agree.
 template <typename K>
 __device__ __forceinline__ int plan_chunk(const ChunkArgs& a, int lane) {
@@ -156,13 +170,11 @@ __device__ __forceinline__ int plan_chunk(const ChunkArgs& a, int lane) {
         // unlike lengths leave pieces that are not full: small ones even out the end
         return max((int)ceilf(total / K::kAtOnce), kLeast);
     }
-    // lane l tries l + 1 pieces per segment: rounds, and what one takes
-    const int c = max((int)((uint32_t)(longest + lane) / (uint32_t)(lane + 1)), kLeast);
-    const float items = segs * (float)((uint32_t)(longest + c - 1) / (uint32_t)c);
-    float cost = ceilf(items / K::kAtOnce) * (float)(c + K::kCost);
-    if (items > kMost && lane > 0) cost = 3e38f;
-    const float least = wave_min(cost);
-    return max(1, __builtin_amdgcn_readlane(c, __builtin_ctzll(__builtin_amdgcn_ballot_w64(cost == least))));
+    // lane l tries l + 1 pieces per segment
+    const int c = plan_try(longest, lane);
+    const float cost = plan_cost<K>(segs, longest, c), least = wave_min(cost);
+    const int best = __builtin_amdgcn_readlane(c, __builtin_ctzll(__builtin_amdgcn_ballot_w64(cost == least)));
+    return best >= longest ? kWhole : best;
 }
 
 __device__ __forceinline__ int pieces(int units, int chunk) { return max(1, (units - 1) / chunk + 1); }
@@ -210,6 +222,7 @@ __device__ __forceinline__ Item find_item(const ChunkArgs& a, int id, int lane) 
         return it;
     }
     it.chunk = plan_chunk<K>(a, lane);
+    if (SEGMENT && it.chunk == kWhole) return it;    // nothing to merge
     auto at = [&](int b0) { return b0 + lane < a.B ? seq_of<K>(a, b0 + lane) : Seq{0, 0, 0, 0}; };
     const bool by_head = !SEGMENT && a.H % 8 == 0;
     const int heads = by_head ? a.H / 8 : a.H;   // of those that x counts
@@ -1120,7 +1133,7 @@ template <typename K>
 __device__ __forceinline__ void merge_rows(const ChunkArgs& a, int id, int lane) {
     constexpr int R = K::kRows, kParts = R / kMergeRows;
     const Item it = find_item<K, true>(a, id / kParts, lane);
-    if (it.tile < 0) return;
+    if (it.tile < 0 || it.chunk == kWhole) return;
     const int b = __builtin_amdgcn_readfirstlane(it.b), h = __builtin_amdgcn_readfirstlane(it.h);
     const int tile = __builtin_amdgcn_readfirstlane(it.tile);
     const Seq seq = seq_of<K>(a, b);
@@ -1135,8 +1148,16 @@ __device__ __forceinline__ void merge_rows(const ChunkArgs& a, int id, int lane)
         if (r >= rows) break;
         const float* ml = a.ws_ml + slot * 2 * R + in;
         const float* acc = a.ws_acc + (slot * R + in) * kD + ch;
-        // 32 pieces at a time: lane c % 32 has piece c's maximum and sum
+        // 32 pieces at a time: lane c % 32 has piece c's maximum and sum; sums come
+        // eight loads at a time, the first ones on their way beside those
         const int mine = lane & 31;
+        f32x4 v[8];
+        auto sums = [&](int c0) {
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+                v[c] = *reinterpret_cast<const f32x4*>(acc + (int64_t)min(c0 + c, nc - 1) * R * kD);
+        };
+        sums(0);
         float top = -INFINITY;
         for (int c = mine; c < nc; c += 32) top = fmaxf(top, ml[(int64_t)c * 2 * R]);
         top = half_reduce(top, lane, [](float p, float q) { return fmaxf(p, q); });
@@ -1151,10 +1172,7 @@ __device__ __forceinline__ void merge_rows(const ChunkArgs& a, int id, int lane)
             }
             const int n = min(32, nc - c0);
             for (int c1 = 0; c1 < n; c1 += 8) {
-                f32x4 v[8];                      // (eight loads on their way at a time)
-#pragma unroll
-                for (int c = 0; c < 8; ++c)
-                    v[c] = *reinterpret_cast<const f32x4*>(acc + (int64_t)(c0 + min(c1 + c, n - 1)) * R * kD);
+                if (c0 + c1 > 0) sums(c0 + c1);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int c = 0; c < 8; ++c) {
@@ -1191,7 +1209,7 @@ struct HostPlan {
 };
 
 template <typename K>
-HostPlan host_plan(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t t_cap, bool lens) {
+HostPlan host_plan(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t t_cap, bool lens, int units = 0) {
     HostPlan p;
     const int64_t rows = (int64_t)n_q * (Hq / Hkv);
     // chunks of unlike lengths may be of either kind
@@ -1204,7 +1222,15 @@ HostPlan host_plan(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t t_ca
     // here where all chunks are full.
     // Every workgroup reads all lengths then: not of more than 128 sequences,
     // which fill the GPU by themselves.
-    const bool cuts = p.runs && pieces > 1 && B <= 128 && (lens || p.segs < 2 * K::kAtOnce);
+    bool cuts = p.runs && pieces > 1 && B <= 128 && (lens || p.segs < 2 * K::kAtOnce);
+    if (cuts && units > 0) {
+        // every segment has these blocks, so the plan is known here: none is cut
+        // where no plan costs less, and nothing is merged
+        float least = plan_cost<K>((float)p.segs, units, std::max(units, kLeast));
+        bool better = false;
+        for (int n = 1; n < kWave; ++n) better |= plan_cost<K>((float)p.segs, units, plan_try(units, n)) < least;
+        cuts = better;
+    }
     p.slots = cuts ? std::min<int64_t>(4 * K::kAtOnce + 8, p.segs * pieces) : 0;
     p.grid = (std::max(p.segs, p.slots) + 7) / 8 * 8;
     p.merges = cuts ? std::min<int64_t>(2 * K::kAtOnce, p.segs) * (K::kRows / kMergeRows) : 0;
@@ -1232,8 +1258,10 @@ size_t chunk_workspace_bytes(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, in
 }
 
 int launch_chunk(const ChunkSource& src, const ChunkCall& c, void* ws, uint32_t* status, hipStream_t stream) {
-    const HostPlan pf = host_plan<Few>(c.B, c.n_q, c.Hq, c.Hkv, c.t_cap, c.q_lens != nullptr);
-    const HostPlan pm = host_plan<Many>(c.B, c.n_q, c.Hq, c.Hkv, c.t_cap, c.q_lens != nullptr);
+    // blocks of every segment, where no lengths on the device say otherwise
+    const int units = c.q_lens || c.seq_lens || c.window > 0 ? 0 : (int)(((int64_t)c.t_cap + kBlk - 1) / kBlk);
+    const HostPlan pf = host_plan<Few>(c.B, c.n_q, c.Hq, c.Hkv, c.t_cap, c.q_lens != nullptr, units);
+    const HostPlan pm = host_plan<Many>(c.B, c.n_q, c.Hq, c.Hkv, c.t_cap, c.q_lens != nullptr, units);
     ChunkArgs a;
     a.q = c.q.p;
     a.q_sb = c.q.sb;
