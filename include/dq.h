@@ -637,7 +637,8 @@ int dq_q8_evict_paged(int32_t batch, int32_t kv_heads, const int32_t* seq_lens, 
  *       contiguous; either may be absent (NULL, 0 heads).  q_out, k_out: where
  *       the results go, at strides of their own: the same tensor (same address
  *       and strides), or one that overlaps neither input, in which no two
- *       elements share an address.
+ *       elements share an address.  Queries and keys that start at one address
+ *       are not rotated in place.
  *   positions: device int32, position of token t of sequence b at
  *       positions[b pos_stride_b + t pos_stride_t], of any sign; or NULL:
  *       positions are t0 + t, plus starts[b] where starts (device int32 [batch])
@@ -672,6 +673,7 @@ int dq_rope(int32_t layout, int32_t transposed, const double* freq, float magnit
  *   q:   bf16 [batch][n_q][q_heads][128] at element strides, channels contiguous;
  *        query head i reads KV head i / (q_heads / kv_heads)
  *   out: bf16 [batch][n_q][q_heads][128] likewise, no two elements at one address
+ *        and none at one of the inputs
  *   q_lens: device int32 [batch] or NULL: the first q_lens[b] of the n_q queries
  *        count (each in [0, n_q]); NULL: all.  Output rows behind them are left
  *        as they are.
@@ -702,9 +704,11 @@ int dq_rope(int32_t layout, int32_t transposed, const double* freq, float magnit
  *        [0, n_kv]); NULL: n_kv
  *   mask: device u8 [batch][n_kv], rows mask_stride_b apart, or NULL: states with
  *        0 are hidden (their keys and values may hold anything)
- * A query whose sequence has no visible state gives zeros.  Infinities and NaN
- * in a query or a visible state give what the formula gives.  Weights are rounded to
- * bf16 for the product with the values.  n_kv is at most 2^30.
+ * A query whose sequence has no visible state gives zeros.  Infinities and NaN in
+ * a query or a visible state give what the formula gives in fp32, in which the
+ * scores are held, but a query whose every score is -infinity gives zeros.
+ * Weights are rounded to bf16 for the product with the values.  n_kv is at most
+ * 2^30.
  *
  * dq_chunk_workspace_bytes: for both; t_cap is the cache's capacity (max_pages *
  * page_tokens) or n_kv.  0 for sizes that the calls refuse.

@@ -441,15 +441,15 @@ struct Rows {
             }
             if (a.negative) q[j] ^= 0x80008000u;
         }
+        int top = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                top = max(top, max((int)(q[j][i] & 0x7FFFu), (int)((q[j][i] >> 16) & 0x7FFFu)));
+        top = max(top, __float_as_int(xor_lane<32>(__int_as_float(top), lane)));
+        const bool nan = top >= 0x7F80;          // infinities and NaN make the row NaN, if it sees a token
         if constexpr (q8) {
-            int top = 0;
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    top = max(top, max((int)(q[j][i] & 0x7FFFu), (int)((q[j][i] >> 16) & 0x7FFFu)));
-            top = max(top, __float_as_int(xor_lane<32>(__int_as_float(top), lane)));
-            const bool nan = top >= 0x7F80;      // infinities and NaN make the row NaN
             if (nan && end > 0 && T > 0) l = NAN;
             const int up = 13 - (top >= 0x80 ? (top >> 7) - 127 : -126);
             qc = ldexpf(qc, -up);
@@ -461,6 +461,8 @@ struct Rows {
                     const float y = ldexpf(__uint_as_float(q[j][i] & 0xFFFF0000u), up);
                     q[j][i] = nan ? 0u : weights2<SRC>(x, y);
                 }
+        } else if (nan) {                        // (one NaN channel: NaN with every key)
+            q[0][0] = 0x7FC07FC0u;
         }
     }
 
@@ -520,6 +522,7 @@ struct Rows {
         float top = s[0];                        // (NaN where every score is)
 #pragma unroll
         for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
+        if constexpr (!q8) l = top == INFINITY ? NAN : l;    // as the formula has it
         top *= c;
         // scores so large that a fused product would differ from the maximum by
         // more than a rounding of it

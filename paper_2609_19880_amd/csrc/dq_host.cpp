@@ -948,6 +948,8 @@ int dq_rope(int32_t layout, int32_t transposed, const double* freq, float magnit
     if (int rc = check_rope_rows(rq, B, T, head_dim)) return rc;
     if (int rc = check_rope_rows(rk, B, T, head_dim)) return rc;
     if (!freq || Hq + Hkv == 0) return DQ_ERR_INVALID_ARG;
+    // one's result over the other or its result
+    if (Hq && Hkv && (qo == k || ko == q || qo == ko)) return DQ_ERR_INVALID_ARG;
     return dq::launch_rope(layout, transposed, freq, magnitude, rotary_dim, rq, rk, B, T, head_dim, positions, psb,
                            pst, starts, t0, static_cast<hipStream_t>(stream));
 }

@@ -25,7 +25,7 @@ def _with(args, changes):
 
 
 ROPE = dict(layout=0, tr=0, freq=P, mag=1.0, r=128, d=128, B=2, T=5, q=P, qsb=5 * 4096, qst=4096, qsh=128, Hq=32, qo=P,
-            qosb=5 * 4096, qost=4096, qosh=128, k=P, ksb=5 * 1024, kst=1024, ksh=128, Hkv=8, ko=P, kosb=5 * 1024,
+            qosb=5 * 4096, qost=4096, qosh=128, k=2 * P, ksb=5 * 1024, kst=1024, ksh=128, Hkv=8, ko=2 * P, kosb=5 * 1024,
             kost=1024, kosh=128, pos=None, psb=0, pst=0, starts=None, t0=0, stream=None)
 
 
@@ -37,6 +37,8 @@ ROPE = dict(layout=0, tr=0, freq=P, mag=1.0, r=128, d=128, B=2, T=5, q=P, qsb=5 
     dict(qosb=0), dict(qost=0), dict(qosh=0), dict(qosh=64), dict(kost=512), dict(kosb=1024), dict(pos=P, starts=P),
     dict(pos=P, t0=1), dict(pos=P, psb=-1), dict(pos=P, pst=-1),
     dict(Hq=0, q=None, qo=None, Hkv=0, k=None, ko=None),
+    # a result over the other's input or result
+    dict(k=P), dict(ko=P), dict(qo=2 * P), dict(k=3 * P, ko=P), dict(k=P, ko=3 * P),
     # in place the strides have to be the same
     dict(qsh=256, qosh=128), dict(ksb=0, kosb=5 * 1024), dict(qosb=1 << 62)])
 def test_rope_refusals(bad):

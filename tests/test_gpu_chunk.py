@@ -528,6 +528,38 @@ def test_cross_extremes(dq):
         assert bool(torch.isnan(out[0, :, 0, 9]).all())
 
 
+@pytest.mark.parametrize("n", [40, 200])
+def test_cross_infinities(dq, n):
+    """What the formula gives: an infinite query or a score of +infinity NaN, a
+    score of -infinity no weight, an infinite value itself."""
+    k, v = _kv(1, 1, 200, 1)
+    q = _q(1, 1, n, 1)
+    q[0, 7, 0, 9] = 0
+    clean = _cross(dq, q, k, v)
+    for x in (math.inf, -math.inf):
+        bad = q.clone()
+        bad[0, 3, 0, 5] = x
+        out = _cross(dq, bad, k, v)
+        keep = torch.arange(n) != 3
+        assert bool(torch.isnan(out[0, 3]).all()) and torch.equal(out[0, keep], clean[0, keep])
+        zeros = _cross(dq, bad, k, v, [0])
+        assert bool((zeros == 0).all())
+        key, value = k.clone(), v.clone()
+        key[0, 150, 0, 9], value[0, 150, 0, 9] = x, x
+        out = _cross(dq, q, key, v)
+        without = torch.arange(200)[None] != 150
+        hidden = _cross(dq, q, k, v, None, without)
+        none = ((q[0, :, 0, 9] * x) < 0)                  # (0 times infinity: NaN)
+        assert bool(torch.isnan(out[0][~none]).all())
+        # (another maximum than with the token hidden by the mask: close, not equal)
+        assert bool(((out[0][none].double() - hidden[0][none].double()).norm(dim=-1)
+                     <= 2.0 ** -6 * v.double().norm(dim=-1).max().item()).all())
+        out = _cross(dq, q, k, value)
+        assert bool((out[0, :, 0, 9] == x).all())
+        rest = torch.arange(128) != 9
+        assert torch.equal(out[..., rest], clean[..., rest])
+
+
 def test_cross_graph(dq):
     B, T, n, H = 3, 700, 1, 2
     k, v = (x.to(DEV) for x in _kv(1, B, T, H))
