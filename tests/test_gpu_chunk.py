@@ -171,6 +171,21 @@ def test_window(dq, fmt, window, sinks):
     _check_all(out, q, _held(k, fmt), _held(v, fmt), lens, [n] * B, window=window, sinks=sinks)
 
 
+@pytest.mark.parametrize("window,sinks", [(0, 0), (900, 50)])
+@pytest.mark.parametrize("B,T,n,H,G", [(1, 4100, 63, 1, 1), (1, 4100, 64, 8, 1), (1, 4100, 65, 1, 1), (2, 3001, 13, 8, 5),
+                                       (2, 3001, 26, 8, 5), (1, 2050, 129, 16, 1), (3, 1999, 43, 5, 3)])
+def test_pieces(dq, B, T, n, H, G, window, sinks):
+    """Sequences that are cut, of row counts around the variants' borders, heads
+    that are and are not a multiple of 8."""
+    fmt = FMTS[n % 2]
+    k, v = _kv(T + n, B, T, H)
+    q = _q(T, B, n, H * G)
+    cache = _filled(dq, fmt, k, v, H * G)
+    lens = [T - 5 * b for b in range(B)]
+    out = cache.attend_chunk(q.to(DEV), _i32(lens), window=window, sinks=sinks)
+    _check_all(out, q, _held(k, fmt), _held(v, fmt), lens, [n] * B, window=window, sinks=sinks)
+
+
 @pytest.mark.parametrize("n,window,sinks", [(3, 64, 4), (300, 64, 40)])
 def test_window_of_a_long_sequence(dq, n, window, sinks):
     """Far behind the window nothing is read: what lies there may be anything."""
@@ -484,6 +499,19 @@ def test_cross_lengths_and_masks(dq, n):
             x[b, :lens[b]] = (k if x is dirty_k else v)[b, :lens[b]]
     got = _cross(dq, q, dirty_k, dirty_v, lens, None, new)
     _check_cross(got, q, k, v, lens, new)
+
+
+@pytest.mark.parametrize("B,T,n,H,G", [(1, 4100, 64, 8, 1), (1, 4100, 65, 1, 1), (2, 2500, 40, 3, 4)])
+def test_cross_pieces(dq, B, T, n, H, G):
+    """Sequences that are cut, pieces among them that the mask leaves nothing of."""
+    k, v = _kv(n, B, T, H)
+    q = _q(n, B, n, H * G)
+    mask = torch.rand((B, T), generator=torch.Generator().manual_seed(5)) < 0.5
+    mask[0, 300:1900] = False
+    lens = [T - 40 * b for b in range(B)]
+    for m in (None, mask):
+        _check_cross(_cross(dq, q, k, v, lens, m), q, k, v, lens, [n] * B, m)
+        _check_cross(_cross(dq, q, k, v, None, m), q, k, v, [T] * B, [n] * B, m)
 
 
 @pytest.mark.parametrize("n", [2, 90])
