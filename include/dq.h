@@ -706,7 +706,8 @@ int dq_rope(int32_t layout, int32_t transposed, const double* freq, float magnit
  *        0 are hidden (their keys and values may hold anything)
  * A query whose sequence has no visible state gives zeros.  Infinities and NaN in
  * a query or a visible state give what the formula gives in fp32, in which the
- * scores are held, but a query whose every score is -infinity gives zeros.
+ * scores are held, but a query whose every score is -infinity gives zeros
+ * and sums of values above 2^80 may overflow.
  * Weights are rounded to bf16 for the product with the values.  n_kv is at most
  * 2^30.
  *

@@ -542,6 +542,9 @@ def test_cross_extremes(dq):
     assert dq.dq_cross_attention(q[:, :0].to(DEV), k.to(DEV), v.to(DEV)).shape == (1, 0, 1, 128)
     for scale in (0.0, -0.2, 2.0):
         _check_cross(_cross(dq, q, k, v, scale=scale), q, k, v, [T], [40], scale=scale)
+    big = (v.float() * 2.0 ** 76).to(torch.bfloat16)
+    out, want = _cross(dq, q, k, big), _cross(dq, q, k, v)
+    assert torch.equal(out.float() * 2.0 ** -76, want.float())
     out = _cross(dq, q, k, v, scale=1e30)
     assert bool(torch.isfinite(out.float()).all())
     bad = q.clone()
