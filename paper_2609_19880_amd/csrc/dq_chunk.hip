@@ -595,6 +595,19 @@ typedef const __attribute__((address_space(1))) float* GlobalFloats;
 typedef const __attribute__((address_space(1))) int32_t* GlobalInts;
 typedef const __attribute__((address_space(1))) u32x4* GlobalPieces;
 
+// Eight channels of a BF16 row.
+__device__ __forceinline__ u32x4 row_piece(const uint16_t* x, bool aligned) {
+    if (aligned) return *reinterpret_cast<GlobalPieces>(reinterpret_cast<uintptr_t>(x));
+    u32x4 r;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) r[w] = (uint32_t)x[2 * w] | ((uint32_t)x[2 * w + 1] << 16);
+    return r;
+}
+
+// Of a block's tokens, bit by bit, the first n (rows behind the last token are
+// read as the last one's and hidden).
+__device__ __forceinline__ uint32_t shown_to(int n) { return n >= kBlk ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
+
 template <int SRC>
 __device__ __forceinline__ void read_keys(const char* at, int part, int lane, u32x4 (&kf)[4]) {
     const char* p = at + (lane >> 5) * (Lds<SRC>::kKeyOp / 2) + (lane & 31) * 16;
@@ -752,8 +765,8 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
     if constexpr (!q8) {
         k_st = a.k_st;
         v_st = a.v_st;
-        k_row = reinterpret_cast<const uint16_t*>(a.k) + b * a.k_sb + h * a.k_sh + (tid >> 4) * k_st + 8 * (tid & 15);
-        v_row = reinterpret_cast<const uint16_t*>(a.v) + b * a.v_sb + h * a.v_sh + (tid >> 4) * v_st + 8 * (tid & 15);
+        k_row = reinterpret_cast<const uint16_t*>(a.k) + b * a.k_sb + h * a.k_sh + 8 * (tid & 15);
+        v_row = reinterpret_cast<const uint16_t*>(a.v) + b * a.v_sb + h * a.v_sh + 8 * (tid & 15);
     }
     auto look_up = [&](int u) {
         if (q8 && a.pg.bt && u < u1) page = table[((block_of(u) * kBlk) >> a.pg.page_shift) + none];
@@ -778,17 +791,8 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
         } else {
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) {
-                const int t0 = u * kBlk + 16 * (i & 1);
-                if (t0 + (tid >> 4) < see.T) {
-                    const uint16_t* x = i >> 1 ? v_row + t0 * v_st : k_row + t0 * k_st;
-                    if (a.kv_aligned) {
-                        reg[i] = *reinterpret_cast<const u32x4*>(x);
-                    } else {
-#pragma unroll
-                        for (int w = 0; w < 4; ++w)
-                            reg[i][w] = (uint32_t)x[2 * w] | ((uint32_t)x[2 * w + 1] << 16);
-                    }
-                }
+                const int t = min(u * kBlk + 16 * (i & 1) + (tid >> 4), see.T - 1);
+                reg[i] = row_piece(i >> 1 ? v_row + t * v_st : k_row + t * k_st, a.kv_aligned);
             }
         }
     };
@@ -801,7 +805,11 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
             mreg = u < u1 && t < see.T ? mask[t] : 0;
         }
     };
-    auto shown_now = [&]() -> uint32_t { return mask ? (uint32_t)__builtin_amdgcn_ballot_w64(mreg != 0) : ~0u; };
+    // of block u, whose mask was requested last
+    auto shown_now = [&](int u) -> uint32_t {
+        const uint32_t all = mask ? (uint32_t)__builtin_amdgcn_ballot_w64(mreg != 0) : ~0u;
+        return q8 ? all : all & shown_to(see.T - u * kBlk);
+    };
     auto keys_at = [&](int step) { return lds + (step & 1) * L::kStage; };
     auto values_at = [&](int step) { return lds + (step & 1) * L::kStage + L::kKeys; };
     // where this thread's pieces of stage 0 go
@@ -835,7 +843,7 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
             for (int i = 0; i < 2; ++i) {
                 *reinterpret_cast<u32x4*>(to + k_to + 256 * i) = reg[i];
                 // (a hidden token's value must not reach the sum, whatever it is)
-                if (mask && !((shown >> (16 * i + (tid >> 4))) & 1)) reg[2 + i] = u32x4{0u, 0u, 0u, 0u};
+                if (!((shown >> (16 * i + (tid >> 4))) & 1)) reg[2 + i] = u32x4{0u, 0u, 0u, 0u};
                 *reinterpret_cast<u32x4*>(to + v_to + 16 * i * L::kValRow) = reg[2 + i];
             }
         }
@@ -846,7 +854,7 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
         request_mask(u0);
         request(u0);
         look_up(u0 + 1);
-        uint32_t shown = shown_now();
+        uint32_t shown = shown_now(u0);
         lay(0, shown);
         request_mask(u0 + 1);
         request(u0 + 1);
@@ -854,7 +862,7 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
         __syncthreads();
         int step = 0;
         for (int u = u0; u < u1; ++u, ++step) {
-            const uint32_t shown_next = shown_now();
+            const uint32_t shown_next = shown_now(u + 1);
             lay(step + 1, shown_next);
             request_mask(u + 2);
             request(u + 2);
@@ -1009,20 +1017,15 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_kernel(ChunkArgs a) {
             const int64_t st = values ? a.v_st : a.k_st;
             const uint16_t* base = reinterpret_cast<const uint16_t*>(values ? a.v : a.k) +
                                    b * (values ? a.v_sb : a.k_sb) + h * (values ? a.v_sh : a.k_sh) + 8 * (lane & 15);
+            const int t = u * kBlk + (lane >> 4);
+            if (a.kv_aligned && u * kBlk + kBlk <= see.T) {
+                const uint16_t* x = base + t * st;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int t = u * kBlk + 4 * i + (lane >> 4);
-                raw[i] = u32x4{0u, 0u, 0u, 0u};
-                if (t < see.T) {
-                    const uint16_t* x = base + t * st;
-                    if (a.kv_aligned) {
-                        raw[i] = *reinterpret_cast<const u32x4*>(x);
-                    } else {
+                for (int i = 0; i < 8; ++i, x += 4 * st)
+                    raw[i] = *reinterpret_cast<GlobalPieces>(reinterpret_cast<uintptr_t>(x));
+            } else {
 #pragma unroll
-                        for (int w = 0; w < 4; ++w)
-                            raw[i][w] = (uint32_t)x[2 * w] | ((uint32_t)x[2 * w + 1] << 16);
-                    }
-                }
+                for (int i = 0; i < 8; ++i) raw[i] = row_piece(base + min(t + 4 * i, see.T - 1) * st, a.kv_aligned);
             }
         }
     };
@@ -1046,7 +1049,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_kernel(ChunkArgs a) {
     me.load(a, see, b, h, part * kRowsOf, rows, lane);
     for (; u < u1; u += every) {
         const int t0 = block_of(u) * kBlk;
-        const uint32_t shown = mask ? (uint32_t)__builtin_amdgcn_ballot_w64(mreg != 0) : ~0u;
+        uint32_t shown = mask ? (uint32_t)__builtin_amdgcn_ballot_w64(mreg != 0) : ~0u;
+        if (!q8) shown &= shown_to(see.T - t0);
         const bool on = t0 < me.lim_hi && shown != 0;
         f32x16 s = f32x16{};
         u32x4 p[2];
@@ -1093,13 +1097,16 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_kernel(ChunkArgs a) {
                         me.o[2 * i + 1] = mma<SRC>(u32x4{w2[0], w2[1], w3[0], w3[1]}, p[st], me.o[2 * i + 1]);
                     }
             } else {
+                // (a hidden token's value must not reach the sum, whatever it is)
+                if (shown != ~0u) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int t = 4 * i + (lane >> 4);
-                    // (a hidden token's value must not reach the sum, whatever it is)
-                    if (mask && !((shown >> t) & 1)) vraw[i] = u32x4{0u, 0u, 0u, 0u};
-                    *reinterpret_cast<u32x4*>(own + L::kKeys + t * L::kValRow + (lane & 15) * 16) = vraw[i];
+                    for (int i = 0; i < 8; ++i)
+                        if (!((shown >> (4 * i + (lane >> 4))) & 1)) vraw[i] = u32x4{0u, 0u, 0u, 0u};
                 }
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    *reinterpret_cast<u32x4*>(own + L::kKeys + (4 * i + (lane >> 4)) * L::kValRow + (lane & 15) * 16) =
+                        vraw[i];
                 wave_sync();
 #pragma unroll
                 for (int st = 0; st < 2; ++st) {
