@@ -8,8 +8,9 @@
 // rounded to fp32: far positions keep their fraction.  Rotations are computed
 // in fp32 and rounded to bf16 once.
 //
-// Bound by memory: every value is read and written once.  A workgroup takes
-// the heads of a few tokens and computes their cosines and sines once.
+// Bound by memory: every value is read and written once, at 5.7 TB/s over 16384
+// tokens of 40 heads of 128 (59 us).  A workgroup takes all heads of a token and
+// computes their cosines and sines once, into LDS.
 #include <math.h>
 
 #include <algorithm>
@@ -32,14 +33,12 @@ struct RopeArgs {
     const int32_t* positions;
     int64_t psb, pst;
     const int32_t* starts;
-    int64_t n;                   // B T
     int T, t0, rotary, d;
-    int tokens, split;           // tokens of a workgroup, workgroups that share their heads
+    int split;                   // workgroups that share a token's heads
     int copies[2];               // the channels behind the rotated ones are copied
     float magnitude, sign;
 };
 
-constexpr int kTokens = 4;                   // tokens per workgroup, at most
 constexpr int kMostPairs = 512;
 
 __device__ __forceinline__ float lo16(uint32_t w) { return __uint_as_float(w << 16); }
@@ -48,66 +47,86 @@ __device__ __forceinline__ uint32_t pair16(float x, float y) {
     return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x, (__bf16)y});
 }
 
-// WIDE: whole 16-byte pieces of 8 channels (half: one of each half).
+// One workgroup per token, or two that share its heads where tokens are few (fewer
+// than 1024: 2.5 us in place of 3.1 for one token of 40 heads, 4.1 in place of 4.2
+// for 512; 2048 tokens take 7.6 us with one, 8.6 with two).  Several tokens per
+// workgroup gain nothing (16384 tokens: 62 us with one, 66 with four).  An item is a
+// pair, or WIDE 16-byte pieces of 8 channels (half: one of each half), or as much
+// behind the rotated channels.  A thread's first one is on its way while the angles
+// are computed (48 x 33 tokens 11.0 to 7.2 us); more of them at a time only hold
+// registers (two 7.3, three 7.7).
 template <bool HALF, bool WIDE>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
-    __shared__ float2 turn[kTokens][kMostPairs];
-    __shared__ int where[kTokens][2];            // sequence, token
+    __shared__ float2 turn[kMostPairs];
     const int tid = threadIdx.x, pairs = a.rotary / 2;
-    const int64_t n0 = (int64_t)blockIdx.x * a.tokens;
-    const int count = (int)min((int64_t)a.tokens, a.n - n0);
-    for (int i = tid; i < count * pairs; i += 256) {
-        const int k = i / pairs, p = i - k * pairs;
-        const int b = (int)((n0 + k) / a.T), t = (int)((n0 + k) - (int64_t)b * a.T);
+    const int b = (int)(blockIdx.x / (uint32_t)a.T), t = (int)(blockIdx.x - (uint32_t)b * (uint32_t)a.T);
+    const int step = WIDE ? (HALF ? 8 : 4) : 1;                          // pairs per item
+    const int turned = pairs / step;
+    const int rest = WIDE ? (a.d - a.rotary) / 8 : a.d - a.rotary;
+    const uint32_t per = (uint32_t)(turned + rest);                      // items of a head
+    const int items = (a.heads[0] + a.heads[1]) * (int)per, every = 256 * a.split;
+    const uint16_t* in0 = a.in[0] + b * a.isb[0] + t * a.ist[0];
+    const uint16_t* in1 = a.in[1] + b * a.isb[1] + t * a.ist[1];
+    uint16_t* out0 = a.out[0] + b * a.osb[0] + t * a.ost[0];
+    uint16_t* out1 = a.out[1] + b * a.osb[1] + t * a.ost[1];
+    u32x4 x, y;
+    uint16_t* to = nullptr;
+    int e = -1;
+    // first channel of an item
+    auto channel = [&](int e) {
+        if (e >= turned) return a.rotary + (e - turned) * (WIDE ? 8 : 1);
+        return WIDE ? 8 * e : HALF ? e : 2 * e;
+    };
+    auto load = [&](int i) {
+        e = -1;                                  // nothing, or nothing to do
+        if (i >= items) return;
+        int h = (int)((uint32_t)i / per);
+        const int c = i - h * (int)per;
+        const bool key = h >= a.heads[0];
+        if (key) h -= a.heads[0];
+        if (c >= turned && !(key ? a.copies[1] : a.copies[0])) return;
+        e = c;
+        const uint16_t* in = (key ? in1 : in0) + h * (key ? a.ish[1] : a.ish[0]) + channel(c);
+        to = (key ? out1 : out0) + h * (key ? a.osh[1] : a.osh[0]) + channel(c);
+        if constexpr (WIDE) {
+            x = *reinterpret_cast<const u32x4*>(in);
+            if (HALF && c < turned) y = *reinterpret_cast<const u32x4*>(in + pairs);
+        } else {
+            x[0] = in[0];
+            if (c < turned) x[1] = in[HALF ? pairs : 1];
+        }
+    };
+    int i = tid + 256 * (int)blockIdx.y;
+    load(i);
+    for (int p = tid; p < pairs; p += 256) {
         int64_t at = (int64_t)a.t0 + t;
         if (a.positions)
             at = a.positions[b * a.psb + t * a.pst];
         else if (a.starts)
             at += a.starts[b];
-        double x = (double)at * a.freq[p] * 0.15915494309189533577;     // turns
-        x -= rint(x);
+        double z = (double)at * a.freq[p] * 0.15915494309189533577;     // turns
+        z -= rint(z);
         float s, c;
-        sincospif(2.f * (float)x, &s, &c);
-        turn[k][p] = float2{c * a.magnitude, s * a.sign};
-    }
-    if (tid < count) {
-        where[tid][0] = (int)((n0 + tid) / a.T);
-        where[tid][1] = (int)((n0 + tid) % a.T);
+        sincospif(2.f * (float)z, &s, &c);
+        turn[p] = float2{c * a.magnitude, s * a.sign};
     }
     __syncthreads();
-    const int step = WIDE ? (HALF ? 8 : 4) : 1;                          // pairs per item
-    const int turned = pairs / step;
-    const int rest = WIDE ? (a.d - a.rotary) / 8 : a.d - a.rotary;
-    const int per = turned + rest;                                       // items of a head
-    const int heads = a.heads[0] + a.heads[1];
-    const int items = count * heads * per;
-    for (int i = tid + 256 * (int)blockIdx.y; i < items; i += 256 * a.split) {
-        const int e = i % per, hk = i / per, k = hk / heads;
-        int h = hk - k * heads;
-        const int w = h >= a.heads[0];
-        if (w) h -= a.heads[0];
-        const int b = where[k][0], t = where[k][1];
-        const uint16_t* in = a.in[w] + b * a.isb[w] + t * a.ist[w] + h * a.ish[w];
-        uint16_t* out = a.out[w] + b * a.osb[w] + t * a.ost[w] + h * a.osh[w];
+    for (; i < items; i += every, load(i)) {
+        if (e < 0) continue;
         if (e >= turned) {
-            if (!a.copies[w]) continue;
-            const int c = a.rotary + (e - turned) * (WIDE ? 8 : 1);
             if constexpr (WIDE)
-                *reinterpret_cast<u32x4*>(out + c) = *reinterpret_cast<const u32x4*>(in + c);
+                *reinterpret_cast<u32x4*>(to) = x;
             else
-                out[c] = in[c];
+                to[0] = (uint16_t)x[0];
             continue;
         }
-        const float2* cs = &turn[k][e * step];
+        const float2* cs = &turn[e * step];
         if constexpr (!WIDE) {
-            const int ca = HALF ? e : 2 * e, cb = HALF ? e + pairs : 2 * e + 1;
-            const float x = bf16_to_f32(in[ca]), y = bf16_to_f32(in[cb]);
-            const uint32_t r = pair16(fmaf(x, cs->x, -(y * cs->y)), fmaf(x, cs->y, y * cs->x));
-            out[ca] = (uint16_t)r;
-            out[cb] = (uint16_t)(r >> 16);
+            const float p = lo16(x[0]), q = lo16(x[1]);
+            const uint32_t r = pair16(fmaf(p, cs->x, -(q * cs->y)), fmaf(p, cs->y, q * cs->x));
+            to[0] = (uint16_t)r;
+            to[HALF ? pairs : 1] = (uint16_t)(r >> 16);
         } else if constexpr (HALF) {
-            const u32x4 x = *reinterpret_cast<const u32x4*>(in + 8 * e);
-            const u32x4 y = *reinterpret_cast<const u32x4*>(in + pairs + 8 * e);
             u32x4 u, v;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -116,17 +135,16 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
                 u[j] = pair16(fmaf(x0, c0.x, -(y0 * c0.y)), fmaf(x1, c1.x, -(y1 * c1.y)));
                 v[j] = pair16(fmaf(x0, c0.y, y0 * c0.x), fmaf(x1, c1.y, y1 * c1.x));
             }
-            *reinterpret_cast<u32x4*>(out + 8 * e) = u;
-            *reinterpret_cast<u32x4*>(out + pairs + 8 * e) = v;
+            *reinterpret_cast<u32x4*>(to) = u;
+            *reinterpret_cast<u32x4*>(to + pairs) = v;
         } else {
-            const u32x4 x = *reinterpret_cast<const u32x4*>(in + 8 * e);
             u32x4 u;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float p = lo16(x[j]), q = hi16(x[j]);
                 u[j] = pair16(fmaf(p, cs[j].x, -(q * cs[j].y)), fmaf(p, cs[j].y, q * cs[j].x));
             }
-            *reinterpret_cast<u32x4*>(out + 8 * e) = u;
+            *reinterpret_cast<u32x4*>(to) = u;
         }
     }
 }
@@ -163,17 +181,15 @@ int launch_rope(int layout, int transposed, const double* freq, float magnitude,
     a.psb = pos_sb;
     a.pst = pos_st;
     a.starts = starts;
-    a.n = (int64_t)B * T;
     a.T = T;
     a.t0 = t0;
     a.rotary = rotary;
     a.d = d;
     a.magnitude = magnitude;
     a.sign = transposed ? -magnitude : magnitude;
-    a.tokens = a.n >= 1024 * kTokens ? kTokens : 1;
-    // few tokens: workgroups share a token's heads
-    a.split = a.n >= 512 ? 1 : 2;
-    const dim3 grid((unsigned)((a.n + a.tokens - 1) / a.tokens), a.split);
+    const int64_t n = (int64_t)B * T;
+    a.split = n >= 1024 ? 1 : 2;
+    const dim3 grid((unsigned)n, a.split);
     if (layout == DQ_ROPE_HALF)
         wide ? rope_kernel<true, true><<<grid, 256, 0, stream>>>(a) : rope_kernel<true, false><<<grid, 256, 0, stream>>>(a);
     else
