@@ -84,19 +84,22 @@ struct Seq {
 };
 
 // Sequences of few rows and of many have a kernel each (tiles: 0 for the other's).
+// The border, measured on both sides: 64 x 10 queries over 1024 tokens (40 rows a
+// head) take 54 us as few rows, 87 as many; 16 x 20 queries over 16384 tokens (80
+// rows) 201 us as many, 288 as few with tiles of 128.
 struct Few {
     static constexpr int kRows = 64;             // of a tile
     static constexpr bool kFew = true;
-    static constexpr int kAtOnce = 256;          // workgroups that the GPU takes at a time
+    static constexpr int kAtOnce = 256;          // workgroups that the GPU takes at a time: one per CU
     static constexpr int kCost = 16;             // what an item costs besides its blocks, in blocks
 };
 struct Many {
     static constexpr int kRows = 128;
     static constexpr bool kFew = false;
-    static constexpr int kAtOnce = 768;
+    static constexpr int kAtOnce = 768;          // three per CU
     static constexpr int kCost = 8;
 };
-constexpr int kLeast = 8;                        // blocks of one piece, at least
+constexpr int kLeast = 8;                        // blocks of one piece, at least (4: no faster)
 
 template <typename K>
 __device__ __forceinline__ Seq seq_of(const ChunkArgs& a, int b) {
@@ -168,6 +171,8 @@ __device__ __forceinline__ int plan_chunk(const ChunkArgs& a, int lane) {
     if (segs >= kMost) return kWhole;
     if (total < 0.75f * segs * (float)longest) {
         // unlike lengths leave pieces that are not full: small ones even out the end
+        // (48 ragged chunks 600 us with pieces of what a place has, 616 to 630 with
+        // 1.3 of it, or 1/1.5, 1/2 and 1/4)
         return max((int)ceilf(total / K::kAtOnce), kLeast);
     }
     // lane l tries l + 1 pieces per segment
@@ -195,9 +200,10 @@ __device__ __forceinline__ int scan64(int v) {         // inclusive sums over th
 //
 // Workgroups go to the 8 XCDs in turn; what shares keys and values should meet in
 // one L2, and all XCDs should have sequences of every length: each takes its
-// heads of all sequences where there are a multiple of 8, else an eighth of the
-// items.  Items come in three passes, the whole pieces, the last ones of more
-// than half a piece and the rest: short work evens out the end.
+// heads of all sequences where there are a multiple of 8 (4 x 4096 queries over
+// states of unlike lengths 2.57 to 2.11 ms), else an eighth of the items.  Items
+// come in three passes, the whole pieces, the last ones of more than half a piece
+// and the rest: short work evens out the end (48 ragged chunks 0.67 to 0.60 ms).
 template <typename K, bool SEGMENT>
 __device__ __forceinline__ Item find_item(const ChunkArgs& a, int id, int lane) {
     Item it{0, 0, -1, 0, kWhole, 0};
@@ -388,7 +394,9 @@ __device__ __forceinline__ float plus_weights(uint32_t w, float x) {
 // until a block's weights, relative to it, add up to more than 2^15: weights of
 // m itself are 2^2, so fp16 holds what lies 2^13 above and, to its 11 bits, 2^16
 // below (to 2^-25 beyond).  Most blocks so need no maximum and scale nothing:
-// their weights are computed with the m at hand and only checked.  A row's bits
+// their weights are computed with the m at hand and only checked (the exchange of
+// a maximum between two lanes and the scaling of 64 sums would be a third of the
+// vector instructions).  A row's bits
 // do not depend on the rows beside it, but where their scores pass 2^11.  (BF16:
 // m itself weighs 1.  Any limit would do for bf16's range; 2^60 in place of 2^15 is
 // no faster, 2^8 loses 4 %, and larger weights bring the sums of large values
@@ -711,6 +719,15 @@ __device__ __forceinline__ void join_rows(const ChunkArgs& a, const f32x16 (&o)[
 // per block.  Three wavefronts per SIMD, of three workgroups, hide one another's
 // waits; more would leave too few registers for the sums (64), the queries (32)
 // and a block's scores.
+//
+// Bound by no single unit: 4 x 8171 queries over themselves (32 heads, int8) run at
+// 915 TFLOP/s, where the matrix units are busy 42 % of the time, other vector
+// instructions (131 per wavefront and block, 16 of them exponentials) issue about
+// as long, LDS is active 33 %, and the clock falls to 1.9 GHz.  Left out one at a
+// time, exponentials, the weights' sums, conversions, loads or the second product
+// each give back 3 to 9 %.  Not faster: two wavefronts per SIMD with the blocks'
+// steps interleaved, twelve wavefronts per workgroup (2 to 5 % on the largest, slower
+// elsewhere), two or three blocks requested ahead, wavefront priorities.
 template <int SRC>
 __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
     typedef Lds<SRC> L;
@@ -944,7 +961,8 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
 // it for itself; the wavefronts' sums are joined in LDS at the end.  Bound by
 // memory: a block's codes are requested as soon as the registers of the last
 // one's are free, keys while the weights are computed, values while the next
-// scores are.
+// scores are.  16 x 8 queries over 32768 e4m3 tokens (32 heads) take 182 us, 5.9
+// TB/s (262 with the codes converted through LDS for all wavefronts).
 //
 // Values of codes: a lane reads whole 16-byte pieces (two channels 16 apart of 8
 // tokens), so that operand 2 m + e has channels 64 m + 32 (row / 16) + 16 e +
@@ -1129,7 +1147,9 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_kernel(ChunkArgs a) {
 }
 
 // The pieces of a segment's rows joined: a workgroup has 16 rows, half a
-// wavefront each at a time, four channels a lane.
+// wavefront each at a time, four channels a lane.  Bound by latency (lengths, plan,
+// maxima, sums): 7 us for 16 pieces of 16 rows, 4 us where nothing is cut, and by
+// memory where pieces are many (50 MB of them 14 us).
 constexpr int kMergeRows = 16;
 
 // Over the 32 lanes of half a wavefront; every lane gets the result.
