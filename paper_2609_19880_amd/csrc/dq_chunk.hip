@@ -69,6 +69,7 @@ struct ChunkArgs {
     uint32_t* status;
     float* ws_acc;               // [slot][rows][128]
     float* ws_ml;                // [slot][2][rows]
+    int32_t* plan;               // the blocks of one piece, for the merge
 };
 
 // ------------------------------------------------------------------- shares
@@ -139,9 +140,15 @@ __host__ __device__ inline int plan_try(int longest, int n) {
     return c > kLeast ? c : kLeast;
 }
 
-// The blocks of one piece.  All lanes agree.
+// Sequence b0 + lane.
 template <typename K>
-__device__ __forceinline__ int plan_chunk(const ChunkArgs& a, int lane) {
+__device__ __forceinline__ Seq seq_at(const ChunkArgs& a, int b0, int lane) {
+    return b0 + lane < a.B ? seq_of<K>(a, b0 + lane) : Seq{0, 0, 0, 0};
+}
+
+// The blocks of one piece.  All lanes agree.  first: seq_at(a, 0, lane).
+template <typename K>
+__device__ __forceinline__ int plan_chunk(const ChunkArgs& a, const Seq& first, int lane) {
     // (sums in fp32: the same bits wherever they are taken; a chunk a millionth too
     // short adds an item, which the workspace has room for)
     float total = 0, segs = 0;
@@ -153,17 +160,10 @@ __device__ __forceinline__ int plan_chunk(const ChunkArgs& a, int lane) {
         longest = q.units;
     }
     for (int b0 = 0; b0 < a.B && a.B > 1; b0 += kWave) {
-        float t = 0, s = 0;
-        int n = 0;
-        if (b0 + lane < a.B) {
-            const Seq q = seq_of<K>(a, b0 + lane);
-            s = (float)q.tiles;
-            t = s * (float)q.units;
-            n = q.tiles ? q.units : 0;
-        }
-        total += wave_sum(t);
-        segs += wave_sum(s);
-        longest = max(longest, wave_max(n));
+        const Seq q = b0 == 0 ? first : seq_at<K>(a, b0, lane);
+        total += wave_sum((float)q.tiles * (float)q.units);
+        segs += wave_sum((float)q.tiles);
+        longest = max(longest, wave_max(q.tiles ? q.units : 0));
     }
     total *= (float)a.H;
     segs *= (float)a.H;
@@ -227,10 +227,18 @@ __device__ __forceinline__ Item find_item(const ChunkArgs& a, int id, int lane) 
         if (it.tile >= seq_of<K>(a, it.b).tiles) it.tile = -1;
         return it;
     }
-    it.chunk = plan_chunk<K>(a, lane);
-    if (SEGMENT && it.chunk == kWhole) return it;    // nothing to merge
-    auto at = [&](int b0) { return b0 + lane < a.B ? seq_of<K>(a, b0 + lane) : Seq{0, 0, 0, 0}; };
+    if constexpr (SEGMENT) {
+        it.chunk = *a.plan;                      // what the kernel before went by
+        if (it.chunk == kWhole) return it;       // nothing to merge
+    }
     const bool by_head = !SEGMENT && a.H % 8 == 0;
+    Seq first{0, 0, 0, 0};
+    if (a.B > 1 || !(SEGMENT || by_head)) first = seq_at<K>(a, 0, lane);
+    if constexpr (!SEGMENT) {
+        it.chunk = plan_chunk<K>(a, first, lane);
+        if (id == 0 && threadIdx.x == 0) *a.plan = it.chunk;
+    }
+    auto at = [&](int b0) { return b0 == 0 ? first : seq_at<K>(a, b0, lane); };
     const int heads = by_head ? a.H / 8 : a.H;   // of those that x counts
     int x = by_head ? id >> 3 : id;
     // pieces of a sequence's segment in a pass
@@ -394,9 +402,9 @@ __device__ __forceinline__ float plus_weights(uint32_t w, float x) {
 // until a block's weights, relative to it, add up to more than 2^15: weights of
 // m itself are 2^2, so fp16 holds what lies 2^13 above and, to its 11 bits, 2^16
 // below (to 2^-25 beyond).  Most blocks so need no maximum and scale nothing:
-// their weights are computed with the m at hand and only checked (the exchange of
-// a maximum between two lanes and the scaling of 64 sums would be a third of the
-// vector instructions).  A row's bits
+// their weights are computed with the m at hand and only checked (a running maximum
+// adds 16 maxima, an exchange between two lanes and 64 products to the 131 vector
+// instructions that a block takes).  A row's bits
 // do not depend on the rows beside it, but where their scores pass 2^11.  (BF16:
 // m itself weighs 1.  Any limit would do for bf16's range; 2^60 in place of 2^15 is
 // no faster, 2^8 loses 4 %, and larger weights bring the sums of large values
@@ -1238,7 +1246,8 @@ struct HostPlan {
     int64_t segs, slots, grid;
     int64_t merges;              // workgroups of the merge
 
-    int64_t floats() const { return slots * rows * (kD + 2); }
+    // sums, maxima and weights of the slots, and the plan (16 bytes)
+    int64_t floats() const { return slots ? slots * rows * (kD + 2) + 4 : 0; }
 };
 
 template <typename K>
@@ -1341,8 +1350,10 @@ int launch_chunk(const ChunkSource& src, const ChunkCall& c, void* ws, uint32_t*
     many.cuts = pm.slots > 0;
     few.ws_acc = static_cast<float*>(ws);
     few.ws_ml = few.ws_acc + pf.slots * pf.rows * kD;
+    few.plan = reinterpret_cast<int32_t*>(few.ws_ml + pf.slots * pf.rows * 2);
     many.ws_acc = few.ws_acc + pf.floats();
     many.ws_ml = many.ws_acc + pm.slots * pm.rows * kD;
+    many.plan = reinterpret_cast<int32_t*>(many.ws_ml + pm.slots * pm.rows * 2);
     int rc;
     if (src.format == DQ_Q8_E4M3)
         rc = launch_source<DQ_Q8_E4M3>(few, pf, many, pm, stream);
