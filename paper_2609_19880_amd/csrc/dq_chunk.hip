@@ -93,12 +93,14 @@ struct Few {
     static constexpr bool kFew = true;
     static constexpr int kAtOnce = 256;          // workgroups that the GPU takes at a time: one per CU
     static constexpr int kCost = 16;             // what an item costs besides its blocks, in blocks
+    static constexpr int kMergeRows = 8;         // of a merging workgroup
 };
 struct Many {
     static constexpr int kRows = 128;
     static constexpr bool kFew = false;
     static constexpr int kAtOnce = 768;          // three per CU
     static constexpr int kCost = 8;
+    static constexpr int kMergeRows = 16;
 };
 constexpr int kLeast = 8;                        // blocks of one piece, at least (4: no faster)
 
@@ -1154,12 +1156,12 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_kernel(ChunkArgs a) {
                                   parts, rows, 0, b, h, whole, it.slot);
 }
 
-// The pieces of a segment's rows joined: a workgroup has 16 rows, half a
-// wavefront each at a time, four channels a lane.  Bound by latency (lengths, plan,
-// maxima, sums): 7 us for 16 pieces of 16 rows, 4 us where nothing is cut, and by
-// memory where pieces are many (50 MB of them 14 us).
-constexpr int kMergeRows = 16;
-
+// The pieces of a segment's rows joined: half a wavefront has a row at a time, four
+// channels a lane.  Bound by latency (plan, lengths, maxima, sums) where pieces are
+// few: one row for each half of a workgroup's wavefronts, 5.5 us for 16 pieces (7.2
+// with two rows); by memory where they are many (50 MB of them 14 us), and there
+// fewer workgroups, each of which looks its segment up, take less (48 ragged chunks
+// 473 us with two rows, 486 with one).
 // Over the 32 lanes of half a wavefront; every lane gets the result.
 template <typename Op>
 __device__ __forceinline__ float half_reduce(float v, int lane, Op op) {
@@ -1172,7 +1174,7 @@ __device__ __forceinline__ float half_reduce(float v, int lane, Op op) {
 
 template <typename K>
 __device__ __forceinline__ void merge_rows(const ChunkArgs& a, int id, int lane) {
-    constexpr int R = K::kRows, kParts = R / kMergeRows;
+    constexpr int R = K::kRows, kMergeRows = K::kMergeRows, kParts = R / kMergeRows;
     const Item it = find_item<K, true>(a, id / kParts, lane);
     if (it.tile < 0 || it.chunk == kWhole) return;
     const int b = __builtin_amdgcn_readfirstlane(it.b), h = __builtin_amdgcn_readfirstlane(it.h);
@@ -1275,7 +1277,7 @@ HostPlan host_plan(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t t_ca
     }
     p.slots = cuts ? std::min<int64_t>(4 * K::kAtOnce + 8, p.segs * pieces) : 0;
     p.grid = (std::max(p.segs, p.slots) + 7) / 8 * 8;
-    p.merges = cuts ? std::min<int64_t>(2 * K::kAtOnce, p.segs) * (K::kRows / kMergeRows) : 0;
+    p.merges = cuts ? std::min<int64_t>(2 * K::kAtOnce, p.segs) * (K::kRows / K::kMergeRows) : 0;
     return p;
 }
 
