@@ -731,7 +731,7 @@ __device__ __forceinline__ void join_rows(const ChunkArgs& a, const f32x16 (&o)[
 // and a block's scores.
 //
 // Bound by no single unit: 4 x 8171 queries over themselves (32 heads, int8) run at
-// 915 TFLOP/s, where the matrix units are busy 42 % of the time, other vector
+// 910 to 940 TFLOP/s, where the matrix units are busy 42 % of the time, other vector
 // instructions (131 per wavefront and block, 16 of them exponentials) issue about
 // as long, LDS is active 33 %, and the clock falls to 1.9 GHz.  Left out one at a
 // time, exponentials, the weights' sums, conversions, loads or the second product
@@ -971,7 +971,7 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
 // it for itself; the wavefronts' sums are joined in LDS at the end.  Bound by
 // memory: a block's codes are requested as soon as the registers of the last
 // one's are free, keys while the weights are computed, values while the next
-// scores are.  16 x 8 queries over 32768 e4m3 tokens (32 heads) take 182 us, 5.9
+// scores are.  16 x 8 queries over 32768 e4m3 tokens (32 heads) take 177 us, 6.1
 // TB/s (262 with the codes converted through LDS for all wavefronts).
 //
 // Values of codes: a lane reads whole 16-byte pieces (two channels 16 apart of 8
@@ -1158,7 +1158,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_kernel(ChunkArgs a) {
 
 // The pieces of a segment's rows joined: half a wavefront has a row at a time, four
 // channels a lane.  Bound by latency (plan, lengths, maxima, sums) where pieces are
-// few: one row for each half of a workgroup's wavefronts, 5.5 us for 16 pieces (7.2
+// few: one row for each half of a workgroup's wavefronts, 4.5 us for 16 pieces (7.1
 // with two rows); by memory where they are many (50 MB of them 14 us), and there
 // fewer workgroups, each of which looks its segment up, take less (48 ragged chunks
 // 473 us with two rows, 486 with one).
