@@ -66,19 +66,23 @@ struct ChunkArgs {
     float scale_log2;            // |softmax scale| log2 e
     int negative;                // the softmax scale is
     int cuts;                    // pieces may be cut (0: every segment is one item)
+    int planned;                 // the plan was made by a kernel of its own
+    int groups;                  // of 64 sequences
     uint32_t* status;
     float* ws_acc;               // [slot][rows][128]
     float* ws_ml;                // [slot][2][rows]
-    int32_t* plan;               // the blocks of one piece, for the merge
+    int32_t* plan;               // the blocks of one piece, for the merge; planned: and what
+                                 // find_item reads of 64 sequences at a time
 };
 
 // ------------------------------------------------------------------- shares
 //
 // A segment is a tile of rows of one (sequence, KV head).  Where there are
-// fewer segments than would fill the GPU twice, their tokens are cut into
-// pieces of `chunk` blocks; the pieces of a row are joined by the merge kernel.
-// Lengths are known on the device only, so every workgroup derives the same
-// plan from them.
+// fewer segments than would fill the GPU twice, or some have more blocks than a
+// workgroup's share of all, their tokens are cut into pieces of `chunk` blocks;
+// the pieces of a row are joined by the merge kernel.  Lengths are known on the
+// device only, so every workgroup derives the same plan from them (of more than
+// 64 sequences, or where the GPU is full anyway, a kernel of its own).
 
 struct Seq {
     int T, n, tiles, units;      // tokens, new tokens, row tiles, most blocks that a row tile sees
@@ -148,7 +152,28 @@ __device__ __forceinline__ Seq seq_at(const ChunkArgs& a, int b0, int lane) {
     return b0 + lane < a.B ? seq_of<K>(a, b0 + lane) : Seq{0, 0, 0, 0};
 }
 
-// The blocks of one piece.  All lanes agree.  first: seq_at(a, 0, lane).
+// The blocks of one piece, of `segs` segments that have `total` blocks, the longest
+// `longest`.  All lanes agree.
+template <typename K>
+__device__ __forceinline__ int plan_of(float total, float segs, int longest, int lane) {
+    const bool full = segs >= 2 * K::kAtOnce;
+    if (full || total < 0.75f * segs * (float)longest) {
+        // Many segments: those longer than what each place has to do anyway are cut
+        // (one sequence of 65536 tokens among 63 of 1024: 421 to 77 us).  Few:
+        // unlike lengths leave pieces that are not full: small ones even out the end
+        // (48 ragged chunks 600 us with pieces of what a place has, 616 to 630 with
+        // 1.3 of it, or 1/1.5, 1/2 and 1/4)
+        const int c = max((int)ceilf((full ? total + segs * K::kCost : total) / K::kAtOnce), kLeast);
+        return c >= longest ? kWhole : c;
+    }
+    // lane l tries l + 1 pieces per segment
+    const int c = plan_try(longest, lane);
+    const float cost = plan_cost<K>(segs, longest, c), least = wave_min(cost);
+    const int best = __builtin_amdgcn_readlane(c, __builtin_ctzll(__builtin_amdgcn_ballot_w64(cost == least)));
+    return best >= longest ? kWhole : best;
+}
+
+// The same of all sequences.  first: seq_at(a, 0, lane).
 template <typename K>
 __device__ __forceinline__ int plan_chunk(const ChunkArgs& a, const Seq& first, int lane) {
     // (sums in fp32: the same bits wherever they are taken; a chunk a millionth too
@@ -167,21 +192,7 @@ __device__ __forceinline__ int plan_chunk(const ChunkArgs& a, const Seq& first, 
         segs += wave_sum((float)q.tiles);
         longest = max(longest, wave_max(q.tiles ? q.units : 0));
     }
-    total *= (float)a.H;
-    segs *= (float)a.H;
-    constexpr float kMost = 2 * K::kAtOnce;
-    if (segs >= kMost) return kWhole;
-    if (total < 0.75f * segs * (float)longest) {
-        // unlike lengths leave pieces that are not full: small ones even out the end
-        // (48 ragged chunks 600 us with pieces of what a place has, 616 to 630 with
-        // 1.3 of it, or 1/1.5, 1/2 and 1/4)
-        return max((int)ceilf(total / K::kAtOnce), kLeast);
-    }
-    // lane l tries l + 1 pieces per segment
-    const int c = plan_try(longest, lane);
-    const float cost = plan_cost<K>(segs, longest, c), least = wave_min(cost);
-    const int best = __builtin_amdgcn_readlane(c, __builtin_ctzll(__builtin_amdgcn_ballot_w64(cost == least)));
-    return best >= longest ? kWhole : best;
+    return plan_of<K>(total * (float)a.H, segs * (float)a.H, longest, lane);
 }
 
 __device__ __forceinline__ int pieces(int units, int chunk) { return max(1, (units - 1) / chunk + 1); }
@@ -196,9 +207,9 @@ __device__ __forceinline__ int scan64(int v) {         // inclusive sums over th
     return v;
 }
 
-// Work item `id`, or segment `id` (SEGMENT), with the slot of its (first) piece.
-// Slots go sequence after sequence, KV head after KV head, the last row tiles
-// (which see most) first, their pieces in order.
+// Work item `id`, or cut segment `id` (SEGMENT), with the slot of its (first) piece.
+// Slots are those of cut segments, sequence after sequence, KV head after KV head,
+// the last row tiles (which see most) first, their pieces in order.
 //
 // Workgroups go to the 8 XCDs in turn; what shares keys and values should meet in
 // one L2, and all XCDs should have sequences of every length: each takes its
@@ -209,7 +220,9 @@ __device__ __forceinline__ int scan64(int v) {         // inclusive sums over th
 template <typename K, bool SEGMENT>
 __device__ __forceinline__ Item find_item(const ChunkArgs& a, int id, int lane) {
     Item it{0, 0, -1, 0, kWhole, 0};
-    if (!a.cuts) {
+    if (a.cuts && (SEGMENT || a.planned)) it.chunk = *a.plan;
+    if (SEGMENT && it.chunk == kWhole) return it;    // nothing to merge
+    if (!a.cuts || (a.planned && it.chunk == kWhole)) {
         // every segment whole, as many as full chunks have: no lengths needed to find it
         const uint32_t tiles = K::kFew ? 1u : ((uint32_t)a.n_q * (uint32_t)a.G + K::kRows - 1) / K::kRows;
         const bool heads8 = a.H % 8 == 0;
@@ -229,14 +242,10 @@ __device__ __forceinline__ Item find_item(const ChunkArgs& a, int id, int lane) 
         if (it.tile >= seq_of<K>(a, it.b).tiles) it.tile = -1;
         return it;
     }
-    if constexpr (SEGMENT) {
-        it.chunk = *a.plan;                      // what the kernel before went by
-        if (it.chunk == kWhole) return it;       // nothing to merge
-    }
     const bool by_head = !SEGMENT && a.H % 8 == 0;
     Seq first{0, 0, 0, 0};
     if (a.B > 1 || !(SEGMENT || by_head)) first = seq_at<K>(a, 0, lane);
-    if constexpr (!SEGMENT) {
+    if (!SEGMENT && !a.planned) {
         it.chunk = plan_chunk<K>(a, first, lane);
         if (id == 0 && threadIdx.x == 0) *a.plan = it.chunk;
     }
@@ -246,7 +255,7 @@ __device__ __forceinline__ Item find_item(const ChunkArgs& a, int id, int lane) 
     // pieces of a sequence's segment in a pass
     auto full = [&](int units) { return (int)((uint32_t)units / (uint32_t)it.chunk); };
     auto in_pass = [&](int units, int pass) {
-        if (SEGMENT) return 1;
+        if (SEGMENT) return (int)(units > it.chunk);
         const int n = full(units);
         if (pass == 0) return n;
         const int rest = units - n * it.chunk;
@@ -254,10 +263,13 @@ __device__ __forceinline__ Item find_item(const ChunkArgs& a, int id, int lane) 
     };
     if (!SEGMENT && !by_head) {
         int all = 0;
-        for (int b0 = 0; b0 < a.B; b0 += kWave) {
-            const Seq s = at(b0);
-            all += wave_sum(s.tiles * heads * pieces(s.units, it.chunk));
-        }
+        if (a.planned)
+            all = a.plan[1] * heads;
+        else
+            for (int b0 = 0; b0 < a.B; b0 += kWave) {
+                const Seq s = at(b0);
+                all += wave_sum(s.tiles * heads * pieces(s.units, it.chunk));
+            }
         const int per = (all + 7) / 8;
         if ((id >> 3) >= per) return it;
         x = (id & 7) * per + (id >> 3);
@@ -284,10 +296,32 @@ __device__ __forceinline__ Item find_item(const ChunkArgs& a, int id, int lane) 
             x -= own;
             continue;
         }
-        int before = 0, slots = 0;
-        for (int b0 = 0; b0 < a.B; b0 += kWave) {
+        int before = 0, slots = 0, b0 = 0;
+        if (a.planned) {
+            // the 64 sequences that have the item, from the plan
+            const int32_t* counts = a.plan + 4 + (SEGMENT ? 3 : pass) * a.groups;
+            const int32_t* held_of = a.plan + 4 + 4 * a.groups;
+            bool found = false;
+            for (int g0 = 0; g0 < a.groups && !found; g0 += kWave) {
+                const bool in = g0 + lane < a.groups;
+                const int own = in ? counts[g0 + lane] * heads : 0, held = in ? held_of[g0 + lane] * a.H : 0;
+                const int upto = before + scan64(own), held_upto = slots + scan64(held);
+                const int last = __builtin_amdgcn_readlane(upto, 63);
+                found = x < last;
+                const int l = found ? __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > x)) : 63;
+                before = found ? __builtin_amdgcn_readlane(upto - own, l) : last;
+                slots = __builtin_amdgcn_readlane(found ? held_upto - held : held_upto, l);
+                b0 = (g0 + l) * kWave;
+            }
+            if (!found) {
+                x -= before;
+                continue;
+            }
+        }
+        for (; b0 < a.B; b0 += kWave) {
             const Seq s = at(b0);
-            const int own = s.tiles * heads * in_pass(s.units, pass), held = s.tiles * a.H * pieces(s.units, it.chunk);
+            const int own = s.tiles * heads * in_pass(s.units, pass), n = pieces(s.units, it.chunk);
+            const int held = n > 1 ? s.tiles * a.H * n : 0;
             const int upto = before + scan64(own);
             const int last = __builtin_amdgcn_readlane(upto, 63);
             const int held_upto = slots + scan64(held);
@@ -1239,17 +1273,84 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs few, ChunkAr
         merge_rows<Many>(many, (int)blockIdx.x - few_groups, lane);
 }
 
+// The plan of many sequences: the blocks of one piece, and for each 64 sequences
+// their items of each pass, cut segments and slots (of one KV head).
+constexpr int kPlanWaves = 16;
+
+template <typename K>
+__device__ __forceinline__ void plan_all(const ChunkArgs& a, int wave, int lane, float (&sums)[2][kPlanWaves],
+                                         int (&most)[kPlanWaves], int (&items)[kPlanWaves]) {
+    float total = 0, segs = 0;
+    int longest = 0;
+    for (int g = wave; g < a.groups; g += kPlanWaves) {
+        const Seq s = seq_at<K>(a, g * kWave, lane);
+        total += wave_sum((float)s.tiles * (float)s.units);
+        segs += wave_sum((float)s.tiles);
+        longest = max(longest, wave_max(s.tiles ? s.units : 0));
+    }
+    if (lane == 0) {
+        sums[0][wave] = total;
+        sums[1][wave] = segs;
+        most[wave] = longest;
+    }
+    __syncthreads();
+    total = segs = 0;
+    for (int w = 0; w < kPlanWaves; ++w) {
+        total += sums[0][w];
+        segs += sums[1][w];
+        longest = max(longest, most[w]);
+    }
+    const int chunk = plan_of<K>(total * (float)a.H, segs * (float)a.H, longest, lane);
+    int all = 0;
+    if (chunk != kWhole) {
+        for (int g = wave; g < a.groups; g += kPlanWaves) {
+            const Seq s = seq_at<K>(a, g * kWave, lane);
+            const int n = pieces(s.units, chunk), full = s.units / chunk, rest = s.units - full * chunk;
+            const int long_end = rest > chunk / 2, short_end = !long_end && (rest > 0 || full == 0);
+            const int first = wave_sum(s.tiles * full), second = wave_sum(s.tiles * long_end);
+            const int third = wave_sum(s.tiles * short_end), cut = wave_sum(n > 1 ? s.tiles : 0);
+            const int slots = wave_sum(n > 1 ? s.tiles * n : 0);
+            if (lane == 0) {
+                int32_t* t = a.plan + 4 + g;
+                t[0] = first;
+                t[a.groups] = second;
+                t[2 * a.groups] = third;
+                t[3 * a.groups] = cut;
+                t[4 * a.groups] = slots;
+            }
+            all += first + second + third;
+        }
+    }
+    if (lane == 0) items[wave] = all;
+    __syncthreads();
+    if (wave == 0 && lane == 0) {
+        all = 0;
+        for (int w = 0; w < kPlanWaves; ++w) all += items[w];
+        a.plan[0] = chunk;
+        a.plan[1] = all;
+    }
+}
+
+__global__ __launch_bounds__(kPlanWaves * kWave) void chunk_plan_kernel(ChunkArgs few, ChunkArgs many) {
+    __shared__ float sums[2][kPlanWaves];
+    __shared__ int most[kPlanWaves], items[kPlanWaves];
+    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    if (blockIdx.x == 0 && few.planned) plan_all<Few>(few, wave, lane, sums, most, items);
+    if (blockIdx.x == 1 && many.planned) plan_all<Many>(many, wave, lane, sums, most, items);
+}
+
 // ------------------------------------------------------------------- host
 
 // A kernel's part of the work, as far as the host knows it.
 struct HostPlan {
-    bool runs;
+    bool runs, planned;
     int rows;                    // per tile
     int64_t segs, slots, grid;
     int64_t merges;              // workgroups of the merge
+    int64_t plan;                // numbers of the plan
 
-    // sums, maxima and weights of the slots, and the plan (16 bytes)
-    int64_t floats() const { return slots ? slots * rows * (kD + 2) + 4 : 0; }
+    // sums, maxima and weights of the slots, and the plan
+    int64_t floats() const { return slots ? slots * rows * (kD + 2) + plan : 0; }
 };
 
 template <typename K>
@@ -1261,12 +1362,10 @@ HostPlan host_plan(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t t_ca
     p.rows = K::kRows;
     p.segs = (int64_t)B * Hkv * (K::kFew ? 1 : (rows + p.rows - 1) / p.rows);
     const int64_t pieces = std::max<int64_t>(1, ((int64_t)t_cap / kBlk + kLeast) / kLeast);
-    // A plan that cuts has fewer segments than would fill the GPU twice and, all
-    // in all, fewer than twice as many items.  Segments are as many as are counted
-    // here where all chunks are full.
-    // Every workgroup reads all lengths then: not of more than 128 sequences,
-    // which fill the GPU by themselves.
-    bool cuts = p.runs && pieces > 1 && B <= 128 && (lens || p.segs < 2 * K::kAtOnce);
+    // Where one sequence's segments take every place nothing is longer than a
+    // place's share; else what fills the GPU twice may still have a longest one.
+    const int64_t own = p.segs / B;
+    bool cuts = p.runs && pieces > 1 && (lens || p.segs < 2 * K::kAtOnce || own < K::kAtOnce);
     if (cuts && units > 0) {
         // every segment has these blocks, so the plan is known here: none is cut
         // where no plan costs less, and nothing is merged
@@ -1275,9 +1374,16 @@ HostPlan host_plan(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t t_ca
         for (int n = 1; n < kWave; ++n) better |= plan_cost<K>((float)p.segs, units, plan_try(units, n)) < least;
         cuts = better;
     }
-    p.slots = cuts ? std::min<int64_t>(4 * K::kAtOnce + 8, p.segs * pieces) : 0;
-    p.grid = (std::max(p.segs, p.slots) + 7) / 8 * 8;
-    p.merges = cuts ? std::min<int64_t>(2 * K::kAtOnce, p.segs) * (K::kRows / K::kMergeRows) : 0;
+    // Pieces are of a place's share, or of like segments twice as many as places:
+    // there are as many cut segments as places at most, of twice as many pieces, and
+    // a last piece of every segment beside the whole ones.
+    p.planned = cuts && (B > kWave || (!lens && p.segs >= 2 * K::kAtOnce));
+    p.plan = 4 + (5 * (((int64_t)B + kWave - 1) / kWave) + 3) / 4 * 4;
+    p.slots = cuts ? std::min<int64_t>(2 * K::kAtOnce + 8, p.segs * pieces) : 0;
+    const int64_t items = cuts ? std::min<int64_t>(std::max<int64_t>(p.segs, K::kAtOnce) + K::kAtOnce + 8, p.segs * pieces)
+                               : p.segs;
+    p.grid = (items + 7) / 8 * 8;
+    p.merges = cuts ? std::min<int64_t>(K::kAtOnce + 8, p.segs) * (K::kRows / K::kMergeRows) : 0;
     return p;
 }
 
@@ -1337,6 +1443,7 @@ int launch_chunk(const ChunkSource& src, const ChunkCall& c, void* ws, uint32_t*
     a.G = c.Hq / c.Hkv;
     a.n_q = c.n_q;
     a.t_cap = c.t_cap;
+    a.groups = (c.B + kWave - 1) / kWave;
     a.causal = c.causal;
     a.window = c.window;
     a.sinks = c.sinks;
@@ -1350,12 +1457,18 @@ int launch_chunk(const ChunkSource& src, const ChunkCall& c, void* ws, uint32_t*
     ChunkArgs few = a, many = a;
     few.cuts = pf.slots > 0;
     many.cuts = pm.slots > 0;
+    few.planned = pf.planned;
+    many.planned = pm.planned;
     few.ws_acc = static_cast<float*>(ws);
     few.ws_ml = few.ws_acc + pf.slots * pf.rows * kD;
     few.plan = reinterpret_cast<int32_t*>(few.ws_ml + pf.slots * pf.rows * 2);
     many.ws_acc = few.ws_acc + pf.floats();
     many.ws_ml = many.ws_acc + pm.slots * pm.rows * kD;
     many.plan = reinterpret_cast<int32_t*>(many.ws_ml + pm.slots * pm.rows * 2);
+    if (pf.planned || pm.planned) {
+        chunk_plan_kernel<<<2, kPlanWaves * kWave, 0, stream>>>(few, many);
+        if (int rc = hip_check("chunk_plan launch", hipGetLastError())) return rc;
+    }
     int rc;
     if (src.format == DQ_Q8_E4M3)
         rc = launch_source<DQ_Q8_E4M3>(few, pf, many, pm, stream);

@@ -514,6 +514,27 @@ def test_cross_pieces(dq, B, T, n, H, G):
         _check_cross(_cross(dq, q, k, v, None, m), q, k, v, [T] * B, [n] * B, m)
 
 
+@pytest.mark.parametrize("B,H,n,new", [(300, 2, 1, False), (90, 8, 2, False), (40, 3, 130, False), (140, 8, 70, True),
+                                       (200, 1, 200, True), (520, 1, 3, True)])
+def test_cross_one_long_sequence(dq, B, H, n, new):
+    """Many short sequences and a few long ones, which are cut."""
+    T = 9000
+    k, v = _kv(B, 1, T, H)
+    q = _q(n, B, n, H)
+    r = np.random.default_rng(B)
+    lens = r.integers(0, 120, B)
+    lens[[3, B // 2, B - 1]] = [T, 5000, 4000]
+    news = r.integers(0, n + 1, B) if new else np.full(B, n)
+    news[[3, B - 1]] = n
+    kd, vd = (x.to(DEV).expand(B, -1, -1, -1) for x in (k, v))
+    out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device=DEV)
+    dq.dq_cross_attention(q.to(DEV), kd, vd, kv_lens=_i32(lens.tolist()), q_lens=_i32(news.tolist()) if new else None,
+                          out=out)
+    _check_cross(out, q, k.expand(B, -1, -1, -1), v.expand(B, -1, -1, -1), lens, news)
+    for b in range(B):
+        assert bool((out[b, int(news[b]):] == 7.0).all())
+
+
 @pytest.mark.parametrize("n", [2, 90])
 def test_cross_strides(dq, n):
     B, T, H, G = 2, 300, 2, 2
