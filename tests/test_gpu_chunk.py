@@ -640,6 +640,38 @@ def test_cross_graph(dq):
         assert torch.equal(out, want)
 
 
+def test_cross_many_sequences_graph(dq):
+    """20000 sequences that share states, captured: other lengths at every replay,
+    and a workspace that holds NaN."""
+    B, T = 20000, 2100
+    k, v = _kv(2, 1, T, 1)
+    q = _q(2, B, 1, 1)
+    kd, vd, qd = k.to(DEV).expand(B, -1, -1, -1), v.to(DEV).expand(B, -1, -1, -1), q.to(DEV)
+    kk, vv = (x[0].double().to(DEV).permute(1, 0, 2) for x in (k, v))
+    lens = torch.zeros(B, dtype=torch.int32, device=DEV)
+    out = torch.zeros(q.shape, dtype=torch.bfloat16, device=DEV)
+    ws = torch.empty(dq.dq_chunk_workspace_bytes(B, 1, 1, 1, T), dtype=torch.uint8, device=DEV)
+    call = lambda: dq.dq_cross_attention(qd, kd, vd, kv_lens=lens, out=out, workspace=ws)  # noqa: E731
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    r = np.random.default_rng(1)
+    for longest, most in ((T, 1), (T, T), (T, 40), (3, 3)):
+        now = r.integers(0, most + 1, B)
+        now[[0, 63, 64, 9000, B - 1]] = longest
+        lens.copy_(_i32(now.tolist()))
+        ws.fill_(255)
+        out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        see = torch.arange(T, device=DEV)[None] < lens[:, None]
+        _check(out[:, 0], q[:, 0], kk, vv, see, 128 ** -0.5, 8)
+
+
 # ------------------------------------------------------------- together
 
 @pytest.mark.parametrize("fmt", FMTS)
