@@ -1096,15 +1096,22 @@ def _like(x, stream):
 
 
 def _rope_rows(x, out, name, dev, stream):
-    """Rows [B, T, H, d] bf16 and where they go (a new tensor unless given)."""
-    _need(x.dtype is torch.bfloat16 and x.dim() == 4 and x.stride(3) == 1 and x.device == dev,
-          name + " must be bf16 [B, T, H, d], channels contiguous, on the frequencies' GPU")
+    """Rows [B, T, H, d] bf16 and where they go (a new tensor unless given).
+    (A call for one token is as long as this: few of torch's attributes, each once.)"""
+    sb, st, sh, sd = x.stride() if x.dim() == 4 else _NO_ROWS
+    if x.dtype is not torch.bfloat16 or sd != 1 or x.device != dev:
+        raise ValueError(name + " must be bf16 [B, T, H, d], channels contiguous, on the frequencies' GPU")
+    at = x.data_ptr()
     if out is None:
+        if stream is None and x.is_contiguous():
+            out = torch.empty_like(x)
+            return out, (at, sb, st, sh), (out.data_ptr(), sb, st, sh)
         out = _like(x, stream)
-    else:
-        _need(out.dtype is torch.bfloat16 and out.shape == x.shape and out.stride(3) == 1 and out.device == dev,
-              name + "_out must be bf16 of " + name + "'s shape on the same GPU")
-    return out, (x.data_ptr(), *x.stride()[:3]), (out.data_ptr(), *out.stride()[:3])
+    elif out is x:
+        return out, (at, sb, st, sh), (at, sb, st, sh)
+    elif out.dtype is not torch.bfloat16 or out.shape != x.shape or out.stride(3) != 1 or out.device != dev:
+        raise ValueError(name + "_out must be bf16 of " + name + "'s shape on the same GPU")
+    return out, (at, sb, st, sh), (out.data_ptr(), *out.stride()[:3])
 
 
 _NO_ROWS = (0, 0, 0, 0)
@@ -1117,24 +1124,27 @@ def dq_rope(freq, q=None, k=None, positions=None, starts=None, t0: int = 0, layo
     freq: fp64 [rotary_dim / 2] on the GPU.  Returns (q_out, k_out), new tensors
     unless given (the inputs themselves rotate in place)."""
     lay = ROPE_LAYOUTS.get(layout, layout)
-    _need(lay in (DQ_ROPE_HALF, DQ_ROPE_INTERLEAVED), "layout must be 'half' or 'interleaved'")
+    if lay not in (DQ_ROPE_HALF, DQ_ROPE_INTERLEAVED):
+        raise ValueError("layout must be 'half' or 'interleaved'")
     dev = freq.device
-    _need(freq.dtype is torch.float64 and freq.dim() == 1 and freq.is_contiguous() and dev.type == "cuda",
-          "freq must be fp64 [rotary_dim / 2] on a GPU")
+    if freq.dtype is not torch.float64 or freq.dim() != 1 or not freq.is_contiguous() or dev.type != "cuda":
+        raise ValueError("freq must be fp64 [rotary_dim / 2] on a GPU")
     x = k if q is None else q
     _need(x is not None, "q or k")
-    _need(x.dim() == 4, "q and k must be bf16 [B, T, H, d]")
-    B, T, _, d = x.shape
+    if x.dim() != 4:
+        raise ValueError("q and k must be bf16 [B, T, H, d]")
+    B, T, Hq, d = x.shape
     qr = qo = kr = ko = _NO_ROWS
-    Hq = Hkv = 0
+    Hkv = 0
     if q is not None:
         q_out, qr, qo = _rope_rows(q, q_out, "q", dev, stream)
-        Hq = q.shape[2]
+    else:
+        Hq = 0
     if k is not None:
-        _need(k.dim() == 4 and k.shape[0] == B and k.shape[1] == T and k.shape[3] == d,
-              "q and k must have the same sequences, tokens and channels")
+        kB, kT, Hkv, kd = k.shape if k.dim() == 4 else _NO_ROWS
+        if kB != B or kT != T or kd != d:
+            raise ValueError("q and k must have the same sequences, tokens and channels")
         k_out, kr, ko = _rope_rows(k, k_out, "k", dev, stream)
-        Hkv = k.shape[2]
     at = psb = pst = start = 0
     if positions is not None:
         _need(positions.dtype is torch.int32 and positions.shape == (B, T) and positions.device == dev,
@@ -1143,7 +1153,8 @@ def dq_rope(freq, q=None, k=None, positions=None, starts=None, t0: int = 0, layo
         _need(starts is None and t0 == 0, "positions, or starts and t0")
     elif starts is not None:
         start = _q8_lens(starts, B, dev, "starts")
-    _need(-_INT_MAX <= t0 <= _INT_MAX, "t0")
+    if t0:
+        _need(-_INT_MAX <= t0 <= _INT_MAX, "t0")
     rc = _lib.dq_rope(lay, int(bool(transposed)), freq.data_ptr(), magnitude, 2 * freq.shape[0], d, B, T, *qr, Hq, *qo,
                       *kr, Hkv, *ko, at, psb, pst, start, t0, _q8_stream(dev.index, stream))
     if rc:
