@@ -690,6 +690,8 @@ int dq_rope(int32_t layout, int32_t transposed, const double* freq, float magnit
  * A query that sees no token gives zeros; one with an infinity or NaN that sees
  * some gives NaN.  Scores and sums are held in fp32; the weights are rounded to
  * fp16 for the product with the values, which are exact, and the output to bf16.
+ * The same call gives the same bits again; where long sequences are cut follows
+ * from all lengths of the batch, so a sequence's last bits may go by the others.
  * Through a block table the call is the same; an entry outside the pool sets
  * DQ_STATUS_PAGE and page 0 is read in its place.
  * batch and kv_heads at most 65535, n_q q_heads at most 2^26, batch kv_heads
