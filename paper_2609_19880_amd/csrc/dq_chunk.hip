@@ -14,8 +14,9 @@
 // the weights are the second product's operand where they lie.
 //
 // 8-bit codes are exact in fp16.  A key block's scale multiplies the scores; a
-// value block's scale goes into the exponent of the weights, relative to the
-// largest scale so far.  Queries are brought to a largest magnitude of 2^13 by
+// value block's scale goes into the exponent of the weights, as far as a quarter
+// below the power of 2 that the sums are relative to: it follows the blocks.
+// Queries are brought to a largest magnitude of 2^13 by
 // a power of 2 of each row, exactly but for values 2^-37 of the largest.
 #include <math.h>
 
@@ -453,7 +454,7 @@ struct Rows {
 
     u32x4 q[8];
     f32x16 o[4];
-    float m, l, vref, qc;        // vref: log2 of the scale that the values are relative to
+    float m, l, vref, qc;        // vref: log2 of the scale that the sums are relative to, an integer
     int end;                     // the row sees t < end, of those t < sinks or t >= end - window
     int T, window, sinks;
     int lim_lo, lim_hi, start_hi;
@@ -560,12 +561,17 @@ struct Rows {
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[e] = (vis >> (8 * (e >> 2) + (e & 3))) & 1 ? s[e] : -INFINITY;
         }
+        // Of the scale the weights hold 2^-2 to 2^0: less would cost them bits of fp16,
+        // however much the block weighs.
         float d = 0.f;
-        if constexpr (q8) d = vl <= kNoScale ? 0.f : fmaxf(vl - vref, -60.f);
-        float sum = weigh(s, c, kUp + d - mu(), p);
         bool again = careful;
-        // (weights that fp16 would lose need their sum in fp32)
-        if constexpr (q8) again = again || !(d >= -2.f && d <= 0.f);
+        if constexpr (q8) {
+            const float rel = vl <= kNoScale ? 0.f : vl - vref;
+            const bool holds = rel >= -2.f && rel <= 0.f;
+            d = holds ? rel : 0.f;               // (if not, at least what it will be)
+            again = again || !holds;
+        }
+        float sum = weigh(s, c, kUp + d - mu(), p);
         if (again || __builtin_amdgcn_ballot_w64(sum > kMost) != 0) sum = anew(s, c, sum, vl, d, lane, p);
         l += q8 ? sum * __builtin_amdgcn_exp2f(-d) : sum;
     }
@@ -573,6 +579,15 @@ struct Rows {
     // The same with a new maximum or a new scale; d becomes the block's.  sum: of
     // the weights without them.  (Selections rather than branches, and one place
     // that scales the sums: with branches the compiler keeps both results.)
+    //
+    // The scale that the sums are relative to becomes the block's, rounded up to a
+    // power of 2 or twice that, where the weights do not hold it: rows to which a
+    // larger block is nothing, or that do not see it, must not lose the smaller ones.
+    // The sums are scaled by a power of 2, exactly: down by up to 2^99 without a loss
+    // (a weight of 2^-25, a code of 1), up as far as they stay below 2^124 (sums of
+    // usual weights, 2^2 or less, by over 2^100).  Where that is not enough the
+    // block's values are nothing beside the sums of some row of the wavefront, and
+    // are left out.
     __device__ __forceinline__ float anew(f32x16& s, float c, float sum, float vl, float& d, int lane, u32x4 (&p)[2]) {
         float top = s[0];                        // (NaN where every score is)
 #pragma unroll
@@ -589,17 +604,22 @@ struct Rows {
         top = fmaxf(top, xor_lane<32>(top, lane));
         sum = fmaxf(sum, xor_lane<32>(sum, lane));
         const bool higher = (m == -INFINITY || (exact ? top > m + 4.f : sum > kMost)) && top > m;
-        float f = higher ? __builtin_amdgcn_exp2f(m - top) : 1.f;
+        float by = higher ? m - top : 0.f;
+        l *= __builtin_amdgcn_exp2f(by);
         m = higher ? top : m;
-        l *= f;
+        bool lost = false;
         if constexpr (q8) {
-            if (d > 0.f) {
-                // room for scales of twice the size
-                f *= __builtin_amdgcn_exp2f(vref - (vl + 1.f));
-                vref = vl + 1.f;
-                d = -1.f;
+            const float rel = vl - vref;
+            if (vl > kNoScale && !(rel >= -2.f && rel <= 0.f)) {
+                float to = floorf(vl) + 1.f;     // (room for scales of up to twice the size)
+                if (vref - to > 64.f) to = fmaxf(to, vref - most_up());
+                by += vref - to;
+                vref = to;
+                lost = vl - to < -2.f;
+                d = lost ? 0.f : vl - to;
             }
         }
+        const float f = __builtin_amdgcn_exp2f(by);
         // (whole vectors: element by element the compiler holds the sums twice)
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] *= f;
@@ -610,11 +630,18 @@ struct Rows {
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[e] -= less;
         const float rounded = weigh(s, c, e0, p);
-        if (!q8 || d >= -2.f) return rounded;
-        float all = 0.f;
+        if (lost) p[0] = p[1] = u32x4{0u, 0u, 0u, 0u};
+        return rounded;
+    }
+
+    // By how many powers of 2 the wavefront's sums may grow.
+    __device__ __forceinline__ float most_up() const {
+        float top = 0.f;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) all += __builtin_amdgcn_exp2f(fmaf(s[e], c, e0));
-        return all;
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(o[i][e]));
+        return 124.f - ceilf(__builtin_amdgcn_logf(fmaxf(wave_max(top), 0x1p-126f)));
     }
 
     // The values of half of a block's tokens.
