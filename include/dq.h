@@ -693,7 +693,7 @@ int dq_rope(int32_t layout, int32_t transposed, const double* freq, float magnit
  * output to bf16.  (Weights below 2^-14 of a query's largest are rounded to fewer
  * bits than fp16's 11, below 2^-25 to nothing.)  Value blocks may be of any sizes:
  * one counts fully beside others of up to 2^80 times its scale, whatever their
- * weights.
+ * weights, and values up to bf16's largest give no infinity.
  * The same call gives the same bits again; where long sequences are cut follows
  * from all lengths of the batch, so a sequence's last bits may go by the others.
  * Through a block table the call is the same; an entry outside the pool sets

@@ -70,8 +70,8 @@ struct ChunkArgs {
     int planned;                 // the plan was made by a kernel of its own
     int groups;                  // of 64 sequences
     uint32_t* status;
-    float* ws_acc;               // [slot][rows][128]
-    float* ws_ml;                // [slot][2][rows]
+    float* ws_acc;               // [slot][rows][128]: outputs of pieces
+    float* ws_ml;                // [slot][2][rows]: their maxima and sums of weights
     int32_t* plan;               // the blocks of one piece, for the merge; planned: and what
                                  // find_item reads of 64 sequences at a time
 };
@@ -729,16 +729,24 @@ __device__ __forceinline__ void store_row(const ChunkArgs& a, int b, int token, 
 
 constexpr int kThreads = 4 * kWave;
 
-// The sums of a workgroup's wavefronts joined in LDS and written: wavefront w has
-// rows 32 (w % parts) .. of the tokens that it has seen.  PAIRED: operand 2 m + e
+// A part's share in a row whose largest maximum is `top`, before division by the
+// sum of all shares.  (Parts are joined as outputs, the sums divided by their
+// weights: as sums the largest values, times weights of up to 2^15, would not fit.)
+__device__ __forceinline__ float share(float m, float l, float top) {
+    return l * (m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top));
+}
+__device__ __forceinline__ float inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }   // rows that see nothing: zeros
+
+// The outputs of a workgroup's wavefronts, o f up, joined in LDS and written: wavefront
+// w has rows 32 (w % parts) .. of the tokens that it has seen.  PAIRED: operand 2 m + e
 // has channels 64 m + 32 (row / 16) + 16 e + row % 16, else 32 (2 m + e) + row.
 constexpr int kJoinRow = 68;                     // floats: 64 channels, and 4 to keep rows in different banks
 
 template <typename K, int WAVES, bool PAIRED>
-__device__ __forceinline__ void join_rows(const ChunkArgs& a, const f32x16 (&o)[4], float m, float l, float up,
-                                          float* join, float (&wm)[WAVES][kRowsOf], float (&wl)[WAVES][kRowsOf],
+__device__ __forceinline__ void join_rows(const ChunkArgs& a, const f32x16 (&o)[4], float m, float l, float up, float* join, float (&wm)[WAVES][kRowsOf], float (&wl)[WAVES][kRowsOf],
                                           int parts, int rows, int r0, int b, int h, bool whole, int64_t slot) {
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, half = lane >> 5, col = lane & 31;
+    const float f = inverse(l);
     if (half == 0) {
         wm[wave][col] = m;
         wl[wave][col] = l;
@@ -753,7 +761,7 @@ __device__ __forceinline__ void join_rows(const ChunkArgs& a, const f32x16 (&o)[
                 const int ch = PAIRED ? 32 * (i >> 1) + 16 * e + 8 * (i & 1) + 4 * half : 32 * e + 8 * i + 4 * half;
                 const f32x16& x = o[2 * m2 + e];
                 *reinterpret_cast<f32x4*>(join + (wave * kRowsOf + col) * kJoinRow + ch) =
-                    f32x4{x[4 * i] * up, x[4 * i + 1] * up, x[4 * i + 2] * up, x[4 * i + 3] * up};
+                    f32x4{x[4 * i] * f * up, x[4 * i + 1] * f * up, x[4 * i + 2] * f * up, x[4 * i + 3] * f * up};
             }
         __syncthreads();
         for (int i = tid; i < parts * kRowsOf * 16; i += WAVES * kWave) {
@@ -762,17 +770,15 @@ __device__ __forceinline__ void join_rows(const ChunkArgs& a, const f32x16 (&o)[
             float top = -INFINITY;
             for (int w = in >> 5; w < WAVES; w += parts) top = fmaxf(top, wm[w][in & 31]);
             float sum = 0.f;
+            for (int w = in >> 5; w < WAVES; w += parts) sum += share(wm[w][in & 31], wl[w][in & 31], top);
+            const float each = inverse(sum);
             f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-            for (int w = in >> 5; w < WAVES; w += parts) {
-                const float mw = wm[w][in & 31], f = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - top);
-                sum = fmaf(wl[w][in & 31], f, sum);
-                acc += *reinterpret_cast<const f32x4*>(join + (w * kRowsOf + (in & 31)) * kJoinRow + ch) * f;
-            }
+            for (int w = in >> 5; w < WAVES; w += parts)
+                acc += *reinterpret_cast<const f32x4*>(join + (w * kRowsOf + (in & 31)) * kJoinRow + ch) *
+                       (share(wm[w][in & 31], wl[w][in & 31], top) * each);
             if (whole) {
-                const float f = sum == 0.f ? 0.f : 1.f / sum;    // rows that see nothing: zeros
                 const int token = r / a.G, head = h * a.G + r - token * a.G;
-                store_row(a, b, token, head, 64 * m2 + ch, bf16_two(acc[0] * f, acc[1] * f),
-                          bf16_two(acc[2] * f, acc[3] * f));
+                store_row(a, b, token, head, 64 * m2 + ch, bf16_two(acc[0], acc[1]), bf16_two(acc[2], acc[3]));
             } else {
                 *reinterpret_cast<f32x4*>(a.ws_acc + (slot * K::kRows + in) * kD + 64 * m2 + ch) = acc;
                 if (m2 == 0 && ch == 0) {
@@ -994,20 +1000,19 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
 
     // ------------------------------------------------ results
     const float l = me.l + xor_lane<32>(me.l, lane);
-    const float up = q8 ? __builtin_amdgcn_exp2f(me.vref) : 1.f;
+    const float up = q8 ? __builtin_amdgcn_exp2f(me.vref) : 1.f, f = inverse(l);
     const int half = lane >> 5;
     const int64_t slot = it.slot;
     if (whole) {
         const int r = r0 + wave * kRowsOf + (lane & 31), token = r / a.G, head = h * a.G + r - token * a.G;
         if (r >= rows) return;
-        const float f = l == 0.f ? 0.f : up / l; // rows that see nothing: zeros
 #pragma unroll
         for (int np = 0; np < 4; ++np)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 store_row(a, b, token, head, 32 * np + 8 * i + 4 * half,
-                          bf16_two(me.o[np][4 * i] * f, me.o[np][4 * i + 1] * f),
-                          bf16_two(me.o[np][4 * i + 2] * f, me.o[np][4 * i + 3] * f));
+                          bf16_two(me.o[np][4 * i] * f * up, me.o[np][4 * i + 1] * f * up),
+                          bf16_two(me.o[np][4 * i + 2] * f * up, me.o[np][4 * i + 3] * f * up));
         return;
     }
     float* acc = a.ws_acc + (slot * Many::kRows + wave * kRowsOf + (lane & 31)) * kD + 4 * half;
@@ -1016,8 +1021,8 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             *reinterpret_cast<f32x4*>(acc + 32 * np + 8 * i) =
-                f32x4{me.o[np][4 * i] * up, me.o[np][4 * i + 1] * up, me.o[np][4 * i + 2] * up,
-                      me.o[np][4 * i + 3] * up};
+                f32x4{me.o[np][4 * i] * f * up, me.o[np][4 * i + 1] * f * up, me.o[np][4 * i + 2] * f * up,
+                      me.o[np][4 * i + 3] * f * up};
     if (half == 0) {
         float* ml = a.ws_ml + slot * 2 * Many::kRows + wave * kRowsOf + (lane & 31);
         ml[0] = me.m;
@@ -1252,31 +1257,32 @@ __device__ __forceinline__ void merge_rows(const ChunkArgs& a, int id, int lane)
         if (r >= rows) break;
         const float* ml = a.ws_ml + slot * 2 * R + in;
         const float* acc = a.ws_acc + (slot * R + in) * kD + ch;
-        // 32 pieces at a time: lane c % 32 has piece c's maximum and sum; sums come
+        // 32 pieces at a time: lane c % 32 has piece c's maximum and sum; outputs come
         // eight loads at a time, the first ones on their way beside those
         const int mine = lane & 31;
+        auto max_of = [&](int c) { return ml[(int64_t)c * 2 * R]; };
+        auto sum_of = [&](int c) { return ml[(int64_t)c * 2 * R + R]; };
         f32x4 v[8];
-        auto sums = [&](int c0) {
+        auto outputs = [&](int c0) {
 #pragma unroll
             for (int c = 0; c < 8; ++c)
                 v[c] = *reinterpret_cast<const f32x4*>(acc + (int64_t)min(c0 + c, nc - 1) * R * kD);
         };
-        sums(0);
-        float top = -INFINITY;
-        for (int c = mine; c < nc; c += 32) top = fmaxf(top, ml[(int64_t)c * 2 * R]);
+        outputs(0);
+        const float m0 = mine < nc ? max_of(mine) : -INFINITY, l0 = mine < nc ? sum_of(mine) : 0.f;
+        float top = m0;
+        for (int c = mine + 32; c < nc; c += 32) top = fmaxf(top, max_of(c));
         top = half_reduce(top, lane, [](float p, float q) { return fmaxf(p, q); });
-        float l = 0.f;
+        float l = share(m0, l0, top);
+        for (int c = mine + 32; c < nc; c += 32) l += share(max_of(c), sum_of(c), top);
+        const float each = inverse(half_reduce(l, lane, [](float p, float q) { return p + q; }));
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
         for (int c0 = 0; c0 < nc; c0 += 32) {
-            float w = 0.f;
-            if (c0 + mine < nc) {
-                const float mc = ml[(int64_t)(c0 + mine) * 2 * R];
-                w = mc == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - top);
-                l = fmaf(ml[(int64_t)(c0 + mine) * 2 * R + R], w, l);
-            }
+            float w = share(m0, l0, top) * each;
+            if (c0 > 0) w = c0 + mine < nc ? share(max_of(c0 + mine), sum_of(c0 + mine), top) * each : 0.f;
             const int n = min(32, nc - c0);
             for (int c1 = 0; c1 < n; c1 += 8) {
-                if (c0 + c1 > 0) sums(c0 + c1);
+                if (c0 + c1 > 0) outputs(c0 + c1);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int c = 0; c < 8; ++c) {
@@ -1285,10 +1291,8 @@ __device__ __forceinline__ void merge_rows(const ChunkArgs& a, int id, int lane)
                 }
             }
         }
-        l = half_reduce(l, lane, [](float p, float q) { return p + q; });
-        const float f = l == 0.f ? 0.f : 1.f / l;
         const int token = r / a.G, head = h * a.G + r - token * a.G;
-        store_row(a, b, token, head, ch, bf16_two(x[0] * f, x[1] * f), bf16_two(x[2] * f, x[3] * f));
+        store_row(a, b, token, head, ch, bf16_two(x[0], x[1]), bf16_two(x[2], x[3]));
     }
 }
 

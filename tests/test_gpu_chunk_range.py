@@ -98,3 +98,19 @@ def test_a_large_block_between_even_ones(dq, fmt, n):
         cache = _filled(dq, fmt, kk, x, H * G)
         out = cache.attend_chunk(qq.to(DEV), _i32([T]))
         _check_all(out, qq, _held(kk, fmt), _held(x, fmt), [T], [n])
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("n", [4, 40, 150])
+@pytest.mark.parametrize("to", [2.0 ** -88, 2.0 ** -60, 2.0 ** 50, 2.0 ** 90, 2.0 ** 124])
+def test_all_values_small_or_large(dq, fmt, n, to):
+    """All of a cache's values near the ends of the range, whole and cut."""
+    H, G = 1, 2
+    for T in (300, 4100):
+        k, v = _kv(T + n, 1, T, H)
+        q = _q(n, 1, n, H * G)
+        x = (v.float() * to).to(torch.bfloat16)
+        assert bool(torch.isfinite(x.float()).all())
+        cache = _filled(dq, fmt, k, x, H * G)
+        out = cache.attend_chunk(q.to(DEV), _i32([T]))
+        _check_all(out, q, _held(k, fmt), _held(x, fmt), [T], [n])
