@@ -34,12 +34,14 @@ struct RopeArgs {
     int64_t psb, pst;
     const int32_t* starts;
     int T, t0, rotary, d;
+    uint32_t tokens;             // of all sequences
     int split;                   // workgroups that share a token's heads
     int copies[2];               // the channels behind the rotated ones are copied
     float magnitude, sign;
 };
 
 constexpr int kMostPairs = 512;
+constexpr uint32_t kAlongX = 1u << 23;           // tokens along x: a grid has under 2^32 work-items there
 
 __device__ __forceinline__ float lo16(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi16(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
@@ -59,7 +61,9 @@ template <bool HALF, bool WIDE>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
     __shared__ float2 turn[kMostPairs];
     const int tid = threadIdx.x, pairs = a.rotary / 2;
-    const int b = (int)(blockIdx.x / (uint32_t)a.T), t = (int)(blockIdx.x - (uint32_t)b * (uint32_t)a.T);
+    const uint32_t token = blockIdx.z * kAlongX + blockIdx.x;
+    if (token >= a.tokens) return;
+    const int b = (int)(token / (uint32_t)a.T), t = (int)(token - (uint32_t)b * (uint32_t)a.T);
     const int step = WIDE ? (HALF ? 8 : 4) : 1;                          // pairs per item
     const int turned = pairs / step;
     const int rest = WIDE ? (a.d - a.rotary) / 8 : a.d - a.rotary;
@@ -187,9 +191,9 @@ int launch_rope(int layout, int transposed, const double* freq, float magnitude,
     a.d = d;
     a.magnitude = magnitude;
     a.sign = transposed ? -magnitude : magnitude;
-    const int64_t n = (int64_t)B * T;
-    a.split = n >= 1024 ? 1 : 2;
-    const dim3 grid((unsigned)n, a.split);
+    a.tokens = (uint32_t)B * (uint32_t)T;        // at most 2^26
+    a.split = a.tokens >= 1024 ? 1 : 2;
+    const dim3 grid(std::min(a.tokens, kAlongX), a.split, (a.tokens + kAlongX - 1) / kAlongX);
     if (layout == DQ_ROPE_HALF)
         wide ? rope_kernel<true, true><<<grid, 256, 0, stream>>>(a) : rope_kernel<true, false><<<grid, 256, 0, stream>>>(a);
     else

@@ -188,3 +188,26 @@ def test_not_finite(dq):
     want = torch.zeros((4, 128), dtype=torch.bool)
     want[1, [3, 67]] = want[2, [6, 70]] = True
     assert torch.equal(bad.cpu(), want)
+
+
+@pytest.mark.parametrize("B,T,d", [(1, (1 << 23) - 1, 2), (1, (1 << 23) + 1, 2), (1, (1 << 24) + 5, 2), (3, (1 << 23) + 1, 16),
+                                   (1 << 13, 1 << 13, 2), (1 << 26, 1, 2)])
+def test_as_many_tokens_as_are_allowed(dq, B, T, d):
+    """More tokens than one axis of a grid has work-items for: every one is rotated
+    once, by its own position.  (All share one input vector.)"""
+    x = _x(T, 1, 1, 1, d).to(DEV)
+    rope = dq.RotaryPositions(d, layout="half")
+    out = torch.full((B, T, 1, d), math.nan, dtype=torch.bfloat16, device=DEV)
+    starts = torch.arange(B, dtype=torch.int32, device=DEV) * 3
+    rope.apply(x.expand(B, T, 1, d), starts=starts, t0=-7, q_out=out)
+    rows, a, b = out.view(B * T, d), x[0, 0, 0, :d // 2].double(), x[0, 0, 0, d // 2:].double()
+    slack = 2.0 ** -20 * (a.abs() + b.abs())
+    for lo in range(0, B * T, 1 << 22):
+        i = torch.arange(lo, min(B * T, lo + (1 << 22)), device=DEV)
+        turn = (i // T * 3 + i % T - 7).double()[:, None] * rope.freq
+        c, s = torch.cos(turn), torch.sin(turn)
+        for got, y in ((rows[i, :d // 2], a * c - b * s), (rows[i, d // 2:], a * s + b * c)):
+            assert bool(((got.double() - y).abs() <= 2.0 ** -8 * y.abs() + slack).all()), lo
+    # one more sequence than is allowed
+    with pytest.raises(dq.DqError):
+        rope.apply(x.expand((1 << 26) + 1, 1, 1, d))
