@@ -1,13 +1,17 @@
 """Attention of many queries where sizes are far apart: value blocks of unlike
-scales that get next to no weight or are not seen.  Against the formula in 64
-bits, within the bound that test_gpu_chunk.py derives: relative to sum a |v|, so
-that a block without weight does not widen it."""
+scales that get next to no weight or are not seen, values near the ends of the
+range, scores with a large common part.  Against the formula in 64 bits, within
+the bound that test_gpu_chunk.py derives: relative to sum a |v|, so that a block
+without weight does not widen it, and with the scores' size X in it."""
+
+import math
 
 import numpy as np
 import pytest
 import torch
 
-from test_gpu_chunk import DEV, FMTS, LOG2E, _check_all, _filled, _held, _i32, _kv, _q, dq  # noqa: F401
+from test_gpu_chunk import (DEV, FMTS, LOG2E, _check_all, _check_cross, _cross, _filled, _held, _i32, _kv, _q,  # noqa: F401
+                            _visible, dq)
 
 pytestmark = pytest.mark.gpu
 
@@ -114,3 +118,73 @@ def test_all_values_small_or_large(dq, fmt, n, to):
         cache = _filled(dq, fmt, k, x, H * G)
         out = cache.attend_chunk(q.to(DEV), _i32([T]))
         _check_all(out, q, _held(k, fmt), _held(x, fmt), [T], [n])
+
+
+# ----------------------------------------------------------------- large scores
+
+def _common(seed, T, n, H, G, size, rise, mixed=False):
+    """Scores (base 2, softmax scale 128^-0.5) of about `size`, of every row the same
+    to a few units; `rise`: how much higher the last token's are than the first's, evenly.
+    mixed: every other row's are without the common part, every fourth's negative."""
+    k, v = _kv(seed, 1, T, H)
+    q = _q(seed, 1, n, H * G)
+    unit = 128 ** -0.5 * LOG2E
+    k[..., 0], k[..., 1] = 64.0, (torch.arange(T)[:, None] * (60.0 / T)).to(torch.bfloat16)
+    part = torch.full((n, 1), size / (64.0 * unit))
+    if mixed:
+        part[1::2] = 0.0
+        part[2::4] *= -1.0
+    q[..., 0], q[..., 1] = part.to(torch.bfloat16), rise / (60.0 * unit)
+    return k, v, q
+
+
+SCORES = [(2.0 ** 11, 0), (-2.0 ** 11, 20), (2.0 ** 12, 40), (2.0 ** 13, -40), (-2.0 ** 13, 3), (2.0 ** 14, 300), (1500, 900)]
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("T,n,G", [(300, 6, 2), (300, 150, 1), (4100, 5, 4), (4100, 200, 1)])
+@pytest.mark.parametrize("size,rise", SCORES)
+def test_large_scores(dq, fmt, T, n, G, size, rise):
+    for mixed in (False, True):
+        k, v, q = _common(T + n, T, n, 1, G, size, rise, mixed)
+        cache = _filled(dq, fmt, k, v, G)
+        out = cache.attend_chunk(q.to(DEV), _i32([T]))
+        _check_all(out, q, _held(k, fmt), _held(v, fmt), [T], [n])
+
+
+@pytest.mark.parametrize("T,n,G", [(300, 6, 2), (300, 150, 1), (4100, 5, 4), (4100, 200, 1)])
+@pytest.mark.parametrize("size,rise", SCORES)
+def test_large_cross_scores(dq, T, n, G, size, rise):
+    for mixed in (False, True):
+        k, v, q = _common(T + n, T, n, 1, G, size, rise, mixed)
+        _check_cross(_cross(dq, q, k, v), q, k, v, [T], [n])
+
+
+def _steps(out, q, k, v, see, scale):
+    """out [n, 128] of a softmax so steep that it takes the largest score's value:
+    rows whose second score (base 2) lies 64 and the two scores' errors further down.
+    Every value of theirs is rounded once, 2^-8, the rest adds 2^-60 and the
+    quotient's few roundings of 2^-24."""
+    q = q.double().to(DEV)
+    s = torch.where(see, q @ k.T * (scale * LOG2E), -math.inf)
+    X = (q.abs() @ k.abs().T).amax(dim=1) * scale * LOG2E
+    best = s.topk(2, dim=1)
+    alone = best.values[:, 0] - best.values[:, 1] > 64 + 2 * 14 * 2.0 ** -24 * X
+    want = v[best.indices[:, 0]]
+    err = (out.double() - want).abs() / want.abs().amax(dim=1, keepdim=True)
+    assert int(alone.sum()) >= q.shape[0] // 2
+    assert float(err[alone].max()) <= 2.0 ** -8 + 2.0 ** -20
+
+
+@pytest.mark.parametrize("scale", [1e3, 1e4, 1e6, 1e30])
+@pytest.mark.parametrize("T,n", [(1500, 5), (1500, 150), (5000, 40)])
+def test_steep_softmax(dq, scale, T, n):
+    k, v = _kv(2, 1, T, 1)
+    q = _q(2, 1, n, 1)
+    see = _visible(T, n, n, True, 0, 0)
+    for fmt in FMTS:
+        cache = _filled(dq, fmt, k, v, 1)
+        out = cache.attend_chunk(q.to(DEV), _i32([T]), softmax_scale=scale)
+        _steps(out[0, :, 0], q[0, :, 0], _held(k, fmt)[0, 0, :T], _held(v, fmt)[0, 0, :T], see, scale)
+    out = _cross(dq, q, k, v, scale=scale)
+    _steps(out[0, :, 0], q[0, :, 0], *(x[0, :, 0].double().to(DEV) for x in (k, v)), torch.ones_like(see), scale)
