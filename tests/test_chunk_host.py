@@ -249,3 +249,29 @@ def test_binding_checks_on_the_gpu():
         rope.apply(q, q_out=torch.zeros((1, 4, 8, 128), dtype=torch.bfloat16, device=dev).expand(2, 4, 8, 128))
     with pytest.raises(dq.DqError):
         dq.RotaryPositions(256).apply(q)
+
+
+@pytest.mark.parametrize("r", [2, 4, 6, 32, 64, 96, 128, 250, 1024])
+@pytest.mark.parametrize("base", [1e4, 5e5, 10.0, 0.5])
+@pytest.mark.parametrize("factor,original,turns", [(8.0, 8192.0, (1.0, 4.0)), (40.0, 4096.0, (1.0, 32.0)), (1.5, 64.0, (0.25, 30.0)),
+                                                   (3.0, 1e6, (2.0, 2.5)), (2.0, 5.0, (1.0, 32.0)), (4.0, 1e9, (1.0, 32.0))])
+def test_mixed_frequencies(r, base, factor, original, turns):
+    """The two mixtures at every index, from the formulas alone.  A weight's ramp has
+    slope up to 1000 in its variable (the ends are at least 0.001 apart), whose
+    own error is a few of 2^-53 of numbers up to 2^10 (indexes) or of turns / (high -
+    low); both are far below 2^-30."""
+    i = np.arange(r // 2)
+    f = np.array([base ** (-2.0 * x / r) for x in i])
+    low, high = turns
+    w = (original * f / (2 * math.pi) - low) / (high - low)
+    w = np.where(w < 0, 0.0, np.where(w > 1, 1.0, w))
+    got, m = dq.dq_rope_frequencies(r, base=base, scaling="bands", factor=factor, original=original, turns=turns)
+    assert m == 1.0 and np.allclose(got, w * f + (1 - w) * f / factor, rtol=2.0 ** -30, atol=0)
+    j = lambda n: r * math.log(original / (2 * math.pi * n)) / (2 * math.log(base))  # noqa: E731
+    ends = sorted([min(max(math.floor(j(high)), 0), r - 1), min(max(math.ceil(j(low)), 0), r - 1)])
+    if j(high) <= j(low):
+        got, m = dq.dq_rope_frequencies(r, base=base, scaling="yarn", factor=factor, original=original, turns=turns)
+        span = max(ends[1] - ends[0], 0.001)
+        w = np.array([1 - min(max((x - ends[0]) / span, 0.0), 1.0) for x in i])
+        assert abs(m - (0.1 * math.log(factor) + 1)) < 1e-15
+        assert np.allclose(got, w * f + (1 - w) * f / factor, rtol=2.0 ** -30, atol=0)
