@@ -174,24 +174,22 @@ __device__ __forceinline__ int plan_of(float total, float segs, int longest, int
     return best >= longest ? kWhole : best;
 }
 
-// The same of all sequences.  first: seq_at(a, 0, lane).
+// The same of all sequences, at most 64.  first: seq_at(a, 0, lane).
 template <typename K>
 __device__ __forceinline__ int plan_chunk(const ChunkArgs& a, const Seq& first, int lane) {
     // (sums in fp32: the same bits wherever they are taken; a chunk a millionth too
     // short adds an item, which the workspace has room for)
-    float total = 0, segs = 0;
-    int longest = 0;
+    float total, segs;
+    int longest;
     if (a.B == 1) {
         const Seq q = seq_of<K>(a, 0);
         segs = (float)q.tiles;
         total = segs * (float)q.units;
         longest = q.units;
-    }
-    for (int b0 = 0; b0 < a.B && a.B > 1; b0 += kWave) {
-        const Seq q = b0 == 0 ? first : seq_at<K>(a, b0, lane);
-        total += wave_sum((float)q.tiles * (float)q.units);
-        segs += wave_sum((float)q.tiles);
-        longest = max(longest, wave_max(q.tiles ? q.units : 0));
+    } else {
+        total = wave_sum((float)first.tiles * (float)first.units);
+        segs = wave_sum((float)first.tiles);
+        longest = wave_max(first.tiles ? first.units : 0);
     }
     return plan_of<K>(total * (float)a.H, segs * (float)a.H, longest, lane);
 }
@@ -250,7 +248,6 @@ __device__ __forceinline__ Item find_item(const ChunkArgs& a, int id, int lane) 
         it.chunk = plan_chunk<K>(a, first, lane);
         if (id == 0 && threadIdx.x == 0) *a.plan = it.chunk;
     }
-    auto at = [&](int b0) { return b0 == 0 ? first : seq_at<K>(a, b0, lane); };
     const int heads = by_head ? a.H / 8 : a.H;   // of those that x counts
     int x = by_head ? id >> 3 : id;
     // pieces of a sequence's segment in a pass
@@ -263,14 +260,7 @@ __device__ __forceinline__ Item find_item(const ChunkArgs& a, int id, int lane) 
         return (int)(rest > it.chunk / 2 ? pass == 1 : (rest > 0 || n == 0) && pass == 2);
     };
     if (!SEGMENT && !by_head) {
-        int all = 0;
-        if (a.planned)
-            all = a.plan[1] * heads;
-        else
-            for (int b0 = 0; b0 < a.B; b0 += kWave) {
-                const Seq s = at(b0);
-                all += wave_sum(s.tiles * heads * pieces(s.units, it.chunk));
-            }
+        const int all = a.planned ? a.plan[1] * heads : wave_sum(first.tiles * heads * pieces(first.units, it.chunk));
         const int per = (all + 7) / 8;
         if ((id >> 3) >= per) return it;
         x = (id & 7) * per + (id >> 3);
@@ -319,24 +309,20 @@ __device__ __forceinline__ Item find_item(const ChunkArgs& a, int id, int lane) 
                 continue;
             }
         }
-        for (; b0 < a.B; b0 += kWave) {
-            const Seq s = at(b0);
-            const int own = s.tiles * heads * in_pass(s.units, pass), n = pieces(s.units, it.chunk);
-            const int held = n > 1 ? s.tiles * a.H * n : 0;
-            const int upto = before + scan64(own);
-            const int last = __builtin_amdgcn_readlane(upto, 63);
-            const int held_upto = slots + scan64(held);
-            if (x < last) {
-                const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > x));
-                entry(b0 + l, __builtin_amdgcn_readlane(s.tiles, l), __builtin_amdgcn_readlane(s.units, l),
-                      __builtin_amdgcn_readlane(held_upto - held, l), pass,
-                      x - __builtin_amdgcn_readlane(upto - own, l));
-                return it;
-            }
-            before = last;
-            slots = __builtin_amdgcn_readlane(held_upto, 63);
+        // (not planned: all sequences)
+        const Seq s = b0 == 0 ? first : seq_at<K>(a, b0, lane);
+        const int own = s.tiles * heads * in_pass(s.units, pass), n = pieces(s.units, it.chunk);
+        const int held = n > 1 ? s.tiles * a.H * n : 0;
+        const int upto = before + scan64(own);
+        const int last = __builtin_amdgcn_readlane(upto, 63);
+        const int held_upto = slots + scan64(held);
+        if (x < last) {
+            const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > x));
+            entry(b0 + l, __builtin_amdgcn_readlane(s.tiles, l), __builtin_amdgcn_readlane(s.units, l),
+                  __builtin_amdgcn_readlane(held_upto - held, l), pass, x - __builtin_amdgcn_readlane(upto - own, l));
+            return it;
         }
-        x -= before;
+        x -= last;
     }
     return it;
 }
