@@ -694,6 +694,8 @@ int dq_rope(int32_t layout, int32_t transposed, const double* freq, float magnit
  * bits than fp16's 11, below 2^-25 to nothing.)  Value blocks may be of any sizes:
  * one counts fully beside others of up to 2^80 times its scale, whatever their
  * weights, and values up to bf16's largest give no infinity.
+ * (Scales are finite and not negative, as the encoder writes them; one of values
+ * that is NaN or infinite gives NaN to the queries that see its block.)
  * The same call gives the same bits again; where long sequences are cut follows
  * from all lengths of the batch, so a sequence's last bits may go by the others.
  * Through a block table the call is the same; an entry outside the pool sets

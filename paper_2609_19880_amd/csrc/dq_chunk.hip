@@ -406,6 +406,8 @@ __device__ __forceinline__ float clamped(float x) {    // NaN stays
     return x < -kBig ? -kBig : x;
 }
 
+__device__ __forceinline__ float log_scale(float x) { return x == 0.f ? kNoScale : __builtin_amdgcn_logf(x); }
+
 // Two rounded weights' sum added to x, in fp32.
 template <int SRC>
 __device__ __forceinline__ float plus_weights(uint32_t w, float x) {
@@ -536,7 +538,7 @@ struct Rows {
     // The softmax of a block whose scores are s, times c: p are its weights.
     // t0: the block's first token; shown: bit t of it is clear where token t is
     // hidden; vl: log2 of the values' scale, kNoScale for a block of zeros (any
-    // weight will do).
+    // weight will do), NaN or infinity for one of NaN (rows that see it become NaN).
     __device__ __forceinline__ void block(f32x16& s, float c, float vl, int t0, uint32_t shown, int lane,
                                           u32x4 (&p)[2]) {
         c = fmaxf(c, 0x1p-120f);                 // (a factor of 0, which hidden scores could not bear)
@@ -596,7 +598,9 @@ struct Rows {
         bool lost = false;
         if constexpr (q8) {
             const float rel = vl - vref;
-            if (vl > kNoScale && !(rel >= -2.f && rel <= 0.f)) {
+            const bool number = vl < 256.f;
+            l = !number && top != -INFINITY ? NAN : l;
+            if (number && vl > kNoScale && !(rel >= -2.f && rel <= 0.f)) {
                 float to = floorf(vl) + 1.f;     // (room for scales of up to twice the size)
                 if (vref - to > 64.f) to = fmaxf(to, vref - most_up());
                 by += vref - to;
@@ -910,7 +914,7 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
         char* to = lds + (step & 1) * L::kStage;
         if constexpr (q8) {
             if (tid == 0) lscale[step & 1].x = sreg;
-            if (tid == kWave) lscale[step & 1].y = sreg > 0.f ? __builtin_amdgcn_logf(sreg) : kNoScale;
+            if (tid == kWave) lscale[step & 1].y = log_scale(sreg);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const u32x2 w0 = halves4<SRC>(reg[i][0]), w1 = halves4<SRC>(reg[i][1]);
@@ -1139,7 +1143,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_kernel(ChunkArgs a) {
             ks = ks_next;
             vs = vs_next;
             c *= ks;
-            vl = vs > 0.f ? __builtin_amdgcn_logf(vs) : kNoScale;
+            vl = log_scale(vs);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const u32x2 w0 = halves4<SRC>(kraw[i][0]), w1 = halves4<SRC>(kraw[i][1]);

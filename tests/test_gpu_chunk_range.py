@@ -10,8 +10,8 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_chunk import (DEV, FMTS, LOG2E, _check_all, _check_cross, _cross, _filled, _held, _i32, _kv, _q,  # noqa: F401
-                            _visible, dq)
+from test_gpu_chunk import (DEV, FMTS, LOG2E, _check, _check_all, _check_cross, _cross, _filled, _held, _i32, _kv,  # noqa: F401
+                            _q, _visible, dq)
 
 pytestmark = pytest.mark.gpu
 
@@ -118,6 +118,26 @@ def test_all_values_small_or_large(dq, fmt, n, to):
         cache = _filled(dq, fmt, k, x, H * G)
         out = cache.attend_chunk(q.to(DEV), _i32([T]))
         _check_all(out, q, _held(k, fmt), _held(x, fmt), [T], [n])
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("T,n,window", [(300, 200, 0), (200, 8, 36), (200, 40, 36), (4100, 200, 3950), (4100, 200, 3800)])
+def test_a_value_scale_that_is_no_number(dq, fmt, T, n, window):
+    """NaN for the queries that see the block, as the decode step gives; the others
+    are as they were."""
+    k, v = _kv(n, 1, T, 1)
+    q = _q(n, 1, n, 2)
+    see = _visible(T, n, n, True, window, 0)
+    sees = see[:, 128:160].any(dim=1)
+    rest = (~sees).nonzero()[:, 0]
+    assert bool(sees.any()) and (window == 3950 or rest.numel() > 0)
+    for what in (math.nan, math.inf):
+        cache = _filled(dq, fmt, k, v, 2)
+        cache.v_scales[:, :, 4] = what
+        out = cache.attend_chunk(q.to(DEV), _i32([T]), window=window)[0]
+        assert bool(torch.isnan(out[sees]).all())
+        if rest.numel():
+            _check(out[rest], q[0, rest.cpu()], _held(k, fmt)[0, :, :T], _held(v, fmt)[0, :, :T], see[rest], 128 ** -0.5, 11)
 
 
 # ----------------------------------------------------------------- large scores
