@@ -18,6 +18,7 @@
 // below the power of 2 that the sums are relative to: it follows the blocks.
 // Queries are brought to a largest magnitude of 2^13 by
 // a power of 2 of each row, exactly but for values 2^-37 of the largest.
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -1472,7 +1473,7 @@ int launch_chunk(const ChunkSource& src, const ChunkCall& c, void* ws, uint32_t*
     a.kv_aligned = !q8 && aligned16(src.k) && aligned16(src.v);
     a.out_aligned = ((reinterpret_cast<uintptr_t>(c.out.p) | (uintptr_t)(c.out.sb * 2) | (uintptr_t)(c.out.st * 2) |
                       (uintptr_t)(c.out.sh * 2)) & 7) == 0;
-    a.scale_log2 = fabsf(c.scale) * kLog2e;
+    a.scale_log2 = std::min(fabsf(c.scale) * kLog2e, FLT_MAX);           // (infinity times a score of 0: NaN)
     a.negative = c.scale < 0.f;
     a.status = status;
     ChunkArgs few = a, many = a;

@@ -208,3 +208,15 @@ def test_steep_softmax(dq, scale, T, n):
         _steps(out[0, :, 0], q[0, :, 0], _held(k, fmt)[0, 0, :T], _held(v, fmt)[0, 0, :T], see, scale)
     out = _cross(dq, q, k, v, scale=scale)
     _steps(out[0, :, 0], q[0, :, 0], *(x[0, :, 0].double().to(DEV) for x in (k, v)), torch.ones_like(see), scale)
+
+
+@pytest.mark.parametrize("scale", [3.4e38, -3.4e38])
+@pytest.mark.parametrize("T,n", [(300, 6), (300, 150), (4100, 5)])
+def test_the_largest_softmax_scales(dq, scale, T, n):
+    """Scores of 0 stay 0, whatever scale is allowed: the mean of the values."""
+    k, v = _kv(n, 1, T, 1)
+    q = torch.zeros_like(_q(n, 1, n, 2))
+    for fmt in FMTS:
+        out = _filled(dq, fmt, k, v, 2).attend_chunk(q.to(DEV), _i32([T]), softmax_scale=scale)
+        _check_all(out, q, _held(k, fmt), _held(v, fmt), [T], [n], scale=scale)
+    _check_cross(_cross(dq, q, k, v, scale=scale), q, k, v, [T], [n], scale=scale)
