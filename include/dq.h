@@ -690,8 +690,9 @@ int dq_rope(int32_t layout, int32_t transposed, const double* freq, float magnit
  * A query that sees no token gives zeros; one with an infinity or NaN that sees
  * some gives NaN.  Scores and sums are held in fp32; the weights are rounded to
  * fp16 for the product with the codes of the values, which are exact, and the
- * output to bf16.  (Weights below 2^-14 of a query's largest are rounded to fewer
- * bits than fp16's 11, below 2^-25 to nothing.)  Value blocks may be of any sizes:
+ * output to bf16.  (What counts for that is a weight times its block's scale: of a
+ * query's largest, 11 bits down to 2^-14 of it, fewer below, and nothing below
+ * 2^-25.)  Value blocks may be of any sizes:
  * one counts fully beside others of up to 2^80 times its scale, whatever their
  * weights, and values up to bf16's largest give no infinity.
  * (Scales are finite and not negative, as the encoder writes them; one of values

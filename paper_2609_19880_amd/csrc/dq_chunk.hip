@@ -14,8 +14,8 @@
 // the weights are the second product's operand where they lie.
 //
 // 8-bit codes are exact in fp16.  A key block's scale multiplies the scores; a
-// value block's scale goes into the exponent of the weights, as far as a quarter
-// below the power of 2 that the sums are relative to: it follows the blocks.
+// value block's scale goes into the exponent of the weights, relative to a power
+// of 2 that follows what the row's blocks weigh.
 // Queries are brought to a largest magnitude of 2^13 by
 // a power of 2 of each row, exactly but for values 2^-37 of the largest.
 #include <float.h>
@@ -37,6 +37,7 @@ constexpr float kBig = 3e38f;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kRowsOf = 32;                  // rows per wavefront
 constexpr float kNoScale = -1e30f;           // log2 of the scale of a block of zeros
+constexpr float kNoRef = -1e29f;             // of what no sums are relative to (zeros are low beside it)
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
@@ -407,7 +408,10 @@ __device__ __forceinline__ float clamped(float x) {    // NaN stays
     return x < -kBig ? -kBig : x;
 }
 
-__device__ __forceinline__ float log_scale(float x) { return x == 0.f ? kNoScale : __builtin_amdgcn_logf(x); }
+// (infinities and NaN: NaN)
+__device__ __forceinline__ float log_scale(float x) {
+    return x == 0.f ? kNoScale : __builtin_amdgcn_logf(x) + (x - x);
+}
 
 // Two rounded weights' sum added to x, in fp32.
 template <int SRC>
@@ -443,7 +447,8 @@ struct Rows {
 
     u32x4 q[8];
     f32x16 o[4];
-    float m, l, vref, qc;        // vref: log2 of the scale that the sums are relative to, an integer
+    float m, l, vref, qc;        // vref: log2 of the scale that the row's sums are relative to, an integer
+    float off;                   // weights are exp2(score + off + log2 of the values' scale)
     int end;                     // the row sees t < end, of those t < sinks or t >= end - window
     int T, window, sinks;
     int lim_lo, lim_hi, start_hi;
@@ -464,7 +469,8 @@ struct Rows {
         start_hi = start(__builtin_amdgcn_readlane(end, 31));
         m = -INFINITY;
         l = 0.f;
-        vref = kNoScale;
+        vref = kNoRef;
+        off = offset();
         qc = a.scale_log2;
         careful = true;
 #pragma unroll
@@ -535,11 +541,12 @@ struct Rows {
     }
 
     __device__ __forceinline__ float mu() const { return m == -INFINITY ? 0.f : m; }
+    __device__ __forceinline__ float offset() const { return q8 ? kUp - mu() - vref : kUp - mu(); }
 
     // The softmax of a block whose scores are s, times c: p are its weights.
     // t0: the block's first token; shown: bit t of it is clear where token t is
     // hidden; vl: log2 of the values' scale, kNoScale for a block of zeros (any
-    // weight will do), NaN or infinity for one of NaN (rows that see it become NaN).
+    // weight will do), NaN for one that is no number (rows that see it become NaN).
     __device__ __forceinline__ void block(f32x16& s, float c, float vl, int t0, uint32_t shown, int lane,
                                           u32x4 (&p)[2]) {
         c = fmaxf(c, 0x1p-120f);                 // (a factor of 0, which hidden scores could not bear)
@@ -550,18 +557,17 @@ struct Rows {
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[e] = (vis >> (8 * (e >> 2) + (e & 3))) & 1 ? s[e] : -INFINITY;
         }
-        // Of the scale the weights hold 2^-2 to 2^0: less would cost them bits of fp16,
-        // however much the block weighs.
+        // Of the scale the weights hold 2^-2 and more (as long as they fit): less would
+        // cost them bits of fp16, however much the block weighs.
         float d = 0.f;
-        bool again = careful;
+        bool low = false;
         if constexpr (q8) {
-            const float rel = vl <= kNoScale ? 0.f : vl - vref;
-            const bool holds = rel >= -2.f && rel <= 0.f;
-            d = holds ? rel : 0.f;               // (if not, at least what it will be)
-            again = again || !holds;
+            d = vl - vref;
+            low = !(d >= -2.f);                  // (a block of zeros too, and one that is no number)
         }
-        float sum = weigh(s, c, kUp + d - mu(), p);
-        if (again || __builtin_amdgcn_ballot_w64(sum > kMost) != 0) sum = anew(s, c, sum, vl, d, lane, p);
+        float sum = weigh(s, c, q8 ? off + vl : off, p);
+        if (careful || (__builtin_amdgcn_ballot_w64(low) | __builtin_amdgcn_ballot_w64(sum > kMost)) != 0)
+            sum = anew(s, c, sum, vl, low, d, lane, p);
         l += q8 ? sum * __builtin_amdgcn_exp2f(-d) : sum;
     }
 
@@ -569,15 +575,20 @@ struct Rows {
     // the weights without them.  (Selections rather than branches, and one place
     // that scales the sums: with branches the compiler keeps both results.)
     //
-    // The scale that the sums are relative to becomes the block's, rounded up to a
-    // power of 2 or twice that, where the weights do not hold it: rows to which a
-    // larger block is nothing, or that do not see it, must not lose the smaller ones.
-    // The sums are scaled by a power of 2, exactly: down by up to 2^99 without a loss
-    // (a weight of 2^-25, a code of 1), up as far as they stay below 2^124 (sums of
-    // usual weights, 2^2 or less, by over 2^100).  Where that is not enough the
-    // block's values are nothing beside the sums of some row of the wavefront, and
-    // are left out.
-    __device__ __forceinline__ float anew(f32x16& s, float c, float sum, float vl, float& d, int lane, u32x4 (&p)[2]) {
+    // What a row's sums are relative to, 2^(m + vref), goes by what its blocks weigh, a
+    // scale times a weight: a block that is not seen, or weighs next to nothing, changes
+    // nothing however large it is, one that makes up the output by its size alone keeps its
+    // bits, and so do values beside zeros that have nearly all weight.  vref is
+    // - the block's scale, rounded up to a power of 2 or twice that (room for others),
+    //   times its largest weight, where the weights would not fit;
+    // - its scale, where the weights would lose bits of it (low);
+    // - or else as much lower as the maximum is higher.
+    // Sums are scaled by a power of 2, exactly: down to 2^-126, up as far as they
+    // stay below 2^124 (from sums of usual weights, 2^2 or less, by over 2^100).  Where
+    // that is not enough the block's values are nothing beside the row's sums, and are
+    // left out.
+    __device__ __forceinline__ float anew(f32x16& s, float c, float sum, float vl, bool low, float& d, int lane,
+                                          u32x4 (&p)[2]) {
         float top = s[0];                        // (NaN where every score is)
 #pragma unroll
         for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
@@ -592,47 +603,54 @@ struct Rows {
         for (int e = 0; e < 16; ++e) s[e] = exact && s[e] != -INFINITY ? clamped(s[e] * c) : s[e];
         top = fmaxf(top, xor_lane<32>(top, lane));
         sum = fmaxf(sum, xor_lane<32>(sum, lane));
-        const bool higher = (m == -INFINITY || (exact ? top > m + 4.f : sum > kMost)) && top > m;
+        const bool higher = (m == -INFINITY || (exact || low ? top > m + 4.f : sum > kMost)) && top > m;
+        const float rise = higher && m != -INFINITY ? top - m : 0.f;
         float by = higher ? m - top : 0.f;
         l *= __builtin_amdgcn_exp2f(by);
         m = higher ? top : m;
-        bool lost = false;
+        bool whole = true;                       // the weights hold the block's scale
         if constexpr (q8) {
-            const float rel = vl - vref;
-            const bool number = vl < 256.f;
-            l = !number && top != -INFINITY ? NAN : l;
-            if (number && vl > kNoScale && !(rel >= -2.f && rel <= 0.f)) {
-                float to = floorf(vl) + 1.f;     // (room for scales of up to twice the size)
-                if (vref - to > 64.f) to = fmaxf(to, vref - most_up());
-                by += vref - to;
-                vref = to;
-                lost = vl - to < -2.f;
-                d = lost ? 0.f : vl - to;
-            }
+            const bool seen = top != -INFINITY;
+            l = seen && vl != vl ? NAN : l;
+            // (no further down than a weight of 2^-200, which is nothing)
+            const float weighs = vl + fmaxf(fminf(top - m, 0.f), -200.f), base = vref - floorf(rise);
+            const bool over = weighs > base && (higher || sum > kMost || (exact && weighs > base + 4.f));
+            float to = floorf(low ? vl : weighs) + 1.f;      // (room for scales of up to twice the size)
+            to = seen && vl > kNoScale && (low || over) ? to : base;
+            if (__builtin_amdgcn_ballot_w64(vref - rise - to > 64.f) != 0) to = fmaxf(to, vref - rise - most_up(lane));
+            by += vref - to;
+            vref = to;
+            whole = vl > kNoScale && vl - vref >= -2.f;
+            d = whole ? vl - vref : 0.f;
         }
+        off = offset();
         const float f = __builtin_amdgcn_exp2f(by);
         // (whole vectors: element by element the compiler holds the sums twice)
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] *= f;
         careful = __builtin_amdgcn_ballot_w64(!(fabsf(m) < 0x1p11f)) != 0;
         // (large scores: the difference first, which is exact where it counts)
-        const float less = exact ? mu() : 0.f, e0 = exact ? kUp + d : kUp + d - mu();
+        const float less = exact ? mu() : 0.f, e0 = exact ? kUp + d : !whole ? kUp - mu() : q8 ? off + vl : off;
         c = exact ? 1.f : c;
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[e] -= less;
         const float rounded = weigh(s, c, e0, p);
-        if (lost) p[0] = p[1] = u32x4{0u, 0u, 0u, 0u};
+        if (__builtin_amdgcn_ballot_w64(!whole) != 0)
+#pragma unroll
+            for (int st = 0; st < 2; ++st)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) p[st][i] = whole ? p[st][i] : 0u;
         return rounded;
     }
 
-    // By how many powers of 2 the wavefront's sums may grow.
-    __device__ __forceinline__ float most_up() const {
-        float top = 0.f;
+    // By how many powers of 2 the row's sums may grow.
+    __device__ __forceinline__ float most_up(int lane) const {
+        float top = 0x1p-126f;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(o[i][e]));
-        return 124.f - ceilf(__builtin_amdgcn_logf(fmaxf(wave_max(top), 0x1p-126f)));
+        return 124.f - ceilf(__builtin_amdgcn_logf(fmaxf(top, xor_lane<32>(top, lane))));
     }
 
     // The values of half of a block's tokens.
@@ -962,7 +980,7 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
                 if constexpr (q8) {
                     const float2 both = lscale[step & 1];
                     c *= both.x;
-                    vl = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(both.y)));
+                    vl = both.y;
                 }
 #pragma unroll
                 for (int part = 0; part < 2; ++part) {

@@ -51,6 +51,66 @@ def test_large_blocks_without_weight(dq, fmt, B, T, n, H, G, up):
 
 
 @pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("B,T,n,H,G", [(1, 200, 5, 1, 4), (1, 200, 150, 1, 2), (1, 4100, 6, 1, 2), (1, 4100, 150, 1, 1),
+                                       (2, 500, 70, 8, 1)])
+@pytest.mark.parametrize("up,down", [(12, 10), (30, 28), (60, 63), (100, 90), (110, 112)])
+def test_large_blocks_with_little_weight(dq, fmt, B, T, n, H, G, up, down):
+    """Blocks 2^up as large as the others, with weights 2^-down of theirs: they make
+    a good part of the output, or most of it."""
+    k, v = _kv(T + n, B, T, H)
+    q = _q(up, B, n, H * G)
+    last = (T - n) // 32 - 1
+    for blocks in ([0], [1, last], [last // 2, last]):
+        kk, qq = _low(k, q, blocks, down)
+        x = v.float()
+        for j in blocks:
+            x[:, 32 * j:32 * j + 32] *= 2.0 ** up
+        x = x.to(torch.bfloat16)
+        cache = _filled(dq, fmt, kk, x, H * G)
+        out = cache.attend_chunk(qq.to(DEV), _i32([T] * B))
+        _check_all(out, qq, _held(kk, fmt), _held(x, fmt), [T] * B, [n] * B)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("T,n", [(400, 6), (400, 150), (4100, 100)])
+def test_zeros_with_most_of_the_weight(dq, fmt, T, n):
+    """First blocks of zeros that get nearly all weight, then values: what their
+    small weights leave is the output."""
+    k, v = _kv(T + n, 1, T, 1)
+    q = _q(n, 1, n, 2)
+    for down in (5, 30, 100):
+        kk, qq = _low(k, q, range(2, -(-T // 32)), down)
+        x = v.clone()
+        x[:, :64] = 0
+        cache = _filled(dq, fmt, kk, x, 2)
+        out = cache.attend_chunk(qq.to(DEV), _i32([T]))
+        _check_all(out, qq, _held(kk, fmt), _held(x, fmt), [T], [n])
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("T,n", [(600, 6), (600, 150), (4100, 100)])
+@pytest.mark.parametrize("size", [0.0, 3000.0, 2.0 ** 14])
+def test_zeros_between_values(dq, fmt, T, n, size):
+    """Values, zeros that get nearly all weight, then values of the first ones' sizes
+    and larger, with small and with large scores."""
+    k, v = _kv(T + n, 1, T, 1)
+    q = _q(n, 1, n, 2)
+    unit = 128 ** -0.5 * LOG2E
+    for down in (5, 30, 60):
+        kk, qq = _low(k, q, [j for j in range(-(-T // 32)) if j not in (6, 7)], down)
+        kk[..., 1], qq[..., 1] = 64.0, size / (64.0 * unit)
+        x = v.float()
+        x[:, 192:256] = 0
+        x[:, 320:352] *= 2.0 ** 20
+        x[:, 128:160] *= 2.0 ** 50
+        x[:, 384:] *= 2.0 ** 55
+        x = x.to(torch.bfloat16)
+        cache = _filled(dq, fmt, kk, x, 2)
+        out = cache.attend_chunk(qq.to(DEV), _i32([T]))
+        _check_all(out, qq, _held(kk, fmt), _held(x, fmt), [T], [n])
+
+
+@pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("n", [8, 300])
 @pytest.mark.parametrize("window,sinks", [(20, 0), (64, 5), (40, 70)])
 def test_large_blocks_outside_the_window(dq, fmt, n, window, sinks):
