@@ -752,8 +752,10 @@ __device__ __forceinline__ float inverse(float l) { return l == 0.f ? 0.f : 1.f 
 constexpr int kJoinRow = 68;                     // floats: 64 channels, and 4 to keep rows in different banks
 
 template <typename K, int WAVES, bool PAIRED>
-__device__ __forceinline__ void join_rows(const ChunkArgs& a, const f32x16 (&o)[4], float m, float l, float up, float* join, float (&wm)[WAVES][kRowsOf], float (&wl)[WAVES][kRowsOf],
-                                          int parts, int rows, int r0, int b, int h, bool whole, int64_t slot) {
+__device__ __forceinline__ void join_rows(const ChunkArgs& a, const f32x16 (&o)[4], float m, float l, float up,
+                                          float* join, float (&wm)[WAVES][kRowsOf], float (&wl)[WAVES][kRowsOf],
+                                          float (&each)[WAVES][kRowsOf], int parts, int rows, int r0, int b, int h,
+                                          bool whole, int64_t slot) {
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, half = lane >> 5, col = lane & 31;
     const float f = inverse(l);
     if (half == 0) {
@@ -772,28 +774,30 @@ __device__ __forceinline__ void join_rows(const ChunkArgs& a, const f32x16 (&o)[
                 *reinterpret_cast<f32x4*>(join + (wave * kRowsOf + col) * kJoinRow + ch) =
                     f32x4{x[4 * i] * f * up, x[4 * i + 1] * f * up, x[4 * i + 2] * f * up, x[4 * i + 3] * f * up};
             }
+        if (m2 == 0 && tid < WAVES * kRowsOf) {  // (the shares, once; by every thread for itself: 1.5 us more)
+            const int w = tid / kRowsOf, row = tid % kRowsOf;
+            float top = -INFINITY, sum = 0.f;
+            for (int x = w & (parts - 1); x < WAVES; x += parts) top = fmaxf(top, wm[x][row]);
+            for (int x = w & (parts - 1); x < WAVES; x += parts) sum += share(wm[x][row], wl[x][row], top);
+            each[w][row] = share(wm[w][row], wl[w][row], top) * inverse(sum);
+            const int in = w * kRowsOf + row;
+            if (!whole && w < parts && r0 + in < rows) {
+                a.ws_ml[slot * 2 * K::kRows + in] = top;
+                a.ws_ml[slot * 2 * K::kRows + K::kRows + in] = sum;
+            }
+        }
         __syncthreads();
         for (int i = tid; i < parts * kRowsOf * 16; i += WAVES * kWave) {
             const int in = i >> 4, ch = (i & 15) * 4, r = r0 + in;
             if (r >= rows) break;
-            float top = -INFINITY;
-            for (int w = in >> 5; w < WAVES; w += parts) top = fmaxf(top, wm[w][in & 31]);
-            float sum = 0.f;
-            for (int w = in >> 5; w < WAVES; w += parts) sum += share(wm[w][in & 31], wl[w][in & 31], top);
-            const float each = inverse(sum);
             f32x4 acc = {0.f, 0.f, 0.f, 0.f};
             for (int w = in >> 5; w < WAVES; w += parts)
-                acc += *reinterpret_cast<const f32x4*>(join + (w * kRowsOf + (in & 31)) * kJoinRow + ch) *
-                       (share(wm[w][in & 31], wl[w][in & 31], top) * each);
+                acc += *reinterpret_cast<const f32x4*>(join + (w * kRowsOf + (in & 31)) * kJoinRow + ch) * each[w][in & 31];
             if (whole) {
                 const int token = r / a.G, head = h * a.G + r - token * a.G;
                 store_row(a, b, token, head, 64 * m2 + ch, bf16_two(acc[0], acc[1]), bf16_two(acc[2], acc[3]));
             } else {
                 *reinterpret_cast<f32x4*>(a.ws_acc + (slot * K::kRows + in) * kD + 64 * m2 + ch) = acc;
-                if (m2 == 0 && ch == 0) {
-                    a.ws_ml[slot * 2 * K::kRows + in] = top;
-                    a.ws_ml[slot * 2 * K::kRows + K::kRows + in] = sum;
-                }
             }
         }
     }
@@ -1061,7 +1065,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_kernel(ChunkArgs a) {
     constexpr bool q8 = L::q8;
     constexpr int kJoin = kFewWaves * kRowsOf * kJoinRow * 4, kOwn = q8 ? 0 : L::kStage;
     __shared__ __attribute__((aligned(16))) char lds[kJoin > kFewWaves * kOwn ? kJoin : kFewWaves * kOwn];
-    __shared__ float wm[kFewWaves][kRowsOf], wl[kFewWaves][kRowsOf];
+    __shared__ float wm[kFewWaves][kRowsOf], wl[kFewWaves][kRowsOf], each[kFewWaves][kRowsOf];
 
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -1228,7 +1232,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_kernel(ChunkArgs a) {
 
     join_rows<Few, kFewWaves, q8>(a, me.o, me.m, me.l + xor_lane<32>(me.l, lane),
                                   q8 ? __builtin_amdgcn_exp2f(me.vref) : 1.f, reinterpret_cast<float*>(lds), wm, wl,
-                                  parts, rows, 0, b, h, whole, it.slot);
+                                  each, parts, rows, 0, b, h, whole, it.slot);
 }
 
 // The pieces of a segment's rows joined: half a wavefront has a row at a time, four
