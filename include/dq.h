@@ -721,7 +721,10 @@ int dq_rope(int32_t layout, int32_t transposed, const double* freq, float magnit
  * 2^30.
  *
  * dq_chunk_workspace_bytes: for both; t_cap is the cache's capacity (max_pages *
- * page_tokens) or n_kv.  0 for sizes that the calls refuse.
+ * page_tokens) or n_kv.  It holds the outputs of the pieces that the GPU works on
+ * at a time, with or without q_lens: at most 121 MB whatever the sizes are, and as
+ * much wherever one sequence may be cut into many.  0 for sizes that the calls
+ * refuse, and where nothing can be cut.
  */
 size_t dq_chunk_workspace_bytes(int32_t batch, int32_t n_q, int32_t q_heads, int32_t kv_heads, int32_t t_cap);
 int dq_q8_chunk_attention(int32_t format, const uint16_t* q, int64_t q_stride_b, int64_t q_stride_t,

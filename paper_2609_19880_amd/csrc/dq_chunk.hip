@@ -15,9 +15,17 @@
 //
 // 8-bit codes are exact in fp16.  A key block's scale multiplies the scores; a
 // value block's scale goes into the exponent of the weights, relative to a power
-// of 2 that follows what the row's blocks weigh.
-// Queries are brought to a largest magnitude of 2^13 by
-// a power of 2 of each row, exactly but for values 2^-37 of the largest.
+// of 2 that follows what the row's blocks weigh.  Queries are brought to a largest
+// magnitude of 2^13 to 2^14 by a power of 2 of each row: exactly down to 2^-30 of
+// the largest (bf16's 8 bits above fp16's last, 2^-24), to 2^-38 of it below.
+//
+// Weights take the values' type, which the matrix instructions ask for: fp16 (11
+// bits) over codes, bf16 (8 bits) over BF16 states, whose range fp16 does not hold.
+// The denominator is the sum of the rounded weights, so a common error of theirs
+// cancels.  (The decode step keeps 22 bits of the weights with two products; here
+// that is half as much matrix work again, for an error that the output's rounding to
+// bf16 exceeds over codes and equals over BF16 states: 0.0020 to 0.0025 against
+// 0.0017 in all.)
 #include <float.h>
 #include <math.h>
 
@@ -431,9 +439,10 @@ __device__ __forceinline__ float plus_weights(uint32_t w, float x) {
 // The state's maximum m is not the running maximum but one that the sums keep
 // until a block's weights, relative to it, add up to more than 2^15: weights of
 // m itself are 2^2, so fp16 holds what lies 2^13 above and, to its 11 bits, 2^16
-// below (to 2^-25 beyond).  Most blocks so need no maximum and scale nothing:
+// below (to 2^-25 beyond; over codes times the 2^-2 or more of the block's scale that
+// they hold).  Most blocks so need no maximum and scale nothing:
 // their weights are computed with the m at hand and only checked (a running maximum
-// adds 16 maxima, an exchange between two lanes and 64 products to the 131 vector
+// adds 16 maxima, an exchange between two lanes and 64 products to the 128 vector
 // instructions that a block takes).  A row's bits
 // do not depend on the rows beside it, but where their scores pass 2^11.  (BF16:
 // m itself weighs 1.  Any limit would do for bf16's range; 2^60 in place of 2^15 is
@@ -811,13 +820,14 @@ __device__ __forceinline__ void join_rows(const ChunkArgs& a, const f32x16 (&o)[
 // and a block's scores.
 //
 // Bound by no single unit: 4 x 8171 queries over themselves (32 heads, int8) run at
-// 910 to 940 TFLOP/s, where the matrix units are busy 42 % of the time, other vector
-// instructions (131 per wavefront and block, 16 of them exponentials) issue about
+// 930 to 965 TFLOP/s, where the matrix units are busy 42 % of the time, other vector
+// instructions (128 per wavefront and block, 16 of them exponentials) issue about
 // as long, LDS is active 33 %, and the clock falls to 1.9 GHz.  Left out one at a
-// time, exponentials, the weights' sums, conversions, loads or the second product
-// each give back 3 to 9 %.  Not faster: two wavefronts per SIMD with the blocks'
-// steps interleaved, twelve wavefronts per workgroup (2 to 5 % on the largest, slower
-// elsewhere), two or three blocks requested ahead, wavefront priorities.
+// time, the softmax's arithmetic gives back 16 %, the second product 9 %, loads 8 %,
+// exponentials 5 %, the weights' sums or the conversions 2 to 3 %.  Twelve wavefronts
+// per workgroup take 2 to 5 % less on the largest cases and more on the others: left
+// as it is, one form for all.  Not faster: two wavefronts per SIMD with the blocks'
+// steps interleaved, two or three blocks requested ahead, wavefront priorities.
 template <int SRC>
 __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
     typedef Lds<SRC> L;
@@ -1050,7 +1060,7 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
 // it for itself; the wavefronts' sums are joined in LDS at the end.  Bound by
 // memory: a block's codes are requested as soon as the registers of the last
 // one's are free, keys while the weights are computed, values while the next
-// scores are.  16 x 8 queries over 32768 e4m3 tokens (32 heads) take 177 us, 6.1
+// scores are.  16 x 8 queries over 32768 e4m3 tokens (32 heads) take 174 to 177 us, 6.1
 // TB/s (262 with the codes converted through LDS for all wavefronts).
 //
 // Values of codes: a lane reads whole 16-byte pieces (two channels 16 apart of 8
@@ -1238,7 +1248,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_kernel(ChunkArgs a) {
 // The pieces of a segment's rows joined: half a wavefront has a row at a time, four
 // channels a lane.  Bound by latency (plan, lengths, maxima, sums) where pieces are
 // few: one row for each half of a workgroup's wavefronts, 4.5 us for 16 pieces (7.1
-// with two rows); by memory where they are many (50 MB of them 14 us), and there
+// with two rows); by memory where they are many (50 MB of them 13 us), and there
 // fewer workgroups, each of which looks its segment up, take less (48 ragged chunks
 // 473 us with two rows, 486 with one).
 // Over the 32 lanes of half a wavefront; every lane gets the result.
