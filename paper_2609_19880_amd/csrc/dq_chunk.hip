@@ -626,7 +626,8 @@ struct Rows {
             const bool over = weighs > base && (higher || sum > kMost || (exact && weighs > base + 4.f));
             float to = floorf(low ? vl : weighs) + 1.f;      // (room for scales of up to twice the size)
             to = seen && vl > kNoScale && (low || over) ? to : base;
-            if (__builtin_amdgcn_ballot_w64(vref - rise - to > 64.f) != 0) to = fmaxf(to, vref - rise - most_up(lane));
+            // (by any step: they add up)
+            if (__builtin_amdgcn_ballot_w64(vref - rise - to > 0.f) != 0) to = fmaxf(to, ceilf(vref - rise) - most_up(lane));
             by += vref - to;
             vref = to;
             whole = vl > kNoScale && vl - vref >= -2.f;
@@ -644,7 +645,7 @@ struct Rows {
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[e] -= less;
         const float rounded = weigh(s, c, e0, p);
-        if (__builtin_amdgcn_ballot_w64(!whole) != 0)
+        if constexpr (q8)
 #pragma unroll
             for (int st = 0; st < 2; ++st)
 #pragma unroll

@@ -165,6 +165,28 @@ def test_a_large_block_between_even_ones(dq, fmt, n):
 
 
 @pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("B,T,H,n", [(1, 256, 2, 130), (64, 1024, 8, 5)])
+@pytest.mark.parametrize("down", [0, 150])
+def test_sizes_that_fall_step_by_step(dq, fmt, B, T, H, n, down):
+    """Blocks that one wavefront takes one after another, of sizes from 2^60 down to
+    2^-60 and up again, with equal weights or with so little of the first ones' that
+    the small ones make up the output.  (All sequences share keys and values.)"""
+    k, v = _kv(n, 1, T, H)
+    q = _q(n, B, n, H)
+    blocks = T // 32
+    fall = np.linspace(60, -60, blocks)
+    for order in (fall, fall[::-1], np.concatenate([fall[::2], fall[1::2][::-1]])):
+        kk, qq = _low(k, q, [j for j in range(blocks) if order[j] > 0], down) if down else (k, q)
+        x = (v.float() * torch.from_numpy(2.0 ** np.repeat(order, 32)).float()[None, :, None, None]).to(torch.bfloat16)
+        cache = dq.Q8KVCache(B, H, H, T, fmt)
+        cache.append(*(y.to(DEV).expand(B, -1, -1, -1) for y in (kk, x)), 0)
+        out = cache.attend_chunk(qq.to(DEV), _i32([T] * B))
+        some = [0, B - 1]
+        held = [_held(y, fmt).expand(2, -1, -1, -1) for y in (kk, x)]
+        _check_all(out[some], qq[some], *held, [T] * 2, [n] * 2)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("n", [4, 40, 150])
 @pytest.mark.parametrize("to", [2.0 ** -88, 2.0 ** -60, 2.0 ** 50, 2.0 ** 90, 2.0 ** 124])
 def test_all_values_small_or_large(dq, fmt, n, to):
