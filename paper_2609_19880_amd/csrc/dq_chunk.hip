@@ -634,7 +634,7 @@ struct Rows {
             d = whole ? vl - vref : 0.f;
         }
         off = offset();
-        const float f = __builtin_amdgcn_exp2f(by);
+        const float f = __builtin_amdgcn_exp2f(fminf(by, 127.f));        // (zeros may have any: they stay)
         // (whole vectors: element by element the compiler holds the sums twice)
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] *= f;
@@ -653,14 +653,15 @@ struct Rows {
         return rounded;
     }
 
-    // By how many powers of 2 the row's sums may grow.
+    // By how many powers of 2 the row's sums may grow: zeros by any.
     __device__ __forceinline__ float most_up(int lane) const {
-        float top = 0x1p-126f;
+        float top = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(o[i][e]));
-        return 124.f - ceilf(__builtin_amdgcn_logf(fmaxf(top, xor_lane<32>(top, lane))));
+        top = fmaxf(top, xor_lane<32>(top, lane));
+        return top == 0.f ? 1e4f : 124.f - fmaxf(ceilf(__builtin_amdgcn_logf(top)), 0.f);
     }
 
     // The values of half of a block's tokens.

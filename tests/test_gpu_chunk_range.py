@@ -146,6 +146,24 @@ def test_a_large_value_of_a_hidden_token(dq, fmt, n, up):
 
 
 @pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("n", [8, 150])
+@pytest.mark.parametrize("size,up", [(0, 30), (0, 100), (-50, 150), (-80, 200)])
+def test_a_large_value_between_the_first_tokens_and_the_window(dq, fmt, n, size, up):
+    """First tokens whose block's scale comes from one that no query sees, and rounds
+    theirs to zero: the window's values are all there is."""
+    T = 300
+    k, v = _kv(n, 1, T, 1)
+    q = _q(up, 1, n, 2)
+    x = v.float() * 2.0 ** size
+    x[:, 25] = v[:, 25].float() * 2.0 ** (size + up)
+    x = x.to(torch.bfloat16)
+    assert bool(torch.isfinite(x.float()).all())
+    cache = _filled(dq, fmt, k, x, 2)
+    out = cache.attend_chunk(q.to(DEV), _i32([T]), window=64, sinks=20)
+    _check_all(out, q, _held(k, fmt), _held(x, fmt), [T], [n], window=64, sinks=20)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("n", [6, 200])
 def test_a_large_block_between_even_ones(dq, fmt, n):
     """A block without weight that is larger, then blocks of the first ones' size
