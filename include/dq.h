@@ -690,11 +690,11 @@ int dq_rope(int32_t layout, int32_t transposed, const double* freq, float magnit
  * A query that sees no token gives zeros; one with an infinity or NaN that sees
  * some gives NaN.  Scores and sums are held in fp32; the weights are rounded to
  * fp16 for the product with the codes of the values, which are exact, and the
- * output to bf16.  (What counts for that is a weight times its block's scale: of a
- * query's largest, 11 bits down to 2^-14 of it, fewer below, and nothing below
- * 2^-25.)  Value blocks may be of any sizes:
- * one counts fully beside others of up to 2^80 times its scale, whatever their
- * weights, and values up to bf16's largest give no infinity.
+ * output to bf16.  (What is rounded is a weight times its block's scale, relative
+ * to a query's largest such product: 11 bits down to 2^-14 of that, fewer below,
+ * nothing below 2^-25.)  Value blocks may be of any sizes: one that a query does
+ * not see, or that has no weight, takes no bits from others, down to 2^-80 of its
+ * scale, and values up to bf16's largest give no infinity.
  * (Scales are finite and not negative, as the encoder writes them; one of values
  * that is NaN or infinite gives NaN to the queries that see its block.)
  * The same call gives the same bits again; where long sequences are cut follows

@@ -610,7 +610,7 @@ struct Rows {
         top = top == -INFINITY ? top : clamped(top);
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[e] = exact && s[e] != -INFINITY ? clamped(s[e] * c) : s[e];
-        top = fmaxf(top, xor_lane<32>(top, lane));
+        top = ceilf(fmaxf(top, xor_lane<32>(top, lane)));            // (so that all scaling is by powers of 2)
         sum = fmaxf(sum, xor_lane<32>(sum, lane));
         const bool higher = (m == -INFINITY || (exact || low ? top > m + 4.f : sum > kMost)) && top > m;
         const float rise = higher && m != -INFINITY ? top - m : 0.f;
@@ -622,22 +622,23 @@ struct Rows {
             const bool seen = top != -INFINITY;
             l = seen && vl != vl ? NAN : l;
             // (no further down than a weight of 2^-200, which is nothing)
-            const float weighs = vl + fmaxf(fminf(top - m, 0.f), -200.f), base = vref - floorf(rise);
+            const float weighs = vl + fmaxf(fminf(top - m, 0.f), -200.f), base = vref - rise;
             const bool over = weighs > base && (higher || sum > kMost || (exact && weighs > base + 4.f));
             float to = floorf(low ? vl : weighs) + 1.f;      // (room for scales of up to twice the size)
             to = seen && vl > kNoScale && (low || over) ? to : base;
             // (by any step: they add up)
-            if (__builtin_amdgcn_ballot_w64(vref - rise - to > 0.f) != 0) to = fmaxf(to, ceilf(vref - rise) - most_up(lane));
+            if (__builtin_amdgcn_ballot_w64(base > to) != 0) to = fmaxf(to, base - most_up(lane));
             by += vref - to;
             vref = to;
             whole = vl > kNoScale && vl - vref >= -2.f;
             d = whole ? vl - vref : 0.f;
         }
         off = offset();
-        const float f = __builtin_amdgcn_exp2f(fminf(by, 127.f));        // (zeros may have any: they stay)
-        // (whole vectors: element by element the compiler holds the sums twice)
+        const int shift = (int)fmaxf(fminf(by, 400.f), -400.f);      // (zeros may have any: they stay)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] *= f;
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[i][e] = ldexpf(o[i][e], shift);
         careful = __builtin_amdgcn_ballot_w64(!(fabsf(m) < 0x1p11f)) != 0;
         // (large scores: the difference first, which is exact where it counts)
         const float less = exact ? mu() : 0.f, e0 = exact ? kUp + d : !whole ? kUp - mu() : q8 ? off + vl : off;

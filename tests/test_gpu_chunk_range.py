@@ -164,6 +164,26 @@ def test_a_large_value_between_the_first_tokens_and_the_window(dq, fmt, n, size,
 
 
 @pytest.mark.parametrize("fmt", FMTS)
+def test_zeros_beside_a_large_block_of_little_weight(dq, fmt):
+    """A large block, blocks 2^-110 of it, then zeros with nearly all weight whose
+    scale, from a value that is not seen, is as large: the first block's values are the
+    output, after their sums were scaled by 2^110 and back."""
+    T, n = 256, 30
+    k, v = _kv(n, 1, T, 1)
+    q = _q(n, 1, n, 4)
+    kk, qq = _low(k, q, [0], 17)
+    more, _ = _low(k, q, range(1, 7), 24)
+    kk[:, 32:224] = more[:, 32:224]
+    x = v.float() * 2.0 ** -55
+    x[:, :32] *= 2.0 ** 110
+    x[:, 255] *= 2.0 ** 110
+    x = x.to(torch.bfloat16)
+    cache = _filled(dq, fmt, kk, x, 4)
+    out = cache.attend_chunk(qq.to(DEV), _i32([T]))
+    _check_all(out, qq, _held(kk, fmt), _held(x, fmt), [T], [n])
+
+
+@pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("n", [6, 200])
 def test_a_large_block_between_even_ones(dq, fmt, n):
     """A block without weight that is larger, then blocks of the first ones' size
