@@ -550,6 +550,7 @@ struct Rows {
     }
 
     __device__ __forceinline__ float mu() const { return m == -INFINITY ? 0.f : m; }
+    __device__ __forceinline__ int relative_to() const { return q8 ? (int)fmaxf(vref, -400.f) : 0; }
     __device__ __forceinline__ float offset() const { return q8 ? kUp - mu() - vref : kUp - mu(); }
 
     // The softmax of a block whose scores are s, times c: p are its weights.
@@ -758,13 +759,16 @@ __device__ __forceinline__ float share(float m, float l, float top) {
 }
 __device__ __forceinline__ float inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }   // rows that see nothing: zeros
 
-// The outputs of a workgroup's wavefronts, o f up, joined in LDS and written: wavefront
+// A sum, divided by its weights' and times the 2^up that it is relative to.
+__device__ __forceinline__ float output(float sum, float f, int up) { return ldexpf(sum * f, up); }
+
+// The outputs of a workgroup's wavefronts joined in LDS and written: wavefront
 // w has rows 32 (w % parts) .. of the tokens that it has seen.  PAIRED: operand 2 m + e
 // has channels 64 m + 32 (row / 16) + 16 e + row % 16, else 32 (2 m + e) + row.
 constexpr int kJoinRow = 68;                     // floats: 64 channels, and 4 to keep rows in different banks
 
 template <typename K, int WAVES, bool PAIRED>
-__device__ __forceinline__ void join_rows(const ChunkArgs& a, const f32x16 (&o)[4], float m, float l, float up,
+__device__ __forceinline__ void join_rows(const ChunkArgs& a, const f32x16 (&o)[4], float m, float l, int up,
                                           float* join, float (&wm)[WAVES][kRowsOf], float (&wl)[WAVES][kRowsOf],
                                           float (&each)[WAVES][kRowsOf], int parts, int rows, int r0, int b, int h,
                                           bool whole, int64_t slot) {
@@ -784,7 +788,8 @@ __device__ __forceinline__ void join_rows(const ChunkArgs& a, const f32x16 (&o)[
                 const int ch = PAIRED ? 32 * (i >> 1) + 16 * e + 8 * (i & 1) + 4 * half : 32 * e + 8 * i + 4 * half;
                 const f32x16& x = o[2 * m2 + e];
                 *reinterpret_cast<f32x4*>(join + (wave * kRowsOf + col) * kJoinRow + ch) =
-                    f32x4{x[4 * i] * f * up, x[4 * i + 1] * f * up, x[4 * i + 2] * f * up, x[4 * i + 3] * f * up};
+                    f32x4{output(x[4 * i], f, up), output(x[4 * i + 1], f, up), output(x[4 * i + 2], f, up),
+                          output(x[4 * i + 3], f, up)};
             }
         if (m2 == 0 && tid < WAVES * kRowsOf) {  // (the shares, once; by every thread for itself: 1.5 us more)
             const int w = tid / kRowsOf, row = tid % kRowsOf;
@@ -1026,7 +1031,8 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
 
     // ------------------------------------------------ results
     const float l = me.l + xor_lane<32>(me.l, lane);
-    const float up = q8 ? __builtin_amdgcn_exp2f(me.vref) : 1.f, f = inverse(l);
+    const float f = inverse(l);
+    const int up = me.relative_to();
     const int half = lane >> 5;
     const int64_t slot = it.slot;
     if (whole) {
@@ -1037,8 +1043,8 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 store_row(a, b, token, head, 32 * np + 8 * i + 4 * half,
-                          bf16_two(me.o[np][4 * i] * f * up, me.o[np][4 * i + 1] * f * up),
-                          bf16_two(me.o[np][4 * i + 2] * f * up, me.o[np][4 * i + 3] * f * up));
+                          bf16_two(output(me.o[np][4 * i], f, up), output(me.o[np][4 * i + 1], f, up)),
+                          bf16_two(output(me.o[np][4 * i + 2], f, up), output(me.o[np][4 * i + 3], f, up)));
         return;
     }
     float* acc = a.ws_acc + (slot * Many::kRows + wave * kRowsOf + (lane & 31)) * kD + 4 * half;
@@ -1047,8 +1053,8 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             *reinterpret_cast<f32x4*>(acc + 32 * np + 8 * i) =
-                f32x4{me.o[np][4 * i] * f * up, me.o[np][4 * i + 1] * f * up, me.o[np][4 * i + 2] * f * up,
-                      me.o[np][4 * i + 3] * f * up};
+                f32x4{output(me.o[np][4 * i], f, up), output(me.o[np][4 * i + 1], f, up),
+                      output(me.o[np][4 * i + 2], f, up), output(me.o[np][4 * i + 3], f, up)};
     if (half == 0) {
         float* ml = a.ws_ml + slot * 2 * Many::kRows + wave * kRowsOf + (lane & 31);
         ml[0] = me.m;
@@ -1243,9 +1249,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_kernel(ChunkArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(me.o[i]));
 
-    join_rows<Few, kFewWaves, q8>(a, me.o, me.m, me.l + xor_lane<32>(me.l, lane),
-                                  q8 ? __builtin_amdgcn_exp2f(me.vref) : 1.f, reinterpret_cast<float*>(lds), wm, wl,
-                                  each, parts, rows, 0, b, h, whole, it.slot);
+    join_rows<Few, kFewWaves, q8>(a, me.o, me.m, me.l + xor_lane<32>(me.l, lane), me.relative_to(),
+                                  reinterpret_cast<float*>(lds), wm, wl, each, parts, rows, 0, b, h, whole, it.slot);
 }
 
 // The pieces of a segment's rows joined: half a wavefront has a row at a time, four

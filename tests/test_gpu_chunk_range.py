@@ -184,6 +184,22 @@ def test_zeros_beside_a_large_block_of_little_weight(dq, fmt):
 
 
 @pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("T,n", [(250, 6), (250, 150), (4100, 100)])
+def test_small_values_of_little_weight(dq, fmt, T, n):
+    """Outputs near the end of the type's range: values of 2^-85 with weights of 2^-38,
+    beside zeros."""
+    k, v = _kv(T + n, 1, T, 1)
+    q = _q(n, 1, n, 2)
+    kk, qq = _low(k, q, [j for j in range(-(-T // 32)) if j != 1], 38)
+    x = v.float() * 2.0 ** -85
+    x[:, 32:64] = 0
+    x = x.to(torch.bfloat16)
+    cache = _filled(dq, fmt, kk, x, 2)
+    out = cache.attend_chunk(qq.to(DEV), _i32([T]))
+    _check_all(out, qq, _held(kk, fmt), _held(x, fmt), [T], [n])
+
+
+@pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("n", [6, 200])
 def test_a_large_block_between_even_ones(dq, fmt, n):
     """A block without weight that is larger, then blocks of the first ones' size
