@@ -717,8 +717,9 @@ int dq_rope(int32_t layout, int32_t transposed, const double* freq, float magnit
  * a query or a visible state give what the formula gives in fp32, in which the
  * scores are held, but a query whose every score is -infinity gives zeros
  * and sums of values above 2^80 may overflow.
- * Weights are rounded to bf16 for the product with the values.  n_kv is at most
- * 2^30.
+ * Weights are rounded for the product with the values, to two terms of bf16 (16
+ * bits) where n_q (or q_lens[b]) (q_heads / kv_heads) is at most 64, to one (8 bits)
+ * where it is more.  n_kv is at most 2^30.
  *
  * dq_chunk_workspace_bytes: for both; t_cap is the cache's capacity (max_pages *
  * page_tokens) or n_kv.  It holds the outputs of the pieces that the GPU works on

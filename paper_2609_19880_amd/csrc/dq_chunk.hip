@@ -21,11 +21,11 @@
 //
 // Weights take the values' type, which the matrix instructions ask for: fp16 (11
 // bits) over codes, bf16 (8 bits) over BF16 states, whose range fp16 does not hold.
-// The denominator is the sum of the rounded weights, so a common error of theirs
-// cancels.  (The decode step keeps 22 bits of the weights with two products; here
-// that is half as much matrix work again, for an error that the output's rounding to
-// bf16 exceeds over codes and equals over BF16 states: 0.0020 to 0.0025 against
-// 0.0017 in all.)
+// Where memory is what a call waits for (few rows) weights over BF16 states are two
+// terms, 16 bits, and a product each; with many rows that would be half as much matrix
+// work again, for an error beside the output's own rounding to bf16 of 0.0021 in place
+// of 0.0017 in all.  The denominator is the sum of the rounded weights, so a common
+// error of theirs cancels.
 #include <float.h>
 #include <math.h>
 
@@ -42,6 +42,7 @@ constexpr int kD = 128;
 constexpr int kBlk = DQ_Q8_BLOCK;
 constexpr int kBlkBytes = kBlk * kD;
 constexpr float kBig = 3e38f;
+constexpr float kMostBf16 = 0x1.FEp127f;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kRowsOf = 32;                  // rows per wavefront
 constexpr float kNoScale = -1e30f;           // log2 of the scale of a block of zeros
@@ -54,6 +55,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
@@ -448,9 +450,12 @@ __device__ __forceinline__ float plus_weights(uint32_t w, float x) {
 // m itself weighs 1.  Any limit would do for bf16's range; 2^60 in place of 2^15 is
 // no faster, 2^8 loses 4 %, and larger weights bring the sums of large values
 // nearer to their end.)
-template <int SRC>
+//
+// FINE: weights are two terms, p[2 + st] what rounding p[st] has left.
+template <int SRC, bool FINE>
 struct Rows {
     static constexpr bool q8 = SRC != kChunkBf16;
+    static constexpr int kTerms = FINE ? 2 : 1;
     static constexpr float kUp = q8 ? 2.f : 0.f;
     static constexpr float kMost = 0x1p15f;
 
@@ -534,17 +539,26 @@ struct Rows {
     }
 
     // The weights exp2(s c + e) and their sum, of the rounded ones.
-    __device__ __forceinline__ float weigh(const f32x16& s, float c, float e, u32x4 (&p)[2]) const {
+    __device__ __forceinline__ float weigh(const f32x16& s, float c, float e, u32x4 (&p)[2 * kTerms]) const {
         float sum = 0.f;
 #pragma unroll
         for (int st = 0; st < 2; ++st)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int at = 4 * st + 8 * (i >> 1) + 2 * (i & 1);
-                const float x = __builtin_amdgcn_exp2f(fmaf(s[at], c, e));
-                const float y = __builtin_amdgcn_exp2f(fmaf(s[at + 1], c, e));
+                float x = __builtin_amdgcn_exp2f(fmaf(s[at], c, e));
+                float y = __builtin_amdgcn_exp2f(fmaf(s[at + 1], c, e));
+                if constexpr (FINE) {            // (infinity would leave NaN)
+                    x = x > kMostBf16 ? kMostBf16 : x;
+                    y = y > kMostBf16 ? kMostBf16 : y;
+                }
                 p[st][i] = weights2<SRC>(x, y);
                 sum = plus_weights<SRC>(p[st][i], sum);
+                if constexpr (FINE) {
+                    p[2 + st][i] = weights2<SRC>(x - __uint_as_float(p[st][i] << 16),
+                                                 y - __uint_as_float(p[st][i] & 0xFFFF0000u));
+                    sum = plus_weights<SRC>(p[2 + st][i], sum);
+                }
             }
         return sum;
     }
@@ -558,7 +572,7 @@ struct Rows {
     // hidden; vl: log2 of the values' scale, kNoScale for a block of zeros (any
     // weight will do), NaN for one that is no number (rows that see it become NaN).
     __device__ __forceinline__ void block(f32x16& s, float c, float vl, int t0, uint32_t shown, int lane,
-                                          u32x4 (&p)[2]) {
+                                          u32x4 (&p)[2 * kTerms]) {
         c = fmaxf(c, 0x1p-120f);                 // (a factor of 0, which hidden scores could not bear)
         if (shown != ~0u || t0 + kBlk > lim_lo || (start_hi > 0 && t0 < start_hi && t0 + kBlk > sinks)) {
             auto below = [&](int t) { return t <= t0 ? 0u : t - t0 >= kBlk ? ~0u : (1u << (t - t0)) - 1u; };
@@ -598,7 +612,7 @@ struct Rows {
     // that is not enough the block's values are nothing beside the row's sums, and are
     // left out.
     __device__ __forceinline__ float anew(f32x16& s, float c, float sum, float vl, bool low, float& d, int lane,
-                                          u32x4 (&p)[2]) {
+                                          u32x4 (&p)[2 * kTerms]) {
         float top = s[0];                        // (NaN where every score is)
 #pragma unroll
         for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
@@ -736,6 +750,26 @@ __device__ __forceinline__ void read_values(const char* at, int st, int lane, u3
     }
 }
 
+// Infinities (and NaN) of BF16 values made zeros: what the weights' first terms have
+// made of them stays as it is, whatever the second ones' signs are.
+__device__ __forceinline__ void zeros_for_infinities(u32x4 (&vf)[4]) {
+    u16x2 top = {0, 0};
+#pragma unroll
+    for (int np = 0; np < 4; ++np)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, vf[np][i] & 0x7FFF7FFFu));
+    if (__builtin_amdgcn_ballot_w64(top[0] >= 0x7F80 || top[1] >= 0x7F80) == 0) return;
+#pragma unroll
+    for (int np = 0; np < 4; ++np)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t w = vf[np][i];
+            vf[np][i] = ((w & 0x7F80u) == 0x7F80u ? 0u : w & 0xFFFFu) |
+                        ((w & 0x7F800000u) == 0x7F800000u ? 0u : w & 0xFFFF0000u);
+        }
+}
+
 __device__ __forceinline__ void store_row(const ChunkArgs& a, int b, int token, int head, int ch, uint32_t w0,
                                           uint32_t w1) {
     uint16_t* x = a.out + (int64_t)b * a.o_sb + (int64_t)token * a.o_st + (int64_t)head * a.o_sh + ch;
@@ -860,7 +894,7 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_kernel(ChunkArgs a) {
     if (u0 >= see.count && piece > 0) return;    // the merge does not ask for it
     const int u1 = (int)min((int64_t)u0 + chunk, (int64_t)see.count);
 
-    Rows<SRC> me;
+    Rows<SRC, false> me;
     me.load(a, see, b, h, r0 + wave * kRowsOf, rows, lane);
 
     // ------------------------------------------------ loads
@@ -1171,7 +1205,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_kernel(ChunkArgs a) {
     request(kraw, u, false);
     request(vraw, u, true);
     look_up(u + every);
-    Rows<SRC> me;
+    constexpr bool fine = !q8;
+    Rows<SRC, fine> me;
     me.load(a, see, b, h, part * kRowsOf, rows, lane);
     for (; u < u1; u += every) {
         const int t0 = block_of(u) * kBlk;
@@ -1179,7 +1214,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_kernel(ChunkArgs a) {
         if (!q8) shown &= shown_to(see.T - t0);
         const bool on = t0 < me.lim_hi && shown != 0;
         f32x16 s = f32x16{};
-        u32x4 p[2];
+        u32x4 p[fine ? 4 : 2];
         float c = me.qc, vl = kNoScale;
         if constexpr (q8) {
             ks = ks_next;
@@ -1239,6 +1274,10 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_kernel(ChunkArgs a) {
                     u32x4 vf[4];
                     read_values<SRC>(own + L::kKeys, st, lane, vf);
                     me.values(vf, p[st]);
+                    if constexpr (fine) {
+                        zeros_for_infinities(vf);
+                        me.values(vf, p[2 + st]);
+                    }
                 }
             }
         }

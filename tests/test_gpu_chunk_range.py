@@ -356,3 +356,32 @@ def test_the_largest_softmax_scales(dq, scale, T, n):
         out = _filled(dq, fmt, k, v, 2).attend_chunk(q.to(DEV), _i32([T]), softmax_scale=scale)
         _check_all(out, q, _held(k, fmt), _held(v, fmt), [T], [n], scale=scale)
     _check_cross(_cross(dq, q, k, v, scale=scale), q, k, v, [T], [n], scale=scale)
+
+
+# -------------------------------------------- bits of the cross attention's weights
+
+@pytest.mark.parametrize("B,T,n,H,G", [(3, 100, 1, 2, 1), (2, 1500, 1, 2, 1), (1, 700, 8, 2, 8), (1, 5000, 2, 1, 3),
+                                       (2, 40, 33, 1, 1)])
+@pytest.mark.parametrize("spread", [0.05, 0.3])
+def test_few_cross_rows_keep_the_weights(dq, B, T, n, H, G, spread):
+    """Up to 64 rows: an output is the formula's, rounded once, but for what fp32 and
+    weights of two bf16 terms (2^-16) leave of sum a |v|, channel by channel: the
+    errors of the scores as in test_gpu_chunk.py and 2^-18 for the sums (1500
+    weights and products of one sign each, in parts of at most 2^6 blocks)."""
+    k, v = _kv(T, B, T, H)
+    q = (_q(n, B, n, H * G).float() * spread).to(torch.bfloat16)
+    mask = torch.rand((B, T), generator=torch.Generator().manual_seed(T)) < 0.8
+    for m in (None, mask):
+        out = _cross(dq, q, k, v, None, m).double()
+        for b in range(B):
+            for i in range(H * G):
+                kk, vv = (y[b, :, i // G].double().to(DEV) for y in (k, v))
+                x = q[b, :, i].double().to(DEV)
+                s = (x @ kk.T) * 128 ** -0.5
+                if m is not None:
+                    s[:, ~m[b].to(DEV)] = -math.inf
+                a = torch.softmax(s, dim=1)
+                ref, size = a @ vv, a @ vv.abs()
+                X = float((x.abs() @ kk.abs().T).max()) * 128 ** -0.5 * LOG2E
+                tol = 2.0 ** -8 * ref.abs() + (2.0 ** -16 + 2 * math.log(2) * 14 * 2.0 ** -24 * X + 2.0 ** -18) * size
+                assert bool(((out[b, :, i] - ref).abs() <= tol).all()), (b, i)
