@@ -444,7 +444,7 @@ __device__ __forceinline__ float plus_weights(uint32_t w, float x) {
 // below (to 2^-25 beyond; over codes times the 2^-2 or more of the block's scale that
 // they hold).  Most blocks so need no maximum and scale nothing:
 // their weights are computed with the m at hand and only checked (a running maximum
-// adds 16 maxima, an exchange between two lanes and 64 products to the 128 vector
+// adds 16 maxima, an exchange between two lanes and 64 products to the 126 vector
 // instructions that a block takes).  A row's bits
 // do not depend on the rows beside it, but where their scores pass 2^11.  (BF16:
 // m itself weighs 1.  Any limit would do for bf16's range; 2^60 in place of 2^15 is
@@ -862,9 +862,9 @@ __device__ __forceinline__ void join_rows(const ChunkArgs& a, const f32x16 (&o)[
 // and a block's scores.
 //
 // Bound by no single unit: 4 x 8171 queries over themselves (32 heads, int8) run at
-// 930 to 965 TFLOP/s, where the matrix units are busy 42 % of the time, other vector
-// instructions (128 per wavefront and block, 16 of them exponentials) issue about
-// as long, LDS is active 33 %, and the clock falls to 1.9 GHz.  Left out one at a
+// 910 to 965 TFLOP/s, where the matrix units are busy 44 % of the time, other vector
+// instructions (126 per wavefront and block, 16 of them exponentials) issue about
+// as long, LDS is active 34 %, and the clock falls to 1.8 or 1.9 GHz.  Left out one at a
 // time, the softmax's arithmetic gives back 16 %, the second product 9 %, loads 8 %,
 // exponentials 5 %, the weights' sums or the conversions 2 to 3 %.  Twelve wavefronts
 // per workgroup take 2 to 5 % less on the largest cases and more on the others: left
