@@ -438,18 +438,17 @@ __device__ __forceinline__ float plus_weights(uint32_t w, float x) {
 // sums, and the softmax state.  The lanes l and l ^ 32 share row l % 32; each
 // has the scores of 16 of a block's 32 tokens, 8 (i / 4) + 4 (l / 32) + i % 4.
 //
-// The state's maximum m is not the running maximum but one that the sums keep
-// until a block's weights, relative to it, add up to more than 2^15: weights of
-// m itself are 2^2, so fp16 holds what lies 2^13 above and, to its 11 bits, 2^16
+// The state's maximum m, a whole number, is not the running maximum but one that the
+// sums keep until a block's weights, relative to it, add up to more than 2^15: weights
+// of m itself are 2^2, so fp16 holds what lies 2^13 above and, to its 11 bits, 2^16
 // below (to 2^-25 beyond; over codes times the 2^-2 or more of the block's scale that
-// they hold).  Most blocks so need no maximum and scale nothing:
-// their weights are computed with the m at hand and only checked (a running maximum
-// adds 16 maxima, an exchange between two lanes and 64 products to the 126 vector
-// instructions that a block takes).  A row's bits
-// do not depend on the rows beside it, but where their scores pass 2^11.  (BF16:
-// m itself weighs 1.  Any limit would do for bf16's range; 2^60 in place of 2^15 is
-// no faster, 2^8 loses 4 %, and larger weights bring the sums of large values
-// nearer to their end.)
+// they hold).  Most blocks so need no maximum and scale nothing: their weights are
+// computed with the m at hand and only checked (a running maximum adds 16 maxima, an
+// exchange between two lanes and 64 products to the 126 vector instructions that a
+// block takes).  A row's bits do not depend on the rows beside it, but where their
+// scores pass 2^11.  (BF16: m itself weighs 1.  Any limit would do for bf16's range;
+// 2^60 in place of 2^15 is no faster, 2^8 loses 4 %, and larger weights bring the sums
+// of large values nearer to their end.)
 //
 // FINE: weights are two terms, p[2 + st] what rounding p[st] has left.
 template <int SRC, bool FINE>
